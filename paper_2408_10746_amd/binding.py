@@ -36,8 +36,12 @@ EXPORTS = [
     "pac_dequant_linear_to_cache",
     "pac_tier_window_bytes", "pac_tier_fill", "pac_tier_stage", "pac_adapter_loss_grad_staged", "pac_adapter_step_staged",
     "pac_ladder_param_count", "pac_ladder_workspace_bytes", "pac_ladder_tiles", "pac_ladder_loss_grad", "pac_ladder_step",
+    "pac_mx4_code_pitch", "pac_mx4_scale_pitch", "pac_mx4_quantize", "pac_mx4_dequantize", "pac_mx4_linear", "pac_mx4_linear_x4",
+    "pac_mx4_linear_dx",
+    "pac_block_norm_forward", "pac_block_norm_workspace_bytes", "pac_block_norm_backward",
 ]
 PAC_STATIC_WORKSPACE_BYTES = 64 << 20
+PAC_MX4_ACT_NONE, PAC_MX4_ACT_GELU = 0, 1
 
 
 class pac_config(C.Structure):
@@ -64,6 +68,12 @@ class pac_plan_result(C.Structure):
                 ("stage_first_dev", _ip), ("stage_n_dev", _ip), ("samples", _ip), ("slowest_stage", C.c_double),
                 ("L_b", C.c_double), ("L_e", C.c_double), ("L_n", C.c_double),
                 ("latency_by_stage_count", _dp), ("slowest_by_stage_count", _dp)]
+
+
+class pac_block_norm(C.Structure):
+    _fields_ = [("d", C.c_int32), ("dtype", C.c_int32), ("layer", C.c_int32), ("gate_len", C.c_int32), ("eps", C.c_float),
+                ("w_post", C.c_void_p), ("b_post", C.c_void_p), ("gate", C.c_void_p), ("res", C.c_void_p), ("w_pre", C.c_void_p),
+                ("b_pre", C.c_void_p)]
 
 
 class PacError(RuntimeError):
@@ -164,6 +174,26 @@ def lib():
         L.pac_ladder_step.restype = C.c_int
         L.pac_ladder_step.argtypes = [vp, vp, vp, i32, vp, i32, vp, vp, vp, C.POINTER(i64), C.POINTER(pac_adamw), vp, i64,
                                       vp, vp, vp]
+        L.pac_mx4_code_pitch.restype = i64
+        L.pac_mx4_code_pitch.argtypes = [i32]
+        L.pac_mx4_scale_pitch.restype = i64
+        L.pac_mx4_scale_pitch.argtypes = [i32]
+        L.pac_mx4_quantize.restype = C.c_int
+        L.pac_mx4_quantize.argtypes = [vp, i32, i64, i32, i64, vp, vp, vp]
+        L.pac_mx4_dequantize.restype = C.c_int
+        L.pac_mx4_dequantize.argtypes = [vp, vp, i64, i32, vp, i32, i64, vp]
+        L.pac_mx4_linear.restype = C.c_int
+        L.pac_mx4_linear.argtypes = [vp, i32, i32, i64, vp, vp, i32, vp, i32, vp, i32, i64, vp]
+        L.pac_mx4_linear_x4.restype = C.c_int
+        L.pac_mx4_linear_x4.argtypes = [vp, vp, i32, i32, vp, vp, i32, vp, i32, vp, i32, i64, vp]
+        L.pac_mx4_linear_dx.restype = C.c_int
+        L.pac_mx4_linear_dx.argtypes = [vp, i32, i32, i64, vp, vp, i32, vp, i32, i64, vp]
+        L.pac_block_norm_forward.restype = C.c_int
+        L.pac_block_norm_forward.argtypes = [C.POINTER(pac_block_norm), i64, vp, vp, vp, vp, vp]
+        L.pac_block_norm_workspace_bytes.restype = i64
+        L.pac_block_norm_workspace_bytes.argtypes = [C.POINTER(pac_block_norm), i64]
+        L.pac_block_norm_backward.restype = C.c_int
+        L.pac_block_norm_backward.argtypes = [C.POINTER(pac_block_norm), i64] + [vp] * 13 + [i64, vp]
         L.pac_profile_begin.restype = C.c_int
         L.pac_profile_begin.argtypes = [vp]
         L.pac_profile_end.restype = C.c_int
@@ -460,3 +490,52 @@ def pac_ladder_step(ctx, cache_ptr, sample_ids, labels_ptr, heads, params_ptr, m
                                  C.byref(st), C.byref(hp), ws_ptr, ws_bytes, loss_ptr, grads_ptr, stream),
            "pac_ladder_step")
     return st.value
+
+
+def pac_mx4_code_pitch(cols: int) -> int:
+    return int(lib().pac_mx4_code_pitch(cols))
+
+
+def pac_mx4_scale_pitch(cols: int) -> int:
+    return int(lib().pac_mx4_scale_pitch(cols))
+
+
+def pac_mx4_quantize(x_ptr, x_dtype: int, rows: int, cols: int, x_stride: int, codes_ptr, scales_ptr, stream=0) -> None:
+    _check(lib().pac_mx4_quantize(x_ptr, x_dtype, rows, cols, x_stride, codes_ptr, scales_ptr, stream), "pac_mx4_quantize")
+
+
+def pac_mx4_dequantize(codes_ptr, scales_ptr, rows: int, cols: int, out_ptr, out_dtype: int, out_stride: int, stream=0) -> None:
+    _check(lib().pac_mx4_dequantize(codes_ptr, scales_ptr, rows, cols, out_ptr, out_dtype, out_stride, stream), "pac_mx4_dequantize")
+
+
+def pac_mx4_linear(x_ptr, M: int, K: int, x_stride: int, codes_ptr, scales_ptr, N: int, bias_ptr, act: int, y_ptr, y_dtype: int,
+                   y_stride: int, stream=0) -> None:
+    _check(lib().pac_mx4_linear(x_ptr, M, K, x_stride, codes_ptr, scales_ptr, N, bias_ptr, act, y_ptr, y_dtype, y_stride, stream),
+           "pac_mx4_linear")
+
+
+def pac_mx4_linear_x4(x_codes_ptr, x_scales_ptr, M: int, K: int, codes_ptr, scales_ptr, N: int, bias_ptr, act: int, y_ptr,
+                      y_dtype: int, y_stride: int, stream=0) -> None:
+    _check(lib().pac_mx4_linear_x4(x_codes_ptr, x_scales_ptr, M, K, codes_ptr, scales_ptr, N, bias_ptr, act, y_ptr, y_dtype,
+                                   y_stride, stream), "pac_mx4_linear_x4")
+
+
+def pac_mx4_linear_dx(dy_ptr, M: int, N: int, dy_stride: int, codes_ptr, scales_ptr, K: int, dx_ptr, dx_dtype: int, dx_stride: int,
+                      stream=0) -> None:
+    _check(lib().pac_mx4_linear_dx(dy_ptr, M, N, dy_stride, codes_ptr, scales_ptr, K, dx_ptr, dx_dtype, dx_stride, stream),
+           "pac_mx4_linear_dx")
+
+
+def pac_block_norm_forward(b: pac_block_norm, rows: int, x_ptr, o_ptr, y_ptr, n_ptr, stream=0) -> None:
+    _check(lib().pac_block_norm_forward(C.byref(b), rows, x_ptr, o_ptr, y_ptr, n_ptr, stream), "pac_block_norm_forward")
+
+
+def pac_block_norm_workspace_bytes(b: pac_block_norm, rows: int) -> int:
+    return int(lib().pac_block_norm_workspace_bytes(C.byref(b), rows))
+
+
+def pac_block_norm_backward(b: pac_block_norm, rows: int, x_ptr, o_ptr, dy_ptr, dn_ptr, dx_ptr, do_ptr, dw_post_ptr, db_post_ptr,
+                            dgate_ptr, dres_ptr, dw_pre_ptr, db_pre_ptr, ws_ptr, ws_bytes: int, stream=0) -> None:
+    _check(lib().pac_block_norm_backward(C.byref(b), rows, x_ptr, o_ptr, dy_ptr, dn_ptr, dx_ptr, do_ptr, dw_post_ptr, db_post_ptr,
+                                         dgate_ptr, dres_ptr, dw_pre_ptr, db_pre_ptr, ws_ptr, ws_bytes, stream),
+           "pac_block_norm_backward")

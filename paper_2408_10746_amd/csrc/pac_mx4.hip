@@ -1,0 +1,461 @@
+// Microscaled 4-bit floating point: quantisation, its inverse, the linear layer on stored weights and its gradient into the
+// input (declared in include/pac_mx4.h, where the stored form is described).
+#include "../../include/pac_mx4.h"
+#include "pac_mma.h"
+
+namespace pac {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+static inline bool m_aligned(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+// The conversions take a block's scale as the exponent field of a float, which is the scale byte itself (0: 2^-127, 255: NaN).
+__device__ __forceinline__ float mx4_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// ---------------------------------------------------------------------------
+// quantise: four lanes a block, eight neighbouring values each (16-byte loads where the rows allow them: VEC).  The block's
+// absmax goes round its four lanes; the scale's exponent is the absmax's own exponent less two, so no logarithm is taken;
+// the conversion divides by the scale, rounds to nearest even and saturates at 6 in one instruction a pair.
+// ---------------------------------------------------------------------------
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void k_mx4_quant(const T *__restrict__ x, uint32_t units, uint32_t upr, int cols, int64_t ldx,
+                                                   uint32_t *__restrict__ codes, uint8_t *__restrict__ scales)
+{
+    // a unit is 256 columns of a row: 32 lanes
+    const uint32_t u = blockIdx.x * 8u + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31;
+    if (u >= units) return; // whole groups of 32 lanes leave: the exchanges below stay within four
+    const uint32_t row = u / upr, col = (u - row * upr) * 256u + lane * 8u;
+    const T *src = x + (int64_t)row * ldx + col;
+    float v[8];
+    if (VEC && (int)col + 8 <= cols) {
+        if constexpr (sizeof(T) == 2) {
+            const bf16x8 r = *reinterpret_cast<const bf16x8 *>(src);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = (float)r[e];
+        } else {
+            const f32x4 r0 = *reinterpret_cast<const f32x4 *>(src), r1 = *reinterpret_cast<const f32x4 *>(src + 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = r0[e], v[4 + e] = r1[e];
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = (int)col + e < cols ? (float)src[e] : 0.f;
+    }
+    uint32_t top = 0; // bits of the absmax: for non-negative floats, infinities and NaN among them, bits order as values do
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[e]) & 0x7fffffffu);
+    top = max(top, (uint32_t)__shfl_xor((int)top, 1, 64));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 2, 64));
+    const uint32_t ex = top >> 23; // floor(log2) + 127; 0 for what is below 2^-126, whose scale is the least anyhow
+    const bool none = ex == 255;
+    const uint32_t byte = none ? 255u : ex > 2 ? ex - 2 : 0u;
+    uint32_t w = 0;
+    if (!none) {
+        const float s = mx4_scale(byte);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[0], v[1], s, 0);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2], v[3], s, 1);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4], v[5], s, 2);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6], v[7], s, 3);
+    }
+    codes[(int64_t)u * 32 + lane] = w;
+    if ((lane & 3) == 0) scales[(int64_t)u * 8 + (lane >> 2)] = (uint8_t)byte;
+}
+
+__device__ __forceinline__ void mx4_values(uint32_t w, float s, float (&v)[8])
+{
+    bf16x2 p;
+    p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0); v[0] = (float)p[0]; v[1] = (float)p[1];
+    p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1); v[2] = (float)p[0]; v[3] = (float)p[1];
+    p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2); v[4] = (float)p[0]; v[5] = (float)p[1];
+    p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3); v[6] = (float)p[0]; v[7] = (float)p[1];
+}
+
+// eight codes as bf16, which holds every e2m1 value times a power of two exactly
+__device__ __forceinline__ bf16x8 mx4_bf16(uint32_t w, float s)
+{
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3);
+    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void k_mx4_dequant(const uint32_t *__restrict__ codes, const uint8_t *__restrict__ scales,
+                                                     uint32_t units, uint32_t upr, int cols, T *__restrict__ out, int64_t ldo)
+{
+    const uint32_t u = blockIdx.x * 8u + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31;
+    if (u >= units) return;
+    const uint32_t row = u / upr, col = (u - row * upr) * 256u + lane * 8u;
+    if ((int)col >= cols) return;
+    float v[8];
+    mx4_values(codes[(int64_t)u * 32 + lane], mx4_scale(scales[(int64_t)u * 8 + (lane >> 2)]), v);
+    T *dst = out + (int64_t)row * ldo + col;
+    if (VEC && (int)col + 8 <= cols) {
+        if constexpr (sizeof(T) == 2) {
+            bf16x8 r;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) r[e] = (bf16_t)v[e];
+            *reinterpret_cast<bf16x8 *>(dst) = r;
+        } else {
+            *reinterpret_cast<f32x4 *>(dst) = f32x4{v[0], v[1], v[2], v[3]};
+            *reinterpret_cast<f32x4 *>(dst + 4) = f32x4{v[4], v[5], v[6], v[7]};
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if ((int)col + e < cols) dst[e] = (T)v[e];
+    }
+}
+
+// ---------------------------------------------------------------------------
+// products
+// ---------------------------------------------------------------------------
+struct Mx4Args {
+    const void *x;     // bf16 [M][ldx], or codes of the stored form
+    const uint8_t *xs; // scales of the stored form
+    int64_t ldx;
+    const uint8_t *w, *ws; // W, stored form
+    int M, K, N;
+    int64_t wp, sp; // pitches of W's codes and scales
+    const float *bias;
+    int gelu;
+    void *y;
+    int y_f32;
+    int64_t ldy;
+};
+
+// GELU in the erf form; erf by the rational approximation 7.1.26 of Abramowitz and Stegun, |error| < 1.5e-7: below one part in
+// 2^22 of what the next product reads, in a third of erff's instructions.
+__device__ __forceinline__ float mx4_gelu(float u)
+{
+    const float x = fabsf(u) * 0.70710678118654752f;
+    const float t = __builtin_amdgcn_rcpf(1.f + 0.3275911f * x);
+    const float poly = t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+    const float tail = 0.5f * poly * __expf(-0.5f * u * u); // 1 - Phi(|u|)
+    return u * (u < 0.f ? tail : 1.f - tail);
+}
+
+__device__ __forceinline__ void mx4_put(const Mx4Args &a, int m, int n, float v)
+{
+    if (a.bias) v += a.bias[n];
+    if (a.gelu) v = mx4_gelu(v);
+    if (a.y_f32) reinterpret_cast<float *>(a.y)[(int64_t)m * a.ldy + n] = v;
+    else reinterpret_cast<bf16_t *>(a.y)[(int64_t)m * a.ldy + n] = (bf16_t)v;
+}
+
+// eight bf16 of which those from `valid` on do not count
+__device__ __forceinline__ u32x4 mx4_keep(u32x4 v, int valid)
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = valid >= 2 * e + 2 ? v[e] : valid == 2 * e + 1 ? v[e] & 0xffffu : 0u;
+    return v;
+}
+
+// A tile of 16 columns of y by 16 RM rows a workgroup, the contraction dealt over its NW wavefronts in steps of 128 and joined in
+// LDS in a fixed order.  Operands go from memory straight into registers: lane (i, q) holds row i's block of 32 number q of the
+// step, so that a lane has one scale, its 16 bytes of codes are one load, and four matrix instructions of 32 (one of 128 where x
+// is stored too) take eight codes of every lane's block each: the order of the sum does not matter to it.
+template <bool X4, int RM, int NW> __global__ __launch_bounds__(64 * NW) void k_mx4_rows(Mx4Args a)
+{
+    constexpr int TM = 16 * RM, PITCH = 20;
+    __shared__ __attribute__((aligned(16))) float red[NW * TM * PITCH];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
+    const int nt = (a.N + 15) / 16, n0 = (int)(blockIdx.x % nt) * 16, m0 = (int)(blockIdx.x / nt) * TM;
+    const int nrow = min(n0 + i, a.N - 1), steps = (a.K + 255) / 256 * 2;
+    const uint8_t *wr = a.w + nrow * a.wp + 16 * q, *sr = a.ws + nrow * a.sp + q;
+    f32x4 acc[RM];
+    const char *xr[RM];
+    const uint8_t *xsr[RM];
+#pragma unroll
+    for (int r = 0; r < RM; ++r) {
+        acc[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const int64_t m = min(m0 + 16 * r + i, a.M - 1);
+        xr[r] = X4 ? reinterpret_cast<const char *>(a.x) + m * a.wp + 16 * q
+                   : reinterpret_cast<const char *>(a.x) + m * a.ldx * 2;
+        xsr[r] = X4 ? a.xs + m * a.sp + q : nullptr;
+    }
+    const int last = (a.K + 7) / 8 * 8 - 8; // the last chunk of x that is there
+    for (int s = wave; s < steps; s += NW) {
+        const u32x4 w = *reinterpret_cast<const u32x4 *>(wr + 64 * s);
+        const uint32_t sc = sr[4 * s];
+        if constexpr (X4) {
+            const i32x8 wf = {(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0};
+#pragma unroll
+            for (int r = 0; r < RM; ++r) {
+                const u32x4 x = *reinterpret_cast<const u32x4 *>(xr[r] + 64 * s);
+                const i32x8 xf = {(int)x[0], (int)x[1], (int)x[2], (int)x[3], 0, 0, 0, 0};
+                acc[r] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wf, xf, acc[r], 4, 4, 0, (int)sc, 0, (int)xsr[r][4 * s]);
+            }
+        } else {
+            bf16x8 wf[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) wf[j] = mx4_bf16(w[j], mx4_scale(sc));
+            const int k0 = 128 * s + 32 * q;
+#pragma unroll
+            for (int r = 0; r < RM; ++r)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int k = k0 + 8 * j;
+                    u32x4 x = *reinterpret_cast<const u32x4 *>(xr[r] + 2 * min(k, last));
+                    if (128 * s + 128 > a.K) x = mx4_keep(x, a.K - k);
+                    acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[j], *reinterpret_cast<bf16x8 *>(&x), acc[r], 0, 0, 0);
+                }
+        }
+    }
+    // lane (i, q) holds columns 4 q .. 4 q + 3 of row i
+#pragma unroll
+    for (int r = 0; r < RM; ++r) *reinterpret_cast<f32x4 *>(red + (wave * TM + 16 * r + i) * PITCH + 4 * q) = acc[r];
+    __syncthreads();
+    for (int e = threadIdx.x; e < TM * 16; e += 64 * NW) {
+        const int m = e >> 4, n = e & 15;
+        if (m0 + m >= a.M || n0 + n >= a.N) continue;
+        float v = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) v += red[(w * TM + m) * PITCH + n];
+        mx4_put(a, m0 + m, n0 + n, v);
+    }
+}
+
+// dx: a tile of 128 columns of dx by 16 RM rows, the rows of W dealt over NW wavefronts in steps of 32.  The contraction runs
+// across W's rows, eight of which a lane needs for one column: a lane loads 4 bytes (eight columns) of eight rows, converts them
+// with each row's scale and swaps halves of register pairs, which leaves it the eight rows of eight columns.  The matrix
+// instruction number c takes column c of every lane, so lanes i = 0 .. 15 cover 128 neighbouring columns and an output lane holds
+// eight neighbouring ones: no transposed copy of W anywhere.
+__device__ __forceinline__ uint32_t pk_lo(bf16x2 a, bf16x2 b) // {a[0], b[0]}
+{
+    return __builtin_amdgcn_perm(*reinterpret_cast<uint32_t *>(&b), *reinterpret_cast<uint32_t *>(&a), 0x05040100u);
+}
+__device__ __forceinline__ uint32_t pk_hi(bf16x2 a, bf16x2 b) // {a[1], b[1]}
+{
+    return __builtin_amdgcn_perm(*reinterpret_cast<uint32_t *>(&b), *reinterpret_cast<uint32_t *>(&a), 0x07060302u);
+}
+
+// w[e], s[e]: eight columns' codes and the scale of row e; col[c]: the eight rows of column c
+__device__ __forceinline__ void mx4_columns(const uint32_t (&w)[8], const float (&s)[8], u32x4 (&col)[8])
+{
+#pragma unroll
+    for (int p = 0; p < 4; ++p) { // rows 2 p and 2 p + 1
+#define PAC_MX4_PAIR(C)                                                                                                        \
+    {                                                                                                                          \
+        const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[2 * p], s[2 * p], C);                                     \
+        const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[2 * p + 1], s[2 * p + 1], C);                             \
+        col[2 * C][p] = pk_lo(a, b);                                                                                           \
+        col[2 * C + 1][p] = pk_hi(a, b);                                                                                       \
+    }
+        PAC_MX4_PAIR(0) PAC_MX4_PAIR(1) PAC_MX4_PAIR(2) PAC_MX4_PAIR(3)
+#undef PAC_MX4_PAIR
+    }
+}
+
+template <int RM, int NW> __global__ __launch_bounds__(64 * NW) void k_mx4_dx_rows(Mx4Args a)
+{
+    constexpr int TM = 16 * RM, PITCH = 132;
+    __shared__ __attribute__((aligned(16))) float red[NW * TM * PITCH];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
+    const int kt = (a.K + 127) / 128, kc0 = (int)(blockIdx.x % kt) * 128, m0 = (int)(blockIdx.x / kt) * TM;
+    const uint8_t *wc = a.w + kc0 / 2 + 4 * i, *sc = a.ws + kc0 / 32 + (i >> 2);
+    f32x4 acc[8][RM];
+    const bf16_t *dyr[RM];
+#pragma unroll
+    for (int r = 0; r < RM; ++r) {
+        dyr[r] = reinterpret_cast<const bf16_t *>(a.x) + min(m0 + 16 * r + i, a.M - 1) * a.ldx;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) acc[c][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const int steps = (a.N + 31) / 32, last = (a.N + 7) / 8 * 8 - 8;
+    for (int s = wave; s < steps; s += NW) {
+        const int n0 = 32 * s + 8 * q;
+        uint32_t w[8];
+        float f[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int64_t n = min(n0 + e, a.N - 1); // past the end dy counts as zero
+            w[e] = *reinterpret_cast<const uint32_t *>(wc + n * a.wp);
+            f[e] = mx4_scale(sc[n * a.sp]);
+        }
+        u32x4 col[8];
+        mx4_columns(w, f, col);
+#pragma unroll
+        for (int r = 0; r < RM; ++r) {
+            u32x4 d = *reinterpret_cast<const u32x4 *>(dyr[r] + min(n0, last));
+            if (32 * s + 32 > a.N) d = mx4_keep(d, a.N - n0);
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+                acc[c][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<bf16x8 *>(&col[c]), *reinterpret_cast<bf16x8 *>(&d),
+                                                                    acc[c][r], 0, 0, 0);
+        }
+    }
+    // lane (i, q): row i, columns 8 (4 q + v) + c
+#pragma unroll
+    for (int r = 0; r < RM; ++r)
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+#pragma unroll
+            for (int c = 0; c < 8; c += 4)
+                *reinterpret_cast<f32x4 *>(red + (wave * TM + 16 * r + i) * PITCH + 8 * (4 * q + v) + c) =
+                    f32x4{acc[c][r][v], acc[c + 1][r][v], acc[c + 2][r][v], acc[c + 3][r][v]};
+    __syncthreads();
+    for (int e = threadIdx.x; e < TM * 128; e += 64 * NW) {
+        const int m = e >> 7, c = e & 127;
+        if (m0 + m >= a.M || kc0 + c >= a.K) continue;
+        float v = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) v += red[(w * TM + m) * PITCH + c];
+        mx4_put(a, m0 + m, kc0 + c, v);
+    }
+}
+
+static inline int64_t code_pitch(int cols) { return ((int64_t)cols + 255) / 256 * 128; }
+static inline int64_t scale_pitch(int cols) { return ((int64_t)cols + 255) / 256 * 8; }
+static inline bool dtype_ok(int32_t t) { return t == PAC_BF16 || t == PAC_F32; }
+
+constexpr int32_t kMx4Most = 1 << 30; // rows and columns: places past a tile's end still fit 32 bits
+// tiles of a launch, or -1 where they pass a grid's limit
+static int64_t tile_count(int64_t a, int64_t b) { return a * b <= 0x7fffffffll ? a * b : -1; }
+
+static pac_status check_convert(const void *x, int32_t dtype, int64_t rows, int32_t cols, int64_t stride, const uint8_t *codes,
+                                const uint8_t *scales)
+{
+    if (rows != 0 && (!x || !codes || !scales)) return PAC_ERR_NULL; // an empty tensor has no address
+    if (cols < 1 || !dtype_ok(dtype)) return PAC_ERR_SHAPE;
+    if (rows < 0 || stride < cols) return PAC_ERR_RANGE;
+    if (!m_aligned(x, dtype == PAC_F32 ? 4 : 2) || !m_aligned(codes, 16) || !m_aligned(scales, 8)) return PAC_ERR_ALIGN;
+    if (cols > kMx4Most) return PAC_ERR_UNSUPPORTED;
+    const int64_t upr = ((int64_t)cols + 255) / 256;
+    if (rows > 0x7fffffffll / upr) return PAC_ERR_UNSUPPORTED;
+    return PAC_OK;
+}
+
+static pac_status done() { return hipGetLastError() == hipSuccess ? PAC_OK : PAC_ERR_DEVICE; }
+
+static pac_status check_product(const void *x, int32_t M, int32_t K, int32_t N, const uint8_t *codes, const uint8_t *scales, const void *y,
+                                int32_t y_dtype)
+{
+    if (!codes || !scales || (M != 0 && (!x || !y))) return PAC_ERR_NULL; // an empty tensor has no address
+    if (M < 0 || K < 1 || N < 1 || !dtype_ok(y_dtype)) return PAC_ERR_SHAPE;
+    if (M > kMx4Most || K > kMx4Most || N > kMx4Most) return PAC_ERR_UNSUPPORTED;
+    if (!m_aligned(codes, 16) || !m_aligned(scales, 8) || !m_aligned(x, 16) || !m_aligned(y, y_dtype == PAC_F32 ? 4 : 2))
+        return PAC_ERR_ALIGN;
+    return PAC_OK;
+}
+
+template <bool X4> static pac_status launch_linear(const Mx4Args &a, hipStream_t st)
+{
+    (void)hipGetLastError();
+    const int64_t nt = ((int64_t)a.N + 15) / 16;
+    const int rm = a.M <= 16 ? 1 : a.M <= 32 ? 2 : 4;
+    const int64_t tiles = tile_count(nt, ((int64_t)a.M + 16 * rm - 1) / (16 * rm));
+    if (tiles < 0) return PAC_ERR_UNSUPPORTED;
+    const dim3 g((unsigned)tiles);
+    if (rm == 1) hipLaunchKernelGGL((k_mx4_rows<X4, 1, 8>), g, dim3(512), 0, st, a);
+    else if (rm == 2) hipLaunchKernelGGL((k_mx4_rows<X4, 2, 8>), g, dim3(512), 0, st, a);
+    else hipLaunchKernelGGL((k_mx4_rows<X4, 4, 8>), g, dim3(512), 0, st, a);
+    return done();
+}
+
+} // namespace pac
+
+using namespace pac;
+
+extern "C" {
+
+int64_t pac_mx4_code_pitch(int32_t cols) { return cols < 1 ? -1 : code_pitch(cols); }
+int64_t pac_mx4_scale_pitch(int32_t cols) { return cols < 1 ? -1 : scale_pitch(cols); }
+
+pac_status pac_mx4_quantize(const void *x, int32_t x_dtype, int64_t rows, int32_t cols, int64_t x_stride, uint8_t *codes,
+                            uint8_t *scales, void *hip_stream)
+{
+    const pac_status s = check_convert(x, x_dtype, rows, cols, x_stride, codes, scales);
+    if (s != PAC_OK || rows == 0) return s;
+    (void)hipGetLastError();
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    const uint32_t upr = (uint32_t)(((int64_t)cols + 255) / 256), units = (uint32_t)rows * upr;
+    const dim3 g((units + 7) / 8), b(256);
+    uint32_t *c = reinterpret_cast<uint32_t *>(codes);
+    const bool vec = m_aligned(x, 16) && x_stride % (x_dtype == PAC_F32 ? 4 : 8) == 0;
+    if (x_dtype == PAC_F32) {
+        const float *p = static_cast<const float *>(x);
+        if (vec) hipLaunchKernelGGL((k_mx4_quant<float, true>), g, b, 0, st, p, units, upr, cols, x_stride, c, scales);
+        else hipLaunchKernelGGL((k_mx4_quant<float, false>), g, b, 0, st, p, units, upr, cols, x_stride, c, scales);
+    } else {
+        const bf16_t *p = static_cast<const bf16_t *>(x);
+        if (vec) hipLaunchKernelGGL((k_mx4_quant<bf16_t, true>), g, b, 0, st, p, units, upr, cols, x_stride, c, scales);
+        else hipLaunchKernelGGL((k_mx4_quant<bf16_t, false>), g, b, 0, st, p, units, upr, cols, x_stride, c, scales);
+    }
+    return done();
+}
+
+pac_status pac_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows, int32_t cols, void *out, int32_t out_dtype,
+                              int64_t out_stride, void *hip_stream)
+{
+    const pac_status s = check_convert(out, out_dtype, rows, cols, out_stride, codes, scales);
+    if (s != PAC_OK || rows == 0) return s;
+    (void)hipGetLastError();
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    const uint32_t upr = (uint32_t)(((int64_t)cols + 255) / 256), units = (uint32_t)rows * upr;
+    const dim3 g((units + 7) / 8), b(256);
+    const uint32_t *c = reinterpret_cast<const uint32_t *>(codes);
+    const bool vec = m_aligned(out, 16) && out_stride % (out_dtype == PAC_F32 ? 4 : 8) == 0;
+    if (out_dtype == PAC_F32) {
+        float *p = static_cast<float *>(out);
+        if (vec) hipLaunchKernelGGL((k_mx4_dequant<float, true>), g, b, 0, st, c, scales, units, upr, cols, p, out_stride);
+        else hipLaunchKernelGGL((k_mx4_dequant<float, false>), g, b, 0, st, c, scales, units, upr, cols, p, out_stride);
+    } else {
+        bf16_t *p = static_cast<bf16_t *>(out);
+        if (vec) hipLaunchKernelGGL((k_mx4_dequant<bf16_t, true>), g, b, 0, st, c, scales, units, upr, cols, p, out_stride);
+        else hipLaunchKernelGGL((k_mx4_dequant<bf16_t, false>), g, b, 0, st, c, scales, units, upr, cols, p, out_stride);
+    }
+    return done();
+}
+
+pac_status pac_mx4_linear(const void *x, int32_t M, int32_t K, int64_t x_stride, const uint8_t *codes, const uint8_t *scales, int32_t N,
+                          const float *bias, int32_t act, void *y, int32_t y_dtype, int64_t y_stride, void *hip_stream)
+{
+    const pac_status s = check_product(x, M, K, N, codes, scales, y, y_dtype);
+    if (s != PAC_OK) return s;
+    if (act != PAC_MX4_ACT_NONE && act != PAC_MX4_ACT_GELU) return PAC_ERR_SHAPE;
+    if (x_stride < K || y_stride < N) return PAC_ERR_RANGE;
+    if (x_stride % 8 || !m_aligned(bias, 4)) return PAC_ERR_ALIGN;
+    if (M == 0) return PAC_OK;
+    return launch_linear<false>(Mx4Args{x, nullptr, x_stride, codes, scales, M, K, N, code_pitch(K), scale_pitch(K), bias, act, y,
+                                        y_dtype == PAC_F32, y_stride}, static_cast<hipStream_t>(hip_stream));
+}
+
+pac_status pac_mx4_linear_x4(const uint8_t *x_codes, const uint8_t *x_scales, int32_t M, int32_t K, const uint8_t *codes,
+                             const uint8_t *scales, int32_t N, const float *bias, int32_t act, void *y, int32_t y_dtype,
+                             int64_t y_stride, void *hip_stream)
+{
+    if (M != 0 && !x_scales) return PAC_ERR_NULL;
+    const pac_status s = check_product(x_codes, M, K, N, codes, scales, y, y_dtype);
+    if (s != PAC_OK) return s;
+    if (act != PAC_MX4_ACT_NONE && act != PAC_MX4_ACT_GELU) return PAC_ERR_SHAPE;
+    if (y_stride < N) return PAC_ERR_RANGE;
+    if (!m_aligned(x_scales, 8) || !m_aligned(bias, 4)) return PAC_ERR_ALIGN;
+    if (M == 0) return PAC_OK;
+    return launch_linear<true>(Mx4Args{x_codes, x_scales, 0, codes, scales, M, K, N, code_pitch(K), scale_pitch(K), bias, act, y,
+                                       y_dtype == PAC_F32, y_stride}, static_cast<hipStream_t>(hip_stream));
+}
+
+pac_status pac_mx4_linear_dx(const void *dy, int32_t M, int32_t N, int64_t dy_stride, const uint8_t *codes, const uint8_t *scales,
+                             int32_t K, void *dx, int32_t dx_dtype, int64_t dx_stride, void *hip_stream)
+{
+    const pac_status s = check_product(dy, M, K, N, codes, scales, dx, dx_dtype);
+    if (s != PAC_OK) return s;
+    if (dy_stride < N || dx_stride < K) return PAC_ERR_RANGE;
+    if (dy_stride % 8) return PAC_ERR_ALIGN;
+    if (M == 0) return PAC_OK;
+    const Mx4Args a{dy, nullptr, dy_stride, codes, scales, M, K, N, code_pitch(K), scale_pitch(K), nullptr, 0, dx, dx_dtype == PAC_F32,
+                    dx_stride};
+    (void)hipGetLastError();
+    const int rm = M <= 16 ? 1 : 2;
+    const int64_t tiles = tile_count(((int64_t)K + 127) / 128, ((int64_t)M + 16 * rm - 1) / (16 * rm));
+    if (tiles < 0) return PAC_ERR_UNSUPPORTED;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    if (rm == 1) hipLaunchKernelGGL((k_mx4_dx_rows<1, 4>), dim3((unsigned)tiles), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_mx4_dx_rows<2, 4>), dim3((unsigned)tiles), dim3(256), 0, st, a);
+    return done();
+}
+
+} // extern "C"

@@ -199,3 +199,179 @@ class TieredSession(Session):
         n = self.w.L * ln * self.w.d
         raw = self.host_cache[off * es:(off + n) * es].numpy()
         return raw.view(np.uint16 if es == 2 else np.float32).reshape(self.w.L, ln, self.w.d).copy()
+
+
+# ---- blocks of the frozen backbone (include/pac_mx4.h, include/pac_norm.h) ------------------------------------------
+def _kind(t) -> int:
+    if t.dtype == torch.bfloat16:
+        return pb.PAC_BF16
+    if t.dtype == torch.float32:
+        return pb.PAC_F32
+    raise ValueError(f"bfloat16 or float32 is wanted, not {t.dtype}")
+
+
+def _matrix(t, name: str, shape=None, dtype=None, device=None):
+    """The row stride of a device matrix whose columns are neighbours (the launch takes addresses alone, so what they stand
+    for is checked here)."""
+    if t.dim() != 2 or t.device.type != "cuda" or (device is not None and t.device != device):
+        raise ValueError(f"{name}: a matrix on the device is wanted")
+    if shape is not None and tuple(t.shape) != shape:
+        raise ValueError(f"{name}: shape {shape} is wanted, not {tuple(t.shape)}")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name}: {dtype} is wanted, not {t.dtype}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: neighbouring columns are wanted")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _stored(codes, scales, cols: int, rows=None, device=None):
+    rows = codes.shape[0] if rows is None else rows
+    for t, pitch, name in ((codes, pb.pac_mx4_code_pitch(cols), "codes"), (scales, pb.pac_mx4_scale_pitch(cols), "scales")):
+        _matrix(t, name, (rows, pitch), torch.uint8, device)
+        if not t.is_contiguous():
+            raise ValueError(f"{name}: a dense matrix is wanted")
+
+
+def _padded_stride(t, name: str, cols: int, device):
+    """The row stride of a bf16 matrix that is read in 16-byte pieces, in the last row too."""
+    stride = _matrix(t, name, (t.shape[0], cols), torch.bfloat16, device)
+    pad = (cols + 7) // 8 * 8
+    if t.shape[0] == 1:
+        stride = max(stride, pad) // 8 * 8
+    if t.shape[0] and cols % 8:
+        after = t.storage_offset() + (t.shape[0] - 1) * stride + pad
+        if after * 2 > t.untyped_storage().nbytes():
+            raise ValueError(f"{name}: rows are read up to a multiple of 8 columns, the last one too")
+    return stride
+
+
+def _on(device) -> int:
+    return int(torch.cuda.current_stream(device).cuda_stream)
+
+
+def mx4_empty(rows: int, cols: int, device="cuda:0"):
+    """Buffers for a matrix in the stored form: (codes, scales)."""
+    return (torch.empty(rows, pb.pac_mx4_code_pitch(cols), dtype=torch.uint8, device=device),
+            torch.empty(rows, pb.pac_mx4_scale_pitch(cols), dtype=torch.uint8, device=device))
+
+
+def mx4_quantize(x, codes, scales) -> None:
+    """x (bf16 or fp32, any row stride) into the stored form."""
+    stride = _matrix(x, "x")
+    _stored(codes, scales, x.shape[1], x.shape[0], x.device)
+    with torch.cuda.device(x.device):
+        pb.pac_mx4_quantize(x.data_ptr(), _kind(x), x.shape[0], x.shape[1], stride, codes.data_ptr(), scales.data_ptr(), _on(x.device))
+
+
+def mx4_dequantize(codes, scales, out) -> None:
+    """The values a stored matrix stands for, into out (bf16 or fp32, both exact)."""
+    stride = _matrix(out, "out")
+    _stored(codes, scales, out.shape[1], out.shape[0], out.device)
+    with torch.cuda.device(out.device):
+        pb.pac_mx4_dequantize(codes.data_ptr(), scales.data_ptr(), out.shape[0], out.shape[1], out.data_ptr(), _kind(out), stride,
+                              _on(out.device))
+
+
+class Mx4Linear:
+    """A frozen linear layer with weights in the stored form: y = act(x W^T + bias), and dx = dy W on the way back."""
+
+    def __init__(self, codes, scales, K: int, bias=None):
+        _stored(codes, scales, K)
+        self.codes, self.scales, self.bias = codes, scales, bias
+        self.N, self.K, self.dev = codes.shape[0], K, codes.device
+        if bias is not None and (bias.shape != (self.N,) or bias.dtype != torch.float32 or bias.device != self.dev or not bias.is_contiguous()):
+            raise ValueError("bias: float32, one value an output, on the weights' device")
+        self._w = (codes.data_ptr(), scales.data_ptr())
+        self._b = None if bias is None else bias.data_ptr()
+
+    @classmethod
+    def from_weights(cls, w, bias=None):
+        """w [N][K], bf16 or fp32, is quantised; the layer keeps the stored form only."""
+        codes, scales = mx4_empty(w.shape[0], w.shape[1], w.device)
+        mx4_quantize(w, codes, scales)
+        return cls(codes, scales, w.shape[1], bias)
+
+    def forward(self, x, y, gelu: bool = False, x4: bool = False) -> None:
+        """x [M][K] bf16, rows on 16 bytes; y [M][N] bf16 or fp32.  x4: x is quantised too, and the product runs on 4-bit operands."""
+        M = x.shape[0]
+        sy = _matrix(y, "y", (M, self.N), None, self.dev)
+        act = pb.PAC_MX4_ACT_GELU if gelu else pb.PAC_MX4_ACT_NONE
+        with torch.cuda.device(self.dev):
+            st = _on(self.dev)
+            if x4:
+                sx = _matrix(x, "x", (M, self.K), None, self.dev)
+                # x in the stored form lives for this call, on this stream: codes (whole multiples of 128 bytes), then scales
+                c = M * pb.pac_mx4_code_pitch(self.K)
+                buf = torch.empty(c + M * pb.pac_mx4_scale_pitch(self.K), dtype=torch.uint8, device=self.dev)
+                c, s = buf.data_ptr(), buf.data_ptr() + c
+                pb.pac_mx4_quantize(x.data_ptr(), _kind(x), M, self.K, sx, c, s, st)
+                pb.pac_mx4_linear_x4(c, s, M, self.K, *self._w, self.N, self._b, act, y.data_ptr(), _kind(y), sy, st)
+            else:
+                sx = _padded_stride(x, "x", self.K, self.dev)
+                pb.pac_mx4_linear(x.data_ptr(), M, self.K, sx, *self._w, self.N, self._b, act, y.data_ptr(), _kind(y), sy, st)
+
+    def input_grad(self, dy, dx) -> None:
+        """dy [M][N] bf16, rows on 16 bytes; dx [M][K] bf16 or fp32."""
+        M = dy.shape[0]
+        sdy = _padded_stride(dy, "dy", self.N, self.dev)
+        sdx = _matrix(dx, "dx", (M, self.K), None, self.dev)
+        with torch.cuda.device(self.dev):
+            pb.pac_mx4_linear_dx(dy.data_ptr(), M, self.N, sdy, *self._w, self.K, dx.data_ptr(), _kind(dx), sdx, _on(self.dev))
+
+
+class BlockNorm:
+    """The norms after and before a block with its gate and the residual scale (include/pac_norm.h).  Parameters are float32
+    tensors that the caller owns and may change in place."""
+
+    def __init__(self, d: int, layer: bool = False, eps: float = 1e-5, w_post=None, b_post=None, gate=None, res=None, w_pre=None,
+                 b_pre=None):
+        self.d, self.params = d, dict(w_post=w_post, b_post=b_post, gate=gate, res=res, w_pre=w_pre, b_pre=b_pre)
+        self.dev = None
+        for name, p in self.params.items():
+            if p is None:
+                continue
+            lens = {"gate": (1, d), "res": (1,)}.get(name, (d,))
+            if p.dtype != torch.float32 or p.dim() != 1 or p.shape[0] not in lens or not p.is_contiguous() or p.device.type != "cuda":
+                raise ValueError(f"{name}: float32 on the device, {' or '.join(map(str, lens))} values")
+            if self.dev not in (None, p.device):
+                raise ValueError(f"{name}: on another device than the parameters before it")
+            self.dev = p.device
+        ptr = lambda p: None if p is None else p.data_ptr()  # noqa: E731
+        self._b = {kind: pb.pac_block_norm(d, kind, int(layer), 0 if gate is None else gate.shape[0], eps,
+                                           *(ptr(self.params[k]) for k in ("w_post", "b_post", "gate", "res", "w_pre", "b_pre")))
+                   for kind in (pb.PAC_BF16, pb.PAC_F32)}
+
+    def _rows(self, x, *others):
+        if self.dev is not None and x.device != self.dev:
+            raise ValueError("states: on the parameters' device")
+        for t in (x,) + others:
+            if t is None:
+                continue
+            if t.dim() != 2 or t.shape != x.shape or t.shape[1] != self.d or t.dtype != x.dtype or t.device != x.device or not t.is_contiguous():
+                raise ValueError(f"states: dense, [rows][{self.d}], of one type, on one device")
+        if x.device.type != "cuda":
+            raise ValueError("states: on the device")
+        return x.shape[0]
+
+    def forward(self, x, o=None, y=None, n=None) -> None:
+        rows = self._rows(x, o, y, n)
+        ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+        with torch.cuda.device(x.device):
+            pb.pac_block_norm_forward(self._b[_kind(x)], rows, x.data_ptr(), ptr(o), ptr(y), ptr(n), _on(x.device))
+
+    def backward(self, x, o, dy, dn, dx=None, do=None, dparams=None) -> None:
+        """Gradients; dparams: {name: float32 tensor like the parameter} for those that are wanted."""
+        rows = self._rows(x, o, dy, dn, dx, do)
+        dparams = dparams or {}
+        for name, g in dparams.items():
+            p = self.params.get(name)
+            if p is None or g.shape != p.shape or g.dtype != torch.float32 or g.device != p.device or not g.is_contiguous():
+                raise ValueError(f"d{name}: like the parameter of that name")
+        b = self._b[_kind(x)]
+        need = pb.pac_block_norm_workspace_bytes(b, rows) if dparams else 0
+        ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
+        ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+        with torch.cuda.device(x.device):
+            pb.pac_block_norm_backward(b, rows, x.data_ptr(), ptr(o), ptr(dy), ptr(dn), ptr(dx), ptr(do),
+                                       *(ptr(dparams.get(k)) for k in ("w_post", "b_post", "gate", "res", "w_pre", "b_pre")),
+                                       ptr(ws), need, _on(x.device))

@@ -1,0 +1,269 @@
+"""GPU parity of microscaled 4-bit floating point (quantisation, its inverse, the products) against oracle/block_oracle.py.
+
+Bars, derived from the arithmetic: codes, scale bytes and dequantised values equal; a product's elements within
+2 K 2^-24 of the sum of the absolute products (each product is exact in fp32, and each of at most K additions loses at most one
+unit in the last place of a partial sum that this sum bounds), the bias' and GELU's own part, and half a step of the output's type
+(2^-8 bf16, 2^-24 fp32)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import block_oracle as bo
+from paper_2408_10746_amd import binding as pb
+from paper_2408_10746_amd import runtime as rt
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def dev(a, dtype=None):
+    t = torch.from_numpy(np.ascontiguousarray(a))
+    return t.cuda() if dtype is None else t.to(dtype).cuda()
+
+
+def host(t):
+    return t.detach().cpu().double().numpy()
+
+
+# ---- conversions -----------------------------------------------------------------------------------------------------------
+def test_every_code_with_every_scale():
+    scales = np.tile(np.arange(256, dtype=np.uint8).reshape(-1, 1), (1, 8))
+    codes = np.tile(np.array([(2 * b) | ((2 * b + 1) << 4) for b in range(8)], np.uint8), (256, 16))
+    ref = bo.values(codes, scales, 256)
+    for name, dt in DT.items():
+        out = torch.zeros(256, 256, dtype=dt, device="cuda")
+        rt.mx4_dequantize(dev(codes), dev(scales), out)
+        with np.errstate(over="ignore"):
+            want = torch.from_numpy(ref).to(dt)         # 6 x 2^127 and its like pass the type's largest value
+        got = out.cpu()
+        assert torch.equal(torch.isnan(got), torch.isnan(want)), name
+        keep = ~torch.isnan(want)
+        bad = (got[keep] != want[keep]).nonzero()
+        assert bad.numel() == 0, (name, got[keep][bad[:4, 0]], want[keep][bad[:4, 0]])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols,stride", [(1, 1, 1), (3, 31, 31), (2, 32, 32), (5, 33, 40), (7, 255, 255), (4, 256, 256),
+                                              (3, 257, 264), (70, 776, 776), (33, 1003, 1003), (9, 2048, 2056)])
+def test_quantize_and_back(rows, cols, stride, dtype):
+    rng = np.random.default_rng(rows * 1000 + cols)
+    x = rng.standard_normal((rows, stride)) * np.exp(rng.uniform(-20, 20, size=(rows, 1))) * np.exp(rng.uniform(-3, 3, size=(rows, stride)))
+    x[:, :cols:5] = bo.GRID[rng.integers(0, 8, size=x[:, :cols:5].shape)]
+    x[0, : min(cols, 32)] = 0.0
+    xd = dev(x.astype(np.float32), DT[dtype])[:, :cols]
+    ref_codes, ref_scales = bo.quantize(host(xd))
+    codes, scales = rt.mx4_empty(rows, cols)
+    codes.fill_(0xAA), scales.fill_(0xAA)               # the padding has to be written too
+    rt.mx4_quantize(xd, codes, scales)
+    assert np.array_equal(scales.cpu().numpy(), ref_scales)
+    assert np.array_equal(codes.cpu().numpy(), ref_codes)
+    out = torch.full((rows, stride), 7.0, dtype=DT[dtype], device="cuda")
+    rt.mx4_dequantize(codes, scales, out[:, :cols])
+    assert np.array_equal(host(out[:, :cols]), bo.values(ref_codes, ref_scales, cols))
+    assert (out[:, cols:] == 7.0).all()                  # what lies past the columns is left alone
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_quantize_at_the_borders(dtype):
+    """Ties, values next to them, saturation, infinities, NaN, denormals and the largest values, over the whole range of scales."""
+    tie = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 7.0, 7.9375])
+    around = np.concatenate([tie, tie * (1 + 2.0 ** -7), tie * (1 - 2.0 ** -7)])
+    row = np.zeros(32)
+    row[:27], row[27], row[28] = around, 4.0, -0.0
+    exps = np.arange(-149, 125)
+    x = np.ldexp(row[None, :], exps[:, None]) * np.where(np.arange(32) % 3 == 0, -1.0, 1.0)
+    x = np.concatenate([x, np.full((1, 32), np.finfo(np.float32).max), np.full((1, 32), -np.inf), np.where(np.arange(32) == 9, np.nan, 1.0)[None, :],
+                        np.where(np.arange(32) == 31, np.inf, 0.0)[None, :], np.full((1, 32), 2.0 ** -149), np.full((1, 32), 2.0 ** -133)])
+    xd = dev(x.astype(np.float32), DT[dtype])
+    ref_codes, ref_scales = bo.quantize(host(xd))
+    codes, scales = rt.mx4_empty(*x.shape)
+    rt.mx4_quantize(xd, codes, scales)
+    assert np.array_equal(scales.cpu().numpy(), ref_scales)
+    # where zeros have a sign the value is what counts
+    got, want = bo.values(codes.cpu().numpy(), scales.cpu().numpy(), 32), bo.values(ref_codes, ref_scales, 32)
+    bad = np.argwhere(~((got == want) | (np.isnan(got) & np.isnan(want))))
+    assert bad.size == 0, [(tuple(b), host(xd)[tuple(b)], got[tuple(b)], want[tuple(b)]) for b in bad[:8]]
+
+
+# ---- products --------------------------------------------------------------------------------------------------------------
+def layer(rng, N, K):
+    w = rng.standard_normal((N, K)) / np.sqrt(K) * np.exp(rng.standard_normal((N, 1)))
+    w.ravel()[rng.integers(0, N * K, size=max(1, N * K // 500))] *= 20.0
+    codes, scales = bo.quantize(w) if N * K < 20000 else (None, None)
+    if codes is None:
+        cd, sd = rt.mx4_empty(N, K)
+        rt.mx4_quantize(dev(w.astype(np.float32)), cd, sd)
+        codes, scales = cd.cpu().numpy(), sd.cpu().numpy()
+    return dev(codes), dev(scales), bo.values(codes, scales, K)
+
+
+def rows_of(rng, M, K, junk=float("nan")):
+    """bf16 rows that start on 16 bytes; what lies past them must not count."""
+    stride = (K + 7) // 8 * 8 + 8
+    t = torch.full((M, stride), junk, dtype=torch.bfloat16, device="cuda")
+    t[:, :K] = dev(rng.standard_normal((M, K)) * np.exp(rng.uniform(-1, 1, size=(M, 1))), torch.bfloat16)
+    return t[:, :K]
+
+
+def bar(ref, absum, K, dtype, bias=None, gelu=False):
+    err = 2 * K * 2.0 ** -24 * absum
+    if bias is not None:
+        err = err + 2.0 ** -23 * (absum + np.abs(bias))
+    if gelu:
+        # |GELU'| < 1.13; erf within 1.5e-7 and a few units of the last place of u itself
+        err = 1.13 * err + 4e-7 * (absum + (0 if bias is None else np.abs(bias)))
+    return err + (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) * (np.abs(ref) + err) + 1e-38
+
+
+def check(got, ref, err):
+    assert got.shape == ref.shape and np.isfinite(got).all()
+    worst = np.max(np.abs(got - ref) / err)
+    assert worst <= 1.0, worst
+
+
+SHAPES = [(1, 1, 1), (1, 64, 16), (1, 4096, 128), (2, 33, 17), (16, 100, 31), (17, 256, 48), (31, 777, 130), (33, 512, 257), (64, 1000, 64),
+          (65, 775, 100), (130, 1024, 300), (257, 320, 515), (300, 2048, 129), (520, 96, 1030)]
+
+
+@pytest.mark.parametrize("x4", [False, True], ids=["x16", "x4"])
+@pytest.mark.parametrize("M,K,N", SHAPES)
+def test_linear(M, K, N, x4):
+    rng = np.random.default_rng(M * 7 + K * 3 + N + x4)
+    codes, scales, w = layer(rng, N, K)
+    x = rows_of(rng, M, K)
+    xv = host(x)
+    if x4:
+        xv = bo.values(*bo.quantize(xv), K)
+    bias = rng.standard_normal(N)
+    for dtype, use_bias, gelu in (("f32", False, False), ("bf16", True, True), ("f32", True, True), ("bf16", False, False)):
+        b32 = bias.astype(np.float32).astype(np.float64) if use_bias else None
+        ref, absum = bo.linear(xv, w, b32, int(gelu))
+        store = torch.full((M, N + 3), 5.0, dtype=DT[dtype], device="cuda")
+        y = store[:, :N]
+        lin = rt.Mx4Linear(codes, scales, K, bias=dev(bias, torch.float32) if use_bias else None)
+        lin.forward(x, y, gelu=gelu, x4=x4)
+        check(host(y), ref, bar(ref, absum, K, dtype, b32, gelu))
+        assert (store[:, N:] == 5.0).all()
+
+
+@pytest.mark.parametrize("M,K,N", SHAPES + [(1, 300, 4096), (40, 1030, 900)])
+def test_input_grad(M, K, N):
+    rng = np.random.default_rng(M * 5 + K + N * 11)
+    codes, scales, w = layer(rng, N, K)
+    dy = rows_of(rng, M, N)
+    ref, absum = bo.linear(host(dy), w.T)
+    for dtype in ("f32", "bf16"):
+        store = torch.full((M, K + 5), 5.0, dtype=DT[dtype], device="cuda")
+        lin = rt.Mx4Linear(codes, scales, K)
+        lin.input_grad(dy, store[:, :K])
+        check(host(store[:, :K]), ref, bar(ref, absum, N, dtype))
+        assert (store[:, K:] == 5.0).all()
+
+
+def test_input_grad_is_the_forward_products_gradient():
+    """<dy, x W^T> = <dx, x> for the library's own two products, with W only ever in the stored form."""
+    rng = np.random.default_rng(5)
+    M, K, N = 37, 300, 190
+    codes, scales, w = layer(rng, N, K)
+    lin = rt.Mx4Linear(codes, scales, K)
+    x, dy = rows_of(rng, M, K), rows_of(rng, M, N)
+    y, dx = torch.empty(M, N, device="cuda"), torch.empty(M, K, device="cuda")
+    lin.forward(x, y)
+    lin.input_grad(dy, dx)
+    a, b = (host(y) * host(dy)).sum(), (host(dx) * host(x)).sum()
+    scale = (np.abs(host(dy)) @ np.abs(w) * np.abs(host(x))).sum()
+    assert abs(a - b) <= 2 * (K + N) * 2.0 ** -24 * scale
+
+
+def test_blocks_without_a_value_stay_where_they_are():
+    """A block of W that stands for NaN makes its own outputs NaN and no others; an infinity in x the row's."""
+    rng = np.random.default_rng(6)
+    M, K, N = 40, 300, 70
+    codes, scales, w = layer(rng, N, K)
+    scales[9, 2] = 255
+    x, dy = rows_of(rng, M, K), rows_of(rng, M, N)
+    y, dx = torch.empty(M, N, device="cuda"), torch.empty(M, K, device="cuda")
+    lin = rt.Mx4Linear(codes, scales, K)
+    for x4 in (False, True):
+        lin.forward(x, y, x4=x4)
+        nan = torch.isnan(y)
+        assert nan[:, 9].all() and int(nan.sum()) == M
+    lin.input_grad(dy, dx)
+    nan = torch.isnan(dx)
+    assert nan[:, 64:96].all() and int(nan.sum()) == M * 32
+    scales[9, 2] = 127
+    x[3, 7] = float("inf")
+    lin.forward(x, y)
+    assert not torch.isfinite(y[3]).any() or (host(torch.isfinite(y[3])) <= (w[:, 7] == 0)).all()
+    assert torch.isfinite(y[:3]).all() and torch.isfinite(y[4:]).all()
+    lin.forward(x, y, x4=True)
+    assert torch.isnan(y[3]).all() and torch.isfinite(y[:3]).all() and torch.isfinite(y[4:]).all()
+
+
+def test_no_rows_is_no_work():
+    codes, scales = rt.mx4_empty(5, 40)
+    rt.mx4_quantize(torch.ones(5, 40, device="cuda"), codes, scales)
+    lin = rt.Mx4Linear(codes, scales, 40)
+    x, y = torch.empty(0, 40, dtype=torch.bfloat16, device="cuda"), torch.empty(0, 5, device="cuda")
+    lin.forward(x, y)
+    lin.forward(x, y, x4=True)
+    lin.input_grad(torch.empty(0, 8, dtype=torch.bfloat16, device="cuda")[:, :5], torch.empty(0, 40, device="cuda"))
+    rt.mx4_quantize(torch.empty(0, 40, device="cuda"), *rt.mx4_empty(0, 40))
+
+
+def test_the_same_call_gives_the_same_bits_on_another_stream_and_in_a_graph():
+    rng = np.random.default_rng(8)
+    M, K, N = 200, 1024, 500
+    codes, scales, _ = layer(rng, N, K)
+    lin = rt.Mx4Linear(codes, scales, K)
+    x, dy = rows_of(rng, M, K, 0.0), rows_of(rng, M, N, 0.0)
+    outs = lambda: (torch.empty(M, N, device="cuda"), torch.empty(M, N, device="cuda"), torch.empty(M, K, device="cuda"))  # noqa: E731
+
+    def go(o):
+        lin.forward(x, o[0])
+        lin.forward(x, o[1], x4=True)
+        lin.input_grad(dy, o[2])
+
+    ref, other, graph = outs(), outs(), outs()
+    go(ref)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        go(other)
+        go(graph)
+    s.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(ref, other))
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        go(graph)
+    for k in range(3):
+        x.mul_(-1.0)
+        for t in graph:
+            t.zero_()
+        go(ref)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(ref, graph)), k
+
+
+def test_layer_from_weights_and_what_python_refuses():
+    w = torch.randn(24, 40, device="cuda")
+    lin = rt.Mx4Linear.from_weights(w)
+    x, y = torch.randn(3, 40, device="cuda").bfloat16(), torch.empty(3, 24, device="cuda")
+    lin.forward(x, y)
+    back = torch.empty(24, 40, device="cuda")
+    rt.mx4_dequantize(lin.codes, lin.scales, back)
+    ref, absum = bo.linear(host(x), host(back))
+    check(host(y), ref, bar(ref, absum, 40, "f32"))
+    for bad in (lambda: lin.forward(x.float(), y), lambda: lin.forward(x[:, :39], y), lambda: lin.forward(x, y[:, :23]),
+                lambda: lin.forward(x, y.t().contiguous().t()), lambda: lin.forward(x.cpu(), y), lambda: lin.forward(x, y.half()),
+                lambda: lin.input_grad(y, x), lambda: rt.Mx4Linear(lin.codes, lin.scales, 400),
+                lambda: rt.Mx4Linear(lin.codes, lin.scales, 40, bias=torch.zeros(23, device="cuda")),
+                # the last row's 16-byte piece would end past the allocation's last element
+                lambda: rt.Mx4Linear(*rt.mx4_empty(24, 37), 37).forward(torch.empty(64, 40, dtype=torch.bfloat16, device="cuda").view(-1)[-40 * 2 + 3:][:77].as_strided((2, 37), (40, 1)), y[:2])):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(pb.PacError) as e:                # rows that do not start on 16 bytes
+        rt.Mx4Linear(*rt.mx4_empty(24, 37), 37).forward(torch.zeros(4, 37, dtype=torch.bfloat16, device="cuda")[:3], y)
+    assert e.value.status == pb.PAC_ERR_ALIGN
