@@ -2,6 +2,7 @@
 // input (declared in include/pac_mx4.h, where the stored form is described).
 #include "../../include/pac_mx4.h"
 #include "pac_mma.h"
+#include <mutex>
 
 namespace pac {
 
@@ -143,6 +144,36 @@ __device__ __forceinline__ void mx4_put(const Mx4Args &a, int m, int n, float v)
     if (a.gelu) v = mx4_gelu(v);
     if (a.y_f32) reinterpret_cast<float *>(a.y)[(int64_t)m * a.ldy + n] = v;
     else reinterpret_cast<bf16_t *>(a.y)[(int64_t)m * a.ldy + n] = (bf16_t)v;
+}
+
+// W neighbouring outputs, in one store where all of them are there and lie on a store's boundary
+template <int W> __device__ __forceinline__ void mx4_store(const Mx4Args &a, int64_t at, int n, const float (&o)[W], bool wide)
+{
+    typedef float fv __attribute__((ext_vector_type(W)));
+    typedef bf16_t hv __attribute__((ext_vector_type(W)));
+    if (a.y_f32) {
+        float *p = reinterpret_cast<float *>(a.y) + at;
+        if (wide) {
+            fv r;
+#pragma unroll
+            for (int e = 0; e < W; ++e) r[e] = o[e];
+            *reinterpret_cast<fv *>(p) = r;
+        } else
+#pragma unroll
+            for (int e = 0; e < W; ++e)
+                if (n + e < a.N) p[e] = o[e];
+    } else {
+        bf16_t *p = reinterpret_cast<bf16_t *>(a.y) + at;
+        if (wide) {
+            hv r;
+#pragma unroll
+            for (int e = 0; e < W; ++e) r[e] = (bf16_t)o[e];
+            *reinterpret_cast<hv *>(p) = r;
+        } else
+#pragma unroll
+            for (int e = 0; e < W; ++e)
+                if (n + e < a.N) p[e] = (bf16_t)o[e];
+    }
 }
 
 // eight bf16 of which those from `valid` on do not count
@@ -307,6 +338,212 @@ template <int RM, int NW> __global__ __launch_bounds__(64 * NW) void k_mx4_dx_ro
     }
 }
 
+
+// ---------------------------------------------------------------------------
+// products of many rows: a workgroup's tile of 32 WM WTM rows by 32 WN WTN columns, wavefronts of WTM x WTN accumulators of 32 x 32.
+// Both operands stream into a ring of LDS stages as they are stored (pac_mma.h: 16-byte transfers, swizzled chunks, counted waits):
+// the 4-bit codes take a quarter of the space and of the LDS reads that bf16 would, and become bf16 in registers, eight a
+// conversion group, between the matrix instructions of the piece before.  With x stored too both sides go to the scaled matrix
+// instructions as they lie.  A lane (i, g) owns row i and, of each step, the blocks of its half g: one 16-byte read is a block of
+// codes, and a lane has one scale a block.  Scales come eight bytes a row and 256 columns straight into registers, a step ahead.
+// Fragment i of subtile y stands for column WTN i + y of the wavefront's, so that a lane ends up with WTN neighbouring columns.
+// ---------------------------------------------------------------------------
+template <bool X4_, int WM_, int WN_, int WTM_, int WTN_, int STAGES_> struct Mx4Tile {
+    static constexpr bool X4 = X4_;
+    static constexpr int WM = WM_, WN = WN_, WTM = WTM_, WTN = WTN_, STAGES = STAGES_, NW = WM * WN;
+    static constexpr int TM = 32 * WM * WTM, TN = 32 * WN * WTN;
+    static constexpr int BK = X4 ? 128 : 64, PER = 256 / BK;   // columns a step, steps a group of 256
+    static constexpr int AB = X4 ? 64 : 128, BB = X4 ? 64 : 32; // bytes of a row a step
+    static constexpr int AI = TM * AB / 1024, TOTAL = AI + TN * BB / 1024, NI = (TOTAL + NW - 1) / NW;
+    static constexpr int STAGE_BYTES = TM * AB + TN * BB, LDS_BYTES = STAGES * STAGE_BYTES;
+    static_assert(STAGES >= 2 && NI * (STAGES - 1) < 60, "transfers in flight must fit the counter");
+};
+// chunk swizzle of rows of 128, 64 and 32 bytes: the 16 rows that one pass of a 16-byte read covers meet every bank once
+template <int BYTES> __device__ __forceinline__ int mx4_swz(int row)
+{
+    return BYTES == 128 ? (row >> 1) & 7 : BYTES == 64 ? (row >> 2) & 3 : (row >> 3) & 1;
+}
+
+// A die (blocks go round the eight of them) takes a run of tiles eight high, whose operands stay in its L2
+__device__ __forceinline__ void mx4_place(int mt, int nt, int &tm, int &tn)
+{
+    const int all = nt * mt, die = blockIdx.x & 7;
+    const int v = die * (all >> 3) + min(die, all & 7) + (blockIdx.x >> 3), mg = v / (8 * nt) * 8, high = min(8, mt - mg);
+    tm = mg + v % (8 * nt) % high;
+    tn = v % (8 * nt) / high;
+}
+
+template <class TL> __global__ __launch_bounds__(64 * TL::NW) void k_mx4_tiles(Mx4Args a)
+{
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    constexpr int WTM = TL::WTM, WTN = TL::WTN;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / TL::WN, wn = wave % TL::WN, i = lane & 31, g = lane >> 5;
+    int m0, n0;
+    mx4_place((a.M + TL::TM - 1) / TL::TM, (a.N + TL::TN - 1) / TL::TN, m0, n0);
+    m0 *= TL::TM;
+    n0 *= TL::TN;
+    const int nsteps = (a.K + TL::BK - 1) / TL::BK, ngroups = (nsteps + TL::PER - 1) / TL::PER;
+    const int64_t xpitch = TL::X4 ? a.wp : a.ldx * 2;
+
+    // this lane's share of a stage's transfers
+    const char *gp[TL::NI];
+    uint32_t goff[TL::NI], glim[TL::NI];
+#pragma unroll
+    for (int q = 0; q < TL::NI; ++q) {
+        const int ii = min(wave + TL::NW * q, TL::TOTAL - 1);
+        if (ii < TL::AI) {
+            const int row = ii * (1024 / TL::AB) + lane / (TL::AB / 16);
+            goff[q] = 16 * ((lane % (TL::AB / 16)) ^ mx4_swz<TL::AB>(row));
+            gp[q] = reinterpret_cast<const char *>(a.x) + min(m0 + row, a.M - 1) * xpitch;
+            glim[q] = TL::X4 ? 0x7fffffffu : 2u * ((a.K + 7) / 8 * 8 - 8); // x has no chunk past this one
+        } else {
+            const int row = (ii - TL::AI) * (1024 / TL::BB) + lane / (TL::BB / 16), w = row / (32 * WTN), y = row / 32 % WTN;
+            goff[q] = 16 * ((lane % (TL::BB / 16)) ^ mx4_swz<TL::BB>(row));
+            gp[q] = reinterpret_cast<const char *>(a.w) + min(n0 + w * 32 * WTN + (row & 31) * WTN + y, a.N - 1) * a.wp;
+            glim[q] = 0x7fffffffu;
+        }
+    }
+    auto issue = [&](int slot, int step) {
+        const uint32_t s = min(step, nsteps - 1); // past the end: the last step again, never used
+#pragma unroll
+        for (int q = 0; q < TL::NI; ++q) {
+            const int ii = min(wave + TL::NW * q, TL::TOTAL - 1);
+            const uint32_t by = s * (ii < TL::AI ? TL::AB : TL::BB);
+            dma16_at(gp[q] + min(by + goff[q], glim[q]), lds_address(lds) + slot * TL::STAGE_BYTES + ii * 1024);
+        }
+    };
+    // scales: eight bytes a row and 256 columns; this lane's half shifted to the bottom
+    const uint8_t *bs[WTN], *as[TL::X4 ? WTM : 1];
+#pragma unroll
+    for (int y = 0; y < WTN; ++y) bs[y] = a.ws + min(n0 + wn * 32 * WTN + i * WTN + y, a.N - 1) * a.sp;
+    if constexpr (TL::X4)
+#pragma unroll
+        for (int x = 0; x < WTM; ++x) as[x] = a.xs + min(m0 + (wm * WTM + x) * 32 + i, a.M - 1) * a.sp;
+    uint64_t bsn[WTN], bsc[WTN], asn[TL::X4 ? WTM : 1], asc[TL::X4 ? WTM : 1];
+    auto scales = [&](int group) {
+        const int o = 8 * min(group, ngroups - 1);
+#pragma unroll
+        for (int y = 0; y < WTN; ++y) bsn[y] = *reinterpret_cast<const uint64_t *>(bs[y] + o);
+        if constexpr (TL::X4)
+#pragma unroll
+            for (int x = 0; x < WTM; ++x) asn[x] = *reinterpret_cast<const uint64_t *>(as[x] + o);
+    };
+    scales(0);
+#pragma unroll
+    for (int s = 0; s < TL::STAGES - 1; ++s) issue(s, s);
+
+    f32x16 acc[WTM][WTN];
+#pragma unroll
+    for (int x = 0; x < WTM; ++x)
+#pragma unroll
+        for (int y = 0; y < WTN; ++y)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[x][y][v] = 0.f;
+    int arow[WTM], brow[WTN], asw[WTM], bsw[WTN];
+#pragma unroll
+    for (int x = 0; x < WTM; ++x) {
+        const int row = (wm * WTM + x) * 32 + i;
+        arow[x] = row * TL::AB;
+        asw[x] = mx4_swz<TL::AB>(row);
+    }
+#pragma unroll
+    for (int y = 0; y < WTN; ++y) {
+        const int row = (wn * WTN + y) * 32 + i;
+        brow[y] = TL::TM * TL::AB + row * TL::BB;
+        bsw[y] = mx4_swz<TL::BB>(row);
+    }
+    int slot = 0;
+    for (int grp = 0; grp < ngroups; ++grp) {
+        const int half = TL::X4 ? 16 * g : 8 * g;
+#pragma unroll
+        for (int y = 0; y < WTN; ++y) bsc[y] = bsn[y] >> half;
+        if constexpr (TL::X4)
+#pragma unroll
+            for (int x = 0; x < WTM; ++x) asc[x] = asn[x] >> half;
+        scales(grp + 1);
+#pragma unroll
+        for (int u = 0; u < TL::PER; ++u) {
+            const int st = grp * TL::PER + u;
+            if (st >= nsteps) break;
+            wait_vm<TL::NI * (TL::STAGES - 2)>(); // this wavefront's share of the stage has landed
+            __syncthreads();                       // ... and everybody else's; the stage before is free
+            const char *sb = lds + slot * TL::STAGE_BYTES;
+            issue(slot == 0 ? TL::STAGES - 1 : slot - 1, st + TL::STAGES - 1);
+            if constexpr (TL::X4) {
+                u32x4 af[2][WTM], bf[2][WTN];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                    for (int y = 0; y < WTN; ++y) bf[j][y] = *reinterpret_cast<const u32x4 *>(sb + brow[y] + (((2 * g + j) ^ bsw[y]) << 4));
+#pragma unroll
+                    for (int x = 0; x < WTM; ++x) af[j][x] = *reinterpret_cast<const u32x4 *>(sb + arow[x] + (((2 * g + j) ^ asw[x]) << 4));
+                }
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int x = 0; x < WTM; ++x)
+#pragma unroll
+                        for (int y = 0; y < WTN; ++y) {
+                            const i32x8 p = {(int)af[j][x][0], (int)af[j][x][1], (int)af[j][x][2], (int)af[j][x][3], 0, 0, 0, 0};
+                            const i32x8 q = {(int)bf[j][y][0], (int)bf[j][y][1], (int)bf[j][y][2], (int)bf[j][y][3], 0, 0, 0, 0};
+                            const int sa = (int)(asc[x] >> (32 * u)), sc = (int)(bsc[y] >> (32 * u));
+                            if (j == 0) acc[x][y] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(p, q, acc[x][y], 4, 4, 0, sa, 0, sc);
+                            else acc[x][y] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(p, q, acc[x][y], 4, 4, 1, sa, 1, sc);
+                        }
+            } else {
+                const bool tail = st * 64 + 64 > a.K;
+                u32x4 bw[WTN], af[2][WTM];
+#pragma unroll
+                for (int y = 0; y < WTN; ++y) bw[y] = *reinterpret_cast<const u32x4 *>(sb + brow[y] + ((g ^ bsw[y]) << 4));
+                auto rd = [&](int j) {
+#pragma unroll
+                    for (int x = 0; x < WTM; ++x) af[j & 1][x] = *reinterpret_cast<const u32x4 *>(sb + arow[x] + (((4 * g + j) ^ asw[x]) << 4));
+                };
+                rd(0);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (j < 3) rd(j + 1);
+                    bf16x8 bf[WTN];
+#pragma unroll
+                    for (int y = 0; y < WTN; ++y) bf[y] = mx4_bf16(bw[y][j], mx4_scale((uint32_t)(bsc[y] >> (16 * u)) & 255u));
+                    if (tail)
+#pragma unroll
+                        for (int x = 0; x < WTM; ++x) af[j & 1][x] = mx4_keep(af[j & 1][x], a.K - (st * 64 + 32 * g + 8 * j));
+#pragma unroll
+                    for (int x = 0; x < WTM; ++x)
+#pragma unroll
+                        for (int y = 0; y < WTN; ++y)
+                            acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<bf16x8 *>(&af[j & 1][x]), bf[y], acc[x][y], 0, 0, 0);
+                }
+            }
+            slot = slot + 1 == TL::STAGES ? 0 : slot + 1;
+        }
+    }
+    wait_vm<0>(); // the repeated transfers of the last steps end before the workgroup's LDS does
+
+    const int n = n0 + wn * 32 * WTN + i * WTN;
+    float bias[WTN];
+#pragma unroll
+    for (int y = 0; y < WTN; ++y) bias[y] = a.bias ? a.bias[min(n + y, a.N - 1)] : 0.f;
+    const int size = a.y_f32 ? 4 : 2;
+    const bool wide = n + WTN <= a.N && a.ldy % WTN == 0 && (reinterpret_cast<uintptr_t>(a.y) & (WTN * size - 1)) == 0;
+#pragma unroll
+    for (int x = 0; x < WTM; ++x)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            const int m = m0 + (wm * WTM + x) * 32 + 8 * (v >> 2) + 4 * g + (v & 3);
+            if (m >= a.M) continue;
+            float o[WTN];
+#pragma unroll
+            for (int y = 0; y < WTN; ++y) {
+                o[y] = acc[x][y][v] + bias[y];
+                if (a.gelu) o[y] = mx4_gelu(o[y]);
+            }
+            mx4_store<WTN>(a, (int64_t)m * a.ldy + n, n, o, wide);
+        }
+}
+
 static inline int64_t code_pitch(int cols) { return ((int64_t)cols + 255) / 256 * 128; }
 static inline int64_t scale_pitch(int cols) { return ((int64_t)cols + 255) / 256 * 8; }
 static inline bool dtype_ok(int32_t t) { return t == PAC_BF16 || t == PAC_F32; }
@@ -341,9 +578,22 @@ static pac_status check_product(const void *x, int32_t M, int32_t K, int32_t N, 
     return PAC_OK;
 }
 
+template <class TL> static pac_status launch_tiles(const Mx4Args &a, hipStream_t st)
+{
+    const int64_t tiles = tile_count(((int64_t)a.N + TL::TN - 1) / TL::TN, ((int64_t)a.M + TL::TM - 1) / TL::TM);
+    if (tiles < 0) return PAC_ERR_UNSUPPORTED;
+    static std::once_flag once;
+    std::call_once(once, [] {
+        (void)hipFuncSetAttribute(reinterpret_cast<const void *>(&k_mx4_tiles<TL>), hipFuncAttributeMaxDynamicSharedMemorySize, TL::LDS_BYTES);
+    });
+    hipLaunchKernelGGL((k_mx4_tiles<TL>), dim3((unsigned)tiles), dim3(64 * TL::NW), TL::LDS_BYTES, st, a);
+    return done();
+}
+
 template <bool X4> static pac_status launch_linear(const Mx4Args &a, hipStream_t st)
 {
     (void)hipGetLastError();
+    if (a.M > 128) return launch_tiles<Mx4Tile<X4, 2, 4, 4, 2, X4 ? 4 : 3>>(a, st);
     const int64_t nt = ((int64_t)a.N + 15) / 16;
     const int rm = a.M <= 16 ? 1 : a.M <= 32 ? 2 : 4;
     const int64_t tiles = tile_count(nt, ((int64_t)a.M + 16 * rm - 1) / (16 * rm));
