@@ -147,7 +147,7 @@ __device__ __forceinline__ void mx4_put(const Mx4Args &a, int m, int n, float v)
 }
 
 // W neighbouring outputs, in one store where all of them are there and lie on a store's boundary
-template <int W> __device__ __forceinline__ void mx4_store(const Mx4Args &a, int64_t at, int n, const float (&o)[W], bool wide)
+template <int W> __device__ __forceinline__ void mx4_store(const Mx4Args &a, int cols, int64_t at, int n, const float (&o)[W], bool wide)
 {
     typedef float fv __attribute__((ext_vector_type(W)));
     typedef bf16_t hv __attribute__((ext_vector_type(W)));
@@ -161,7 +161,7 @@ template <int W> __device__ __forceinline__ void mx4_store(const Mx4Args &a, int
         } else
 #pragma unroll
             for (int e = 0; e < W; ++e)
-                if (n + e < a.N) p[e] = o[e];
+                if (n + e < cols) p[e] = o[e];
     } else {
         bf16_t *p = reinterpret_cast<bf16_t *>(a.y) + at;
         if (wide) {
@@ -172,7 +172,7 @@ template <int W> __device__ __forceinline__ void mx4_store(const Mx4Args &a, int
         } else
 #pragma unroll
             for (int e = 0; e < W; ++e)
-                if (n + e < a.N) p[e] = (bf16_t)o[e];
+                if (n + e < cols) p[e] = (bf16_t)o[e];
     }
 }
 
@@ -540,7 +540,159 @@ template <class TL> __global__ __launch_bounds__(64 * TL::NW) void k_mx4_tiles(M
                 o[y] = acc[x][y][v] + bias[y];
                 if (a.gelu) o[y] = mx4_gelu(o[y]);
             }
-            mx4_store<WTN>(a, (int64_t)m * a.ldy + n, n, o, wide);
+            mx4_store<WTN>(a, a.N, (int64_t)m * a.ldy + n, n, o, wide);
+        }
+}
+
+// dx for many rows: a workgroup's tile of 32 WM WTM rows by 256 columns, W's rows in steps of 64.  dy streams into LDS as above.
+// W's step is turned round on its way: a thread takes eight columns of four rows (four loads of 4 bytes, 128 bytes a row and 32
+// threads), converts them with each row's scale, and writes the four rows of each column side by side, as the fragments want them.
+// It is loaded two steps ahead, converted and written one step ahead, a quarter after each quarter of the matrix instructions.
+// LDS row c 32 + i holds column 8 i + c: the writes of 32 threads and the reads of a fragment then go to neighbouring rows, and
+// subtile c of lane i is column 8 i + c of the tile, WTN neighbouring ones a lane.
+template <int WM_, int WN_, int WTM_, int WTN_, int STAGES_> struct Mx4DxTile {
+    static constexpr int WM = WM_, WN = WN_, WTM = WTM_, WTN = WTN_, STAGES = STAGES_, NW = WM * WN;
+    static constexpr int TM = 32 * WM * WTM, TK = 256, BK = 64;
+    static constexpr int TOTAL = TM / 8, NI = (TOTAL + NW - 1) / NW, TASKS = 512 / (64 * NW);
+    static constexpr int A_BYTES = TM * 128, B_BYTES = TK * 128, LDS_BYTES = STAGES * A_BYTES + 2 * B_BYTES;
+    static_assert(WN * WTN == 8 && TASKS * NW == 8, "256 columns, 512 tasks a step");
+    static_assert(STAGES >= 2 && NI * (STAGES - 1) < 60, "transfers in flight must fit the counter");
+};
+
+template <class TL> __global__ __launch_bounds__(64 * TL::NW) void k_mx4_dx_tiles(Mx4Args a)
+{
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    constexpr int WTM = TL::WTM, WTN = TL::WTN, NT = 64 * TL::NW;
+    char *const bbuf = lds + TL::STAGES * TL::A_BYTES;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / TL::WN, wn = wave % TL::WN, i = lane & 31, g = lane >> 5;
+    int m0, k0;
+    mx4_place((a.M + TL::TM - 1) / TL::TM, (a.K + TL::TK - 1) / TL::TK, m0, k0);
+    m0 *= TL::TM;
+    k0 *= TL::TK;
+    const int nsteps = (a.N + 63) / 64;
+
+    const char *gp[TL::NI];
+    uint32_t goff[TL::NI];
+    const uint32_t glim = 2u * ((a.N + 7) / 8 * 8 - 8); // dy has no chunk past this one
+#pragma unroll
+    for (int q = 0; q < TL::NI; ++q) {
+        const int ii = min(wave + TL::NW * q, TL::TOTAL - 1), row = ii * 8 + lane / 8;
+        goff[q] = 16 * ((lane & 7) ^ mx4_swz<128>(row));
+        gp[q] = reinterpret_cast<const char *>(a.x) + min(m0 + row, a.M - 1) * (a.ldx * 2);
+    }
+    auto issue = [&](int slot, int step) {
+        const uint32_t s = min(step, nsteps - 1); // past the end: the last step again, never used
+#pragma unroll
+        for (int q = 0; q < TL::NI; ++q) {
+            const int ii = min(wave + TL::NW * q, TL::TOTAL - 1);
+            dma16_at(gp[q] + min(128 * s + goff[q], glim), lds_address(lds) + slot * TL::A_BYTES + ii * 1024);
+        }
+    };
+    // this thread's tasks: columns 8 cg .. 8 cg + 7, rows 4 ng .. 4 ng + 3 of a step
+    const int cg = threadIdx.x & 31;
+    const uint8_t *wc = a.w + k0 / 2 + 4 * cg, *sc = a.ws + k0 / 32 + (cg >> 2);
+    uint32_t wr[2][TL::TASKS][4], sr[2][TL::TASKS][4];
+    auto fetch = [&](int set, int step) {
+#pragma unroll
+        for (int h = 0; h < TL::TASKS; ++h)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int64_t n = min(64 * min(step, nsteps - 1) + 4 * (int)((threadIdx.x + h * NT) >> 5) + e, a.N - 1); // past the end dy counts as zero
+                wr[set][h][e] = *reinterpret_cast<const uint32_t *>(wc + n * a.wp);
+                sr[set][h][e] = sc[n * a.sp];
+            }
+    };
+    uint32_t wat[TL::TASKS]; // where a task's column 0 goes; column c: 4096 bytes further (the swizzle repeats every 16 rows)
+#pragma unroll
+    for (int h = 0; h < TL::TASKS; ++h) {
+        const int ng = (threadIdx.x + h * NT) >> 5;
+        wat[h] = cg * 128 + (((ng >> 1) ^ mx4_swz<128>(cg)) << 4) + 8 * (ng & 1);
+    }
+#define PAC_MX4_TURN(SET, C, TO)                                                                                               \
+    _Pragma("unroll") for (int h = 0; h < TL::TASKS; ++h)                                                                      \
+    {                                                                                                                          \
+        bf16x2 p[4];                                                                                                           \
+        _Pragma("unroll") for (int e = 0; e < 4; ++e) p[e] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(wr[SET][h][e], mx4_scale(sr[SET][h][e]), C); \
+        typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));                                                            \
+        *reinterpret_cast<u32x2 *>((TO) + wat[h] + 8192 * C) = u32x2{pk_lo(p[0], p[1]), pk_lo(p[2], p[3])};                   \
+        *reinterpret_cast<u32x2 *>((TO) + wat[h] + 8192 * C + 4096) = u32x2{pk_hi(p[0], p[1]), pk_hi(p[2], p[3])};            \
+    }
+    fetch(0, 0);
+    fetch(1, 1);
+#pragma unroll
+    for (int s = 0; s < TL::STAGES - 1; ++s) issue(s, s);
+    PAC_MX4_TURN(0, 0, bbuf)
+    PAC_MX4_TURN(0, 1, bbuf)
+    PAC_MX4_TURN(0, 2, bbuf)
+    PAC_MX4_TURN(0, 3, bbuf)
+
+    f32x16 acc[WTM][WTN];
+#pragma unroll
+    for (int x = 0; x < WTM; ++x)
+#pragma unroll
+        for (int y = 0; y < WTN; ++y)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[x][y][v] = 0.f;
+    int arow[WTM], asw[WTM];
+#pragma unroll
+    for (int x = 0; x < WTM; ++x) {
+        arow[x] = ((wm * WTM + x) * 32 + i) * 128;
+        asw[x] = mx4_swz<128>((wm * WTM + x) * 32 + i);
+    }
+    const int brow = (wn * WTN * 32 + i) * 128, bsw = mx4_swz<128>(i);
+    int slot = 0;
+    auto step = [&](int st, auto odd) __attribute__((always_inline)) {
+        constexpr int now = decltype(odd)::value, next = now ^ 1; // the set that holds step st + 1 is `next`
+        wait_vm<TL::NI * (TL::STAGES - 2)>();
+        __syncthreads();
+        const char *sa = lds + slot * TL::A_BYTES, *sb = bbuf + now * TL::B_BYTES;
+        char *to = bbuf + next * TL::B_BYTES;
+        fetch(now, st + 2);
+        issue(slot == 0 ? TL::STAGES - 1 : slot - 1, st + TL::STAGES - 1);
+        const bool tail = st * 64 + 64 > a.N;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            u32x4 af[WTM], bf[WTN];
+#pragma unroll
+            for (int x = 0; x < WTM; ++x) af[x] = *reinterpret_cast<const u32x4 *>(sa + arow[x] + (((4 * g + j) ^ asw[x]) << 4));
+#pragma unroll
+            for (int y = 0; y < WTN; ++y) bf[y] = *reinterpret_cast<const u32x4 *>(sb + brow + y * 4096 + (((4 * g + j) ^ bsw) << 4));
+            if (tail)
+#pragma unroll
+                for (int x = 0; x < WTM; ++x) af[x] = mx4_keep(af[x], a.N - (st * 64 + 32 * g + 8 * j));
+#pragma unroll
+            for (int x = 0; x < WTM; ++x)
+#pragma unroll
+                for (int y = 0; y < WTN; ++y)
+                    acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<bf16x8 *>(&af[x]), *reinterpret_cast<bf16x8 *>(&bf[y]), acc[x][y], 0, 0, 0);
+            if (j == 0) { PAC_MX4_TURN(next, 0, to) }
+            else if (j == 1) { PAC_MX4_TURN(next, 1, to) }
+            else if (j == 2) { PAC_MX4_TURN(next, 2, to) }
+            else { PAC_MX4_TURN(next, 3, to) }
+        }
+        slot = slot + 1 == TL::STAGES ? 0 : slot + 1;
+    };
+    for (int st = 0; st < nsteps; st += 2) {
+        step(st, std::integral_constant<int, 0>());
+        if (st + 1 < nsteps) step(st + 1, std::integral_constant<int, 1>());
+    }
+#undef PAC_MX4_TURN
+    wait_vm<0>(); // the repeated transfers of the last steps end before the workgroup's LDS does
+
+    const int col = k0 + 8 * i + WTN * wn;
+    const int size = a.y_f32 ? 4 : 2;
+    const bool wide = col + WTN <= a.K && a.ldy % WTN == 0 && (reinterpret_cast<uintptr_t>(a.y) & (WTN * size - 1)) == 0;
+#pragma unroll
+    for (int x = 0; x < WTM; ++x)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            const int m = m0 + (wm * WTM + x) * 32 + 8 * (v >> 2) + 4 * g + (v & 3);
+            if (m >= a.M) continue;
+            float o[WTN];
+#pragma unroll
+            for (int y = 0; y < WTN; ++y) o[y] = acc[x][y][v];
+            mx4_store<WTN>(a, a.K, (int64_t)m * a.ldy + col, col, o, wide);
         }
 }
 
@@ -587,6 +739,18 @@ template <class TL> static pac_status launch_tiles(const Mx4Args &a, hipStream_t
         (void)hipFuncSetAttribute(reinterpret_cast<const void *>(&k_mx4_tiles<TL>), hipFuncAttributeMaxDynamicSharedMemorySize, TL::LDS_BYTES);
     });
     hipLaunchKernelGGL((k_mx4_tiles<TL>), dim3((unsigned)tiles), dim3(64 * TL::NW), TL::LDS_BYTES, st, a);
+    return done();
+}
+
+template <class TL> static pac_status launch_dx_tiles(const Mx4Args &a, hipStream_t st)
+{
+    const int64_t tiles = tile_count(((int64_t)a.K + TL::TK - 1) / TL::TK, ((int64_t)a.M + TL::TM - 1) / TL::TM);
+    if (tiles < 0) return PAC_ERR_UNSUPPORTED;
+    static std::once_flag once;
+    std::call_once(once, [] {
+        (void)hipFuncSetAttribute(reinterpret_cast<const void *>(&k_mx4_dx_tiles<TL>), hipFuncAttributeMaxDynamicSharedMemorySize, TL::LDS_BYTES);
+    });
+    hipLaunchKernelGGL((k_mx4_dx_tiles<TL>), dim3((unsigned)tiles), dim3(64 * TL::NW), TL::LDS_BYTES, st, a);
     return done();
 }
 
@@ -699,6 +863,7 @@ pac_status pac_mx4_linear_dx(const void *dy, int32_t M, int32_t N, int64_t dy_st
     const Mx4Args a{dy, nullptr, dy_stride, codes, scales, M, K, N, code_pitch(K), scale_pitch(K), nullptr, 0, dx, dx_dtype == PAC_F32,
                     dx_stride};
     (void)hipGetLastError();
+    if (M > 512) return launch_dx_tiles<Mx4DxTile<4, 2, 2, 4, 2>>(a, static_cast<hipStream_t>(hip_stream));
     const int rm = M <= 16 ? 1 : 2;
     const int64_t tiles = tile_count(((int64_t)K + 127) / 128, ((int64_t)M + 16 * rm - 1) / (16 * rm));
     if (tiles < 0) return PAC_ERR_UNSUPPORTED;
