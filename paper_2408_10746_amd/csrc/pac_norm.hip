@@ -18,51 +18,64 @@ struct NormArgs {
     int nv, v_a, v_b, v_c, v_d; // vectors of cols, and which is which (-1: not wanted)
 };
 
-// sums of a row's NS values over its TPR threads, on all of them; `red` belongs to the row, [2][TPR / 64][4], `turn` alternates
+// Sum over a wavefront, the same bits on every lane: four rotations inside rows of 16 lanes, then the four rows' sums in order.
+// (Lane exchanges through LDS take six round trips for it; a row needs up to four such sums one after the other.)
+template <int R> __device__ __forceinline__ float add_ror(float v) // v + v of the lane R to the side, in rows of 16
+{
+    return v + __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x120 + R, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float wave_sum(float v)
+{
+    v = add_ror<1>(add_ror<2>(add_ror<4>(add_ror<8>(v))));
+    auto at = [&](int l) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), l)); };
+    return (at(0) + at(16)) + (at(32) + at(48));
+}
+
+// sums of a row's NS values over its TPR threads, on all of them; `red` belongs to the row, [2][TPR / 64][2], `turn` alternates
 // so that one barrier a sum is enough
 template <int TPR, int NS> __device__ __forceinline__ void row_sums(float (&s)[NS], float *red, int &turn)
 {
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1)
-#pragma unroll
-        for (int k = 0; k < NS; ++k) s[k] += __shfl_xor(s[k], o, 64);
+    for (int k = 0; k < NS; ++k) s[k] = wave_sum(s[k]);
     if constexpr (TPR > 64) {
         constexpr int W = TPR / 64;
-        float *r = red + turn * W * 4;
+        float *r = red + turn * W * 2;
         turn ^= 1;
         const int wave = (threadIdx.x % TPR) >> 6;
         if ((threadIdx.x & 63) == 0)
 #pragma unroll
-            for (int k = 0; k < NS; ++k) r[wave * 4 + k] = s[k];
+            for (int k = 0; k < NS; ++k) r[k * W + wave] = s[k];
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < NS; ++k) {
             s[k] = 0.f;
 #pragma unroll
-            for (int w = 0; w < W; ++w) s[k] += r[w * 4 + k];
+            for (int w = 0; w < W; ++w) s[k] += r[k * W + w];
         }
     }
 }
 
-// E neighbouring-by-VEC values of a row a thread: chunk c holds columns (c TPR + t) VEC and the VEC - 1 after it
+// E values of a row a thread, in chunks of VEC neighbours: chunk c holds columns (c TPR + t) VEC and the VEC - 1 after it
 template <typename T, int VEC, int TPR, int E> struct RowIO {
     static constexpr int CH = E / VEC;
     typedef T vec __attribute__((ext_vector_type(VEC)));
+    struct Raw { vec v[CH]; }; // as it comes from memory: the coming row waits in this form while the present one is worked on
     static __device__ __forceinline__ int col(int t, int c) { return (c * TPR + t) * VEC; }
-    static __device__ __forceinline__ void load(const void *p, int64_t row, int d, int t, float (&v)[E])
+    static __device__ __forceinline__ bool in(int t, int e, int d) { return col(t, e / VEC) + e % VEC < d; }
+    static __device__ __forceinline__ void fetch(Raw &r, const void *p, int64_t row, int d, int t)
     {
         const T *src = reinterpret_cast<const T *>(p) + row * d;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int j = col(t, c);
-            if constexpr (VEC == 1) v[c] = j < d ? (float)src[j] : 0.f;
-            else {
-                const bool in = j < d; // d is a multiple of VEC
-                const vec r = *reinterpret_cast<const vec *>(src + (in ? j : 0));
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) v[c * VEC + e] = in ? (float)r[e] : 0.f;
-            }
+            // past the row's end: its first values, which widen() leaves out (d is a multiple of VEC)
+            r.v[c] = *reinterpret_cast<const vec *>(src + (j < d ? j : 0));
         }
+    }
+    static __device__ __forceinline__ void widen(const Raw &r, int d, int t, float (&v)[E])
+    {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = in(t, e, d) ? (float)r.v[e / VEC][e % VEC] : 0.f;
     }
     static __device__ __forceinline__ void store(void *p, int64_t row, int d, int t, const float (&v)[E])
     {
@@ -71,25 +84,25 @@ template <typename T, int VEC, int TPR, int E> struct RowIO {
         for (int c = 0; c < CH; ++c) {
             const int j = col(t, c);
             if (j >= d) continue;
-            if constexpr (VEC == 1) dst[j] = (T)v[c];
-            else {
-                vec r;
+            vec r;
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) r[e] = (T)v[c * VEC + e];
-                *reinterpret_cast<vec *>(dst + j) = r;
-            }
+            for (int e = 0; e < VEC; ++e) r[e] = (T)v[c * VEC + e];
+            *reinterpret_cast<vec *>(dst + j) = r;
         }
     }
-    // a parameter's values at this thread's columns (`none` where there is no such parameter or no such column)
+    // a parameter's values at this thread's columns (`none` where there is no such parameter; anything where no such column)
     static __device__ __forceinline__ void param(const float *p, int d, int t, float none, float (&v)[E])
     {
+        constexpr int PV = VEC >= 4 ? 4 : 1;
+        typedef float pv __attribute__((ext_vector_type(PV)));
 #pragma unroll
-        for (int c = 0; c < CH; ++c)
+        for (int e = 0; e < E; e += PV) {
+            const int j = col(t, e / VEC) + e % VEC;
+            pv r;
+            if (p) r = *reinterpret_cast<const pv *>(p + (j < d ? j : 0));
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                const int j = col(t, c) + e;
-                v[c * VEC + e] = p && j < d ? p[j] : none;
-            }
+            for (int k = 0; k < PV; ++k) v[e + k] = p ? r[k] : none;
+        }
     }
 };
 
@@ -106,7 +119,7 @@ __device__ __forceinline__ float normalise(float (&v)[E], const NormArgs &a, int
         row_sums<TPR, 1>(s, red, turn);
         const float mean = s[0] * a.inv_d;
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = IO::col(t, e / (E / IO::CH)) < a.d ? v[e] - mean : 0.f;
+        for (int e = 0; e < E; ++e) v[e] = IO::in(t, e, a.d) ? v[e] - mean : 0.f;
     }
     s[0] = 0.f;
 #pragma unroll
@@ -120,179 +133,252 @@ __device__ __forceinline__ float normalise(float (&v)[E], const NormArgs &a, int
 
 // g becomes the gradient of N's input, given that of its output; h: N's output, r: 1 / deviation
 template <int TPR, int E, class IO, bool LAYER>
-__device__ __forceinline__ void norm_back(float (&g)[E], const float (&h)[E], float r, const NormArgs &a, int t, float *red, int &turn)
+__device__ __forceinline__ void norm_back(float (&g)[E], const float (&h)[E], float r, const NormArgs &a, float *red, int &turn)
 {
-    float s[2] = {0.f, 0.f};
+    float along, mean = 0.f;
+    if constexpr (LAYER) {
+        float s[2] = {0.f, 0.f};
 #pragma unroll
-    for (int e = 0; e < E; ++e) s[0] = fmaf(g[e], h[e], s[0]), s[1] += g[e];
-    if constexpr (LAYER) row_sums<TPR, 2>(s, red, turn);
-    else {
-        float s1[1] = {s[0]};
-        row_sums<TPR, 1>(s1, red, turn);
-        s[0] = s1[0];
+        for (int e = 0; e < E; ++e) s[0] = fmaf(g[e], h[e], s[0]), s[1] += g[e];
+        row_sums<TPR, 2>(s, red, turn);
+        along = s[0] * a.inv_d;
+        mean = s[1] * a.inv_d;
+    } else {
+        float s[1] = {0.f};
+#pragma unroll
+        for (int e = 0; e < E; ++e) s[0] = fmaf(g[e], h[e], s[0]);
+        row_sums<TPR, 1>(s, red, turn);
+        along = s[0] * a.inv_d;
     }
-    const float along = s[0] * a.inv_d, mean = LAYER ? s[1] * a.inv_d : 0.f;
 #pragma unroll
     for (int e = 0; e < E; ++e) g[e] = r * (g[e] - mean - h[e] * along);
 }
 
-template <typename T, int VEC, int TPR, int E, bool LAYER>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_fwd(NormArgs a)
+template <int TPR> constexpr int kRowsPerBlock = TPR < 512 ? 512 / TPR : 1;
+template <int TPR> constexpr int kNormThreads = TPR < 512 ? 512 : TPR;
+
+template <typename T, int VEC, int TPR, int E, bool LAYER> __global__ __launch_bounds__(kNormThreads<TPR>) void k_norm_fwd(NormArgs a)
 {
-    constexpr int RPB = TPR < 256 ? 256 / TPR : 1;
+    constexpr int RPB = kRowsPerBlock<TPR>;
     using IO = RowIO<T, VEC, TPR, E>;
-    __shared__ float redm[RPB * 2 * (TPR / 64) * 4];
+    __shared__ __attribute__((aligned(16))) float redm[RPB * 2 * (TPR / 64) * 2];
     const int t = threadIdx.x % TPR, slot = threadIdx.x / TPR;
-    float *red = redm + slot * 2 * (TPR / 64) * 4;
+    float *red = redm + slot * 2 * (TPR / 64) * 2;
     int turn = 0;
-    const float res = a.res ? a.res[0] : 1.f;
-    float wp[E], bp[E], gt[E], wn[E], bn[E];
-    IO::param(a.w_post, a.d, t, 1.f, wp);
-    IO::param(a.b_post, a.d, t, 0.f, bp);
-    IO::param(a.w_pre, a.d, t, 0.f, wn);
-    IO::param(a.b_pre, a.d, t, 0.f, bn);
-    if (a.gate_len > 1) IO::param(a.gate, a.d, t, 0.f, gt);
-    else {
-        const float g = a.gate ? a.gate[0] : 1.f;
-#pragma unroll
-        for (int e = 0; e < E; ++e) gt[e] = g;
-    }
+    const int64_t stride = (int64_t)gridDim.x * RPB;
     // every thread of a block goes round as often (barriers): a slot whose row is past the end works on the last one, unstored
-    for (int64_t row0 = (int64_t)blockIdx.x * RPB; row0 < a.rows; row0 += (int64_t)gridDim.x * RPB) {
+    int64_t row0 = (int64_t)blockIdx.x * RPB;
+    auto clamp = [&](int64_t r) { return r < a.rows ? r : a.rows - 1; };
+    const void *const po = a.o ? a.o : a.x; // what is not there is not used
+    typename IO::Raw rx, ro;
+    IO::fetch(rx, a.x, clamp(row0 + slot), a.d, t);
+    IO::fetch(ro, po, clamp(row0 + slot), a.d, t);
+    const float res = a.res ? a.res[0] : 1.f, g0 = a.gate_len == 1 ? a.gate[0] : 1.f;
+    for (; row0 < a.rows; row0 += stride) {
         const bool live = row0 + slot < a.rows;
-        const int64_t row = live ? row0 + slot : a.rows - 1;
-        float y[E];
-        IO::load(a.x, row, a.d, t, y);
+        const int64_t row = clamp(row0 + slot);
+        float y[E], o[E], p[E];
+        IO::widen(rx, a.d, t, y);
+        IO::widen(ro, a.d, t, o);
+        if (row0 + stride < a.rows) {
+            const int64_t next = clamp(row0 + stride + slot);
+            IO::fetch(rx, a.x, next, a.d, t);
+            IO::fetch(ro, po, next, a.d, t);
+        }
         if (a.o) {
-            float o[E];
-            IO::load(a.o, row, a.d, t, o);
             if (a.w_post) {
                 normalise<TPR, E, IO, LAYER>(o, a, t, red, turn);
+                IO::param(a.w_post, a.d, t, 1.f, p);
+                if constexpr (LAYER) {
+                    float b[E];
+                    IO::param(a.b_post, a.d, t, 0.f, b);
 #pragma unroll
-                for (int e = 0; e < E; ++e) o[e] = fmaf(o[e], wp[e], bp[e]);
+                    for (int e = 0; e < E; ++e) o[e] = fmaf(o[e], p[e], b[e]);
+                } else if (a.b_post) {
+                    float b[E];
+                    IO::param(a.b_post, a.d, t, 0.f, b);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) o[e] = fmaf(o[e], p[e], b[e]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) o[e] *= p[e];
+                }
             }
+            if (a.gate_len > 1) {
+                IO::param(a.gate, a.d, t, 0.f, p);
 #pragma unroll
-            for (int e = 0; e < E; ++e) y[e] = fmaf(res, y[e], gt[e] * o[e]);
+                for (int e = 0; e < E; ++e) y[e] = fmaf(res, y[e], p[e] * o[e]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e) y[e] = fmaf(res, y[e], g0 * o[e]);
+            }
         } else {
 #pragma unroll
             for (int e = 0; e < E; ++e) y[e] *= res;
         }
         if (a.y && live) IO::store(a.y, row, a.d, t, y);
         if (a.w_pre) {
-            normalise<TPR, E, IO, LAYER>(y, a, t, red, turn);
 #pragma unroll
-            for (int e = 0; e < E; ++e) y[e] = fmaf(y[e], wn[e], bn[e]);
+            for (int e = 0; e < E; ++e) y[e] = IO::in(t, e, a.d) ? y[e] : 0.f; // (a parameter has any value past the row's end)
+            normalise<TPR, E, IO, LAYER>(y, a, t, red, turn);
+            IO::param(a.w_pre, a.d, t, 0.f, p);
+            float b[E];
+            IO::param(a.b_pre, a.d, t, 0.f, b);
+#pragma unroll
+            for (int e = 0; e < E; ++e) y[e] = fmaf(y[e], p[e], b[e]);
             if (live) IO::store(a.n, row, a.d, t, y);
         }
     }
 }
 
-template <typename T, int VEC, int TPR, int E, bool LAYER>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_bwd(NormArgs a)
+// SHIFT: sums of g and of dn for the shifts' gradients (b_post, b_pre) are wanted too
+template <typename T, int VEC, int TPR, int E, bool LAYER, bool SHIFT>
+__global__ __launch_bounds__(kNormThreads<TPR>, 4) void k_norm_bwd(NormArgs a)
 {
-    constexpr int RPB = TPR < 256 ? 256 / TPR : 1, W = RPB * TPR / 64;
+    constexpr int RPB = kRowsPerBlock<TPR>, W = RPB * TPR / 64;
     using IO = RowIO<T, VEC, TPR, E>;
-    __shared__ float redm[RPB * 2 * (TPR / 64) * 4];
+    __shared__ __attribute__((aligned(16))) float redm[RPB * 2 * (TPR / 64) * 2];
     __shared__ double sred[2 * W];
+    __shared__ float join[RPB > 1 ? RPB * TPR * E : 1];
     const int t = threadIdx.x % TPR, slot = threadIdx.x / TPR;
-    float *red = redm + slot * 2 * (TPR / 64) * 4;
+    float *red = redm + slot * 2 * (TPR / 64) * 2;
     int turn = 0;
+    const int64_t stride = (int64_t)gridDim.x * RPB;
+    int64_t row0 = (int64_t)blockIdx.x * RPB;
+    auto clamp = [&](int64_t r) { return r < a.rows ? r : a.rows - 1; };
+    const void *const po = a.o ? a.o : a.x, *const pn = a.dn ? a.dn : a.x, *const py = a.dy ? a.dy : a.x; // what is not there is not used
+    typename IO::Raw rx, ro, ry, rn;
+    auto fetch = [&](int64_t r) {
+        IO::fetch(rx, a.x, r, a.d, t);
+        IO::fetch(ro, po, r, a.d, t);
+        IO::fetch(rn, pn, r, a.d, t);
+        IO::fetch(ry, py, r, a.d, t);
+    };
+    fetch(clamp(row0 + slot));
     const float res = a.res ? a.res[0] : 1.f, g0 = a.gate_len == 1 ? a.gate[0] : 1.f;
     float ca[E], cb[E], cc[E], cd[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) ca[e] = cb[e] = cc[e] = cd[e] = 0.f;
     double s_res = 0., s_gate = 0.;
-    for (int64_t row0 = (int64_t)blockIdx.x * RPB; row0 < a.rows; row0 += (int64_t)gridDim.x * RPB) {
+    for (; row0 < a.rows; row0 += stride) {
         const bool live = row0 + slot < a.rows;
-        const int64_t row = live ? row0 + slot : a.rows - 1;
-        float x[E], oh[E], gt[E], wp[E], g[E];
-        IO::load(a.x, row, a.d, t, x);
-        if (a.gate_len > 1) IO::param(a.gate, a.d, t, 0.f, gt);
-        else {
+        const int64_t row = clamp(row0 + slot);
+        float x[E], oh[E], p[E], g[E], w[E];
+        IO::widen(rx, a.d, t, x);
+        IO::widen(ro, a.d, t, oh);
+        IO::widen(ry, a.d, t, g);
+        float dn[E];
+        IO::widen(rn, a.d, t, dn);
+        if (row0 + stride < a.rows) fetch(clamp(row0 + stride + slot));
+        if (!a.dy)
 #pragma unroll
-            for (int e = 0; e < E; ++e) gt[e] = g0;
-        }
-        IO::param(a.w_post, a.d, t, 1.f, wp);
-        float ro = 1.f;
-        float p[E];
-        if (a.o) {
-            IO::load(a.o, row, a.d, t, oh);
-            if (a.w_post) {
-                ro = normalise<TPR, E, IO, LAYER>(oh, a, t, red, turn);
-                float bp[E];
-                IO::param(a.b_post, a.d, t, 0.f, bp);
+            for (int e = 0; e < E; ++e) g[e] = 0.f;
+        float r_o = 1.f;
+        if (!a.o) {
 #pragma unroll
-                for (int e = 0; e < E; ++e) p[e] = fmaf(oh[e], wp[e], bp[e]);
-            } else {
+            for (int e = 0; e < E; ++e) p[e] = oh[e] = 0.f;
+        } else if (a.w_post) {
+            r_o = normalise<TPR, E, IO, LAYER>(oh, a, t, red, turn);
+            IO::param(a.w_post, a.d, t, 1.f, w);
 #pragma unroll
-                for (int e = 0; e < E; ++e) p[e] = oh[e];
+            for (int e = 0; e < E; ++e) p[e] = oh[e] * w[e];
+            if (a.b_post) {
+                IO::param(a.b_post, a.d, t, 0.f, w);
+#pragma unroll
+                for (int e = 0; e < E; ++e) p[e] = IO::in(t, e, a.d) ? p[e] + w[e] : 0.f;
             }
         } else {
 #pragma unroll
-            for (int e = 0; e < E; ++e) p[e] = oh[e] = 0.f;
+            for (int e = 0; e < E; ++e) p[e] = oh[e];
         }
         if (a.w_pre) {
-            float yh[E], wn[E], dn[E];
+            float yh[E];
+            if (a.gate_len > 1) {
+                IO::param(a.gate, a.d, t, 0.f, w);
 #pragma unroll
-            for (int e = 0; e < E; ++e) yh[e] = fmaf(res, x[e], gt[e] * p[e]);
-            IO::load(a.dn, row, a.d, t, dn);
-            IO::param(a.w_pre, a.d, t, 0.f, wn);
-            const float ry = normalise<TPR, E, IO, LAYER>(yh, a, t, red, turn);
+                for (int e = 0; e < E; ++e) yh[e] = fmaf(res, x[e], w[e] * p[e]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e) yh[e] = fmaf(res, x[e], g0 * p[e]);
+            }
+            const float r_y = normalise<TPR, E, IO, LAYER>(yh, a, t, red, turn);
+            IO::param(a.w_pre, a.d, t, 0.f, w);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                if (live) cc[e] = fmaf(dn[e], yh[e], cc[e]), cd[e] += dn[e];
-                g[e] = dn[e] * wn[e];
+                if (live) {
+                    cc[e] = fmaf(dn[e], yh[e], cc[e]);
+                    if constexpr (SHIFT) cd[e] += dn[e];
+                }
+                dn[e] *= w[e];
             }
-            norm_back<TPR, E, IO, LAYER>(g, yh, ry, a, t, red, turn);
-            if (a.dy) {
-                float dy[E];
-                IO::load(a.dy, row, a.d, t, dy);
+            norm_back<TPR, E, IO, LAYER>(dn, yh, r_y, a, red, turn);
 #pragma unroll
-                for (int e = 0; e < E; ++e) g[e] += dy[e];
-            }
-        } else if (a.dy) IO::load(a.dy, row, a.d, t, g);
-        else {
-#pragma unroll
-            for (int e = 0; e < E; ++e) g[e] = 0.f;
+            for (int e = 0; e < E; ++e) g[e] = IO::in(t, e, a.d) ? g[e] + dn[e] : 0.f;
         }
         float sr = 0.f, sg = 0.f;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const bool in = IO::col(t, e / VEC) + e % VEC < a.d;
-            if (!in) g[e] = 0.f;
             sr = fmaf(g[e], x[e], sr);
             sg = fmaf(g[e], p[e], sg);
-            if (live) ca[e] = fmaf(g[e], oh[e], ca[e]), cb[e] += g[e];
+            if (live) {
+                ca[e] = fmaf(g[e], oh[e], ca[e]);
+                if constexpr (SHIFT) cb[e] += g[e];
+            }
         }
         if (live) s_res += sr, s_gate += sg;
         if (a.dx && live) {
-            float dx[E];
 #pragma unroll
-            for (int e = 0; e < E; ++e) dx[e] = res * g[e];
-            IO::store(a.dx, row, a.d, t, dx);
+            for (int e = 0; e < E; ++e) x[e] = res * g[e];
+            IO::store(a.dx, row, a.d, t, x);
         }
-        if (a.o && a.d_o) {
+        if (a.d_o) {
+            if (a.gate_len > 1) {
+                IO::param(a.gate, a.d, t, 0.f, w);
 #pragma unroll
-            for (int e = 0; e < E; ++e) g[e] *= gt[e] * wp[e];
-            if (a.w_post) norm_back<TPR, E, IO, LAYER>(g, oh, ro, a, t, red, turn);
+                for (int e = 0; e < E; ++e) g[e] *= w[e];
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e) g[e] *= g0;
+            }
+            if (a.w_post) {
+                IO::param(a.w_post, a.d, t, 1.f, w);
+#pragma unroll
+                for (int e = 0; e < E; ++e) g[e] *= w[e];
+                norm_back<TPR, E, IO, LAYER>(g, oh, r_o, a, red, turn);
+            }
             if (live) IO::store(a.d_o, row, a.d, t, g);
         }
     }
-    if (a.nv == 0 && !a.scal) return;
-    // the block's sums: rows dealt over its slots are joined slot by slot
+    // the block's partial sums, its slots' joined in their order
     auto put = [&](int v, const float (&c)[E]) {
         if (v < 0) return;
-        float *dst = a.cols + ((int64_t)(blockIdx.x * RPB + slot) * a.nv + v) * a.d;
+        float *dst = a.cols + ((int64_t)blockIdx.x * a.nv + v) * a.d;
+        if constexpr (RPB > 1) {
+            __syncthreads();
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const int j = IO::col(t, e / VEC) + e % VEC;
-            if (j < a.d) dst[j] = c[e];
+            for (int e = 0; e < E; ++e) join[(slot * E + e) * TPR + t] = c[e];
+            __syncthreads();
+            for (int k = threadIdx.x; k < TPR * E; k += kNormThreads<TPR>) {
+                const int e = k / TPR, j = IO::col(k % TPR, e / VEC) + e % VEC;
+                float s = 0.f;
+#pragma unroll
+                for (int q = 0; q < RPB; ++q) s += join[q * E * TPR + k];
+                if (j < a.d) dst[j] = s;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const int j = IO::col(t, e / VEC) + e % VEC;
+                if (j < a.d) dst[j] = c[e];
+            }
         }
     };
     put(a.v_a, ca);
-    put(a.v_b, cb);
     put(a.v_c, cc);
-    put(a.v_d, cd);
+    if constexpr (SHIFT) {
+        put(a.v_b, cb);
+        put(a.v_d, cd);
+    }
     if (a.scal) {
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) s_res += __shfl_xor(s_res, o, 64), s_gate += __shfl_xor(s_gate, o, 64);
@@ -309,53 +395,61 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_bwd(NormArgs a)
 struct NormSums {
     const float *cols;
     const double *scal;
-    int parts, blocks, d, nv, v_a, v_b, v_c, v_d, gate_len;
+    int parts, d, nv, v_a, v_b, v_c, v_d, gate_len;
     const float *w_post, *b_post, *gate;
     float *dw_post, *db_post, *dgate, *dres, *dw_pre, *db_pre;
-    int post;
 };
 
-// The parameters' gradients from the blocks' partial sums, in their order and in 64 bits.  16 columns a block, 16 threads a column.
-__global__ __launch_bounds__(256) void k_norm_sums(NormSums a)
+// The parameters' gradients from the blocks' partial sums, in a fixed order and in 64 bits.  16 columns a block, 32 threads a
+// column, eight loads under way each.
+template <int NV> __global__ __launch_bounds__(512) void k_norm_sums(NormSums a)
 {
-    __shared__ double red[4][16][17];
+    constexpr int NR = NV > 0 ? NV : 1;
+    __shared__ double red[NR][32][17];
     const int cj = threadIdx.x & 15, part = threadIdx.x >> 4, j = blockIdx.x * 16 + cj;
-    double s[4] = {0., 0., 0., 0.};
-    if (j < a.d)
-        for (int p = part; p < a.parts; p += 16)
-            for (int v = 0; v < a.nv; ++v) s[v] += (double)a.cols[((int64_t)p * a.nv + v) * a.d + j];
+    if constexpr (NV > 0) {
+        double s[NV];
 #pragma unroll
-    for (int v = 0; v < 4; ++v) red[v][part][cj] = s[v];
-    __syncthreads();
-    if (threadIdx.x < 16 && j < a.d) {
-        double t[4];
+        for (int v = 0; v < NV; ++v) s[v] = 0.;
+        const float *src = a.cols + min(j, a.d - 1);
+        for (int p0 = part; p0 < a.parts; p0 += 4 * 32) {
+            float f[4][NV];
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            t[v] = 0.;
-            for (int p = 0; p < 16; ++p) t[v] += red[v][p][cj];
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int v = 0; v < NV; ++v) f[u][v] = src[((int64_t)min(p0 + 32 * u, a.parts - 1) * NV + v) * a.d];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int v = 0; v < NV; ++v) s[v] += p0 + 32 * u < a.parts ? (double)f[u][v] : 0.;
         }
-        auto pick = [&](int v) { return v == 0 ? t[0] : v == 1 ? t[1] : v == 2 ? t[2] : v == 3 ? t[3] : 0.; };
-        const double ga = a.gate ? (double)a.gate[a.gate_len > 1 ? j : 0] : 1.;
-        if (a.dw_post) a.dw_post[j] = (float)(ga * pick(a.v_a));
-        if (a.db_post) a.db_post[j] = (float)(ga * pick(a.v_b));
-        if (a.dgate && a.gate_len > 1)
-            a.dgate[j] = (float)(a.post ? (double)a.w_post[j] * pick(a.v_a) + (a.b_post ? (double)a.b_post[j] * pick(a.v_b) : 0.) : pick(a.v_a));
-        if (a.dw_pre) a.dw_pre[j] = (float)pick(a.v_c);
-        if (a.db_pre) a.db_pre[j] = (float)pick(a.v_d);
+#pragma unroll
+        for (int v = 0; v < NV; ++v) red[v][part][cj] = s[v];
+        __syncthreads();
+        if (threadIdx.x < 16 && j < a.d) {
+            double t[4] = {0., 0., 0., 0.};
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int p = 0; p < 32; ++p) t[v] += red[v][p][cj];
+            auto pick = [&](int v) { return v == 0 ? t[0] : v == 1 ? t[1] : v == 2 ? t[2] : v == 3 ? t[3] : 0.; };
+            const double ga = a.gate ? (double)a.gate[a.gate_len > 1 ? j : 0] : 1.;
+            if (a.dw_post) a.dw_post[j] = (float)(ga * pick(a.v_a));
+            if (a.db_post) a.db_post[j] = (float)(ga * pick(a.v_b));
+            if (a.dgate && a.gate_len > 1)
+                a.dgate[j] = (float)(a.w_post ? (double)a.w_post[j] * pick(a.v_a) + (a.b_post ? (double)a.b_post[j] * pick(a.v_b) : 0.) : pick(a.v_a));
+            if (a.dw_pre) a.dw_pre[j] = (float)pick(a.v_c);
+            if (a.db_pre) a.db_pre[j] = (float)pick(a.v_d);
+        }
     }
-    if (blockIdx.x == 0 && (a.dres || (a.dgate && a.gate_len == 1))) {
-        __syncthreads();
-        double *r = &red[0][0][0];
-        double u[2] = {0., 0.};
-        for (int p = threadIdx.x; p < a.blocks; p += 256) u[0] += a.scal[2 * p], u[1] += a.scal[2 * p + 1];
-        r[2 * threadIdx.x] = u[0];
-        r[2 * threadIdx.x + 1] = u[1];
-        __syncthreads();
-        if (threadIdx.x < 2) {
-            double t = 0.;
-            for (int p = 0; p < 256; ++p) t += r[2 * p + threadIdx.x];
-            if (threadIdx.x == 0 && a.dres) a.dres[0] = (float)t;
-            if (threadIdx.x == 1 && a.dgate && a.gate_len == 1) a.dgate[0] = (float)t;
+    if (blockIdx.x == 0 && threadIdx.x < 64 && (a.dres || (a.dgate && a.gate_len == 1))) {
+        double u = 0., w = 0.;
+        for (int p = threadIdx.x; p < a.parts; p += 64) u += a.scal[2 * p], w += a.scal[2 * p + 1];
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) u += __shfl_xor(u, o, 64), w += __shfl_xor(w, o, 64);
+        if (threadIdx.x == 0) {
+            if (a.dres) a.dres[0] = (float)u;
+            if (a.dgate && a.gate_len == 1) a.dgate[0] = (float)w;
         }
     }
 }
@@ -377,33 +471,34 @@ static pac_status check_norm(const pac_block_norm *b, int64_t rows)
     return PAC_OK;
 }
 
-// Threads a row: as few as hold it at `E` values each, so that short rows take one wavefront and no barrier.
-static int threads_for(int d, int e) { return d <= 64 * e ? 64 : d <= 256 * e ? 256 : 1024; }
-
-constexpr int kNormE = 16; // values a thread
+// Threads a row: as few as hold it at eight values each, so that short rows take one wavefront and no barrier; rows past 8192 take
+// sixteen values a thread.
+static int threads_for(int d) { return d <= 512 ? 64 : d <= 1024 ? 128 : d <= 2048 ? 256 : d <= 4096 ? 512 : 1024; }
 
 static int64_t norm_blocks(int d, int64_t rows, bool backward)
 {
-    const int tpr = threads_for(d, kNormE), rpb = tpr < 256 ? 256 / tpr : 1;
-    const int64_t want = (rows + rpb - 1) / rpb, most = backward ? (tpr == 1024 ? 256 : 512) : (tpr == 1024 ? 512 : 2048);
+    const int tpr = threads_for(d), rpb = tpr < 512 ? 512 / tpr : 1;
+    const int64_t want = (rows + rpb - 1) / rpb, most = backward ? (tpr == 1024 ? 256 : 512) : 1024;
     return want < most ? want : most;
-}
-static int64_t norm_parts(int d, int64_t rows)
-{
-    const int tpr = threads_for(d, kNormE);
-    return norm_blocks(d, rows, true) * (tpr < 256 ? 256 / tpr : 1);
 }
 
 template <typename T, int VEC, bool LAYER> static void launch_norm(const NormArgs &a, bool backward, hipStream_t st)
 {
-    const int tpr = threads_for(a.d, kNormE);
-    const dim3 g((unsigned)norm_blocks(a.d, a.rows, backward)), b(tpr < 256 ? 256 : tpr);
-#define PAC_NORM_LAUNCH(TPR)                                                                                                   \
-    if (backward) hipLaunchKernelGGL((k_norm_bwd<T, VEC, TPR, kNormE, LAYER>), g, b, 0, st, a);                                \
-    else hipLaunchKernelGGL((k_norm_fwd<T, VEC, TPR, kNormE, LAYER>), g, b, 0, st, a);
-    if (tpr == 64) { PAC_NORM_LAUNCH(64) }
-    else if (tpr == 256) { PAC_NORM_LAUNCH(256) }
-    else { PAC_NORM_LAUNCH(1024) }
+    const int tpr = threads_for(a.d);
+    const dim3 g((unsigned)norm_blocks(a.d, a.rows, backward)), b(tpr < 512 ? 512 : tpr);
+    const bool shift = a.v_b >= 0 || a.v_d >= 0;
+#define PAC_NORM_LAUNCH(TPR, E)                                                                                                \
+    {                                                                                                                          \
+        if (!backward) hipLaunchKernelGGL((k_norm_fwd<T, VEC, TPR, E, LAYER>), g, b, 0, st, a);                                \
+        else if (shift) hipLaunchKernelGGL((k_norm_bwd<T, VEC, TPR, E, LAYER, true>), g, b, 0, st, a);                         \
+        else hipLaunchKernelGGL((k_norm_bwd<T, VEC, TPR, E, LAYER, false>), g, b, 0, st, a);                                   \
+    }
+    if (tpr == 64) PAC_NORM_LAUNCH(64, 8)
+    else if (tpr == 128) PAC_NORM_LAUNCH(128, 8)
+    else if (tpr == 256) PAC_NORM_LAUNCH(256, 8)
+    else if (tpr == 512) PAC_NORM_LAUNCH(512, 8)
+    else if (a.d <= 8192) PAC_NORM_LAUNCH(1024, 8)
+    else PAC_NORM_LAUNCH(1024, 16)
 #undef PAC_NORM_LAUNCH
 }
 
@@ -423,6 +518,7 @@ static NormArgs norm_args(const pac_block_norm *b, int64_t rows, const void *x, 
 {
     NormArgs a = {};
     a.x = x; a.o = o; a.rows = rows; a.d = b->d; a.eps = b->eps; a.inv_d = 1.f / (float)b->d;
+    a.v_a = a.v_b = a.v_c = a.v_d = -1;
     a.w_post = b->w_post; a.b_post = b->b_post; a.gate = b->gate; a.res = b->res; a.w_pre = b->w_pre; a.b_pre = b->b_pre;
     a.gate_len = b->gate ? (b->gate_len == 1 ? 1 : b->d) : 0;
     return a;
@@ -433,6 +529,8 @@ static bool norm_vec(const pac_block_norm *b, std::initializer_list<const void *
 {
     if (b->d % (b->dtype == PAC_F32 ? 4 : 8)) return false;
     for (const void *p : ps)
+        if (!n_aligned(p, 16)) return false;
+    for (const float *p : {b->w_post, b->b_post, b->gate_len > 1 ? b->gate : nullptr, b->w_pre, b->b_pre})
         if (!n_aligned(p, 16)) return false;
     return true;
 }
@@ -465,8 +563,7 @@ pac_status pac_block_norm_forward(const pac_block_norm *b, int64_t rows, const v
 int64_t pac_block_norm_workspace_bytes(const pac_block_norm *b, int64_t rows)
 {
     if (check_norm(b, rows) != PAC_OK) return -1;
-    const int64_t blocks = norm_blocks(b->d, rows < 1 ? 1 : rows, true), parts = norm_parts(b->d, rows < 1 ? 1 : rows);
-    return (16 * blocks + 4 * parts * 4 * (int64_t)b->d + 255) / 256 * 256;
+    return (norm_blocks(b->d, rows < 1 ? 1 : rows, true) * (16 + 16 * (int64_t)b->d) + 255) / 256 * 256; // two doubles, four rows of floats
 }
 
 pac_status pac_block_norm_backward(const pac_block_norm *b, int64_t rows, const void *x, const void *o, const void *dy, const void *dn,
@@ -508,9 +605,14 @@ pac_status pac_block_norm_backward(const pac_block_norm *b, int64_t rows, const 
         if (r != PAC_OK) return r;
     }
     if (!sums) return PAC_OK;
-    const NormSums u{a.cols, a.scal, (int)(rows ? norm_parts(b->d, rows) : 0), (int)blocks, b->d, a.nv, a.v_a, a.v_b, a.v_c, a.v_d, a.gate_len,
-                     b->w_post, b->b_post, b->gate, dw_post, db_post, dgate, dres, dw_pre, db_pre, b->w_post != nullptr};
-    hipLaunchKernelGGL(k_norm_sums, dim3(a.nv ? (unsigned)((b->d + 15) / 16) : 1u), dim3(256), 0, st, u);
+    const NormSums u{a.cols, a.scal, (int)blocks, b->d, a.nv, a.v_a, a.v_b, a.v_c, a.v_d, a.gate_len,
+                     b->w_post, b->b_post, b->gate, dw_post, db_post, dgate, dres, dw_pre, db_pre};
+    const dim3 gs(a.nv ? (unsigned)((b->d + 15) / 16) : 1u);
+    if (a.nv == 0) hipLaunchKernelGGL(k_norm_sums<0>, gs, dim3(512), 0, st, u);
+    else if (a.nv == 1) hipLaunchKernelGGL(k_norm_sums<1>, gs, dim3(512), 0, st, u);
+    else if (a.nv == 2) hipLaunchKernelGGL(k_norm_sums<2>, gs, dim3(512), 0, st, u);
+    else if (a.nv == 3) hipLaunchKernelGGL(k_norm_sums<3>, gs, dim3(512), 0, st, u);
+    else hipLaunchKernelGGL(k_norm_sums<4>, gs, dim3(512), 0, st, u);
     return hipGetLastError() == hipSuccess ? PAC_OK : PAC_ERR_DEVICE;
 }
 
