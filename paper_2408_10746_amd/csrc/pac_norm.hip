@@ -157,7 +157,9 @@ __device__ __forceinline__ void norm_back(float (&g)[E], const float (&h)[E], fl
 template <int TPR> constexpr int kRowsPerBlock = TPR < 512 ? 512 / TPR : 1;
 template <int TPR> constexpr int kNormThreads = TPR < 512 ? 512 : TPR;
 
-template <typename T, int VEC, int TPR, int E, bool LAYER> __global__ __launch_bounds__(kNormThreads<TPR>) void k_norm_fwd(NormArgs a)
+// HOLD: the parameters stay in registers from row to row, loaded along with the first row; else (rows past 8192, whose values fill
+// the registers) they are loaded for every row
+template <typename T, int VEC, int TPR, int E, bool LAYER, bool HOLD> __global__ __launch_bounds__(kNormThreads<TPR>) void k_norm_fwd(NormArgs a)
 {
     constexpr int RPB = kRowsPerBlock<TPR>;
     using IO = RowIO<T, VEC, TPR, E>;
@@ -174,12 +176,22 @@ template <typename T, int VEC, int TPR, int E, bool LAYER> __global__ __launch_b
     IO::fetch(rx, a.x, clamp(row0 + slot), a.d, t);
     IO::fetch(ro, po, clamp(row0 + slot), a.d, t);
     const float res = a.res ? a.res[0] : 1.f, g0 = a.gate_len == 1 ? a.gate[0] : 1.f;
+    float wo[E], bo[E], gt[E], wn[E], bn[E];
+    auto params = [&] {
+        IO::param(a.w_post, a.d, t, 1.f, wo);
+        IO::param(a.b_post, a.d, t, 0.f, bo);
+        IO::param(a.gate_len > 1 ? a.gate : nullptr, a.d, t, g0, gt);
+        IO::param(a.w_pre, a.d, t, 0.f, wn);
+        IO::param(a.b_pre, a.d, t, 0.f, bn);
+    };
+    if constexpr (HOLD) params();
     for (; row0 < a.rows; row0 += stride) {
         const bool live = row0 + slot < a.rows;
         const int64_t row = clamp(row0 + slot);
-        float y[E], o[E], p[E];
+        float y[E], o[E];
         IO::widen(rx, a.d, t, y);
         IO::widen(ro, a.d, t, o);
+        if constexpr (!HOLD) params();
         if (row0 + stride < a.rows) {
             const int64_t next = clamp(row0 + stride + slot);
             IO::fetch(rx, a.x, next, a.d, t);
@@ -188,30 +200,11 @@ template <typename T, int VEC, int TPR, int E, bool LAYER> __global__ __launch_b
         if (a.o) {
             if (a.w_post) {
                 normalise<TPR, E, IO, LAYER>(o, a, t, red, turn);
-                IO::param(a.w_post, a.d, t, 1.f, p);
-                if constexpr (LAYER) {
-                    float b[E];
-                    IO::param(a.b_post, a.d, t, 0.f, b);
 #pragma unroll
-                    for (int e = 0; e < E; ++e) o[e] = fmaf(o[e], p[e], b[e]);
-                } else if (a.b_post) {
-                    float b[E];
-                    IO::param(a.b_post, a.d, t, 0.f, b);
-#pragma unroll
-                    for (int e = 0; e < E; ++e) o[e] = fmaf(o[e], p[e], b[e]);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < E; ++e) o[e] *= p[e];
-                }
+                for (int e = 0; e < E; ++e) o[e] = fmaf(o[e], wo[e], bo[e]);
             }
-            if (a.gate_len > 1) {
-                IO::param(a.gate, a.d, t, 0.f, p);
 #pragma unroll
-                for (int e = 0; e < E; ++e) y[e] = fmaf(res, y[e], p[e] * o[e]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < E; ++e) y[e] = fmaf(res, y[e], g0 * o[e]);
-            }
+            for (int e = 0; e < E; ++e) y[e] = fmaf(res, y[e], gt[e] * o[e]);
         } else {
 #pragma unroll
             for (int e = 0; e < E; ++e) y[e] *= res;
@@ -221,18 +214,15 @@ template <typename T, int VEC, int TPR, int E, bool LAYER> __global__ __launch_b
 #pragma unroll
             for (int e = 0; e < E; ++e) y[e] = IO::in(t, e, a.d) ? y[e] : 0.f; // (a parameter has any value past the row's end)
             normalise<TPR, E, IO, LAYER>(y, a, t, red, turn);
-            IO::param(a.w_pre, a.d, t, 0.f, p);
-            float b[E];
-            IO::param(a.b_pre, a.d, t, 0.f, b);
 #pragma unroll
-            for (int e = 0; e < E; ++e) y[e] = fmaf(y[e], p[e], b[e]);
+            for (int e = 0; e < E; ++e) y[e] = fmaf(y[e], wn[e], bn[e]);
             if (live) IO::store(a.n, row, a.d, t, y);
         }
     }
 }
 
 // SHIFT: sums of g and of dn for the shifts' gradients (b_post, b_pre) are wanted too
-template <typename T, int VEC, int TPR, int E, bool LAYER, bool SHIFT>
+template <typename T, int VEC, int TPR, int E, bool LAYER, bool SHIFT, bool HOLD>
 __global__ __launch_bounds__(kNormThreads<TPR>, 4) void k_norm_bwd(NormArgs a)
 {
     constexpr int RPB = kRowsPerBlock<TPR>, W = RPB * TPR / 64;
@@ -256,6 +246,13 @@ __global__ __launch_bounds__(kNormThreads<TPR>, 4) void k_norm_bwd(NormArgs a)
     };
     fetch(clamp(row0 + slot));
     const float res = a.res ? a.res[0] : 1.f, g0 = a.gate_len == 1 ? a.gate[0] : 1.f;
+    float wo[E], bo[E], gt[E], wn[E];
+    if constexpr (HOLD) {
+        IO::param(a.w_post, a.d, t, 1.f, wo);
+        IO::param(a.b_post, a.d, t, 0.f, bo);
+        IO::param(a.gate_len > 1 ? a.gate : nullptr, a.d, t, g0, gt);
+        IO::param(a.w_pre, a.d, t, 0.f, wn);
+    }
     float ca[E], cb[E], cc[E], cd[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) ca[e] = cb[e] = cc[e] = cd[e] = 0.f;
@@ -263,7 +260,7 @@ __global__ __launch_bounds__(kNormThreads<TPR>, 4) void k_norm_bwd(NormArgs a)
     for (; row0 < a.rows; row0 += stride) {
         const bool live = row0 + slot < a.rows;
         const int64_t row = clamp(row0 + slot);
-        float x[E], oh[E], p[E], g[E], w[E];
+        float x[E], oh[E], p[E], g[E];
         IO::widen(rx, a.d, t, x);
         IO::widen(ro, a.d, t, oh);
         IO::widen(ry, a.d, t, g);
@@ -279,37 +276,26 @@ __global__ __launch_bounds__(kNormThreads<TPR>, 4) void k_norm_bwd(NormArgs a)
             for (int e = 0; e < E; ++e) p[e] = oh[e] = 0.f;
         } else if (a.w_post) {
             r_o = normalise<TPR, E, IO, LAYER>(oh, a, t, red, turn);
-            IO::param(a.w_post, a.d, t, 1.f, w);
+            if constexpr (!HOLD) IO::param(a.w_post, a.d, t, 1.f, wo), IO::param(a.b_post, a.d, t, 0.f, bo);
 #pragma unroll
-            for (int e = 0; e < E; ++e) p[e] = oh[e] * w[e];
-            if (a.b_post) {
-                IO::param(a.b_post, a.d, t, 0.f, w);
-#pragma unroll
-                for (int e = 0; e < E; ++e) p[e] = IO::in(t, e, a.d) ? p[e] + w[e] : 0.f;
-            }
+            for (int e = 0; e < E; ++e) p[e] = IO::in(t, e, a.d) ? fmaf(oh[e], wo[e], bo[e]) : 0.f;
         } else {
 #pragma unroll
             for (int e = 0; e < E; ++e) p[e] = oh[e];
         }
         if (a.w_pre) {
             float yh[E];
-            if (a.gate_len > 1) {
-                IO::param(a.gate, a.d, t, 0.f, w);
+            if constexpr (!HOLD) IO::param(a.gate_len > 1 ? a.gate : nullptr, a.d, t, g0, gt), IO::param(a.w_pre, a.d, t, 0.f, wn);
 #pragma unroll
-                for (int e = 0; e < E; ++e) yh[e] = fmaf(res, x[e], w[e] * p[e]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < E; ++e) yh[e] = fmaf(res, x[e], g0 * p[e]);
-            }
+            for (int e = 0; e < E; ++e) yh[e] = fmaf(res, x[e], gt[e] * p[e]);
             const float r_y = normalise<TPR, E, IO, LAYER>(yh, a, t, red, turn);
-            IO::param(a.w_pre, a.d, t, 0.f, w);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 if (live) {
                     cc[e] = fmaf(dn[e], yh[e], cc[e]);
                     if constexpr (SHIFT) cd[e] += dn[e];
                 }
-                dn[e] *= w[e];
+                dn[e] *= wn[e];
             }
             norm_back<TPR, E, IO, LAYER>(dn, yh, r_y, a, red, turn);
 #pragma unroll
@@ -332,18 +318,10 @@ __global__ __launch_bounds__(kNormThreads<TPR>, 4) void k_norm_bwd(NormArgs a)
             IO::store(a.dx, row, a.d, t, x);
         }
         if (a.d_o) {
-            if (a.gate_len > 1) {
-                IO::param(a.gate, a.d, t, 0.f, w);
+            if constexpr (!HOLD) IO::param(a.gate_len > 1 ? a.gate : nullptr, a.d, t, g0, gt), IO::param(a.w_post, a.d, t, 1.f, wo);
 #pragma unroll
-                for (int e = 0; e < E; ++e) g[e] *= w[e];
-            } else {
-#pragma unroll
-                for (int e = 0; e < E; ++e) g[e] *= g0;
-            }
+            for (int e = 0; e < E; ++e) g[e] *= gt[e] * wo[e];
             if (a.w_post) {
-                IO::param(a.w_post, a.d, t, 1.f, w);
-#pragma unroll
-                for (int e = 0; e < E; ++e) g[e] *= w[e];
                 norm_back<TPR, E, IO, LAYER>(g, oh, r_o, a, red, turn);
             }
             if (live) IO::store(a.d_o, row, a.d, t, g);
@@ -471,45 +449,64 @@ static pac_status check_norm(const pac_block_norm *b, int64_t rows)
     return PAC_OK;
 }
 
-// Threads a row: as few as hold it at eight values each, so that short rows take one wavefront and no barrier; rows past 8192 take
-// sixteen values a thread.
-static int threads_for(int d) { return d <= 512 ? 64 : d <= 1024 ? 128 : d <= 2048 ? 256 : d <= 4096 ? 512 : 1024; }
+// Values a thread and threads a row: as few threads as hold it, so that short rows take one wavefront and no barrier.
+struct NormForm { int e, tpr; };
+static NormForm norm_form(int d, bool backward)
+{
+    const int e = d > 8192 ? 16 : d > 4096 || !backward ? 8 : 4;
+    int tpr = 64;
+    while (tpr * e < d) tpr *= 2;
+    return {e, tpr};
+}
 
 static int64_t norm_blocks(int d, int64_t rows, bool backward)
 {
-    const int tpr = threads_for(d), rpb = tpr < 512 ? 512 / tpr : 1;
+    const int tpr = norm_form(d, backward).tpr, rpb = tpr < 512 ? 512 / tpr : 1;
     const int64_t want = (rows + rpb - 1) / rpb, most = backward ? (tpr == 1024 ? 256 : 512) : 1024;
     return want < most ? want : most;
 }
 
-template <typename T, int VEC, bool LAYER> static void launch_norm(const NormArgs &a, bool backward, hipStream_t st)
+template <typename T, int VEC, int TPR, int E, bool LAYER> static void launch_fwd(const NormArgs &a, dim3 g, hipStream_t st)
 {
-    const int tpr = threads_for(a.d);
-    const dim3 g((unsigned)norm_blocks(a.d, a.rows, backward)), b(tpr < 512 ? 512 : tpr);
-    const bool shift = a.v_b >= 0 || a.v_d >= 0;
-#define PAC_NORM_LAUNCH(TPR, E)                                                                                                \
-    {                                                                                                                          \
-        if (!backward) hipLaunchKernelGGL((k_norm_fwd<T, VEC, TPR, E, LAYER>), g, b, 0, st, a);                                \
-        else if (shift) hipLaunchKernelGGL((k_norm_bwd<T, VEC, TPR, E, LAYER, true>), g, b, 0, st, a);                         \
-        else hipLaunchKernelGGL((k_norm_bwd<T, VEC, TPR, E, LAYER, false>), g, b, 0, st, a);                                   \
-    }
-    if (tpr == 64) PAC_NORM_LAUNCH(64, 8)
-    else if (tpr == 128) PAC_NORM_LAUNCH(128, 8)
-    else if (tpr == 256) PAC_NORM_LAUNCH(256, 8)
-    else if (tpr == 512) PAC_NORM_LAUNCH(512, 8)
-    else if (a.d <= 8192) PAC_NORM_LAUNCH(1024, 8)
-    else PAC_NORM_LAUNCH(1024, 16)
-#undef PAC_NORM_LAUNCH
+    hipLaunchKernelGGL((k_norm_fwd<T, VEC, TPR, E, LAYER, (E < 16)>), g, dim3(kNormThreads<TPR>), 0, st, a);
+}
+template <typename T, int VEC, int TPR, int E, bool LAYER> static void launch_bwd(const NormArgs &a, dim3 g, hipStream_t st)
+{
+    if (a.v_b >= 0 || a.v_d >= 0) hipLaunchKernelGGL((k_norm_bwd<T, VEC, TPR, E, LAYER, true, (E < 8)>), g, dim3(kNormThreads<TPR>), 0, st, a);
+    else hipLaunchKernelGGL((k_norm_bwd<T, VEC, TPR, E, LAYER, false, (E < 8)>), g, dim3(kNormThreads<TPR>), 0, st, a);
+}
+
+template <typename T, bool WIDE, bool LAYER> static void launch_norm(const NormArgs &a, bool backward, hipStream_t st)
+{
+    const NormForm f = norm_form(a.d, backward);
+    const dim3 g((unsigned)norm_blocks(a.d, a.rows, backward));
+    constexpr int V8 = WIDE ? 16 / (int)sizeof(T) : 1, V4 = WIDE ? 4 : 1;
+    if (backward) {
+        if (f.e == 4) {
+            if (f.tpr == 64) launch_bwd<T, V4, 64, 4, LAYER>(a, g, st);
+            else if (f.tpr == 128) launch_bwd<T, V4, 128, 4, LAYER>(a, g, st);
+            else if (f.tpr == 256) launch_bwd<T, V4, 256, 4, LAYER>(a, g, st);
+            else if (f.tpr == 512) launch_bwd<T, V4, 512, 4, LAYER>(a, g, st);
+            else launch_bwd<T, V4, 1024, 4, LAYER>(a, g, st);
+        } else if (f.e == 8) launch_bwd<T, V8, 1024, 8, LAYER>(a, g, st);
+        else launch_bwd<T, V8, 1024, 16, LAYER>(a, g, st);
+    } else if (f.e == 8) {
+        if (f.tpr == 64) launch_fwd<T, V8, 64, 8, LAYER>(a, g, st);
+        else if (f.tpr == 128) launch_fwd<T, V8, 128, 8, LAYER>(a, g, st);
+        else if (f.tpr == 256) launch_fwd<T, V8, 256, 8, LAYER>(a, g, st);
+        else if (f.tpr == 512) launch_fwd<T, V8, 512, 8, LAYER>(a, g, st);
+        else launch_fwd<T, V8, 1024, 8, LAYER>(a, g, st);
+    } else launch_fwd<T, V8, 1024, 16, LAYER>(a, g, st);
 }
 
 static pac_status run_norm(const pac_block_norm *b, const NormArgs &a, bool vec, bool backward, hipStream_t st)
 {
     if (b->dtype == PAC_F32) {
-        if (vec) b->layer ? launch_norm<float, 4, true>(a, backward, st) : launch_norm<float, 4, false>(a, backward, st);
-        else b->layer ? launch_norm<float, 1, true>(a, backward, st) : launch_norm<float, 1, false>(a, backward, st);
+        if (vec) b->layer ? launch_norm<float, true, true>(a, backward, st) : launch_norm<float, true, false>(a, backward, st);
+        else b->layer ? launch_norm<float, false, true>(a, backward, st) : launch_norm<float, false, false>(a, backward, st);
     } else {
-        if (vec) b->layer ? launch_norm<bf16_t, 8, true>(a, backward, st) : launch_norm<bf16_t, 8, false>(a, backward, st);
-        else b->layer ? launch_norm<bf16_t, 1, true>(a, backward, st) : launch_norm<bf16_t, 1, false>(a, backward, st);
+        if (vec) b->layer ? launch_norm<bf16_t, true, true>(a, backward, st) : launch_norm<bf16_t, true, false>(a, backward, st);
+        else b->layer ? launch_norm<bf16_t, false, true>(a, backward, st) : launch_norm<bf16_t, false, false>(a, backward, st);
     }
     return hipGetLastError() == hipSuccess ? PAC_OK : PAC_ERR_DEVICE;
 }
