@@ -213,15 +213,17 @@ def _kind(t) -> int:
 def _matrix(t, name: str, shape=None, dtype=None, device=None):
     """The row stride of a device matrix whose columns are neighbours (the launch takes addresses alone, so what they stand
     for is checked here)."""
-    if t.dim() != 2 or t.device.type != "cuda" or (device is not None and t.device != device):
+    have, dev = t.shape, t.device
+    if len(have) != 2 or dev.type != "cuda" or (device is not None and dev != device):
         raise ValueError(f"{name}: a matrix on the device is wanted")
-    if shape is not None and tuple(t.shape) != shape:
-        raise ValueError(f"{name}: shape {shape} is wanted, not {tuple(t.shape)}")
+    if shape is not None and have != shape:
+        raise ValueError(f"{name}: shape {shape} is wanted, not {tuple(have)}")
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{name}: {dtype} is wanted, not {t.dtype}")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    row, col = t.stride()
+    if col != 1 and have[1] > 1:
         raise ValueError(f"{name}: neighbouring columns are wanted")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    return row if have[0] > 1 else max(row, have[1])
 
 
 def _stored(codes, scales, cols: int, rows=None, device=None):
@@ -245,8 +247,18 @@ def _padded_stride(t, name: str, cols: int, device):
     return stride
 
 
-def _on(device) -> int:
-    return int(torch.cuda.current_stream(device).cuda_stream)
+def _launch(device, call, *args) -> None:
+    """call(*args, the device's current stream), with that device current (switching costs more than looking)."""
+    i = device.index
+    if torch.cuda.current_device() == i:
+        call(*args, torch._C._cuda_getCurrentRawStream(i))
+    else:
+        with torch.cuda.device(i):
+            call(*args, torch._C._cuda_getCurrentRawStream(i))
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
 
 
 def mx4_empty(rows: int, cols: int, device="cuda:0"):
@@ -259,17 +271,15 @@ def mx4_quantize(x, codes, scales) -> None:
     """x (bf16 or fp32, any row stride) into the stored form."""
     stride = _matrix(x, "x")
     _stored(codes, scales, x.shape[1], x.shape[0], x.device)
-    with torch.cuda.device(x.device):
-        pb.pac_mx4_quantize(x.data_ptr(), _kind(x), x.shape[0], x.shape[1], stride, codes.data_ptr(), scales.data_ptr(), _on(x.device))
+    _launch(x.device, pb.pac_mx4_quantize, x.data_ptr(), _kind(x), x.shape[0], x.shape[1], stride, codes.data_ptr(), scales.data_ptr())
 
 
 def mx4_dequantize(codes, scales, out) -> None:
     """The values a stored matrix stands for, into out (bf16 or fp32, both exact)."""
     stride = _matrix(out, "out")
     _stored(codes, scales, out.shape[1], out.shape[0], out.device)
-    with torch.cuda.device(out.device):
-        pb.pac_mx4_dequantize(codes.data_ptr(), scales.data_ptr(), out.shape[0], out.shape[1], out.data_ptr(), _kind(out), stride,
-                              _on(out.device))
+    _launch(out.device, pb.pac_mx4_dequantize, codes.data_ptr(), scales.data_ptr(), out.shape[0], out.shape[1], out.data_ptr(), _kind(out),
+            stride)
 
 
 class Mx4Linear:
@@ -296,27 +306,24 @@ class Mx4Linear:
         M = x.shape[0]
         sy = _matrix(y, "y", (M, self.N), None, self.dev)
         act = pb.PAC_MX4_ACT_GELU if gelu else pb.PAC_MX4_ACT_NONE
-        with torch.cuda.device(self.dev):
-            st = _on(self.dev)
-            if x4:
-                sx = _matrix(x, "x", (M, self.K), None, self.dev)
-                # x in the stored form lives for this call, on this stream: codes (whole multiples of 128 bytes), then scales
-                c = M * pb.pac_mx4_code_pitch(self.K)
-                buf = torch.empty(c + M * pb.pac_mx4_scale_pitch(self.K), dtype=torch.uint8, device=self.dev)
-                c, s = buf.data_ptr(), buf.data_ptr() + c
-                pb.pac_mx4_quantize(x.data_ptr(), _kind(x), M, self.K, sx, c, s, st)
-                pb.pac_mx4_linear_x4(c, s, M, self.K, *self._w, self.N, self._b, act, y.data_ptr(), _kind(y), sy, st)
-            else:
-                sx = _padded_stride(x, "x", self.K, self.dev)
-                pb.pac_mx4_linear(x.data_ptr(), M, self.K, sx, *self._w, self.N, self._b, act, y.data_ptr(), _kind(y), sy, st)
+        if x4:
+            sx = _matrix(x, "x", (M, self.K), None, self.dev)
+            # x in the stored form lives for this call, on this stream: codes (whole multiples of 128 bytes), then scales
+            c = M * self.codes.shape[1]
+            buf = torch.empty(c + M * self.scales.shape[1], dtype=torch.uint8, device=self.dev)
+            c, s = buf.data_ptr(), buf.data_ptr() + c
+            _launch(self.dev, pb.pac_mx4_quantize, x.data_ptr(), _kind(x), M, self.K, sx, c, s)
+            _launch(self.dev, pb.pac_mx4_linear_x4, c, s, M, self.K, *self._w, self.N, self._b, act, y.data_ptr(), _kind(y), sy)
+        else:
+            sx = _padded_stride(x, "x", self.K, self.dev)
+            _launch(self.dev, pb.pac_mx4_linear, x.data_ptr(), M, self.K, sx, *self._w, self.N, self._b, act, y.data_ptr(), _kind(y), sy)
 
     def input_grad(self, dy, dx) -> None:
         """dy [M][N] bf16, rows on 16 bytes; dx [M][K] bf16 or fp32."""
         M = dy.shape[0]
         sdy = _padded_stride(dy, "dy", self.N, self.dev)
         sdx = _matrix(dx, "dx", (M, self.K), None, self.dev)
-        with torch.cuda.device(self.dev):
-            pb.pac_mx4_linear_dx(dy.data_ptr(), M, self.N, sdy, *self._w, self.K, dx.data_ptr(), _kind(dx), sdx, _on(self.dev))
+        _launch(self.dev, pb.pac_mx4_linear_dx, dy.data_ptr(), M, self.N, sdy, *self._w, self.K, dx.data_ptr(), _kind(dx), sdx)
 
 
 class BlockNorm:
@@ -336,28 +343,22 @@ class BlockNorm:
             if self.dev not in (None, p.device):
                 raise ValueError(f"{name}: on another device than the parameters before it")
             self.dev = p.device
-        ptr = lambda p: None if p is None else p.data_ptr()  # noqa: E731
         self._b = {kind: pb.pac_block_norm(d, kind, int(layer), 0 if gate is None else gate.shape[0], eps,
-                                           *(ptr(self.params[k]) for k in ("w_post", "b_post", "gate", "res", "w_pre", "b_pre")))
+                                           *(_ptr(self.params[k]) for k in ("w_post", "b_post", "gate", "res", "w_pre", "b_pre")))
                    for kind in (pb.PAC_BF16, pb.PAC_F32)}
 
     def _rows(self, x, *others):
-        if self.dev is not None and x.device != self.dev:
-            raise ValueError("states: on the parameters' device")
-        for t in (x,) + others:
-            if t is None:
-                continue
-            if t.dim() != 2 or t.shape != x.shape or t.shape[1] != self.d or t.dtype != x.dtype or t.device != x.device or not t.is_contiguous():
+        shape, dtype, dev = x.shape, x.dtype, x.device
+        if len(shape) != 2 or shape[1] != self.d or dev.type != "cuda" or not x.is_contiguous() or self.dev not in (None, dev):
+            raise ValueError(f"states: dense, [rows][{self.d}], on the parameters' device")
+        for t in others:
+            if t is not None and (t.shape != shape or t.dtype != dtype or t.device != dev or not t.is_contiguous()):
                 raise ValueError(f"states: dense, [rows][{self.d}], of one type, on one device")
-        if x.device.type != "cuda":
-            raise ValueError("states: on the device")
-        return x.shape[0]
+        return shape[0]
 
     def forward(self, x, o=None, y=None, n=None) -> None:
         rows = self._rows(x, o, y, n)
-        ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-        with torch.cuda.device(x.device):
-            pb.pac_block_norm_forward(self._b[_kind(x)], rows, x.data_ptr(), ptr(o), ptr(y), ptr(n), _on(x.device))
+        _launch(x.device, pb.pac_block_norm_forward, self._b[_kind(x)], rows, x.data_ptr(), _ptr(o), _ptr(y), _ptr(n))
 
     def backward(self, x, o, dy, dn, dx=None, do=None, dparams=None) -> None:
         """Gradients; dparams: {name: float32 tensor like the parameter} for those that are wanted."""
@@ -370,8 +371,5 @@ class BlockNorm:
         b = self._b[_kind(x)]
         need = pb.pac_block_norm_workspace_bytes(b, rows) if dparams else 0
         ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
-        ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-        with torch.cuda.device(x.device):
-            pb.pac_block_norm_backward(b, rows, x.data_ptr(), ptr(o), ptr(dy), ptr(dn), ptr(dx), ptr(do),
-                                       *(ptr(dparams.get(k)) for k in ("w_post", "b_post", "gate", "res", "w_pre", "b_pre")),
-                                       ptr(ws), need, _on(x.device))
+        _launch(x.device, pb.pac_block_norm_backward, b, rows, x.data_ptr(), _ptr(o), _ptr(dy), _ptr(dn), _ptr(dx), _ptr(do),
+                *(_ptr(dparams.get(k)) for k in ("w_post", "b_post", "gate", "res", "w_pre", "b_pre")), _ptr(ws), need)
