@@ -345,7 +345,8 @@ template <int RM, int NW> __global__ __launch_bounds__(64 * NW) void k_mx4_dx_ro
 // the 4-bit codes take a quarter of the space and of the LDS reads that bf16 would, and become bf16 in registers, eight a
 // conversion group, between the matrix instructions of the piece before.  With x stored too both sides go to the scaled matrix
 // instructions as they lie.  A lane (i, g) owns row i and, of each step, the blocks of its half g: one 16-byte read is a block of
-// codes, and a lane has one scale a block.  Scales come eight bytes a row and 256 columns straight into registers, a step ahead.
+// codes, and a lane has one scale a block.  Scales, eight bytes a row and 256 columns, come the same way into a ring of their own:
+// loaded into registers they make the compiler, which does not count the transfers, wait for all of these at every use.
 // Fragment i of subtile y stands for column WTN i + y of the wavefront's, so that a lane ends up with WTN neighbouring columns.
 // ---------------------------------------------------------------------------
 template <bool X4_, int WM_, int WN_, int WTM_, int WTN_, int STAGES_> struct Mx4Tile {
@@ -355,9 +356,18 @@ template <bool X4_, int WM_, int WN_, int WTM_, int WTN_, int STAGES_> struct Mx
     static constexpr int BK = X4 ? 128 : 64, PER = 256 / BK;   // columns a step, steps a group of 256
     static constexpr int AB = X4 ? 64 : 128, BB = X4 ? 64 : 32; // bytes of a row a step
     static constexpr int AI = TM * AB / 1024, TOTAL = AI + TN * BB / 1024, NI = (TOTAL + NW - 1) / NW;
-    static constexpr int STAGE_BYTES = TM * AB + TN * BB, LDS_BYTES = STAGES * STAGE_BYTES;
-    static_assert(STAGES >= 2 && NI * (STAGES - 1) < 60, "transfers in flight must fit the counter");
+    static constexpr int STAGE_BYTES = TM * AB + TN * BB;
+    // scales: rows of W, then of x; rings deep enough that no group of 256 columns in use is written over
+    static constexpr int SR = TN + (X4 ? TM : 0), STOTAL = SR / 32, SI = (STOTAL + NW - 1) / NW, RING = (STAGES - 2) / PER + 2;
+    static constexpr int LDS_BYTES = STAGES * STAGE_BYTES + RING * SR * 8;
+    static_assert(STAGES >= 2 && (NI + SI) * (STAGES - 1) < 60, "transfers in flight must fit the counter");
 };
+// 4 bytes a lane from global memory into LDS, as dma16_at
+__device__ __forceinline__ void dma4_at(const void *g, uint32_t lds_wave_address)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
+                 : : "s"(__builtin_amdgcn_readfirstlane(lds_wave_address)), "v"(g) : "memory", "m0");
+}
 // chunk swizzle of rows of 128, 64 and 32 bytes: the 16 rows that one pass of a 16-byte read covers meet every bank once
 template <int BYTES> __device__ __forceinline__ int mx4_swz(int row)
 {
@@ -404,32 +414,32 @@ template <class TL> __global__ __launch_bounds__(64 * TL::NW) void k_mx4_tiles(M
             glim[q] = 0x7fffffffu;
         }
     }
+    // ... and of a group's scales: two lanes a row
+    const uint8_t *sp[TL::SI];
+#pragma unroll
+    for (int q = 0; q < TL::SI; ++q) {
+        const int row = min(wave + TL::NW * q, TL::STOTAL - 1) * 32 + lane / 2;
+        if (row < TL::TN) {
+            const int w = row / (32 * WTN), y = row / 32 % WTN;
+            sp[q] = a.ws + min(n0 + w * 32 * WTN + (row & 31) * WTN + y, a.N - 1) * a.sp + 4 * (lane & 1);
+        } else sp[q] = a.xs + min(m0 + row - TL::TN, a.M - 1) * a.sp + 4 * (lane & 1);
+    }
+    const uint32_t lds0 = lds_address(lds), ring0 = lds0 + TL::STAGES * TL::STAGE_BYTES;
     auto issue = [&](int slot, int step) {
         const uint32_t s = min(step, nsteps - 1); // past the end: the last step again, never used
+        if (step % TL::PER == 0) {
+            const int grp = min(step / TL::PER, ngroups - 1);
+#pragma unroll
+            for (int q = 0; q < TL::SI; ++q)
+                dma4_at(sp[q] + 8 * grp, ring0 + step / TL::PER % TL::RING * (TL::SR * 8) + min(wave + TL::NW * q, TL::STOTAL - 1) * 256);
+        }
 #pragma unroll
         for (int q = 0; q < TL::NI; ++q) {
             const int ii = min(wave + TL::NW * q, TL::TOTAL - 1);
             const uint32_t by = s * (ii < TL::AI ? TL::AB : TL::BB);
-            dma16_at(gp[q] + min(by + goff[q], glim[q]), lds_address(lds) + slot * TL::STAGE_BYTES + ii * 1024);
+            dma16_at(gp[q] + min(by + goff[q], glim[q]), lds0 + slot * TL::STAGE_BYTES + ii * 1024);
         }
     };
-    // scales: eight bytes a row and 256 columns; this lane's half shifted to the bottom
-    const uint8_t *bs[WTN], *as[TL::X4 ? WTM : 1];
-#pragma unroll
-    for (int y = 0; y < WTN; ++y) bs[y] = a.ws + min(n0 + wn * 32 * WTN + i * WTN + y, a.N - 1) * a.sp;
-    if constexpr (TL::X4)
-#pragma unroll
-        for (int x = 0; x < WTM; ++x) as[x] = a.xs + min(m0 + (wm * WTM + x) * 32 + i, a.M - 1) * a.sp;
-    uint64_t bsn[WTN], bsc[WTN], asn[TL::X4 ? WTM : 1], asc[TL::X4 ? WTM : 1];
-    auto scales = [&](int group) {
-        const int o = 8 * min(group, ngroups - 1);
-#pragma unroll
-        for (int y = 0; y < WTN; ++y) bsn[y] = *reinterpret_cast<const uint64_t *>(bs[y] + o);
-        if constexpr (TL::X4)
-#pragma unroll
-            for (int x = 0; x < WTM; ++x) asn[x] = *reinterpret_cast<const uint64_t *>(as[x] + o);
-    };
-    scales(0);
 #pragma unroll
     for (int s = 0; s < TL::STAGES - 1; ++s) issue(s, s);
 
@@ -454,20 +464,23 @@ template <class TL> __global__ __launch_bounds__(64 * TL::NW) void k_mx4_tiles(M
         bsw[y] = mx4_swz<TL::BB>(row);
     }
     int slot = 0;
+    uint64_t bsc[WTN], asc[TL::X4 ? WTM : 1]; // this lane's half of a group's scales, shifted to the bottom
     for (int grp = 0; grp < ngroups; ++grp) {
-        const int half = TL::X4 ? 16 * g : 8 * g;
-#pragma unroll
-        for (int y = 0; y < WTN; ++y) bsc[y] = bsn[y] >> half;
-        if constexpr (TL::X4)
-#pragma unroll
-            for (int x = 0; x < WTM; ++x) asc[x] = asn[x] >> half;
-        scales(grp + 1);
 #pragma unroll
         for (int u = 0; u < TL::PER; ++u) {
             const int st = grp * TL::PER + u;
             if (st >= nsteps) break;
-            wait_vm<TL::NI * (TL::STAGES - 2)>(); // this wavefront's share of the stage has landed
+            wait_vm<TL::NI * (TL::STAGES - 2)>(); // this wavefront's share of the stage, and of its scales, has landed
             __syncthreads();                       // ... and everybody else's; the stage before is free
+            if (u == 0) {
+                const char *sc = lds + TL::STAGES * TL::STAGE_BYTES + grp % TL::RING * (TL::SR * 8);
+                const int half = TL::X4 ? 16 * g : 8 * g;
+#pragma unroll
+                for (int y = 0; y < WTN; ++y) bsc[y] = *reinterpret_cast<const uint64_t *>(sc + ((wn * WTN + y) * 32 + i) * 8) >> half;
+                if constexpr (TL::X4)
+#pragma unroll
+                    for (int x = 0; x < WTM; ++x) asc[x] = *reinterpret_cast<const uint64_t *>(sc + (TL::TN + (wm * WTM + x) * 32 + i) * 8) >> half;
+            }
             const char *sb = lds + slot * TL::STAGE_BYTES;
             issue(slot == 0 ? TL::STAGES - 1 : slot - 1, st + TL::STAGES - 1);
             if constexpr (TL::X4) {
