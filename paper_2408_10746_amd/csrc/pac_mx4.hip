@@ -358,9 +358,9 @@ template <bool X4_, int WM_, int WN_, int WTM_, int WTN_, int STAGES_> struct Mx
     static constexpr int AI = TM * AB / 1024, TOTAL = AI + TN * BB / 1024, NI = (TOTAL + NW - 1) / NW;
     static constexpr int STAGE_BYTES = TM * AB + TN * BB;
     // scales: rows of W, then of x; rings deep enough that no group of 256 columns in use is written over
-    static constexpr int SR = TN + (X4 ? TM : 0), STOTAL = SR / 32, SI = (STOTAL + NW - 1) / NW, RING = (STAGES - 2) / PER + 2;
+    static constexpr int SR = TN + (X4 ? TM : 0), STOTAL = SR / 32, SI = (STOTAL + NW - 1) / NW, RING = (STAGES - 1) / PER + 2;
     static constexpr int LDS_BYTES = STAGES * STAGE_BYTES + RING * SR * 8;
-    static_assert(STAGES >= 2 && (NI + SI) * (STAGES - 1) < 60, "transfers in flight must fit the counter");
+    static_assert(STAGES >= 2 && (NI + SI) * STAGES < 60, "transfers in flight must fit the counter");
 };
 // 4 bytes a lane from global memory into LDS, as dma16_at
 __device__ __forceinline__ void dma4_at(const void *g, uint32_t lds_wave_address)
@@ -441,7 +441,7 @@ template <class TL> __global__ __launch_bounds__(64 * TL::NW) void k_mx4_tiles(M
         }
     };
 #pragma unroll
-    for (int s = 0; s < TL::STAGES - 1; ++s) issue(s, s);
+    for (int s = 0; s < TL::STAGES; ++s) issue(s, s);
 
     f32x16 acc[WTM][WTN];
 #pragma unroll
@@ -463,74 +463,94 @@ template <class TL> __global__ __launch_bounds__(64 * TL::NW) void k_mx4_tiles(M
         brow[y] = TL::TM * TL::AB + row * TL::BB;
         bsw[y] = mx4_swz<TL::BB>(row);
     }
-    int slot = 0;
+    // A step is walked in its J sub-steps, each reading the next one's fragments before its own matrix instructions.  The last
+    // sub-step's come after the barrier that hands over the next stage, so that they cover the latency of that stage's first reads.
+    constexpr int J = TL::X4 ? 2 : 4;
     uint64_t bsc[WTN], asc[TL::X4 ? WTM : 1]; // this lane's half of a group's scales, shifted to the bottom
+    u32x4 af[2][WTM], bf[2][WTN];             // fragments; for bf16 rows bf[0] holds the step's codes
+    auto read_scales = [&](int grp, uint64_t (&bs)[WTN], uint64_t (&as)[TL::X4 ? WTM : 1]) {
+        const char *sc = lds + TL::STAGES * TL::STAGE_BYTES + grp % TL::RING * (TL::SR * 8);
+        const int half = TL::X4 ? 16 * g : 8 * g;
+#pragma unroll
+        for (int y = 0; y < WTN; ++y) bs[y] = *reinterpret_cast<const uint64_t *>(sc + ((wn * WTN + y) * 32 + i) * 8) >> half;
+        if constexpr (TL::X4)
+#pragma unroll
+            for (int x = 0; x < WTM; ++x) as[x] = *reinterpret_cast<const uint64_t *>(sc + (TL::TN + (wm * WTM + x) * 32 + i) * 8) >> half;
+    };
+    auto read_a = [&](const char *sb, int j) {
+#pragma unroll
+        for (int x = 0; x < WTM; ++x) af[j & 1][x] = *reinterpret_cast<const u32x4 *>(sb + arow[x] + (((J * g + j) ^ asw[x]) << 4));
+    };
+    auto read_b = [&](const char *sb, int j, u32x4 (&to)[WTN]) {
+#pragma unroll
+        for (int y = 0; y < WTN; ++y) to[y] = *reinterpret_cast<const u32x4 *>(sb + brow[y] + (((TL::X4 ? J * g + j : g) ^ bsw[y]) << 4));
+    };
+    wait_vm<TL::NI * (TL::STAGES - 1)>();
+    __syncthreads();
+    read_scales(0, bsc, asc);
+    read_a(lds, 0);
+    read_b(lds, 0, bf[0]);
+    int slot = 0;
     for (int grp = 0; grp < ngroups; ++grp) {
 #pragma unroll
         for (int u = 0; u < TL::PER; ++u) {
             const int st = grp * TL::PER + u;
             if (st >= nsteps) break;
-            wait_vm<TL::NI * (TL::STAGES - 2)>(); // this wavefront's share of the stage, and of its scales, has landed
-            __syncthreads();                       // ... and everybody else's; the stage before is free
-            if (u == 0) {
-                const char *sc = lds + TL::STAGES * TL::STAGE_BYTES + grp % TL::RING * (TL::SR * 8);
-                const int half = TL::X4 ? 16 * g : 8 * g;
-#pragma unroll
-                for (int y = 0; y < WTN; ++y) bsc[y] = *reinterpret_cast<const uint64_t *>(sc + ((wn * WTN + y) * 32 + i) * 8) >> half;
-                if constexpr (TL::X4)
-#pragma unroll
-                    for (int x = 0; x < WTM; ++x) asc[x] = *reinterpret_cast<const uint64_t *>(sc + (TL::TN + (wm * WTM + x) * 32 + i) * 8) >> half;
-            }
             const char *sb = lds + slot * TL::STAGE_BYTES;
-            issue(slot == 0 ? TL::STAGES - 1 : slot - 1, st + TL::STAGES - 1);
-            if constexpr (TL::X4) {
-                u32x4 af[2][WTM], bf[2][WTN];
+            uint64_t bsn[WTN], asn[TL::X4 ? WTM : 1];
+            u32x4 bn[WTN];
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-#pragma unroll
-                    for (int y = 0; y < WTN; ++y) bf[j][y] = *reinterpret_cast<const u32x4 *>(sb + brow[y] + (((2 * g + j) ^ bsw[y]) << 4));
-#pragma unroll
-                    for (int x = 0; x < WTM; ++x) af[j][x] = *reinterpret_cast<const u32x4 *>(sb + arow[x] + (((2 * g + j) ^ asw[x]) << 4));
+            for (int j = 0; j < J; ++j) {
+                if (j + 1 < J) {
+                    read_a(sb, j + 1);
+                    if constexpr (TL::X4) read_b(sb, j + 1, bf[(j + 1) & 1]);
+                } else {
+                    wait_vm<TL::NI * (TL::STAGES - 2)>(); // this wavefront's share of the next stage, and of its scales, has landed
+                    __syncthreads();                       // ... and everybody else's; this stage has been read
+                    const int next = slot + 1 == TL::STAGES ? 0 : slot + 1;
+                    const char *nb = lds + next * TL::STAGE_BYTES;
+                    read_a(nb, 0);
+                    read_b(nb, 0, bn);
+                    if (u == TL::PER - 1) read_scales(grp + 1, bsn, asn);
+                    issue(slot, st + TL::STAGES);
+                    slot = next;
                 }
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
+                __builtin_amdgcn_sched_barrier(0); // the reads stay ahead of the matrix instructions
+                if constexpr (TL::X4) {
 #pragma unroll
                     for (int x = 0; x < WTM; ++x)
 #pragma unroll
                         for (int y = 0; y < WTN; ++y) {
-                            const i32x8 p = {(int)af[j][x][0], (int)af[j][x][1], (int)af[j][x][2], (int)af[j][x][3], 0, 0, 0, 0};
-                            const i32x8 q = {(int)bf[j][y][0], (int)bf[j][y][1], (int)bf[j][y][2], (int)bf[j][y][3], 0, 0, 0, 0};
+                            const u32x4 &pa = af[j & 1][x], &pb = bf[j & 1][y];
+                            const i32x8 p = {(int)pa[0], (int)pa[1], (int)pa[2], (int)pa[3], 0, 0, 0, 0};
+                            const i32x8 q = {(int)pb[0], (int)pb[1], (int)pb[2], (int)pb[3], 0, 0, 0, 0};
                             const int sa = (int)(asc[x] >> (32 * u)), sc = (int)(bsc[y] >> (32 * u));
                             if (j == 0) acc[x][y] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(p, q, acc[x][y], 4, 4, 0, sa, 0, sc);
                             else acc[x][y] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(p, q, acc[x][y], 4, 4, 1, sa, 1, sc);
                         }
-            } else {
-                const bool tail = st * 64 + 64 > a.K;
-                u32x4 bw[WTN], af[2][WTM];
+                } else {
+                    bf16x8 w[WTN];
 #pragma unroll
-                for (int y = 0; y < WTN; ++y) bw[y] = *reinterpret_cast<const u32x4 *>(sb + brow[y] + ((g ^ bsw[y]) << 4));
-                auto rd = [&](int j) {
-#pragma unroll
-                    for (int x = 0; x < WTM; ++x) af[j & 1][x] = *reinterpret_cast<const u32x4 *>(sb + arow[x] + (((4 * g + j) ^ asw[x]) << 4));
-                };
-                rd(0);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (j < 3) rd(j + 1);
-                    bf16x8 bf[WTN];
-#pragma unroll
-                    for (int y = 0; y < WTN; ++y) bf[y] = mx4_bf16(bw[y][j], mx4_scale((uint32_t)(bsc[y] >> (16 * u)) & 255u));
-                    if (tail)
+                    for (int y = 0; y < WTN; ++y) w[y] = mx4_bf16(bf[0][y][j], mx4_scale((uint32_t)(bsc[y] >> (16 * u)) & 255u));
+                    if (st * 64 + 64 > a.K)
 #pragma unroll
                         for (int x = 0; x < WTM; ++x) af[j & 1][x] = mx4_keep(af[j & 1][x], a.K - (st * 64 + 32 * g + 8 * j));
 #pragma unroll
                     for (int x = 0; x < WTM; ++x)
 #pragma unroll
                         for (int y = 0; y < WTN; ++y)
-                            acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<bf16x8 *>(&af[j & 1][x]), bf[y], acc[x][y], 0, 0, 0);
+                            acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<bf16x8 *>(&af[j & 1][x]), w[y], acc[x][y], 0, 0, 0);
                 }
             }
-            slot = slot + 1 == TL::STAGES ? 0 : slot + 1;
+#pragma unroll
+            for (int y = 0; y < WTN; ++y) bf[0][y] = bn[y];
+            if (u == TL::PER - 1) {
+#pragma unroll
+                for (int y = 0; y < WTN; ++y) bsc[y] = bsn[y];
+                if constexpr (TL::X4)
+#pragma unroll
+                    for (int x = 0; x < WTM; ++x) asc[x] = asn[x];
+            }
         }
     }
     wait_vm<0>(); // the repeated transfers of the last steps end before the workgroup's LDS does
