@@ -425,20 +425,21 @@ template <class TL> __global__ __launch_bounds__(64 * TL::NW) void k_mx4_tiles(M
         } else sp[q] = a.xs + min(m0 + row - TL::TN, a.M - 1) * a.sp + 4 * (lane & 1);
     }
     const uint32_t lds0 = lds_address(lds), ring0 = lds0 + TL::STAGES * TL::STAGE_BYTES;
+    auto issue_scales = [&](int q, int step) {
+        if (step % TL::PER == 0)
+            dma4_at(sp[q] + 8 * min(step / TL::PER, ngroups - 1),
+                    ring0 + step / TL::PER % TL::RING * (TL::SR * 8) + min(wave + TL::NW * q, TL::STOTAL - 1) * 256);
+    };
+    auto issue_rows = [&](int q, int slot, int step) {
+        const int ii = min(wave + TL::NW * q, TL::TOTAL - 1);
+        const uint32_t by = min(step, nsteps - 1) * (ii < TL::AI ? TL::AB : TL::BB); // past the end: the last step again, never used
+        dma16_at(gp[q] + min(by + goff[q], glim[q]), lds0 + slot * TL::STAGE_BYTES + ii * 1024);
+    };
     auto issue = [&](int slot, int step) {
-        const uint32_t s = min(step, nsteps - 1); // past the end: the last step again, never used
-        if (step % TL::PER == 0) {
-            const int grp = min(step / TL::PER, ngroups - 1);
 #pragma unroll
-            for (int q = 0; q < TL::SI; ++q)
-                dma4_at(sp[q] + 8 * grp, ring0 + step / TL::PER % TL::RING * (TL::SR * 8) + min(wave + TL::NW * q, TL::STOTAL - 1) * 256);
-        }
+        for (int q = 0; q < TL::SI; ++q) issue_scales(q, step);
 #pragma unroll
-        for (int q = 0; q < TL::NI; ++q) {
-            const int ii = min(wave + TL::NW * q, TL::TOTAL - 1);
-            const uint32_t by = s * (ii < TL::AI ? TL::AB : TL::BB);
-            dma16_at(gp[q] + min(by + goff[q], glim[q]), lds0 + slot * TL::STAGE_BYTES + ii * 1024);
-        }
+        for (int q = 0; q < TL::NI; ++q) issue_rows(q, slot, step);
     };
 #pragma unroll
     for (int s = 0; s < TL::STAGES; ++s) issue(s, s);
@@ -505,6 +506,7 @@ template <class TL> __global__ __launch_bounds__(64 * TL::NW) void k_mx4_tiles(M
                     read_a(sb, j + 1);
                     if constexpr (TL::X4) read_b(sb, j + 1, bf[(j + 1) & 1]);
                 } else {
+                    __builtin_amdgcn_sched_barrier(0);     // the matrix instructions so far go before the wait
                     wait_vm<TL::NI * (TL::STAGES - 2)>(); // this wavefront's share of the next stage, and of its scales, has landed
                     __syncthreads();                       // ... and everybody else's; this stage has been read
                     const int next = slot + 1 == TL::STAGES ? 0 : slot + 1;
@@ -512,10 +514,20 @@ template <class TL> __global__ __launch_bounds__(64 * TL::NW) void k_mx4_tiles(M
                     read_a(nb, 0);
                     read_b(nb, 0, bn);
                     if (u == TL::PER - 1) read_scales(grp + 1, bsn, asn);
-                    issue(slot, st + TL::STAGES);
-                    slot = next;
                 }
                 __builtin_amdgcn_sched_barrier(0); // the reads stay ahead of the matrix instructions
+                // the transfers of the stage that takes this one's place go between the last sub-step's matrix instructions: issued in
+                // a row they keep both wavefronts of a SIMD from issuing anything else
+                auto between = [&](int k) __attribute__((always_inline)) {
+                    if (j + 1 < J) return;
+                    constexpr int N = TL::SI + TL::NI, M = WTM * WTN;
+#pragma unroll
+                    for (int q = k * N / M; q < (k + 1) * N / M; ++q) {
+                        if (q < TL::SI) issue_scales(q, st + TL::STAGES);
+                        else issue_rows(q - TL::SI, slot, st + TL::STAGES);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                };
                 if constexpr (TL::X4) {
 #pragma unroll
                     for (int x = 0; x < WTM; ++x)
@@ -527,6 +539,7 @@ template <class TL> __global__ __launch_bounds__(64 * TL::NW) void k_mx4_tiles(M
                             const int sa = (int)(asc[x] >> (32 * u)), sc = (int)(bsc[y] >> (32 * u));
                             if (j == 0) acc[x][y] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(p, q, acc[x][y], 4, 4, 0, sa, 0, sc);
                             else acc[x][y] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(p, q, acc[x][y], 4, 4, 1, sa, 1, sc);
+                            between(x * WTN + y);
                         }
                 } else {
                     bf16x8 w[WTN];
@@ -538,10 +551,13 @@ template <class TL> __global__ __launch_bounds__(64 * TL::NW) void k_mx4_tiles(M
 #pragma unroll
                     for (int x = 0; x < WTM; ++x)
 #pragma unroll
-                        for (int y = 0; y < WTN; ++y)
+                        for (int y = 0; y < WTN; ++y) {
                             acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<bf16x8 *>(&af[j & 1][x]), w[y], acc[x][y], 0, 0, 0);
+                            between(x * WTN + y);
+                        }
                 }
             }
+            slot = slot + 1 == TL::STAGES ? 0 : slot + 1;
 #pragma unroll
             for (int y = 0; y < WTN; ++y) bf[0][y] = bn[y];
             if (u == TL::PER - 1) {
