@@ -146,33 +146,53 @@ __device__ __forceinline__ void mx4_put(const Mx4Args &a, int m, int n, float v)
     else reinterpret_cast<bf16_t *>(a.y)[(int64_t)m * a.ldy + n] = (bf16_t)v;
 }
 
-// W neighbouring outputs, in one store where all of them are there and lie on a store's boundary
-template <int W> __device__ __forceinline__ void mx4_store(const Mx4Args &a, int cols, int64_t at, int n, const float (&o)[W], bool wide)
+// The epilogue of a wavefront's WTM x WTN accumulators: rows mw + 32 x + (8 (v / 4) + 4 g + v % 4), this lane's WTN neighbouring
+// columns from n on, `cols` in all.  Everything that does not change from value to value is decided once, outside: written plainly,
+// with the type, the bounds and GELU asked for at each value, a tile of 256 x 256 spent 16 us here.
+template <int WTM, int WTN>
+__device__ __forceinline__ void mx4_write(const Mx4Args &a, const f32x16 (&acc)[WTM][WTN], int mw, int n, int g, int cols)
 {
-    typedef float fv __attribute__((ext_vector_type(W)));
-    typedef bf16_t hv __attribute__((ext_vector_type(W)));
-    if (a.y_f32) {
-        float *p = reinterpret_cast<float *>(a.y) + at;
-        if (wide) {
-            fv r;
+    float bias[WTN];
 #pragma unroll
-            for (int e = 0; e < W; ++e) r[e] = o[e];
-            *reinterpret_cast<fv *>(p) = r;
-        } else
+    for (int y = 0; y < WTN; ++y) bias[y] = a.bias ? a.bias[min(n + y, cols - 1)] : 0.f;
+    auto put = [&](auto f32, auto gelu, auto full) __attribute__((always_inline)) {
+        typedef typename std::conditional<decltype(f32)::value, float, bf16_t>::type T;
+        typedef T vec __attribute__((ext_vector_type(WTN)));
+        T *const y0 = reinterpret_cast<T *>(a.y) + (int64_t)mw * a.ldy; // the same for all lanes
+        const bool wide = n + WTN <= cols && a.ldy % WTN == 0 && (reinterpret_cast<uintptr_t>(a.y) & (sizeof(vec) - 1)) == 0;
+        const int64_t lane_at = 4 * g * a.ldy + n;
 #pragma unroll
-            for (int e = 0; e < W; ++e)
-                if (n + e < cols) p[e] = o[e];
+        for (int x = 0; x < WTM; ++x)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int r = x * 32 + 8 * (v >> 2) + (v & 3);
+                if (!decltype(full)::value && mw + r + 4 * g >= a.M) continue;
+                vec o;
+#pragma unroll
+                for (int y = 0; y < WTN; ++y) {
+                    float f = acc[x][y][v] + bias[y];
+                    if constexpr (decltype(gelu)::value) f = mx4_gelu(f);
+                    o[y] = (T)f;
+                }
+                T *const p = y0 + r * a.ldy + lane_at;
+                if (decltype(full)::value || wide) *reinterpret_cast<vec *>(p) = o;
+                else
+#pragma unroll
+                    for (int y = 0; y < WTN; ++y)
+                        if (n + y < cols) p[y] = o[y];
+            }
+    };
+    using yes = std::integral_constant<bool, true>;
+    using no = std::integral_constant<bool, false>;
+    // a whole tile whose rows take whole stores (the column test is the same for all lanes: the last lane's)
+    const int n_last = __builtin_amdgcn_readlane(n, 63) + WTN, size = a.y_f32 ? 4 : 2;
+    const bool full = mw + 32 * WTM <= a.M && n_last <= cols && a.ldy % WTN == 0 && (reinterpret_cast<uintptr_t>(a.y) & (WTN * size - 1)) == 0;
+    if (full) {
+        if (a.y_f32) a.gelu ? put(yes(), yes(), yes()) : put(yes(), no(), yes());
+        else a.gelu ? put(no(), yes(), yes()) : put(no(), no(), yes());
     } else {
-        bf16_t *p = reinterpret_cast<bf16_t *>(a.y) + at;
-        if (wide) {
-            hv r;
-#pragma unroll
-            for (int e = 0; e < W; ++e) r[e] = (bf16_t)o[e];
-            *reinterpret_cast<hv *>(p) = r;
-        } else
-#pragma unroll
-            for (int e = 0; e < W; ++e)
-                if (n + e < cols) p[e] = (bf16_t)o[e];
+        if (a.y_f32) a.gelu ? put(yes(), yes(), no()) : put(yes(), no(), no());
+        else a.gelu ? put(no(), yes(), no()) : put(no(), no(), no());
     }
 }
 
@@ -571,26 +591,7 @@ template <class TL> __global__ __launch_bounds__(64 * TL::NW) void k_mx4_tiles(M
     }
     wait_vm<0>(); // the repeated transfers of the last steps end before the workgroup's LDS does
 
-    const int n = n0 + wn * 32 * WTN + i * WTN;
-    float bias[WTN];
-#pragma unroll
-    for (int y = 0; y < WTN; ++y) bias[y] = a.bias ? a.bias[min(n + y, a.N - 1)] : 0.f;
-    const int size = a.y_f32 ? 4 : 2;
-    const bool wide = n + WTN <= a.N && a.ldy % WTN == 0 && (reinterpret_cast<uintptr_t>(a.y) & (WTN * size - 1)) == 0;
-#pragma unroll
-    for (int x = 0; x < WTM; ++x)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-            const int m = m0 + (wm * WTM + x) * 32 + 8 * (v >> 2) + 4 * g + (v & 3);
-            if (m >= a.M) continue;
-            float o[WTN];
-#pragma unroll
-            for (int y = 0; y < WTN; ++y) {
-                o[y] = acc[x][y][v] + bias[y];
-                if (a.gelu) o[y] = mx4_gelu(o[y]);
-            }
-            mx4_store<WTN>(a, a.N, (int64_t)m * a.ldy + n, n, o, wide);
-        }
+    mx4_write<WTM, WTN>(a, acc, m0 + wm * WTM * 32, n0 + wn * 32 * WTN + i * WTN, g, a.N);
 }
 
 // dx for many rows: a workgroup's tile of 32 WM WTM rows by 256 columns, W's rows in steps of 64.  dy streams into LDS as above.
@@ -729,20 +730,7 @@ template <class TL> __global__ __launch_bounds__(64 * TL::NW) void k_mx4_dx_tile
 #undef PAC_MX4_TURN
     wait_vm<0>(); // the repeated transfers of the last steps end before the workgroup's LDS does
 
-    const int col = k0 + 8 * i + WTN * wn;
-    const int size = a.y_f32 ? 4 : 2;
-    const bool wide = col + WTN <= a.K && a.ldy % WTN == 0 && (reinterpret_cast<uintptr_t>(a.y) & (WTN * size - 1)) == 0;
-#pragma unroll
-    for (int x = 0; x < WTM; ++x)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-            const int m = m0 + (wm * WTM + x) * 32 + 8 * (v >> 2) + 4 * g + (v & 3);
-            if (m >= a.M) continue;
-            float o[WTN];
-#pragma unroll
-            for (int y = 0; y < WTN; ++y) o[y] = acc[x][y][v];
-            mx4_store<WTN>(a, a.K, (int64_t)m * a.ldy + col, col, o, wide);
-        }
+    mx4_write<WTM, WTN>(a, acc, m0 + wm * WTM * 32, k0 + 8 * i + WTN * wn, g, a.K);
 }
 
 static inline int64_t code_pitch(int cols) { return ((int64_t)cols + 255) / 256 * 128; }
