@@ -303,7 +303,7 @@ __device__ __forceinline__ void mx4_columns(const uint32_t (&w)[8], const float 
 template <int RM, int NW> __global__ __launch_bounds__(64 * NW) void k_mx4_dx_rows(Mx4Args a)
 {
     constexpr int TM = 16 * RM, PITCH = 132;
-    __shared__ __attribute__((aligned(16))) float red[NW * TM * PITCH];
+    extern __shared__ __attribute__((aligned(16))) float red[]; // [NW][TM][PITCH]
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
     const int kt = (a.K + 127) / 128, kc0 = (int)(blockIdx.x % kt) * 128, m0 = (int)(blockIdx.x / kt) * TM;
     const uint8_t *wc = a.w + kc0 / 2 + 4 * i, *sc = a.ws + kc0 / 32 + (i >> 2);
@@ -316,27 +316,37 @@ template <int RM, int NW> __global__ __launch_bounds__(64 * NW) void k_mx4_dx_ro
         for (int c = 0; c < 8; ++c) acc[c][r] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     const int steps = (a.N + 31) / 32, last = (a.N + 7) / 8 * 8 - 8;
-    for (int s = wave; s < steps; s += NW) {
-        const int n0 = 32 * s + 8 * q;
-        uint32_t w[8];
-        float f[8];
+    // the coming step's operands are under way while the present one's are multiplied; past the end: the last step's, unused
+    uint32_t wn[8], sn[8];
+    u32x4 dn[RM];
+    auto fetch = [&](int s) {
+        const int n0 = 32 * min(s, steps - 1) + 8 * q;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int64_t n = min(n0 + e, a.N - 1); // past the end dy counts as zero
-            w[e] = *reinterpret_cast<const uint32_t *>(wc + n * a.wp);
-            f[e] = mx4_scale(sc[n * a.sp]);
+            wn[e] = *reinterpret_cast<const uint32_t *>(wc + n * a.wp);
+            sn[e] = sc[n * a.sp];
         }
-        u32x4 col[8];
+#pragma unroll
+        for (int r = 0; r < RM; ++r) dn[r] = *reinterpret_cast<const u32x4 *>(dyr[r] + min(n0, last));
+    };
+    fetch(wave);
+    for (int s = wave; s < steps; s += NW) {
+        uint32_t w[8];
+        float f[8];
+        u32x4 d[RM], col[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = wn[e], f[e] = mx4_scale(sn[e]);
+#pragma unroll
+        for (int r = 0; r < RM; ++r) d[r] = 32 * s + 32 > a.N ? mx4_keep(dn[r], a.N - (32 * s + 8 * q)) : dn[r];
+        fetch(s + NW);
         mx4_columns(w, f, col);
 #pragma unroll
-        for (int r = 0; r < RM; ++r) {
-            u32x4 d = *reinterpret_cast<const u32x4 *>(dyr[r] + min(n0, last));
-            if (32 * s + 32 > a.N) d = mx4_keep(d, a.N - n0);
+        for (int r = 0; r < RM; ++r)
 #pragma unroll
             for (int c = 0; c < 8; ++c)
-                acc[c][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<bf16x8 *>(&col[c]), *reinterpret_cast<bf16x8 *>(&d),
+                acc[c][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<bf16x8 *>(&col[c]), *reinterpret_cast<bf16x8 *>(&d[r]),
                                                                     acc[c][r], 0, 0, 0);
-        }
     }
     // lane (i, q): row i, columns 8 (4 q + v) + c
 #pragma unroll
@@ -381,6 +391,7 @@ template <bool X4_, int WM_, int WN_, int WTM_, int WTN_, int STAGES_> struct Mx
     static constexpr int SR = TN + (X4 ? TM : 0), STOTAL = SR / 32, SI = (STOTAL + NW - 1) / NW, RING = (STAGES - 1) / PER + 2;
     static constexpr int LDS_BYTES = STAGES * STAGE_BYTES + RING * SR * 8;
     static_assert(STAGES >= 2 && (NI + SI) * STAGES < 60, "transfers in flight must fit the counter");
+    static constexpr bool AHEAD = WTM * WTN <= 4; // the next step's fragments are all read during this one's matrix instructions
 };
 // 4 bytes a lane from global memory into LDS, as dma16_at
 __device__ __forceinline__ void dma4_at(const void *g, uint32_t lds_wave_address)
@@ -394,6 +405,19 @@ template <int BYTES> __device__ __forceinline__ int mx4_swz(int row)
     return BYTES == 128 ? (row >> 1) & 7 : BYTES == 64 ? (row >> 2) & 3 : (row >> 3) & 1;
 }
 
+// bf16 rows of a step that ends past the contraction's length: what lies there is cleared in LDS, before anyone reads it.  All
+// threads call this, with the step's stage in place and a barrier behind it.
+template <int ROWS, int THREADS> __device__ __forceinline__ void mx4_clip(char *stage, int valid)
+{
+    for (int e = threadIdx.x; e < ROWS * 8; e += THREADS) {
+        const int row = e >> 3, c = e & 7;
+        if (8 * c + 8 <= valid) continue;
+        u32x4 *p = reinterpret_cast<u32x4 *>(stage + row * 128 + ((c ^ mx4_swz<128>(row)) << 4));
+        *p = mx4_keep(*p, valid - 8 * c);
+    }
+    __syncthreads();
+}
+
 // A die (blocks go round the eight of them) takes a run of tiles eight high, whose operands stay in its L2
 __device__ __forceinline__ void mx4_place(int mt, int nt, int &tm, int &tn)
 {
@@ -403,7 +427,8 @@ __device__ __forceinline__ void mx4_place(int mt, int nt, int &tm, int &tn)
     tn = v % (8 * nt) / high;
 }
 
-template <class TL> __global__ __launch_bounds__(64 * TL::NW) void k_mx4_tiles(Mx4Args a)
+// (two wavefronts a SIMD: with the 512 registers that one may have the compiler moves accumulators in and out at every instruction)
+template <class TL> __global__ __launch_bounds__(64 * TL::NW, 2) void k_mx4_tiles(Mx4Args a)
 {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     constexpr int WTM = TL::WTM, WTN = TL::WTN;
@@ -484,11 +509,9 @@ template <class TL> __global__ __launch_bounds__(64 * TL::NW) void k_mx4_tiles(M
         brow[y] = TL::TM * TL::AB + row * TL::BB;
         bsw[y] = mx4_swz<TL::BB>(row);
     }
-    // A step is walked in its J sub-steps, each reading the next one's fragments before its own matrix instructions.  The last
-    // sub-step's come after the barrier that hands over the next stage, so that they cover the latency of that stage's first reads.
-    constexpr int J = TL::X4 ? 2 : 4;
+    constexpr int J = TL::X4 ? 2 : 4, FB = TL::AHEAD ? 2 * J : 2; // sub-steps; fragments held
     uint64_t bsc[WTN], asc[TL::X4 ? WTM : 1]; // this lane's half of a group's scales, shifted to the bottom
-    u32x4 af[2][WTM], bf[2][WTN];             // fragments; for bf16 rows bf[0] holds the step's codes
+    u32x4 af[FB][WTM], bf[TL::X4 ? FB : 2][WTN]; // fragments; beside bf16 rows bf holds a step's codes
     auto read_scales = [&](int grp, uint64_t (&bs)[WTN], uint64_t (&as)[TL::X4 ? WTM : 1]) {
         const char *sc = lds + TL::STAGES * TL::STAGE_BYTES + grp % TL::RING * (TL::SR * 8);
         const int half = TL::X4 ? 16 * g : 8 * g;
@@ -498,94 +521,143 @@ template <class TL> __global__ __launch_bounds__(64 * TL::NW) void k_mx4_tiles(M
 #pragma unroll
             for (int x = 0; x < WTM; ++x) as[x] = *reinterpret_cast<const uint64_t *>(sc + (TL::TN + (wm * WTM + x) * 32 + i) * 8) >> half;
     };
-    auto read_a = [&](const char *sb, int j) {
+    auto read_a = [&](const char *sb, int j, u32x4 (&to)[WTM]) {
 #pragma unroll
-        for (int x = 0; x < WTM; ++x) af[j & 1][x] = *reinterpret_cast<const u32x4 *>(sb + arow[x] + (((J * g + j) ^ asw[x]) << 4));
+        for (int x = 0; x < WTM; ++x) to[x] = *reinterpret_cast<const u32x4 *>(sb + arow[x] + (((J * g + j) ^ asw[x]) << 4));
     };
     auto read_b = [&](const char *sb, int j, u32x4 (&to)[WTN]) {
 #pragma unroll
         for (int y = 0; y < WTN; ++y) to[y] = *reinterpret_cast<const u32x4 *>(sb + brow[y] + (((TL::X4 ? J * g + j : g) ^ bsw[y]) << 4));
     };
-    wait_vm<TL::NI * (TL::STAGES - 1)>();
-    __syncthreads();
+    // the matrix instructions of a sub-step, `after(k)` behind the k-th of them
+    auto multiply = [&](int u, int j, u32x4 (&pa)[WTM], const u32x4 (&pb)[WTN], auto after) __attribute__((always_inline)) {
+        if constexpr (TL::X4) {
+#pragma unroll
+            for (int x = 0; x < WTM; ++x)
+#pragma unroll
+                for (int y = 0; y < WTN; ++y) {
+                    const i32x8 p = {(int)pa[x][0], (int)pa[x][1], (int)pa[x][2], (int)pa[x][3], 0, 0, 0, 0};
+                    const i32x8 q = {(int)pb[y][0], (int)pb[y][1], (int)pb[y][2], (int)pb[y][3], 0, 0, 0, 0};
+                    const int sa = (int)(asc[x] >> (32 * u)), sc = (int)(bsc[y] >> (32 * u));
+                    if (j == 0) acc[x][y] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(p, q, acc[x][y], 4, 4, 0, sa, 0, sc);
+                    else acc[x][y] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(p, q, acc[x][y], 4, 4, 1, sa, 1, sc);
+                    after(x * WTN + y);
+                }
+        } else {
+            bf16x8 w[WTN];
+#pragma unroll
+            for (int y = 0; y < WTN; ++y) w[y] = mx4_bf16(pb[y][j], mx4_scale((uint32_t)(bsc[y] >> (16 * u)) & 255u));
+#pragma unroll
+            for (int x = 0; x < WTM; ++x)
+#pragma unroll
+                for (int y = 0; y < WTN; ++y) {
+                    acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<bf16x8 *>(&pa[x]), w[y], acc[x][y], 0, 0, 0);
+                    after(x * WTN + y);
+                }
+        }
+    };
+    // The transfers of the stage that takes a used one's place go between matrix instructions (k of m): issued in a row they keep
+    // both wavefronts of a SIMD from issuing anything else.
+    auto transfers = [&](int k, int m, int slot, int step) __attribute__((always_inline)) {
+        constexpr int N = TL::SI + TL::NI;
+#pragma unroll
+        for (int q = k * N / m; q < (k + 1) * N / m; ++q) {
+            if (q < TL::SI) issue_scales(q, step);
+            else issue_rows(q - TL::SI, slot, step);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // hands over stage `step`: this wavefront's share of it, and of its scales, has landed, then everybody else's
+    auto arrive = [&](char *stage, int step, auto pending) __attribute__((always_inline)) {
+        wait_vm<decltype(pending)::value>();
+        __syncthreads();
+        if constexpr (!TL::X4)
+            if (step == nsteps - 1 && a.K % 64) mx4_clip<TL::TM, 64 * TL::NW>(stage, a.K - step * 64);
+    };
+    arrive(lds, 0, std::integral_constant<int, TL::NI * (TL::STAGES - 1)>());
     read_scales(0, bsc, asc);
-    read_a(lds, 0);
-    read_b(lds, 0, bf[0]);
     int slot = 0;
-    for (int grp = 0; grp < ngroups; ++grp) {
+    if constexpr (TL::AHEAD) {
+        // Few matrix instructions a step: fragments are read a whole step ahead, else the latency of LDS shows at every sub-step
+        // (64 x 64 tiles at K = 4096: 27 us a tile with sub-steps as below).
 #pragma unroll
-        for (int u = 0; u < TL::PER; ++u) {
-            const int st = grp * TL::PER + u;
-            if (st >= nsteps) break;
-            const char *sb = lds + slot * TL::STAGE_BYTES;
-            uint64_t bsn[WTN], asn[TL::X4 ? WTM : 1];
-            u32x4 bn[WTN];
+        for (int j = 0; j < J; ++j) {
+            read_a(lds, j, af[j]);
+            if (TL::X4 || j == 0) read_b(lds, j, bf[j]);
+        }
+        for (int grp = 0; grp < ngroups; ++grp) {
 #pragma unroll
-            for (int j = 0; j < J; ++j) {
-                if (j + 1 < J) {
-                    read_a(sb, j + 1);
-                    if constexpr (TL::X4) read_b(sb, j + 1, bf[(j + 1) & 1]);
-                } else {
-                    __builtin_amdgcn_sched_barrier(0);     // the matrix instructions so far go before the wait
-                    wait_vm<TL::NI * (TL::STAGES - 2)>(); // this wavefront's share of the next stage, and of its scales, has landed
-                    __syncthreads();                       // ... and everybody else's; this stage has been read
-                    const int next = slot + 1 == TL::STAGES ? 0 : slot + 1;
-                    const char *nb = lds + next * TL::STAGE_BYTES;
-                    read_a(nb, 0);
-                    read_b(nb, 0, bn);
-                    if (u == TL::PER - 1) read_scales(grp + 1, bsn, asn);
+            for (int u = 0; u < TL::PER; ++u) {
+                const int st = grp * TL::PER + u;
+                if (st >= nsteps) break;
+                char *nb = lds + (slot + 1 == TL::STAGES ? 0 : slot + 1) * TL::STAGE_BYTES;
+                arrive(nb, st + 1, std::integral_constant<int, TL::NI * (TL::STAGES - 2)>()); // (this stage has been read)
+                uint64_t bsn[WTN], asn[TL::X4 ? WTM : 1];
+                const int now = (u & 1) * J, next = J - now;
+                if (u == TL::PER - 1) read_scales(grp + 1, bsn, asn);
+#pragma unroll
+                for (int j = 0; j < J; ++j) {
+                    read_a(nb, j, af[next + j]);
+                    if (TL::X4) read_b(nb, j, bf[TL::X4 ? next + j : 0]);
+                    else if (j == 0) read_b(nb, 0, bf[(u & 1) ^ 1]);
                 }
                 __builtin_amdgcn_sched_barrier(0); // the reads stay ahead of the matrix instructions
-                // the transfers of the stage that takes this one's place go between the last sub-step's matrix instructions: issued in
-                // a row they keep both wavefronts of a SIMD from issuing anything else
-                auto between = [&](int k) __attribute__((always_inline)) {
-                    if (j + 1 < J) return;
-                    constexpr int N = TL::SI + TL::NI, M = WTM * WTN;
 #pragma unroll
-                    for (int q = k * N / M; q < (k + 1) * N / M; ++q) {
-                        if (q < TL::SI) issue_scales(q, st + TL::STAGES);
-                        else issue_rows(q - TL::SI, slot, st + TL::STAGES);
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-                };
-                if constexpr (TL::X4) {
+                for (int j = 0; j < J; ++j)
+                    multiply(u, j, af[now + j], bf[TL::X4 ? now + j : (u & 1)], [&](int k) __attribute__((always_inline)) {
+                        transfers(j * WTM * WTN + k, J * WTM * WTN, slot, st + TL::STAGES);
+                    });
+                if (u == TL::PER - 1) {
 #pragma unroll
-                    for (int x = 0; x < WTM; ++x)
+                    for (int y = 0; y < WTN; ++y) bsc[y] = bsn[y];
+                    if constexpr (TL::X4)
 #pragma unroll
-                        for (int y = 0; y < WTN; ++y) {
-                            const u32x4 &pa = af[j & 1][x], &pb = bf[j & 1][y];
-                            const i32x8 p = {(int)pa[0], (int)pa[1], (int)pa[2], (int)pa[3], 0, 0, 0, 0};
-                            const i32x8 q = {(int)pb[0], (int)pb[1], (int)pb[2], (int)pb[3], 0, 0, 0, 0};
-                            const int sa = (int)(asc[x] >> (32 * u)), sc = (int)(bsc[y] >> (32 * u));
-                            if (j == 0) acc[x][y] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(p, q, acc[x][y], 4, 4, 0, sa, 0, sc);
-                            else acc[x][y] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(p, q, acc[x][y], 4, 4, 1, sa, 1, sc);
-                            between(x * WTN + y);
-                        }
-                } else {
-                    bf16x8 w[WTN];
-#pragma unroll
-                    for (int y = 0; y < WTN; ++y) w[y] = mx4_bf16(bf[0][y][j], mx4_scale((uint32_t)(bsc[y] >> (16 * u)) & 255u));
-                    if (st * 64 + 64 > a.K)
-#pragma unroll
-                        for (int x = 0; x < WTM; ++x) af[j & 1][x] = mx4_keep(af[j & 1][x], a.K - (st * 64 + 32 * g + 8 * j));
-#pragma unroll
-                    for (int x = 0; x < WTM; ++x)
-#pragma unroll
-                        for (int y = 0; y < WTN; ++y) {
-                            acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<bf16x8 *>(&af[j & 1][x]), w[y], acc[x][y], 0, 0, 0);
-                            between(x * WTN + y);
-                        }
+                        for (int x = 0; x < WTM; ++x) asc[x] = asn[x];
                 }
+                slot = slot + 1 == TL::STAGES ? 0 : slot + 1;
             }
-            slot = slot + 1 == TL::STAGES ? 0 : slot + 1;
+        }
+    } else {
+        // A step is walked in its J sub-steps, each reading the next one's fragments before its own matrix instructions.  The last
+        // sub-step's come after the barrier that hands over the next stage, so that they cover the latency of that stage's first reads.
+        read_a(lds, 0, af[0]);
+        read_b(lds, 0, bf[0]);
+        for (int grp = 0; grp < ngroups; ++grp) {
 #pragma unroll
-            for (int y = 0; y < WTN; ++y) bf[0][y] = bn[y];
-            if (u == TL::PER - 1) {
+            for (int u = 0; u < TL::PER; ++u) {
+                const int st = grp * TL::PER + u;
+                if (st >= nsteps) break;
+                const char *sb = lds + slot * TL::STAGE_BYTES;
+                uint64_t bsn[WTN], asn[TL::X4 ? WTM : 1];
+                u32x4 bn[WTN];
 #pragma unroll
-                for (int y = 0; y < WTN; ++y) bsc[y] = bsn[y];
-                if constexpr (TL::X4)
+                for (int j = 0; j < J; ++j) {
+                    if (j + 1 < J) {
+                        read_a(sb, j + 1, af[(j + 1) & 1]);
+                        if constexpr (TL::X4) read_b(sb, j + 1, bf[(j + 1) & 1]);
+                    } else {
+                        __builtin_amdgcn_sched_barrier(0); // the matrix instructions so far go before the wait
+                        char *nb = lds + (slot + 1 == TL::STAGES ? 0 : slot + 1) * TL::STAGE_BYTES;
+                        arrive(nb, st + 1, std::integral_constant<int, TL::NI * (TL::STAGES - 2)>()); // (this stage has been read)
+                        read_a(nb, 0, af[0]);
+                        read_b(nb, 0, bn);
+                        if (u == TL::PER - 1) read_scales(grp + 1, bsn, asn);
+                    }
+                    __builtin_amdgcn_sched_barrier(0); // the reads stay ahead of the matrix instructions
+                    multiply(u, j, af[j & 1], bf[TL::X4 ? j & 1 : 0], [&](int k) __attribute__((always_inline)) {
+                        if (j + 1 == J) transfers(k, WTM * WTN, slot, st + TL::STAGES);
+                    });
+                }
+                slot = slot + 1 == TL::STAGES ? 0 : slot + 1;
 #pragma unroll
-                    for (int x = 0; x < WTM; ++x) asc[x] = asn[x];
+                for (int y = 0; y < WTN; ++y) bf[0][y] = bn[y];
+                if (u == TL::PER - 1) {
+#pragma unroll
+                    for (int y = 0; y < WTN; ++y) bsc[y] = bsn[y];
+                    if constexpr (TL::X4)
+#pragma unroll
+                        for (int x = 0; x < WTM; ++x) asc[x] = asn[x];
+                }
             }
         }
     }
@@ -594,26 +666,28 @@ template <class TL> __global__ __launch_bounds__(64 * TL::NW) void k_mx4_tiles(M
     mx4_write<WTM, WTN>(a, acc, m0 + wm * WTM * 32, n0 + wn * 32 * WTN + i * WTN, g, a.N);
 }
 
-// dx for many rows: a workgroup's tile of 32 WM WTM rows by 256 columns, W's rows in steps of 64.  dy streams into LDS as above.
-// W's step is turned round on its way: a thread takes eight columns of four rows (four loads of 4 bytes, 128 bytes a row and 32
-// threads), converts them with each row's scale, and writes the four rows of each column side by side, as the fragments want them.
-// It is loaded two steps ahead, converted and written one step ahead, a quarter after each quarter of the matrix instructions.
+// dx for many rows: a workgroup's tile of 32 WM WTM rows by 256 columns, W's rows in steps of 64.  dy and W's codes and scales stream
+// into LDS as above.  W's step is turned round there, one step ahead, a part after each of the first three sub-steps' matrix
+// instructions: a thread takes eight columns of four rows, converts them with each row's scale, and writes the four rows of each
+// column side by side, as the fragments want them.  Stage t of the ring holds dy's step t and W's step t + 1.
 // LDS row c 32 + i holds column 8 i + c: the writes of 32 threads and the reads of a fragment then go to neighbouring rows, and
 // subtile c of lane i is column 8 i + c of the tile, WTN neighbouring ones a lane.
 template <int WM_, int WN_, int WTM_, int WTN_, int STAGES_> struct Mx4DxTile {
     static constexpr int WM = WM_, WN = WN_, WTM = WTM_, WTN = WTN_, STAGES = STAGES_, NW = WM * WN;
-    static constexpr int TM = 32 * WM * WTM, TK = 256, BK = 64;
-    static constexpr int TOTAL = TM / 8, NI = (TOTAL + NW - 1) / NW, TASKS = 512 / (64 * NW);
-    static constexpr int A_BYTES = TM * 128, B_BYTES = TK * 128, LDS_BYTES = STAGES * A_BYTES + 2 * B_BYTES;
-    static_assert(WN * WTN == 8 && TASKS * NW == 8, "256 columns, 512 tasks a step");
-    static_assert(STAGES >= 2 && NI * (STAGES - 1) < 60, "transfers in flight must fit the counter");
+    static constexpr int TM = 32 * WM * WTM, TK = 256;
+    static constexpr int AI = TM / 8, TOTAL = AI + 8, NI = TOTAL / NW; // transfers of 1 KB: dy, then W's codes
+    static constexpr int W_AT = TM * 128, S_AT = W_AT + 8192, STAGE_BYTES = S_AT + 512, B_BYTES = TK * 128;
+    static constexpr int LDS_BYTES = STAGES * STAGE_BYTES + 2 * B_BYTES;
+    static_assert(WN * WTN == 8 && NW == 8 && TOTAL % NW == 0, "256 columns, 512 threads");
+    static_assert(STAGES >= 2 && (NI + 1) * STAGES < 60, "transfers in flight must fit the counter");
 };
 
-template <class TL> __global__ __launch_bounds__(64 * TL::NW) void k_mx4_dx_tiles(Mx4Args a)
+template <class TL> __global__ __launch_bounds__(64 * TL::NW, 2) void k_mx4_dx_tiles(Mx4Args a)
 {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
-    constexpr int WTM = TL::WTM, WTN = TL::WTN, NT = 64 * TL::NW;
-    char *const bbuf = lds + TL::STAGES * TL::A_BYTES;
+    constexpr int WTM = TL::WTM, WTN = TL::WTN;
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    char *const bbuf = lds + TL::STAGES * TL::STAGE_BYTES;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / TL::WN, wn = wave % TL::WN, i = lane & 31, g = lane >> 5;
     int m0, k0;
@@ -622,60 +696,65 @@ template <class TL> __global__ __launch_bounds__(64 * TL::NW) void k_mx4_dx_tile
     k0 *= TL::TK;
     const int nsteps = (a.N + 63) / 64;
 
+    // this lane's share of a stage's transfers: wavefronts take 1 KB pieces in turn, eight rows of 128 bytes each
     const char *gp[TL::NI];
     uint32_t goff[TL::NI];
     const uint32_t glim = 2u * ((a.N + 7) / 8 * 8 - 8); // dy has no chunk past this one
 #pragma unroll
     for (int q = 0; q < TL::NI; ++q) {
-        const int ii = min(wave + TL::NW * q, TL::TOTAL - 1), row = ii * 8 + lane / 8;
+        const int ii = wave + TL::NW * q, row = ii * 8 + lane / 8;
         goff[q] = 16 * ((lane & 7) ^ mx4_swz<128>(row));
         gp[q] = reinterpret_cast<const char *>(a.x) + min(m0 + row, a.M - 1) * (a.ldx * 2);
     }
-    auto issue = [&](int slot, int step) {
-        const uint32_t s = min(step, nsteps - 1); // past the end: the last step again, never used
-#pragma unroll
-        for (int q = 0; q < TL::NI; ++q) {
-            const int ii = min(wave + TL::NW * q, TL::TOTAL - 1);
-            dma16_at(gp[q] + min(128 * s + goff[q], glim), lds_address(lds) + slot * TL::A_BYTES + ii * 1024);
+    const uint32_t lds0 = lds_address(lds);
+    auto issue_rows = [&](int q, int slot, int step) {
+        const int ii = wave + TL::NW * q;
+        const uint32_t to = lds0 + slot * TL::STAGE_BYTES + ii * 1024;
+        const int s = min(step, nsteps - 1); // past the end: the last step again, never used
+        if (ii < TL::AI) dma16_at(gp[q] + min(128u * s + goff[q], glim), to);
+        else {
+            const int64_t n = min(64 * min(step + 1, nsteps - 1) + (ii - TL::AI) * 8 + lane / 8, a.N - 1); // past the end dy counts as zero
+            dma16_at(a.w + n * a.wp + k0 / 2 + 16 * (lane & 7), to);
         }
     };
-    // this thread's tasks: columns 8 cg .. 8 cg + 7, rows 4 ng .. 4 ng + 3 of a step
-    const int cg = threadIdx.x & 31;
-    const uint8_t *wc = a.w + k0 / 2 + 4 * cg, *sc = a.ws + k0 / 32 + (cg >> 2);
-    uint32_t wr[2][TL::TASKS][4], sr[2][TL::TASKS][4];
-    auto fetch = [&](int set, int step) {
-#pragma unroll
-        for (int h = 0; h < TL::TASKS; ++h)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int64_t n = min(64 * min(step, nsteps - 1) + 4 * (int)((threadIdx.x + h * NT) >> 5) + e, a.N - 1); // past the end dy counts as zero
-                wr[set][h][e] = *reinterpret_cast<const uint32_t *>(wc + n * a.wp);
-                sr[set][h][e] = sc[n * a.sp];
-            }
+    auto issue_scales = [&](int slot, int step) { // two lanes a row, 32 rows a piece; the other wavefronts repeat the second piece
+        const int piece = min(wave, 1);
+        const int64_t n = min(64 * min(step + 1, nsteps - 1) + piece * 32 + lane / 2, a.N - 1);
+        dma4_at(a.ws + n * a.sp + k0 / 32 + 4 * (lane & 1), lds0 + slot * TL::STAGE_BYTES + TL::S_AT + piece * 256);
     };
-    uint32_t wat[TL::TASKS]; // where a task's column 0 goes; column c: 4096 bytes further (the swizzle repeats every 16 rows)
+    // this thread's part of turning W: columns 8 cg .. 8 cg + 7, rows 4 ng .. 4 ng + 3 of a step
+    const int cg = threadIdx.x & 31, ng = threadIdx.x >> 5;
+    const int wat = cg * 128 + (((ng >> 1) ^ mx4_swz<128>(cg)) << 4) + 8 * (ng & 1); // where column 8 cg goes; the next: 4096 bytes on
+    uint32_t wr[4], sr[4];
+    auto turn = [&](auto c, char *to) __attribute__((always_inline)) {
+        constexpr int C = decltype(c)::value;
+        bf16x2 p[4];
 #pragma unroll
-    for (int h = 0; h < TL::TASKS; ++h) {
-        const int ng = (threadIdx.x + h * NT) >> 5;
-        wat[h] = cg * 128 + (((ng >> 1) ^ mx4_swz<128>(cg)) << 4) + 8 * (ng & 1);
-    }
-#define PAC_MX4_TURN(SET, C, TO)                                                                                               \
-    _Pragma("unroll") for (int h = 0; h < TL::TASKS; ++h)                                                                      \
-    {                                                                                                                          \
-        bf16x2 p[4];                                                                                                           \
-        _Pragma("unroll") for (int e = 0; e < 4; ++e) p[e] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(wr[SET][h][e], mx4_scale(sr[SET][h][e]), C); \
-        typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));                                                            \
-        *reinterpret_cast<u32x2 *>((TO) + wat[h] + 8192 * C) = u32x2{pk_lo(p[0], p[1]), pk_lo(p[2], p[3])};                   \
-        *reinterpret_cast<u32x2 *>((TO) + wat[h] + 8192 * C + 4096) = u32x2{pk_hi(p[0], p[1]), pk_hi(p[2], p[3])};            \
-    }
-    fetch(0, 0);
-    fetch(1, 1);
+        for (int e = 0; e < 4; ++e) p[e] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(wr[e], mx4_scale(sr[e]), C);
+        *reinterpret_cast<u32x2 *>(to + wat + 8192 * C) = u32x2{pk_lo(p[0], p[1]), pk_lo(p[2], p[3])};
+        *reinterpret_cast<u32x2 *>(to + wat + 8192 * C + 4096) = u32x2{pk_hi(p[0], p[1]), pk_hi(p[2], p[3])};
+    };
+    using c0 = std::integral_constant<int, 0>;
+    using c1 = std::integral_constant<int, 1>;
+    using c2 = std::integral_constant<int, 2>;
+    using c3 = std::integral_constant<int, 3>;
+    // W's first step comes through registers
 #pragma unroll
-    for (int s = 0; s < TL::STAGES - 1; ++s) issue(s, s);
-    PAC_MX4_TURN(0, 0, bbuf)
-    PAC_MX4_TURN(0, 1, bbuf)
-    PAC_MX4_TURN(0, 2, bbuf)
-    PAC_MX4_TURN(0, 3, bbuf)
+    for (int e = 0; e < 4; ++e) {
+        const int64_t n = min(4 * ng + e, a.N - 1);
+        wr[e] = *reinterpret_cast<const uint32_t *>(a.w + n * a.wp + k0 / 2 + 4 * cg);
+        sr[e] = a.ws[n * a.sp + k0 / 32 + (cg >> 2)];
+    }
+    turn(c0(), bbuf);
+    turn(c1(), bbuf);
+    turn(c2(), bbuf);
+    turn(c3(), bbuf);
+#pragma unroll
+    for (int s = 0; s < TL::STAGES; ++s) {
+        issue_scales(s, s);
+#pragma unroll
+        for (int q = 0; q < TL::NI; ++q) issue_rows(q, s, s);
+    }
 
     f32x16 acc[WTM][WTN];
 #pragma unroll
@@ -684,52 +763,72 @@ template <class TL> __global__ __launch_bounds__(64 * TL::NW) void k_mx4_dx_tile
         for (int y = 0; y < WTN; ++y)
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[x][y][v] = 0.f;
-    int arow[WTM], asw[WTM];
+    int arow[WTM];
 #pragma unroll
-    for (int x = 0; x < WTM; ++x) {
-        arow[x] = ((wm * WTM + x) * 32 + i) * 128;
-        asw[x] = mx4_swz<128>((wm * WTM + x) * 32 + i);
-    }
-    const int brow = (wn * WTN * 32 + i) * 128, bsw = mx4_swz<128>(i);
-    int slot = 0;
-    auto step = [&](int st, auto odd) __attribute__((always_inline)) {
-        constexpr int now = decltype(odd)::value, next = now ^ 1; // the set that holds step st + 1 is `next`
-        wait_vm<TL::NI * (TL::STAGES - 2)>();
+    for (int x = 0; x < WTM; ++x) arow[x] = ((wm * WTM + x) * 32 + i) * 128;
+    const int brow = (wn * WTN * 32 + i) * 128, swz = mx4_swz<128>(i); // (the swizzle repeats every 16 rows)
+    u32x4 af[2][WTM], bf[2][WTN];
+    auto read = [&](const char *sa, const char *sb, int j) {
+#pragma unroll
+        for (int x = 0; x < WTM; ++x) af[j & 1][x] = *reinterpret_cast<const u32x4 *>(sa + arow[x] + (((4 * g + j) ^ swz) << 4));
+#pragma unroll
+        for (int y = 0; y < WTN; ++y) bf[j & 1][y] = *reinterpret_cast<const u32x4 *>(sb + brow + y * 4096 + (((4 * g + j) ^ swz) << 4));
+    };
+    auto read_w = [&](const char *sa) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            wr[e] = *reinterpret_cast<const uint32_t *>(sa + TL::W_AT + (4 * ng + e) * 128 + 4 * cg);
+            sr[e] = *reinterpret_cast<const uint8_t *>(sa + TL::S_AT + (4 * ng + e) * 8 + (cg >> 2));
+        }
+    };
+    // hands over stage `step`: this wavefront's share of it has landed, then everybody else's
+    auto arrive = [&](char *stage, int step, auto pending) __attribute__((always_inline)) {
+        wait_vm<decltype(pending)::value>();
         __syncthreads();
-        const char *sa = lds + slot * TL::A_BYTES, *sb = bbuf + now * TL::B_BYTES;
-        char *to = bbuf + next * TL::B_BYTES;
-        fetch(now, st + 2);
-        issue(slot == 0 ? TL::STAGES - 1 : slot - 1, st + TL::STAGES - 1);
-        const bool tail = st * 64 + 64 > a.N;
+        if (step == nsteps - 1 && a.N % 64) mx4_clip<TL::TM, 64 * TL::NW>(stage, a.N - step * 64);
+    };
+    arrive(lds, 0, std::integral_constant<int, (TL::NI + 1) * (TL::STAGES - 1)>());
+    read(lds, bbuf, 0);
+    read_w(lds);
+    int slot = 0;
+    for (int st = 0; st < nsteps; ++st) {
+        const char *sa = lds + slot * TL::STAGE_BYTES, *sb = bbuf + (st & 1) * TL::B_BYTES;
+        char *to = bbuf + ((st + 1) & 1) * TL::B_BYTES;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            u32x4 af[WTM], bf[WTN];
-#pragma unroll
-            for (int x = 0; x < WTM; ++x) af[x] = *reinterpret_cast<const u32x4 *>(sa + arow[x] + (((4 * g + j) ^ asw[x]) << 4));
-#pragma unroll
-            for (int y = 0; y < WTN; ++y) bf[y] = *reinterpret_cast<const u32x4 *>(sb + brow + y * 4096 + (((4 * g + j) ^ bsw) << 4));
-            if (tail)
-#pragma unroll
-                for (int x = 0; x < WTM; ++x) af[x] = mx4_keep(af[x], a.N - (st * 64 + 32 * g + 8 * j));
+            if (j < 3) read(sa, sb, j + 1);
+            else {
+                __builtin_amdgcn_sched_barrier(0); // the matrix instructions so far go before the wait
+                char *na = lds + (slot + 1 == TL::STAGES ? 0 : slot + 1) * TL::STAGE_BYTES;
+                arrive(na, st + 1, std::integral_constant<int, (TL::NI + 1) * (TL::STAGES - 2)>()); // (this stage has been read, W's next step turned)
+                read(na, to, 0);
+                read_w(na);
+            }
+            __builtin_amdgcn_sched_barrier(0); // the reads stay ahead of the matrix instructions
 #pragma unroll
             for (int x = 0; x < WTM; ++x)
 #pragma unroll
-                for (int y = 0; y < WTN; ++y)
-                    acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<bf16x8 *>(&af[x]), *reinterpret_cast<bf16x8 *>(&bf[y]), acc[x][y], 0, 0, 0);
-            if (j == 0) { PAC_MX4_TURN(next, 0, to) }
-            else if (j == 1) { PAC_MX4_TURN(next, 1, to) }
-            else if (j == 2) { PAC_MX4_TURN(next, 2, to) }
-            else { PAC_MX4_TURN(next, 3, to) }
+                for (int y = 0; y < WTN; ++y) {
+                    acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<bf16x8 *>(&af[j & 1][x]), *reinterpret_cast<bf16x8 *>(&bf[j & 1][y]),
+                                                                        acc[x][y], 0, 0, 0);
+                    if (j == 3) { // transfers between matrix instructions, as above
+                        constexpr int N = TL::NI + 1, M = WTM * WTN;
+                        const int k = x * WTN + y;
+#pragma unroll
+                        for (int q = k * N / M; q < (k + 1) * N / M; ++q) {
+                            if (q == 0) issue_scales(slot, st + TL::STAGES);
+                            else issue_rows(q - 1, slot, st + TL::STAGES);
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+            if (j == 0) turn(c0(), to), turn(c1(), to);
+            else if (j == 1) turn(c2(), to);
+            else if (j == 2) turn(c3(), to);
         }
         slot = slot + 1 == TL::STAGES ? 0 : slot + 1;
-    };
-    for (int st = 0; st < nsteps; st += 2) {
-        step(st, std::integral_constant<int, 0>());
-        if (st + 1 < nsteps) step(st + 1, std::integral_constant<int, 1>());
     }
-#undef PAC_MX4_TURN
     wait_vm<0>(); // the repeated transfers of the last steps end before the workgroup's LDS does
-
     mx4_write<WTM, WTN>(a, acc, m0 + wm * WTM * 32, k0 + 8 * i + WTN * wn, g, a.K);
 }
 
@@ -791,19 +890,67 @@ template <class TL> static pac_status launch_dx_tiles(const Mx4Args &a, hipStrea
     return done();
 }
 
+template <bool X4, int RM> static pac_status launch_rows(const Mx4Args &a, hipStream_t st)
+{
+    const int64_t tiles = tile_count(((int64_t)a.N + 15) / 16, ((int64_t)a.M + 16 * RM - 1) / (16 * RM));
+    if (tiles < 0) return PAC_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL((k_mx4_rows<X4, RM, 8>), dim3((unsigned)tiles), dim3(512), 0, st, a);
+    return done();
+}
+template <int RM> static pac_status launch_dx_rows(const Mx4Args &a, hipStream_t st)
+{
+    const int64_t tiles = tile_count(((int64_t)a.K + 127) / 128, ((int64_t)a.M + 16 * RM - 1) / (16 * RM));
+    if (tiles < 0) return PAC_ERR_UNSUPPORTED;
+    constexpr int NW = 8, LDS = NW * 16 * RM * 132 * 4;
+    static std::once_flag once;
+    std::call_once(once, [] {
+        (void)hipFuncSetAttribute(reinterpret_cast<const void *>(&k_mx4_dx_rows<RM, NW>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+    });
+    hipLaunchKernelGGL((k_mx4_dx_rows<RM, NW>), dim3((unsigned)tiles), dim3(64 * NW), LDS, st, a);
+    return done();
+}
+
+enum Mx4Form { MX4_ROWS_16, MX4_ROWS_32, MX4_ROWS_64, MX4_64x64, MX4_64x128, MX4_128x128, MX4_128x256, MX4_256x256 };
+
+static Mx4Form linear_form(bool x4, int M, int K, int N)
+{
+    if (M <= 16) return MX4_ROWS_16;
+    if (M <= 32) return MX4_ROWS_32;
+    if (M <= 128) return MX4_ROWS_64;
+    return MX4_256x256;
+}
+static Mx4Form dx_form(int M, int K, int N)
+{
+    return M <= 16 ? MX4_ROWS_16 : M <= 512 ? MX4_ROWS_32 : MX4_256x256;
+}
+
 template <bool X4> static pac_status launch_linear(const Mx4Args &a, hipStream_t st)
 {
     (void)hipGetLastError();
-    if (a.M > 128) return launch_tiles<Mx4Tile<X4, 2, 4, 4, 2, X4 ? 4 : 3>>(a, st);
-    const int64_t nt = ((int64_t)a.N + 15) / 16;
-    const int rm = a.M <= 16 ? 1 : a.M <= 32 ? 2 : 4;
-    const int64_t tiles = tile_count(nt, ((int64_t)a.M + 16 * rm - 1) / (16 * rm));
-    if (tiles < 0) return PAC_ERR_UNSUPPORTED;
-    const dim3 g((unsigned)tiles);
-    if (rm == 1) hipLaunchKernelGGL((k_mx4_rows<X4, 1, 8>), g, dim3(512), 0, st, a);
-    else if (rm == 2) hipLaunchKernelGGL((k_mx4_rows<X4, 2, 8>), g, dim3(512), 0, st, a);
-    else hipLaunchKernelGGL((k_mx4_rows<X4, 4, 8>), g, dim3(512), 0, st, a);
-    return done();
+    const Mx4Form form = linear_form(X4, a.M, a.K, a.N);
+    switch (form) {
+    case MX4_ROWS_16: return launch_rows<X4, 1>(a, st);
+    case MX4_ROWS_32: return launch_rows<X4, 2>(a, st);
+    case MX4_ROWS_64: return launch_rows<X4, 4>(a, st);
+    case MX4_64x64: return launch_tiles<Mx4Tile<X4, 2, 2, 1, 1, 4>>(a, st);
+    case MX4_64x128: return launch_tiles<Mx4Tile<X4, 2, 2, 1, 2, 4>>(a, st);
+    case MX4_128x128: return launch_tiles<Mx4Tile<X4, 2, 2, 2, 2, X4 ? 4 : 3>>(a, st);
+    case MX4_128x256: return launch_tiles<Mx4Tile<X4, 2, 4, 2, 2, 4>>(a, st);
+    default: return launch_tiles<Mx4Tile<X4, 2, 4, 4, 2, X4 ? 4 : 3>>(a, st);
+    }
+}
+
+static pac_status launch_dx(const Mx4Args &a, hipStream_t st)
+{
+    (void)hipGetLastError();
+    const Mx4Form form = dx_form(a.M, a.K, a.N);
+    switch (form) {
+    case MX4_ROWS_16: return launch_dx_rows<1>(a, st);
+    case MX4_ROWS_32: return launch_dx_rows<2>(a, st);
+    case MX4_64x128: return launch_dx_tiles<Mx4DxTile<2, 4, 1, 2, 5>>(a, st);
+    case MX4_128x256: return launch_dx_tiles<Mx4DxTile<2, 4, 2, 2, 3>>(a, st);
+    default: return launch_dx_tiles<Mx4DxTile<4, 2, 2, 4, 2>>(a, st);
+    }
 }
 
 } // namespace pac
@@ -899,15 +1046,7 @@ pac_status pac_mx4_linear_dx(const void *dy, int32_t M, int32_t N, int64_t dy_st
     if (M == 0) return PAC_OK;
     const Mx4Args a{dy, nullptr, dy_stride, codes, scales, M, K, N, code_pitch(K), scale_pitch(K), nullptr, 0, dx, dx_dtype == PAC_F32,
                     dx_stride};
-    (void)hipGetLastError();
-    if (M > 512) return launch_dx_tiles<Mx4DxTile<4, 2, 2, 4, 2>>(a, static_cast<hipStream_t>(hip_stream));
-    const int rm = M <= 16 ? 1 : 2;
-    const int64_t tiles = tile_count(((int64_t)K + 127) / 128, ((int64_t)M + 16 * rm - 1) / (16 * rm));
-    if (tiles < 0) return PAC_ERR_UNSUPPORTED;
-    hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    if (rm == 1) hipLaunchKernelGGL((k_mx4_dx_rows<1, 4>), dim3((unsigned)tiles), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((k_mx4_dx_rows<2, 4>), dim3((unsigned)tiles), dim3(256), 0, st, a);
-    return done();
+    return launch_dx(a, static_cast<hipStream_t>(hip_stream));
 }
 
 } // extern "C"
