@@ -304,9 +304,9 @@ template <int RM, int NW> __global__ __launch_bounds__(64 * NW) void k_mx4_dx_ro
 {
     constexpr int TM = 16 * RM, PITCH = 132;
     extern __shared__ __attribute__((aligned(16))) float red[]; // [NW][TM][PITCH]
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, q = lane >> 4;
     const int kt = (a.K + 127) / 128, kc0 = (int)(blockIdx.x % kt) * 128, m0 = (int)(blockIdx.x / kt) * TM;
-    const uint8_t *wc = a.w + kc0 / 2 + 4 * i, *sc = a.ws + kc0 / 32 + (i >> 2);
+    const int64_t w_at = 8 * q * a.wp + kc0 / 2 + 4 * i, s_at = 8 * q * a.sp + kc0 / 32 + (i >> 2); // this lane's place in a step
     f32x4 acc[8][RM];
     const bf16_t *dyr[RM];
 #pragma unroll
@@ -316,19 +316,32 @@ template <int RM, int NW> __global__ __launch_bounds__(64 * NW) void k_mx4_dx_ro
         for (int c = 0; c < 8; ++c) acc[c][r] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     const int steps = (a.N + 31) / 32, last = (a.N + 7) / 8 * 8 - 8;
-    // the coming step's operands are under way while the present one's are multiplied; past the end: the last step's, unused
+    // The coming step's operands are under way while the present one's are multiplied; past the end: the last step's, unused.  Rows'
+    // addresses are a scalar's work (at an address a lane and row the vector units bound small M).
     uint32_t wn[8], sn[8];
     u32x4 dn[RM];
     auto fetch = [&](int s) {
-        const int n0 = 32 * min(s, steps - 1) + 8 * q;
+        s = min(s, steps - 1);
+        if (32 * s + 32 <= a.N) {
+            const uint8_t *w0 = a.w + 32 * s * a.wp, *s0 = a.ws + 32 * s * a.sp;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int64_t n = min(n0 + e, a.N - 1); // past the end dy counts as zero
-            wn[e] = *reinterpret_cast<const uint32_t *>(wc + n * a.wp);
-            sn[e] = sc[n * a.sp];
+            for (int e = 0; e < 8; ++e) {
+                wn[e] = *reinterpret_cast<const uint32_t *>(w0 + e * a.wp + w_at);
+                sn[e] = *(s0 + e * a.sp + s_at);
+            }
+#pragma unroll
+            for (int r = 0; r < RM; ++r) dn[r] = *reinterpret_cast<const u32x4 *>(dyr[r] + 32 * s + 8 * q);
+        } else {
+            const int n0 = 32 * s + 8 * q;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int64_t n = min(n0 + e, a.N - 1); // past the end dy counts as zero
+                wn[e] = *reinterpret_cast<const uint32_t *>(a.w + n * a.wp + kc0 / 2 + 4 * i);
+                sn[e] = a.ws[n * a.sp + kc0 / 32 + (i >> 2)];
+            }
+#pragma unroll
+            for (int r = 0; r < RM; ++r) dn[r] = mx4_keep(*reinterpret_cast<const u32x4 *>(dyr[r] + min(n0, last)), a.N - n0);
         }
-#pragma unroll
-        for (int r = 0; r < RM; ++r) dn[r] = *reinterpret_cast<const u32x4 *>(dyr[r] + min(n0, last));
     };
     fetch(wave);
     for (int s = wave; s < steps; s += NW) {
@@ -338,7 +351,7 @@ template <int RM, int NW> __global__ __launch_bounds__(64 * NW) void k_mx4_dx_ro
 #pragma unroll
         for (int e = 0; e < 8; ++e) w[e] = wn[e], f[e] = mx4_scale(sn[e]);
 #pragma unroll
-        for (int r = 0; r < RM; ++r) d[r] = 32 * s + 32 > a.N ? mx4_keep(dn[r], a.N - (32 * s + 8 * q)) : dn[r];
+        for (int r = 0; r < RM; ++r) d[r] = dn[r];
         fetch(s + NW);
         mx4_columns(w, f, col);
 #pragma unroll
@@ -722,8 +735,9 @@ template <class TL> __global__ __launch_bounds__(64 * TL::NW, 2) void k_mx4_dx_t
         const int64_t n = min(64 * min(step + 1, nsteps - 1) + piece * 32 + lane / 2, a.N - 1);
         dma4_at(a.ws + n * a.sp + k0 / 32 + 4 * (lane & 1), lds0 + slot * TL::STAGE_BYTES + TL::S_AT + piece * 256);
     };
-    // this thread's part of turning W: columns 8 cg .. 8 cg + 7, rows 4 ng .. 4 ng + 3 of a step
-    const int cg = threadIdx.x & 31, ng = threadIdx.x >> 5;
+    // this thread's part of turning W: columns 8 cg .. 8 cg + 7, rows 4 ng .. 4 ng + 3 of a step; 32 lanes are 16 cg and two ng, whose
+    // 8-byte writes fill each other's 16 bytes (32 cg of one ng met every second bank twice)
+    const int cg = (lane & 15) + 16 * g, ng = 2 * wave + ((lane >> 4) & 1);
     const int wat = cg * 128 + (((ng >> 1) ^ mx4_swz<128>(cg)) << 4) + 8 * (ng & 1); // where column 8 cg goes; the next: 4096 bytes on
     uint32_t wr[4], sr[4];
     auto turn = [&](auto c, char *to) __attribute__((always_inline)) {
@@ -910,13 +924,12 @@ template <int RM> static pac_status launch_dx_rows(const Mx4Args &a, hipStream_t
     return done();
 }
 
-enum Mx4Form { MX4_ROWS_16, MX4_ROWS_32, MX4_ROWS_64, MX4_64x64, MX4_64x128, MX4_128x128, MX4_128x256, MX4_256x256 };
+enum Mx4Form { MX4_ROWS_16, MX4_ROWS_32, MX4_64x64, MX4_64x128, MX4_128x128, MX4_256x256 };
 
 static Mx4Form linear_form(bool x4, int M, int K, int N)
 {
     if (M <= 16) return MX4_ROWS_16;
     if (M <= 32) return MX4_ROWS_32;
-    if (M <= 128) return MX4_ROWS_64;
     return MX4_256x256;
 }
 static Mx4Form dx_form(int M, int K, int N)
@@ -931,11 +944,9 @@ template <bool X4> static pac_status launch_linear(const Mx4Args &a, hipStream_t
     switch (form) {
     case MX4_ROWS_16: return launch_rows<X4, 1>(a, st);
     case MX4_ROWS_32: return launch_rows<X4, 2>(a, st);
-    case MX4_ROWS_64: return launch_rows<X4, 4>(a, st);
     case MX4_64x64: return launch_tiles<Mx4Tile<X4, 2, 2, 1, 1, 4>>(a, st);
     case MX4_64x128: return launch_tiles<Mx4Tile<X4, 2, 2, 1, 2, 4>>(a, st);
     case MX4_128x128: return launch_tiles<Mx4Tile<X4, 2, 2, 2, 2, X4 ? 4 : 3>>(a, st);
-    case MX4_128x256: return launch_tiles<Mx4Tile<X4, 2, 4, 2, 2, 4>>(a, st);
     default: return launch_tiles<Mx4Tile<X4, 2, 4, 4, 2, X4 ? 4 : 3>>(a, st);
     }
 }
@@ -948,7 +959,7 @@ static pac_status launch_dx(const Mx4Args &a, hipStream_t st)
     case MX4_ROWS_16: return launch_dx_rows<1>(a, st);
     case MX4_ROWS_32: return launch_dx_rows<2>(a, st);
     case MX4_64x128: return launch_dx_tiles<Mx4DxTile<2, 4, 1, 2, 5>>(a, st);
-    case MX4_128x256: return launch_dx_tiles<Mx4DxTile<2, 4, 2, 2, 3>>(a, st);
+    case MX4_128x128: return launch_dx_tiles<Mx4DxTile<2, 4, 2, 2, 3>>(a, st);
     default: return launch_dx_tiles<Mx4DxTile<4, 2, 2, 4, 2>>(a, st);
     }
 }
