@@ -73,6 +73,15 @@ pac_status pac_mx4_linear_dx(const void *dy /*DEVICE*/, int32_t M, int32_t N, in
                              const uint8_t *codes /*DEVICE*/, const uint8_t *scales /*DEVICE*/, int32_t K,
                              void *dx /*DEVICE*/, int32_t dx_dtype, int64_t dx_stride, void *hip_stream);
 
+/* Which output tiles a product runs on (the same result up to the order of fp32 sums; host logic, for measurements and tests that
+ * have to know which form they ran): out[0] rows of M, out[1] columns of N (of K for dx) per tile.  Tiles of 16 and 32 rows deal
+ * the contraction over a workgroup's wavefronts, larger ones stream it through LDS.
+ * Errors: NULL, SHAPE (product, M, K or N < 1), UNSUPPORTED as above. */
+#define PAC_MX4_LINEAR 0
+#define PAC_MX4_LINEAR_X4 1
+#define PAC_MX4_LINEAR_DX 2
+pac_status pac_mx4_tiles(int32_t product, int32_t M, int32_t K, int32_t N, int32_t out[2] /*HOST*/);
+
 #ifdef __cplusplus
 }
 #endif

@@ -37,11 +37,12 @@ EXPORTS = [
     "pac_tier_window_bytes", "pac_tier_fill", "pac_tier_stage", "pac_adapter_loss_grad_staged", "pac_adapter_step_staged",
     "pac_ladder_param_count", "pac_ladder_workspace_bytes", "pac_ladder_tiles", "pac_ladder_loss_grad", "pac_ladder_step",
     "pac_mx4_code_pitch", "pac_mx4_scale_pitch", "pac_mx4_quantize", "pac_mx4_dequantize", "pac_mx4_linear", "pac_mx4_linear_x4",
-    "pac_mx4_linear_dx",
+    "pac_mx4_linear_dx", "pac_mx4_tiles",
     "pac_block_norm_forward", "pac_block_norm_workspace_bytes", "pac_block_norm_backward",
 ]
 PAC_STATIC_WORKSPACE_BYTES = 64 << 20
 PAC_MX4_ACT_NONE, PAC_MX4_ACT_GELU = 0, 1
+PAC_MX4_LINEAR, PAC_MX4_LINEAR_X4, PAC_MX4_LINEAR_DX = 0, 1, 2
 
 
 class pac_config(C.Structure):
@@ -188,6 +189,8 @@ def lib():
         L.pac_mx4_linear_x4.argtypes = [vp, vp, i32, i32, vp, vp, i32, vp, i32, vp, i32, i64, vp]
         L.pac_mx4_linear_dx.restype = C.c_int
         L.pac_mx4_linear_dx.argtypes = [vp, i32, i32, i64, vp, vp, i32, vp, i32, i64, vp]
+        L.pac_mx4_tiles.restype = C.c_int
+        L.pac_mx4_tiles.argtypes = [i32, i32, i32, i32, C.POINTER(i32)]
         L.pac_block_norm_forward.restype = C.c_int
         L.pac_block_norm_forward.argtypes = [C.POINTER(pac_block_norm), i64, vp, vp, vp, vp, vp]
         L.pac_block_norm_workspace_bytes.restype = i64
@@ -524,6 +527,13 @@ def pac_mx4_linear_dx(dy_ptr, M: int, N: int, dy_stride: int, codes_ptr, scales_
                       stream=0) -> None:
     _check(lib().pac_mx4_linear_dx(dy_ptr, M, N, dy_stride, codes_ptr, scales_ptr, K, dx_ptr, dx_dtype, dx_stride, stream),
            "pac_mx4_linear_dx")
+
+
+def pac_mx4_tiles(product: int, M: int, K: int, N: int):
+    """(rows, columns) of the output tiles a product runs on (host logic)."""
+    out = (C.c_int32 * 2)()
+    _check(lib().pac_mx4_tiles(product, M, K, N, out), "pac_mx4_tiles")
+    return int(out[0]), int(out[1])
 
 
 def pac_block_norm_forward(b: pac_block_norm, rows: int, x_ptr, o_ptr, y_ptr, n_ptr, stream=0) -> None:

@@ -96,3 +96,18 @@ def test_norm_calls_refuse():
     assert g(b=norm(), dn=None, dy=None) == g(b=norm(), dn=A) == g(b=norm(), dn=None, wp=None, ga=None, wn=None) == pb.PAC_ERR_NULL
     assert g(rows=-1) == pb.PAC_ERR_RANGE and g(n=need - 1) == pb.PAC_ERR_WORKSPACE
     assert g(ws=A + 8) == g(dy=A + 2) == g(do=A + 2) == g(wp=A + 2) == g(re=A + 1) == pb.PAC_ERR_ALIGN
+
+
+def test_tiles_of_the_products():
+    """Host logic: every form of the three products is taken somewhere, and the line between them follows the sizes."""
+    t = pb.pac_mx4_tiles
+    assert t(0, 1, 4096, 4096) == t(1, 1, 4096, 4096) == (16, 16) and t(2, 1, 4096, 4096) == (16, 128)
+    assert t(0, 4096, 4096, 4096) == t(1, 4096, 4096, 4096) == t(2, 4096, 4096, 4096) == (256, 256)
+    assert t(0, 64, 4096, 4096) == (64, 64) and t(0, 333, 1024, 4096) == (64, 128) and t(0, 1024, 2048, 4096) == (128, 128)
+    big = 1 << 30
+    assert t(0, big, big, big) == t(2, big, big, big) == (256, 256)
+    out = (C.c_int32 * 2)()
+    L = pb.lib()
+    assert L.pac_mx4_tiles(0, 1, 1, 1, None) == pb.PAC_ERR_NULL
+    assert L.pac_mx4_tiles(3, 1, 1, 1, out) == L.pac_mx4_tiles(-1, 1, 1, 1, out) == L.pac_mx4_tiles(0, 0, 1, 1, out) == pb.PAC_ERR_SHAPE
+    assert L.pac_mx4_tiles(0, 1, big + 1, 1, out) == pb.PAC_ERR_UNSUPPORTED

@@ -160,6 +160,40 @@ def test_input_grad(M, K, N):
         assert (store[:, K:] == 5.0).all()
 
 
+# Every form of the three products on tiles, steps and rows that end raggedly, and on sizes that divide; contractions that go round
+# the rings of LDS stages more than once, and ones shorter than a ring
+FORMS = [(0, (32, 16), 17, 31, 8721), (0, (64, 64), 33, 521, 8510), (0, (64, 64), 700, 100, 3001), (0, (64, 128), 66, 779, 8903),
+         (0, (64, 128), 2050, 130, 4111), (0, (128, 128), 348, 2065, 7235), (0, (128, 128), 1024, 2048, 4096), (0, (256, 256), 4282, 523, 2958),
+         (0, (256, 256), 4096, 512, 4096),
+         (1, (32, 16), 2079, 30, 18), (1, (64, 64), 33, 514, 8834), (1, (64, 64), 300, 2049, 1030), (1, (128, 128), 711, 1153, 7671),
+         (1, (256, 256), 4562, 515, 2978), (1, (256, 256), 4096, 512, 4096),
+         (2, (32, 128), 5963, 30, 1123), (2, (64, 256), 5011, 286, 517), (2, (64, 256), 1024, 2049, 1000), (2, (128, 256), 5704, 562, 540),
+         (2, (256, 256), 5447, 1482, 500), (2, (256, 256), 4096, 4096, 256)]
+
+
+@pytest.mark.parametrize("product,tile,M,K,N", FORMS)
+def test_products_on_each_form(product, tile, M, K, N):
+    assert pb.pac_mx4_tiles(product, M, K, N) == tile
+    rng = np.random.default_rng(M + K + N)
+    codes, scales, w = layer(rng, N, K)
+    lin = rt.Mx4Linear(codes, scales, K)
+    x = rows_of(rng, M, N if product == 2 else K)
+    xv = host(x)
+    if product == 1:
+        xv = bo.values(*bo.quantize(xv), K)
+    ref, absum = bo.linear(xv, w.T if product == 2 else w)
+    for dtype in ("f32", "bf16"):
+        wide = ref.shape[1]
+        store = torch.full((M, wide + 3), 5.0, dtype=DT[dtype], device="cuda")  # rows that no whole store fits, too
+        for y in (store[:, :wide], torch.empty(M, wide, dtype=DT[dtype], device="cuda")):
+            if product == 2:
+                lin.input_grad(x, y)
+            else:
+                lin.forward(x, y, x4=product == 1)
+            check(host(y), ref, bar(ref, absum, N if product == 2 else K, dtype))
+        assert (store[:, wide:] == 5.0).all()
+
+
 def test_input_grad_is_the_forward_products_gradient():
     """<dy, x W^T> = <dx, x> for the library's own two products, with W only ever in the stored form."""
     rng = np.random.default_rng(5)
