@@ -202,59 +202,57 @@ class TieredSession(Session):
 
 
 # ---- blocks of the frozen backbone (include/pac_mx4.h, include/pac_norm.h) ------------------------------------------
-def _kind(t) -> int:
-    if t.dtype == torch.bfloat16:
-        return pb.PAC_BF16
-    if t.dtype == torch.float32:
-        return pb.PAC_F32
-    raise ValueError(f"bfloat16 or float32 is wanted, not {t.dtype}")
+# The library takes addresses alone, so what they stand for is checked here.  A single token's kernel takes 4 us: the checks are
+# written to cost little beside it.
+_KIND = {torch.bfloat16: pb.PAC_BF16, torch.float32: pb.PAC_F32}
 
 
-def _matrix(t, name: str, shape=None, dtype=None, device=None):
-    """The row stride of a device matrix whose columns are neighbours (the launch takes addresses alone, so what they stand
-    for is checked here)."""
-    have, dev = t.shape, t.device
-    if len(have) != 2 or dev.type != "cuda" or (device is not None and dev != device):
-        raise ValueError(f"{name}: a matrix on the device is wanted")
-    if shape is not None and have != shape:
-        raise ValueError(f"{name}: shape {shape} is wanted, not {tuple(have)}")
-    if dtype is not None and t.dtype != dtype:
-        raise ValueError(f"{name}: {dtype} is wanted, not {t.dtype}")
-    row, col = t.stride()
-    if col != 1 and have[1] > 1:
+def _rows_of(t, name: str, rows: int, cols: int, device):
+    """(row stride, pac_dtype) of a [rows][cols] device matrix with neighbouring columns."""
+    kind = _KIND.get(t.dtype)
+    if kind is None or t.device != device or device.type != "cuda" or t.shape != (rows, cols):
+        raise ValueError(f"{name}: bfloat16 or float32, ({rows}, {cols}), on {device} (a GPU) is wanted, not {t.dtype}, {tuple(t.shape)}, "
+                         f"on {t.device}")
+    stride = t.stride()
+    if stride[1] != 1 and cols > 1:
         raise ValueError(f"{name}: neighbouring columns are wanted")
-    return row if have[0] > 1 else max(row, have[1])
+    return (stride[0] if rows > 1 else max(stride[0], cols)), kind
 
 
-def _stored(codes, scales, cols: int, rows=None, device=None):
-    rows = codes.shape[0] if rows is None else rows
-    for t, pitch, name in ((codes, pb.pac_mx4_code_pitch(cols), "codes"), (scales, pb.pac_mx4_scale_pitch(cols), "scales")):
-        _matrix(t, name, (rows, pitch), torch.uint8, device)
-        if not t.is_contiguous():
-            raise ValueError(f"{name}: a dense matrix is wanted")
-
-
-def _padded_stride(t, name: str, cols: int, device):
+def _chunked_rows(t, name: str, rows: int, cols: int, device) -> int:
     """The row stride of a bf16 matrix that is read in 16-byte pieces, in the last row too."""
-    stride = _matrix(t, name, (t.shape[0], cols), torch.bfloat16, device)
-    pad = (cols + 7) // 8 * 8
-    if t.shape[0] == 1:
-        stride = max(stride, pad) // 8 * 8
-    if t.shape[0] and cols % 8:
-        after = t.storage_offset() + (t.shape[0] - 1) * stride + pad
-        if after * 2 > t.untyped_storage().nbytes():
+    stride, kind = _rows_of(t, name, rows, cols, device)
+    if kind != pb.PAC_BF16:
+        raise ValueError(f"{name}: bfloat16 is wanted")
+    if cols % 8:
+        pad = (cols + 7) // 8 * 8
+        if rows == 1:
+            stride = pad
+        if rows and 2 * (t.storage_offset() + (rows - 1) * stride + pad) > t.untyped_storage().nbytes():
             raise ValueError(f"{name}: rows are read up to a multiple of 8 columns, the last one too")
+    elif rows == 1:
+        stride = cols
     return stride
 
 
-def _launch(device, call, *args) -> None:
-    """call(*args, the device's current stream), with that device current (switching costs more than looking)."""
+def _stored(codes, scales, rows: int, cols: int, device) -> None:
+    for t, pitch, name in ((codes, pb.pac_mx4_code_pitch(cols), "codes"), (scales, pb.pac_mx4_scale_pitch(cols), "scales")):
+        if t.dtype != torch.uint8 or t.shape != (rows, pitch) or t.device != device or not t.is_contiguous():
+            raise ValueError(f"{name}: dense uint8, ({rows}, {pitch}), on {device} is wanted")
+
+
+def _call(device, name: str, *args) -> None:
+    """The library's function of that name on args and the device's current stream, with that device current."""
     i = device.index
-    if torch.cuda.current_device() == i:
-        call(*args, torch._C._cuda_getCurrentRawStream(i))
-    else:
+    if torch._C._cuda_getDevice() != i:
         with torch.cuda.device(i):
-            call(*args, torch._C._cuda_getCurrentRawStream(i))
+            return _call(device, name, *args)
+    status = getattr(_lib(), name)(*args, torch._C._cuda_getCurrentRawStream(i))
+    if status:
+        raise pb.PacError(status, name)
+
+
+_lib = pb.lib
 
 
 def _ptr(t):
@@ -269,30 +267,34 @@ def mx4_empty(rows: int, cols: int, device="cuda:0"):
 
 def mx4_quantize(x, codes, scales) -> None:
     """x (bf16 or fp32, any row stride) into the stored form."""
-    stride = _matrix(x, "x")
-    _stored(codes, scales, x.shape[1], x.shape[0], x.device)
-    _launch(x.device, pb.pac_mx4_quantize, x.data_ptr(), _kind(x), x.shape[0], x.shape[1], stride, codes.data_ptr(), scales.data_ptr())
+    rows, cols = x.shape
+    stride, kind = _rows_of(x, "x", rows, cols, x.device)
+    _stored(codes, scales, rows, cols, x.device)
+    _call(x.device, "pac_mx4_quantize", x.data_ptr(), kind, rows, cols, stride, codes.data_ptr(), scales.data_ptr())
 
 
 def mx4_dequantize(codes, scales, out) -> None:
     """The values a stored matrix stands for, into out (bf16 or fp32, both exact)."""
-    stride = _matrix(out, "out")
-    _stored(codes, scales, out.shape[1], out.shape[0], out.device)
-    _launch(out.device, pb.pac_mx4_dequantize, codes.data_ptr(), scales.data_ptr(), out.shape[0], out.shape[1], out.data_ptr(), _kind(out),
-            stride)
+    rows, cols = out.shape
+    stride, kind = _rows_of(out, "out", rows, cols, out.device)
+    _stored(codes, scales, rows, cols, out.device)
+    _call(out.device, "pac_mx4_dequantize", codes.data_ptr(), scales.data_ptr(), rows, cols, out.data_ptr(), kind, stride)
 
 
 class Mx4Linear:
     """A frozen linear layer with weights in the stored form: y = act(x W^T + bias), and dx = dy W on the way back."""
 
     def __init__(self, codes, scales, K: int, bias=None):
-        _stored(codes, scales, K)
-        self.codes, self.scales, self.bias = codes, scales, bias
         self.N, self.K, self.dev = codes.shape[0], K, codes.device
+        _stored(codes, scales, self.N, K, self.dev)
+        if self.dev.type != "cuda":
+            raise ValueError("codes: on a GPU")
         if bias is not None and (bias.shape != (self.N,) or bias.dtype != torch.float32 or bias.device != self.dev or not bias.is_contiguous()):
             raise ValueError("bias: float32, one value an output, on the weights' device")
+        self.codes, self.scales, self.bias = codes, scales, bias
+        # the tail of every product's arguments: W, and the bias
         self._w = (codes.data_ptr(), scales.data_ptr())
-        self._b = None if bias is None else bias.data_ptr()
+        self._wb = self._w + (self.N, _ptr(bias))
 
     @classmethod
     def from_weights(cls, w, bias=None):
@@ -302,28 +304,29 @@ class Mx4Linear:
         return cls(codes, scales, w.shape[1], bias)
 
     def forward(self, x, y, gelu: bool = False, x4: bool = False) -> None:
-        """x [M][K] bf16, rows on 16 bytes; y [M][N] bf16 or fp32.  x4: x is quantised too, and the product runs on 4-bit operands."""
-        M = x.shape[0]
-        sy = _matrix(y, "y", (M, self.N), None, self.dev)
+        """x [M][K] bf16, rows on 16 bytes; y [M][N] bf16 or fp32.  x4: x (bf16 or fp32, any row stride) is quantised too, and the
+        product runs on 4-bit operands."""
+        M, dev = x.shape[0], self.dev
+        sy, kind = _rows_of(y, "y", M, self.N, dev)
         act = pb.PAC_MX4_ACT_GELU if gelu else pb.PAC_MX4_ACT_NONE
         if x4:
-            sx = _matrix(x, "x", (M, self.K), None, self.dev)
-            # x in the stored form lives for this call, on this stream: codes (whole multiples of 128 bytes), then scales
+            sx, xkind = _rows_of(x, "x", M, self.K, dev)
+            # x in the stored form lives for this call, on this stream: codes (whole multiples of 128 bytes a row), then scales
             c = M * self.codes.shape[1]
-            buf = torch.empty(c + M * self.scales.shape[1], dtype=torch.uint8, device=self.dev)
-            c, s = buf.data_ptr(), buf.data_ptr() + c
-            _launch(self.dev, pb.pac_mx4_quantize, x.data_ptr(), _kind(x), M, self.K, sx, c, s)
-            _launch(self.dev, pb.pac_mx4_linear_x4, c, s, M, self.K, *self._w, self.N, self._b, act, y.data_ptr(), _kind(y), sy)
+            buf = torch.empty(c + M * self.scales.shape[1], dtype=torch.uint8, device=dev)
+            at = buf.data_ptr()
+            _call(dev, "pac_mx4_quantize", x.data_ptr(), xkind, M, self.K, sx, at, at + c)
+            _call(dev, "pac_mx4_linear_x4", at, at + c, M, self.K, *self._wb, act, y.data_ptr(), kind, sy)
         else:
-            sx = _padded_stride(x, "x", self.K, self.dev)
-            _launch(self.dev, pb.pac_mx4_linear, x.data_ptr(), M, self.K, sx, *self._w, self.N, self._b, act, y.data_ptr(), _kind(y), sy)
+            sx = _chunked_rows(x, "x", M, self.K, dev)
+            _call(dev, "pac_mx4_linear", x.data_ptr(), M, self.K, sx, *self._wb, act, y.data_ptr(), kind, sy)
 
     def input_grad(self, dy, dx) -> None:
         """dy [M][N] bf16, rows on 16 bytes; dx [M][K] bf16 or fp32."""
-        M = dy.shape[0]
-        sdy = _padded_stride(dy, "dy", self.N, self.dev)
-        sdx = _matrix(dx, "dx", (M, self.K), None, self.dev)
-        _launch(self.dev, pb.pac_mx4_linear_dx, dy.data_ptr(), M, self.N, sdy, *self._w, self.K, dx.data_ptr(), _kind(dx), sdx)
+        M, dev = dy.shape[0], self.dev
+        sdy = _chunked_rows(dy, "dy", M, self.N, dev)
+        sdx, kind = _rows_of(dx, "dx", M, self.K, dev)
+        _call(dev, "pac_mx4_linear_dx", dy.data_ptr(), M, self.N, sdy, *self._w, self.K, dx.data_ptr(), kind, sdx)
 
 
 class BlockNorm:
@@ -332,6 +335,7 @@ class BlockNorm:
 
     def __init__(self, d: int, layer: bool = False, eps: float = 1e-5, w_post=None, b_post=None, gate=None, res=None, w_pre=None,
                  b_pre=None):
+        # in the order of the library's structure and of its gradients
         self.d, self.params = d, dict(w_post=w_post, b_post=b_post, gate=gate, res=res, w_pre=w_pre, b_pre=b_pre)
         self.dev = None
         for name, p in self.params.items():
@@ -343,33 +347,34 @@ class BlockNorm:
             if self.dev not in (None, p.device):
                 raise ValueError(f"{name}: on another device than the parameters before it")
             self.dev = p.device
-        self._b = {kind: pb.pac_block_norm(d, kind, int(layer), 0 if gate is None else gate.shape[0], eps,
-                                           *(_ptr(self.params[k]) for k in ("w_post", "b_post", "gate", "res", "w_pre", "b_pre")))
-                   for kind in (pb.PAC_BF16, pb.PAC_F32)}
+        self._b = {dtype: pb.pac_block_norm(d, kind, int(layer), 0 if gate is None else gate.shape[0], eps, *(_ptr(p) for p in self.params.values()))
+                   for dtype, kind in _KIND.items()}
 
-    def _rows(self, x, *others):
+    def _rows(self, x, *others) -> int:
         shape, dtype, dev = x.shape, x.dtype, x.device
-        if len(shape) != 2 or shape[1] != self.d or dev.type != "cuda" or not x.is_contiguous() or self.dev not in (None, dev):
-            raise ValueError(f"states: dense, [rows][{self.d}], on the parameters' device")
+        if len(shape) != 2 or shape[1] != self.d or dtype not in _KIND or dev.type != "cuda" or not x.is_contiguous() or self.dev not in (None, dev):
+            raise ValueError(f"states: dense, bfloat16 or float32, [rows][{self.d}], on the parameters' device")
         for t in others:
             if t is not None and (t.shape != shape or t.dtype != dtype or t.device != dev or not t.is_contiguous()):
                 raise ValueError(f"states: dense, [rows][{self.d}], of one type, on one device")
         return shape[0]
 
     def forward(self, x, o=None, y=None, n=None) -> None:
+        """y and n of x and a block's output o (None: no block yet), into the buffers given."""
         rows = self._rows(x, o, y, n)
-        _launch(x.device, pb.pac_block_norm_forward, self._b[_kind(x)], rows, x.data_ptr(), _ptr(o), _ptr(y), _ptr(n))
+        _call(x.device, "pac_block_norm_forward", self._b[x.dtype], rows, x.data_ptr(), _ptr(o), _ptr(y), _ptr(n))
 
     def backward(self, x, o, dy, dn, dx=None, do=None, dparams=None) -> None:
-        """Gradients; dparams: {name: float32 tensor like the parameter} for those that are wanted."""
+        """Gradients, given dy (None: zero) and dn (None without w_pre), into the buffers given; dparams: {name: float32 tensor like
+        the parameter} for those that are wanted."""
         rows = self._rows(x, o, dy, dn, dx, do)
-        dparams = dparams or {}
-        for name, g in dparams.items():
-            p = self.params.get(name)
-            if p is None or g.shape != p.shape or g.dtype != torch.float32 or g.device != p.device or not g.is_contiguous():
-                raise ValueError(f"d{name}: like the parameter of that name")
-        b = self._b[_kind(x)]
-        need = pb.pac_block_norm_workspace_bytes(b, rows) if dparams else 0
-        ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
-        _launch(x.device, pb.pac_block_norm_backward, b, rows, x.data_ptr(), _ptr(o), _ptr(dy), _ptr(dn), _ptr(dx), _ptr(do),
-                *(_ptr(dparams.get(k)) for k in ("w_post", "b_post", "gate", "res", "w_pre", "b_pre")), _ptr(ws), need)
+        b, grads, ws, need = self._b[x.dtype], [None] * 6, None, 0
+        if dparams:
+            for name, g in dparams.items():
+                p = self.params.get(name)
+                if p is None or g.shape != p.shape or g.dtype != torch.float32 or g.device != p.device or not g.is_contiguous():
+                    raise ValueError(f"d{name}: like the parameter of that name")
+            grads = [_ptr(dparams.get(name)) for name in self.params]
+            need = pb.pac_block_norm_workspace_bytes(b, rows)
+            ws = torch.empty(need, dtype=torch.uint8, device=x.device)  # for this call, on this stream
+        _call(x.device, "pac_block_norm_backward", b, rows, x.data_ptr(), _ptr(o), _ptr(dy), _ptr(dn), _ptr(dx), _ptr(do), *grads, _ptr(ws), need)
