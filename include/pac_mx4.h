@@ -67,6 +67,15 @@ pac_status pac_mx4_linear_x4(const uint8_t *x_codes /*DEVICE*/, const uint8_t *x
                              const float *bias /*DEVICE*/, int32_t act, void *y /*DEVICE*/, int32_t y_dtype,
                              int64_t y_stride, void *hip_stream);
 
+/* The same with x quantised in the call: x DEVICE [M][x_stride] of x_dtype, any alignment of its type; what pac_mx4_quantize and
+ * pac_mx4_linear_x4 give, bit for bit, few rows in one launch.  workspace DEVICE, 16-byte aligned, as many bytes as the function says
+ * (-1 on bad arguments); its contents are scratch.  Errors as above, and WORKSPACE. */
+int64_t pac_mx4_linear_qx_workspace_bytes(int32_t M, int32_t K);
+pac_status pac_mx4_linear_qx(const void *x /*DEVICE*/, int32_t x_dtype, int32_t M, int32_t K, int64_t x_stride,
+                             const uint8_t *codes /*DEVICE*/, const uint8_t *scales /*DEVICE*/, int32_t N,
+                             const float *bias /*DEVICE*/, int32_t act, void *y /*DEVICE*/, int32_t y_dtype, int64_t y_stride,
+                             void *workspace /*DEVICE*/, int64_t workspace_bytes, void *hip_stream);
+
 /* dx = dy W.  dy DEVICE bf16 [M][dy_stride], laid out and read as x above (with N for K); W [N][K] in the stored form;
  * dx DEVICE [M][dx_stride] of dx_dtype, any alignment of its type.  Errors as above. */
 pac_status pac_mx4_linear_dx(const void *dy /*DEVICE*/, int32_t M, int32_t N, int64_t dy_stride,

@@ -37,7 +37,7 @@ EXPORTS = [
     "pac_tier_window_bytes", "pac_tier_fill", "pac_tier_stage", "pac_adapter_loss_grad_staged", "pac_adapter_step_staged",
     "pac_ladder_param_count", "pac_ladder_workspace_bytes", "pac_ladder_tiles", "pac_ladder_loss_grad", "pac_ladder_step",
     "pac_mx4_code_pitch", "pac_mx4_scale_pitch", "pac_mx4_quantize", "pac_mx4_dequantize", "pac_mx4_linear", "pac_mx4_linear_x4",
-    "pac_mx4_linear_dx", "pac_mx4_tiles",
+    "pac_mx4_linear_qx_workspace_bytes", "pac_mx4_linear_qx", "pac_mx4_linear_dx", "pac_mx4_tiles",
     "pac_block_norm_forward", "pac_block_norm_workspace_bytes", "pac_block_norm_backward",
 ]
 PAC_STATIC_WORKSPACE_BYTES = 64 << 20
@@ -187,6 +187,10 @@ def lib():
         L.pac_mx4_linear.argtypes = [vp, i32, i32, i64, vp, vp, i32, vp, i32, vp, i32, i64, vp]
         L.pac_mx4_linear_x4.restype = C.c_int
         L.pac_mx4_linear_x4.argtypes = [vp, vp, i32, i32, vp, vp, i32, vp, i32, vp, i32, i64, vp]
+        L.pac_mx4_linear_qx_workspace_bytes.restype = i64
+        L.pac_mx4_linear_qx_workspace_bytes.argtypes = [i32, i32]
+        L.pac_mx4_linear_qx.restype = C.c_int
+        L.pac_mx4_linear_qx.argtypes = [vp, i32, i32, i32, i64, vp, vp, i32, vp, i32, vp, i32, i64, vp, i64, vp]
         L.pac_mx4_linear_dx.restype = C.c_int
         L.pac_mx4_linear_dx.argtypes = [vp, i32, i32, i64, vp, vp, i32, vp, i32, i64, vp]
         L.pac_mx4_tiles.restype = C.c_int
@@ -521,6 +525,16 @@ def pac_mx4_linear_x4(x_codes_ptr, x_scales_ptr, M: int, K: int, codes_ptr, scal
                       y_dtype: int, y_stride: int, stream=0) -> None:
     _check(lib().pac_mx4_linear_x4(x_codes_ptr, x_scales_ptr, M, K, codes_ptr, scales_ptr, N, bias_ptr, act, y_ptr, y_dtype,
                                    y_stride, stream), "pac_mx4_linear_x4")
+
+
+def pac_mx4_linear_qx_workspace_bytes(M: int, K: int) -> int:
+    return int(lib().pac_mx4_linear_qx_workspace_bytes(M, K))
+
+
+def pac_mx4_linear_qx(x_ptr, x_dtype: int, M: int, K: int, x_stride: int, codes_ptr, scales_ptr, N: int, bias_ptr, act: int, y_ptr,
+                      y_dtype: int, y_stride: int, ws_ptr, ws_bytes: int, stream=0) -> None:
+    _check(lib().pac_mx4_linear_qx(x_ptr, x_dtype, M, K, x_stride, codes_ptr, scales_ptr, N, bias_ptr, act, y_ptr, y_dtype, y_stride,
+                                   ws_ptr, ws_bytes, stream), "pac_mx4_linear_qx")
 
 
 def pac_mx4_linear_dx(dy_ptr, M: int, N: int, dy_stride: int, codes_ptr, scales_ptr, K: int, dx_ptr, dx_dtype: int, dx_stride: int,

@@ -214,8 +214,43 @@ __device__ __forceinline__ u32x4 mx4_keep(u32x4 v, int valid)
 // LDS in a fixed order.  Operands go from memory straight into registers: lane (i, q) holds row i's block of 32 number q of the
 // step, so that a lane has one scale, its 16 bytes of codes are one load, and four matrix instructions of 32 (one of 128 where x
 // is stored too) take eight codes of every lane's block each: the order of the sum does not matter to it.
-template <bool X4, int RM, int NW> __global__ __launch_bounds__(64 * NW) void k_mx4_rows(Mx4Args a)
+// What x is to it: bf16 rows, the stored form, or bf16 rows that are to count as their mx4 values: a lane holds whole blocks, so it
+// quantises them by itself, and the call needs no launch and no memory for x's stored form.
+enum { MX4_X16, MX4_X4, MX4_XQ };
+
+// 32 bf16 as e2m1 with one scale: what k_mx4_quant stores of them, bit for bit
+__device__ __forceinline__ uint32_t mx4_block(const u32x4 (&x)[4], i32x8 &codes)
 {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    u16x2 top = {0, 0}; // absolute values' bits order as the values do
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t b = x[j][e] & 0x7fff7fffu;
+            top = __builtin_elementwise_max(top, *reinterpret_cast<const u16x2 *>(&b));
+        }
+    const uint32_t ex = (uint32_t)max(top[0], top[1]) >> 7;
+    const bool none = ex == 255;
+    const uint32_t byte = none ? 255u : ex > 2 ? ex - 2 : 0u;
+    const float s = mx4_scale(byte);
+    codes = i32x8{0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        uint32_t w = 0;
+        const bf16x2 *p = reinterpret_cast<const bf16x2 *>(&x[j]);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, p[0], s, 0);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, p[1], s, 1);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, p[2], s, 2);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, p[3], s, 3);
+        codes[j] = none ? 0 : (int)w;
+    }
+    return byte;
+}
+
+template <int X, int RM, int NW> __global__ __launch_bounds__(64 * NW) void k_mx4_rows(Mx4Args a)
+{
+    constexpr bool X4 = X == MX4_X4;
     constexpr int TM = 16 * RM, PITCH = 20;
     __shared__ __attribute__((aligned(16))) float red[NW * TM * PITCH];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
@@ -244,6 +279,21 @@ template <bool X4, int RM, int NW> __global__ __launch_bounds__(64 * NW) void k_
                 const u32x4 x = *reinterpret_cast<const u32x4 *>(xr[r] + 64 * s);
                 const i32x8 xf = {(int)x[0], (int)x[1], (int)x[2], (int)x[3], 0, 0, 0, 0};
                 acc[r] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wf, xf, acc[r], 4, 4, 0, (int)sc, 0, (int)xsr[r][4 * s]);
+            }
+        } else if constexpr (X == MX4_XQ) {
+            const i32x8 wf = {(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0};
+            const int k0 = 128 * s + 32 * q;
+#pragma unroll
+            for (int r = 0; r < RM; ++r) {
+                u32x4 x[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[j] = *reinterpret_cast<const u32x4 *>(xr[r] + 2 * min(k0 + 8 * j, last));
+                if (128 * s + 128 > a.K)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[j] = mx4_keep(x[j], a.K - (k0 + 8 * j));
+                i32x8 xf;
+                const uint32_t xs = mx4_block(x, xf);
+                acc[r] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wf, xf, acc[r], 4, 4, 0, (int)sc, 0, (int)xs);
             }
         } else {
             bf16x8 wf[4];
@@ -914,11 +964,11 @@ template <class TL> static pac_status launch_dx_tiles(const Mx4Args &a, hipStrea
     return done();
 }
 
-template <bool X4, int RM> static pac_status launch_rows(const Mx4Args &a, hipStream_t st)
+template <int X, int RM> static pac_status launch_rows(const Mx4Args &a, hipStream_t st)
 {
     const int64_t tiles = tile_count(((int64_t)a.N + 15) / 16, ((int64_t)a.M + 16 * RM - 1) / (16 * RM));
     if (tiles < 0) return PAC_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL((k_mx4_rows<X4, RM, 8>), dim3((unsigned)tiles), dim3(512), 0, st, a);
+    hipLaunchKernelGGL((k_mx4_rows<X, RM, 8>), dim3((unsigned)tiles), dim3(512), 0, st, a);
     return done();
 }
 template <int RM> static pac_status launch_dx_rows(const Mx4Args &a, hipStream_t st)
@@ -982,8 +1032,8 @@ template <bool X4> static pac_status launch_linear(const Mx4Args &a, hipStream_t
     (void)hipGetLastError();
     const int form = linear_form(X4, a.M, a.K, a.N);
     switch (X4 ? kMx4LinearX4[form].cols + kMx4LinearX4[form].rows : kMx4Linear[form].cols + kMx4Linear[form].rows) {
-    case 16 + 16: return launch_rows<X4, 1>(a, st);
-    case 32 + 16: return launch_rows<X4, 2>(a, st);
+    case 16 + 16: return launch_rows<X4 ? MX4_X4 : MX4_X16, 1>(a, st);
+    case 32 + 16: return launch_rows<X4 ? MX4_X4 : MX4_X16, 2>(a, st);
     case 64 + 64: return launch_tiles<Mx4Tile<X4, 2, 2, 1, 1, 4>>(a, st);
     case 64 + 128: if constexpr (!X4) return launch_tiles<Mx4Tile<X4, 2, 2, 1, 2, 4>>(a, st); [[fallthrough]];
     case 128 + 128: return launch_tiles<Mx4Tile<X4, 2, 2, 2, 2, X4 ? 4 : 3>>(a, st);
@@ -1003,6 +1053,25 @@ static pac_status launch_dx(const Mx4Args &a, hipStream_t st)
     }
 }
 
+static pac_status launch_quant(const void *x, int32_t x_dtype, int64_t rows, int32_t cols, int64_t x_stride, uint8_t *codes, uint8_t *scales,
+                               hipStream_t st)
+{
+    const uint32_t upr = (uint32_t)(((int64_t)cols + 255) / 256), units = (uint32_t)rows * upr;
+    const dim3 g((units + 7) / 8), b(256);
+    uint32_t *c = reinterpret_cast<uint32_t *>(codes);
+    const bool vec = m_aligned(x, 16) && x_stride % (x_dtype == PAC_F32 ? 4 : 8) == 0;
+    if (x_dtype == PAC_F32) {
+        const float *p = static_cast<const float *>(x);
+        if (vec) hipLaunchKernelGGL((k_mx4_quant<float, true>), g, b, 0, st, p, units, upr, cols, x_stride, c, scales);
+        else hipLaunchKernelGGL((k_mx4_quant<float, false>), g, b, 0, st, p, units, upr, cols, x_stride, c, scales);
+    } else {
+        const bf16_t *p = static_cast<const bf16_t *>(x);
+        if (vec) hipLaunchKernelGGL((k_mx4_quant<bf16_t, true>), g, b, 0, st, p, units, upr, cols, x_stride, c, scales);
+        else hipLaunchKernelGGL((k_mx4_quant<bf16_t, false>), g, b, 0, st, p, units, upr, cols, x_stride, c, scales);
+    }
+    return done();
+}
+
 } // namespace pac
 
 using namespace pac;
@@ -1018,21 +1087,7 @@ pac_status pac_mx4_quantize(const void *x, int32_t x_dtype, int64_t rows, int32_
     const pac_status s = check_convert(x, x_dtype, rows, cols, x_stride, codes, scales);
     if (s != PAC_OK || rows == 0) return s;
     (void)hipGetLastError();
-    hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    const uint32_t upr = (uint32_t)(((int64_t)cols + 255) / 256), units = (uint32_t)rows * upr;
-    const dim3 g((units + 7) / 8), b(256);
-    uint32_t *c = reinterpret_cast<uint32_t *>(codes);
-    const bool vec = m_aligned(x, 16) && x_stride % (x_dtype == PAC_F32 ? 4 : 8) == 0;
-    if (x_dtype == PAC_F32) {
-        const float *p = static_cast<const float *>(x);
-        if (vec) hipLaunchKernelGGL((k_mx4_quant<float, true>), g, b, 0, st, p, units, upr, cols, x_stride, c, scales);
-        else hipLaunchKernelGGL((k_mx4_quant<float, false>), g, b, 0, st, p, units, upr, cols, x_stride, c, scales);
-    } else {
-        const bf16_t *p = static_cast<const bf16_t *>(x);
-        if (vec) hipLaunchKernelGGL((k_mx4_quant<bf16_t, true>), g, b, 0, st, p, units, upr, cols, x_stride, c, scales);
-        else hipLaunchKernelGGL((k_mx4_quant<bf16_t, false>), g, b, 0, st, p, units, upr, cols, x_stride, c, scales);
-    }
-    return done();
+    return launch_quant(x, x_dtype, rows, cols, x_stride, codes, scales, static_cast<hipStream_t>(hip_stream));
 }
 
 pac_status pac_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows, int32_t cols, void *out, int32_t out_dtype,
@@ -1084,6 +1139,42 @@ pac_status pac_mx4_linear_x4(const uint8_t *x_codes, const uint8_t *x_scales, in
     if (M == 0) return PAC_OK;
     return launch_linear<true>(Mx4Args{x_codes, x_scales, 0, codes, scales, M, K, N, code_pitch(K), scale_pitch(K), bias, act, y,
                                        y_dtype == PAC_F32, y_stride}, static_cast<hipStream_t>(hip_stream));
+}
+
+int64_t pac_mx4_linear_qx_workspace_bytes(int32_t M, int32_t K)
+{
+    if (M < 0 || K < 1 || M > kMx4Most || K > kMx4Most) return -1;
+    return (int64_t)M * (code_pitch(K) + scale_pitch(K));
+}
+
+pac_status pac_mx4_linear_qx(const void *x, int32_t x_dtype, int32_t M, int32_t K, int64_t x_stride, const uint8_t *codes,
+                             const uint8_t *scales, int32_t N, const float *bias, int32_t act, void *y, int32_t y_dtype, int64_t y_stride,
+                             void *workspace, int64_t workspace_bytes, void *hip_stream)
+{
+    if (!codes || !scales || (M != 0 && (!x || !y || !workspace))) return PAC_ERR_NULL;
+    if (M < 0 || K < 1 || N < 1 || !dtype_ok(x_dtype) || !dtype_ok(y_dtype) || (act != PAC_MX4_ACT_NONE && act != PAC_MX4_ACT_GELU))
+        return PAC_ERR_SHAPE;
+    if (M > kMx4Most || K > kMx4Most || N > kMx4Most) return PAC_ERR_UNSUPPORTED;
+    if (x_stride < K || y_stride < N) return PAC_ERR_RANGE;
+    if (!m_aligned(x, x_dtype == PAC_F32 ? 4 : 2) || !m_aligned(codes, 16) || !m_aligned(scales, 8) || !m_aligned(bias, 4) ||
+        !m_aligned(y, y_dtype == PAC_F32 ? 4 : 2) || !m_aligned(workspace, 16))
+        return PAC_ERR_ALIGN;
+    if (M == 0) return PAC_OK;
+    if (workspace_bytes < pac_mx4_linear_qx_workspace_bytes(M, K)) return PAC_ERR_WORKSPACE;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    Mx4Args a{x, nullptr, x_stride, codes, scales, M, K, N, code_pitch(K), scale_pitch(K), bias, act, y, y_dtype == PAC_F32, y_stride};
+    (void)hipGetLastError();
+    const Mx4Form &form = kMx4LinearX4[linear_form(true, M, K, N)];
+    // few rows in whole 16-byte pieces: quantised where they are multiplied (one launch)
+    if (form.rows <= 32 && x_dtype == PAC_BF16 && K % 8 == 0 && x_stride % 8 == 0 && m_aligned(x, 16))
+        return form.rows == 16 ? launch_rows<MX4_XQ, 1>(a, st) : launch_rows<MX4_XQ, 2>(a, st);
+    uint8_t *xc = static_cast<uint8_t *>(workspace), *xs = xc + (int64_t)M * a.wp; // rows of codes are whole multiples of 128 bytes
+    if ((int64_t)M > 0x7fffffffll / (a.wp / 128)) return PAC_ERR_UNSUPPORTED;
+    const pac_status s = launch_quant(x, x_dtype, M, K, x_stride, xc, xs, st);
+    if (s != PAC_OK) return s;
+    a.x = xc;
+    a.xs = xs;
+    return launch_linear<true>(a, st);
 }
 
 pac_status pac_mx4_tiles(int32_t product, int32_t M, int32_t K, int32_t N, int32_t out[2])

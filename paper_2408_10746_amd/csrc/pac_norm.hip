@@ -378,53 +378,57 @@ struct NormSums {
     float *dw_post, *db_post, *dgate, *dres, *dw_pre, *db_pre;
 };
 
-// The parameters' gradients from the blocks' partial sums, in a fixed order and in 64 bits.  16 columns a block, 32 threads a
-// column, eight loads under way each.
-template <int NV> __global__ __launch_bounds__(512) void k_norm_sums(NormSums a)
+__device__ __forceinline__ double add_lanes(double v, int o) { return v + __shfl_xor(v, o, 64); }
+
+// The parameters' gradients from the blocks' partial sums, in a fixed order and in 64 bits.  A block takes 16 columns (64 bytes a
+// row) of one vector, 32 threads a column, four loads under way each; a gate's gradient takes the first vector and the second.
+__global__ __launch_bounds__(512) void k_norm_sums(NormSums a)
 {
-    constexpr int NR = NV > 0 ? NV : 1;
-    __shared__ double red[NR][32][17];
-    const int cj = threadIdx.x & 15, part = threadIdx.x >> 4, j = blockIdx.x * 16 + cj;
-    if constexpr (NV > 0) {
-        double s[NV];
-#pragma unroll
-        for (int v = 0; v < NV; ++v) s[v] = 0.;
-        const float *src = a.cols + min(j, a.d - 1);
+    __shared__ double red[2][8][16];
+    const int cj = threadIdx.x & 15, part = threadIdx.x >> 4, j = blockIdx.x * 16 + cj, v = blockIdx.y, wave = threadIdx.x >> 6;
+    if (v < a.nv) {
+        const bool gates = v == a.v_a && a.dgate && a.gate_len > 1, two = gates && a.b_post;
+        double s[2] = {0., 0.};
+        const int64_t row = (int64_t)a.nv * a.d;
+        const float *src = a.cols + (int64_t)v * a.d + min(j, a.d - 1), *src2 = a.cols + (int64_t)(two ? a.v_b : v) * a.d + min(j, a.d - 1);
         for (int p0 = part; p0 < a.parts; p0 += 4 * 32) {
-            float f[4][NV];
+            float f[4], g[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int64_t at = min(p0 + 32 * u, a.parts - 1) * row;
+                f[u] = src[at];
+                if (two) g[u] = src2[at];
+            }
 #pragma unroll
             for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int v = 0; v < NV; ++v) f[u][v] = src[((int64_t)min(p0 + 32 * u, a.parts - 1) * NV + v) * a.d];
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int v = 0; v < NV; ++v) s[v] += p0 + 32 * u < a.parts ? (double)f[u][v] : 0.;
+                if (p0 + 32 * u < a.parts) {
+                    s[0] += (double)f[u];
+                    if (two) s[1] += (double)g[u];
+                }
         }
+        // a wavefront holds four threads a column
 #pragma unroll
-        for (int v = 0; v < NV; ++v) red[v][part][cj] = s[v];
+        for (int k = 0; k < 2; ++k) {
+            s[k] = add_lanes(add_lanes(s[k], 16), 32);
+            if ((threadIdx.x & 63) < 16) red[k][wave][cj] = s[k];
+        }
         __syncthreads();
         if (threadIdx.x < 16 && j < a.d) {
-            double t[4] = {0., 0., 0., 0.};
+            double t = 0., t2 = 0.;
 #pragma unroll
-            for (int v = 0; v < NV; ++v)
-#pragma unroll
-                for (int p = 0; p < 32; ++p) t[v] += red[v][p][cj];
-            auto pick = [&](int v) { return v == 0 ? t[0] : v == 1 ? t[1] : v == 2 ? t[2] : v == 3 ? t[3] : 0.; };
+            for (int w = 0; w < 8; ++w) t += red[0][w][cj], t2 += red[1][w][cj];
             const double ga = a.gate ? (double)a.gate[a.gate_len > 1 ? j : 0] : 1.;
-            if (a.dw_post) a.dw_post[j] = (float)(ga * pick(a.v_a));
-            if (a.db_post) a.db_post[j] = (float)(ga * pick(a.v_b));
-            if (a.dgate && a.gate_len > 1)
-                a.dgate[j] = (float)(a.w_post ? (double)a.w_post[j] * pick(a.v_a) + (a.b_post ? (double)a.b_post[j] * pick(a.v_b) : 0.) : pick(a.v_a));
-            if (a.dw_pre) a.dw_pre[j] = (float)pick(a.v_c);
-            if (a.db_pre) a.db_pre[j] = (float)pick(a.v_d);
+            if (v == a.v_a && a.dw_post) a.dw_post[j] = (float)(ga * t);
+            if (v == a.v_b && a.db_post) a.db_post[j] = (float)(ga * t);
+            if (gates) a.dgate[j] = (float)(a.w_post ? (double)a.w_post[j] * t + (two ? (double)a.b_post[j] * t2 : 0.) : t);
+            if (v == a.v_c && a.dw_pre) a.dw_pre[j] = (float)t;
+            if (v == a.v_d && a.db_pre) a.db_pre[j] = (float)t;
         }
-    }
-    if (blockIdx.x == 0 && threadIdx.x < 64 && (a.dres || (a.dgate && a.gate_len == 1))) {
+    } else if (blockIdx.x == 0 && threadIdx.x < 64 && (a.dres || (a.dgate && a.gate_len == 1))) { // one block behind the vectors': the two scalars
         double u = 0., w = 0.;
         for (int p = threadIdx.x; p < a.parts; p += 64) u += a.scal[2 * p], w += a.scal[2 * p + 1];
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) u += __shfl_xor(u, o, 64), w += __shfl_xor(w, o, 64);
+        for (int o = 1; o < 64; o <<= 1) u = add_lanes(u, o), w = add_lanes(w, o);
         if (threadIdx.x == 0) {
             if (a.dres) a.dres[0] = (float)u;
             if (a.dgate && a.gate_len == 1) a.dgate[0] = (float)w;
@@ -604,12 +608,9 @@ pac_status pac_block_norm_backward(const pac_block_norm *b, int64_t rows, const 
     if (!sums) return PAC_OK;
     const NormSums u{a.cols, a.scal, (int)blocks, b->d, a.nv, a.v_a, a.v_b, a.v_c, a.v_d, a.gate_len,
                      b->w_post, b->b_post, b->gate, dw_post, db_post, dgate, dres, dw_pre, db_pre};
-    const dim3 gs(a.nv ? (unsigned)((b->d + 15) / 16) : 1u);
-    if (a.nv == 0) hipLaunchKernelGGL(k_norm_sums<0>, gs, dim3(512), 0, st, u);
-    else if (a.nv == 1) hipLaunchKernelGGL(k_norm_sums<1>, gs, dim3(512), 0, st, u);
-    else if (a.nv == 2) hipLaunchKernelGGL(k_norm_sums<2>, gs, dim3(512), 0, st, u);
-    else if (a.nv == 3) hipLaunchKernelGGL(k_norm_sums<3>, gs, dim3(512), 0, st, u);
-    else hipLaunchKernelGGL(k_norm_sums<4>, gs, dim3(512), 0, st, u);
+    // columns by vectors, and where scalars are wanted one more row of blocks, of which the first sums them
+    const dim3 gs(a.nv ? (unsigned)((b->d + 15) / 16) : 1u, (unsigned)(a.nv + (scalars ? 1 : 0)));
+    hipLaunchKernelGGL(k_norm_sums, gs, dim3(512), 0, st, u);
     return hipGetLastError() == hipSuccess ? PAC_OK : PAC_ERR_DEVICE;
 }
 

@@ -295,6 +295,7 @@ class Mx4Linear:
         # the tail of every product's arguments: W, and the bias
         self._w = (codes.data_ptr(), scales.data_ptr())
         self._wb = self._w + (self.N, _ptr(bias))
+        self._x_bytes = pb.pac_mx4_linear_qx_workspace_bytes(1, K)
 
     @classmethod
     def from_weights(cls, w, bias=None):
@@ -311,12 +312,9 @@ class Mx4Linear:
         act = pb.PAC_MX4_ACT_GELU if gelu else pb.PAC_MX4_ACT_NONE
         if x4:
             sx, xkind = _rows_of(x, "x", M, self.K, dev)
-            # x in the stored form lives for this call, on this stream: codes (whole multiples of 128 bytes a row), then scales
-            c = M * self.codes.shape[1]
-            buf = torch.empty(c + M * self.scales.shape[1], dtype=torch.uint8, device=dev)
-            at = buf.data_ptr()
-            _call(dev, "pac_mx4_quantize", x.data_ptr(), xkind, M, self.K, sx, at, at + c)
-            _call(dev, "pac_mx4_linear_x4", at, at + c, M, self.K, *self._wb, act, y.data_ptr(), kind, sy)
+            need = M * self._x_bytes  # x in the stored form, for this call, on this stream
+            ws = torch.empty(need, dtype=torch.uint8, device=dev)
+            _call(dev, "pac_mx4_linear_qx", x.data_ptr(), xkind, M, self.K, sx, *self._wb, act, y.data_ptr(), kind, sy, ws.data_ptr(), need)
         else:
             sx = _chunked_rows(x, "x", M, self.K, dev)
             _call(dev, "pac_mx4_linear", x.data_ptr(), M, self.K, sx, *self._wb, act, y.data_ptr(), kind, sy)
@@ -347,6 +345,7 @@ class BlockNorm:
             if self.dev not in (None, p.device):
                 raise ValueError(f"{name}: on another device than the parameters before it")
             self.dev = p.device
+        self._shapes = {name: p.shape for name, p in self.params.items() if p is not None}
         self._b = {dtype: pb.pac_block_norm(d, kind, int(layer), 0 if gate is None else gate.shape[0], eps, *(_ptr(p) for p in self.params.values()))
                    for dtype, kind in _KIND.items()}
 
@@ -370,11 +369,11 @@ class BlockNorm:
         rows = self._rows(x, o, dy, dn, dx, do)
         b, grads, ws, need = self._b[x.dtype], [None] * 6, None, 0
         if dparams:
+            dev = x.device
             for name, g in dparams.items():
-                p = self.params.get(name)
-                if p is None or g.shape != p.shape or g.dtype != torch.float32 or g.device != p.device or not g.is_contiguous():
+                if g.shape != self._shapes.get(name) or g.dtype is not torch.float32 or g.device != dev or not g.is_contiguous():
                     raise ValueError(f"d{name}: like the parameter of that name")
             grads = [_ptr(dparams.get(name)) for name in self.params]
-            need = pb.pac_block_norm_workspace_bytes(b, rows)
+            need = _lib().pac_block_norm_workspace_bytes(b, rows)
             ws = torch.empty(need, dtype=torch.uint8, device=x.device)  # for this call, on this stream
         _call(x.device, "pac_block_norm_backward", b, rows, x.data_ptr(), _ptr(o), _ptr(dy), _ptr(dn), _ptr(dx), _ptr(do), *grads, _ptr(ws), need)

@@ -57,6 +57,18 @@ def test_products_refuse():
     assert lin(sx=32) == lin(sy=6) == lin4(sy=6) == dx(sdy=6) == dx(sdx=39) == pb.PAC_ERR_RANGE
     assert lin(sx=44) == lin(x=A + 8) == lin(y=A + 2) == lin(bias=A + 2) == lin4(x=A + 8) == lin4(xs=A + 4) == pb.PAC_ERR_ALIGN
     assert dx(sdy=12) == dx(dy=A + 8) == dx(out=A + 1, dt=pb.PAC_BF16) == pb.PAC_ERR_ALIGN
+    assert pb.pac_mx4_linear_qx_workspace_bytes(4, 40) == 4 * 136 and pb.pac_mx4_linear_qx_workspace_bytes(-1, 40) == -1
+    assert pb.pac_mx4_linear_qx_workspace_bytes(4, 0) == -1
+
+    def linq(x=A, xdt=pb.PAC_BF16, M=4, K=40, sx=40, codes=A, scales=A, N=7, bias=None, act=0, y=A, dt=pb.PAC_F32, sy=7, ws=A, n=4 * 136):
+        return L.pac_mx4_linear_qx(x, xdt, M, K, sx, codes, scales, N, bias, act, y, dt, sy, ws, n, None)
+
+    assert linq(M=0, x=None, y=None, ws=None, n=0) == pb.PAC_OK
+    assert linq(x=None) == linq(codes=None) == linq(scales=None) == linq(y=None) == linq(ws=None) == pb.PAC_ERR_NULL
+    assert linq(M=-1) == linq(K=0) == linq(N=0) == linq(dt=5) == linq(xdt=5) == linq(act=2) == pb.PAC_ERR_SHAPE
+    assert linq(sx=39) == linq(sy=6) == pb.PAC_ERR_RANGE and linq(n=4 * 136 - 1) == pb.PAC_ERR_WORKSPACE
+    assert linq(x=A + 1) == linq(x=A + 2, xdt=pb.PAC_F32) == linq(codes=A + 8) == linq(scales=A + 4) == linq(bias=A + 2) == linq(ws=A + 8) == pb.PAC_ERR_ALIGN
+    assert linq(M=(1 << 30) + 1) == linq(K=(1 << 30) + 1, sx=1 << 31) == pb.PAC_ERR_UNSUPPORTED
     big = 1 << 30
     assert lin(M=big, N=big, sy=big) == lin4(M=big, N=big, sy=big) == dx(M=big, K=big, sdx=big) == pb.PAC_ERR_UNSUPPORTED
 

@@ -146,6 +146,31 @@ def test_linear(M, K, N, x4):
         assert (store[:, N:] == 5.0).all()
 
 
+@pytest.mark.parametrize("M,K,N", [(1, 8, 3), (1, 4096, 300), (5, 232, 77), (16, 1000, 64), (17, 2048, 33), (30, 777, 700), (2079, 32, 18), (300, 2048, 1030)])
+def test_quantising_in_the_call_is_quantising_before_it(M, K, N):
+    """The same bits from rows of any alignment and type, over the whole range of scales, with blocks that stand for nothing."""
+    rng = np.random.default_rng(M + K + N)
+    codes, scales, _ = layer(rng, N, K)
+    lin = rt.Mx4Linear(codes, scales, K)
+    x = rows_of(rng, M, K)
+    x *= torch.from_numpy(np.exp2(rng.integers(-140, 120, size=(M, 1)).astype(np.float64))).cuda()
+    x[0, :5] = torch.tensor([0.25, -1.25, 2.5, 6.9, 0.0], device="cuda").bfloat16() * float(x[0].abs().max()) if K > 8 else 1.0
+    if M > 3 and K > 70:
+        x[2, 64], x[3, 3], x[1, :32] = float("inf"), float("nan"), 0
+    xc, xs = rt.mx4_empty(M, K)
+    rt.mx4_quantize(x, xc, xs)
+    ref = torch.empty(M, N, device="cuda")
+    pb.pac_mx4_linear_x4(xc.data_ptr(), xs.data_ptr(), M, K, codes.data_ptr(), scales.data_ptr(), N, None, 0, ref.data_ptr(), pb.PAC_F32, N,
+                         torch.cuda.current_stream().cuda_stream)
+    off = torch.empty(M * (K + 1) + 1, dtype=torch.bfloat16, device="cuda")[1:].as_strided((M, K), (K + 1, 1))
+    off.copy_(x)
+    for t in (x, off, x.float(), x.clone()):
+        y = torch.empty(M, N, device="cuda")
+        lin.forward(t, y, x4=True)
+        same = (y == ref) | (torch.isnan(y) & torch.isnan(ref))
+        assert same.all()
+
+
 @pytest.mark.parametrize("M,K,N", SHAPES + [(1, 300, 4096), (40, 1030, 900)])
 def test_input_grad(M, K, N):
     rng = np.random.default_rng(M * 5 + K + N * 11)
