@@ -450,12 +450,12 @@ template <int RM, int NW> __global__ __launch_bounds__(64 * NW) void k_mx4_dx_ro
 // The 256 x 256 tiles of stored x take steps of 256 columns through two stages, half the barriers of steps of 128 through four:
 // 4096 x 4096 x 16384 166 -> 161 us.  What bounds them there: reads of LDS and matrix instructions, each about as long as the other.
 // ---------------------------------------------------------------------------
-template <bool X4_, int WM_, int WN_, int WTM_, int WTN_, int STAGES_> struct Mx4Tile {
+template <bool X4_, int WM_, int WN_, int WTM_, int WTN_, int STAGES_, int BK_> struct Mx4Tile {
     static constexpr bool X4 = X4_;
     static constexpr int WM = WM_, WN = WN_, WTM = WTM_, WTN = WTN_, STAGES = STAGES_, NW = WM * WN;
     static constexpr int TM = 32 * WM * WTM, TN = 32 * WN * WTN;
-    static constexpr int BK = X4 ? (STAGES == 2 ? 256 : 128) : 64, PER = 256 / BK;   // columns a step, steps a group of 256
-    static constexpr int AB = X4 ? BK / 2 : 128, BB = X4 ? BK / 2 : 32; // bytes of a row a step
+    static constexpr int BK = BK_, PER = 256 / BK;   // columns a step, steps a group of 256
+    static constexpr int AB = X4 ? BK / 2 : BK * 2, BB = BK / 2; // bytes of a row a step
     static constexpr int AI = TM * AB / 1024, TOTAL = AI + TN * BB / 1024, NI = (TOTAL + NW - 1) / NW;
     static constexpr int STAGE_BYTES = TM * AB + TN * BB;
     // scales: rows of W, then of x; rings deep enough that no group of 256 columns in use is written over
@@ -470,20 +470,21 @@ __device__ __forceinline__ void dma4_at(const void *g, uint32_t lds_wave_address
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
                  : : "s"(__builtin_amdgcn_readfirstlane(lds_wave_address)), "v"(g) : "memory", "m0");
 }
-// chunk swizzle of rows of 128, 64 and 32 bytes: the 16 rows that one pass of a 16-byte read covers meet every bank once
+// chunk swizzle of rows of 256, 128, 64 and 32 bytes: the 16 rows that one pass of a 16-byte read covers meet every bank once
 template <int BYTES> __device__ __forceinline__ int mx4_swz(int row)
 {
-    return BYTES == 128 ? (row >> 1) & 7 : BYTES == 64 ? (row >> 2) & 3 : (row >> 3) & 1;
+    return BYTES == 256 ? row & 15 : BYTES == 128 ? (row >> 1) & 7 : BYTES == 64 ? (row >> 2) & 3 : (row >> 3) & 1;
 }
 
 // bf16 rows of a step that ends past the contraction's length: what lies there is cleared in LDS, before anyone reads it.  All
 // threads call this, with the step's stage in place and a barrier behind it.
-template <int ROWS, int THREADS> __device__ __forceinline__ void mx4_clip(char *stage, int valid)
+template <int ROWS, int BYTES, int THREADS> __device__ __forceinline__ void mx4_clip(char *stage, int valid)
 {
-    for (int e = threadIdx.x; e < ROWS * 8; e += THREADS) {
-        const int row = e >> 3, c = e & 7;
+    constexpr int CH = BYTES / 16;
+    for (int e = threadIdx.x; e < ROWS * CH; e += THREADS) {
+        const int row = e / CH, c = e % CH;
         if (8 * c + 8 <= valid) continue;
-        u32x4 *p = reinterpret_cast<u32x4 *>(stage + row * 128 + ((c ^ mx4_swz<128>(row)) << 4));
+        u32x4 *p = reinterpret_cast<u32x4 *>(stage + row * BYTES + ((c ^ mx4_swz<BYTES>(row)) << 4));
         *p = mx4_keep(*p, valid - 8 * c);
     }
     __syncthreads();
@@ -580,12 +581,13 @@ template <class TL> __global__ __launch_bounds__(64 * TL::NW, 2) void k_mx4_tile
         brow[y] = TL::TM * TL::AB + row * TL::BB;
         bsw[y] = mx4_swz<TL::BB>(row);
     }
-    constexpr int J = TL::X4 ? TL::BK / 64 : 4, FB = TL::AHEAD ? 2 * J : 2; // sub-steps; fragments held
+    constexpr int BL = TL::BK / 64, J = TL::X4 ? BL : 4 * BL, FB = TL::AHEAD ? 2 * J : 2; // a lane's blocks a step, sub-steps, fragments held
+    constexpr int CB = TL::AHEAD && !TL::X4 ? 2 * BL : 2; // steps' codes held beside bf16 rows, a lane's block each
     uint64_t bsc[WTN], asc[TL::X4 ? WTM : 1]; // this lane's half of a group's scales, shifted to the bottom
-    u32x4 af[FB][WTM], bf[TL::X4 ? FB : 2][WTN]; // fragments; beside bf16 rows bf holds a step's codes
+    u32x4 af[FB][WTM], bf[TL::X4 ? FB : CB][WTN]; // fragments; beside bf16 rows bf holds codes
     auto read_scales = [&](int grp, uint64_t (&bs)[WTN], uint64_t (&as)[TL::X4 ? WTM : 1]) {
         const char *sc = lds + TL::STAGES * TL::STAGE_BYTES + grp % TL::RING * (TL::SR * 8);
-        const int half = TL::X4 ? 8 * J * g : 8 * g;
+        const int half = 8 * BL * g;
 #pragma unroll
         for (int y = 0; y < WTN; ++y) bs[y] = *reinterpret_cast<const uint64_t *>(sc + ((wn * WTN + y) * 32 + i) * 8) >> half;
         if constexpr (TL::X4)
@@ -598,7 +600,7 @@ template <class TL> __global__ __launch_bounds__(64 * TL::NW, 2) void k_mx4_tile
     };
     auto read_b = [&](const char *sb, int j, u32x4 (&to)[WTN]) {
 #pragma unroll
-        for (int y = 0; y < WTN; ++y) to[y] = *reinterpret_cast<const u32x4 *>(sb + brow[y] + (((TL::X4 ? J * g + j : g) ^ bsw[y]) << 4));
+        for (int y = 0; y < WTN; ++y) to[y] = *reinterpret_cast<const u32x4 *>(sb + brow[y] + (((BL * g + j) ^ bsw[y]) << 4));
     };
     // the matrix instructions of a sub-step, `after(k)` behind the k-th of them
     auto multiply = [&](int u, int j, u32x4 (&pa)[WTM], const u32x4 (&pb)[WTN], auto after) __attribute__((always_inline)) {
@@ -619,7 +621,7 @@ template <class TL> __global__ __launch_bounds__(64 * TL::NW, 2) void k_mx4_tile
         } else {
             bf16x8 w[WTN];
 #pragma unroll
-            for (int y = 0; y < WTN; ++y) w[y] = mx4_bf16(pb[y][j], mx4_scale((uint32_t)(bsc[y] >> (16 * u)) & 255u));
+            for (int y = 0; y < WTN; ++y) w[y] = mx4_bf16(pb[y][j % 4], mx4_scale((uint32_t)(bsc[y] >> (16 * BL * u + 8 * (j / 4))) & 255u));
 #pragma unroll
             for (int x = 0; x < WTM; ++x)
 #pragma unroll
@@ -645,7 +647,7 @@ template <class TL> __global__ __launch_bounds__(64 * TL::NW, 2) void k_mx4_tile
         wait_vm<decltype(pending)::value>();
         __syncthreads();
         if constexpr (!TL::X4)
-            if (step == nsteps - 1 && a.K % 64) mx4_clip<TL::TM, 64 * TL::NW>(stage, a.K - step * 64);
+            if (step == nsteps - 1 && a.K % TL::BK) mx4_clip<TL::TM, TL::AB, 64 * TL::NW>(stage, a.K - step * TL::BK);
     };
     arrive(lds, 0, std::integral_constant<int, TL::NI * (TL::STAGES - 1)>());
     read_scales(0, bsc, asc);
@@ -656,7 +658,7 @@ template <class TL> __global__ __launch_bounds__(64 * TL::NW, 2) void k_mx4_tile
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             read_a(lds, j, af[j]);
-            if (TL::X4 || j == 0) read_b(lds, j, bf[j]);
+            if (j < BL) read_b(lds, j, bf[j]);
         }
         for (int grp = 0; grp < ngroups; ++grp) {
 #pragma unroll
@@ -666,18 +668,17 @@ template <class TL> __global__ __launch_bounds__(64 * TL::NW, 2) void k_mx4_tile
                 char *nb = lds + (slot + 1 == TL::STAGES ? 0 : slot + 1) * TL::STAGE_BYTES;
                 arrive(nb, st + 1, std::integral_constant<int, TL::NI * (TL::STAGES - 2)>()); // (this stage has been read)
                 uint64_t bsn[WTN], asn[TL::X4 ? WTM : 1];
-                const int now = (u & 1) * J, next = J - now;
+                const int now = (u & 1) * J, next = J - now, nowb = (u & 1) * BL, nextb = BL - nowb;
                 if (u == TL::PER - 1) read_scales(grp + 1, bsn, asn);
 #pragma unroll
                 for (int j = 0; j < J; ++j) {
                     read_a(nb, j, af[next + j]);
-                    if (TL::X4) read_b(nb, j, bf[TL::X4 ? next + j : 0]);
-                    else if (j == 0) read_b(nb, 0, bf[(u & 1) ^ 1]);
+                    if (j < BL) read_b(nb, j, bf[nextb + j]);
                 }
                 __builtin_amdgcn_sched_barrier(0); // the reads stay ahead of the matrix instructions
 #pragma unroll
                 for (int j = 0; j < J; ++j)
-                    multiply(u, j, af[now + j], bf[TL::X4 ? now + j : (u & 1)], [&](int k) __attribute__((always_inline)) {
+                    multiply(u, j, af[now + j], bf[nowb + (TL::X4 ? j : j / 4)], [&](int k) __attribute__((always_inline)) {
                         transfers(j * WTM * WTN + k, J * WTM * WTN, slot, st + TL::STAGES);
                     });
                 if (u == TL::PER - 1) {
@@ -859,7 +860,7 @@ template <class TL> __global__ __launch_bounds__(64 * TL::NW, 2) void k_mx4_dx_t
     auto arrive = [&](char *stage, int step, auto pending) __attribute__((always_inline)) {
         wait_vm<decltype(pending)::value>();
         __syncthreads();
-        if (step == nsteps - 1 && a.N % 64) mx4_clip<TL::TM, 64 * TL::NW>(stage, a.N - step * 64);
+        if (step == nsteps - 1 && a.N % 64) mx4_clip<TL::TM, 128, 64 * TL::NW>(stage, a.N - step * 64);
     };
     arrive(lds, 0, std::integral_constant<int, (TL::NI + 1) * (TL::STAGES - 1)>());
     read(lds, bbuf, 0);
@@ -1034,10 +1035,10 @@ template <bool X4> static pac_status launch_linear(const Mx4Args &a, hipStream_t
     switch (X4 ? kMx4LinearX4[form].cols + kMx4LinearX4[form].rows : kMx4Linear[form].cols + kMx4Linear[form].rows) {
     case 16 + 16: return launch_rows<X4 ? MX4_X4 : MX4_X16, 1>(a, st);
     case 32 + 16: return launch_rows<X4 ? MX4_X4 : MX4_X16, 2>(a, st);
-    case 64 + 64: return launch_tiles<Mx4Tile<X4, 2, 2, 1, 1, 4>>(a, st);
-    case 64 + 128: if constexpr (!X4) return launch_tiles<Mx4Tile<X4, 2, 2, 1, 2, 4>>(a, st); [[fallthrough]];
-    case 128 + 128: return launch_tiles<Mx4Tile<X4, 2, 2, 2, 2, X4 ? 4 : 3>>(a, st);
-    default: return launch_tiles<Mx4Tile<X4, 2, 4, 4, 2, X4 ? 2 : 3>>(a, st);
+    case 64 + 64: return launch_tiles<Mx4Tile<X4, 2, 2, 1, 1, X4 ? 4 : 3, 128>>(a, st);
+    case 64 + 128: if constexpr (!X4) return launch_tiles<Mx4Tile<X4, 2, 2, 1, 2, X4 ? 4 : 3, 128>>(a, st); [[fallthrough]];
+    case 128 + 128: return launch_tiles<Mx4Tile<X4, 2, 2, 2, 2, X4 ? 4 : 3, X4 ? 128 : 64>>(a, st);
+    default: return launch_tiles<Mx4Tile<X4, 2, 4, 4, 2, X4 ? 2 : 3, X4 ? 256 : 64>>(a, st);
     }
 }
 
