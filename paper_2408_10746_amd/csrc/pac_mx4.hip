@@ -987,54 +987,55 @@ template <int RM> static pac_status launch_dx_rows(const Mx4Args &a, hipStream_t
 
 // Which tiles a product runs on.  For each form the time in us is estimated as  start + tile n + steps max(least, share n)  with n
 // its tiles over 256 compute units (whole rounds where one tile fills a unit): a step's latency where units have less than one tile,
-// its throughput where they have more.  The constants are fitted to all forms' times at 446 shapes (M to 4096, K to 8192, N to
-// 16384): the form taken costs 0.5 % (x in bf16), 1.0 % (x in mx4) and 0.1 % (dx) over the best one, on the geometric mean.
-// Both sides, us: x in bf16, 64 x 4096 x 4096: 16 rows 25, 64 x 64 18; 1024 x 1024 x 4096: 64 x 64 17, 64 x 128 13.2, 128 x 128
-// 12.7, 256 x 256 25; 4096^3: 124 on 128 x 128, 106 on 256 x 256.  dx, 333 x 4096 x 4096: 16 rows 40, 32 rows 37, 64 rows 62.
+// its throughput where they have more.  The constants are fitted to all forms' times at 594 shapes (446 for dx; M to 4096, K to 8192,
+// N to 16384): the form taken costs 0.5 % (x in bf16), 0.4 % (x in mx4) and 0.1 % (dx) over the best one, on the geometric mean.
+// Both sides, us: x in bf16, 64 x 4096 x 4096: 16 rows 25, 64 x 64 14; 1024 x 1024 x 4096: 64 x 64 17.1, 64 x 128 13.5, 128 x 128
+// 13.1, 256 x 256 25; 4096^3: 123 on 128 x 128, 106 on 256 x 256.  In mx4, 64 x 4096 x 4096: 32 rows 13.3, 64 x 64 8.5.
+// dx, 333 x 4096 x 4096: 16 rows 40, 32 rows 37, 64 rows 62.
 struct Mx4Form {
-    int rows, cols; // of a tile
+    int rows, cols, step; // of a tile; of the contraction (with 16 and 32 rows all of a workgroup's wavefronts together)
     bool whole;
     float start, tile, least, share;
 };
-constexpr Mx4Form kMx4Linear[] = {{16, 16, false, 2.42f, 0.f, 0.753f, 0.685f},    {32, 16, false, 2.01f, 0.f, 3.161f, 1.285f},
-                                  {64, 64, false, 5.26f, 0.62f, 0.112f, 0.203f},  {64, 128, false, 5.57f, 1.09f, 0.2f, 0.369f},
-                                  {128, 128, false, 7.88f, 3.23f, 0.355f, 0.601f}, {256, 256, true, 2.43f, 20.7f, 0.434f, 1.082f}};
-constexpr Mx4Form kMx4LinearX4[] = {{16, 16, false, 2.36f, 0.f, 0.23f, 0.478f},     {32, 16, false, 2.35f, 0.f, 0.483f, 0.653f},
-                                    {64, 64, false, 4.27f, 0.58f, 0.117f, 0.169f},
-                                    {128, 128, false, 6.64f, 2.43f, 0.302f, 0.495f}, {256, 256, true, 0.97f, 18.f, 0.798f, 0.204f}};
-constexpr Mx4Form kMx4Dx[] = {{16, 128, false, 4.06f, 0.58f, 0.035f, 0.801f}, {32, 128, false, 3.55f, 3.64f, 0.876f, 0.993f},
-                              {64, 256, true, 2.04f, 5.51f, 0.285f, 0.75f},   {128, 256, true, 0.04f, 8.42f, 0.101f, 0.897f},
-                              {256, 256, true, 1.19f, 6.65f, 0.763f, 1.608f}};
+constexpr Mx4Form kMx4Linear[] = {{16, 16, 1024, false, 1.02f, 0.f, 0.607f, 0.693f},
+                                  {64, 64, 128, false, 4.86f, 0.91f, 0.15f, 0.429f},
+                                  {64, 128, 128, false, 5.55f, 1.41f, 0.692f, 0.609f},
+                                  {128, 128, 64, false, 6.48f, 1.64f, 0.768f, 0.594f},
+                                  {256, 256, 64, true, 0.46f, 32.22f, 0.434f, 0.937f}};
+constexpr Mx4Form kMx4LinearX4[] = {{16, 16, 1024, false, 2.35f, 0.f, 0.055f, 0.522f},
+                                    {32, 16, 1024, false, 2.57f, 0.f, 0.461f, 0.705f},
+                                    {64, 64, 128, false, 5.15f, 0.63f, 0.064f, 0.166f},
+                                    {128, 128, 128, false, 7.87f, 2.39f, 0.279f, 0.422f},
+                                    {256, 256, 256, true, 0.26f, 23.01f, 0.806f, 1.223f}};
+constexpr Mx4Form kMx4Dx[] = {{16, 128, 256, false, 4.06f, 0.58f, 0.035f, 0.801f},
+                              {32, 128, 256, false, 3.55f, 3.64f, 0.876f, 0.993f},
+                              {64, 256, 64, true, 2.04f, 5.51f, 0.285f, 0.75f},
+                              {128, 256, 64, true, 0.04f, 8.42f, 0.101f, 0.897f},
+                              {256, 256, 64, true, 1.19f, 6.65f, 0.763f, 1.608f}};
 
-// the number of the form for a product of M x `deep` by `deep` x `wide`; small_step, step: contraction of a step of the forms of
-// 16 and 32 rows (all of a workgroup's wavefronts together) and of the others
-template <int F> static int mx4_form(const Mx4Form (&forms)[F], int64_t M, int64_t deep, int64_t wide, int small_step, int step)
+// the form for a product of M x `deep` by `deep` x `wide`
+template <int F> static const Mx4Form &mx4_form(const Mx4Form (&forms)[F], int64_t M, int64_t deep, int64_t wide)
 {
-    int best = 0;
+    const Mx4Form *best = nullptr;
     float least = 0.f;
-    for (int f = 0; f < F; ++f) {
-        const Mx4Form &q = forms[f];
+    for (const Mx4Form &q : forms) {
         const int64_t tiles = ((M + q.rows - 1) / q.rows) * ((wide + q.cols - 1) / q.cols);
-        const int d = q.rows <= 32 ? small_step : step;
-        const float n = q.whole ? (float)((tiles + 255) / 256) : (float)tiles / 256.f, steps = (float)((deep + d - 1) / d);
+        const float n = q.whole ? (float)((tiles + 255) / 256) : (float)tiles / 256.f, steps = (float)((deep + q.step - 1) / q.step);
         const float t = q.start + q.tile * n + steps * (q.least > q.share * n ? q.least : q.share * n);
-        if (f == 0 || t < least) best = f, least = t;
+        if (!best || t < least) best = &q, least = t;
     }
-    return best;
+    return *best;
 }
-static int linear_form(bool x4, int M, int K, int N)
-{
-    return x4 ? mx4_form(kMx4LinearX4, M, K, N, 1024, 128) : mx4_form(kMx4Linear, M, K, N, 1024, 64);
-}
-static int dx_form(int M, int K, int N) { return mx4_form(kMx4Dx, M, N, K, 256, 64); }
+static const Mx4Form &linear_form(bool x4, int M, int K, int N) { return x4 ? mx4_form(kMx4LinearX4, M, K, N) : mx4_form(kMx4Linear, M, K, N); }
+static const Mx4Form &dx_form(int M, int K, int N) { return mx4_form(kMx4Dx, M, N, K); }
 
 template <bool X4> static pac_status launch_linear(const Mx4Args &a, hipStream_t st)
 {
     (void)hipGetLastError();
-    const int form = linear_form(X4, a.M, a.K, a.N);
-    switch (X4 ? kMx4LinearX4[form].cols + kMx4LinearX4[form].rows : kMx4Linear[form].cols + kMx4Linear[form].rows) {
+    const Mx4Form &form = linear_form(X4, a.M, a.K, a.N);
+    switch (form.rows + form.cols) {
     case 16 + 16: return launch_rows<X4 ? MX4_X4 : MX4_X16, 1>(a, st);
-    case 32 + 16: return launch_rows<X4 ? MX4_X4 : MX4_X16, 2>(a, st);
+    case 32 + 16: if constexpr (X4) return launch_rows<MX4_X4, 2>(a, st); [[fallthrough]];
     case 64 + 64: return launch_tiles<Mx4Tile<X4, 2, 2, 1, 1, X4 ? 4 : 3, 128>>(a, st);
     case 64 + 128: if constexpr (!X4) return launch_tiles<Mx4Tile<X4, 2, 2, 1, 2, X4 ? 4 : 3, 128>>(a, st); [[fallthrough]];
     case 128 + 128: return launch_tiles<Mx4Tile<X4, 2, 2, 2, 2, X4 ? 4 : 3, X4 ? 128 : 64>>(a, st);
@@ -1045,11 +1046,11 @@ template <bool X4> static pac_status launch_linear(const Mx4Args &a, hipStream_t
 static pac_status launch_dx(const Mx4Args &a, hipStream_t st)
 {
     (void)hipGetLastError();
-    switch (dx_form(a.M, a.K, a.N)) {
-    case 0: return launch_dx_rows<1>(a, st);
-    case 1: return launch_dx_rows<2>(a, st);
-    case 2: return launch_dx_tiles<Mx4DxTile<2, 4, 1, 2, 5>>(a, st);
-    case 3: return launch_dx_tiles<Mx4DxTile<2, 4, 2, 2, 3>>(a, st);
+    switch (dx_form(a.M, a.K, a.N).rows) {
+    case 16: return launch_dx_rows<1>(a, st);
+    case 32: return launch_dx_rows<2>(a, st);
+    case 64: return launch_dx_tiles<Mx4DxTile<2, 4, 1, 2, 5>>(a, st);
+    case 128: return launch_dx_tiles<Mx4DxTile<2, 4, 2, 2, 3>>(a, st);
     default: return launch_dx_tiles<Mx4DxTile<4, 2, 2, 4, 2>>(a, st);
     }
 }
@@ -1165,7 +1166,7 @@ pac_status pac_mx4_linear_qx(const void *x, int32_t x_dtype, int32_t M, int32_t 
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     Mx4Args a{x, nullptr, x_stride, codes, scales, M, K, N, code_pitch(K), scale_pitch(K), bias, act, y, y_dtype == PAC_F32, y_stride};
     (void)hipGetLastError();
-    const Mx4Form &form = kMx4LinearX4[linear_form(true, M, K, N)];
+    const Mx4Form &form = linear_form(true, M, K, N);
     // few rows in whole 16-byte pieces: quantised where they are multiplied (one launch)
     if (form.rows <= 32 && x_dtype == PAC_BF16 && K % 8 == 0 && x_stride % 8 == 0 && m_aligned(x, 16))
         return form.rows == 16 ? launch_rows<MX4_XQ, 1>(a, st) : launch_rows<MX4_XQ, 2>(a, st);
@@ -1183,8 +1184,7 @@ pac_status pac_mx4_tiles(int32_t product, int32_t M, int32_t K, int32_t N, int32
     if (!out) return PAC_ERR_NULL;
     if (product < PAC_MX4_LINEAR || product > PAC_MX4_LINEAR_DX || M < 1 || K < 1 || N < 1) return PAC_ERR_SHAPE;
     if (M > kMx4Most || K > kMx4Most || N > kMx4Most) return PAC_ERR_UNSUPPORTED;
-    const Mx4Form &f = product == PAC_MX4_LINEAR ? kMx4Linear[linear_form(false, M, K, N)]
-                       : product == PAC_MX4_LINEAR_X4 ? kMx4LinearX4[linear_form(true, M, K, N)] : kMx4Dx[dx_form(M, K, N)];
+    const Mx4Form &f = product == PAC_MX4_LINEAR_DX ? dx_form(M, K, N) : linear_form(product == PAC_MX4_LINEAR_X4, M, K, N);
     out[0] = f.rows;
     out[1] = f.cols;
     return PAC_OK;

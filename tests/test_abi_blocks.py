@@ -115,7 +115,8 @@ def test_tiles_of_the_products():
     t = pb.pac_mx4_tiles
     assert t(0, 1, 4096, 4096) == t(1, 1, 4096, 4096) == (16, 16) and t(2, 1, 4096, 4096) == (16, 128)
     assert t(0, 4096, 4096, 4096) == t(1, 4096, 4096, 4096) == t(2, 4096, 4096, 4096) == (256, 256)
-    assert t(0, 64, 4096, 4096) == (64, 64) and t(0, 333, 1024, 4096) == (64, 128) and t(0, 1024, 2048, 4096) == (128, 128)
+    assert t(0, 64, 4096, 4096) == (64, 64) and t(0, 1024, 2048, 4096) == (64, 128) and t(0, 5913, 541, 655) == (128, 128)
+    assert t(1, 64, 4096, 2048) == (32, 16) and t(1, 1024, 2048, 4096) == (128, 128)
     big = 1 << 30
     assert t(0, big, big, big) == t(2, big, big, big) == (256, 256)
     out = (C.c_int32 * 2)()

@@ -187,11 +187,10 @@ def test_input_grad(M, K, N):
 
 # Every form of the three products on tiles, steps and rows that end raggedly, and on sizes that divide; contractions that go round
 # the rings of LDS stages more than once, and ones shorter than a ring
-FORMS = [(0, (32, 16), 17, 31, 8721), (0, (64, 64), 33, 521, 8510), (0, (64, 64), 700, 100, 3001), (0, (64, 128), 66, 779, 8903),
-         (0, (64, 128), 2050, 130, 4111), (0, (128, 128), 348, 2065, 7235), (0, (128, 128), 1024, 2048, 4096), (0, (256, 256), 4282, 523, 2958),
-         (0, (256, 256), 4096, 512, 4096),
-         (1, (32, 16), 2079, 30, 18), (1, (64, 64), 33, 514, 8834), (1, (64, 64), 300, 2049, 1030), (1, (128, 128), 711, 1153, 7671),
-         (1, (256, 256), 4562, 515, 2978), (1, (256, 256), 4096, 512, 4096),
+FORMS = [(0, (64, 64), 5582, 1036, 33), (0, (64, 64), 700, 100, 3001), (0, (64, 128), 194, 523, 7276), (0, (64, 128), 1024, 2048, 4096),
+         (0, (128, 128), 5913, 541, 655), (0, (128, 128), 2050, 130, 4111), (0, (256, 256), 4237, 937, 3687), (0, (256, 256), 4096, 1024, 4096),
+         (1, (32, 16), 2834, 30, 17), (1, (64, 64), 33, 1173, 5327), (1, (64, 64), 300, 2049, 1030), (1, (128, 128), 711, 1153, 7671),
+         (1, (256, 256), 4231, 730, 3830), (1, (256, 256), 4096, 1024, 4096),
          (2, (32, 128), 5963, 30, 1123), (2, (64, 256), 5011, 286, 517), (2, (64, 256), 1024, 2049, 1000), (2, (128, 256), 5704, 562, 540),
          (2, (256, 256), 5447, 1482, 500), (2, (256, 256), 4096, 4096, 256)]
 
