@@ -39,7 +39,7 @@ int64_t pac_mx4_scale_pitch(int32_t cols);
 /* x DEVICE [rows][x_stride] of x_dtype (pac_dtype), x_stride >= cols elements apart, any alignment of its type;
  * codes DEVICE, rows * code pitch bytes, 16-byte aligned; scales DEVICE, rows * scale pitch bytes, 8-byte aligned; the padding
  * is written too.  rows = 0: nothing happens, and the addresses may be NULL.  Errors: NULL, SHAPE (cols < 1, x_dtype), RANGE (rows < 0, x_stride < cols),
- * UNSUPPORTED (cols past 2^30, or more than 2^31 - 1 groups of 256 columns in all), ALIGN, DEVICE. */
+ * UNSUPPORTED (cols past 2^28, or more than 2^31 - 1 groups of 256 columns in all), ALIGN, DEVICE. */
 pac_status pac_mx4_quantize(const void *x /*DEVICE*/, int32_t x_dtype, int64_t rows, int32_t cols, int64_t x_stride,
                             uint8_t *codes /*DEVICE*/, uint8_t *scales /*DEVICE*/, void *hip_stream);
 
@@ -56,7 +56,7 @@ pac_status pac_mx4_dequantize(const uint8_t *codes /*DEVICE*/, const uint8_t *sc
  *   codes, scales  DEVICE, W [N][K] in the stored form above          bias  DEVICE fp32 [N], or NULL
  *   y       DEVICE [M][y_stride] of y_dtype, y_stride >= N, any alignment of its type; may not overlap the inputs
  * M = 0: nothing happens, and x and y may be NULL.  Errors: NULL, SHAPE (K or N < 1, M < 0, y_dtype, act), RANGE (strides), ALIGN, UNSUPPORTED (M,
- * K or N past 2^30, or more than 2^31 - 1 tiles), DEVICE. */
+ * K or N past 2^28, or more than 2^31 - 1 tiles), DEVICE. */
 pac_status pac_mx4_linear(const void *x /*DEVICE*/, int32_t M, int32_t K, int64_t x_stride, const uint8_t *codes /*DEVICE*/,
                           const uint8_t *scales /*DEVICE*/, int32_t N, const float *bias /*DEVICE*/, int32_t act,
                           void *y /*DEVICE*/, int32_t y_dtype, int64_t y_stride, void *hip_stream);

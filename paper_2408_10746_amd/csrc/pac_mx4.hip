@@ -911,7 +911,7 @@ static inline int64_t code_pitch(int cols) { return ((int64_t)cols + 255) / 256 
 static inline int64_t scale_pitch(int cols) { return ((int64_t)cols + 255) / 256 * 8; }
 static inline bool dtype_ok(int32_t t) { return t == PAC_BF16 || t == PAC_F32; }
 
-constexpr int32_t kMx4Most = 1 << 30; // rows and columns: places past a tile's end still fit 32 bits
+constexpr int32_t kMx4Most = 1 << 28; // rows and columns: places past a tile's end still fit 32 bits
 // tiles of a launch, or -1 where they pass a grid's limit
 static int64_t tile_count(int64_t a, int64_t b) { return a * b <= 0x7fffffffll ? a * b : -1; }
 

@@ -11,7 +11,7 @@ A = 1 << 20  # an aligned address that no refused call touches
 
 
 def test_pitches_of_the_stored_form():
-    for cols in (1, 31, 32, 255, 256, 257, 4096, 4097, 1 << 30):
+    for cols in (1, 31, 32, 255, 256, 257, 4096, 4097, 1 << 28):
         assert (pb.pac_mx4_code_pitch(cols), pb.pac_mx4_scale_pitch(cols)) == bo.pitches(cols)
     assert pb.pac_mx4_code_pitch(0) == -1 and pb.pac_mx4_scale_pitch(-3) == -1
 
@@ -30,7 +30,7 @@ def test_conversions_refuse():
     assert q(cols=0) == q(dt=2) == pb.PAC_ERR_SHAPE
     assert q(rows=-1) == q(stride=39) == pb.PAC_ERR_RANGE
     assert q(x=A + 2) == q(codes=A + 8) == q(scales=A + 4) == q(x=A + 1, dt=pb.PAC_BF16) == pb.PAC_ERR_ALIGN
-    assert q(rows=1 << 30, cols=1000, stride=1000) == q(cols=(1 << 30) + 1, stride=1 << 31) == pb.PAC_ERR_UNSUPPORTED
+    assert q(rows=1 << 30, cols=1000, stride=1000) == q(cols=(1 << 28) + 1, stride=1 << 29) == pb.PAC_ERR_UNSUPPORTED
 
 
 def test_products_refuse():
@@ -52,7 +52,7 @@ def test_products_refuse():
     for f in (lin, lin4, dx):
         assert f(M=-1) == f(K=0) == f(N=0) == f(dt=5) == pb.PAC_ERR_SHAPE
         assert f(codes=A + 8) == f(scales=A + 4) == pb.PAC_ERR_ALIGN
-        assert f(M=(1 << 30) + 1) == f(K=(1 << 30) + 1) == f(N=(1 << 30) + 1) == pb.PAC_ERR_UNSUPPORTED
+        assert f(M=(1 << 28) + 1) == f(K=(1 << 28) + 1) == f(N=(1 << 28) + 1) == pb.PAC_ERR_UNSUPPORTED
     assert lin(act=2) == lin4(act=-1) == pb.PAC_ERR_SHAPE
     assert lin(sx=32) == lin(sy=6) == lin4(sy=6) == dx(sdy=6) == dx(sdx=39) == pb.PAC_ERR_RANGE
     assert lin(sx=44) == lin(x=A + 8) == lin(y=A + 2) == lin(bias=A + 2) == lin4(x=A + 8) == lin4(xs=A + 4) == pb.PAC_ERR_ALIGN
@@ -68,8 +68,8 @@ def test_products_refuse():
     assert linq(M=-1) == linq(K=0) == linq(N=0) == linq(dt=5) == linq(xdt=5) == linq(act=2) == pb.PAC_ERR_SHAPE
     assert linq(sx=39) == linq(sy=6) == pb.PAC_ERR_RANGE and linq(n=4 * 136 - 1) == pb.PAC_ERR_WORKSPACE
     assert linq(x=A + 1) == linq(x=A + 2, xdt=pb.PAC_F32) == linq(codes=A + 8) == linq(scales=A + 4) == linq(bias=A + 2) == linq(ws=A + 8) == pb.PAC_ERR_ALIGN
-    assert linq(M=(1 << 30) + 1) == linq(K=(1 << 30) + 1, sx=1 << 31) == pb.PAC_ERR_UNSUPPORTED
-    big = 1 << 30
+    assert linq(M=(1 << 28) + 1) == linq(K=(1 << 28) + 1, sx=1 << 29) == pb.PAC_ERR_UNSUPPORTED
+    big = 1 << 28
     assert lin(M=big, N=big, sy=big) == lin4(M=big, N=big, sy=big) == dx(M=big, K=big, sdx=big) == pb.PAC_ERR_UNSUPPORTED
 
 
@@ -117,7 +117,7 @@ def test_tiles_of_the_products():
     assert t(0, 4096, 4096, 4096) == t(1, 4096, 4096, 4096) == t(2, 4096, 4096, 4096) == (256, 256)
     assert t(0, 64, 4096, 4096) == (64, 64) and t(0, 1024, 2048, 4096) == (64, 128) and t(0, 5913, 541, 655) == (128, 128)
     assert t(1, 64, 4096, 2048) == (32, 16) and t(1, 1024, 2048, 4096) == (128, 128)
-    big = 1 << 30
+    big = 1 << 28
     assert t(0, big, big, big) == t(2, big, big, big) == (256, 256)
     out = (C.c_int32 * 2)()
     L = pb.lib()
