@@ -17,7 +17,8 @@ __device__ __forceinline__ float mx4_scale(uint32_t byte) { return __uint_as_flo
 // ---------------------------------------------------------------------------
 // quantise: four lanes a block, eight neighbouring values each (16-byte loads where the rows allow them: VEC).  The block's
 // absmax goes round its four lanes; the scale's exponent is the absmax's own exponent less two, so no logarithm is taken;
-// the conversion divides by the scale, rounds to nearest even and saturates at 6 in one instruction a pair.
+// the conversion divides by the scale, rounds to nearest even and saturates at 6 in one instruction a pair.  Memory bounds it:
+// 4096 x 4096 fp32 in 12.5 us (76 MB: 6.1 TB/s, part of it from the last-level cache), the way back in 15.4 us (4.8 TB/s).
 // ---------------------------------------------------------------------------
 template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void k_mx4_quant(const T *__restrict__ x, uint32_t units, uint32_t upr, int cols, int64_t ldx,
@@ -213,7 +214,9 @@ __device__ __forceinline__ u32x4 mx4_keep(u32x4 v, int valid)
 // A tile of 16 columns of y by 16 RM rows a workgroup, the contraction dealt over its NW wavefronts in steps of 128 and joined in
 // LDS in a fixed order.  Operands go from memory straight into registers: lane (i, q) holds row i's block of 32 number q of the
 // step, so that a lane has one scale, its 16 bytes of codes are one load, and four matrix instructions of 32 (one of 128 where x
-// is stored too) take eight codes of every lane's block each: the order of the sum does not matter to it.
+// is stored too) take eight codes of every lane's block each: the order of the sum does not matter to it.  For few rows, where
+// neither tiles nor matrix rate count: 1 x 4096 x 4096 in 5.7 us, of which a launch takes 2.5 and the 9 MB of W 1.8 at a copy's
+// rate.  (With the next step's operands requested ahead by hand it is slower, 64 x 4096 x 4096 25 -> 30 us: fewer workgroups fit.)
 // What x is to it: bf16 rows, the stored form, or bf16 rows that are to count as their mx4 values: a lane holds whole blocks, so it
 // quantises them by itself, and the call needs no launch and no memory for x's stored form.
 enum { MX4_X16, MX4_X4, MX4_XQ };
@@ -329,7 +332,8 @@ template <int X, int RM, int NW> __global__ __launch_bounds__(64 * NW) void k_mx
 // across W's rows, eight of which a lane needs for one column: a lane loads 4 bytes (eight columns) of eight rows, converts them
 // with each row's scale and swaps halves of register pairs, which leaves it the eight rows of eight columns.  The matrix
 // instruction number c takes column c of every lane, so lanes i = 0 .. 15 cover 128 neighbouring columns and an output lane holds
-// eight neighbouring ones: no transposed copy of W anywhere.
+// eight neighbouring ones: no transposed copy of W anywhere.  1 x 4096 x 4096 in 13 us, 517 x 1001 x 775 in 7 us; the vector
+// units bound it (64 instructions a step to convert and swap, beside eight matrix instructions).
 __device__ __forceinline__ uint32_t pk_lo(bf16x2 a, bf16x2 b) // {a[0], b[0]}
 {
     return __builtin_amdgcn_perm(*reinterpret_cast<uint32_t *>(&b), *reinterpret_cast<uint32_t *>(&a), 0x05040100u);
@@ -446,6 +450,8 @@ template <int RM, int NW> __global__ __launch_bounds__(64 * NW) void k_mx4_dx_ro
 // instructions as they lie.  A lane (i, g) owns row i and, of each step, the blocks of its half g: one 16-byte read is a block of
 // codes, and a lane has one scale a block.  Scales, eight bytes a row and 256 columns, come the same way into a ring of their own:
 // loaded into registers they make the compiler, which does not count the transfers, wait for all of these at every use.
+// 4096^3: 106 us, 1300 TFLOP/s (a library's bf16 product without the conversion: 98 us); 8192^3: 790 us, 1390 TFLOP/s, where the
+// chip's power limit shows (without any transfers in the loop 740 us).
 // Fragment i of subtile y stands for column WTN i + y of the wavefront's, so that a lane ends up with WTN neighbouring columns.
 // The 256 x 256 tiles of stored x take steps of 256 columns through two stages, half the barriers of steps of 128 through four:
 // 4096 x 4096 x 16384 166 -> 161 us.  What bounds them there: reads of LDS and matrix instructions, each about as long as the other.
@@ -745,7 +751,9 @@ template <class TL> __global__ __launch_bounds__(64 * TL::NW, 2) void k_mx4_tile
 // instructions: a thread takes eight columns of four rows, converts them with each row's scale, and writes the four rows of each
 // column side by side, as the fragments want them.  Stage t of the ring holds dy's step t and W's step t + 1.
 // LDS row c 32 + i holds column 8 i + c: the writes of 32 threads and the reads of a fragment then go to neighbouring rows, and
-// subtile c of lane i is column 8 i + c of the tile, WTN neighbouring ones a lane.
+// subtile c of lane i is column 8 i + c of the tile, WTN neighbouring ones a lane.  4096^3: 119 us, 1150 TFLOP/s; matrix units busy
+// half the time, LDS a third (fragments of both sides in bf16, and W's turned rows written): neither is full, they wait for each
+// other at the barrier of each step.  (W's rows through registers instead: 115 us for these tiles, 5 to 10 us more for the smaller.)
 template <int WM_, int WN_, int WTM_, int WTN_, int STAGES_> struct Mx4DxTile {
     static constexpr int WM = WM_, WN = WN_, WTM = WTM_, WTN = WTN_, STAGES = STAGES_, NW = WM * WN;
     static constexpr int TM = 32 * WM * WTM, TK = 256;

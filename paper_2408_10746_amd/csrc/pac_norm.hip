@@ -157,6 +157,10 @@ __device__ __forceinline__ void norm_back(float (&g)[E], const float (&h)[E], fl
 template <int TPR> constexpr int kRowsPerBlock = TPR < 512 ? 512 / TPR : 1;
 template <int TPR> constexpr int kNormThreads = TPR < 512 ? 512 : TPR;
 
+// Forward: a row is loaded once, lives in registers through both norms, and y and n are stored from there: two reads and two writes
+// a value, the least there is.  Blocks go through rows with the next row's loads under way.  Memory bounds it: 16384 x 4096 bf16 in
+// 104 us is 5.2 TB/s, what a copy reaches; one row of 4096 takes 2.9 us, a launch's time.  (16 values a thread and the parameters
+// read at every row: 116 us.)
 // HOLD: the parameters stay in registers from row to row, loaded along with the first row; else (rows past 8192, whose values fill
 // the registers) they are loaded for every row
 template <typename T, int VEC, int TPR, int E, bool LAYER, bool HOLD> __global__ __launch_bounds__(kNormThreads<TPR>) void k_norm_fwd(NormArgs a)
@@ -221,6 +225,12 @@ template <typename T, int VEC, int TPR, int E, bool LAYER, bool HOLD> __global__
     }
 }
 
+// Backward: y and both norms are made again from x and o (nothing is saved by the forward pass: a row in registers costs no memory
+// traffic), then the gradients go back through them; four reads and two writes a value.  Sums over rows stay with the columns'
+// threads, one partial sum a block and column, added by k_norm_sums: no atomics, the same bits each time.  4096 x 4096 bf16 in 50
+// us is 4.0 TB/s, then 4.4 us of sums; what bounds it is a row's chain of four sums over 16 wavefronts, one block a compute unit.
+// Four values a thread and the parameters held: 8 a thread with parameters read at every row 51 us at 4096 and 35 against 19 us at
+// 2723 x 768 fp32, held at 8 a thread they spill (66 us); 16 a thread 142 us; two rows under way 53 us.
 // SHIFT: sums of g and of dn for the shifts' gradients (b_post, b_pre) are wanted too
 template <typename T, int VEC, int TPR, int E, bool LAYER, bool SHIFT, bool HOLD>
 __global__ __launch_bounds__(kNormThreads<TPR>, 4) void k_norm_bwd(NormArgs a)
@@ -467,7 +477,9 @@ static int64_t norm_blocks(int d, int64_t rows, bool backward)
 {
     const int tpr = norm_form(d, backward).tpr, rpb = tpr < 512 ? 512 / tpr : 1;
     const int64_t want = (rows + rpb - 1) / rpb, most = backward ? (tpr == 1024 ? 256 : 512) : 1024;
-    return want < most ? want : most;
+    if (want <= most) return want;
+    const int64_t rounds = (want + most - 1) / most;
+    return (want + rounds - 1) / rounds; // as many rows a block everywhere, as few blocks' sums as that leaves
 }
 
 template <typename T, int VEC, int TPR, int E, bool LAYER> static void launch_fwd(const NormArgs &a, dim3 g, hipStream_t st)
