@@ -753,7 +753,7 @@ template <class TL> __global__ __launch_bounds__(64 * TL::NW, 2) void k_mx4_tile
 // LDS row c 32 + i holds column 8 i + c: the writes of 32 threads and the reads of a fragment then go to neighbouring rows, and
 // subtile c of lane i is column 8 i + c of the tile, WTN neighbouring ones a lane.  4096^3: 119 us, 1150 TFLOP/s; matrix units busy
 // half the time, LDS a third (fragments of both sides in bf16, and W's turned rows written): neither is full, they wait for each
-// other at the barrier of each step.  (W's rows through registers instead: 115 us for these tiles, 5 to 10 us more for the smaller.)
+// other at the barrier of each step.  (W through registers instead of LDS, in the same loop: 125 us.)
 template <int WM_, int WN_, int WTM_, int WTN_, int STAGES_> struct Mx4DxTile {
     static constexpr int WM = WM_, WN = WN_, WTM = WTM_, WTN = WTN_, STAGES = STAGES_, NW = WM * WN;
     static constexpr int TM = 32 * WM * WTM, TK = 256;
@@ -805,7 +805,7 @@ template <class TL> __global__ __launch_bounds__(64 * TL::NW, 2) void k_mx4_dx_t
         dma4_at(a.ws + n * a.sp + k0 / 32 + 4 * (lane & 1), lds0 + slot * TL::STAGE_BYTES + TL::S_AT + piece * 256);
     };
     // this thread's part of turning W: columns 8 cg .. 8 cg + 7, rows 4 ng .. 4 ng + 3 of a step; 32 lanes are 16 cg and two ng, whose
-    // 8-byte writes fill each other's 16 bytes (32 cg of one ng met every second bank twice)
+    // 8-byte writes fill each other's 16 bytes
     const int cg = (lane & 15) + 16 * g, ng = 2 * wave + ((lane >> 4) & 1);
     const int wat = cg * 128 + (((ng >> 1) ^ mx4_swz<128>(cg)) << 4) + 8 * (ng & 1); // where column 8 cg goes; the next: 4096 bytes on
     uint32_t wr[4], sr[4];
