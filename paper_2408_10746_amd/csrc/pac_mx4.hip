@@ -450,11 +450,13 @@ template <int RM, int NW> __global__ __launch_bounds__(64 * NW) void k_mx4_dx_ro
 // instructions as they lie.  A lane (i, g) owns row i and, of each step, the blocks of its half g: one 16-byte read is a block of
 // codes, and a lane has one scale a block.  Scales, eight bytes a row and 256 columns, come the same way into a ring of their own:
 // loaded into registers they make the compiler, which does not count the transfers, wait for all of these at every use.
-// 4096^3: 106 us, 1300 TFLOP/s (a library's bf16 product without the conversion: 98 us); 8192^3: 790 us, 1390 TFLOP/s, where the
-// chip's power limit shows (without any transfers in the loop 740 us).
+// 4096^3: 106 us, 1300 TFLOP/s (a library's bf16 product without the conversion: 98 us); 8192^3: 790 us, 1390 TFLOP/s
+// (740 us with no transfers in the loop, on whatever LDS held).
 // Fragment i of subtile y stands for column WTN i + y of the wavefront's, so that a lane ends up with WTN neighbouring columns.
 // The 256 x 256 tiles of stored x take steps of 256 columns through two stages, half the barriers of steps of 128 through four:
-// 4096 x 4096 x 16384 166 -> 161 us.  What bounds them there: reads of LDS and matrix instructions, each about as long as the other.
+// 4096 x 4096 x 16384 166 -> 161 us.  A step of theirs takes 2.07 us on the whole chip; 1.52 with no transfers, on whatever LDS
+// held, so that up to a quarter is theirs (other operands may draw less power); its matrix instructions would take 0.98 at the rate
+// that they reach alone.  Busy by counters: matrix units 39 %, LDS reads 18 %; what fills the rest is not settled.
 // ---------------------------------------------------------------------------
 template <bool X4_, int WM_, int WN_, int WTM_, int WTN_, int STAGES_, int BK_> struct Mx4Tile {
     static constexpr bool X4 = X4_;
@@ -752,8 +754,8 @@ template <class TL> __global__ __launch_bounds__(64 * TL::NW, 2) void k_mx4_tile
 // column side by side, as the fragments want them.  Stage t of the ring holds dy's step t and W's step t + 1.
 // LDS row c 32 + i holds column 8 i + c: the writes of 32 threads and the reads of a fragment then go to neighbouring rows, and
 // subtile c of lane i is column 8 i + c of the tile, WTN neighbouring ones a lane.  4096^3: 119 us, 1150 TFLOP/s; matrix units busy
-// half the time, LDS a third (fragments of both sides in bf16, and W's turned rows written): neither is full, they wait for each
-// other at the barrier of each step.  (W through registers instead of LDS, in the same loop: 125 us.)
+// 53 % of the time, LDS reads 38 % (fragments of both sides in bf16; W's turned rows are written beside them), wavefronts waiting
+// 26 %: neither unit is full, and what holds the loop is not settled.  (W through registers instead of LDS, in the same loop: 125 us.)
 template <int WM_, int WN_, int WTM_, int WTN_, int STAGES_> struct Mx4DxTile {
     static constexpr int WM = WM_, WN = WN_, WTM = WTM_, WTN = WTN_, STAGES = STAGES_, NW = WM * WN;
     static constexpr int TM = 32 * WM * WTM, TK = 256;
