@@ -43,7 +43,8 @@ typedef struct {
 pac_status pac_block_norm_forward(const pac_block_norm *b /*HOST*/, int64_t rows, const void *x /*DEVICE*/,
                                   const void *o /*DEVICE*/, void *y /*DEVICE*/, void *n /*DEVICE*/, void *hip_stream);
 
-/* Bytes of workspace for the gradients of `rows` rows (partial sums of the parameters' gradients); -1 on bad arguments. */
+/* Bytes of workspace for the gradients of `rows` rows (partial sums of the parameters' gradients), never fewer for more rows: one
+ * workspace for the largest batch serves them all.  -1 on bad arguments. */
 int64_t pac_block_norm_workspace_bytes(const pac_block_norm *b /*HOST*/, int64_t rows);
 
 /* Gradients.  x, o as in the forward pass; dy, dn DEVICE [rows][d], the gradients of y (NULL: zero) and of n (there where

@@ -473,13 +473,19 @@ static NormForm norm_form(int d, bool backward)
     return {e, tpr};
 }
 
-static int64_t norm_blocks(int d, int64_t rows, bool backward)
+// Blocks that rows may take, which never falls as they grow: a workspace for many rows serves fewer ...
+static int64_t norm_blocks_most(int d, int64_t rows, bool backward)
 {
     const int tpr = norm_form(d, backward).tpr, rpb = tpr < 512 ? 512 / tpr : 1;
     const int64_t want = (rows + rpb - 1) / rpb, most = backward ? (tpr == 1024 ? 256 : 512) : 1024;
-    if (want <= most) return want;
-    const int64_t rounds = (want + most - 1) / most;
-    return (want + rounds - 1) / rounds; // as many rows a block everywhere, as few blocks' sums as that leaves
+    return want < most ? want : most;
+}
+// ... and those that a launch has: as many rows a block everywhere, as few blocks' sums as that leaves
+static int64_t norm_blocks(int d, int64_t rows, bool backward)
+{
+    const int tpr = norm_form(d, backward).tpr, rpb = tpr < 512 ? 512 / tpr : 1;
+    const int64_t want = (rows + rpb - 1) / rpb, most = norm_blocks_most(d, rows, backward), rounds = (want + most - 1) / most;
+    return (want + rounds - 1) / rounds;
 }
 
 template <typename T, int VEC, int TPR, int E, bool LAYER> static void launch_fwd(const NormArgs &a, dim3 g, hipStream_t st)
@@ -576,7 +582,7 @@ pac_status pac_block_norm_forward(const pac_block_norm *b, int64_t rows, const v
 int64_t pac_block_norm_workspace_bytes(const pac_block_norm *b, int64_t rows)
 {
     if (check_norm(b, rows) != PAC_OK) return -1;
-    return (norm_blocks(b->d, rows < 1 ? 1 : rows, true) * (16 + 16 * (int64_t)b->d) + 255) / 256 * 256; // two doubles, four rows of floats
+    return (norm_blocks_most(b->d, rows < 1 ? 1 : rows, true) * (16 + 16 * (int64_t)b->d) + 255) / 256 * 256; // two doubles, four rows of floats
 }
 
 pac_status pac_block_norm_backward(const pac_block_norm *b, int64_t rows, const void *x, const void *o, const void *dy, const void *dn,

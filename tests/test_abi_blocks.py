@@ -124,3 +124,13 @@ def test_tiles_of_the_products():
     assert L.pac_mx4_tiles(0, 1, 1, 1, None) == pb.PAC_ERR_NULL
     assert L.pac_mx4_tiles(3, 1, 1, 1, out) == L.pac_mx4_tiles(-1, 1, 1, 1, out) == L.pac_mx4_tiles(0, 0, 1, 1, out) == pb.PAC_ERR_SHAPE
     assert L.pac_mx4_tiles(0, 1, big + 1, 1, out) == pb.PAC_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("d", [40, 96, 768, 1032, 4096, 5120, 16384])
+def test_a_workspace_for_many_rows_serves_fewer(d):
+    """A caller sizes one workspace for its largest batch: the bytes never fall as rows grow (forms of every width)."""
+    b = norm(d=d, w_post=A)
+    for rows in (range(1, 2001), range(2001, 40000, 97), [1 << k for k in range(16, 40)]):
+        need = [pb.pac_block_norm_workspace_bytes(b, r) for r in rows]
+        assert need[0] > 0 and need == sorted(need)
+    assert pb.pac_block_norm_workspace_bytes(b, 0) <= pb.pac_block_norm_workspace_bytes(b, 1)
