@@ -16,7 +16,8 @@
  *     dw_post = sum gate g N(o)    db_post = sum gate g    dw_pre = sum dn N(y)    db_pre = sum dn    (sums over the rows)
  *
  * One pass over the data in each direction.  States and their gradients are bf16 or fp32, everything else fp32; y enters N
- * before it is rounded.  Sums over rows have a fixed order: the same call gives the same bits.
+ * before it is rounded.  Sums over rows have a fixed order: the same call gives the same bits.  They are added in 32 bits over at
+ * most 64 rows one after the other (8 such sums at most after that), and in 64 bits from there (to 2^30 rows).
  */
 #ifndef PAC_NORM_H
 #define PAC_NORM_H

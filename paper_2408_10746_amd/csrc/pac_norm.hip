@@ -473,12 +473,17 @@ static NormForm norm_form(int d, bool backward)
     return {e, tpr};
 }
 
+// A block adds its columns over rows in 32 bits, this many one after the other at most: past that there are more blocks instead, whose
+// sums are joined in 64 bits, so that the error does not grow with the batch (to the 2^30 rows that the last number is good for).
+constexpr int64_t kNormRounds = 64, kNormBlocks = 1 << 21;
+
 // Blocks that rows may take, which never falls as they grow: a workspace for many rows serves fewer ...
 static int64_t norm_blocks_most(int d, int64_t rows, bool backward)
 {
     const int tpr = norm_form(d, backward).tpr, rpb = tpr < 512 ? 512 / tpr : 1;
     const int64_t want = (rows + rpb - 1) / rpb, most = backward ? (tpr == 1024 ? 256 : 512) : 1024;
-    return want < most ? want : most;
+    const int64_t more = backward ? (want + kNormRounds - 1) / kNormRounds : 0;
+    return want < most ? want : more < most ? most : more < kNormBlocks ? more : kNormBlocks;
 }
 // ... and those that a launch has: as many rows a block everywhere, as few blocks' sums as that leaves
 static int64_t norm_blocks(int d, int64_t rows, bool backward)

@@ -134,3 +134,11 @@ def test_a_workspace_for_many_rows_serves_fewer(d):
         need = [pb.pac_block_norm_workspace_bytes(b, r) for r in rows]
         assert need[0] > 0 and need == sorted(need)
     assert pb.pac_block_norm_workspace_bytes(b, 0) <= pb.pac_block_norm_workspace_bytes(b, 1)
+
+
+@pytest.mark.parametrize("d", [40, 768, 4096, 16384])
+def test_blocks_add_at_most_64_rows_one_after_another(d):
+    """The workspace holds a block's sums, 16 bytes a column and 16 more; a block of narrow rows takes eight side by side."""
+    b, side = norm(d=d, w_post=A), {40: 8, 768: 2}.get(d, 1)
+    for rows in (1 << 16, 1 << 20, (1 << 26) + 1):
+        assert pb.pac_block_norm_workspace_bytes(b, rows) >= rows / (64 * side) * (16 + 16 * d)

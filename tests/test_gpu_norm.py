@@ -233,3 +233,20 @@ def test_what_python_refuses():
                 lambda: bn.forward(x, x[:2], x, x), lambda: bn.forward(x.t().contiguous().t(), x, x, x), lambda: bn.backward(x, x, x, x, x, x, {"gate": one})):
         with pytest.raises(ValueError):
             bad()
+
+
+def test_sums_over_many_rows_lose_no_more_than_over_few():
+    """2^23 rows: columns of equal terms, whose roundings all lean one way where they are added one after another."""
+    rows, d = 1 << 23, 8
+    rng = np.random.default_rng(6)
+    x = dev(np.float32(1 + rng.random((1, d)))).expand(rows, d).contiguous()
+    dn = dev(np.float32(1 + rng.random((1, d)))).expand(rows, d).contiguous()
+    p = {"w_pre": torch.ones(d, device="cuda"), "b_pre": torch.zeros(d, device="cuda"), "res": torch.ones(1, device="cuda")}
+    dp = {k: torch.empty_like(t) for k, t in p.items()}
+    rt.BlockNorm(d, layer=True, **p).backward(x, None, None, dn, dparams=dp)
+    hx, hn = host(x[:1]), host(dn[:1])
+    ref = bo.block_norm_grad(hx, None, None, hn, layer=True, eps=1e-5, **{k: host(t) for k, t in p.items()})
+    h, r = bo._norm(hx, True, 1e-5)
+    amp = 1 + np.abs(hx).max() * r
+    for k, scale in (("b_pre", np.abs(hn)[0]), ("w_pre", (np.abs(hn) * (np.abs(h) + 1) * amp)[0])):
+        assert np.max(np.abs(host(dp[k]) - rows * ref[k]) / (128 * U * rows * scale)) <= 1.0, k
