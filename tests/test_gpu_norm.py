@@ -250,3 +250,80 @@ def test_sums_over_many_rows_lose_no_more_than_over_few():
     amp = 1 + np.abs(hx).max() * r
     for k, scale in (("b_pre", np.abs(hn)[0]), ("w_pre", (np.abs(hn) * (np.abs(h) + 1) * amp)[0])):
         assert np.max(np.abs(host(dp[k]) - rows * ref[k]) / (128 * U * rows * scale)) <= 1.0, k
+
+
+# (rows, d) whose blocks go on to a second and third row, the last round ragged: every count of threads a row, values held and
+# loaded again, whole pieces and single values (a width or an address off 16 bytes)
+ROUNDS = [(17003, 40), (17001, 130), (9003, 1000), (4103, 1500), (2081, 2056), (2051, 4096), (2053, 5120), (2050, 8200), (2049, 16383)]
+ROUNDS_GRAD = [(9003, 40), (9001, 96), (4501, 392), (2077, 776), (1083, 1032), (531, 4096), (533, 4099), (517, 5120), (515, 16384), (515, 16383)]
+
+
+def parts_of(rng, rows, d, dtype, form):
+    kw = {k: form[k] for k in ("gate", "res", "post", "pre", "bias")}
+    return make(rng, rows, d, dtype, **kw)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("c", FORMS[:2], ids=ids)
+@pytest.mark.parametrize("rows,d", ROUNDS)
+def test_a_row_is_the_same_in_any_round_forward(rows, d, c, dtype):
+    """A block's later rows give the bits that they give alone, at a place where a block has one row (a row's dealing over threads
+    depends on d alone), and rows of the first, a middle and the last round agree with the oracle."""
+    rng = np.random.default_rng(rows + d)
+    v, p = parts_of(rng, rows, d, dtype, c)
+    bn = rt.BlockNorm(d, layer=c["layer"], **p)
+    y, n = torch.empty_like(v["x"]), torch.empty_like(v["x"])
+    bn.forward(v["x"], v["o"], y, n)
+    few = 500
+    for at in range(0, rows, few):
+        x, o = v["x"][at:at + few].clone(), v["o"][at:at + few].clone()
+        y1, n1 = torch.empty_like(x), torch.empty_like(x)
+        bn.forward(x, o, y1, n1)
+        assert torch.equal(y1, y[at:at + few]) and torch.equal(n1, n[at:at + few]), at
+    pick = [0, rows // 2, rows - 1]
+    ry, rn = bo.block_norm(host(v["x"][pick]), host(v["o"][pick]), layer=c["layer"], eps=1e-5, **{k: host(t) for k, t in p.items()})
+    big = 4 * np.abs(ry).max() + 4
+    near(y[pick], ry, big, dtype, "y")
+    near(n[pick], rn, big * np.abs(rn).max(), dtype, "n")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("c", FORMS[:2], ids=ids)
+@pytest.mark.parametrize("rows,d", ROUNDS_GRAD)
+def test_a_row_is_the_same_in_any_round_backward(rows, d, c, dtype):
+    """States' gradients: the bits that a block's single rows give.  Parameters': 128 x 2^-24 of the sum of the absolute terms off the sum
+    of the single rounds' own, of which each is as near to its own."""
+    rng = np.random.default_rng(rows * 3 + d)
+    v, p = parts_of(rng, rows, d, dtype, c)
+    bn = rt.BlockNorm(d, layer=c["layer"], **p)
+    dy, dn = dev(rng.standard_normal((rows, d)), DT[dtype]), dev(rng.standard_normal((rows, d)), DT[dtype])
+    dx, do = torch.empty_like(dy), torch.empty_like(dy)
+    dp = {k: torch.empty_like(t) for k, t in p.items()}
+    bn.backward(v["x"], v["o"], dy, dn, dx, do, dp)
+    few, sums = 250, {k: np.zeros(t.numel()) for k, t in p.items()}
+    for at in range(0, rows, few):
+        s = slice(at, at + few)
+        x, o, gy, gn = (t[s].clone() for t in (v["x"], v["o"], dy, dn))
+        dx1, do1 = torch.empty_like(x), torch.empty_like(x)
+        dp1 = {k: torch.empty_like(t) for k, t in p.items()}
+        bn.backward(x, o, gy, gn, dx1, do1, dp1)
+        assert torch.equal(dx1, dx[s]) and torch.equal(do1, do[s]), at
+        for k in sums:
+            sums[k] += host(dp1[k])
+    # the terms' absolute values, from the oracle on all rows
+    hp = {k: host(t) for k, t in p.items()}
+    hx, ho, hy, hn = host(v["x"]), host(v["o"]), host(dy), host(dn)
+    L = c["layer"]
+    oh = bo._norm(ho, L, 1e-5)[0]
+    post = oh * hp["w_post"] + hp.get("b_post", 0.0)
+    yh, ry = bo._norm(hp["res"][0] * hx + hp["gate"] * post, L, 1e-5)
+    g = np.abs(hy + bo._norm_back(hn * hp["w_pre"], yh, ry, L))
+    gate = np.abs(hp["gate"])
+    terms = {"w_post": (gate * g * np.abs(oh)).sum(0), "b_post": (gate * g).sum(0), "res": (g * np.abs(hx)).sum(), "w_pre": (np.abs(hn) * np.abs(yh)).sum(0),
+             "b_pre": np.abs(hn).sum(0), "gate": (g * np.abs(post)).sum(0) if c["gate"] == 2 else (g * np.abs(post)).sum()}
+    ref = bo.block_norm_grad(hx, ho, hy, hn, layer=L, eps=1e-5, **hp)
+    for k, t in dp.items():
+        assert np.max(np.abs(host(t) - sums[k]) / (2 * 128 * U * terms[k] + 1e-30)) <= 1.0, k
+        # an element's own error: statistics of d terms (64 x 2^-24) of row-sized parts, in g through two norms
+        own = 64 * U * 16 * (1 + np.abs(oh).max() + np.abs(yh).max())
+        assert np.max(np.abs(host(t) - ref[k]) / ((128 * U + own) * (terms[k] + terms[k].max()))) <= 1.0, k
