@@ -325,3 +325,99 @@ def test_layer_from_weights_and_what_python_refuses():
     with pytest.raises(pb.PacError) as e:                # rows that do not start on 16 bytes
         rt.Mx4Linear(*rt.mx4_empty(24, 37), 37).forward(torch.zeros(4, 37, dtype=torch.bfloat16, device="cuda")[:3], y)
     assert e.value.status == pb.PAC_ERR_ALIGN
+
+
+def stored_rows(x, K):
+    """The values that x's quantised rows stand for (the quantiser itself is compared with the oracle above)."""
+    xc, xs = rt.mx4_empty(x.shape[0], K)
+    rt.mx4_quantize(x, xc, xs)
+    return bo.values(xc.cpu().numpy(), xs.cpu().numpy(), K)
+
+
+@pytest.mark.parametrize("product,tile,M,K,N", [f for f in FORMS if f[0] != 2])
+def test_bias_and_gelu_on_each_form(product, tile, M, K, N):
+    """The epilogue of every tile form: bias at ragged edges and in whole stores, GELU, both types, rows that take whole stores and not."""
+    assert pb.pac_mx4_tiles(product, M, K, N) == tile
+    rng = np.random.default_rng(M * 3 + K + N)
+    codes, scales, w = layer(rng, N, K)
+    x = rows_of(rng, M, K)
+    bias = rng.standard_normal(N).astype(np.float32)
+    lin, plain = rt.Mx4Linear(codes, scales, K, bias=dev(bias)), rt.Mx4Linear(codes, scales, K)
+    pre, absum = bo.linear(stored_rows(x, K) if product == 1 else host(x), w)
+    bias = bias.astype(np.float64)
+    act = lambda u: (0.5 * torch.from_numpy(u) * torch.special.erfc(torch.from_numpy(-u / np.sqrt(2)))).numpy()  # noqa: E731
+    with_bias = pre + bias
+    both = act(with_bias)
+    for layer_, ref, b, gelu, dtype in ((lin, with_bias, bias, False, "f32"), (lin, both, bias, True, "bf16"), (lin, both, bias, True, "f32"),
+                                        (lin, with_bias, bias, False, "bf16"), (plain, act(pre), None, True, "bf16")):
+        err = bar(ref, absum, K, dtype, b, gelu)
+        store = torch.full((M, N + 3), 5.0, dtype=DT[dtype], device="cuda")
+        for y in (store[:, :N], torch.empty(M, N, dtype=DT[dtype], device="cuda")):
+            layer_.forward(x, y, gelu=gelu, x4=product == 1)
+            check(host(y), ref, err)
+        assert (store[:, N:] == 5.0).all()
+
+
+@pytest.mark.parametrize("product,tile,M,K,N", FORMS)
+def test_blocks_without_a_value_on_each_form(product, tile, M, K, N):
+    """As above on every tile form: a block of W that stands for NaN, an infinity in one row of x or dy."""
+    assert pb.pac_mx4_tiles(product, M, K, N) == tile
+    rng = np.random.default_rng(M + 2 * K + N)
+    codes, scales, _ = layer(rng, N, K)
+    row, block, bad = N - 1 - N // 3, (K - 1) // 64, M - 1 - M // 5
+    lin = rt.Mx4Linear(codes, scales, K)
+    x = rows_of(rng, M, N if product == 2 else K)
+    y = torch.empty(M, K if product == 2 else N, device="cuda")
+    go = (lambda: lin.input_grad(x, y)) if product == 2 else (lambda: lin.forward(x, y, x4=product == 1))  # noqa: E731
+    was, scales[row, block] = int(scales[row, block]), 255
+    go()
+    nan = torch.isnan(y)
+    if product == 2:
+        wide = min(32, K - 32 * block)
+        assert nan[:, 32 * block:32 * block + wide].all() and int(nan.sum()) == M * wide
+    else:
+        assert nan[:, row].all() and int(nan.sum()) == M
+    scales[row, block] = was
+    x[bad, x.shape[1] // 2] = float("inf")
+    go()
+    fine = torch.isfinite(y)
+    assert not fine[bad].all() and int(fine.sum()) == (M - 1) * y.shape[1] + int(fine[bad].sum())
+    if product == 1:
+        assert torch.isnan(y[bad]).all()
+
+
+@pytest.mark.parametrize("M,K,N", [(2000, 3001, 1000), (1024, 4096, 4096), (4096, 1024, 4096), (5447, 1482, 500)])
+def test_tile_kernels_in_a_graph_and_on_another_stream(M, K, N):
+    assert all(pb.pac_mx4_tiles(p, M, K, N)[0] >= 64 for p in (0, 1)) and pb.pac_mx4_tiles(2, M, K, N)[0] >= 64
+    rng = np.random.default_rng(9)
+    codes, scales, _ = layer(rng, N, K)
+    lin = rt.Mx4Linear(codes, scales, K, bias=dev(rng.standard_normal(N), torch.float32))
+    x, dy = rows_of(rng, M, K, 0.0), rows_of(rng, M, N, 0.0)
+    outs = lambda: (torch.empty(M, N, device="cuda"), torch.empty(M, N, device="cuda"), torch.empty(M, K, device="cuda"))  # noqa: E731
+
+    def go(o):
+        lin.forward(x, o[0], gelu=True)
+        lin.forward(x, o[1], gelu=True, x4=True)
+        lin.input_grad(dy, o[2])
+
+    ref, other, graph = outs(), outs(), outs()
+    go(ref)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        go(other)
+        go(graph)
+    s.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(ref, other))
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        go(graph)
+    for k in range(3):
+        x.mul_(-0.5), dy.mul_(-0.5)
+        for t in graph:
+            t.zero_()
+        go(ref)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(ref, graph)), k
