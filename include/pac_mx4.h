@@ -56,7 +56,7 @@ pac_status pac_mx4_dequantize(const uint8_t *codes /*DEVICE*/, const uint8_t *sc
  *   codes, scales  DEVICE, W [N][K] in the stored form above          bias  DEVICE fp32 [N], or NULL
  *   y       DEVICE [M][y_stride] of y_dtype, y_stride >= N, any alignment of its type; may not overlap the inputs
  * M = 0: nothing happens, and x and y may be NULL.  Errors: NULL, SHAPE (K or N < 1, M < 0, y_dtype, act), RANGE (strides), ALIGN, UNSUPPORTED (M,
- * K or N past 2^28, or more than 2^31 - 1 tiles), DEVICE. */
+ * K or N past 2^28, or more than 2^23 - 1 tiles in every form: past 2^38 results where they fill tiles), DEVICE. */
 pac_status pac_mx4_linear(const void *x /*DEVICE*/, int32_t M, int32_t K, int64_t x_stride, const uint8_t *codes /*DEVICE*/,
                           const uint8_t *scales /*DEVICE*/, int32_t N, const float *bias /*DEVICE*/, int32_t act,
                           void *y /*DEVICE*/, int32_t y_dtype, int64_t y_stride, void *hip_stream);

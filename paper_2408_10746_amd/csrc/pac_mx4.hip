@@ -922,8 +922,10 @@ static inline int64_t scale_pitch(int cols) { return ((int64_t)cols + 255) / 256
 static inline bool dtype_ok(int32_t t) { return t == PAC_BF16 || t == PAC_F32; }
 
 constexpr int32_t kMx4Most = 1 << 28; // rows and columns: places past a tile's end still fit 32 bits
-// tiles of a launch, or -1 where they pass a grid's limit
-static int64_t tile_count(int64_t a, int64_t b) { return a * b <= 0x7fffffffll ? a * b : -1; }
+// A launch takes fewer than 2^32 threads, blocks of all sizes counted together: with 512 a block these many tiles
+constexpr int64_t kMx4Tiles = (1ll << 32) / 512 - 1;
+// tiles of a launch, or -1 where they pass that
+static int64_t tile_count(int64_t a, int64_t b) { return a * b <= kMx4Tiles ? a * b : -1; }
 
 static pac_status check_convert(const void *x, int32_t dtype, int64_t rows, int32_t cols, int64_t stride, const uint8_t *codes,
                                 const uint8_t *scales)
@@ -1023,16 +1025,19 @@ constexpr Mx4Form kMx4Dx[] = {{16, 128, 256, false, 4.06f, 0.58f, 0.035f, 0.801f
                               {128, 256, 64, true, 0.04f, 8.42f, 0.101f, 0.897f},
                               {256, 256, 64, true, 1.19f, 6.65f, 0.763f, 1.608f}};
 
-// the form for a product of M x `deep` by `deep` x `wide`
+// the form for a product of M x `deep` by `deep` x `wide`: of those whose tiles one launch takes the one that is estimated fastest (of
+// all of them where it takes none's, which the launch then refuses)
 template <int F> static const Mx4Form &mx4_form(const Mx4Form (&forms)[F], int64_t M, int64_t deep, int64_t wide)
 {
     const Mx4Form *best = nullptr;
     float least = 0.f;
+    bool best_fits = false;
     for (const Mx4Form &q : forms) {
         const int64_t tiles = ((M + q.rows - 1) / q.rows) * ((wide + q.cols - 1) / q.cols);
+        const bool fits = tiles <= kMx4Tiles;
         const float n = q.whole ? (float)((tiles + 255) / 256) : (float)tiles / 256.f, steps = (float)((deep + q.step - 1) / q.step);
         const float t = q.start + q.tile * n + steps * (q.least > q.share * n ? q.least : q.share * n);
-        if (!best || t < least) best = &q, least = t;
+        if (!best || (fits == best_fits ? t < least : fits)) best = &q, least = t, best_fits = fits;
     }
     return *best;
 }
@@ -1065,23 +1070,60 @@ static pac_status launch_dx(const Mx4Args &a, hipStream_t st)
     }
 }
 
+// The conversions' kernels take 32 threads a group of 256 columns, so that one launch takes fewer than 2^27 groups: more rows go in
+// several, of this many groups at most.  call(first row, groups of its rows)
+constexpr int64_t kMx4Groups = 1 << 26;
+template <class Call> static pac_status by_rows(int64_t rows, int32_t cols, Call call)
+{
+    const int64_t upr = ((int64_t)cols + 255) / 256, step = kMx4Groups / upr; // (a row has 2^20 groups at most)
+    for (int64_t r = 0; r < rows; r += step) {
+        call(r, (uint32_t)((rows - r < step ? rows - r : step) * upr));
+        const pac_status s = done();
+        if (s != PAC_OK) return s;
+    }
+    return PAC_OK;
+}
+
 static pac_status launch_quant(const void *x, int32_t x_dtype, int64_t rows, int32_t cols, int64_t x_stride, uint8_t *codes, uint8_t *scales,
                                hipStream_t st)
 {
-    const uint32_t upr = (uint32_t)(((int64_t)cols + 255) / 256), units = (uint32_t)rows * upr;
-    const dim3 g((units + 7) / 8), b(256);
-    uint32_t *c = reinterpret_cast<uint32_t *>(codes);
+    const uint32_t upr = (uint32_t)(((int64_t)cols + 255) / 256);
     const bool vec = m_aligned(x, 16) && x_stride % (x_dtype == PAC_F32 ? 4 : 8) == 0;
-    if (x_dtype == PAC_F32) {
-        const float *p = static_cast<const float *>(x);
-        if (vec) hipLaunchKernelGGL((k_mx4_quant<float, true>), g, b, 0, st, p, units, upr, cols, x_stride, c, scales);
-        else hipLaunchKernelGGL((k_mx4_quant<float, false>), g, b, 0, st, p, units, upr, cols, x_stride, c, scales);
-    } else {
-        const bf16_t *p = static_cast<const bf16_t *>(x);
-        if (vec) hipLaunchKernelGGL((k_mx4_quant<bf16_t, true>), g, b, 0, st, p, units, upr, cols, x_stride, c, scales);
-        else hipLaunchKernelGGL((k_mx4_quant<bf16_t, false>), g, b, 0, st, p, units, upr, cols, x_stride, c, scales);
-    }
-    return done();
+    return by_rows(rows, cols, [&](int64_t row, uint32_t units) {
+        const dim3 g((units + 7) / 8), b(256);
+        uint32_t *c = reinterpret_cast<uint32_t *>(codes) + row * upr * 32;
+        uint8_t *s = scales + row * upr * 8;
+        if (x_dtype == PAC_F32) {
+            const float *p = static_cast<const float *>(x) + row * x_stride;
+            if (vec) hipLaunchKernelGGL((k_mx4_quant<float, true>), g, b, 0, st, p, units, upr, cols, x_stride, c, s);
+            else hipLaunchKernelGGL((k_mx4_quant<float, false>), g, b, 0, st, p, units, upr, cols, x_stride, c, s);
+        } else {
+            const bf16_t *p = static_cast<const bf16_t *>(x) + row * x_stride;
+            if (vec) hipLaunchKernelGGL((k_mx4_quant<bf16_t, true>), g, b, 0, st, p, units, upr, cols, x_stride, c, s);
+            else hipLaunchKernelGGL((k_mx4_quant<bf16_t, false>), g, b, 0, st, p, units, upr, cols, x_stride, c, s);
+        }
+    });
+}
+
+static pac_status launch_dequant(const uint8_t *codes, const uint8_t *scales, int64_t rows, int32_t cols, void *out, int32_t out_dtype,
+                                 int64_t out_stride, hipStream_t st)
+{
+    const uint32_t upr = (uint32_t)(((int64_t)cols + 255) / 256);
+    const bool vec = m_aligned(out, 16) && out_stride % (out_dtype == PAC_F32 ? 4 : 8) == 0;
+    return by_rows(rows, cols, [&](int64_t row, uint32_t units) {
+        const dim3 g((units + 7) / 8), b(256);
+        const uint32_t *c = reinterpret_cast<const uint32_t *>(codes) + row * upr * 32;
+        const uint8_t *s = scales + row * upr * 8;
+        if (out_dtype == PAC_F32) {
+            float *p = static_cast<float *>(out) + row * out_stride;
+            if (vec) hipLaunchKernelGGL((k_mx4_dequant<float, true>), g, b, 0, st, c, s, units, upr, cols, p, out_stride);
+            else hipLaunchKernelGGL((k_mx4_dequant<float, false>), g, b, 0, st, c, s, units, upr, cols, p, out_stride);
+        } else {
+            bf16_t *p = static_cast<bf16_t *>(out) + row * out_stride;
+            if (vec) hipLaunchKernelGGL((k_mx4_dequant<bf16_t, true>), g, b, 0, st, c, s, units, upr, cols, p, out_stride);
+            else hipLaunchKernelGGL((k_mx4_dequant<bf16_t, false>), g, b, 0, st, c, s, units, upr, cols, p, out_stride);
+        }
+    });
 }
 
 } // namespace pac
@@ -1108,21 +1150,7 @@ pac_status pac_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64
     const pac_status s = check_convert(out, out_dtype, rows, cols, out_stride, codes, scales);
     if (s != PAC_OK || rows == 0) return s;
     (void)hipGetLastError();
-    hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    const uint32_t upr = (uint32_t)(((int64_t)cols + 255) / 256), units = (uint32_t)rows * upr;
-    const dim3 g((units + 7) / 8), b(256);
-    const uint32_t *c = reinterpret_cast<const uint32_t *>(codes);
-    const bool vec = m_aligned(out, 16) && out_stride % (out_dtype == PAC_F32 ? 4 : 8) == 0;
-    if (out_dtype == PAC_F32) {
-        float *p = static_cast<float *>(out);
-        if (vec) hipLaunchKernelGGL((k_mx4_dequant<float, true>), g, b, 0, st, c, scales, units, upr, cols, p, out_stride);
-        else hipLaunchKernelGGL((k_mx4_dequant<float, false>), g, b, 0, st, c, scales, units, upr, cols, p, out_stride);
-    } else {
-        bf16_t *p = static_cast<bf16_t *>(out);
-        if (vec) hipLaunchKernelGGL((k_mx4_dequant<bf16_t, true>), g, b, 0, st, c, scales, units, upr, cols, p, out_stride);
-        else hipLaunchKernelGGL((k_mx4_dequant<bf16_t, false>), g, b, 0, st, c, scales, units, upr, cols, p, out_stride);
-    }
-    return done();
+    return launch_dequant(codes, scales, rows, cols, out, out_dtype, out_stride, static_cast<hipStream_t>(hip_stream));
 }
 
 pac_status pac_mx4_linear(const void *x, int32_t M, int32_t K, int64_t x_stride, const uint8_t *codes, const uint8_t *scales, int32_t N,

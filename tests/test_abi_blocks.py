@@ -142,3 +142,13 @@ def test_blocks_add_at_most_64_rows_one_after_another(d):
     b, side = norm(d=d, w_post=A), {40: 8, 768: 2}.get(d, 1)
     for rows in (1 << 16, 1 << 20, (1 << 26) + 1):
         assert pb.pac_block_norm_workspace_bytes(b, rows) >= rows / (64 * side) * (16 + 16 * d)
+
+
+def test_tiles_fit_a_launch():
+    """A launch takes fewer than 2^32 threads, 2^23 blocks of 512: a form with more tiles gives way to one with fewer."""
+    t = pb.pac_mx4_tiles
+    assert t(0, 1, 1024, (1 << 27) - 16) == (16, 16)
+    for product in (0, 1, 2):
+        for M, K, N in ((1, 1024, 1 << 27), (1, 1024, 1 << 28), (16, 2048, 1 << 28), (1, 1 << 28, 1 << 11), (1 << 28, 32, 16), (1 << 28, 16, 32), (1 << 28, 1, 1)):
+            rows, cols = t(product, M, K, N)
+            assert -(-M // rows) * -(-(K if product == 2 else N) // cols) < 1 << 23, (product, M, K, N)

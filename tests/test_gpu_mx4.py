@@ -421,3 +421,22 @@ def test_tile_kernels_in_a_graph_and_on_another_stream(M, K, N):
         g.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(ref, graph)), k
+
+
+def test_conversions_of_more_groups_than_one_launch_takes():
+    """2^27 and some rows of one group each: values on the grid come back as they are, the last ones too, and the stored form is that of
+    the first rows again and again."""
+    rows, cols, period = (1 << 27) + 4097, 32, 4096
+    rng = np.random.default_rng(10)
+    some = np.ldexp(bo.GRID[rng.integers(1, 8, size=(period, cols))] * rng.choice([-1.0, 1.0], size=(period, cols)), rng.integers(-100, 100, size=(period, 1)))
+    some[:, 7] = 6.0 * np.exp2(np.floor(np.log2(np.abs(some).max(1))) - 2)
+    x = dev(some, torch.bfloat16).repeat(-(-rows // period), 1)[:rows]
+    codes, scales = rt.mx4_empty(rows, cols)
+    rt.mx4_quantize(x, codes, scales)
+    ref_codes, ref_scales = (dev(a) for a in bo.quantize(some))
+    whole = rows // period * period
+    for got, ref in ((codes, ref_codes), (scales, ref_scales)):
+        assert (got[:whole].view(-1, *ref.shape) == ref).all() and torch.equal(got[whole:], ref[:rows - whole])
+    out = torch.zeros_like(x)
+    rt.mx4_dequantize(codes, scales, out)
+    assert torch.equal(out, x)
