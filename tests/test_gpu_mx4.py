@@ -440,3 +440,36 @@ def test_conversions_of_more_groups_than_one_launch_takes():
     out = torch.zeros_like(x)
     rt.mx4_dequantize(codes, scales, out)
     assert torch.equal(out, x)
+
+
+@pytest.mark.parametrize("M", [1, 300])
+def test_gelu_over_its_range(M):
+    """u = bias (x is zero), on the row form and on tiles.  Bars: 2e-7 |u| and, for negative u down to -11, 1.4e-3 of the value (the stated
+    ones, with 2^-22 |u| for the exponential's and the last rounding); below that less than 1e-26; infinities go to infinity and zero."""
+    u = np.concatenate([np.linspace(-12, 12, 24001), -np.geomspace(1e-6, 60, 3000), np.geomspace(1e-30, 1e30, 500), [-1e30, -np.inf, np.inf, 0.0]]).astype(np.float32)
+    K, N = 40, u.size
+    codes, scales = rt.mx4_empty(N, K)
+    rt.mx4_quantize(torch.ones(N, K, device="cuda"), codes, scales)
+    lin = rt.Mx4Linear(codes, scales, K, bias=dev(u))
+    assert (pb.pac_mx4_tiles(0, M, K, N)[0] == 16) == (pb.pac_mx4_tiles(1, M, K, N)[0] == 16) == (M == 1)
+    x, y = torch.zeros(M, K, dtype=torch.bfloat16, device="cuda"), torch.empty(M, N, device="cuda")
+    h = torch.from_numpy(u).double()
+    ref = torch.where(torch.isinf(h), h.clamp(min=0), 0.5 * h * torch.special.erfc(-h / np.sqrt(2))).numpy()
+    off = lambda got: np.abs(np.where(got == ref, 0.0, got) - np.where(got == ref, 0.0, ref))  # noqa: E731
+    size = np.abs(u.astype(np.float64))
+    for x4 in (False, True):
+        lin.forward(x, y, gelu=True, x4=x4)
+        assert (y == y[0]).all()
+        got = host(y[0])
+        assert np.array_equal(got[np.isinf(u)], ref[np.isinf(u)])
+        ok = np.isfinite(u)
+        err = off(got)
+        assert (err[ok] <= (2e-7 + 2.0 ** -22) * size[ok]).all(), u[ok][np.argmax(err[ok] / (size[ok] + 1e-300))]
+        neg = ok & (u < -1) & (u >= -11)
+        assert (err[neg] <= (1.4e-3 + 2.0 ** -16) * np.abs(ref[neg])).all(), u[neg][np.argmax(err[neg] / np.abs(ref[neg]))]
+        assert (np.abs(got[ok & (u < -11)]) < 1e-26).all()
+    low = torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
+    lin.forward(x, low, gelu=True)
+    got = host(low[0])
+    neg = (u < 0) & (u >= -11)
+    assert (off(got)[neg] <= (2.0 ** -8 + 1.4e-3) * np.abs(ref[neg]) + 2e-7 * size[neg]).all()
