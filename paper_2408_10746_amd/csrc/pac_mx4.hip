@@ -958,14 +958,22 @@ static pac_status check_product(const void *x, int32_t M, int32_t K, int32_t N, 
     return PAC_OK;
 }
 
+// asked for once a kernel; where it was refused every launch of that kernel is an error
+template <auto Kern> static hipError_t allow_lds_once(int lds)
+{
+    static std::once_flag once;
+    static hipError_t result = hipSuccess;
+    std::call_once(once, [&] {
+        result = hipFuncSetAttribute(reinterpret_cast<const void *>(Kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    });
+    return result;
+}
+
 template <class TL> static pac_status launch_tiles(const Mx4Args &a, hipStream_t st)
 {
     const int64_t tiles = tile_count(((int64_t)a.N + TL::TN - 1) / TL::TN, ((int64_t)a.M + TL::TM - 1) / TL::TM);
     if (tiles < 0) return PAC_ERR_UNSUPPORTED;
-    static std::once_flag once;
-    std::call_once(once, [] {
-        (void)hipFuncSetAttribute(reinterpret_cast<const void *>(&k_mx4_tiles<TL>), hipFuncAttributeMaxDynamicSharedMemorySize, TL::LDS_BYTES);
-    });
+    if (allow_lds_once<&k_mx4_tiles<TL>>(TL::LDS_BYTES) != hipSuccess) return PAC_ERR_DEVICE;
     hipLaunchKernelGGL((k_mx4_tiles<TL>), dim3((unsigned)tiles), dim3(64 * TL::NW), TL::LDS_BYTES, st, a);
     return done();
 }
@@ -974,10 +982,7 @@ template <class TL> static pac_status launch_dx_tiles(const Mx4Args &a, hipStrea
 {
     const int64_t tiles = tile_count(((int64_t)a.K + TL::TK - 1) / TL::TK, ((int64_t)a.M + TL::TM - 1) / TL::TM);
     if (tiles < 0) return PAC_ERR_UNSUPPORTED;
-    static std::once_flag once;
-    std::call_once(once, [] {
-        (void)hipFuncSetAttribute(reinterpret_cast<const void *>(&k_mx4_dx_tiles<TL>), hipFuncAttributeMaxDynamicSharedMemorySize, TL::LDS_BYTES);
-    });
+    if (allow_lds_once<&k_mx4_dx_tiles<TL>>(TL::LDS_BYTES) != hipSuccess) return PAC_ERR_DEVICE;
     hipLaunchKernelGGL((k_mx4_dx_tiles<TL>), dim3((unsigned)tiles), dim3(64 * TL::NW), TL::LDS_BYTES, st, a);
     return done();
 }
@@ -994,10 +999,7 @@ template <int RM> static pac_status launch_dx_rows(const Mx4Args &a, hipStream_t
     const int64_t tiles = tile_count(((int64_t)a.K + 127) / 128, ((int64_t)a.M + 16 * RM - 1) / (16 * RM));
     if (tiles < 0) return PAC_ERR_UNSUPPORTED;
     constexpr int NW = 8, LDS = NW * 16 * RM * 132 * 4;
-    static std::once_flag once;
-    std::call_once(once, [] {
-        (void)hipFuncSetAttribute(reinterpret_cast<const void *>(&k_mx4_dx_rows<RM, NW>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
-    });
+    if (allow_lds_once<&k_mx4_dx_rows<RM, NW>>(LDS) != hipSuccess) return PAC_ERR_DEVICE;
     hipLaunchKernelGGL((k_mx4_dx_rows<RM, NW>), dim3((unsigned)tiles), dim3(64 * NW), LDS, st, a);
     return done();
 }
