@@ -282,20 +282,28 @@ def mx4_dequantize(codes, scales, out) -> None:
 
 
 class Mx4Linear:
-    """A frozen linear layer with weights in the stored form: y = act(x W^T + bias), and dx = dy W on the way back."""
+    """A frozen linear layer with weights in the stored form: y = act(x W^T + bias), and dx = dy W on the way back.  Between calls its
+    tensors may be changed in place, and may be given other storage."""
 
     def __init__(self, codes, scales, K: int, bias=None):
         self.N, self.K, self.dev = codes.shape[0], K, codes.device
-        _stored(codes, scales, self.N, K, self.dev)
         if self.dev.type != "cuda":
             raise ValueError("codes: on a GPU")
-        if bias is not None and (bias.shape != (self.N,) or bias.dtype != torch.float32 or bias.device != self.dev or not bias.is_contiguous()):
-            raise ValueError("bias: float32, one value an output, on the weights' device")
         self.codes, self.scales, self.bias = codes, scales, bias
-        # the tail of every product's arguments: W, and the bias
-        self._w = (codes.data_ptr(), scales.data_ptr())
-        self._wb = self._w + (self.N, _ptr(bias))
+        self._w = None
+        self._weights()
         self._x_bytes = pb.pac_mx4_linear_qx_workspace_bytes(1, K)
+
+    def _weights(self):
+        """(codes, scales, bias): addresses as they are now, looked at again where they are not what they were."""
+        w = self.codes.data_ptr(), self.scales.data_ptr(), _ptr(self.bias)
+        if w != self._w:
+            bias = self.bias
+            _stored(self.codes, self.scales, self.N, self.K, self.dev)
+            if bias is not None and (bias.shape != (self.N,) or bias.dtype != torch.float32 or bias.device != self.dev or not bias.is_contiguous()):
+                raise ValueError("bias: float32, one value an output, on the weights' device")
+            self._w = w
+        return w
 
     @classmethod
     def from_weights(cls, w, bias=None):
@@ -310,44 +318,59 @@ class Mx4Linear:
         M, dev = x.shape[0], self.dev
         sy, kind = _rows_of(y, "y", M, self.N, dev)
         act = pb.PAC_MX4_ACT_GELU if gelu else pb.PAC_MX4_ACT_NONE
+        codes, scales, bias = self._weights()
         if x4:
             sx, xkind = _rows_of(x, "x", M, self.K, dev)
             need = M * self._x_bytes  # x in the stored form, for this call, on this stream
             ws = torch.empty(need, dtype=torch.uint8, device=dev)
-            _call(dev, "pac_mx4_linear_qx", x.data_ptr(), xkind, M, self.K, sx, *self._wb, act, y.data_ptr(), kind, sy, ws.data_ptr(), need)
+            _call(dev, "pac_mx4_linear_qx", x.data_ptr(), xkind, M, self.K, sx, codes, scales, self.N, bias, act, y.data_ptr(), kind, sy,
+                  ws.data_ptr(), need)
         else:
             sx = _chunked_rows(x, "x", M, self.K, dev)
-            _call(dev, "pac_mx4_linear", x.data_ptr(), M, self.K, sx, *self._wb, act, y.data_ptr(), kind, sy)
+            _call(dev, "pac_mx4_linear", x.data_ptr(), M, self.K, sx, codes, scales, self.N, bias, act, y.data_ptr(), kind, sy)
 
     def input_grad(self, dy, dx) -> None:
         """dy [M][N] bf16, rows on 16 bytes; dx [M][K] bf16 or fp32."""
         M, dev = dy.shape[0], self.dev
         sdy = _chunked_rows(dy, "dy", M, self.N, dev)
         sdx, kind = _rows_of(dx, "dx", M, self.K, dev)
-        _call(dev, "pac_mx4_linear_dx", dy.data_ptr(), M, self.N, sdy, *self._w, self.K, dx.data_ptr(), kind, sdx)
+        codes, scales, _ = self._weights()
+        _call(dev, "pac_mx4_linear_dx", dy.data_ptr(), M, self.N, sdy, codes, scales, self.K, dx.data_ptr(), kind, sdx)
 
 
 class BlockNorm:
     """The norms after and before a block with its gate and the residual scale (include/pac_norm.h).  Parameters are float32
-    tensors that the caller owns and may change in place."""
+    tensors that the caller owns; between calls they may be changed in place, and may be given other storage."""
 
     def __init__(self, d: int, layer: bool = False, eps: float = 1e-5, w_post=None, b_post=None, gate=None, res=None, w_pre=None,
                  b_pre=None):
         # in the order of the library's structure and of its gradients
         self.d, self.params = d, dict(w_post=w_post, b_post=b_post, gate=gate, res=res, w_pre=w_pre, b_pre=b_pre)
-        self.dev = None
-        for name, p in self.params.items():
-            if p is None:
-                continue
-            lens = {"gate": (1, d), "res": (1,)}.get(name, (d,))
-            if p.dtype != torch.float32 or p.dim() != 1 or p.shape[0] not in lens or not p.is_contiguous() or p.device.type != "cuda":
-                raise ValueError(f"{name}: float32 on the device, {' or '.join(map(str, lens))} values")
-            if self.dev not in (None, p.device):
-                raise ValueError(f"{name}: on another device than the parameters before it")
-            self.dev = p.device
         self._shapes = {name: p.shape for name, p in self.params.items() if p is not None}
-        self._b = {dtype: pb.pac_block_norm(d, kind, int(layer), 0 if gate is None else gate.shape[0], eps, *(_ptr(p) for p in self.params.values()))
-                   for dtype, kind in _KIND.items()}
+        for name, shape in self._shapes.items():
+            lens = {"gate": (1, d), "res": (1,)}.get(name, (d,))
+            if len(shape) != 1 or shape[0] not in lens:
+                raise ValueError(f"{name}: {' or '.join(map(str, lens))} values")
+        self.dev = next((p.device for p in self.params.values() if p is not None), None)
+        self._b = {dtype: pb.pac_block_norm(d, kind, int(layer), 0 if gate is None else gate.shape[0], eps) for dtype, kind in _KIND.items()}
+        self._at = None
+        self._structure(torch.float32)
+
+    def _structure(self, dtype):
+        """The library's structure for states of that type, with the parameters' addresses as they are now, looked at again where they
+        are not what they were."""
+        at = [None if p is None else p.data_ptr() for p in self.params.values()]
+        if at != self._at:
+            for name, p in self.params.items():
+                if (p is None) != (name not in self._shapes):
+                    raise ValueError(f"{name}: there or not as in the beginning")
+                if p is not None and (p.dtype != torch.float32 or p.shape != self._shapes[name] or not p.is_contiguous() or p.device != self.dev
+                                      or self.dev.type != "cuda"):
+                    raise ValueError(f"{name}: float32, dense, of the length it had, on one GPU with the other parameters")
+            for b in self._b.values():
+                b.w_post, b.b_post, b.gate, b.res, b.w_pre, b.b_pre = at
+            self._at = at
+        return self._b[dtype]
 
     def _rows(self, x, *others) -> int:
         shape, dtype, dev = x.shape, x.dtype, x.device
@@ -361,13 +384,13 @@ class BlockNorm:
     def forward(self, x, o=None, y=None, n=None) -> None:
         """y and n of x and a block's output o (None: no block yet), into the buffers given."""
         rows = self._rows(x, o, y, n)
-        _call(x.device, "pac_block_norm_forward", self._b[x.dtype], rows, x.data_ptr(), _ptr(o), _ptr(y), _ptr(n))
+        _call(x.device, "pac_block_norm_forward", self._structure(x.dtype), rows, x.data_ptr(), _ptr(o), _ptr(y), _ptr(n))
 
     def backward(self, x, o, dy, dn, dx=None, do=None, dparams=None) -> None:
         """Gradients, given dy (None: zero) and dn (None without w_pre), into the buffers given; dparams: {name: float32 tensor like
         the parameter} for those that are wanted."""
         rows = self._rows(x, o, dy, dn, dx, do)
-        b, grads, ws, need = self._b[x.dtype], [None] * 6, None, 0
+        b, grads, ws, need = self._structure(x.dtype), [None] * 6, None, 0
         if dparams:
             dev = x.device
             for name, g in dparams.items():

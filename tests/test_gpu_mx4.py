@@ -473,3 +473,44 @@ def test_gelu_over_its_range(M):
     got = host(low[0])
     neg = (u < 0) & (u >= -11)
     assert (off(got)[neg] <= (2.0 ** -8 + 1.4e-3) * np.abs(ref[neg]) + 2e-7 * size[neg]).all()
+
+
+def test_weights_given_other_storage():
+    """What the layer's tensors are at the call counts, wherever their storage is by then; what no longer fits is refused."""
+    rng = np.random.default_rng(12)
+    M, K, N = 5, 300, 70
+    new = lambda: layer(rng, N, K)[:2] + (dev(rng.standard_normal(N), torch.float32),)  # noqa: E731
+    codes, scales, bias = new()
+    lin = rt.Mx4Linear(codes, scales, K, bias=bias)
+    x, dy = rows_of(rng, M, K), rows_of(rng, M, N)
+
+    def go(l):
+        y, z, dx = torch.empty(M, N, device="cuda"), torch.empty(M, N, device="cuda"), torch.empty(M, K, device="cuda")
+        l.forward(x, y)
+        l.forward(x, z, x4=True)
+        l.input_grad(dy, dx)
+        return y, z, dx
+
+    keep = []                                             # the old storages stay, so that a stale address would be read, not faulted on
+    for how in range(3):
+        before = go(lin)
+        keep += [t.detach() for t in (lin.codes, lin.scales, lin.bias)]
+        other = new()
+        if how == 0:
+            lin.codes.data, lin.scales.data, lin.bias.data = other
+        elif how == 1:
+            for t, o in zip((lin.codes, lin.scales, lin.bias), other):
+                t.set_(o)
+        else:
+            lin.codes, lin.scales, lin.bias = other
+        after = go(lin)
+        assert all(torch.equal(a, b) for a, b in zip(after, go(rt.Mx4Linear(*other[:2], K, bias=other[2])))), how
+        assert not any(torch.equal(a, b) for a, b in zip(after, before)), how
+    for name, bad in (("codes", lin.codes[:-1].clone()), ("scales", lin.scales.cpu()), ("bias", lin.bias.double())):
+        was = getattr(lin, name)
+        setattr(lin, name, bad)
+        for call in (lambda: lin.forward(x, torch.empty(M, N, device="cuda")), lambda: lin.input_grad(dy, torch.empty(M, K, device="cuda"))):
+            with pytest.raises(ValueError):
+                call()
+        setattr(lin, name, was)
+    go(lin)

@@ -327,3 +327,41 @@ def test_a_row_is_the_same_in_any_round_backward(rows, d, c, dtype):
         # an element's own error: statistics of d terms (64 x 2^-24) of row-sized parts, in g through two norms
         own = 64 * U * 16 * (1 + np.abs(oh).max() + np.abs(yh).max())
         assert np.max(np.abs(host(t) - ref[k]) / ((128 * U + own) * (terms[k] + terms[k].max()))) <= 1.0, k
+
+
+def test_parameters_given_other_storage():
+    """What a parameter is at the call counts, wherever its storage is by then; what no longer fits is refused."""
+    rng = np.random.default_rng(11)
+    rows, d = 9, 96
+    v, p = make(rng, rows, d, "f32", 2, True, True, True, True)
+    bn = rt.BlockNorm(d, layer=True, **p)
+    dy, dn = torch.ones_like(v["x"]), torch.ones_like(v["x"])
+
+    def go(b):
+        y, n, dx, do = (torch.empty_like(v["x"]) for _ in range(4))
+        dp = {k: torch.empty_like(t) for k, t in p.items()}
+        b.forward(v["x"], v["o"], y, n)
+        b.backward(v["x"], v["o"], dy, dn, dx, do, dp)
+        return [y, n, dx, do, *dp.values()]
+
+    keep = []                                             # the old storages stay, so that a stale address would be read, not faulted on
+    for k in list(p):
+        before = go(bn)
+        keep.append(p[k].detach())
+        other = dev(rng.standard_normal(p[k].numel()))
+        if k.startswith("w"):
+            p[k].data = other
+        elif k.startswith("b"):
+            p[k].set_(other)
+        else:
+            p[k] = bn.params[k] = other
+        after = go(bn)
+        assert all(torch.equal(a, b) for a, b in zip(after, go(rt.BlockNorm(d, layer=True, **p)))), k
+        assert any(not torch.equal(a, b) for a, b in zip(after, before)), k
+    for k, bad in (("w_post", torch.ones(d - 1, device="cuda")), ("gate", torch.ones(d)), ("w_pre", None), ("b_pre", torch.ones(d, device="cuda").double())):
+        was, bn.params[k] = bn.params[k], bad
+        for call in (lambda: bn.forward(v["x"], v["o"], dy, dn), lambda: bn.backward(v["x"], v["o"], dy, dn)):
+            with pytest.raises(ValueError):
+                call()
+        bn.params[k] = was
+    go(bn)
