@@ -207,6 +207,13 @@ class TieredSession(Session):
 _KIND = {torch.bfloat16: pb.PAC_BF16, torch.float32: pb.PAC_F32}
 
 
+def _fits(n: int, what: str) -> int:
+    """n, which the library takes in 32 bits (ctypes drops what lies above)."""
+    if n >= 1 << 31:
+        raise ValueError(f"{what}: {n} is past 2^31 - 1")
+    return n
+
+
 def _rows_of(t, name: str, rows: int, cols: int, device):
     """(row stride, pac_dtype) of a [rows][cols] device matrix with neighbouring columns."""
     kind = _KIND.get(t.dtype)
@@ -236,6 +243,7 @@ def _chunked_rows(t, name: str, rows: int, cols: int, device) -> int:
 
 
 def _stored(codes, scales, rows: int, cols: int, device) -> None:
+    _fits(cols, "columns")
     for t, pitch, name in ((codes, pb.pac_mx4_code_pitch(cols), "codes"), (scales, pb.pac_mx4_scale_pitch(cols), "scales")):
         if t.dtype != torch.uint8 or t.shape != (rows, pitch) or t.device != device or not t.is_contiguous():
             raise ValueError(f"{name}: dense uint8, ({rows}, {pitch}), on {device} is wanted")
@@ -261,6 +269,7 @@ def _ptr(t):
 
 def mx4_empty(rows: int, cols: int, device="cuda:0"):
     """Buffers for a matrix in the stored form: (codes, scales)."""
+    _fits(cols, "columns")
     return (torch.empty(rows, pb.pac_mx4_code_pitch(cols), dtype=torch.uint8, device=device),
             torch.empty(rows, pb.pac_mx4_scale_pitch(cols), dtype=torch.uint8, device=device))
 
@@ -286,7 +295,7 @@ class Mx4Linear:
     tensors may be changed in place, and may be given other storage."""
 
     def __init__(self, codes, scales, K: int, bias=None):
-        self.N, self.K, self.dev = codes.shape[0], K, codes.device
+        self.N, self.K, self.dev = _fits(codes.shape[0], "outputs"), K, codes.device
         if self.dev.type != "cuda":
             raise ValueError("codes: on a GPU")
         self.codes, self.scales, self.bias = codes, scales, bias
@@ -315,7 +324,7 @@ class Mx4Linear:
     def forward(self, x, y, gelu: bool = False, x4: bool = False) -> None:
         """x [M][K] bf16, rows on 16 bytes; y [M][N] bf16 or fp32.  x4: x (bf16 or fp32, any row stride) is quantised too, and the
         product runs on 4-bit operands."""
-        M, dev = x.shape[0], self.dev
+        M, dev = _fits(x.shape[0], "rows"), self.dev
         sy, kind = _rows_of(y, "y", M, self.N, dev)
         act = pb.PAC_MX4_ACT_GELU if gelu else pb.PAC_MX4_ACT_NONE
         codes, scales, bias = self._weights()
@@ -331,7 +340,7 @@ class Mx4Linear:
 
     def input_grad(self, dy, dx) -> None:
         """dy [M][N] bf16, rows on 16 bytes; dx [M][K] bf16 or fp32."""
-        M, dev = dy.shape[0], self.dev
+        M, dev = _fits(dy.shape[0], "rows"), self.dev
         sdy = _chunked_rows(dy, "dy", M, self.N, dev)
         sdx, kind = _rows_of(dx, "dx", M, self.K, dev)
         codes, scales, _ = self._weights()
@@ -345,7 +354,7 @@ class BlockNorm:
     def __init__(self, d: int, layer: bool = False, eps: float = 1e-5, w_post=None, b_post=None, gate=None, res=None, w_pre=None,
                  b_pre=None):
         # in the order of the library's structure and of its gradients
-        self.d, self.params = d, dict(w_post=w_post, b_post=b_post, gate=gate, res=res, w_pre=w_pre, b_pre=b_pre)
+        self.d, self.params = _fits(d, "d"), dict(w_post=w_post, b_post=b_post, gate=gate, res=res, w_pre=w_pre, b_pre=b_pre)
         self._shapes = {name: p.shape for name, p in self.params.items() if p is not None}
         for name, shape in self._shapes.items():
             lens = {"gate": (1, d), "res": (1,)}.get(name, (d,))

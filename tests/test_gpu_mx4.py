@@ -514,3 +514,13 @@ def test_weights_given_other_storage():
                 call()
         setattr(lin, name, was)
     go(lin)
+
+
+def test_rows_past_32_bits_are_refused_not_cut_off():
+    """(the buffers are never touched)"""
+    lin = rt.Mx4Linear.from_weights(torch.ones(1, 1, device="cuda"))
+    rows = (1 << 32) + 4
+    x, y = torch.empty(rows, 8, dtype=torch.bfloat16, device="cuda")[:, :1], torch.empty(rows, 1, dtype=torch.bfloat16, device="cuda")
+    for bad in (lambda: lin.forward(x, y), lambda: lin.forward(x, y, x4=True), lambda: lin.input_grad(x, y)):
+        with pytest.raises(ValueError):
+            bad()
