@@ -38,8 +38,9 @@ int64_t pac_mx4_scale_pitch(int32_t cols);
 
 /* x DEVICE [rows][x_stride] of x_dtype (pac_dtype), x_stride >= cols elements apart, any alignment of its type;
  * codes DEVICE, rows * code pitch bytes, 16-byte aligned; scales DEVICE, rows * scale pitch bytes, 8-byte aligned; the padding
- * is written too.  rows = 0: nothing happens, and the addresses may be NULL.  Errors: NULL, SHAPE (cols < 1, x_dtype), RANGE (rows < 0, x_stride < cols),
- * UNSUPPORTED (cols past 2^28, or more than 2^31 - 1 groups of 256 columns in all), ALIGN, DEVICE. */
+ * is written too.  The three share no memory.  rows = 0: nothing happens, and the addresses may be NULL.  Errors: NULL, SHAPE (cols < 1,
+ * x_dtype), RANGE (rows < 0, x_stride < cols, shared memory), UNSUPPORTED (cols past 2^28, or more than 2^31 - 1 groups of 256
+ * columns in all), ALIGN, DEVICE. */
 pac_status pac_mx4_quantize(const void *x /*DEVICE*/, int32_t x_dtype, int64_t rows, int32_t cols, int64_t x_stride,
                             uint8_t *codes /*DEVICE*/, uint8_t *scales /*DEVICE*/, void *hip_stream);
 
@@ -54,9 +55,10 @@ pac_status pac_mx4_dequantize(const uint8_t *codes /*DEVICE*/, const uint8_t *sc
  *   x       DEVICE bf16 [M][x_stride], 16-byte aligned, x_stride >= K and a multiple of 8; of the elements past K those up
  *           to the next multiple of 8 are read, in the last row too, and ignored whatever they hold
  *   codes, scales  DEVICE, W [N][K] in the stored form above          bias  DEVICE fp32 [N], or NULL
- *   y       DEVICE [M][y_stride] of y_dtype, y_stride >= N, any alignment of its type; may not overlap the inputs
- * M = 0: nothing happens, and x and y may be NULL.  Errors: NULL, SHAPE (K or N < 1, M < 0, y_dtype, act), RANGE (strides), ALIGN, UNSUPPORTED (M,
- * K or N past 2^28, or more than 2^23 - 1 tiles in every form: past 2^38 results where they fill tiles), DEVICE. */
+ *   y       DEVICE [M][y_stride] of y_dtype, y_stride >= N, any alignment of its type; may not overlap the inputs (rows side by side
+ *           in one buffer, x's columns before y's, do not)
+ * M = 0: nothing happens, and x and y may be NULL.  Errors: NULL, SHAPE (K or N < 1, M < 0, y_dtype, act), RANGE (strides, overlap),
+ * ALIGN, UNSUPPORTED (M, K or N past 2^28, or more than 2^23 - 1 tiles in every form: past 2^38 results where they fill tiles), DEVICE. */
 pac_status pac_mx4_linear(const void *x /*DEVICE*/, int32_t M, int32_t K, int64_t x_stride, const uint8_t *codes /*DEVICE*/,
                           const uint8_t *scales /*DEVICE*/, int32_t N, const float *bias /*DEVICE*/, int32_t act,
                           void *y /*DEVICE*/, int32_t y_dtype, int64_t y_stride, void *hip_stream);
@@ -69,7 +71,7 @@ pac_status pac_mx4_linear_x4(const uint8_t *x_codes /*DEVICE*/, const uint8_t *x
 
 /* The same with x quantised in the call: x DEVICE [M][x_stride] of x_dtype, any alignment of its type; what pac_mx4_quantize and
  * pac_mx4_linear_x4 give, bit for bit, few rows in one launch.  workspace DEVICE, 16-byte aligned, as many bytes as the function says
- * (-1 on bad arguments); its contents are scratch.  Errors as above, and WORKSPACE. */
+ * (-1 on bad arguments); its contents are scratch, and it overlaps nothing else.  Errors as above, and WORKSPACE. */
 int64_t pac_mx4_linear_qx_workspace_bytes(int32_t M, int32_t K);
 pac_status pac_mx4_linear_qx(const void *x /*DEVICE*/, int32_t x_dtype, int32_t M, int32_t K, int64_t x_stride,
                              const uint8_t *codes /*DEVICE*/, const uint8_t *scales /*DEVICE*/, int32_t N,

@@ -39,8 +39,10 @@ typedef struct {
 } pac_block_norm;
 
 /* x, o, y, n DEVICE [rows][d], of any alignment of their type.  o NULL: no block yet (y = res x; then w_post, b_post and gate
- * are NULL).  y NULL: not wanted.  n is there where w_pre is.  y may be x, and n may be o: a row is read before it is written.
- * rows = 0: nothing happens, and the states may be NULL.  Errors: NULL, SHAPE (d, dtype, layer, gate_len, eps), RANGE (rows < 0), ALIGN, DEVICE. */
+ * are NULL).  y NULL: not wanted.  n is there where w_pre is.  y may be x, and n may be o: a row is read before it is written.  Else
+ * what is written shares no memory with what is read.
+ * rows = 0: nothing happens, and the states may be NULL.  Errors: NULL, SHAPE (d, dtype, layer, gate_len, eps), RANGE (rows < 0, shared
+ * memory), ALIGN, DEVICE. */
 pac_status pac_block_norm_forward(const pac_block_norm *b /*HOST*/, int64_t rows, const void *x /*DEVICE*/,
                                   const void *o /*DEVICE*/, void *y /*DEVICE*/, void *n /*DEVICE*/, void *hip_stream);
 
@@ -50,7 +52,8 @@ int64_t pac_block_norm_workspace_bytes(const pac_block_norm *b /*HOST*/, int64_t
 
 /* Gradients.  x, o as in the forward pass; dy, dn DEVICE [rows][d], the gradients of y (NULL: zero) and of n (there where
  * w_pre is); dx, do_ DEVICE [rows][d], or NULL: not wanted (dx may be dy, do_ may be dn); the parameters' gradients DEVICE
- * fp32 of the parameters' lengths, overwritten, or NULL: not wanted (NULL where the parameter is).
+ * fp32 of the parameters' lengths, overwritten, or NULL: not wanted (NULL where the parameter is).  Else outputs and workspace share
+ * no memory with each other or with inputs.
  * workspace DEVICE, 16-byte aligned, may be NULL if no parameter's gradient is wanted.  rows = 0: the parameters' gradients
  * are zero, and the states may be NULL.  Errors as above, and WORKSPACE. */
 pac_status pac_block_norm_backward(const pac_block_norm *b /*HOST*/, int64_t rows, const void *x /*DEVICE*/,

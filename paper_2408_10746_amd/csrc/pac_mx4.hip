@@ -2,6 +2,7 @@
 // input (declared in include/pac_mx4.h, where the stored form is described).
 #include "../../include/pac_mx4.h"
 #include "pac_mma.h"
+#include "pac_span.h"
 #include <mutex>
 
 namespace pac {
@@ -929,8 +930,13 @@ static inline bool dtype_ok(int32_t t) { return t == PAC_BF16 || t == PAC_F32; }
 constexpr int32_t kMx4Most = 1 << 28; // rows and columns: places past a tile's end still fit 32 bits
 // A launch takes fewer than 2^32 threads, blocks of all sizes counted together: with 512 a block these many tiles
 constexpr int64_t kMx4Tiles = (1ll << 32) / 512 - 1;
-// tiles of a launch, or -1 where they pass that
-static int64_t tile_count(int64_t a, int64_t b) { return a * b <= kMx4Tiles ? a * b : -1; }
+
+// do a matrix, its codes and its scales share memory?
+static bool stored_shares(const uint8_t *codes, const uint8_t *scales, int64_t rows, int32_t cols, const Span &x)
+{
+    const Span c(codes, rows * code_pitch(cols)), s(scales, rows * scale_pitch(cols));
+    return shares(x, {c, s}) || share(c, s);
+}
 
 static pac_status check_convert(const void *x, int32_t dtype, int64_t rows, int32_t cols, int64_t stride, const uint8_t *codes,
                                 const uint8_t *scales)
@@ -942,6 +948,8 @@ static pac_status check_convert(const void *x, int32_t dtype, int64_t rows, int3
     if (cols > kMx4Most) return PAC_ERR_UNSUPPORTED;
     const int64_t upr = ((int64_t)cols + 255) / 256;
     if (rows > 0x7fffffffll / upr) return PAC_ERR_UNSUPPORTED;
+    const int size = dtype == PAC_F32 ? 4 : 2;
+    if (stored_shares(codes, scales, rows, cols, Span(x, rows, stride * size, (int64_t)cols * size))) return PAC_ERR_RANGE;
     return PAC_OK;
 }
 
@@ -971,8 +979,7 @@ template <auto Kern> static hipError_t allow_lds_once(int lds)
 
 template <class TL> static pac_status launch_tiles(const Mx4Args &a, hipStream_t st)
 {
-    const int64_t tiles = tile_count(((int64_t)a.N + TL::TN - 1) / TL::TN, ((int64_t)a.M + TL::TM - 1) / TL::TM);
-    if (tiles < 0) return PAC_ERR_UNSUPPORTED;
+    const int64_t tiles = ((int64_t)a.N + TL::TN - 1) / TL::TN * (((int64_t)a.M + TL::TM - 1) / TL::TM);
     if (allow_lds_once<&k_mx4_tiles<TL>>(TL::LDS_BYTES) != hipSuccess) return PAC_ERR_DEVICE;
     hipLaunchKernelGGL((k_mx4_tiles<TL>), dim3((unsigned)tiles), dim3(64 * TL::NW), TL::LDS_BYTES, st, a);
     return done();
@@ -980,8 +987,7 @@ template <class TL> static pac_status launch_tiles(const Mx4Args &a, hipStream_t
 
 template <class TL> static pac_status launch_dx_tiles(const Mx4Args &a, hipStream_t st)
 {
-    const int64_t tiles = tile_count(((int64_t)a.K + TL::TK - 1) / TL::TK, ((int64_t)a.M + TL::TM - 1) / TL::TM);
-    if (tiles < 0) return PAC_ERR_UNSUPPORTED;
+    const int64_t tiles = ((int64_t)a.K + TL::TK - 1) / TL::TK * (((int64_t)a.M + TL::TM - 1) / TL::TM);
     if (allow_lds_once<&k_mx4_dx_tiles<TL>>(TL::LDS_BYTES) != hipSuccess) return PAC_ERR_DEVICE;
     hipLaunchKernelGGL((k_mx4_dx_tiles<TL>), dim3((unsigned)tiles), dim3(64 * TL::NW), TL::LDS_BYTES, st, a);
     return done();
@@ -989,15 +995,13 @@ template <class TL> static pac_status launch_dx_tiles(const Mx4Args &a, hipStrea
 
 template <int X, int RM> static pac_status launch_rows(const Mx4Args &a, hipStream_t st)
 {
-    const int64_t tiles = tile_count(((int64_t)a.N + 15) / 16, ((int64_t)a.M + 16 * RM - 1) / (16 * RM));
-    if (tiles < 0) return PAC_ERR_UNSUPPORTED;
+    const int64_t tiles = ((int64_t)a.N + 15) / 16 * (((int64_t)a.M + 16 * RM - 1) / (16 * RM));
     hipLaunchKernelGGL((k_mx4_rows<X, RM, 8>), dim3((unsigned)tiles), dim3(512), 0, st, a);
     return done();
 }
 template <int RM> static pac_status launch_dx_rows(const Mx4Args &a, hipStream_t st)
 {
-    const int64_t tiles = tile_count(((int64_t)a.K + 127) / 128, ((int64_t)a.M + 16 * RM - 1) / (16 * RM));
-    if (tiles < 0) return PAC_ERR_UNSUPPORTED;
+    const int64_t tiles = ((int64_t)a.K + 127) / 128 * (((int64_t)a.M + 16 * RM - 1) / (16 * RM));
     constexpr int NW = 8, LDS = NW * 16 * RM * 132 * 4;
     if (allow_lds_once<&k_mx4_dx_rows<RM, NW>>(LDS) != hipSuccess) return PAC_ERR_DEVICE;
     hipLaunchKernelGGL((k_mx4_dx_rows<RM, NW>), dim3((unsigned)tiles), dim3(64 * NW), LDS, st, a);
@@ -1048,6 +1052,16 @@ template <int F> static const Mx4Form &mx4_form(const Mx4Form (&forms)[F], int64
     }
     return *best;
 }
+static bool fits_launch(const Mx4Form &q, int64_t M, int64_t wide)
+{
+    return ((M + q.rows - 1) / q.rows) * ((wide + q.cols - 1) / q.cols) <= kMx4Tiles;
+}
+// the results, and whether they lie over W or the bias
+static Span results(const Mx4Args &a, int64_t wide) { return Span(a.y, a.M, a.ldy * (a.y_f32 ? 4 : 2), wide * (a.y_f32 ? 4 : 2)); }
+static bool over_weights(const Mx4Args &a, const Span &out)
+{
+    return shares(out, {Span(a.w, a.N * a.wp), Span(a.ws, a.N * a.sp), Span(a.bias, (int64_t)a.N * 4)});
+}
 static const Mx4Form &linear_form(bool x4, int M, int K, int N) { return x4 ? mx4_form(kMx4LinearX4, M, K, N) : mx4_form(kMx4Linear, M, K, N); }
 static const Mx4Form &dx_form(int M, int K, int N) { return mx4_form(kMx4Dx, M, N, K); }
 
@@ -1055,6 +1069,10 @@ template <bool X4> static pac_status launch_linear(const Mx4Args &a, hipStream_t
 {
     (void)hipGetLastError();
     const Mx4Form &form = linear_form(X4, a.M, a.K, a.N);
+    if (!fits_launch(form, a.M, a.N)) return PAC_ERR_UNSUPPORTED;
+    const Span y = results(a, a.N);
+    if (over_weights(a, y) || (X4 ? shares(y, {Span(a.x, a.M * a.wp), Span(a.xs, a.M * a.sp)}) : share(y, Span(a.x, a.M, a.ldx * 2, (int64_t)a.K * 2))))
+        return PAC_ERR_RANGE;
     switch (form.rows + form.cols) {
     case 16 + 16: return launch_rows<X4 ? MX4_X4 : MX4_X16, 1>(a, st);
     case 32 + 16: if constexpr (X4) return launch_rows<MX4_X4, 2>(a, st); [[fallthrough]];
@@ -1068,7 +1086,11 @@ template <bool X4> static pac_status launch_linear(const Mx4Args &a, hipStream_t
 static pac_status launch_dx(const Mx4Args &a, hipStream_t st)
 {
     (void)hipGetLastError();
-    switch (dx_form(a.M, a.K, a.N).rows) {
+    const Mx4Form &form = dx_form(a.M, a.K, a.N);
+    if (!fits_launch(form, a.M, a.K)) return PAC_ERR_UNSUPPORTED;
+    const Span dx = results(a, a.K);
+    if (over_weights(a, dx) || share(dx, Span(a.x, a.M, a.ldx * 2, (int64_t)a.N * 2))) return PAC_ERR_RANGE;
+    switch (form.rows) {
     case 16: return launch_dx_rows<1>(a, st);
     case 32: return launch_dx_rows<2>(a, st);
     case 64: return launch_dx_tiles<Mx4DxTile<2, 4, 1, 2, 5>>(a, st);
@@ -1212,6 +1234,10 @@ pac_status pac_mx4_linear_qx(const void *x, int32_t x_dtype, int32_t M, int32_t 
     Mx4Args a{x, nullptr, x_stride, codes, scales, M, K, N, code_pitch(K), scale_pitch(K), bias, act, y, y_dtype == PAC_F32, y_stride};
     (void)hipGetLastError();
     const Mx4Form &form = linear_form(true, M, K, N);
+    if (!fits_launch(form, M, N)) return PAC_ERR_UNSUPPORTED;
+    const int size = x_dtype == PAC_F32 ? 4 : 2;
+    const Span rows(x, M, x_stride * size, (int64_t)K * size), y_rows = results(a, N), ws(workspace, pac_mx4_linear_qx_workspace_bytes(M, K));
+    if (over_weights(a, y_rows) || over_weights(a, ws) || share(y_rows, rows) || share(ws, rows) || share(ws, y_rows)) return PAC_ERR_RANGE;
     // few rows in whole 16-byte pieces: quantised where they are multiplied (one launch)
     if (form.rows <= 32 && x_dtype == PAC_BF16 && K % 8 == 0 && x_stride % 8 == 0 && m_aligned(x, 16))
         return form.rows == 16 ? launch_rows<MX4_XQ, 1>(a, st) : launch_rows<MX4_XQ, 2>(a, st);

@@ -2,6 +2,7 @@
 // in include/pac_norm.h).
 #include "../../include/pac_norm.h"
 #include "pac_gemm.h"
+#include "pac_span.h"
 
 namespace pac {
 
@@ -565,6 +566,18 @@ static bool norm_typed(const pac_block_norm *b, std::initializer_list<const void
     return true;
 }
 
+// States that are written: in the place of one that is read (a row is read before it is written), or away from all of them, and away
+// from the parameters
+static bool state_misplaced(const pac_block_norm *b, int64_t rows, const void *out, std::initializer_list<const void *> in)
+{
+    const int64_t bytes = rows * b->d * (b->dtype == PAC_F32 ? 4 : 2), vec = (int64_t)b->d * 4;
+    const Span o(out, bytes);
+    for (const void *p : in)
+        if (p != out && share(o, Span(p, bytes))) return true;
+    return shares(o, {Span(b->w_post, vec), Span(b->b_post, vec), Span(b->gate, (int64_t)b->gate_len * 4), Span(b->res, 4), Span(b->w_pre, vec),
+                      Span(b->b_pre, vec)});
+}
+
 } // namespace pac
 
 using namespace pac;
@@ -578,6 +591,7 @@ pac_status pac_block_norm_forward(const pac_block_norm *b, int64_t rows, const v
     if (rows && (!x || (!o && (b->w_post || b->gate)) || (b->w_pre && !n) || (!b->w_pre && (n || !y)))) return PAC_ERR_NULL;
     if (!norm_typed(b, {x, o, y, n})) return PAC_ERR_ALIGN;
     if (rows == 0) return PAC_OK;
+    if (state_misplaced(b, rows, y, {x, o}) || state_misplaced(b, rows, n, {x, o, y})) return PAC_ERR_RANGE;
     NormArgs a = norm_args(b, rows, x, o);
     a.y = y; a.n = n;
     (void)hipGetLastError();
@@ -607,6 +621,21 @@ pac_status pac_block_norm_backward(const pac_block_norm *b, int64_t rows, const 
         if (!n_aligned(p, 4)) return PAC_ERR_ALIGN;
     if (sums && !n_aligned(workspace, 16)) return PAC_ERR_ALIGN;
     if (sums && workspace_bytes < pac_block_norm_workspace_bytes(b, rows)) return PAC_ERR_WORKSPACE;
+    if (state_misplaced(b, rows, dx, {x, o, dy, dn, do_}) || state_misplaced(b, rows, do_, {x, o, dy, dn, dx}) || (dx && dx == do_ && rows))
+        return PAC_ERR_RANGE;
+    if (sums) {
+        // the sums' launch reads the parameters and the workspace while it writes the gradients
+        const int64_t vec = (int64_t)b->d * 4, states = rows * b->d * (b->dtype == PAC_F32 ? 4 : 2);
+        const Span outs[] = {Span(dw_post, vec), Span(db_post, vec), Span(dgate, (int64_t)b->gate_len * 4), Span(dres, 4), Span(dw_pre, vec),
+                             Span(db_pre, vec), Span(workspace, pac_block_norm_workspace_bytes(b, rows))};
+        for (const Span &u : outs) {
+            if (shares(u, {Span(b->w_post, vec), Span(b->b_post, vec), Span(b->gate, (int64_t)b->gate_len * 4), Span(b->res, 4), Span(b->w_pre, vec),
+                           Span(b->b_pre, vec), Span(x, states), Span(o, states), Span(dy, states), Span(dn, states), Span(dx, states), Span(do_, states)}))
+                return PAC_ERR_RANGE;
+            for (const Span &v : outs)
+                if (&u != &v && share(u, v)) return PAC_ERR_RANGE;
+        }
+    }
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     NormArgs a = norm_args(b, rows, x, o);
     a.dy = dy; a.dn = dn; a.dx = dx; a.d_o = do_;

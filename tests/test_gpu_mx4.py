@@ -524,3 +524,26 @@ def test_rows_past_32_bits_are_refused_not_cut_off():
     for bad in (lambda: lin.forward(x, y), lambda: lin.forward(x, y, x4=True), lambda: lin.input_grad(x, y)):
         with pytest.raises(ValueError):
             bad()
+
+
+def test_results_beside_and_over_the_inputs():
+    """x and y side by side in one buffer give what they give apart; y over x is refused, and nothing is written."""
+    rng = np.random.default_rng(13)
+    M, K, N = 70, 300, 64
+    codes, scales, _ = layer(rng, N, K)
+    lin = rt.Mx4Linear(codes, scales, K)
+    apart = torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
+    both = torch.zeros(M, 400, dtype=torch.bfloat16, device="cuda")
+    both[:, :K] = dev(rng.standard_normal((M, K)), torch.bfloat16)
+    x, y = both[:, :K], both[:, K:K + N]
+    for x4 in (False, True):
+        lin.forward(x.clone() if x4 else torch.nn.functional.pad(x, (0, 4))[:, :K], apart, x4=x4)
+        lin.forward(x, y, x4=x4)
+        assert torch.equal(y, apart)
+    was = both.clone()
+    for call in (lambda: lin.forward(x, both[:, K - 1:K - 1 + N]), lambda: lin.forward(x, x[:, :N], x4=True), lambda: lin.input_grad(both[:, :N], both[:, 50:50 + K]),
+                 lambda: rt.mx4_quantize(x, both.view(-1).view(torch.uint8)[:M * 256].view(M, 256), scales[:1].expand(M, -1).contiguous())):
+        with pytest.raises(pb.PacError) as e:
+            call()
+        assert e.value.status == pb.PAC_ERR_RANGE
+    assert torch.equal(both, was)
