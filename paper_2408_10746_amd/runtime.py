@@ -214,21 +214,20 @@ def _fits(n: int, what: str) -> int:
     return n
 
 
-def _rows_of(t, name: str, rows: int, cols: int, device):
-    """(row stride, pac_dtype) of a [rows][cols] device matrix with neighbouring columns."""
+def _rows_of(t, name: str, rows: int, cols: int, gpu: int):
+    """(row stride, pac_dtype) of a [rows][cols] matrix with neighbouring columns on the GPU of that number (-1: none)."""
     kind = _KIND.get(t.dtype)
-    if kind is None or t.device != device or device.type != "cuda" or t.shape != (rows, cols):
-        raise ValueError(f"{name}: bfloat16 or float32, ({rows}, {cols}), on {device} (a GPU) is wanted, not {t.dtype}, {tuple(t.shape)}, "
-                         f"on {t.device}")
+    if kind is None or t.get_device() != gpu or gpu < 0 or t.shape != (rows, cols):
+        raise ValueError(f"{name}: bfloat16 or float32, ({rows}, {cols}), on GPU {gpu} is wanted, not {t.dtype}, {tuple(t.shape)}, on {t.device}")
     stride = t.stride()
     if stride[1] != 1 and cols > 1:
         raise ValueError(f"{name}: neighbouring columns are wanted")
     return (stride[0] if rows > 1 else max(stride[0], cols)), kind
 
 
-def _chunked_rows(t, name: str, rows: int, cols: int, device) -> int:
+def _chunked_rows(t, name: str, rows: int, cols: int, gpu: int) -> int:
     """The row stride of a bf16 matrix that is read in 16-byte pieces, in the last row too."""
-    stride, kind = _rows_of(t, name, rows, cols, device)
+    stride, kind = _rows_of(t, name, rows, cols, gpu)
     if kind != pb.PAC_BF16:
         raise ValueError(f"{name}: bfloat16 is wanted")
     if cols % 8:
@@ -249,13 +248,12 @@ def _stored(codes, scales, rows: int, cols: int, device) -> None:
             raise ValueError(f"{name}: dense uint8, ({rows}, {pitch}), on {device} is wanted")
 
 
-def _call(device, name: str, *args) -> None:
-    """The library's function of that name on args and the device's current stream, with that device current."""
-    i = device.index
-    if torch._C._cuda_getDevice() != i:
-        with torch.cuda.device(i):
-            return _call(device, name, *args)
-    status = getattr(_lib(), name)(*args, torch._C._cuda_getCurrentRawStream(i))
+def _call(gpu: int, name: str, *args) -> None:
+    """The library's function of that name on args and that GPU's current stream, with that GPU current."""
+    if torch._C._cuda_getDevice() != gpu:
+        with torch.cuda.device(gpu):
+            return _call(gpu, name, *args)
+    status = getattr(_lib(), name)(*args, torch._C._cuda_getCurrentRawStream(gpu))
     if status:
         raise pb.PacError(status, name)
 
@@ -277,17 +275,19 @@ def mx4_empty(rows: int, cols: int, device="cuda:0"):
 def mx4_quantize(x, codes, scales) -> None:
     """x (bf16 or fp32, any row stride) into the stored form."""
     rows, cols = x.shape
-    stride, kind = _rows_of(x, "x", rows, cols, x.device)
+    gpu = x.get_device()
+    stride, kind = _rows_of(x, "x", rows, cols, gpu)
     _stored(codes, scales, rows, cols, x.device)
-    _call(x.device, "pac_mx4_quantize", x.data_ptr(), kind, rows, cols, stride, codes.data_ptr(), scales.data_ptr())
+    _call(gpu, "pac_mx4_quantize", x.data_ptr(), kind, rows, cols, stride, codes.data_ptr(), scales.data_ptr())
 
 
 def mx4_dequantize(codes, scales, out) -> None:
     """The values a stored matrix stands for, into out (bf16 or fp32, both exact)."""
     rows, cols = out.shape
-    stride, kind = _rows_of(out, "out", rows, cols, out.device)
+    gpu = out.get_device()
+    stride, kind = _rows_of(out, "out", rows, cols, gpu)
     _stored(codes, scales, rows, cols, out.device)
-    _call(out.device, "pac_mx4_dequantize", codes.data_ptr(), scales.data_ptr(), rows, cols, out.data_ptr(), kind, stride)
+    _call(gpu, "pac_mx4_dequantize", codes.data_ptr(), scales.data_ptr(), rows, cols, out.data_ptr(), kind, stride)
 
 
 class Mx4Linear:
@@ -296,7 +296,8 @@ class Mx4Linear:
 
     def __init__(self, codes, scales, K: int, bias=None):
         self.N, self.K, self.dev = _fits(codes.shape[0], "outputs"), K, codes.device
-        if self.dev.type != "cuda":
+        self._gpu = codes.get_device()
+        if self._gpu < 0:
             raise ValueError("codes: on a GPU")
         self.codes, self.scales, self.bias = codes, scales, bias
         self._w = None
@@ -324,27 +325,27 @@ class Mx4Linear:
     def forward(self, x, y, gelu: bool = False, x4: bool = False) -> None:
         """x [M][K] bf16, rows on 16 bytes; y [M][N] bf16 or fp32.  x4: x (bf16 or fp32, any row stride) is quantised too, and the
         product runs on 4-bit operands."""
-        M, dev = _fits(x.shape[0], "rows"), self.dev
-        sy, kind = _rows_of(y, "y", M, self.N, dev)
+        M, gpu = _fits(x.shape[0], "rows"), self._gpu
+        sy, kind = _rows_of(y, "y", M, self.N, gpu)
         act = pb.PAC_MX4_ACT_GELU if gelu else pb.PAC_MX4_ACT_NONE
         codes, scales, bias = self._weights()
         if x4:
-            sx, xkind = _rows_of(x, "x", M, self.K, dev)
+            sx, xkind = _rows_of(x, "x", M, self.K, gpu)
             need = M * self._x_bytes  # x in the stored form, for this call, on this stream
-            ws = torch.empty(need, dtype=torch.uint8, device=dev)
-            _call(dev, "pac_mx4_linear_qx", x.data_ptr(), xkind, M, self.K, sx, codes, scales, self.N, bias, act, y.data_ptr(), kind, sy,
+            ws = torch.empty(need, dtype=torch.uint8, device=self.dev)
+            _call(gpu, "pac_mx4_linear_qx", x.data_ptr(), xkind, M, self.K, sx, codes, scales, self.N, bias, act, y.data_ptr(), kind, sy,
                   ws.data_ptr(), need)
         else:
-            sx = _chunked_rows(x, "x", M, self.K, dev)
-            _call(dev, "pac_mx4_linear", x.data_ptr(), M, self.K, sx, codes, scales, self.N, bias, act, y.data_ptr(), kind, sy)
+            sx = _chunked_rows(x, "x", M, self.K, gpu)
+            _call(gpu, "pac_mx4_linear", x.data_ptr(), M, self.K, sx, codes, scales, self.N, bias, act, y.data_ptr(), kind, sy)
 
     def input_grad(self, dy, dx) -> None:
         """dy [M][N] bf16, rows on 16 bytes; dx [M][K] bf16 or fp32."""
-        M, dev = _fits(dy.shape[0], "rows"), self.dev
-        sdy = _chunked_rows(dy, "dy", M, self.N, dev)
-        sdx, kind = _rows_of(dx, "dx", M, self.K, dev)
+        M, gpu = _fits(dy.shape[0], "rows"), self._gpu
+        sdy = _chunked_rows(dy, "dy", M, self.N, gpu)
+        sdx, kind = _rows_of(dx, "dx", M, self.K, gpu)
         codes, scales, _ = self._weights()
-        _call(dev, "pac_mx4_linear_dx", dy.data_ptr(), M, self.N, sdy, codes, scales, self.K, dx.data_ptr(), kind, sdx)
+        _call(gpu, "pac_mx4_linear_dx", dy.data_ptr(), M, self.N, sdy, codes, scales, self.K, dx.data_ptr(), kind, sdx)
 
 
 class BlockNorm:
@@ -361,6 +362,7 @@ class BlockNorm:
             if len(shape) != 1 or shape[0] not in lens:
                 raise ValueError(f"{name}: {' or '.join(map(str, lens))} values")
         self.dev = next((p.device for p in self.params.values() if p is not None), None)
+        self._gpu = None if self.dev is None else self.dev.index
         self._b = {dtype: pb.pac_block_norm(d, kind, int(layer), 0 if gate is None else gate.shape[0], eps) for dtype, kind in _KIND.items()}
         self._at = None
         self._structure(torch.float32)
@@ -381,24 +383,25 @@ class BlockNorm:
             self._at = at
         return self._b[dtype]
 
-    def _rows(self, x, *others) -> int:
-        shape, dtype, dev = x.shape, x.dtype, x.device
-        if len(shape) != 2 or shape[1] != self.d or dtype not in _KIND or dev.type != "cuda" or not x.is_contiguous() or self.dev not in (None, dev):
+    def _rows(self, x, *others):
+        """(rows, GPU) of states."""
+        shape, dtype, gpu = x.shape, x.dtype, x.get_device()
+        if len(shape) != 2 or shape[1] != self.d or dtype not in _KIND or gpu < 0 or not x.is_contiguous() or self._gpu not in (gpu, None):
             raise ValueError(f"states: dense, bfloat16 or float32, [rows][{self.d}], on the parameters' device")
         for t in others:
-            if t is not None and (t.shape != shape or t.dtype != dtype or t.device != dev or not t.is_contiguous()):
+            if t is not None and (t.shape != shape or t.dtype is not dtype or t.get_device() != gpu or not t.is_contiguous()):
                 raise ValueError(f"states: dense, [rows][{self.d}], of one type, on one device")
-        return shape[0]
+        return shape[0], gpu
 
     def forward(self, x, o=None, y=None, n=None) -> None:
         """y and n of x and a block's output o (None: no block yet), into the buffers given."""
-        rows = self._rows(x, o, y, n)
-        _call(x.device, "pac_block_norm_forward", self._structure(x.dtype), rows, x.data_ptr(), _ptr(o), _ptr(y), _ptr(n))
+        rows, gpu = self._rows(x, o, y, n)
+        _call(gpu, "pac_block_norm_forward", self._structure(x.dtype), rows, x.data_ptr(), _ptr(o), _ptr(y), _ptr(n))
 
     def backward(self, x, o, dy, dn, dx=None, do=None, dparams=None) -> None:
         """Gradients, given dy (None: zero) and dn (None without w_pre), into the buffers given; dparams: {name: float32 tensor like
         the parameter} for those that are wanted."""
-        rows = self._rows(x, o, dy, dn, dx, do)
+        rows, gpu = self._rows(x, o, dy, dn, dx, do)
         b, grads, ws, need = self._structure(x.dtype), [None] * 6, None, 0
         if dparams:
             dev = x.device
@@ -408,4 +411,4 @@ class BlockNorm:
             grads = [_ptr(dparams.get(name)) for name in self.params]
             need = _lib().pac_block_norm_workspace_bytes(b, rows)
             ws = torch.empty(need, dtype=torch.uint8, device=x.device)  # for this call, on this stream
-        _call(x.device, "pac_block_norm_backward", b, rows, x.data_ptr(), _ptr(o), _ptr(dy), _ptr(dn), _ptr(dx), _ptr(do), *grads, _ptr(ws), need)
+        _call(gpu, "pac_block_norm_backward", b, rows, x.data_ptr(), _ptr(o), _ptr(dy), _ptr(dn), _ptr(dx), _ptr(do), *grads, _ptr(ws), need)
