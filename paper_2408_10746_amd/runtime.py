@@ -339,6 +339,16 @@ class Mx4Linear:
             sx = _chunked_rows(x, "x", M, self.K, gpu)
             _call(gpu, "pac_mx4_linear", x.data_ptr(), M, self.K, sx, codes, scales, self.N, bias, act, y.data_ptr(), kind, sy)
 
+    def forward_stored(self, codes, scales, y, gelu: bool = False) -> None:
+        """The same with x [M][K] already in the stored form (mx4_quantize): layers that share an input quantise it once.  The same bits as
+        forward with x4."""
+        M, gpu = _fits(codes.shape[0], "rows"), self._gpu
+        _stored(codes, scales, M, self.K, self.dev)
+        sy, kind = _rows_of(y, "y", M, self.N, gpu)
+        w, ws, bias = self._weights()
+        _call(gpu, "pac_mx4_linear_x4", codes.data_ptr(), scales.data_ptr(), M, self.K, w, ws, self.N, bias,
+              pb.PAC_MX4_ACT_GELU if gelu else pb.PAC_MX4_ACT_NONE, y.data_ptr(), kind, sy)
+
     def input_grad(self, dy, dx) -> None:
         """dy [M][N] bf16, rows on 16 bytes; dx [M][K] bf16 or fp32."""
         M, gpu = _fits(dy.shape[0], "rows"), self._gpu

@@ -547,3 +547,25 @@ def test_results_beside_and_over_the_inputs():
             call()
         assert e.value.status == pb.PAC_ERR_RANGE
     assert torch.equal(both, was)
+
+
+@pytest.mark.parametrize("M,K,N", [(1, 300, 77), (40, 1030, 900), (700, 1000, 3001)])
+def test_layers_that_share_a_stored_input(M, K, N):
+    """x quantised once for two layers: the bits that each gives quantising it in the call."""
+    rng = np.random.default_rng(14)
+    x = rows_of(rng, M, K)
+    xc, xs = rt.mx4_empty(M, K)
+    rt.mx4_quantize(x, xc, xs)
+    for n in (N, N + 5):
+        codes, scales, _ = layer(rng, n, K)
+        lin = rt.Mx4Linear(codes, scales, K, bias=dev(rng.standard_normal(n), torch.float32))
+        for dtype, gelu in (("bf16", True), ("f32", False)):
+            got, ref = torch.empty(M, n, dtype=DT[dtype], device="cuda"), torch.empty(M, n, dtype=DT[dtype], device="cuda")
+            lin.forward_stored(xc, xs, got, gelu=gelu)
+            lin.forward(x, ref, gelu=gelu, x4=True)
+            assert torch.equal(got, ref)
+    for bad in (lambda: lin.forward_stored(xc[:, :-128].contiguous(), xs, got), lambda: lin.forward_stored(xc, xs.cpu(), got), lambda: lin.forward_stored(xc, xs, got[:, 1:]),
+                lambda: lin.forward_stored(xc.float(), xs, got), lambda: lin.forward_stored(xc, xs[:0], got)):
+        with pytest.raises(ValueError):
+            bad()
+    lin.forward_stored(xc[:0], xs[:0], got[:0])
