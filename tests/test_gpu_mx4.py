@@ -569,3 +569,34 @@ def test_layers_that_share_a_stored_input(M, K, N):
         with pytest.raises(ValueError):
             bad()
     lin.forward_stored(xc[:0], xs[:0], got[:0])
+
+
+@pytest.mark.parametrize("M", [3, 300])
+def test_the_bindings_functions_are_the_layers_calls(M):
+    """paper_2408_10746_amd.binding on addresses gives the bits that runtime gives on tensors."""
+    rng = np.random.default_rng(15)
+    K, N, st = 320, 72, torch.cuda.current_stream().cuda_stream
+    w, x, dy = dev(rng.standard_normal((N, K)), torch.float32), rows_of(rng, M, K), rows_of(rng, M, N)
+    codes, scales = rt.mx4_empty(N, K)
+    pb.pac_mx4_quantize(w.data_ptr(), pb.PAC_F32, N, K, K, codes.data_ptr(), scales.data_ptr(), st)
+    lin = rt.Mx4Linear.from_weights(w, bias=dev(rng.standard_normal(N), torch.float32))
+    assert torch.equal(codes, lin.codes) and torch.equal(scales, lin.scales)
+    back, ref = torch.empty_like(w), torch.empty_like(w)
+    pb.pac_mx4_dequantize(codes.data_ptr(), scales.data_ptr(), N, K, back.data_ptr(), pb.PAC_F32, K, st)
+    rt.mx4_dequantize(codes, scales, ref)
+    assert torch.equal(back, ref)
+    y, z, d = (torch.empty(M, n, device="cuda") for n in (N, N, K))
+    tail = (codes.data_ptr(), scales.data_ptr(), N, lin.bias.data_ptr(), pb.PAC_MX4_ACT_GELU)
+    pb.pac_mx4_linear(x.data_ptr(), M, K, x.stride(0), *tail, y.data_ptr(), pb.PAC_F32, N, st)
+    lin.forward(x, z, gelu=True)
+    assert torch.equal(y, z)
+    ws = torch.empty(pb.pac_mx4_linear_qx_workspace_bytes(M, K), dtype=torch.uint8, device="cuda")
+    pb.pac_mx4_linear_qx(x.data_ptr(), pb.PAC_BF16, M, K, x.stride(0), *tail, y.data_ptr(), pb.PAC_F32, N, ws.data_ptr(), ws.numel(), st)
+    lin.forward(x, z, gelu=True, x4=True)
+    assert torch.equal(y, z)
+    pb.pac_mx4_linear_dx(dy.data_ptr(), M, N, dy.stride(0), codes.data_ptr(), scales.data_ptr(), K, d.data_ptr(), pb.PAC_F32, K, st)
+    e = torch.empty_like(d)
+    lin.input_grad(dy, e)
+    assert torch.equal(d, e)
+    with pytest.raises(pb.PacError):
+        pb.pac_mx4_linear(x.data_ptr(), M, K, K - 8, *tail, y.data_ptr(), pb.PAC_F32, N, st)

@@ -365,3 +365,26 @@ def test_parameters_given_other_storage():
                 call()
         bn.params[k] = was
     go(bn)
+
+
+def test_the_bindings_functions_are_the_layers_calls():
+    """paper_2408_10746_amd.binding on addresses gives the bits that runtime gives on tensors."""
+    from paper_2408_10746_amd import binding as pb
+    rng = np.random.default_rng(16)
+    rows, d, st = 70, 96, torch.cuda.current_stream().cuda_stream
+    v, p = make(rng, rows, d, "bf16", 2, True, True, True, True)
+    bn = rt.BlockNorm(d, layer=True, eps=1e-5, **p)
+    at = lambda *ts: [t.data_ptr() for t in ts]  # noqa: E731
+    names = ("w_post", "b_post", "gate", "res", "w_pre", "b_pre")
+    b = pb.pac_block_norm(d, pb.PAC_BF16, 1, d, 1e-5, *at(*(p[k] for k in names)))
+    dy, dn = dev(rng.standard_normal((rows, d)), torch.bfloat16), dev(rng.standard_normal((rows, d)), torch.bfloat16)
+    y, n, dx, do, y2, n2, dx2, do2 = (torch.empty_like(dy) for _ in range(8))
+    g, g2 = ({k: torch.empty_like(p[k]) for k in names} for _ in range(2))
+    pb.pac_block_norm_forward(b, rows, *at(v["x"], v["o"], y, n), st)
+    ws = torch.empty(pb.pac_block_norm_workspace_bytes(b, rows), dtype=torch.uint8, device="cuda")
+    pb.pac_block_norm_backward(b, rows, *at(v["x"], v["o"], dy, dn, dx, do, *g.values()), ws.data_ptr(), ws.numel(), st)
+    bn.forward(v["x"], v["o"], y2, n2)
+    bn.backward(v["x"], v["o"], dy, dn, dx2, do2, g2)
+    assert all(torch.equal(s, t) for s, t in zip([y, n, dx, do, *g.values()], [y2, n2, dx2, do2, *g2.values()]))
+    with pytest.raises(pb.PacError):
+        pb.pac_block_norm_forward(b, -1, *at(v["x"], v["o"], y, n), st)
