@@ -10,7 +10,8 @@
  *               (the conversion of the OCP Microscaling Formats specification, v1.0, Sec. 6.3); a block that holds an infinity
  *               or a NaN, which e2m1 has no codes for, gets s = 255 and zero codes
  *   dequantise  x' = e2m1(code) 2^(s - 127), exact in bf16 and in fp32
- *   linear      y = act(x W^T + bias), x in bf16 or itself in mx4: every product is exact, sums are fp32, y is rounded once
+ *   linear      y = act(x W^T + bias), x in bf16 or itself in mx4: every product is exact (where it is a normal fp32 number: factors
+ *               may be as small as 2^-128 each), sums are fp32, y is rounded once
  *   dx          dx = dy W, the way back through a frozen layer (W takes no gradient: Sec. 4.1, the backbone is frozen)
  *
  * STORED FORM of a matrix [rows][cols]: rows padded to a multiple of 256 columns by zero codes and zero scale bytes;

@@ -600,3 +600,29 @@ def test_the_bindings_functions_are_the_layers_calls(M):
     assert torch.equal(d, e)
     with pytest.raises(pb.PacError):
         pb.pac_mx4_linear(x.data_ptr(), M, K, K - 8, *tail, y.data_ptr(), pb.PAC_F32, N, st)
+
+
+@pytest.mark.parametrize("M,K,N", [(2, 200, 40), (40, 520, 900), (700, 320, 600), (4237, 937, 3687), (4096, 1024, 256)])
+@pytest.mark.parametrize("ew,ex", [(-126, 110), (-121, 100), (110, -131), (100, -124), (-60, -40), (60, 50)])
+def test_products_at_the_ends_of_the_range(M, K, N, ew, ex):
+    """Stored values and activations below 2^-126, whose products are ordinary numbers, count in full."""
+    rng = np.random.default_rng(17)
+    w = rng.standard_normal((N, K)) * np.exp2(rng.integers(-2, 3, size=(N, 1)))
+    w = np.ldexp(w, ew).astype(np.float32)
+    codes, scales = rt.mx4_empty(N, K)
+    rt.mx4_quantize(dev(w), codes, scales)
+    wv = bo.values(codes.cpu().numpy(), scales.cpu().numpy(), K)
+    lin = rt.Mx4Linear(codes, scales, K)
+    few = np.r_[0:min(M, 40), M - 1]                     # the oracle takes some of the rows
+    for product in (0, 1, 2):
+        x = rows_of(rng, M, N if product == 2 else K)
+        x *= torch.from_numpy(np.array(2.0 ** ex)).cuda()
+        y = torch.empty(M, K if product == 2 else N, device="cuda")
+        if product == 2:
+            lin.input_grad(x, y)
+        else:
+            lin.forward(x, y, x4=product == 1)
+        xv = (stored_rows(x, K) if product == 1 else host(x))[few]
+        ref, absum = bo.linear(xv, wv.T if product == 2 else wv)
+        assert product == 1 or np.abs(ref).max() > 0     # (x below half the format's least step is stored as zero)
+        check(host(y)[few], ref, bar(ref, absum, x.shape[1], "f32"))
