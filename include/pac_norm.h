@@ -15,6 +15,7 @@
  *     dx = res g      do = the gradient of w_post N(o) for gate g      dres = sum g x      dgate = sum g p
  *     dw_post = sum gate g N(o)    db_post = sum gate g    dw_pre = sum dn N(y)    db_pre = sum dn    (sums over the rows)
  *
+ * Sums of squares are 32-bit: where one overflows (values past 1e19) N gives 0, as its 32-bit formula does.
  * One pass over the data in each direction.  States and their gradients are bf16 or fp32, everything else fp32; y enters N
  * before it is rounded.  Sums over rows have a fixed order: the same call gives the same bits.  They are added in 32 bits over at
  * most 64 rows one after the other (8 such sums at most after that), and in 64 bits from there (to 2^30 rows).

@@ -338,8 +338,9 @@ template <int X, int RM, int NW> __global__ __launch_bounds__(64 * NW) void k_mx
 // across W's rows, eight of which a lane needs for one column: a lane loads 4 bytes (eight columns) of eight rows, converts them
 // with each row's scale and swaps halves of register pairs, which leaves it the eight rows of eight columns.  The matrix
 // instruction number c takes column c of every lane, so lanes i = 0 .. 15 cover 128 neighbouring columns and an output lane holds
-// eight neighbouring ones: no transposed copy of W anywhere.  1 x 4096 x 4096 in 13 us, 517 x 1001 x 775 in 7 us; the vector
-// units bound it (64 instructions a step to convert and swap, beside eight matrix instructions).
+// eight neighbouring ones: no transposed copy of W anywhere.  517 x 1001 x 775 in 6.7 us, 1 x 4096 x 4096 in 11 to 13 us.  Where
+// workgroups fill the chip the vector units bound it (64 instructions a step to convert and swap, beside eight matrix instructions);
+// with few rows it is their number: one for 128 columns, 32 of them at K = 4096, each walking all of N.
 __device__ __forceinline__ uint32_t pk_lo(bf16x2 a, bf16x2 b) // {a[0], b[0]}
 {
     return __builtin_amdgcn_perm(*reinterpret_cast<uint32_t *>(&b), *reinterpret_cast<uint32_t *>(&a), 0x05040100u);
@@ -1011,7 +1012,8 @@ template <int RM> static pac_status launch_dx_rows(const Mx4Args &a, hipStream_t
 // Which tiles a product runs on.  For each form the time in us is estimated as  start + tile n + steps max(least, share n)  with n
 // its tiles over 256 compute units (whole rounds where one tile fills a unit): a step's latency where units have less than one tile,
 // its throughput where they have more.  The constants are fitted to all forms' times at 594 shapes (446 for dx; M to 4096, K to 8192,
-// N to 16384): the form taken costs 0.5 % (x in bf16), 0.4 % (x in mx4) and 0.1 % (dx) over the best one, on the geometric mean.
+// a multiple of 8, N to 16384; profiles/mx4_forms_times.csv): over the best one the form taken costs 0.3 % (x in bf16), 0.5 % (x in mx4)
+// and 0.1 % (dx) on the geometric mean, and 25 %, 33 % and 11 % at the worst shape (665 x 200 x 695, 336 x 816 x 1434, 961 x 1120 x 1427).
 // Both sides, us: x in bf16, 64 x 4096 x 4096: 16 rows 25, 64 x 64 14; 1024 x 1024 x 4096: 64 x 64 17.1, 64 x 128 13.5, 128 x 128
 // 13.1, 256 x 256 25; 4096^3: 123 on 128 x 128, 106 on 256 x 256.  In mx4, 64 x 4096 x 4096: 32 rows 13.3, 64 x 64 8.5.
 // dx, 333 x 4096 x 4096: 16 rows 40, 32 rows 37, 64 rows 62.

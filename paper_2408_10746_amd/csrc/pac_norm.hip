@@ -163,7 +163,8 @@ template <int TPR> constexpr int kNormThreads = TPR < 512 ? 512 : TPR;
 // 104 us is 5.2 TB/s, what a copy reaches; one row of 4096 takes 2.9 us, a launch's time.  (16 values a thread and the parameters
 // read at every row: 116 us.)
 // HOLD: the parameters stay in registers from row to row, loaded along with the first row; else (rows past 8192, whose values fill
-// the registers) they are loaded for every row
+// the registers) they are loaded for every row.  The 16 values a thread of those rows do not fit beside it all the same: 280 to 408 bytes a
+// lane go to scratch (some 1050 with single loads), and 4096 x 16384 bf16 takes 318 us, 1.7 TB/s; 4096 x 8192 46 us.
 template <typename T, int VEC, int TPR, int E, bool LAYER, bool HOLD> __global__ __launch_bounds__(kNormThreads<TPR>) void k_norm_fwd(NormArgs a)
 {
     constexpr int RPB = kRowsPerBlock<TPR>;
@@ -231,7 +232,10 @@ template <typename T, int VEC, int TPR, int E, bool LAYER, bool HOLD> __global__
 // threads, one partial sum a block and column, added by k_norm_sums: no atomics, the same bits each time.  4096 x 4096 bf16 in 50
 // us is 4.0 TB/s, then 4.4 us of sums; what bounds it is a row's chain of four sums over 16 wavefronts, one block a compute unit.
 // Four values a thread and the parameters held: 8 a thread with parameters read at every row 51 us at 4096 and 35 against 19 us at
-// 2723 x 768 fp32, held at 8 a thread they spill (66 us); 16 a thread 142 us; two rows under way 53 us.
+// 2723 x 768 fp32, held at 8 a thread 66 us; 16 a thread 142 us; two rows under way 53 us.
+// Rows past 4096 take 8 a thread and past 8192 16, and their values go to scratch in part, the parameters read at every row or not: 96 to
+// 280 and 544 to 896 bytes a lane, up to 1724 with single loads.  bf16: 4096 x 5120 110 us (2.3 TB/s), 4096 x 8192 135 us (3.0),
+// 4096 x 16384 895 us (0.9); with single loads 4096 x 8191 517 us, 4096 x 16383 1960 us.
 // SHIFT: sums of g and of dn for the shifts' gradients (b_post, b_pre) are wanted too
 template <typename T, int VEC, int TPR, int E, bool LAYER, bool SHIFT, bool HOLD>
 __global__ __launch_bounds__(kNormThreads<TPR>, 4) void k_norm_bwd(NormArgs a)

@@ -292,7 +292,8 @@ def mx4_dequantize(codes, scales, out) -> None:
 
 class Mx4Linear:
     """A frozen linear layer with weights in the stored form: y = act(x W^T + bias), and dx = dy W on the way back.  Between calls its
-    tensors may be changed in place, and may be given other storage."""
+    tensors may be changed in place, and may be given other storage.  bf16 rows have to start on 16 bytes (a view of rows padded to a
+    multiple of 8 columns, where K or N is none); BlockNorm's states are dense, so that such widths are copied between the two."""
 
     def __init__(self, codes, scales, K: int, bias=None):
         self.N, self.K, self.dev = _fits(codes.shape[0], "outputs"), K, codes.device
