@@ -626,3 +626,21 @@ def test_products_at_the_ends_of_the_range(M, K, N, ew, ex):
         ref, absum = bo.linear(xv, wv.T if product == 2 else wv)
         assert product == 1 or np.abs(ref).max() > 0     # (x below half the format's least step is stored as zero)
         check(host(y)[few], ref, bar(ref, absum, x.shape[1], "f32"))
+
+
+@pytest.mark.parametrize("M,K,N", [(3, 300, 70), (700, 100, 3001), (4096, 1024, 4096)])
+def test_gelu_keeps_what_has_no_value(M, K, N):
+    """NaN comes through the activation on every path, beside neighbours that it leaves alone."""
+    rng = np.random.default_rng(18)
+    codes, scales, _ = layer(rng, N, K)
+    scales[N // 2, 0] = 255
+    bias = torch.zeros(N, device="cuda")
+    bias[1] = float("nan")
+    lin = rt.Mx4Linear(codes, scales, K, bias=bias)
+    x = rows_of(rng, M, K)
+    for dtype in DT.values():
+        y = torch.empty(M, N, dtype=dtype, device="cuda")
+        for x4 in (False, True):
+            lin.forward(x, y, gelu=True, x4=x4)
+            nan = torch.isnan(y)
+            assert nan[:, [1, N // 2]].all() and int(nan.sum()) == 2 * M
