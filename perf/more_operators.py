@@ -42,9 +42,9 @@ def listed():
         # the largest: two long samples of odd lengths, grouped heads
         dict(name="grad_long", kind="grad", batch=2, lo=4001, hi=6143, heads=32, kv_heads=8, d=128, causal=True),
         # serving: the newest token of each of 48 sequences into the cache of one layer and back; latency
-        dict(name="store_tokens", kind="store", rows=48, kv_heads=5, d=80, page=16, dtype="f32"),
+        dict(name="store_tokens", kind="store", rows=48, kv_heads=5, d=80, page=16, prompt=False, dtype="f32"),
         # a long prompt's keys and values
-        dict(name="store_prompt", kind="store", rows=8192, kv_heads=8, d=128, page=64, dtype="bf16"),
+        dict(name="store_prompt", kind="store", rows=8192, kv_heads=8, d=128, page=64, prompt=True, dtype="bf16"),
         # serving one short conversation, every query head with keys of its own: latency
         dict(name="decode_one", kind="decode", batch=1, lo=700, hi=700, heads=32, kv_heads=32, d=128, page=16),
         # serving 64 conversations of very different lengths, grouped heads
@@ -73,7 +73,7 @@ def draw(rng):
             _, kv, d = _heads(rng)
             rows = _log_int(rng, 1, 32768)
             if rows * kv * d <= 8192 * 8 * 128:
-                return dict(kind=kind, rows=rows, kv_heads=kv, d=d, page=page, dtype=rng.choice(("bf16", "f32")))
+                return dict(kind=kind, rows=rows, kv_heads=kv, d=d, page=page, prompt=rows > 256 or rng.random() < 0.3, dtype=rng.choice(("bf16", "f32")))
     most = {"attn": 2 ** 25 * 4096, "grad": 2 ** 24 * 4096, "decode": 4 * 60000 * 4096}[kind]
     while True:
         heads, kv, d = _heads(rng)
@@ -160,7 +160,11 @@ def _inputs(case, seed):
     if kind == "store":
         rows, kv, page = case["rows"], case["kv_heads"], case["page"]
         pages = (rows + page - 1) // page + 3
-        slots = torch.randperm(pages * page, generator=g, device=DEV)[:rows]
+        if case["prompt"]:  # one sequence's tokens in order, its pages anywhere
+            at = torch.arange(rows, device=DEV)
+            slots = torch.randperm(pages, generator=g, device=DEV)[at // page] * page + at % page
+        else:  # tokens of as many sequences
+            slots = torch.randperm(pages * page, generator=g, device=DEV)[:rows]
         k, v = (_projected(g, rows, kv, d, DTYPES[case["dtype"]]) for _ in range(2))
         return dict(k=k, v=v, slots=slots, pages=pages)
     lens = _lens(case)
