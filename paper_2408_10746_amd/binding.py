@@ -39,6 +39,8 @@ EXPORTS = [
     "pac_mx4_code_pitch", "pac_mx4_scale_pitch", "pac_mx4_quantize", "pac_mx4_dequantize", "pac_mx4_linear", "pac_mx4_linear_x4",
     "pac_mx4_linear_qx_workspace_bytes", "pac_mx4_linear_qx", "pac_mx4_linear_dx", "pac_mx4_tiles",
     "pac_block_norm_forward", "pac_block_norm_workspace_bytes", "pac_block_norm_backward",
+    "pac_attn_forward", "pac_attn_workspace_bytes", "pac_attn_backward",
+    "pac_kv4_bytes", "pac_kv4_write", "pac_kv4_read", "pac_kv4_attend_workspace_bytes", "pac_kv4_attend",
 ]
 PAC_STATIC_WORKSPACE_BYTES = 64 << 20
 PAC_MX4_ACT_NONE, PAC_MX4_ACT_GELU = 0, 1
@@ -75,6 +77,14 @@ class pac_block_norm(C.Structure):
     _fields_ = [("d", C.c_int32), ("dtype", C.c_int32), ("layer", C.c_int32), ("gate_len", C.c_int32), ("eps", C.c_float),
                 ("w_post", C.c_void_p), ("b_post", C.c_void_p), ("gate", C.c_void_p), ("res", C.c_void_p), ("w_pre", C.c_void_p),
                 ("b_pre", C.c_void_p)]
+
+
+class pac_attn(C.Structure):
+    _fields_ = [("heads", C.c_int32), ("kv_heads", C.c_int32), ("d", C.c_int32), ("causal", C.c_int32), ("scale", C.c_float)]
+
+
+class pac_kv4(C.Structure):
+    _fields_ = [("at", C.c_void_p), ("pages", C.c_int64), ("page", C.c_int32), ("kv_heads", C.c_int32), ("d", C.c_int32)]
 
 
 class PacError(RuntimeError):
@@ -201,6 +211,21 @@ def lib():
         L.pac_block_norm_workspace_bytes.argtypes = [C.POINTER(pac_block_norm), i64]
         L.pac_block_norm_backward.restype = C.c_int
         L.pac_block_norm_backward.argtypes = [C.POINTER(pac_block_norm), i64] + [vp] * 13 + [i64, vp]
+        L.pac_attn_forward.restype = C.c_int
+        L.pac_attn_forward.argtypes = [C.POINTER(pac_attn), vp, i32, i64] + [vp, i64] * 4 + [vp, vp]
+        L.pac_attn_workspace_bytes.restype = i64
+        L.pac_attn_workspace_bytes.argtypes = [C.POINTER(pac_attn), i32, i64]
+        L.pac_attn_backward.restype = C.c_int
+        L.pac_attn_backward.argtypes = [C.POINTER(pac_attn), vp, i32, i64] + [vp, i64] * 4 + [vp] + [vp, i64] * 4 + [vp, i64, vp]
+        L.pac_kv4_bytes.restype = i64
+        L.pac_kv4_bytes.argtypes = [C.POINTER(pac_kv4)]
+        for f in (L.pac_kv4_write, L.pac_kv4_read):
+            f.restype = C.c_int
+            f.argtypes = [C.POINTER(pac_kv4), i64, vp, vp, i64, vp, i64, i32, vp]
+        L.pac_kv4_attend_workspace_bytes.restype = i64
+        L.pac_kv4_attend_workspace_bytes.argtypes = [C.POINTER(pac_kv4), i32, i32, i32]
+        L.pac_kv4_attend.restype = C.c_int
+        L.pac_kv4_attend.argtypes = [C.POINTER(pac_kv4), i32, C.c_float, i32, vp, i32, i64, vp, vp, i64, vp, i64, vp, i64, vp]
         L.pac_profile_begin.restype = C.c_int
         L.pac_profile_begin.argtypes = [vp]
         L.pac_profile_end.restype = C.c_int
@@ -563,3 +588,43 @@ def pac_block_norm_backward(b: pac_block_norm, rows: int, x_ptr, o_ptr, dy_ptr, 
     _check(lib().pac_block_norm_backward(C.byref(b), rows, x_ptr, o_ptr, dy_ptr, dn_ptr, dx_ptr, do_ptr, dw_post_ptr, db_post_ptr,
                                          dgate_ptr, dres_ptr, dw_pre_ptr, db_pre_ptr, ws_ptr, ws_bytes, stream),
            "pac_block_norm_backward")
+
+
+def pac_attn_forward(a: pac_attn, offsets_ptr, batch: int, rows: int, q_ptr, q_stride: int, k_ptr, k_stride: int, v_ptr, v_stride: int,
+                     o_ptr, o_stride: int, lse_ptr=None, stream=0) -> None:
+    _check(lib().pac_attn_forward(C.byref(a), offsets_ptr, batch, rows, q_ptr, q_stride, k_ptr, k_stride, v_ptr, v_stride, o_ptr, o_stride,
+                                  lse_ptr, stream), "pac_attn_forward")
+
+
+def pac_attn_workspace_bytes(a: pac_attn, batch: int, rows: int) -> int:
+    return int(lib().pac_attn_workspace_bytes(C.byref(a), batch, rows))
+
+
+def pac_attn_backward(a: pac_attn, offsets_ptr, batch: int, rows: int, q_ptr, q_stride: int, k_ptr, k_stride: int, v_ptr, v_stride: int,
+                      o_ptr, o_stride: int, lse_ptr, do_ptr, do_stride: int, dq_ptr, dq_stride: int, dk_ptr, dk_stride: int, dv_ptr,
+                      dv_stride: int, ws_ptr, ws_bytes: int, stream=0) -> None:
+    _check(lib().pac_attn_backward(C.byref(a), offsets_ptr, batch, rows, q_ptr, q_stride, k_ptr, k_stride, v_ptr, v_stride, o_ptr,
+                                   o_stride, lse_ptr, do_ptr, do_stride, dq_ptr, dq_stride, dk_ptr, dk_stride, dv_ptr, dv_stride,
+                                   ws_ptr, ws_bytes, stream), "pac_attn_backward")
+
+
+def pac_kv4_bytes(c: pac_kv4) -> int:
+    return int(lib().pac_kv4_bytes(C.byref(c)))
+
+
+def pac_kv4_write(c: pac_kv4, rows: int, slots_ptr, k_ptr, k_stride: int, v_ptr, v_stride: int, dtype: int, stream=0) -> None:
+    _check(lib().pac_kv4_write(C.byref(c), rows, slots_ptr, k_ptr, k_stride, v_ptr, v_stride, dtype, stream), "pac_kv4_write")
+
+
+def pac_kv4_read(c: pac_kv4, rows: int, slots_ptr, k_ptr, k_stride: int, v_ptr, v_stride: int, dtype: int, stream=0) -> None:
+    _check(lib().pac_kv4_read(C.byref(c), rows, slots_ptr, k_ptr, k_stride, v_ptr, v_stride, dtype, stream), "pac_kv4_read")
+
+
+def pac_kv4_attend_workspace_bytes(c: pac_kv4, heads: int, batch: int, table_len: int) -> int:
+    return int(lib().pac_kv4_attend_workspace_bytes(C.byref(c), heads, batch, table_len))
+
+
+def pac_kv4_attend(c: pac_kv4, heads: int, scale: float, batch: int, table_ptr, table_len: int, table_stride: int, lens_ptr, q_ptr,
+                   q_stride: int, o_ptr, o_stride: int, ws_ptr, ws_bytes: int, stream=0) -> None:
+    _check(lib().pac_kv4_attend(C.byref(c), heads, scale, batch, table_ptr, table_len, table_stride, lens_ptr, q_ptr, q_stride, o_ptr,
+                                o_stride, ws_ptr, ws_bytes, stream), "pac_kv4_attend")

@@ -10,14 +10,16 @@ CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libpac.so")
 OBJ_DIR = os.path.join(_HERE, "_build")
 SOURCES = ["pac_api.hip", "pac_kernels.hip", "pac_gram.hip", "pac_gram32.hip", "pac_probe.hip", "pac_plan.hip", "pac_quant.hip", "pac_ladder.hip",
-           "pac_mx4.hip", "pac_norm.hip"]
+           "pac_mx4.hip", "pac_norm.hip", "pac_attn.hip", "pac_kv4.hip"]
 HEADERS = ["pac_gemm.h", "pac_mma.h", "pac_internal.h", "pac_span.h", os.path.join("..", "..", "include", "pac.h"),
            os.path.join("..", "..", "include", "pac_plan.h"),
            os.path.join("..", "..", "include", "pac_quant.h"),
            os.path.join("..", "..", "include", "pac_tier.h"),
            os.path.join("..", "..", "include", "pac_ladder.h"),
            os.path.join("..", "..", "include", "pac_mx4.h"),
-           os.path.join("..", "..", "include", "pac_norm.h")]
+           os.path.join("..", "..", "include", "pac_norm.h"),
+           os.path.join("..", "..", "include", "pac_attn.h"),
+           os.path.join("..", "..", "include", "pac_kv4.h")]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -1,0 +1,612 @@
+// Attention over packed sequences and its gradients (declared in include/pac_attn.h).
+#include "../../include/pac_attn.h"
+#include "pac_mma.h"
+#include "pac_span.h"
+#include <cfloat>
+#include <cmath>
+
+namespace pac {
+
+struct AttnArgs {
+    const int32_t *off; // [batch + 1]
+    int batch, rows;
+    int heads, kv_heads, group, d;
+    float scale, c2; // scale, scale log2(e)
+    const bf16_t *q, *k, *v, *o, *d_o;
+    int64_t qs, ks, vs, os, dos;
+    bf16_t *out; // forward: o
+    float *lse;  // [heads][rows]
+    bf16_t *dq, *dk, *dv;
+    int64_t dqs, dks, dvs;
+    float *delta; // [heads][rows]
+    unsigned tiles; // tiles of a head, of all sequences together
+};
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// ---------------------------------------------------------------------------
+// Which rows a workgroup has.  Tiles begin where sequences do; a sequence that begins at row s has the tiles s / BM + b and up, of
+// which there are never fewer than it needs, so that the grid follows from rows and batch alone and a tile's sequence is found by a
+// search over the offsets, 64 places a time.  (Tiles past a sequence's end do nothing.)
+// ---------------------------------------------------------------------------
+struct AttnSeq {
+    int start, len, tile; // len < 1: nothing to do
+};
+template <int BM> __device__ __forceinline__ AttnSeq attn_seq(const AttnArgs &a, int vt)
+{
+    const int lane = threadIdx.x & 63;
+    auto at = [&](int b) { return min(max(a.off[b], 0), a.rows); };
+    int lo = 0, n = a.batch;
+    for (;;) {
+        const int step = (n + 63) / 64, b = lane * step;
+        const bool before = b < n && at(lo + b) / BM + lo + b <= vt;
+        const int cnt = __builtin_popcountll(__ballot(before));
+        if (cnt == 0) return AttnSeq{0, 0, 0};
+        lo += (cnt - 1) * step;
+        n = min(step, n - (cnt - 1) * step);
+        if (step == 1) break;
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    const int start = at(lo), end = at(lo + 1);
+    const int tile = vt - (start / BM + lo);
+    return AttnSeq{start, (int64_t)tile * BM < end - start ? end - start : 0, tile};
+}
+
+// ---------------------------------------------------------------------------
+// Tiles of keys, values, queries or their gradients in LDS: rows of D values (padded with zeros), read in two ways.
+//   along the row   16 bytes a lane, 16 rows at the same place at a time
+//   turned round    ds_read_b64_tr_b16: 8 bytes a lane, four rows of 64 bytes at a time
+// Both are free of bank conflicts (64 banks of 4 bytes) where 16 neighbouring rows have their 16-byte pieces in 16 different
+// places of the 256-byte line, and any four rows that begin at a multiple of four have theirs in different quarters of it:
+// piece c of row x lies at c ^ swz(x).
+// ---------------------------------------------------------------------------
+template <int D> struct AttnTile {
+    static constexpr int CH = D / 8;                 // 16-byte pieces of a row
+    static constexpr int RB = D == 96 ? 256 : 2 * D; // bytes from row to row
+    static __device__ __forceinline__ int swz(int row)
+    {
+        if constexpr (RB == 256) return (row & 3) << 2 | (row >> 2 & 3);
+        else if constexpr (RB == 128) return (row >> 1 & 1) << 2 | (row >> 2 & 3);
+        else return row >> 2 & 3;
+    }
+    static __device__ __forceinline__ int at(int row, int piece) { return row * RB + ((piece ^ swz(row)) << 4); }
+};
+
+// A tile of ROWS rows on its way from memory to LDS through registers; rows past `have` and values past d are zeros.
+template <int D, int ROWS> struct AttnFetch {
+    using T = AttnTile<D>;
+    static constexpr int N = (ROWS * T::CH + 255) / 256;
+    u32x4 r[N];
+    __device__ __forceinline__ void load(const bf16_t *base, int64_t stride, int have, int d)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int id = i * 256 + threadIdx.x, row = id / T::CH, piece = id % T::CH;
+            r[i] = u32x4{0, 0, 0, 0};
+            if (row < min(have, ROWS) && piece * 8 < d) r[i] = *reinterpret_cast<const u32x4 *>(base + row * stride + piece * 8);
+        }
+    }
+    __device__ __forceinline__ void store(char *lds) const
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int id = i * 256 + threadIdx.x, row = id / T::CH, piece = id % T::CH;
+            if (ROWS * T::CH % 256 == 0 || row < ROWS) *reinterpret_cast<u32x4 *>(lds + T::at(row, piece)) = r[i];
+        }
+    }
+};
+
+// Operands of 32x32x16 products.  "Along": lane (i = lane % 32, h = lane / 32) holds row row0 + i, values 16 ks + 8 h ..+7.
+template <int D> __device__ __forceinline__ bf16x8 along(const char *lds, int row0, int ks)
+{
+    const int lane = threadIdx.x & 63;
+    return *reinterpret_cast<const bf16x8 *>(lds + AttnTile<D>::at(row0 + (lane & 31), 2 * ks + (lane >> 5)));
+}
+// "Turned": lane (i, h) holds value 32 t + i of the rows row0 + 16 j + {4 h ..+3, 8 + 4 h ..+3}, which are the rows of the registers
+// 8 j ..+7 of a 32 x 32 result in the same lane: a result enters the next product as it is.
+template <int D> __device__ __forceinline__ bf16x8 turned(const char *lds, int row0, int j, int t)
+{
+    const int lane = threadIdx.x & 63, p = lane & 15, h = lane >> 5;
+    const int row = row0 + 16 * j + 4 * h + (p >> 2), piece = 4 * t + 2 * (lane >> 4 & 1) + (p >> 1 & 1), in = 8 * (p & 1);
+    return tr_read2(lds + AttnTile<D>::at(row, piece) + in, lds + AttnTile<D>::at(row + 8, piece) + in);
+}
+// The same of a matrix in memory: row i of 32 (zeros past `have`, and past d)
+__device__ __forceinline__ bf16x8 along_mem(const bf16_t *base, int64_t stride, int have, int d, int ks)
+{
+    const int lane = threadIdx.x & 63, i = lane & 31, at = 16 * ks + 8 * (lane >> 5);
+    bf16x8 r{};
+    if (i < have && at < d) r = *reinterpret_cast<const bf16x8 *>(base + i * stride + at);
+    return r;
+}
+__device__ __forceinline__ f32x16 zeros16()
+{
+    f32x16 z;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z[i] = 0.f;
+    return z;
+}
+// row of a 32 x 32 result in register i
+__device__ __forceinline__ int row_of(int i) { return 8 * (i >> 2) + 4 * ((threadIdx.x & 63) >> 5) + (i & 3); }
+__device__ __forceinline__ bf16x8 rounded(const f32x16 &s, int j)
+{
+    bf16x8 r;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = (bf16_t)s[8 * j + e];
+    return r;
+}
+
+// acc[t] += (turned tile)^T p over 32 rows of the tile, p in the registers of a 32 x 32 result.
+template <int D> __device__ __forceinline__ void add_turned(f32x16 (&acc)[D / 32], const char *lds, int row0, const bf16x8 (&p)[2])
+{
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(turned<D>(lds, row0, j, t), p[j], acc[t], 0, 0, 0);
+}
+// Do 32 rows of a tile hold an infinity or NaN?
+template <int D> __device__ __forceinline__ bool any_special(const char *lds, int row0)
+{
+    uint32_t bad = 0;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+        const u32x4 w = __builtin_bit_cast(u32x4, along<D>(lds, row0, ks));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) bad |= ((w[e] & 0x7f80u) == 0x7f80u) | ((w[e] & 0x7f800000u) == 0x7f800000u);
+    }
+    return __any(bad != 0);
+}
+// add_turned where row x of the tile takes part in column c of the result only if part(x, c): a matrix instruction would multiply an
+// infinity or NaN of a row that is masked by 0.  Row by row in the vector units, for the tiles on the diagonal that hold such values.
+template <int D, class Part>
+__device__ __forceinline__ void add_turned_apart(f32x16 (&acc)[D / 32], const char *lds, int row0, const bf16x8 (&p)[2], const Part &part)
+{
+    const int lane = threadIdx.x & 63, h = lane >> 5;
+#pragma unroll 1
+    for (int x = 0; x < 32; ++x) {
+        const int reg = (x >> 3) * 4 + (x & 3); // row_of, the other way round
+        float px = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) px = e == reg ? (float)p[e >> 3][e & 7] : px;
+        px = __shfl(px, (lane & 31) | (x >> 2 & 1) << 5, 64);
+        if (part(x, lane & 31)) {
+#pragma unroll
+            for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    __builtin_amdgcn_sched_barrier(0); // few registers at a time: the kernels need theirs
+                    const bf16x4 w = *reinterpret_cast<const bf16x4 *>(lds + AttnTile<D>::at(row0 + x, 4 * t + g) + 8 * h);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[t][4 * g + e] = fmaf((float)w[e], px, acc[t][4 * g + e]);
+                }
+        }
+    }
+}
+
+// A wavefront's 32 rows of results, turned round: lane's column is its row, register i of acc[t] the value 32 t + row_of(i).
+template <int D> __device__ __forceinline__ void put_rows(bf16_t *base, int64_t stride, int have, int d, const f32x16 (&acc)[D / 32], float by)
+{
+    const int lane = threadIdx.x & 63, i = lane & 31, h = lane >> 5;
+    if (i >= have) return;
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int at = 32 * t + 8 * g + 4 * h;
+            bf16x4 r;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r[e] = (bf16_t)(acc[t][4 * g + e] * by);
+            if (at < d) *reinterpret_cast<bf16x4 *>(base + i * stride + at) = r;
+        }
+}
+
+// Tile and head of a workgroup: heads vary fastest.
+struct AttnWork {
+    int head, vt;
+};
+__device__ __forceinline__ AttnWork attn_work(unsigned heads) { return AttnWork{(int)(blockIdx.x % heads), (int)(blockIdx.x / heads)}; }
+
+// ---------------------------------------------------------------------------
+// forward: 128 rows a workgroup, 32 a wavefront, which holds its queries and o in registers; 64 keys and values at a time in LDS.
+// S^T = K q^T has a query's scores in one column, so that maximum, sum and rescaling stay in a lane, and p in place as the operand
+// of o^T = V^T p^T.
+// ---------------------------------------------------------------------------
+template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_fwd(const AttnArgs a)
+{
+    using T = AttnTile<D>;
+    constexpr int BM = 128, BK = 64;
+    __shared__ __attribute__((aligned(16))) char lds[2 * BK * T::RB];
+    char *lk = lds, *lv = lds + BK * T::RB;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const AttnWork w = attn_work(a.heads);
+    const AttnSeq seq = attn_seq<BM>(a, w.vt);
+    if (seq.len < 1) return;
+    const int head = w.head, hk = head / a.group;
+    const int q0 = seq.tile * BM + wave * 32, have = min(32, seq.len - q0);
+    const bf16_t *kp = a.k + (int64_t)seq.start * a.ks + (int64_t)hk * a.d, *vp = a.v + (int64_t)seq.start * a.vs + (int64_t)hk * a.d;
+    const int keys = CAUSAL ? min(seq.len, seq.tile * BM + BM) : seq.len;
+
+    AttnFetch<D, BK> fk, fv;
+    fk.load(kp, a.ks, keys, a.d);
+    fv.load(vp, a.vs, keys, a.d);
+    bf16x8 q[D / 16];
+    const bf16_t *qp = a.q + (int64_t)(seq.start + q0) * a.qs + (int64_t)head * a.d;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) q[ks] = along_mem(qp, a.qs, have, a.d, ks);
+    f32x16 acc[D / 32];
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t) acc[t] = zeros16();
+    float top = -FLT_MAX, sum = 0.f; // scores are taken relative to `top`, which stays within 2^8 of the largest so far
+
+    for (int k0 = 0; k0 < keys; k0 += BK) {
+        __syncthreads();
+        fk.store(lk);
+        fv.store(lv);
+        __syncthreads();
+        if (k0 + BK < keys) {
+            fk.load(kp + (int64_t)(k0 + BK) * a.ks, a.ks, keys - k0 - BK, a.d);
+            fv.load(vp + (int64_t)(k0 + BK) * a.vs, a.vs, keys - k0 - BK, a.d);
+        }
+#pragma unroll
+        for (int sub = 0; sub < BK; sub += 32) {
+            const int key0 = k0 + sub;
+            if (key0 >= keys || have < 1 || (CAUSAL && key0 > q0)) continue; // the whole wavefront
+            f32x16 s = zeros16();
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(along<D>(lk, sub, ks), q[ks], s, 0, 0, 0);
+            const bool diagonal = CAUSAL && key0 == q0;
+            if (diagonal) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = row_of(i) <= (lane & 31) ? s[i] : -INFINITY;
+            } else if (key0 + 32 > seq.len) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = key0 + row_of(i) < seq.len ? s[i] : -INFINITY;
+            }
+            float most = s[0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) most = fmaxf(most, s[i]);
+            most *= a.c2;
+            if (__any(most > top + 8.f)) {
+                // each row for itself: what its neighbours' scores are changes no bit of it
+                most = fmaxf(most, __shfl_xor(most, 32, 64));
+                const float next = most > top + 8.f ? most : top, by = __builtin_amdgcn_exp2f(top - next);
+                top = next;
+                sum *= by;
+#pragma unroll
+                for (int t = 0; t < D / 32; ++t) acc[t] *= by;
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.c2, -top));
+                sum += s[i];
+            }
+            const bf16x8 p[2] = {rounded(s, 0), rounded(s, 1)};
+            if (diagonal && any_special<D>(lv, sub)) add_turned_apart<D>(acc, lv, sub, p, [](int key, int query) { return key <= query; });
+            else add_turned<D>(acc, lv, sub, p);
+        }
+    }
+    if (have < 1) return;
+    sum += __shfl_xor(sum, 32, 64);
+    put_rows<D>(a.out + (int64_t)(seq.start + q0) * a.os + (int64_t)head * a.d, a.os, have, a.d, acc, 1.f / sum);
+    if (a.lse && lane < have) a.lse[(int64_t)head * a.rows + seq.start + q0 + lane] = (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+}
+
+// ---------------------------------------------------------------------------
+// backward, dq: as the forward kernel, with p = exp(s - lse) known, and ds^T in place as the operand of dq^T = K^T ds^T.  delta comes
+// from the same product that makes do . v (the diagonal of do o^T), so that a row with one key has exactly no gradient in q and k; it
+// goes to memory for the other kernel.
+// ---------------------------------------------------------------------------
+template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a)
+{
+    using T = AttnTile<D>;
+    constexpr int BM = 128, BK = 64;
+    __shared__ __attribute__((aligned(16))) char lds[2 * BK * T::RB];
+    char *lk = lds, *lv = lds + BK * T::RB;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const AttnWork w = attn_work(a.heads);
+    const AttnSeq seq = attn_seq<BM>(a, w.vt);
+    if (seq.len < 1) return;
+    const int head = w.head, hk = head / a.group;
+    const int q0 = seq.tile * BM + wave * 32, have = min(32, seq.len - q0), at = lane & 31;
+    const bf16_t *kp = a.k + (int64_t)seq.start * a.ks + (int64_t)hk * a.d, *vp = a.v + (int64_t)seq.start * a.vs + (int64_t)hk * a.d;
+    const int keys = CAUSAL ? min(seq.len, seq.tile * BM + BM) : seq.len;
+
+    AttnFetch<D, BK> fk, fv;
+    fk.load(kp, a.ks, keys, a.d);
+    fv.load(vp, a.vs, keys, a.d);
+    bf16x8 q[D / 16], d_o[D / 16];
+    const int64_t row = seq.start + q0;
+    f32x16 own = zeros16();
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+        q[ks] = along_mem(a.q + row * a.qs + (int64_t)head * a.d, a.qs, have, a.d, ks);
+        d_o[ks] = along_mem(a.d_o + row * a.dos + (int64_t)head * a.d, a.dos, have, a.d, ks);
+        own = __builtin_amdgcn_mfma_f32_32x32x16_bf16(along_mem(a.o + row * a.os + (int64_t)head * a.d, a.os, have, a.d, ks), d_o[ks], own, 0, 0, 0);
+    }
+    float delta = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) delta = row_of(i) == at ? own[i] : delta;
+    {
+        const float other = __shfl_xor(delta, 32, 64);
+        delta = (at >> 2 & 1) == lane >> 5 ? delta : other;
+    }
+    const float lse2 = at < have ? a.lse[(int64_t)head * a.rows + row + at] * 1.4426950408889634f : 0.f;
+    if (lane < have) a.delta[(int64_t)head * a.rows + row + lane] = delta;
+    f32x16 acc[D / 32];
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t) acc[t] = zeros16();
+
+    for (int k0 = 0; k0 < keys; k0 += BK) {
+        __syncthreads();
+        fk.store(lk);
+        fv.store(lv);
+        __syncthreads();
+        if (k0 + BK < keys) {
+            fk.load(kp + (int64_t)(k0 + BK) * a.ks, a.ks, keys - k0 - BK, a.d);
+            fv.load(vp + (int64_t)(k0 + BK) * a.vs, a.vs, keys - k0 - BK, a.d);
+        }
+#pragma unroll
+        for (int sub = 0; sub < BK; sub += 32) {
+            const int key0 = k0 + sub;
+            if (key0 >= keys || have < 1 || (CAUSAL && key0 > q0)) continue;
+            f32x16 s = zeros16(), dp = zeros16();
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks) {
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(along<D>(lk, sub, ks), q[ks], s, 0, 0, 0);
+                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(along<D>(lv, sub, ks), d_o[ks], dp, 0, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.c2, -lse2)) * (dp[i] - delta);
+            const bool diagonal = CAUSAL && key0 == q0;
+            if (diagonal) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = row_of(i) <= at ? s[i] : 0.f;
+            } else if (key0 + 32 > seq.len) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = key0 + row_of(i) < seq.len ? s[i] : 0.f;
+            }
+            const bf16x8 p[2] = {rounded(s, 0), rounded(s, 1)};
+            if (diagonal && any_special<D>(lk, sub)) add_turned_apart<D>(acc, lk, sub, p, [](int key, int query) { return key <= query; });
+            else add_turned<D>(acc, lk, sub, p);
+        }
+    }
+    if (have < 1) return;
+    put_rows<D>(a.dq + row * a.dqs + (int64_t)head * a.d, a.dqs, have, a.d, acc, a.scale);
+}
+
+// ---------------------------------------------------------------------------
+// backward, dk and dv: 128 keys a workgroup, 32 a wavefront, which holds them, their values and both gradients in registers; 32 queries
+// and their do at a time in LDS, of all heads of the group one after the other.  S = q K^T has a key's scores in one column.
+// ---------------------------------------------------------------------------
+template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 1) void k_attn_dkv(const AttnArgs a)
+{
+    using T = AttnTile<D>;
+    constexpr int BN = 128, BQ = 32;
+    __shared__ __attribute__((aligned(16))) char lds[2 * BQ * T::RB];
+    __shared__ __attribute__((aligned(16))) float stat[2][BQ]; // lse log2(e) and delta of the rows
+    char *lq = lds, *ld = lds + BQ * T::RB;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const AttnWork w = attn_work(a.kv_heads);
+    const AttnSeq seq = attn_seq<BN>(a, w.vt);
+    if (seq.len < 1) return;
+    const int hk = w.head, key0 = seq.tile * BN + wave * 32, have = min(32, seq.len - key0);
+    const int64_t row = seq.start + key0;
+    bf16x8 k[D / 16], v[D / 16];
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+        k[ks] = along_mem(a.k + row * a.ks + (int64_t)hk * a.d, a.ks, have, a.d, ks);
+        v[ks] = along_mem(a.v + row * a.vs + (int64_t)hk * a.d, a.vs, have, a.d, ks);
+    }
+    f32x16 dk[D / 32], dv[D / 32];
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t) dk[t] = dv[t] = zeros16();
+
+    const int first = CAUSAL ? seq.tile * BN : 0, steps = (seq.len - first + BQ - 1) / BQ, total = steps * a.group;
+    AttnFetch<D, BQ> fq, fd;
+    float fs = 0.f;
+    auto fetch = [&](int n) {
+        const int head = hk * a.group + n / steps, q0 = first + n % steps * BQ, rest = seq.len - q0;
+        const int64_t at = seq.start + q0;
+        fq.load(a.q + at * a.qs + (int64_t)head * a.d, a.qs, rest, a.d);
+        fd.load(a.d_o + at * a.dos + (int64_t)head * a.d, a.dos, rest, a.d);
+        if (threadIdx.x < 2 * BQ) {
+            const int x = threadIdx.x % BQ;
+            const int64_t p = (int64_t)head * a.rows + at + x;
+            // rows past the end: p = exp(-infinity) = 0
+            if (threadIdx.x < BQ) fs = x < rest ? a.lse[p] * 1.4426950408889634f : INFINITY;
+            else fs = x < rest ? a.delta[p] : 0.f;
+        }
+    };
+    fetch(0);
+    for (int n = 0; n < total; ++n) {
+        __syncthreads();
+        fq.store(lq);
+        fd.store(ld);
+        if (threadIdx.x < 2 * BQ) stat[threadIdx.x / BQ][threadIdx.x % BQ] = fs;
+        __syncthreads();
+        if (n + 1 < total) fetch(n + 1);
+        const int q0 = first + n % steps * BQ;
+        if (have < 1 || (CAUSAL && q0 < key0)) continue;
+        f32x16 s = zeros16(), dp = zeros16();
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) {
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(along<D>(lq, 0, ks), k[ks], s, 0, 0, 0);
+            dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(along<D>(ld, 0, ks), v[ks], dp, 0, 0, 0);
+        }
+        const bool diagonal = CAUSAL && q0 == key0;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const f32x4 lse2 = *reinterpret_cast<const f32x4 *>(&stat[0][8 * g + 4 * (lane >> 5)]);
+            const f32x4 delta = *reinterpret_cast<const f32x4 *>(&stat[1][8 * g + 4 * (lane >> 5)]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int i = 4 * g + e;
+                s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.c2, -lse2[e]));
+                dp[i] = s[i] * (dp[i] - delta[e]);
+            }
+        }
+        if (diagonal) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const bool in = (lane & 31) <= row_of(i);
+                s[i] = in ? s[i] : 0.f;
+                dp[i] = in ? dp[i] : 0.f;
+            }
+        }
+        const bf16x8 p[2] = {rounded(s, 0), rounded(s, 1)}, ds[2] = {rounded(dp, 0), rounded(dp, 1)};
+        if (diagonal && (any_special<D>(ld, 0) || any_special<D>(lq, 0))) {
+            auto part = [](int query, int key) { return key <= query; };
+            add_turned_apart<D>(dv, ld, 0, p, part);
+            add_turned_apart<D>(dk, lq, 0, ds, part);
+        } else {
+            add_turned<D>(dv, ld, 0, p);
+            add_turned<D>(dk, lq, 0, ds);
+        }
+    }
+    if (have < 1) return;
+    put_rows<D>(a.dk + row * a.dks + (int64_t)hk * a.d, a.dks, have, a.d, dk, a.scale);
+    put_rows<D>(a.dv + row * a.dvs + (int64_t)hk * a.d, a.dvs, have, a.d, dv, 1.f);
+}
+
+// ---------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------
+static inline bool at_aligned(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+static pac_status check_attn(const pac_attn *a, int32_t batch, int64_t rows)
+{
+    if (!a) return PAC_ERR_NULL;
+    if (a->heads < 1 || a->heads > 4096 || a->kv_heads < 1 || a->heads % a->kv_heads || a->d < 8 || a->d > 128 || a->d % 8 ||
+        (a->causal != 0 && a->causal != 1) || !(a->scale > 0.f) || !std::isfinite(a->scale) || batch < 0)
+        return PAC_ERR_SHAPE;
+    if (rows < 0 || rows > INT32_MAX) return PAC_ERR_RANGE;
+    if ((rows / 128 + batch) * a->heads >= 1 << 23) return PAC_ERR_UNSUPPORTED;
+    return PAC_OK;
+}
+struct AttnRows { // a matrix of states
+    const void *at;
+    int64_t stride, cols;
+};
+static pac_status check_rows(const AttnRows &m)
+{
+    const int64_t cols = m.cols;
+    if (m.stride < cols) return PAC_ERR_RANGE;
+    if (m.stride % 8 || !at_aligned(m.at, 16)) return PAC_ERR_ALIGN;
+    return m.stride > 1 << 24 ? PAC_ERR_UNSUPPORTED : PAC_OK;
+}
+static Span rows_span(const AttnRows &m, int64_t rows) { return Span(m.at, rows, m.stride * 2, m.cols * 2); }
+
+static AttnArgs attn_args(const pac_attn *a, const int32_t *off, int32_t batch, int64_t rows)
+{
+    AttnArgs r{};
+    r.off = off; r.batch = batch; r.rows = (int)rows;
+    r.heads = a->heads; r.kv_heads = a->kv_heads; r.group = a->heads / a->kv_heads; r.d = a->d;
+    r.scale = a->scale; r.c2 = a->scale * 1.4426950408889634f;
+    r.tiles = (unsigned)(rows / 128 + batch);
+    return r;
+}
+static int64_t delta_bytes(const pac_attn *a, int64_t rows) { return (rows * a->heads * 4 + 255) / 256 * 256; }
+
+template <typename F> static void by_width(int d, const F &f)
+{
+    if (d <= 32) f(std::integral_constant<int, 32>());
+    else if (d <= 64) f(std::integral_constant<int, 64>());
+    else if (d <= 96) f(std::integral_constant<int, 96>());
+    else f(std::integral_constant<int, 128>());
+}
+
+} // namespace pac
+
+using namespace pac;
+
+extern "C" {
+
+pac_status pac_attn_forward(const pac_attn *a, const int32_t *offsets, int32_t batch, int64_t rows, const void *q, int64_t q_stride,
+                            const void *k, int64_t k_stride, const void *v, int64_t v_stride, void *o, int64_t o_stride, float *lse,
+                            void *hip_stream)
+{
+    pac_status s = check_attn(a, batch, rows);
+    if (s != PAC_OK) return s;
+    if (batch == 0 || rows == 0) return PAC_OK;
+    if (!offsets || !q || !k || !v || !o) return PAC_ERR_NULL;
+    const int64_t qc = (int64_t)a->heads * a->d, kc = (int64_t)a->kv_heads * a->d;
+    const AttnRows qm{q, q_stride, qc}, km{k, k_stride, kc}, vm{v, v_stride, kc}, om{o, o_stride, qc};
+    for (const AttnRows &m : {qm, km, vm, om})
+        if ((s = check_rows(m)) != PAC_OK) return s;
+    if (!at_aligned(offsets, 4) || !at_aligned(lse, 4)) return PAC_ERR_ALIGN;
+    const Span os = rows_span(om, rows), ls(lse, lse ? rows * a->heads * 4 : 0), off(offsets, ((int64_t)batch + 1) * 4);
+    const Span qs = rows_span(qm, rows), ks = rows_span(km, rows), vs = rows_span(vm, rows);
+    if (shares(os, {qs, ks, vs, ls, off}) || shares(ls, {qs, ks, vs, off})) return PAC_ERR_RANGE;
+    AttnArgs r = attn_args(a, offsets, batch, rows);
+    r.q = static_cast<const bf16_t *>(q); r.qs = q_stride;
+    r.k = static_cast<const bf16_t *>(k); r.ks = k_stride;
+    r.v = static_cast<const bf16_t *>(v); r.vs = v_stride;
+    r.out = static_cast<bf16_t *>(o); r.os = o_stride;
+    r.lse = lse;
+    (void)hipGetLastError();
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    by_width(a->d, [&](auto n) {
+        constexpr int D = decltype(n)::value;
+        const dim3 grid(r.tiles * r.heads);
+        if (a->causal) hipLaunchKernelGGL((k_attn_fwd<D, true>), grid, dim3(256), 0, st, r);
+        else hipLaunchKernelGGL((k_attn_fwd<D, false>), grid, dim3(256), 0, st, r);
+    });
+    return hipGetLastError() == hipSuccess ? PAC_OK : PAC_ERR_DEVICE;
+}
+
+int64_t pac_attn_workspace_bytes(const pac_attn *a, int32_t batch, int64_t rows)
+{
+    return check_attn(a, batch, rows) == PAC_OK ? delta_bytes(a, rows) : -1;
+}
+
+pac_status pac_attn_backward(const pac_attn *a, const int32_t *offsets, int32_t batch, int64_t rows, const void *q, int64_t q_stride,
+                             const void *k, int64_t k_stride, const void *v, int64_t v_stride, const void *o, int64_t o_stride,
+                             const float *lse, const void *do_, int64_t do_stride, void *dq, int64_t dq_stride, void *dk,
+                             int64_t dk_stride, void *dv, int64_t dv_stride, void *workspace, int64_t workspace_bytes, void *hip_stream)
+{
+    pac_status s = check_attn(a, batch, rows);
+    if (s != PAC_OK) return s;
+    if (batch == 0 || rows == 0) return PAC_OK;
+    if (!offsets || !q || !k || !v || !o || !lse || !do_ || !dq || !dk || !dv || !workspace) return PAC_ERR_NULL;
+    const int64_t qc = (int64_t)a->heads * a->d, kc = (int64_t)a->kv_heads * a->d;
+    const AttnRows qm{q, q_stride, qc}, km{k, k_stride, kc}, vm{v, v_stride, kc}, om{o, o_stride, qc}, dom{do_, do_stride, qc};
+    const AttnRows dqm{dq, dq_stride, qc}, dkm{dk, dk_stride, kc}, dvm{dv, dv_stride, kc};
+    for (const AttnRows &m : {qm, km, vm, om, dom, dqm, dkm, dvm})
+        if ((s = check_rows(m)) != PAC_OK) return s;
+    if (!at_aligned(offsets, 4) || !at_aligned(lse, 4) || !at_aligned(workspace, 16)) return PAC_ERR_ALIGN;
+    const int64_t need = pac_attn_workspace_bytes(a, batch, rows);
+    if (workspace_bytes < need) return PAC_ERR_WORKSPACE;
+    const Span qs = rows_span(qm, rows), ks = rows_span(km, rows), vs = rows_span(vm, rows), os = rows_span(om, rows);
+    const Span ds = rows_span(dom, rows), ls(lse, rows * a->heads * 4), off(offsets, ((int64_t)batch + 1) * 4);
+    const Span outs[] = {rows_span(dqm, rows), rows_span(dkm, rows), rows_span(dvm, rows), Span(workspace, need)};
+    for (const Span &u : outs) {
+        if (shares(u, {qs, ks, vs, os, ds, ls, off})) return PAC_ERR_RANGE;
+        for (const Span &x : outs)
+            if (&u != &x && share(u, x)) return PAC_ERR_RANGE;
+    }
+    AttnArgs r = attn_args(a, offsets, batch, rows);
+    r.q = static_cast<const bf16_t *>(q); r.qs = q_stride;
+    r.k = static_cast<const bf16_t *>(k); r.ks = k_stride;
+    r.v = static_cast<const bf16_t *>(v); r.vs = v_stride;
+    r.o = static_cast<const bf16_t *>(o); r.os = o_stride;
+    r.d_o = static_cast<const bf16_t *>(do_); r.dos = do_stride;
+    r.dq = static_cast<bf16_t *>(dq); r.dqs = dq_stride;
+    r.dk = static_cast<bf16_t *>(dk); r.dks = dk_stride;
+    r.dv = static_cast<bf16_t *>(dv); r.dvs = dv_stride;
+    r.lse = const_cast<float *>(lse);
+    r.delta = static_cast<float *>(workspace);
+    (void)hipGetLastError();
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    by_width(a->d, [&](auto n) {
+        constexpr int D = decltype(n)::value;
+        if (a->causal) {
+            hipLaunchKernelGGL((k_attn_dq<D, true>), dim3(r.tiles * r.heads), dim3(256), 0, st, r);
+            hipLaunchKernelGGL((k_attn_dkv<D, true>), dim3(r.tiles * r.kv_heads), dim3(256), 0, st, r);
+        } else {
+            hipLaunchKernelGGL((k_attn_dq<D, false>), dim3(r.tiles * r.heads), dim3(256), 0, st, r);
+            hipLaunchKernelGGL((k_attn_dkv<D, false>), dim3(r.tiles * r.kv_heads), dim3(256), 0, st, r);
+        }
+    });
+    return hipGetLastError() == hipSuccess ? PAC_OK : PAC_ERR_DEVICE;
+}
+
+} // extern "C"

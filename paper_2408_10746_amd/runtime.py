@@ -201,7 +201,7 @@ class TieredSession(Session):
         return raw.view(np.uint16 if es == 2 else np.float32).reshape(self.w.L, ln, self.w.d).copy()
 
 
-# ---- blocks of the frozen backbone (include/pac_mx4.h, include/pac_norm.h) ------------------------------------------
+# ---- blocks of the frozen backbone (include/pac_mx4.h, pac_norm.h, pac_attn.h, pac_kv4.h) ------------------------------------------
 # The library takes addresses alone, so what they stand for is checked here.  A single token's kernel takes 4 us: the checks are
 # written to cost little beside it.
 _KIND = {torch.bfloat16: pb.PAC_BF16, torch.float32: pb.PAC_F32}
@@ -423,3 +423,133 @@ class BlockNorm:
             need = _lib().pac_block_norm_workspace_bytes(b, rows)
             ws = torch.empty(need, dtype=torch.uint8, device=x.device)  # for this call, on this stream
         _call(gpu, "pac_block_norm_backward", b, rows, x.data_ptr(), _ptr(o), _ptr(dy), _ptr(dn), _ptr(dx), _ptr(do), *grads, _ptr(ws), need)
+
+
+def _head_rows(t, name: str, rows: int, cols: int, gpu: int) -> int:
+    """The row stride of a bf16 matrix of heads."""
+    if t.dtype != torch.bfloat16 or t.get_device() != gpu or t.shape != (rows, cols):
+        raise ValueError(f"{name}: bfloat16, ({rows}, {cols}), on GPU {gpu} is wanted, not {t.dtype}, {tuple(t.shape)}, on {t.device}")
+    stride = t.stride()
+    if stride[1] != 1 and cols > 1:
+        raise ValueError(f"{name}: neighbouring columns are wanted")
+    return stride[0] if rows > 1 else cols
+
+
+def _scale(scale, d: int) -> float:
+    return d ** -0.5 if scale is None else float(scale)
+
+
+def packed_offsets(lens, device="cuda:0"):
+    """Where sequences of those lengths begin and end in packed rows: int32 [batch + 1]."""
+    at = [0]
+    for n in lens:
+        if n < 0:
+            raise ValueError(f"lens: {n} rows")
+        at.append(at[-1] + int(n))
+    _fits(at[-1], "rows")
+    return torch.tensor(at, dtype=torch.int32, device=device)
+
+
+class Attention:
+    """Attention over sequences packed one after the other, and its gradients (include/pac_attn.h).  q and o are [rows][heads d], k and v
+    [rows][kv_heads d], bf16, rows on 16 bytes and any multiple of 8 apart (q, k and v may be columns of one matrix); offsets as
+    packed_offsets makes them.  lse is float32 [heads][rows], what the way back needs besides o.  scale: 1 / sqrt(d) where none is given."""
+
+    def __init__(self, heads: int, d: int, kv_heads: int | None = None, causal: bool = False, scale: float | None = None):
+        kv_heads = heads if kv_heads is None else kv_heads
+        self._a = pb.pac_attn(_fits(heads, "heads"), _fits(kv_heads, "kv_heads"), _fits(d, "d"), int(causal), _scale(scale, d) if d > 0 else 1.0)
+        if pb.pac_attn_workspace_bytes(self._a, 0, 0) < 0:
+            raise ValueError("heads: a multiple of kv_heads, 1..4096; d: a multiple of 8, 8..128; scale: positive, finite")
+        self.heads, self.kv_heads, self.d = heads, kv_heads, d
+
+    def _rows(self, q, offsets):
+        """(batch, rows, GPU)"""
+        gpu = q.get_device()
+        if gpu < 0 or q.dim() != 2 or offsets.dtype != torch.int32 or offsets.dim() != 1 or offsets.shape[0] < 1 or offsets.get_device() != gpu \
+                or not offsets.is_contiguous():
+            raise ValueError("q: a matrix on a GPU; offsets: int32, dense, [batch + 1], beside it")
+        return offsets.shape[0] - 1, _fits(q.shape[0], "rows"), gpu
+
+    def _lse(self, lse, rows, gpu):
+        if lse is not None and (lse.dtype != torch.float32 or lse.shape != (self.heads, rows) or lse.get_device() != gpu or not lse.is_contiguous()):
+            raise ValueError(f"lse: dense float32, ({self.heads}, {rows}), on GPU {gpu} is wanted")
+        return _ptr(lse)
+
+    def _matrix(self, t, name, cols, rows, gpu):
+        return t.data_ptr(), _head_rows(t, name, rows, cols, gpu)
+
+    def forward(self, q, k, v, offsets, o, lse=None) -> None:
+        """o, and lse where it is given, of the rows that sequences have; others are left as they are."""
+        batch, rows, gpu = self._rows(q, offsets)
+        qc, kc, m = self.heads * self.d, self.kv_heads * self.d, self._matrix
+        _call(gpu, "pac_attn_forward", self._a, offsets.data_ptr(), batch, rows, *m(q, "q", qc, rows, gpu), *m(k, "k", kc, rows, gpu),
+              *m(v, "v", kc, rows, gpu), *m(o, "o", qc, rows, gpu), self._lse(lse, rows, gpu))
+
+    def backward(self, q, k, v, offsets, o, lse, do, dq, dk, dv) -> None:
+        """Gradients of q, k and v, given that of o, into the buffers given; o and lse as forward wrote them."""
+        batch, rows, gpu = self._rows(q, offsets)
+        qc, kc, m = self.heads * self.d, self.kv_heads * self.d, self._matrix
+        if lse is None:
+            raise ValueError("lse: what forward wrote")
+        need = pb.pac_attn_workspace_bytes(self._a, batch, rows)
+        if need < 0:
+            raise ValueError("rows: too many of them by heads")
+        ws = torch.empty(need, dtype=torch.uint8, device=q.device)  # for this call, on this stream
+        _call(gpu, "pac_attn_backward", self._a, offsets.data_ptr(), batch, rows, *m(q, "q", qc, rows, gpu), *m(k, "k", kc, rows, gpu),
+              *m(v, "v", kc, rows, gpu), *m(o, "o", qc, rows, gpu), self._lse(lse, rows, gpu), *m(do, "do", qc, rows, gpu),
+              *m(dq, "dq", qc, rows, gpu), *m(dk, "dk", kc, rows, gpu), *m(dv, "dv", kc, rows, gpu), ws.data_ptr(), need)
+
+
+class Kv4Cache:
+    """Keys and values of one layer in 4 bits, in pages (include/pac_kv4.h).  Slot s is place s % page of page s / page; which pages a
+    sequence has is the caller's: a row of a table."""
+
+    def __init__(self, pages: int, page: int, kv_heads: int, d: int, device="cuda:0"):
+        self._c = pb.pac_kv4(None, pages, _fits(page, "page"), _fits(kv_heads, "kv_heads"), _fits(d, "d"))
+        need = pb.pac_kv4_bytes(self._c)
+        if need < 0:
+            raise ValueError("pages: 0..2^31 - 1; page: a power of two, 8..65536; kv_heads: 1..4096; d: a multiple of 8, 8..128")
+        self.pages, self.page, self.kv_heads, self.d = pages, page, kv_heads, d
+        self.data = torch.zeros(need, dtype=torch.uint8, device=device)
+        self._gpu = self.data.get_device()
+
+    def _at(self):
+        self._c.at = self.data.data_ptr()
+        return self._c
+
+    def _io(self, slots, k, v):
+        rows, cols, gpu = _fits(k.shape[0], "rows"), self.kv_heads * self.d, self._gpu
+        (sk, kind), (sv, other) = _rows_of(k, "k", rows, cols, gpu), _rows_of(v, "v", rows, cols, gpu)
+        if kind != other:
+            raise ValueError("k and v: of one type")
+        if slots.dtype != torch.int64 or slots.shape != (rows,) or slots.get_device() != gpu or not slots.is_contiguous():
+            raise ValueError(f"slots: dense int64, ({rows},), on GPU {gpu} is wanted")
+        return rows, slots.data_ptr(), k.data_ptr(), sk, v.data_ptr(), sv, kind
+
+    def write(self, k, v, slots) -> None:
+        """Row r of k and v [rows][kv_heads d] (bf16 or fp32, any row stride), quantised, into slot slots[r]; rows with a slot outside the
+        cache are left out.  No slot may be named twice."""
+        _call(self._gpu, "pac_kv4_write", self._at(), *self._io(slots, k, v))
+
+    def read(self, slots, k, v) -> None:
+        """The values that slots hold, into rows of k and v; rows with a slot outside the cache are left as they are."""
+        _call(self._gpu, "pac_kv4_read", self._at(), *self._io(slots, k, v))
+
+    def attend(self, q, table, lens, o, scale: float | None = None) -> None:
+        """o [batch][heads d] of one query a sequence, q alike (bf16, rows on 16 bytes), over the first lens[b] (int32) tokens in the pages of
+        row b of table (int32 [batch][pages at most]; a page outside the cache counts as masked).  No tokens: zeros."""
+        batch, gpu, d = _fits(q.shape[0], "sequences"), self._gpu, self.d
+        if q.dim() != 2 or q.shape[1] < d or q.shape[1] % d:
+            raise ValueError(f"q: [sequences][heads {d}]")
+        heads = q.shape[1] // d
+        sq, so = _head_rows(q, "q", batch, heads * d, gpu), _head_rows(o, "o", batch, heads * d, gpu)
+        if lens.dtype != torch.int32 or lens.shape != (batch,) or lens.get_device() != gpu or not lens.is_contiguous():
+            raise ValueError(f"lens: dense int32, ({batch},), on GPU {gpu} is wanted")
+        if table.dtype != torch.int32 or table.dim() != 2 or table.shape[0] != batch or table.get_device() != gpu or (table.shape[1] > 1 and table.stride(1) != 1):
+            raise ValueError(f"table: int32, ({batch}, pages), neighbouring columns, on GPU {gpu} is wanted")
+        pages = _fits(table.shape[1], "pages of a sequence")
+        c, st = self._at(), table.stride(0) if batch > 1 else pages
+        need = _lib().pac_kv4_attend_workspace_bytes(c, heads, batch, pages)
+        ws = torch.empty(max(need, 0), dtype=torch.uint8, device=q.device)  # for this call, on this stream
+        _call(gpu, "pac_kv4_attend", c, heads, _scale(scale, d), batch, table.data_ptr(), pages, st, lens.data_ptr(), q.data_ptr(), sq, o.data_ptr(), so,
+              ws.data_ptr(), need)

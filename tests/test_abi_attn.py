@@ -1,0 +1,150 @@
+"""CPU-only checks of the entry points of attention and the 4-bit key and value cache: sizes, and arguments that are refused on the host
+before anything is launched (no GPU needed; no address is ever read)."""
+import ctypes as C
+import math
+
+import pytest
+
+from paper_2408_10746_amd import binding as pb
+
+A = 1 << 20  # an aligned address that no refused call touches
+FAR = [A * (2 * k + 1) for k in range(16)]
+
+
+def attn(heads=4, kv_heads=2, d=64, causal=0, scale=0.125):
+    return pb.pac_attn(heads, kv_heads, d, causal, scale)
+
+
+def forward(a=None, off=FAR[0], batch=2, rows=10, q=FAR[1], sq=256, k=FAR[2], sk=128, v=FAR[3], sv=128, o=FAR[4], so=256, lse=FAR[5]):
+    return pb.lib().pac_attn_forward(C.byref(a or attn()), off, batch, rows, q, sq, k, sk, v, sv, o, so, lse, None)
+
+
+def backward(a=None, off=FAR[0], batch=2, rows=10, q=FAR[1], sq=256, k=FAR[2], sk=128, v=FAR[3], sv=128, o=FAR[4], so=256, lse=FAR[5], do=FAR[6],
+             sdo=256, dq=FAR[7], sdq=256, dk=FAR[8], sdk=128, dv=FAR[9], sdv=128, ws=FAR[10], n=1 << 30):
+    return pb.lib().pac_attn_backward(C.byref(a or attn()), off, batch, rows, q, sq, k, sk, v, sv, o, so, lse, do, sdo, dq, sdq, dk, sdk, dv, sdv,
+                                      ws, n, None)
+
+
+@pytest.mark.parametrize("kw", [dict(heads=0), dict(heads=3), dict(kv_heads=0), dict(heads=4098, kv_heads=1), dict(d=0), dict(d=12), dict(d=136),
+                                dict(d=-8), dict(causal=2), dict(scale=0.0), dict(scale=-1.0), dict(scale=math.inf), dict(scale=math.nan)])
+def test_attention_structures_that_are_refused(kw):
+    assert forward(attn(**kw)) == backward(attn(**kw)) == pb.PAC_ERR_SHAPE
+    assert pb.pac_attn_workspace_bytes(attn(**kw), 2, 10) == -1
+
+
+def test_attention_calls_refuse():
+    for f in (forward, backward):
+        assert f(batch=0) == f(rows=0) == f(rows=0, q=None, k=None, v=None, o=None) == pb.PAC_OK
+        for name in ("off", "q", "k", "v", "o"):
+            assert f(**{name: None}) == pb.PAC_ERR_NULL, name
+            assert f(**{name: A + 2}) == pb.PAC_ERR_ALIGN, name
+        for name in ("sq", "sk", "sv", "so"):
+            assert f(**{name: 120}) == pb.PAC_ERR_RANGE and f(**{name: 260}) == pb.PAC_ERR_ALIGN and f(**{name: (1 << 24) + 8}) == pb.PAC_ERR_UNSUPPORTED
+        assert f(batch=-1) == pb.PAC_ERR_SHAPE and f(rows=-1) == f(rows=1 << 31) == pb.PAC_ERR_RANGE
+        assert f(lse=A + 2) == pb.PAC_ERR_ALIGN
+        assert f(batch=1 << 22) == f(rows=1 << 29, a=attn(64, 64)) == pb.PAC_ERR_UNSUPPORTED
+    L = pb.lib()
+    assert L.pac_attn_forward(None, *[FAR[0], 1, 1], *[FAR[1], 256] * 4, None, None) == pb.PAC_ERR_NULL
+    for name in ("lse", "do", "dq", "dk", "dv", "ws"):
+        assert backward(**{name: None}) == pb.PAC_ERR_NULL, name
+        assert backward(**{name: A + 2}) == pb.PAC_ERR_ALIGN, name
+    for name in ("sdo", "sdq", "sdk", "sdv"):
+        assert backward(**{name: 120}) == pb.PAC_ERR_RANGE, name
+    need = pb.pac_attn_workspace_bytes(attn(), 2, 10)
+    assert need > 0 and backward(n=need - 1) == pb.PAC_ERR_WORKSPACE
+
+
+def test_attention_results_that_share_memory_are_refused():
+    for other in (FAR[1], FAR[2], FAR[3], FAR[5], FAR[1] + 10 * 512 - 16):
+        assert forward(o=other) == pb.PAC_ERR_RANGE
+    assert forward(lse=FAR[1]) == forward(lse=FAR[0]) == pb.PAC_ERR_RANGE
+    for name in ("dq", "dk", "dv", "ws"):
+        for other in FAR[:10]:
+            own = dict(dq=FAR[7], dk=FAR[8], dv=FAR[9], ws=FAR[10])[name]
+            if other != own:
+                assert backward(**{name: other}) == pb.PAC_ERR_RANGE, (name, other)
+
+
+def test_a_workspace_for_many_rows_serves_fewer():
+    for a in (attn(), attn(64, 1, 128), attn(1, 1, 8), attn(32, 8, 96, 1)):
+        for many in (range(0, 300), range(0, 200000, 977)):
+            need = [pb.pac_attn_workspace_bytes(a, 3, r) for r in many]
+            assert need[0] >= 0 and need == sorted(need)
+        need = [pb.pac_attn_workspace_bytes(a, b, 1000) for b in range(0, 3000, 7)]
+        assert need == sorted(need)
+
+
+def kv4(at=A * 4, pages=10, page=16, kv_heads=2, d=64):
+    return pb.pac_kv4(at, pages, page, kv_heads, d)
+
+
+@pytest.mark.parametrize("kw", [dict(pages=-1), dict(pages=1 << 31), dict(page=0), dict(page=4), dict(page=24), dict(page=1 << 17), dict(kv_heads=0),
+                                dict(kv_heads=4097), dict(d=0), dict(d=4), dict(d=136), dict(d=-8)])
+def test_caches_that_are_refused(kw):
+    c = kv4(**kw)
+    L = pb.lib()
+    assert pb.pac_kv4_bytes(c) == -1 and pb.pac_kv4_attend_workspace_bytes(c, 2, 1, 1) == -1
+    for f in (L.pac_kv4_write, L.pac_kv4_read):
+        assert f(C.byref(c), 1, A, 2 * A, 1 << 20, 3 * A, 1 << 20, pb.PAC_F32, None) == pb.PAC_ERR_SHAPE
+    assert L.pac_kv4_attend(C.byref(c), 4096, 1.0, 1, A, 1, 1, A, A, 1 << 20, A, 1 << 20, A, 1 << 40, None) == pb.PAC_ERR_SHAPE
+
+
+def test_cache_sizes():
+    for d, blocks in ((8, 1), (32, 1), (40, 2), (64, 2), (72, 3), (96, 3), (104, 4), (128, 4)):
+        assert pb.pac_kv4_bytes(kv4(None, 10, 16, 3, d)) == 10 * 16 * 3 * 2 * blocks * 17
+    assert pb.pac_kv4_bytes(kv4(None, 0)) == 0
+    assert pb.pac_kv4_bytes(kv4(None, (1 << 31) - 1, 65536, 1, 128)) == ((1 << 31) - 1) * 65536 * 136
+
+
+def test_cache_conversions_refuse():
+    L = pb.lib()
+
+    def go(f, c=None, rows=4, slots=A, k=2 * A, sk=128, v=3 * A, sv=128, dt=pb.PAC_F32):
+        return f(C.byref(c or kv4()), rows, slots, k, sk, v, sv, dt, None)
+
+    for f in (L.pac_kv4_write, L.pac_kv4_read):
+        assert go(f, rows=0) == go(f, rows=0, slots=None, k=None, v=None) == pb.PAC_OK
+        assert f(None, 1, A, A, 128, A, 128, pb.PAC_F32, None) == pb.PAC_ERR_NULL
+        assert go(f, slots=None) == go(f, k=None) == go(f, v=None) == go(f, kv4(at=None)) == pb.PAC_ERR_NULL
+        assert go(f, dt=2) == pb.PAC_ERR_SHAPE
+        assert go(f, rows=-1) == go(f, sk=127) == go(f, sv=100) == pb.PAC_ERR_RANGE
+        assert go(f, kv4(at=4 * A + 8)) == go(f, slots=A + 4) == go(f, k=2 * A + 2) == go(f, v=3 * A + 1, dt=pb.PAC_BF16) == pb.PAC_ERR_ALIGN
+        assert go(f, rows=1 << 30) == go(f, rows=1 << 62) == pb.PAC_ERR_UNSUPPORTED
+        size = pb.pac_kv4_bytes(kv4())
+        assert go(f, k=4 * A) == go(f, v=4 * A + size - 4) == go(f, slots=4 * A + 16) == go(f, k=4 * A - 16) == pb.PAC_ERR_RANGE
+        assert go(f, kv4(at=None, pages=0)) == pb.PAC_OK
+    assert go(L.pac_kv4_read, v=2 * A) == go(L.pac_kv4_read, slots=2 * A + 16) == go(L.pac_kv4_read, slots=3 * A) == pb.PAC_ERR_RANGE
+
+
+def test_attending_refuses():
+    L = pb.lib()
+    big = 1 << 40
+
+    def go(c=None, heads=4, scale=0.125, batch=3, table=A, tl=5, ts=5, lens=2 * A, q=3 * A, sq=256, o=big, so=256, ws=2 * big, n=1 << 30):
+        return L.pac_kv4_attend(C.byref(c or kv4()), heads, scale, batch, table, tl, ts, lens, q, sq, o, so, ws, n, None)
+
+    assert go(batch=0) == go(batch=0, table=None, lens=None, q=None, o=None) == pb.PAC_OK
+    assert go(lens=None) == go(q=None) == go(o=None) == go(table=None) == go(kv4(at=None)) == pb.PAC_ERR_NULL
+    assert go(heads=0) == go(heads=3) == go(heads=8192) == go(batch=-1) == go(tl=-1) == pb.PAC_ERR_SHAPE
+    assert go(scale=0.0) == go(scale=-1.0) == go(scale=math.nan) == go(scale=math.inf) == pb.PAC_ERR_RANGE
+    assert go(sq=255) == go(so=8) == go(ts=4) == pb.PAC_ERR_RANGE
+    assert go(table=A + 2) == go(lens=2 * A + 1) == go(q=3 * A + 8) == go(o=big + 2) == go(sq=260) == go(so=260) == pb.PAC_ERR_ALIGN
+    assert go(kv4(page=65536), tl=1 << 15, ts=1 << 15) == go(batch=1 << 22) == pb.PAC_ERR_UNSUPPORTED
+    long = kv4(page=65536, pages=4)
+    need = pb.pac_kv4_attend_workspace_bytes(long, 4, 1, 4)
+    assert need > 0
+    assert go(long, batch=1, tl=4, n=100) == pb.PAC_ERR_WORKSPACE and go(long, batch=1, tl=4, ws=None) == pb.PAC_ERR_NULL
+    assert go(long, batch=1, tl=4, ws=2 * big + 8) == pb.PAC_ERR_ALIGN and go(long, batch=1, tl=4, ws=A) == pb.PAC_ERR_RANGE
+    assert go(o=3 * A) == go(o=A) == go(o=2 * A) == go(o=4 * A) == go(o=4 * A + pb.pac_kv4_bytes(kv4()) - 16) == pb.PAC_ERR_RANGE
+
+
+@pytest.mark.parametrize("heads,kv_heads,d,page", [(4, 2, 64, 16), (32, 8, 128, 64), (32, 1, 96, 8), (40, 40, 32, 1024)])
+def test_a_workspace_for_a_large_batch_serves_smaller_ones(heads, kv_heads, d, page):
+    c = kv4(kv_heads=kv_heads, d=d, page=page)
+    need = lambda b, t: pb.pac_kv4_attend_workspace_bytes(c, heads, b, t)  # noqa: E731
+    for t in (0, 1, 7, 100, 5000):
+        by = [need(b, t) for b in range(0, 400)]
+        assert by[0] >= 0 and by == sorted(by)
+    for b in (1, 3, 64):
+        by = [need(b, t) for t in range(0, 3000, 13)]
+        assert by == sorted(by)
