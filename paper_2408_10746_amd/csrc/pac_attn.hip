@@ -72,6 +72,54 @@ template <int D> struct AttnTile {
     static __device__ __forceinline__ int at(int row, int piece) { return row * RB + ((piece ^ swz(row)) << 4); }
 };
 
+// A tile of ROWS rows on its way from memory straight to LDS, 16 bytes a lane, a wavefront's 1 KB in a row; the swizzle is in which
+// piece a lane fetches.  Rows past `have` and pieces past d are not fetched: their places keep what they held (AttnDma::clear).
+// ROWS / WAVES rows a wavefront; offsets of a row's lanes stay under 2^32 bytes (strides up to 2^24).
+template <int D, int ROWS, int WAVES = 4> struct AttnDma {
+    using T = AttnTile<D>;
+    static constexpr int RPI = 1024 / T::RB, N = ROWS / RPI / WAVES; // rows of a transfer, transfers of a wavefront
+    static_assert(N * RPI * WAVES == ROWS, "whole transfers");
+    uint32_t off[N];
+    int row, piece[N];
+    __device__ __forceinline__ void plan(int64_t stride, int d)
+    {
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        constexpr int P = T::RB / 16;
+        row = wave * (N * RPI) + lane / P;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            piece[i] = (lane % P) ^ T::swz(row + i * RPI);
+            off[i] = (uint32_t)(row + i * RPI) * (uint32_t)(stride * 2) + (uint32_t)piece[i] * 16u;
+            piece[i] = piece[i] * 8 < d;
+        }
+    }
+    __device__ __forceinline__ static void one(const bf16_t *base, uint32_t off, uint32_t lds)
+    {
+        // one wait state between the write of M0 and the transfer that reads it; the compiler does not know of the transfer and so does
+        // not wait for it at every LDS read: the kernels do, before the barrier that hands a tile over
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(off), "s"(base) : "memory", "m0");
+    }
+    // base: the tile's first row (the same for all lanes)
+    __device__ __forceinline__ void issue(const bf16_t *base, uint32_t lds, int have, bool whole) const
+    {
+        const uint32_t to = __builtin_amdgcn_readfirstlane(lds + (threadIdx.x >> 6) * (N * 1024));
+        if (whole && have >= ROWS) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) one(base, off[i], to + i * 1024);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (row + i * RPI < have && piece[i]) one(base, off[i], to + i * 1024);
+        }
+    }
+};
+// Zeros in all of a workgroup's tiles, before the first transfer, where some places are never fetched
+template <int BYTES> __device__ __forceinline__ void clear_tiles(char *lds)
+{
+    for (int i = threadIdx.x * 16; i < BYTES; i += blockDim.x * 16) *reinterpret_cast<u32x4 *>(lds + i) = u32x4{0, 0, 0, 0};
+    __syncthreads();
+}
+
 // A tile of ROWS rows on its way from memory to LDS through registers; rows past `have` and values past d are zeros.
 template <int D, int ROWS> struct AttnFetch {
     using T = AttnTile<D>;
@@ -96,20 +144,36 @@ template <int D, int ROWS> struct AttnFetch {
     }
 };
 
-// Operands of 32x32x16 products.  "Along": lane (i = lane % 32, h = lane / 32) holds row row0 + i, values 16 ks + 8 h ..+7.
-template <int D> __device__ __forceinline__ bf16x8 along(const char *lds, int row0, int ks)
-{
-    const int lane = threadIdx.x & 63;
-    return *reinterpret_cast<const bf16x8 *>(lds + AttnTile<D>::at(row0 + (lane & 31), 2 * ks + (lane >> 5)));
-}
+// Operands of 32x32x16 products from a tile at LDS address `tile` (a multiple of 1024).
+// "Along": lane (i = lane % 32, h = lane / 32) holds row row0 + i, values 16 ks + 8 h ..+7.
 // "Turned": lane (i, h) holds value 32 t + i of the rows row0 + 16 j + {4 h ..+3, 8 + 4 h ..+3}, which are the rows of the registers
 // 8 j ..+7 of a 32 x 32 result in the same lane: a result enters the next product as it is.
-template <int D> __device__ __forceinline__ bf16x8 turned(const char *lds, int row0, int j, int t)
-{
-    const int lane = threadIdx.x & 63, p = lane & 15, h = lane >> 5;
-    const int row = row0 + 16 * j + 4 * h + (p >> 2), piece = 4 * t + 2 * (lane >> 4 & 1) + (p >> 1 & 1), in = 8 * (p & 1);
-    return tr_read2(lds + AttnTile<D>::at(row, piece) + in, lds + AttnTile<D>::at(row + 8, piece) + in);
-}
+// What varies from read to read is an exclusive or with a constant (ks, t, the second four rows) and a constant distance, so that a lane
+// keeps one address for each of the two ways.
+typedef const __attribute__((address_space(3))) u32x4 *lds_u32x4;
+template <int D> struct AttnLane {
+    using T = AttnTile<D>;
+    uint32_t a, t;
+    __device__ __forceinline__ explicit AttnLane(uint32_t tile)
+    {
+        const int lane = threadIdx.x & 63, p = lane & 15, h = lane >> 5;
+        a = tile + T::at(lane & 31, h);
+        t = tile + T::at(4 * h + (p >> 2), 2 * (lane >> 4 & 1) + (p >> 1 & 1)) + 8 * (p & 1);
+    }
+    __device__ __forceinline__ bf16x8 along(int row0, int ks) const
+    {
+        return __builtin_bit_cast(bf16x8, *reinterpret_cast<lds_u32x4>((a ^ (uint32_t)(ks << 5)) + (uint32_t)(row0 * T::RB)));
+    }
+    __device__ __forceinline__ bf16x8 turned(int row0, int j, int t_) const
+    {
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        typedef short s16x8 __attribute__((ext_vector_type(8)));
+        const uint32_t lo = (t ^ (uint32_t)(t_ << 6)) + (uint32_t)((row0 + 16 * j) * T::RB), hi = (t ^ (uint32_t)(t_ << 6 | 32)) + (uint32_t)((row0 + 16 * j + 8) * T::RB);
+        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) s16x4 *>(lo));
+        const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) s16x4 *>(hi));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+};
 // The same of a matrix in memory: row i of 32 (zeros past `have`, and past d)
 __device__ __forceinline__ bf16x8 along_mem(const bf16_t *base, int64_t stride, int have, int d, int ks)
 {
@@ -135,34 +199,63 @@ __device__ __forceinline__ bf16x8 rounded(const f32x16 &s, int j)
     return r;
 }
 
-// acc[t] += (turned tile)^T p over 32 rows of the tile, p in the registers of a 32 x 32 result.
-template <int D> __device__ __forceinline__ void add_turned(f32x16 (&acc)[D / 32], const char *lds, int row0, const bf16x8 (&p)[2])
+// Reads run a few operands ahead of the products and no further, because a kernel's registers are spoken for.
+#define PAC_ATTN_PACE __builtin_amdgcn_sched_barrier(0x6) /* only vector and scalar arithmetic moves across */
+
+// s[x] = (rows row0 + 32 x ..+31 of the tile) q^T
+template <int D, int NS> __device__ __forceinline__ void scores(f32x16 (&s)[NS], const AttnLane<D> &l, int row0, const bf16x8 (&q)[D / 16])
 {
+    constexpr int N = NS * D / 16, AHEAD = 4;
+    bf16x8 f[AHEAD];
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int n = 0; n < AHEAD - 1; ++n) f[n] = l.along(row0 + 32 * (n % NS), n / NS);
 #pragma unroll
-        for (int t = 0; t < D / 32; ++t) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(turned<D>(lds, row0, j, t), p[j], acc[t], 0, 0, 0);
+    for (int x = 0; x < NS; ++x) s[x] = zeros16();
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        constexpr int K = AHEAD - 1;
+        if (n + K < N) f[(n + K) % AHEAD] = l.along(row0 + 32 * ((n + K) % NS), (n + K) / NS);
+        s[n % NS] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[n % AHEAD], q[n / NS], s[n % NS], 0, 0, 0);
+        PAC_ATTN_PACE;
+    }
+}
+// acc[t] += (turned tile)^T p over 32 rows of the tile, p in the registers of a 32 x 32 result.
+template <int D> __device__ __forceinline__ void add_turned(f32x16 (&acc)[D / 32], const AttnLane<D> &l, int row0, const bf16x8 (&p)[2])
+{
+    constexpr int N = 2 * D / 32, AHEAD = N < 4 ? N : 4;
+    bf16x8 f[AHEAD];
+#pragma unroll
+    for (int n = 0; n < AHEAD - 1; ++n) f[n] = l.turned(row0, n / (D / 32), n % (D / 32));
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        constexpr int K = AHEAD - 1;
+        if (n + K < N) f[(n + K) % AHEAD] = l.turned(row0, (n + K) / (D / 32), (n + K) % (D / 32));
+        acc[n % (D / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[n % AHEAD], p[n / (D / 32)], acc[n % (D / 32)], 0, 0, 0);
+        PAC_ATTN_PACE;
+    }
 }
 // Do 32 rows of a tile hold an infinity or NaN?
-template <int D> __device__ __forceinline__ bool any_special(const char *lds, int row0)
+template <int D> __device__ __forceinline__ bool any_special(const AttnLane<D> &l, int row0)
 {
     uint32_t bad = 0;
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) {
-        const u32x4 w = __builtin_bit_cast(u32x4, along<D>(lds, row0, ks));
+        const u32x4 w = __builtin_bit_cast(u32x4, l.along(row0, ks));
 #pragma unroll
         for (int e = 0; e < 4; ++e) bad |= ((w[e] & 0x7f80u) == 0x7f80u) | ((w[e] & 0x7f800000u) == 0x7f800000u);
     }
     return __any(bad != 0);
 }
-// add_turned where row x of the tile takes part in column c of the result only if part(x, c): a matrix instruction would multiply an
-// infinity or NaN of a row that is masked by 0.  Row by row in the vector units, for the tiles on the diagonal that hold such values.
+// add_turned where row x of 32 takes part in column c of the result only if part(x, c): a matrix instruction would multiply an infinity or
+// NaN of a row that is masked by 0.  Row by row in the vector units, with the rows from memory, for the tiles at a mask's border that hold
+// such values; rows past `have` take no part.
 template <int D, class Part>
-__device__ __forceinline__ void add_turned_apart(f32x16 (&acc)[D / 32], const char *lds, int row0, const bf16x8 (&p)[2], const Part &part)
+__device__ __forceinline__ void add_turned_apart(f32x16 (&acc)[D / 32], const bf16_t *base, int64_t stride, int have, int d, const bf16x8 (&p)[2],
+                                                 const Part &part)
 {
     const int lane = threadIdx.x & 63, h = lane >> 5;
 #pragma unroll 1
-    for (int x = 0; x < 32; ++x) {
+    for (int x = 0; x < min(have, 32); ++x) {
         const int reg = (x >> 3) * 4 + (x & 3); // row_of, the other way round
         float px = 0.f;
 #pragma unroll
@@ -173,8 +266,9 @@ __device__ __forceinline__ void add_turned_apart(f32x16 (&acc)[D / 32], const ch
             for (int t = 0; t < D / 32; ++t)
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
+                    if (32 * t + 8 * g >= d) continue;
                     __builtin_amdgcn_sched_barrier(0); // few registers at a time: the kernels need theirs
-                    const bf16x4 w = *reinterpret_cast<const bf16x4 *>(lds + AttnTile<D>::at(row0 + x, 4 * t + g) + 8 * h);
+                    const bf16x4 w = *reinterpret_cast<const bf16x4 *>(base + x * stride + 32 * t + 8 * g + 4 * h);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) acc[t][4 * g + e] = fmaf((float)w[e], px, acc[t][4 * g + e]);
                 }
@@ -199,95 +293,144 @@ template <int D> __device__ __forceinline__ void put_rows(bf16_t *base, int64_t 
         }
 }
 
-// Tile and head of a workgroup: heads vary fastest.
+// Tile and head of a workgroup.  Heads vary fastest; workgroups go to the eight dies in turn, so that where their number allows it a
+// die has neighbouring heads, which share keys and values, in its L2.  Later tiles go first: with causal they take longest.
 struct AttnWork {
     int head, vt;
 };
-__device__ __forceinline__ AttnWork attn_work(unsigned heads) { return AttnWork{(int)(blockIdx.x % heads), (int)(blockIdx.x / heads)}; }
+__device__ __forceinline__ AttnWork attn_work(unsigned heads, unsigned tiles, bool last_first)
+{
+    const unsigned i = blockIdx.x % heads, vt = blockIdx.x / heads;
+    return AttnWork{(int)(heads % 8 == 0 ? (i % 8) * (heads / 8) + i / 8 : i), (int)(last_first ? tiles - 1 - vt : vt)};
+}
 
 // ---------------------------------------------------------------------------
-// forward: 128 rows a workgroup, 32 a wavefront, which holds its queries and o in registers; 64 keys and values at a time in LDS.
-// S^T = K q^T has a query's scores in one column, so that maximum, sum and rescaling stay in a lane, and p in place as the operand
-// of o^T = V^T p^T.
+// forward: 128 rows a workgroup, 32 a wavefront, which holds its queries and o in registers; 64 keys and values at a time in LDS, the
+// next ones on their way.  S^T = K q^T has a query's scores in one column, so that maximum, sum and rescaling stay in a lane, and p in
+// place as the operand of o^T = V^T p^T.
 // ---------------------------------------------------------------------------
+template <int D> struct AttnRow { // a wavefront's 32 rows on their way
+    f32x16 acc[D / 32];
+    float top, sum; // scores are taken relative to `top`, which stays within 2^8 of the largest so far
+
+    // `most` is the largest of the scores at hand, in units of log 2
+    __device__ __forceinline__ void raise(float most)
+    {
+        if (__any(most > top + 8.f)) {
+            // each row for itself: what its neighbours' scores are changes no bit of it
+            most = fmaxf(most, __shfl_xor(most, 32, 64));
+            const float next = most > top + 8.f ? most : top, by = __builtin_amdgcn_exp2f(top - next);
+            top = next;
+            sum *= by;
+#pragma unroll
+            for (int t = 0; t < D / 32; ++t) acc[t] *= by;
+        }
+    }
+    __device__ __forceinline__ void weigh(f32x16 &s, float c2)
+    {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c2, -top));
+            sum += s[i];
+        }
+    }
+};
+__device__ __forceinline__ float largest(const f32x16 &s)
+{
+    float most = fmaxf(s[0], s[1]);
+#pragma unroll
+    for (int i = 2; i < 16; i += 2) most = fmaxf(fmaxf(most, s[i]), s[i + 1]);
+    return most;
+}
+
 template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_fwd(const AttnArgs a)
 {
     using T = AttnTile<D>;
-    constexpr int BM = 128, BK = 64;
-    __shared__ __attribute__((aligned(16))) char lds[2 * BK * T::RB];
-    char *lk = lds, *lv = lds + BK * T::RB;
+    constexpr int BM = 128, BK = 64, TILE = BK * T::RB;
+    __shared__ __attribute__((aligned(1024))) char lds[4 * TILE]; // keys, values, keys, values
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const AttnWork w = attn_work(a.heads);
+    const AttnWork w = attn_work(a.heads, a.tiles, CAUSAL);
     const AttnSeq seq = attn_seq<BM>(a, w.vt);
     if (seq.len < 1) return;
     const int head = w.head, hk = head / a.group;
     const int q0 = seq.tile * BM + wave * 32, have = min(32, seq.len - q0);
     const bf16_t *kp = a.k + (int64_t)seq.start * a.ks + (int64_t)hk * a.d, *vp = a.v + (int64_t)seq.start * a.vs + (int64_t)hk * a.d;
     const int keys = CAUSAL ? min(seq.len, seq.tile * BM + BM) : seq.len;
+    const uint32_t at = lds_address(lds);
+    const bool whole = a.d == D;
 
-    AttnFetch<D, BK> fk, fv;
-    fk.load(kp, a.ks, keys, a.d);
-    fv.load(vp, a.vs, keys, a.d);
+    AttnDma<D, BK> fk, fv;
+    fk.plan(a.ks, a.d);
+    fv.plan(a.vs, a.d);
+    if (!whole || keys < 2 * BK) clear_tiles<4 * TILE>(lds);
+    fk.issue(kp, at, keys, whole);
+    fv.issue(vp, at + TILE, keys, whole);
     bf16x8 q[D / 16];
     const bf16_t *qp = a.q + (int64_t)(seq.start + q0) * a.qs + (int64_t)head * a.d;
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) q[ks] = along_mem(qp, a.qs, have, a.d, ks);
-    f32x16 acc[D / 32];
+    AttnRow<D> r;
 #pragma unroll
-    for (int t = 0; t < D / 32; ++t) acc[t] = zeros16();
-    float top = -FLT_MAX, sum = 0.f; // scores are taken relative to `top`, which stays within 2^8 of the largest so far
+    for (int t = 0; t < D / 32; ++t) r.acc[t] = zeros16();
+    r.top = -FLT_MAX;
+    r.sum = 0.f;
+    // keys from `border` on are masked in part; the last of 32 that a query sees; their p where it has to wait for the end
+    const int border = CAUSAL ? q0 : seq.len & ~31, last = CAUSAL ? lane & 31 : seq.len - 1 - border;
+    bf16x8 late[2];
+    bool apart = false;
 
-    for (int k0 = 0; k0 < keys; k0 += BK) {
-        __syncthreads();
-        fk.store(lk);
-        fv.store(lv);
-        __syncthreads();
+    for (int k0 = 0, turn = 0; k0 < keys; k0 += BK, turn ^= 1) {
+        wait_vm<0>();
+        __syncthreads(); // everybody's share of this tile is there, and the other one is free
+        const uint32_t tk = at + turn * (2 * TILE), tv = tk + TILE;
         if (k0 + BK < keys) {
-            fk.load(kp + (int64_t)(k0 + BK) * a.ks, a.ks, keys - k0 - BK, a.d);
-            fv.load(vp + (int64_t)(k0 + BK) * a.vs, a.vs, keys - k0 - BK, a.d);
+            const uint32_t to = at + (turn ^ 1) * (2 * TILE);
+            fk.issue(kp + (int64_t)(k0 + BK) * a.ks, to, keys - k0 - BK, whole);
+            fv.issue(vp + (int64_t)(k0 + BK) * a.vs, to + TILE, keys - k0 - BK, whole);
         }
+        if (have < 1) continue;
+        const AttnLane<D> lk(tk), lv(tv);
+        if (k0 + BK <= (CAUSAL ? q0 : seq.len)) {
+            f32x16 s[2];
+            scores<D, 2>(s, lk, 0, q);
+            r.raise(fmaxf(largest(s[0]), largest(s[1])) * a.c2);
+            r.weigh(s[0], a.c2);
+            const bf16x8 p0[2] = {rounded(s[0], 0), rounded(s[0], 1)};
+            add_turned<D>(r.acc, lv, 0, p0);
+            r.weigh(s[1], a.c2);
+            const bf16x8 p1[2] = {rounded(s[1], 0), rounded(s[1], 1)};
+            add_turned<D>(r.acc, lv, 32, p1);
+        } else {
+#pragma unroll 1
+            for (int sub = 0; sub < BK; sub += 32) {
+                const int key0 = k0 + sub;
+                if (key0 >= keys || (CAUSAL && key0 > q0)) break;
+                f32x16 s1[1];
+                scores<D, 1>(s1, lk, sub, q);
+                f32x16 &s = s1[0];
+                const bool cut = key0 == border;
+                if (cut) {
 #pragma unroll
-        for (int sub = 0; sub < BK; sub += 32) {
-            const int key0 = k0 + sub;
-            if (key0 >= keys || have < 1 || (CAUSAL && key0 > q0)) continue; // the whole wavefront
-            f32x16 s = zeros16();
-#pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(along<D>(lk, sub, ks), q[ks], s, 0, 0, 0);
-            const bool diagonal = CAUSAL && key0 == q0;
-            if (diagonal) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = row_of(i) <= (lane & 31) ? s[i] : -INFINITY;
-            } else if (key0 + 32 > seq.len) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = key0 + row_of(i) < seq.len ? s[i] : -INFINITY;
+                    for (int i = 0; i < 16; ++i) s[i] = row_of(i) <= last ? s[i] : -INFINITY;
+                }
+                r.raise(largest(s) * a.c2);
+                r.weigh(s, a.c2);
+                const bf16x8 p[2] = {rounded(s, 0), rounded(s, 1)};
+                if (cut && any_special<D>(lv, sub)) {
+                    apart = true;
+                    late[0] = p[0];
+                    late[1] = p[1];
+                } else {
+                    add_turned<D>(r.acc, lv, sub, p);
+                }
             }
-            float most = s[0];
-#pragma unroll
-            for (int i = 1; i < 16; ++i) most = fmaxf(most, s[i]);
-            most *= a.c2;
-            if (__any(most > top + 8.f)) {
-                // each row for itself: what its neighbours' scores are changes no bit of it
-                most = fmaxf(most, __shfl_xor(most, 32, 64));
-                const float next = most > top + 8.f ? most : top, by = __builtin_amdgcn_exp2f(top - next);
-                top = next;
-                sum *= by;
-#pragma unroll
-                for (int t = 0; t < D / 32; ++t) acc[t] *= by;
-            }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.c2, -top));
-                sum += s[i];
-            }
-            const bf16x8 p[2] = {rounded(s, 0), rounded(s, 1)};
-            if (diagonal && any_special<D>(lv, sub)) add_turned_apart<D>(acc, lv, sub, p, [](int key, int query) { return key <= query; });
-            else add_turned<D>(acc, lv, sub, p);
         }
     }
     if (have < 1) return;
-    sum += __shfl_xor(sum, 32, 64);
-    put_rows<D>(a.out + (int64_t)(seq.start + q0) * a.os + (int64_t)head * a.d, a.os, have, a.d, acc, 1.f / sum);
-    if (a.lse && lane < have) a.lse[(int64_t)head * a.rows + seq.start + q0 + lane] = (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+    if (apart) add_turned_apart<D>(r.acc, vp + (int64_t)border * a.vs, a.vs, seq.len - border, a.d, late, [&](int key, int) { return key <= last; });
+    const float sum = r.sum + __shfl_xor(r.sum, 32, 64);
+    put_rows<D>(a.out + (int64_t)(seq.start + q0) * a.os + (int64_t)head * a.d, a.os, have, a.d, r.acc, 1.f / sum);
+    if (a.lse && lane < have) a.lse[(int64_t)head * a.rows + seq.start + q0 + lane] = (r.top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
 }
 
 // ---------------------------------------------------------------------------
@@ -299,10 +442,12 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_d
 {
     using T = AttnTile<D>;
     constexpr int BM = 128, BK = 64;
-    __shared__ __attribute__((aligned(16))) char lds[2 * BK * T::RB];
-    char *lk = lds, *lv = lds + BK * T::RB;
+    __shared__ __attribute__((aligned(1024))) char lds[2 * BK * T::RB];
+    char *const lk = lds, *const lv = lds + BK * T::RB;
+    const uint32_t tk = lds_address(lk);
+    const AttnLane<D> ak(tk), av(lds_address(lv));
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const AttnWork w = attn_work(a.heads);
+    const AttnWork w = attn_work(a.heads, a.tiles, CAUSAL);
     const AttnSeq seq = attn_seq<BM>(a, w.vt);
     if (seq.len < 1) return;
     const int head = w.head, hk = head / a.group;
@@ -351,8 +496,8 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_d
             f32x16 s = zeros16(), dp = zeros16();
 #pragma unroll
             for (int ks = 0; ks < D / 16; ++ks) {
-                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(along<D>(lk, sub, ks), q[ks], s, 0, 0, 0);
-                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(along<D>(lv, sub, ks), d_o[ks], dp, 0, 0, 0);
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ak.along(sub, ks), q[ks], s, 0, 0, 0);
+                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av.along(sub, ks), d_o[ks], dp, 0, 0, 0);
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.c2, -lse2)) * (dp[i] - delta);
@@ -365,8 +510,8 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_d
                 for (int i = 0; i < 16; ++i) s[i] = key0 + row_of(i) < seq.len ? s[i] : 0.f;
             }
             const bf16x8 p[2] = {rounded(s, 0), rounded(s, 1)};
-            if (diagonal && any_special<D>(lk, sub)) add_turned_apart<D>(acc, lk, sub, p, [](int key, int query) { return key <= query; });
-            else add_turned<D>(acc, lk, sub, p);
+            if (diagonal && any_special<D>(ak, sub)) add_turned_apart<D>(acc, kp + (int64_t)key0 * a.ks, a.ks, seq.len - key0, a.d, p, [](int key, int query) { return key <= query; });
+            else add_turned<D>(acc, ak, sub, p);
         }
     }
     if (have < 1) return;
@@ -381,11 +526,13 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 1) void k_attn_d
 {
     using T = AttnTile<D>;
     constexpr int BN = 128, BQ = 32;
-    __shared__ __attribute__((aligned(16))) char lds[2 * BQ * T::RB];
+    __shared__ __attribute__((aligned(1024))) char lds[2 * BQ * T::RB];
     __shared__ __attribute__((aligned(16))) float stat[2][BQ]; // lse log2(e) and delta of the rows
-    char *lq = lds, *ld = lds + BQ * T::RB;
+    char *const lq = lds, *const ld = lds + BQ * T::RB;
+    const uint32_t tq = lds_address(lq), td = lds_address(ld);
+    const AttnLane<D> aq(tq), ad(td);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const AttnWork w = attn_work(a.kv_heads);
+    const AttnWork w = attn_work(a.kv_heads, a.tiles, false);
     const AttnSeq seq = attn_seq<BN>(a, w.vt);
     if (seq.len < 1) return;
     const int hk = w.head, key0 = seq.tile * BN + wave * 32, have = min(32, seq.len - key0);
@@ -429,8 +576,8 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 1) void k_attn_d
         f32x16 s = zeros16(), dp = zeros16();
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks) {
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(along<D>(lq, 0, ks), k[ks], s, 0, 0, 0);
-            dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(along<D>(ld, 0, ks), v[ks], dp, 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(aq.along(0, ks), k[ks], s, 0, 0, 0);
+            dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ad.along(0, ks), v[ks], dp, 0, 0, 0);
         }
         const bool diagonal = CAUSAL && q0 == key0;
 #pragma unroll
@@ -453,13 +600,14 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 1) void k_attn_d
             }
         }
         const bf16x8 p[2] = {rounded(s, 0), rounded(s, 1)}, ds[2] = {rounded(dp, 0), rounded(dp, 1)};
-        if (diagonal && (any_special<D>(ld, 0) || any_special<D>(lq, 0))) {
+        if (diagonal && (any_special<D>(ad, 0) || any_special<D>(aq, 0))) {
             auto part = [](int query, int key) { return key <= query; };
-            add_turned_apart<D>(dv, ld, 0, p, part);
-            add_turned_apart<D>(dk, lq, 0, ds, part);
+            const int64_t r0 = seq.start + q0, c0 = (int64_t)(hk * a.group + n / steps) * a.d;
+            add_turned_apart<D>(dv, a.d_o + r0 * a.dos + c0, a.dos, seq.len - q0, a.d, p, part);
+            add_turned_apart<D>(dk, a.q + r0 * a.qs + c0, a.qs, seq.len - q0, a.d, ds, part);
         } else {
-            add_turned<D>(dv, ld, 0, p);
-            add_turned<D>(dk, lq, 0, ds);
+            add_turned<D>(dv, ad, 0, p);
+            add_turned<D>(dk, aq, 0, ds);
         }
     }
     if (have < 1) return;
