@@ -18,7 +18,7 @@ struct AttnArgs {
     float *lse;  // [heads][rows]
     bf16_t *dq, *dk, *dv;
     int64_t dqs, dks, dvs;
-    float *delta; // [heads][rows]
+    float *nlse2, *delta; // [heads][rows] each: -lse log2(e), do . o
     unsigned tiles; // tiles of a head, of all sequences together
 };
 
@@ -73,76 +73,54 @@ template <int D> struct AttnTile {
 };
 
 // A tile of ROWS rows on its way from memory straight to LDS, 16 bytes a lane, a wavefront's 1 KB in a row; the swizzle is in which
-// piece a lane fetches.  Rows past `have` and pieces past d are not fetched: their places keep what they held (AttnDma::clear).
-// ROWS / WAVES rows a wavefront; offsets of a row's lanes stay under 2^32 bytes (strides up to 2^24).
-template <int D, int ROWS, int WAVES = 4> struct AttnDma {
+// piece a lane fetches.  Rows past `have` repeat the last one, so that a wavefront always has N transfers under way; the kernels mask
+// them.  Pieces past d are not fetched: their places keep the zeros of clear_tiles.  (Offsets stay under 2^32 bytes for strides up to 2^24.)
+template <int D, int ROWS> struct AttnDma {
     using T = AttnTile<D>;
-    static constexpr int RPI = 1024 / T::RB, N = ROWS / RPI / WAVES; // rows of a transfer, transfers of a wavefront
-    static_assert(N * RPI * WAVES == ROWS, "whole transfers");
-    uint32_t off[N];
-    int row, piece[N];
+    static constexpr int WAVES = 4, P = T::RB / 16, RPI = 64 / P;                           // pieces of a row, rows of a transfer
+    static constexpr int TOTAL = ROWS / RPI, N = TOTAL / WAVES > 0 ? TOTAL / WAVES : 1; // (few rows: wavefronts repeat one another's transfers)
+    uint32_t stride2, off[N];
+    int row, to, dd; // dd: values of a row that are fetched
     __device__ __forceinline__ void plan(int64_t stride, int d)
     {
-        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        constexpr int P = T::RB / 16;
-        row = wave * (N * RPI) + lane / P;
+        const int lane = threadIdx.x & 63, first = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * N % TOTAL;
+        row = first * RPI + lane / P;
+        to = first * 1024;
+        stride2 = (uint32_t)(stride * 2);
+        // (rows of a transfer begin at a multiple of RPI; the swizzle's period is 16 rows)
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            piece[i] = (lane % P) ^ T::swz(row + i * RPI);
-            off[i] = (uint32_t)(row + i * RPI) * (uint32_t)(stride * 2) + (uint32_t)piece[i] * 16u;
-            piece[i] = piece[i] * 8 < d;
-        }
+        for (int i = 0; i < N; ++i) off[i] = (uint32_t)(row + i * RPI) * stride2 + piece(i) * 16u;
+        dd = d;
     }
+    __device__ __forceinline__ uint32_t piece(int i) const { return (uint32_t)((threadIdx.x & 63) % P ^ T::swz(row + i * RPI)); }
     __device__ __forceinline__ static void one(const bf16_t *base, uint32_t off, uint32_t lds)
     {
         // one wait state between the write of M0 and the transfer that reads it; the compiler does not know of the transfer and so does
         // not wait for it at every LDS read: the kernels do, before the barrier that hands a tile over
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(off), "s"(base) : "memory", "m0");
     }
-    // base: the tile's first row (the same for all lanes)
-    __device__ __forceinline__ void issue(const bf16_t *base, uint32_t lds, int have, bool whole) const
+    // base: the tile's first row, the same for all lanes, as `lds` is
+    __device__ __forceinline__ void issue(const bf16_t *base, uint32_t lds, int have) const
     {
-        const uint32_t to = __builtin_amdgcn_readfirstlane(lds + (threadIdx.x >> 6) * (N * 1024));
-        if (whole && have >= ROWS) {
+        const uint32_t at = __builtin_amdgcn_readfirstlane(lds + to);
+        if (dd == D && have >= ROWS) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) one(base, off[i], to + i * 1024);
+            for (int i = 0; i < N; ++i) one(base, off[i], at + i * 1024);
         } else {
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (row + i * RPI < have && piece[i]) one(base, off[i], to + i * 1024);
+            for (int i = 0; i < N; ++i) {
+                const uint32_t c = piece(i);
+                if ((int)c * 8 < dd) one(base, (uint32_t)min(row + i * RPI, have - 1) * stride2 + c * 16u, at + i * 1024);
+            }
         }
     }
 };
-// Zeros in all of a workgroup's tiles, before the first transfer, where some places are never fetched
+// Zeros in all of a workgroup's tiles, before the first transfer, where some pieces are never fetched
 template <int BYTES> __device__ __forceinline__ void clear_tiles(char *lds)
 {
     for (int i = threadIdx.x * 16; i < BYTES; i += blockDim.x * 16) *reinterpret_cast<u32x4 *>(lds + i) = u32x4{0, 0, 0, 0};
     __syncthreads();
 }
-
-// A tile of ROWS rows on its way from memory to LDS through registers; rows past `have` and values past d are zeros.
-template <int D, int ROWS> struct AttnFetch {
-    using T = AttnTile<D>;
-    static constexpr int N = (ROWS * T::CH + 255) / 256;
-    u32x4 r[N];
-    __device__ __forceinline__ void load(const bf16_t *base, int64_t stride, int have, int d)
-    {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int id = i * 256 + threadIdx.x, row = id / T::CH, piece = id % T::CH;
-            r[i] = u32x4{0, 0, 0, 0};
-            if (row < min(have, ROWS) && piece * 8 < d) r[i] = *reinterpret_cast<const u32x4 *>(base + row * stride + piece * 8);
-        }
-    }
-    __device__ __forceinline__ void store(char *lds) const
-    {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int id = i * 256 + threadIdx.x, row = id / T::CH, piece = id % T::CH;
-            if (ROWS * T::CH % 256 == 0 || row < ROWS) *reinterpret_cast<u32x4 *>(lds + T::at(row, piece)) = r[i];
-        }
-    }
-};
 
 // Operands of 32x32x16 products from a tile at LDS address `tile` (a multiple of 1024).
 // "Along": lane (i = lane % 32, h = lane / 32) holds row row0 + i, values 16 ks + 8 h ..+7.
@@ -357,14 +335,13 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_f
     const bf16_t *kp = a.k + (int64_t)seq.start * a.ks + (int64_t)hk * a.d, *vp = a.v + (int64_t)seq.start * a.vs + (int64_t)hk * a.d;
     const int keys = CAUSAL ? min(seq.len, seq.tile * BM + BM) : seq.len;
     const uint32_t at = lds_address(lds);
-    const bool whole = a.d == D;
 
     AttnDma<D, BK> fk, fv;
     fk.plan(a.ks, a.d);
     fv.plan(a.vs, a.d);
-    if (!whole || keys < 2 * BK) clear_tiles<4 * TILE>(lds);
-    fk.issue(kp, at, keys, whole);
-    fv.issue(vp, at + TILE, keys, whole);
+    if (a.d != D) clear_tiles<4 * TILE>(lds);
+    fk.issue(kp, at, keys);
+    fv.issue(vp, at + TILE, keys);
     bf16x8 q[D / 16];
     const bf16_t *qp = a.q + (int64_t)(seq.start + q0) * a.qs + (int64_t)head * a.d;
 #pragma unroll
@@ -385,8 +362,8 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_f
         const uint32_t tk = at + turn * (2 * TILE), tv = tk + TILE;
         if (k0 + BK < keys) {
             const uint32_t to = at + (turn ^ 1) * (2 * TILE);
-            fk.issue(kp + (int64_t)(k0 + BK) * a.ks, to, keys - k0 - BK, whole);
-            fv.issue(vp + (int64_t)(k0 + BK) * a.vs, to + TILE, keys - k0 - BK, whole);
+            fk.issue(kp + (int64_t)(k0 + BK) * a.ks, to, keys - k0 - BK);
+            fv.issue(vp + (int64_t)(k0 + BK) * a.vs, to + TILE, keys - k0 - BK);
         }
         if (have < 1) continue;
         const AttnLane<D> lk(tk), lv(tv);
@@ -434,181 +411,277 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_f
 }
 
 // ---------------------------------------------------------------------------
-// backward, dq: as the forward kernel, with p = exp(s - lse) known, and ds^T in place as the operand of dq^T = K^T ds^T.  delta comes
-// from the same product that makes do . v (the diagonal of do o^T), so that a row with one key has exactly no gradient in q and k; it
-// goes to memory for the other kernel.
+// backward.  Both kernels walk over subtiles of 32 x 32 pairs, whose rows come through a ring of four LDS slots: two products (scores,
+// do . v), 16 values of p and ds a lane, and the products that p and ds enter.  A wavefront has its SIMD to itself (its sums and operands
+// take more than half of the registers), so the vector work of a subtile is written between the matrix instructions of the products that
+// the one before it enters.
 // ---------------------------------------------------------------------------
-template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a)
+constexpr int kAttnRing = 4;
+
+// sn = (rows of the first tile) b1^T, dn = (rows of the second) b2^T
+template <int D>
+__device__ __forceinline__ void pair_products(f32x16 &sn, f32x16 &dn, const AttnLane<D> &l1, const AttnLane<D> &l2, const bf16x8 (&b1)[D / 16],
+                                              const bf16x8 (&b2)[D / 16])
+{
+    constexpr int N = D / 8, AHEAD = 4, K = AHEAD - 1;
+    bf16x8 f[AHEAD];
+#pragma unroll
+    for (int n = 0; n < K; ++n) f[n] = (n % 2 ? l2 : l1).along(0, n / 2);
+    sn = zeros16();
+    dn = zeros16();
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        if (n + K < N) f[(n + K) % AHEAD] = ((n + K) % 2 ? l2 : l1).along(0, (n + K) / 2);
+        if (n % 2) dn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[n % AHEAD], b2[n / 2], dn, 0, 0, 0);
+        else sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[n % AHEAD], b1[n / 2], sn, 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+// acc[t] += (first tile, turned)^T p,  more[t] += (second tile, turned)^T q, and element(i), i = 0..15, in between.  SAME: both are one tile.
+template <int D, bool SAME, class El>
+__device__ __forceinline__ void add_pair(f32x16 (&acc)[D / 32], f32x16 (&more)[D / 32], const AttnLane<D> &l1, const AttnLane<D> &l2, const bf16x8 (&p)[2],
+                                         const bf16x8 (&q)[2], const El &element)
+{
+    // product n: tile n % 2, 16 rows j, 32 values t; operand m = n, or n / 2 where both tiles are one
+    constexpr int T = D / 32, N = 4 * T, M = SAME ? N / 2 : N, AHEAD = 4, K = SAME ? 2 : 3;
+    bf16x8 f[AHEAD];
+    auto read = [&](int m) { return SAME ? l1.turned(0, m / T, m % T) : (m % 2 ? l2 : l1).turned(0, m / 2 / T, m / 2 % T); };
+#pragma unroll
+    for (int m = 0; m < K; ++m) f[m] = read(m);
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const int m = SAME ? n / 2 : n;
+        if ((!SAME || n % 2 == 0) && m + K < M) f[(m + K) % AHEAD] = read(m + K);
+        const bf16x8 &x = f[m % AHEAD];
+        if (n % 2) more[n / 2 % T] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[n / 2 / T], more[n / 2 % T], 0, 0, 0);
+        else acc[n / 2 % T] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, p[n / 2 / T], acc[n / 2 % T], 0, 0, 0);
+#pragma unroll
+        for (int i = n * 16 / N; i < (n + 1) * 16 / N; ++i) element(i);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// dq: 128 rows a workgroup, 32 a wavefront.
+//     dq_i = scale sum_j p_ij (dp_ij - delta_i) k_j
+// o is at hand in bf16 only, and delta' = do . bf16(o) would make dq twice as far off as all other roundings together.  With
+// r_i = sum_j p_ij (dp_ij - delta'_i), which is delta_i - delta'_i because p sums to 1, and y_i = sum_j p_ij k_j,
+//     dq_i = scale (sum_j p_ij (dp_ij - delta'_i) k_j - r_i y_i)
+// has the exact delta; r is small, so that p in bf16 is more than enough for y, whose products share their operand from LDS with dq's.
+// delta' + r goes to memory for the other kernel, with -lse log2(e).  delta' comes from the product that makes do . v too (the diagonal of
+// do o^T), so that a row with one key has exactly no gradient in q and k.
+// ---------------------------------------------------------------------------
+template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 1) void k_attn_dq(const AttnArgs a)
 {
     using T = AttnTile<D>;
-    constexpr int BM = 128, BK = 64;
-    __shared__ __attribute__((aligned(1024))) char lds[2 * BK * T::RB];
-    char *const lk = lds, *const lv = lds + BK * T::RB;
-    const uint32_t tk = lds_address(lk);
-    const AttnLane<D> ak(tk), av(lds_address(lv));
+    constexpr int BM = 128, TILE = 32 * T::RB > 1024 ? 32 * T::RB : 1024;
+    __shared__ __attribute__((aligned(1024))) char lds[kAttnRing * 2 * TILE]; // 32 keys and their values, four times
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const AttnWork w = attn_work(a.heads, a.tiles, CAUSAL);
     const AttnSeq seq = attn_seq<BM>(a, w.vt);
     if (seq.len < 1) return;
     const int head = w.head, hk = head / a.group;
-    const int q0 = seq.tile * BM + wave * 32, have = min(32, seq.len - q0), at = lane & 31;
+    const int q0 = seq.tile * BM + wave * 32, have = min(32, seq.len - q0), me = lane & 31;
     const bf16_t *kp = a.k + (int64_t)seq.start * a.ks + (int64_t)hk * a.d, *vp = a.v + (int64_t)seq.start * a.vs + (int64_t)hk * a.d;
-    const int keys = CAUSAL ? min(seq.len, seq.tile * BM + BM) : seq.len;
+    const int keys = CAUSAL ? min(seq.len, seq.tile * BM + BM) : seq.len, tiles = (keys + 31) / 32;
+    const int subs = have < 1 ? 0 : CAUSAL ? q0 / 32 + 1 : tiles; // of this wavefront
+    const uint32_t at = lds_address(lds);
 
-    AttnFetch<D, BK> fk, fv;
-    fk.load(kp, a.ks, keys, a.d);
-    fv.load(vp, a.vs, keys, a.d);
+    AttnDma<D, 32> fk, fv;
+    fk.plan(a.ks, a.d);
+    fv.plan(a.vs, a.d);
+    if (a.d != D) clear_tiles<kAttnRing * 2 * TILE>(lds);
+    auto slot = [&](int tile) { return at + (uint32_t)(tile % kAttnRing) * (2 * TILE); };
+    auto issue = [&](int tile) {
+        fk.issue(kp + (int64_t)tile * 32 * a.ks, slot(tile), keys - tile * 32);
+        fv.issue(vp + (int64_t)tile * 32 * a.vs, slot(tile) + TILE, keys - tile * 32);
+    };
     bf16x8 q[D / 16], d_o[D / 16];
     const int64_t row = seq.start + q0;
-    f32x16 own = zeros16();
+    f32x16 s = zeros16(), dp;
+    issue(0);
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) {
         q[ks] = along_mem(a.q + row * a.qs + (int64_t)head * a.d, a.qs, have, a.d, ks);
         d_o[ks] = along_mem(a.d_o + row * a.dos + (int64_t)head * a.d, a.dos, have, a.d, ks);
-        own = __builtin_amdgcn_mfma_f32_32x32x16_bf16(along_mem(a.o + row * a.os + (int64_t)head * a.d, a.os, have, a.d, ks), d_o[ks], own, 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(along_mem(a.o + row * a.os + (int64_t)head * a.d, a.os, have, a.d, ks), d_o[ks], s, 0, 0, 0);
     }
-    float delta = 0.f;
+    const float nlse2 = me < have ? a.lse[(int64_t)head * a.rows + row + me] * -1.4426950408889634f : 0.f;
+    if (tiles > 1) issue(1);
+    float delta = 0.f, rest = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) delta = row_of(i) == at ? own[i] : delta;
+    for (int i = 0; i < 16; ++i) delta = row_of(i) == me ? s[i] : delta;
     {
         const float other = __shfl_xor(delta, 32, 64);
-        delta = (at >> 2 & 1) == lane >> 5 ? delta : other;
+        delta = (me >> 2 & 1) == lane >> 5 ? delta : other;
     }
-    const float lse2 = at < have ? a.lse[(int64_t)head * a.rows + row + at] * 1.4426950408889634f : 0.f;
-    if (lane < have) a.delta[(int64_t)head * a.rows + row + lane] = delta;
-    f32x16 acc[D / 32];
+    f32x16 acc[D / 32], y[D / 32];
 #pragma unroll
-    for (int t = 0; t < D / 32; ++t) acc[t] = zeros16();
+    for (int t = 0; t < D / 32; ++t) acc[t] = y[t] = zeros16();
+    bf16x8 p[2], ds[2];
+    bool apart = false;
 
-    for (int k0 = 0; k0 < keys; k0 += BK) {
+    for (int n = 0; n < tiles; ++n) {
+        // this tile is there; the next one's transfers may still be under way
+        if (n + 1 < tiles) wait_vm<fk.N + fv.N>();
+        else wait_vm<0>();
         __syncthreads();
-        fk.store(lk);
-        fv.store(lv);
-        __syncthreads();
-        if (k0 + BK < keys) {
-            fk.load(kp + (int64_t)(k0 + BK) * a.ks, a.ks, keys - k0 - BK, a.d);
-            fv.load(vp + (int64_t)(k0 + BK) * a.vs, a.vs, keys - k0 - BK, a.d);
-        }
+        if (n + 2 < tiles) issue(n + 2); // in the place of the one that everybody has left behind
+        if (n >= subs) continue;
+        const AttnLane<D> lk(slot(n)), lv(slot(n) + TILE), before(slot(n + kAttnRing - 1));
+        pair_products<D>(s, dp, lk, lv, q, d_o);
+        const bool border = n == subs - 1; // where the mask ends
+        if (n > 0 && !border) {
+            bf16x8 pn[2], dn[2];
+            add_pair<D, true>(acc, y, before, before, ds, p, [&](int i) {
+                const float e = __builtin_amdgcn_exp2f(fmaf(s[i], a.c2, nlse2)), z = e * (dp[i] - delta);
+                rest += z;
+                pn[i >> 3][i & 7] = (bf16_t)e;
+                dn[i >> 3][i & 7] = (bf16_t)z;
+            });
+            p[0] = pn[0], p[1] = pn[1], ds[0] = dn[0], ds[1] = dn[1];
+        } else {
+            if (n > 0) add_pair<D, true>(acc, y, before, before, ds, p, [](int) {});
+            const int last = !border ? 31 : CAUSAL ? me : seq.len - 1 - 32 * n;
 #pragma unroll
-        for (int sub = 0; sub < BK; sub += 32) {
-            const int key0 = k0 + sub;
-            if (key0 >= keys || have < 1 || (CAUSAL && key0 > q0)) continue;
-            f32x16 s = zeros16(), dp = zeros16();
-#pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks) {
-                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ak.along(sub, ks), q[ks], s, 0, 0, 0);
-                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av.along(sub, ks), d_o[ks], dp, 0, 0, 0);
+            for (int i = 0; i < 16; ++i) {
+                const bool in = row_of(i) <= last;
+                const float e = __builtin_amdgcn_exp2f(fmaf(s[i], a.c2, nlse2)), z = in ? e * (dp[i] - delta) : 0.f;
+                rest += z;
+                p[i >> 3][i & 7] = (bf16_t)(in ? e : 0.f);
+                ds[i >> 3][i & 7] = (bf16_t)z;
             }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.c2, -lse2)) * (dp[i] - delta);
-            const bool diagonal = CAUSAL && key0 == q0;
-            if (diagonal) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = row_of(i) <= at ? s[i] : 0.f;
-            } else if (key0 + 32 > seq.len) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = key0 + row_of(i) < seq.len ? s[i] : 0.f;
+            if (border) {
+                apart = any_special<D>(lk, 0);
+                if (!apart) add_pair<D, true>(acc, y, lk, lk, ds, p, [](int) {});
             }
-            const bf16x8 p[2] = {rounded(s, 0), rounded(s, 1)};
-            if (diagonal && any_special<D>(ak, sub)) add_turned_apart<D>(acc, kp + (int64_t)key0 * a.ks, a.ks, seq.len - key0, a.d, p, [](int key, int query) { return key <= query; });
-            else add_turned<D>(acc, ak, sub, p);
         }
     }
     if (have < 1) return;
+    if (apart) {
+        const int key0 = 32 * (subs - 1);
+        auto part = [&](int key, int query) { return !CAUSAL || key <= query; };
+        add_turned_apart<D>(acc, kp + (int64_t)key0 * a.ks, a.ks, seq.len - key0, a.d, ds, part);
+        add_turned_apart<D>(y, kp + (int64_t)key0 * a.ks, a.ks, seq.len - key0, a.d, p, part);
+    }
+    rest += __shfl_xor(rest, 32, 64);
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[t][i] = fmaf(-rest, y[t][i], acc[t][i]);
     put_rows<D>(a.dq + row * a.dqs + (int64_t)head * a.d, a.dqs, have, a.d, acc, a.scale);
+    if (lane < have) {
+        a.nlse2[(int64_t)head * a.rows + row + lane] = nlse2;
+        a.delta[(int64_t)head * a.rows + row + lane] = delta + rest;
+    }
 }
 
 // ---------------------------------------------------------------------------
-// backward, dk and dv: 128 keys a workgroup, 32 a wavefront, which holds them, their values and both gradients in registers; 32 queries
-// and their do at a time in LDS, of all heads of the group one after the other.  S = q K^T has a key's scores in one column.
+// dk and dv: 128 keys a workgroup, 32 a wavefront, which holds them, their values and both gradients in registers; 32 queries and their
+// do at a time in LDS, of all heads of the group one after the other.  S = q K^T has a key's scores in one column.
 // ---------------------------------------------------------------------------
 template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 1) void k_attn_dkv(const AttnArgs a)
 {
     using T = AttnTile<D>;
-    constexpr int BN = 128, BQ = 32;
-    __shared__ __attribute__((aligned(1024))) char lds[2 * BQ * T::RB];
-    __shared__ __attribute__((aligned(16))) float stat[2][BQ]; // lse log2(e) and delta of the rows
-    char *const lq = lds, *const ld = lds + BQ * T::RB;
-    const uint32_t tq = lds_address(lq), td = lds_address(ld);
-    const AttnLane<D> aq(tq), ad(td);
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr int BN = 128, TILE = 32 * T::RB > 1024 ? 32 * T::RB : 1024, SLOT = 2 * TILE;
+    __shared__ __attribute__((aligned(1024))) char lds[kAttnRing * (SLOT + 256)]; // 32 queries and their do, four times; -lse log2(e) and delta
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), me = lane & 31;
     const AttnWork w = attn_work(a.kv_heads, a.tiles, false);
     const AttnSeq seq = attn_seq<BN>(a, w.vt);
     if (seq.len < 1) return;
     const int hk = w.head, key0 = seq.tile * BN + wave * 32, have = min(32, seq.len - key0);
     const int64_t row = seq.start + key0;
+    const int first = CAUSAL ? seq.tile * BN : 0, per = (seq.len - first + 31) / 32, tiles = per * a.group; // tiles of a head, of all
+    const uint32_t at = lds_address(lds);
+
+    AttnDma<D, 32> fq, fd;
+    fq.plan(a.qs, a.d);
+    fd.plan(a.dos, a.d);
+    if (a.d != D) clear_tiles<kAttnRing * SLOT>(lds);
+    auto slot = [&](int tile) { return at + (uint32_t)(tile % kAttnRing) * SLOT; };
+    auto stats = [&](int tile) { return at + kAttnRing * SLOT + (uint32_t)(tile % kAttnRing) * 256; };
+    // the tile to be fetched next, and the one that is looked at: head and first query, counted along instead of divided
+    int f_head = hk * a.group, f_row = first, n_head = f_head, n_row = first, f_tile = 0;
+    auto issue = [&]() {
+        const int rest = seq.len - f_row;
+        const int64_t r = seq.start + f_row;
+        fq.issue(a.q + r * a.qs + (int64_t)f_head * a.d, slot(f_tile), rest);
+        fd.issue(a.d_o + r * a.dos + (int64_t)f_head * a.d, slot(f_tile) + TILE, rest);
+        // every wavefront fetches them, so that all have as many transfers under way
+        const float *from = (lane < 32 ? a.nlse2 : a.delta) + (int64_t)f_head * a.rows + r + min(me, rest - 1);
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
+                     : : "s"(__builtin_amdgcn_readfirstlane(stats(f_tile))), "v"(from) : "memory", "m0");
+        ++f_tile;
+        f_row += 32;
+        if (f_row >= seq.len) f_row = first, ++f_head;
+    };
+    issue();
     bf16x8 k[D / 16], v[D / 16];
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) {
         k[ks] = along_mem(a.k + row * a.ks + (int64_t)hk * a.d, a.ks, have, a.d, ks);
         v[ks] = along_mem(a.v + row * a.vs + (int64_t)hk * a.d, a.vs, have, a.d, ks);
     }
-    f32x16 dk[D / 32], dv[D / 32];
+    if (tiles > 1) issue();
+    f32x16 dk[D / 32], dv[D / 32], s, dp;
 #pragma unroll
     for (int t = 0; t < D / 32; ++t) dk[t] = dv[t] = zeros16();
+    bf16x8 p[2], ds[2];
+    bool pending = false, apart = false; // p and ds of the tile before are still to be added; row by row
+    int p_head = 0, p_row = 0;
+    typedef const __attribute__((address_space(3))) f32x4 *lds_f32x4;
 
-    const int first = CAUSAL ? seq.tile * BN : 0, steps = (seq.len - first + BQ - 1) / BQ, total = steps * a.group;
-    AttnFetch<D, BQ> fq, fd;
-    float fs = 0.f;
-    auto fetch = [&](int n) {
-        const int head = hk * a.group + n / steps, q0 = first + n % steps * BQ, rest = seq.len - q0;
-        const int64_t at = seq.start + q0;
-        fq.load(a.q + at * a.qs + (int64_t)head * a.d, a.qs, rest, a.d);
-        fd.load(a.d_o + at * a.dos + (int64_t)head * a.d, a.dos, rest, a.d);
-        if (threadIdx.x < 2 * BQ) {
-            const int x = threadIdx.x % BQ;
-            const int64_t p = (int64_t)head * a.rows + at + x;
-            // rows past the end: p = exp(-infinity) = 0
-            if (threadIdx.x < BQ) fs = x < rest ? a.lse[p] * 1.4426950408889634f : INFINITY;
-            else fs = x < rest ? a.delta[p] : 0.f;
-        }
-    };
-    fetch(0);
-    for (int n = 0; n < total; ++n) {
-        __syncthreads();
-        fq.store(lq);
-        fd.store(ld);
-        if (threadIdx.x < 2 * BQ) stat[threadIdx.x / BQ][threadIdx.x % BQ] = fs;
-        __syncthreads();
-        if (n + 1 < total) fetch(n + 1);
-        const int q0 = first + n % steps * BQ;
-        if (have < 1 || (CAUSAL && q0 < key0)) continue;
-        f32x16 s = zeros16(), dp = zeros16();
+    for (int n = 0; n <= tiles; ++n) {
+        if (n + 1 < tiles) wait_vm<fq.N + fd.N + 1>();
+        else wait_vm<0>();
+        if (n < tiles) __syncthreads();
+        if (n + 2 < tiles) issue();
+        const bool active = n < tiles && have > 0 && (!CAUSAL || n_row >= key0);
+        const AttnLane<D> lq(slot(n)), ld(slot(n) + TILE), bq(slot(n + kAttnRing - 1)), bd(slot(n + kAttnRing - 1) + TILE);
+        const bool border = (CAUSAL && n_row == key0) || n_row + 32 > seq.len;
+        f32x4 nl[4], dl[4];
+        if (active) {
+            const uint32_t st = stats(n) + 16 * (lane >> 5);
 #pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) {
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(aq.along(0, ks), k[ks], s, 0, 0, 0);
-            dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ad.along(0, ks), v[ks], dp, 0, 0, 0);
-        }
-        const bool diagonal = CAUSAL && q0 == key0;
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const f32x4 lse2 = *reinterpret_cast<const f32x4 *>(&stat[0][8 * g + 4 * (lane >> 5)]);
-            const f32x4 delta = *reinterpret_cast<const f32x4 *>(&stat[1][8 * g + 4 * (lane >> 5)]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int i = 4 * g + e;
-                s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.c2, -lse2[e]));
-                dp[i] = s[i] * (dp[i] - delta[e]);
+            for (int g = 0; g < 4; ++g) {
+                nl[g] = *reinterpret_cast<lds_f32x4>(st + 32 * g);
+                dl[g] = *reinterpret_cast<lds_f32x4>(st + 128 + 32 * g);
             }
+            pair_products<D>(s, dp, lq, ld, k, v);
         }
-        if (diagonal) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const bool in = (lane & 31) <= row_of(i);
-                s[i] = in ? s[i] : 0.f;
-                dp[i] = in ? dp[i] : 0.f;
-            }
-        }
-        const bf16x8 p[2] = {rounded(s, 0), rounded(s, 1)}, ds[2] = {rounded(dp, 0), rounded(dp, 1)};
-        if (diagonal && (any_special<D>(ad, 0) || any_special<D>(aq, 0))) {
-            auto part = [](int query, int key) { return key <= query; };
-            const int64_t r0 = seq.start + q0, c0 = (int64_t)(hk * a.group + n / steps) * a.d;
-            add_turned_apart<D>(dv, a.d_o + r0 * a.dos + c0, a.dos, seq.len - q0, a.d, p, part);
-            add_turned_apart<D>(dk, a.q + r0 * a.qs + c0, a.qs, seq.len - q0, a.d, ds, part);
+        if (active && pending && !border && !apart) {
+            bf16x8 pn[2], dn[2];
+            add_pair<D, false>(dv, dk, bd, bq, p, ds, [&](int i) {
+                const float e = __builtin_amdgcn_exp2f(fmaf(s[i], a.c2, nl[i >> 2][i & 3]));
+                pn[i >> 3][i & 7] = (bf16_t)e;
+                dn[i >> 3][i & 7] = (bf16_t)(e * (dp[i] - dl[i >> 2][i & 3]));
+            });
+            p[0] = pn[0], p[1] = pn[1], ds[0] = dn[0], ds[1] = dn[1];
         } else {
-            add_turned<D>(dv, ad, 0, p);
-            add_turned<D>(dk, aq, 0, ds);
+            if (pending && !apart) add_pair<D, false>(dv, dk, bd, bq, p, ds, [](int) {});
+            if (pending && apart) {
+                const int64_t r0 = seq.start + p_row, c0 = (int64_t)p_head * a.d;
+                auto part = [&](int query, int key) { return !CAUSAL || p_row != key0 || key <= query; };
+                add_turned_apart<D>(dv, a.d_o + r0 * a.dos + c0, a.dos, seq.len - p_row, a.d, p, part);
+                add_turned_apart<D>(dk, a.q + r0 * a.qs + c0, a.qs, seq.len - p_row, a.d, ds, part);
+            }
+            apart = false;
+            if (active) {
+                const int from = CAUSAL && n_row == key0 ? me : 0, to = seq.len - n_row; // the queries that see the lane's key
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const bool in = row_of(i) >= from && row_of(i) < to;
+                    const float e = __builtin_amdgcn_exp2f(fmaf(s[i], a.c2, nl[i >> 2][i & 3]));
+                    p[i >> 3][i & 7] = (bf16_t)(in ? e : 0.f);
+                    ds[i >> 3][i & 7] = (bf16_t)(in ? e * (dp[i] - dl[i >> 2][i & 3]) : 0.f);
+                }
+                if (border) apart = any_special<D>(lq, 0) || any_special<D>(ld, 0);
+            }
         }
+        pending = active;
+        p_head = n_head, p_row = n_row;
+        n_row += 32;
+        if (n_row >= seq.len) n_row = first, ++n_head;
     }
     if (have < 1) return;
     put_rows<D>(a.dk + row * a.dks + (int64_t)hk * a.d, a.dks, have, a.d, dk, a.scale);
@@ -652,7 +725,7 @@ static AttnArgs attn_args(const pac_attn *a, const int32_t *off, int32_t batch, 
     r.tiles = (unsigned)(rows / 128 + batch);
     return r;
 }
-static int64_t delta_bytes(const pac_attn *a, int64_t rows) { return (rows * a->heads * 4 + 255) / 256 * 256; }
+static int64_t stat_bytes(const pac_attn *a, int64_t rows) { return (rows * a->heads * 4 + 255) / 256 * 256; }
 
 template <typename F> static void by_width(int d, const F &f)
 {
@@ -703,7 +776,7 @@ pac_status pac_attn_forward(const pac_attn *a, const int32_t *offsets, int32_t b
 
 int64_t pac_attn_workspace_bytes(const pac_attn *a, int32_t batch, int64_t rows)
 {
-    return check_attn(a, batch, rows) == PAC_OK ? delta_bytes(a, rows) : -1;
+    return check_attn(a, batch, rows) == PAC_OK ? 2 * stat_bytes(a, rows) : -1;
 }
 
 pac_status pac_attn_backward(const pac_attn *a, const int32_t *offsets, int32_t batch, int64_t rows, const void *q, int64_t q_stride,
@@ -741,7 +814,8 @@ pac_status pac_attn_backward(const pac_attn *a, const int32_t *offsets, int32_t 
     r.dk = static_cast<bf16_t *>(dk); r.dks = dk_stride;
     r.dv = static_cast<bf16_t *>(dv); r.dvs = dv_stride;
     r.lse = const_cast<float *>(lse);
-    r.delta = static_cast<float *>(workspace);
+    r.nlse2 = static_cast<float *>(workspace);
+    r.delta = reinterpret_cast<float *>(static_cast<char *>(workspace) + stat_bytes(a, rows));
     (void)hipGetLastError();
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     by_width(a->d, [&](auto n) {
