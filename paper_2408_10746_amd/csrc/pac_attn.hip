@@ -356,53 +356,59 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_f
     bf16x8 late[2];
     bool apart = false;
 
-    for (int k0 = 0, turn = 0; k0 < keys; k0 += BK, turn ^= 1) {
+    const int tiles = (keys + BK - 1) / BK, full = have < 1 ? 0 : (CAUSAL ? q0 : seq.len) / BK; // of all wavefronts; unmasked ones of this one
+    auto arrive = [&](int t) {
         wait_vm<0>();
         __syncthreads(); // everybody's share of this tile is there, and the other one is free
-        const uint32_t tk = at + turn * (2 * TILE), tv = tk + TILE;
-        if (k0 + BK < keys) {
-            const uint32_t to = at + (turn ^ 1) * (2 * TILE);
-            fk.issue(kp + (int64_t)(k0 + BK) * a.ks, to, keys - k0 - BK);
-            fv.issue(vp + (int64_t)(k0 + BK) * a.vs, to + TILE, keys - k0 - BK);
+        if (t + 1 < tiles) {
+            const uint32_t to = at + (uint32_t)((t + 1) & 1) * (2 * TILE);
+            fk.issue(kp + (int64_t)(t + 1) * BK * a.ks, to, keys - (t + 1) * BK);
+            fv.issue(vp + (int64_t)(t + 1) * BK * a.vs, to + TILE, keys - (t + 1) * BK);
         }
-        if (have < 1) continue;
-        const AttnLane<D> lk(tk), lv(tv);
-        if (k0 + BK <= (CAUSAL ? q0 : seq.len)) {
-            f32x16 s[2];
-            scores<D, 2>(s, lk, 0, q);
-            r.raise(fmaxf(largest(s[0]), largest(s[1])) * a.c2);
-            r.weigh(s[0], a.c2);
-            const bf16x8 p0[2] = {rounded(s[0], 0), rounded(s[0], 1)};
-            add_turned<D>(r.acc, lv, 0, p0);
-            r.weigh(s[1], a.c2);
-            const bf16x8 p1[2] = {rounded(s[1], 0), rounded(s[1], 1)};
-            add_turned<D>(r.acc, lv, 32, p1);
-        } else {
+    };
+    int t = 0;
+    for (; t < full; ++t) {
+        arrive(t);
+        const AttnLane<D> lk(at + (uint32_t)(t & 1) * (2 * TILE)), lv(at + (uint32_t)(t & 1) * (2 * TILE) + TILE);
+        f32x16 s[2];
+        scores<D, 2>(s, lk, 0, q);
+        r.raise(fmaxf(largest(s[0]), largest(s[1])) * a.c2);
+        r.weigh(s[0], a.c2);
+        const bf16x8 p0[2] = {rounded(s[0], 0), rounded(s[0], 1)};
+        add_turned<D>(r.acc, lv, 0, p0);
+        r.weigh(s[1], a.c2);
+        const bf16x8 p1[2] = {rounded(s[1], 0), rounded(s[1], 1)};
+        add_turned<D>(r.acc, lv, 32, p1);
+    }
+    if (t < tiles && have > 0) {
+        arrive(t);
+        const AttnLane<D> lk(at + (uint32_t)(t & 1) * (2 * TILE)), lv(at + (uint32_t)(t & 1) * (2 * TILE) + TILE);
 #pragma unroll 1
-            for (int sub = 0; sub < BK; sub += 32) {
-                const int key0 = k0 + sub;
-                if (key0 >= keys || (CAUSAL && key0 > q0)) break;
-                f32x16 s1[1];
-                scores<D, 1>(s1, lk, sub, q);
-                f32x16 &s = s1[0];
-                const bool cut = key0 == border;
-                if (cut) {
+        for (int sub = 0; sub < BK; sub += 32) {
+            const int key0 = t * BK + sub;
+            if (key0 >= keys || (CAUSAL && key0 > q0)) break;
+            f32x16 s1[1];
+            scores<D, 1>(s1, lk, sub, q);
+            f32x16 &s = s1[0];
+            const bool cut = key0 == border;
+            if (cut) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[i] = row_of(i) <= last ? s[i] : -INFINITY;
-                }
-                r.raise(largest(s) * a.c2);
-                r.weigh(s, a.c2);
-                const bf16x8 p[2] = {rounded(s, 0), rounded(s, 1)};
-                if (cut && any_special<D>(lv, sub)) {
-                    apart = true;
-                    late[0] = p[0];
-                    late[1] = p[1];
-                } else {
-                    add_turned<D>(r.acc, lv, sub, p);
-                }
+                for (int i = 0; i < 16; ++i) s[i] = row_of(i) <= last ? s[i] : -INFINITY;
+            }
+            r.raise(largest(s) * a.c2);
+            r.weigh(s, a.c2);
+            const bf16x8 p[2] = {rounded(s, 0), rounded(s, 1)};
+            if (cut && any_special<D>(lv, sub)) {
+                apart = true;
+                late[0] = p[0];
+                late[1] = p[1];
+            } else {
+                add_turned<D>(r.acc, lv, sub, p);
             }
         }
+        ++t;
     }
+    for (; t < tiles; ++t) arrive(t); // what other wavefronts see
     if (have < 1) return;
     if (apart) add_turned_apart<D>(r.acc, vp + (int64_t)border * a.vs, a.vs, seq.len - border, a.d, late, [&](int key, int) { return key <= last; });
     const float sum = r.sum + __shfl_xor(r.sum, 32, 64);
@@ -521,42 +527,57 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 1) void k_attn_d
     bf16x8 p[2], ds[2];
     bool apart = false;
 
-    for (int n = 0; n < tiles; ++n) {
+    auto arrive = [&](int n) {
         // this tile is there; the next one's transfers may still be under way
         if (n + 1 < tiles) wait_vm<fk.N + fv.N>();
         else wait_vm<0>();
         __syncthreads();
         if (n + 2 < tiles) issue(n + 2); // in the place of the one that everybody has left behind
-        if (n >= subs) continue;
-        const AttnLane<D> lk(slot(n)), lv(slot(n) + TILE), before(slot(n + kAttnRing - 1));
-        pair_products<D>(s, dp, lk, lv, q, d_o);
-        const bool border = n == subs - 1; // where the mask ends
-        if (n > 0 && !border) {
-            bf16x8 pn[2], dn[2];
-            add_pair<D, true>(acc, y, before, before, ds, p, [&](int i) {
-                const float e = __builtin_amdgcn_exp2f(fmaf(s[i], a.c2, nlse2)), z = e * (dp[i] - delta);
-                rest += z;
-                pn[i >> 3][i & 7] = (bf16_t)e;
-                dn[i >> 3][i & 7] = (bf16_t)z;
-            });
-            p[0] = pn[0], p[1] = pn[1], ds[0] = dn[0], ds[1] = dn[1];
-        } else {
-            if (n > 0) add_pair<D, true>(acc, y, before, before, ds, p, [](int) {});
-            const int last = !border ? 31 : CAUSAL ? me : seq.len - 1 - 32 * n;
+    };
+    // the vector work of a subtile; of queries that see keys up to `last`
+    bf16x8 pn[2], dn[2];
+    auto element = [&](int i) {
+        const float e = __builtin_amdgcn_exp2f(fmaf(s[i], a.c2, nlse2)), z = e * (dp[i] - delta);
+        rest += z;
+        pn[i >> 3][i & 7] = (bf16_t)e;
+        dn[i >> 3][i & 7] = (bf16_t)z;
+    };
+    auto taken = [&]() { p[0] = pn[0], p[1] = pn[1], ds[0] = dn[0], ds[1] = dn[1]; };
+    int n = 0;
+    if (subs > 1) {
+        arrive(0);
+        pair_products<D>(s, dp, AttnLane<D>(slot(0)), AttnLane<D>(slot(0) + TILE), q, d_o);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const bool in = row_of(i) <= last;
-                const float e = __builtin_amdgcn_exp2f(fmaf(s[i], a.c2, nlse2)), z = in ? e * (dp[i] - delta) : 0.f;
-                rest += z;
-                p[i >> 3][i & 7] = (bf16_t)(in ? e : 0.f);
-                ds[i >> 3][i & 7] = (bf16_t)z;
-            }
-            if (border) {
-                apart = any_special<D>(lk, 0);
-                if (!apart) add_pair<D, true>(acc, y, lk, lk, ds, p, [](int) {});
-            }
+        for (int i = 0; i < 16; ++i) element(i);
+        taken();
+        for (n = 1; n < subs - 1; ++n) {
+            arrive(n);
+            pair_products<D>(s, dp, AttnLane<D>(slot(n)), AttnLane<D>(slot(n) + TILE), q, d_o);
+            const AttnLane<D> before(slot(n + kAttnRing - 1));
+            add_pair<D, true>(acc, y, before, before, ds, p, element);
+            taken();
         }
+        const AttnLane<D> before(slot(n + kAttnRing - 1));
+        add_pair<D, true>(acc, y, before, before, ds, p, [](int) {});
     }
+    if (subs > 0) { // the last subtile, where the mask ends
+        arrive(n);
+        const AttnLane<D> lk(slot(n));
+        pair_products<D>(s, dp, lk, AttnLane<D>(slot(n) + TILE), q, d_o);
+        const int last = CAUSAL ? me : seq.len - 1 - 32 * n;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const bool in = row_of(i) <= last;
+            const float e = __builtin_amdgcn_exp2f(fmaf(s[i], a.c2, nlse2)), z = in ? e * (dp[i] - delta) : 0.f;
+            rest += z;
+            p[i >> 3][i & 7] = (bf16_t)(in ? e : 0.f);
+            ds[i >> 3][i & 7] = (bf16_t)z;
+        }
+        apart = any_special<D>(lk, 0);
+        if (!apart) add_pair<D, true>(acc, y, lk, lk, ds, p, [](int) {});
+        ++n;
+    }
+    for (; n < tiles; ++n) arrive(n); // what other wavefronts see
     if (have < 1) return;
     if (apart) {
         const int key0 = 32 * (subs - 1);
@@ -591,7 +612,7 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 1) void k_attn_d
     if (seq.len < 1) return;
     const int hk = w.head, key0 = seq.tile * BN + wave * 32, have = min(32, seq.len - key0);
     const int64_t row = seq.start + key0;
-    const int first = CAUSAL ? seq.tile * BN : 0, per = (seq.len - first + 31) / 32, tiles = per * a.group; // tiles of a head, of all
+    const int first = CAUSAL ? seq.tile * BN : 0, per = (seq.len - first + 31) / 32, tiles = per * a.group; // subtiles of a head, of all
     const uint32_t at = lds_address(lds);
 
     AttnDma<D, 32> fq, fd;
@@ -600,8 +621,7 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 1) void k_attn_d
     if (a.d != D) clear_tiles<kAttnRing * SLOT>(lds);
     auto slot = [&](int tile) { return at + (uint32_t)(tile % kAttnRing) * SLOT; };
     auto stats = [&](int tile) { return at + kAttnRing * SLOT + (uint32_t)(tile % kAttnRing) * 256; };
-    // the tile to be fetched next, and the one that is looked at: head and first query, counted along instead of divided
-    int f_head = hk * a.group, f_row = first, n_head = f_head, n_row = first, f_tile = 0;
+    int f_head = hk * a.group, f_row = first, f_tile = 0; // the tile to be fetched next: head and first query, counted along instead of divided
     auto issue = [&]() {
         const int rest = seq.len - f_row;
         const int64_t r = seq.start + f_row;
@@ -626,62 +646,80 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 1) void k_attn_d
     f32x16 dk[D / 32], dv[D / 32], s, dp;
 #pragma unroll
     for (int t = 0; t < D / 32; ++t) dk[t] = dv[t] = zeros16();
-    bf16x8 p[2], ds[2];
-    bool pending = false, apart = false; // p and ds of the tile before are still to be added; row by row
-    int p_head = 0, p_row = 0;
+    bf16x8 p[2], ds[2], pn[2], dn[2];
+    f32x4 nl[4], dl[4];
     typedef const __attribute__((address_space(3))) f32x4 *lds_f32x4;
-
-    for (int n = 0; n <= tiles; ++n) {
+    int n = 0; // tiles so far
+    auto arrive = [&]() {
         if (n + 1 < tiles) wait_vm<fq.N + fd.N + 1>();
         else wait_vm<0>();
-        if (n < tiles) __syncthreads();
+        __syncthreads();
         if (n + 2 < tiles) issue();
-        const bool active = n < tiles && have > 0 && (!CAUSAL || n_row >= key0);
-        const AttnLane<D> lq(slot(n)), ld(slot(n) + TILE), bq(slot(n + kAttnRing - 1)), bd(slot(n + kAttnRing - 1) + TILE);
-        const bool border = (CAUSAL && n_row == key0) || n_row + 32 > seq.len;
-        f32x4 nl[4], dl[4];
-        if (active) {
-            const uint32_t st = stats(n) + 16 * (lane >> 5);
+        ++n;
+    };
+    auto products = [&]() { // of the tile that has arrived
+        const uint32_t st = stats(n - 1) + 16 * (lane >> 5);
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                nl[g] = *reinterpret_cast<lds_f32x4>(st + 32 * g);
-                dl[g] = *reinterpret_cast<lds_f32x4>(st + 128 + 32 * g);
-            }
-            pair_products<D>(s, dp, lq, ld, k, v);
+        for (int g = 0; g < 4; ++g) {
+            nl[g] = *reinterpret_cast<lds_f32x4>(st + 32 * g);
+            dl[g] = *reinterpret_cast<lds_f32x4>(st + 128 + 32 * g);
         }
-        if (active && pending && !border && !apart) {
-            bf16x8 pn[2], dn[2];
-            add_pair<D, false>(dv, dk, bd, bq, p, ds, [&](int i) {
-                const float e = __builtin_amdgcn_exp2f(fmaf(s[i], a.c2, nl[i >> 2][i & 3]));
-                pn[i >> 3][i & 7] = (bf16_t)e;
-                dn[i >> 3][i & 7] = (bf16_t)(e * (dp[i] - dl[i >> 2][i & 3]));
-            });
-            p[0] = pn[0], p[1] = pn[1], ds[0] = dn[0], ds[1] = dn[1];
-        } else {
-            if (pending && !apart) add_pair<D, false>(dv, dk, bd, bq, p, ds, [](int) {});
-            if (pending && apart) {
-                const int64_t r0 = seq.start + p_row, c0 = (int64_t)p_head * a.d;
-                auto part = [&](int query, int key) { return !CAUSAL || p_row != key0 || key <= query; };
-                add_turned_apart<D>(dv, a.d_o + r0 * a.dos + c0, a.dos, seq.len - p_row, a.d, p, part);
-                add_turned_apart<D>(dk, a.q + r0 * a.qs + c0, a.qs, seq.len - p_row, a.d, ds, part);
-            }
-            apart = false;
-            if (active) {
-                const int from = CAUSAL && n_row == key0 ? me : 0, to = seq.len - n_row; // the queries that see the lane's key
+        pair_products<D>(s, dp, AttnLane<D>(slot(n - 1)), AttnLane<D>(slot(n - 1) + TILE), k, v);
+    };
+    auto element = [&](int i) {
+        const float e = __builtin_amdgcn_exp2f(fmaf(s[i], a.c2, nl[i >> 2][i & 3]));
+        pn[i >> 3][i & 7] = (bf16_t)e;
+        dn[i >> 3][i & 7] = (bf16_t)(e * (dp[i] - dl[i >> 2][i & 3]));
+    };
+    auto taken = [&]() { p[0] = pn[0], p[1] = pn[1], ds[0] = dn[0], ds[1] = dn[1]; };
+    // this wavefront's subtiles of a head: none, the first ones, where causal queries see none of its keys; then the diagonal, the main ones, and
+    // one that ends with the sequence
+    const int idle = have < 1 ? per : CAUSAL ? wave : 0, active = per - idle;
+    const bool odd_end = seq.len % 32 != 0;
+    const int middle = active - (CAUSAL && active > 0) - (odd_end && active > (CAUSAL ? 1 : 0));
+#pragma unroll 1
+    for (int head = hk * a.group; head < (hk + 1) * a.group; ++head) {
+        for (int i = 0; i < idle; ++i) arrive();
+        if (active < 1) continue;
+#pragma unroll 1
+        for (int side = 0; side < 2; ++side) {
+            if (side == 0 ? CAUSAL : odd_end && active > (CAUSAL ? 1 : 0)) {
+                const int qr = side == 0 ? key0 : seq.len & ~31;
+                arrive();
+                products();
+                const int from = CAUSAL && qr == key0 ? me : 0, to = seq.len - qr; // the queries that see the lane's key
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const bool in = row_of(i) >= from && row_of(i) < to;
-                    const float e = __builtin_amdgcn_exp2f(fmaf(s[i], a.c2, nl[i >> 2][i & 3]));
-                    p[i >> 3][i & 7] = (bf16_t)(in ? e : 0.f);
-                    ds[i >> 3][i & 7] = (bf16_t)(in ? e * (dp[i] - dl[i >> 2][i & 3]) : 0.f);
+                    element(i);
+                    pn[i >> 3][i & 7] = in ? pn[i >> 3][i & 7] : (bf16_t)0.f;
+                    dn[i >> 3][i & 7] = in ? dn[i >> 3][i & 7] : (bf16_t)0.f;
                 }
-                if (border) apart = any_special<D>(lq, 0) || any_special<D>(ld, 0);
+                const AttnLane<D> lq(slot(n - 1)), ld(slot(n - 1) + TILE);
+                if (any_special<D>(lq, 0) || any_special<D>(ld, 0)) {
+                    const int64_t r0 = seq.start + qr, c0 = (int64_t)head * a.d;
+                    auto part = [&](int query, int) { return query >= from; };
+                    add_turned_apart<D>(dv, a.d_o + r0 * a.dos + c0, a.dos, to, a.d, pn, part);
+                    add_turned_apart<D>(dk, a.q + r0 * a.qs + c0, a.qs, to, a.d, dn, part);
+                } else {
+                    add_pair<D, false>(dv, dk, ld, lq, pn, dn, [](int) {});
+                }
+            }
+            if (side == 0 && middle > 0) {
+                arrive();
+                products();
+#pragma unroll
+                for (int i = 0; i < 16; ++i) element(i);
+                taken();
+                for (int i = 1; i < middle; ++i) {
+                    arrive();
+                    products();
+                    add_pair<D, false>(dv, dk, AttnLane<D>(slot(n + kAttnRing - 2) + TILE), AttnLane<D>(slot(n + kAttnRing - 2)), p, ds, element);
+                    taken();
+                }
+                add_pair<D, false>(dv, dk, AttnLane<D>(slot(n - 1) + TILE), AttnLane<D>(slot(n - 1)), p, ds, [](int) {});
             }
         }
-        pending = active;
-        p_head = n_head, p_row = n_row;
-        n_row += 32;
-        if (n_row >= seq.len) n_row = first, ++n_head;
     }
     if (have < 1) return;
     put_rows<D>(a.dk + row * a.dks + (int64_t)hk * a.d, a.dks, have, a.d, dk, a.scale);
