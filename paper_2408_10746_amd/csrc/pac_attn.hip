@@ -212,16 +212,21 @@ template <int D> __device__ __forceinline__ void add_turned(f32x16 (&acc)[D / 32
         PAC_ATTN_PACE;
     }
 }
-// Do 32 rows of a tile hold an infinity or NaN?
+// Is one of eight values an infinity or NaN?
+__device__ __forceinline__ uint32_t special(const bf16x8 &x)
+{
+    const u32x4 w = __builtin_bit_cast(u32x4, x);
+    uint32_t bad = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) bad |= ((w[e] & 0x7f80u) == 0x7f80u) | ((w[e] & 0x7f800000u) == 0x7f800000u);
+    return bad;
+}
+// Do 32 rows of a tile hold one?
 template <int D> __device__ __forceinline__ bool any_special(const AttnLane<D> &l, int row0)
 {
     uint32_t bad = 0;
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) {
-        const u32x4 w = __builtin_bit_cast(u32x4, l.along(row0, ks));
-#pragma unroll
-        for (int e = 0; e < 4; ++e) bad |= ((w[e] & 0x7f80u) == 0x7f80u) | ((w[e] & 0x7f800000u) == 0x7f800000u);
-    }
+    for (int ks = 0; ks < D / 16; ++ks) bad |= special(l.along(row0, ks));
     return __any(bad != 0);
 }
 // add_turned where row x of 32 takes part in column c of the result only if part(x, c): a matrix instruction would multiply an infinity or
@@ -417,53 +422,63 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_f
 }
 
 // ---------------------------------------------------------------------------
-// backward.  Both kernels walk over subtiles of 32 x 32 pairs, whose rows come through a ring of four LDS slots: two products (scores,
-// do . v), 16 values of p and ds a lane, and the products that p and ds enter.  A wavefront has its SIMD to itself (its sums and operands
-// take more than half of the registers), so the vector work of a subtile is written between the matrix instructions of the products that
-// the one before it enters.
+// backward.  Both kernels walk over subtiles of 32 x 32 pairs, whose rows come through a ring of LDS slots: two products (scores, do . v),
+// 16 values of p and ds a lane, and the products that p and ds enter.  Two wavefronts share a SIMD: alone on it, one issues a vector
+// instruction in every second slot at best (measured: 6.5 cycles each against 4 with two).  At 128 values a head that takes one of the
+// wavefront's own two operands out of the registers: do (of dq) or v (of dk and dv) is read from LDS again for every subtile.
 // ---------------------------------------------------------------------------
-constexpr int kAttnRing = 4;
+template <int D> struct AttnBack {
+    using T = AttnTile<D>;
+    static constexpr bool OWN = D == 128;                  // the second operand lies in LDS
+    static constexpr int TILE = 32 * T::RB > 1024 ? 32 * T::RB : 1024, SLOT = 2 * TILE, RING = OWN ? 2 : 3;
+    static constexpr int HELD = OWN ? 128 * T::RB : 0;     // bytes of the second operand
+    static constexpr int REGS = OWN ? 1 : D / 16;
+};
 
-// sn = (rows of the first tile) b1^T, dn = (rows of the second) b2^T
+// s = (rows of the first tile) b1^T, dn = (rows of the second) b2^T, b2 from registers or from `own`; operands are read ahead
 template <int D>
-__device__ __forceinline__ void pair_products(f32x16 &sn, f32x16 &dn, const AttnLane<D> &l1, const AttnLane<D> &l2, const bf16x8 (&b1)[D / 16],
-                                              const bf16x8 (&b2)[D / 16])
+__device__ __forceinline__ void pair_products(f32x16 &s, f32x16 &dn, const AttnLane<D> &l1, const AttnLane<D> &l2, const bf16x8 (&b1)[D / 16],
+                                              const bf16x8 (&b2)[AttnBack<D>::REGS], const AttnLane<D> &own, int own_row)
 {
-    constexpr int N = D / 8, AHEAD = 4, K = AHEAD - 1;
-    bf16x8 f[AHEAD];
+    constexpr int N = D / 16, AHEAD = 2;
+    constexpr bool OWN = AttnBack<D>::OWN;
+    bf16x8 f1[AHEAD + 1], f2[AHEAD + 1], f3[AHEAD + 1];
+    auto read = [&](int n) {
+        f1[n % (AHEAD + 1)] = l1.along(0, n);
+        f2[n % (AHEAD + 1)] = l2.along(0, n);
+        if constexpr (OWN) f3[n % (AHEAD + 1)] = own.along(own_row, n);
+    };
 #pragma unroll
-    for (int n = 0; n < K; ++n) f[n] = (n % 2 ? l2 : l1).along(0, n / 2);
-    sn = zeros16();
+    for (int n = 0; n < AHEAD; ++n) read(n);
+    s = zeros16();
     dn = zeros16();
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-        if (n + K < N) f[(n + K) % AHEAD] = ((n + K) % 2 ? l2 : l1).along(0, (n + K) / 2);
-        if (n % 2) dn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[n % AHEAD], b2[n / 2], dn, 0, 0, 0);
-        else sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[n % AHEAD], b1[n / 2], sn, 0, 0, 0);
-        __builtin_amdgcn_sched_barrier(0);
+        if (n + AHEAD < N) read(n + AHEAD);
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f1[n % (AHEAD + 1)], b1[n], s, 0, 0, 0);
+        dn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f2[n % (AHEAD + 1)], OWN ? f3[n % (AHEAD + 1)] : b2[OWN ? 0 : n], dn, 0, 0, 0);
+        PAC_ATTN_PACE;
     }
 }
-// acc[t] += (first tile, turned)^T p,  more[t] += (second tile, turned)^T q, and element(i), i = 0..15, in between.  SAME: both are one tile.
-template <int D, bool SAME, class El>
-__device__ __forceinline__ void add_pair(f32x16 (&acc)[D / 32], f32x16 (&more)[D / 32], const AttnLane<D> &l1, const AttnLane<D> &l2, const bf16x8 (&p)[2],
-                                         const bf16x8 (&q)[2], const El &element)
+// acc[t] += (first tile, turned)^T p,  more[t] += (second tile, turned)^T q.  SAME: both are one tile, whose operands serve both.
+template <int D, bool SAME>
+__device__ __forceinline__ void pair_sums(f32x16 (&acc)[D / 32], f32x16 (&more)[D / 32], const AttnLane<D> &l1, const AttnLane<D> &l2, const bf16x8 (&p)[2],
+                                          const bf16x8 (&q)[2])
 {
     // product n: tile n % 2, 16 rows j, 32 values t; operand m = n, or n / 2 where both tiles are one
-    constexpr int T = D / 32, N = 4 * T, M = SAME ? N / 2 : N, AHEAD = 4, K = SAME ? 2 : 3;
-    bf16x8 f[AHEAD];
-    auto read = [&](int m) { return SAME ? l1.turned(0, m / T, m % T) : (m % 2 ? l2 : l1).turned(0, m / 2 / T, m / 2 % T); };
+    constexpr int T = D / 32, N = 4 * T, M = SAME ? N / 2 : N, K = SAME ? 2 : 3;
+    bf16x8 g[4];
+    auto read = [&](int m) { g[m % 4] = SAME ? l1.turned(0, m / T, m % T) : (m % 2 ? l2 : l1).turned(0, m / 2 / T, m / 2 % T); };
 #pragma unroll
-    for (int m = 0; m < K; ++m) f[m] = read(m);
+    for (int m = 0; m < K; ++m)
+        if (m < M) read(m);
 #pragma unroll
     for (int n = 0; n < N; ++n) {
         const int m = SAME ? n / 2 : n;
-        if ((!SAME || n % 2 == 0) && m + K < M) f[(m + K) % AHEAD] = read(m + K);
-        const bf16x8 &x = f[m % AHEAD];
-        if (n % 2) more[n / 2 % T] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[n / 2 / T], more[n / 2 % T], 0, 0, 0);
-        else acc[n / 2 % T] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, p[n / 2 / T], acc[n / 2 % T], 0, 0, 0);
-#pragma unroll
-        for (int i = n * 16 / N; i < (n + 1) * 16 / N; ++i) element(i);
-        __builtin_amdgcn_sched_barrier(0);
+        if ((!SAME || n % 2 == 0) && m + K < M) read(m + K);
+        if (n % 2) more[n / 2 % T] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(g[m % 4], q[n / 2 / T], more[n / 2 % T], 0, 0, 0);
+        else acc[n / 2 % T] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(g[m % 4], p[n / 2 / T], acc[n / 2 % T], 0, 0, 0);
+        PAC_ATTN_PACE;
     }
 }
 
@@ -477,11 +492,11 @@ __device__ __forceinline__ void add_pair(f32x16 (&acc)[D / 32], f32x16 (&more)[D
 // delta' + r goes to memory for the other kernel, with -lse log2(e).  delta' comes from the product that makes do . v too (the diagonal of
 // do o^T), so that a row with one key has exactly no gradient in q and k.
 // ---------------------------------------------------------------------------
-template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 1) void k_attn_dq(const AttnArgs a)
+template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a)
 {
-    using T = AttnTile<D>;
-    constexpr int BM = 128, TILE = 32 * T::RB > 1024 ? 32 * T::RB : 1024;
-    __shared__ __attribute__((aligned(1024))) char lds[kAttnRing * 2 * TILE]; // 32 keys and their values, four times
+    using B = AttnBack<D>;
+    constexpr int BM = 128, RING = B::RING;
+    __shared__ __attribute__((aligned(1024))) char lds[RING * B::SLOT + B::HELD]; // 32 keys and their values a slot; do
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const AttnWork w = attn_work(a.heads, a.tiles, CAUSAL);
     const AttnSeq seq = attn_seq<BM>(a, w.vt);
@@ -492,28 +507,36 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 1) void k_attn_d
     const int keys = CAUSAL ? min(seq.len, seq.tile * BM + BM) : seq.len, tiles = (keys + 31) / 32;
     const int subs = have < 1 ? 0 : CAUSAL ? q0 / 32 + 1 : tiles; // of this wavefront
     const uint32_t at = lds_address(lds);
+    const AttnLane<D> own(at + RING * B::SLOT);
 
     AttnDma<D, 32> fk, fv;
     fk.plan(a.ks, a.d);
     fv.plan(a.vs, a.d);
-    if (a.d != D) clear_tiles<kAttnRing * 2 * TILE>(lds);
-    auto slot = [&](int tile) { return at + (uint32_t)(tile % kAttnRing) * (2 * TILE); };
+    if (a.d != D) clear_tiles<RING * B::SLOT + B::HELD>(lds);
+    auto slot = [&](int tile) { return at + (uint32_t)(tile % RING) * B::SLOT; };
     auto issue = [&](int tile) {
         fk.issue(kp + (int64_t)tile * 32 * a.ks, slot(tile), keys - tile * 32);
-        fv.issue(vp + (int64_t)tile * 32 * a.vs, slot(tile) + TILE, keys - tile * 32);
+        fv.issue(vp + (int64_t)tile * 32 * a.vs, slot(tile) + B::TILE, keys - tile * 32);
     };
-    bf16x8 q[D / 16], d_o[D / 16];
+    bf16x8 q[D / 16], d_o[B::REGS];
     const int64_t row = seq.start + q0;
-    f32x16 s = zeros16(), dp;
+    if constexpr (B::OWN) {
+        AttnDma<D, 128> fo; // a wavefront's transfers are its own 32 rows
+        fo.plan(a.dos, a.d);
+        fo.issue(a.d_o + (int64_t)(seq.start + seq.tile * BM) * a.dos + (int64_t)head * a.d, at + RING * B::SLOT, seq.len - seq.tile * BM);
+    }
     issue(0);
+    f32x16 s = zeros16(), dp;
+    if constexpr (B::OWN) wait_vm<fk.N + fv.N>();
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) {
         q[ks] = along_mem(a.q + row * a.qs + (int64_t)head * a.d, a.qs, have, a.d, ks);
-        d_o[ks] = along_mem(a.d_o + row * a.dos + (int64_t)head * a.d, a.dos, have, a.d, ks);
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(along_mem(a.o + row * a.os + (int64_t)head * a.d, a.os, have, a.d, ks), d_o[ks], s, 0, 0, 0);
+        bf16x8 x;
+        if constexpr (B::OWN) x = own.along(wave * 32, ks);
+        else x = d_o[ks] = along_mem(a.d_o + row * a.dos + (int64_t)head * a.d, a.dos, have, a.d, ks);
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(along_mem(a.o + row * a.os + (int64_t)head * a.d, a.os, have, a.d, ks), x, s, 0, 0, 0);
     }
     const float nlse2 = me < have ? a.lse[(int64_t)head * a.rows + row + me] * -1.4426950408889634f : 0.f;
-    if (tiles > 1) issue(1);
     float delta = 0.f, rest = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) delta = row_of(i) == me ? s[i] : delta;
@@ -527,43 +550,32 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 1) void k_attn_d
     bf16x8 p[2], ds[2];
     bool apart = false;
 
+    if (RING > 2 && tiles > 1) issue(1);
     auto arrive = [&](int n) {
-        // this tile is there; the next one's transfers may still be under way
-        if (n + 1 < tiles) wait_vm<fk.N + fv.N>();
+        // this tile is there; with three slots the next one's transfers may still be under way
+        if (RING > 2 && n + 1 < tiles) wait_vm<fk.N + fv.N>();
         else wait_vm<0>();
         __syncthreads();
-        if (n + 2 < tiles) issue(n + 2); // in the place of the one that everybody has left behind
+        if (n + RING - 1 < tiles) issue(n + RING - 1); // in the place of the one that everybody has left behind
     };
-    // the vector work of a subtile; of queries that see keys up to `last`
-    bf16x8 pn[2], dn[2];
-    auto element = [&](int i) {
-        const float e = __builtin_amdgcn_exp2f(fmaf(s[i], a.c2, nlse2)), z = e * (dp[i] - delta);
-        rest += z;
-        pn[i >> 3][i & 7] = (bf16_t)e;
-        dn[i >> 3][i & 7] = (bf16_t)z;
-    };
-    auto taken = [&]() { p[0] = pn[0], p[1] = pn[1], ds[0] = dn[0], ds[1] = dn[1]; };
     int n = 0;
-    if (subs > 1) {
-        arrive(0);
-        pair_products<D>(s, dp, AttnLane<D>(slot(0)), AttnLane<D>(slot(0) + TILE), q, d_o);
+    for (; n < subs - 1; ++n) {
+        arrive(n);
+        const AttnLane<D> lk(slot(n)), lv(slot(n) + B::TILE);
+        pair_products<D>(s, dp, lk, lv, q, d_o, own, wave * 32);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) element(i);
-        taken();
-        for (n = 1; n < subs - 1; ++n) {
-            arrive(n);
-            pair_products<D>(s, dp, AttnLane<D>(slot(n)), AttnLane<D>(slot(n) + TILE), q, d_o);
-            const AttnLane<D> before(slot(n + kAttnRing - 1));
-            add_pair<D, true>(acc, y, before, before, ds, p, element);
-            taken();
+        for (int i = 0; i < 16; ++i) {
+            const float e = __builtin_amdgcn_exp2f(fmaf(s[i], a.c2, nlse2)), z = e * (dp[i] - delta);
+            rest += z;
+            p[i >> 3][i & 7] = (bf16_t)e;
+            ds[i >> 3][i & 7] = (bf16_t)z;
         }
-        const AttnLane<D> before(slot(n + kAttnRing - 1));
-        add_pair<D, true>(acc, y, before, before, ds, p, [](int) {});
+        pair_sums<D, true>(acc, y, lk, lk, ds, p);
     }
     if (subs > 0) { // the last subtile, where the mask ends
         arrive(n);
-        const AttnLane<D> lk(slot(n));
-        pair_products<D>(s, dp, lk, AttnLane<D>(slot(n) + TILE), q, d_o);
+        const AttnLane<D> lk(slot(n)), lv(slot(n) + B::TILE);
+        pair_products<D>(s, dp, lk, lv, q, d_o, own, wave * 32);
         const int last = CAUSAL ? me : seq.len - 1 - 32 * n;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -574,7 +586,7 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 1) void k_attn_d
             ds[i >> 3][i & 7] = (bf16_t)z;
         }
         apart = any_special<D>(lk, 0);
-        if (!apart) add_pair<D, true>(acc, y, lk, lk, ds, p, [](int) {});
+        if (!apart) pair_sums<D, true>(acc, y, lk, lk, ds, p);
         ++n;
     }
     for (; n < tiles; ++n) arrive(n); // what other wavefronts see
@@ -601,11 +613,11 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 1) void k_attn_d
 // dk and dv: 128 keys a workgroup, 32 a wavefront, which holds them, their values and both gradients in registers; 32 queries and their
 // do at a time in LDS, of all heads of the group one after the other.  S = q K^T has a key's scores in one column.
 // ---------------------------------------------------------------------------
-template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 1) void k_attn_dkv(const AttnArgs a)
+template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_dkv(const AttnArgs a)
 {
-    using T = AttnTile<D>;
-    constexpr int BN = 128, TILE = 32 * T::RB > 1024 ? 32 * T::RB : 1024, SLOT = 2 * TILE;
-    __shared__ __attribute__((aligned(1024))) char lds[kAttnRing * (SLOT + 256)]; // 32 queries and their do, four times; -lse log2(e) and delta
+    using B = AttnBack<D>;
+    constexpr int BN = 128, RING = B::RING;
+    __shared__ __attribute__((aligned(1024))) char lds[RING * B::SLOT + B::HELD + RING * 256]; // 32 queries and their do a slot; v; -lse log2(e) and delta
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), me = lane & 31;
     const AttnWork w = attn_work(a.kv_heads, a.tiles, false);
     const AttnSeq seq = attn_seq<BN>(a, w.vt);
@@ -614,111 +626,140 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 1) void k_attn_d
     const int64_t row = seq.start + key0;
     const int first = CAUSAL ? seq.tile * BN : 0, per = (seq.len - first + 31) / 32, tiles = per * a.group; // subtiles of a head, of all
     const uint32_t at = lds_address(lds);
+    const AttnLane<D> own(at + RING * B::SLOT);
 
     AttnDma<D, 32> fq, fd;
     fq.plan(a.qs, a.d);
     fd.plan(a.dos, a.d);
-    if (a.d != D) clear_tiles<kAttnRing * SLOT>(lds);
-    auto slot = [&](int tile) { return at + (uint32_t)(tile % kAttnRing) * SLOT; };
-    auto stats = [&](int tile) { return at + kAttnRing * SLOT + (uint32_t)(tile % kAttnRing) * 256; };
-    int f_head = hk * a.group, f_row = first, f_tile = 0; // the tile to be fetched next: head and first query, counted along instead of divided
+    if (a.d != D) clear_tiles<RING * B::SLOT + B::HELD>(lds);
+    auto slot = [&](int tile) { return at + (uint32_t)(tile % RING) * B::SLOT; };
+    auto stats = [&](int tile) { return at + RING * B::SLOT + B::HELD + (uint32_t)(tile % RING) * 256; };
+    // the tile to be fetched next: its number, how many of its head are left, and where its rows are
+    int f_tile = 0, f_rest = seq.len - first;
+    const bf16_t *f_q = a.q + (int64_t)(seq.start + first) * a.qs + (int64_t)hk * a.group * a.d;
+    const bf16_t *f_d = a.d_o + (int64_t)(seq.start + first) * a.dos + (int64_t)hk * a.group * a.d;
+    const float *f_s = (lane < 32 ? a.nlse2 : a.delta) + (int64_t)hk * a.group * a.rows + seq.start + first;
     auto issue = [&]() {
-        const int rest = seq.len - f_row;
-        const int64_t r = seq.start + f_row;
-        fq.issue(a.q + r * a.qs + (int64_t)f_head * a.d, slot(f_tile), rest);
-        fd.issue(a.d_o + r * a.dos + (int64_t)f_head * a.d, slot(f_tile) + TILE, rest);
+        fq.issue(f_q, slot(f_tile), f_rest);
+        fd.issue(f_d, slot(f_tile) + B::TILE, f_rest);
         // every wavefront fetches them, so that all have as many transfers under way
-        const float *from = (lane < 32 ? a.nlse2 : a.delta) + (int64_t)f_head * a.rows + r + min(me, rest - 1);
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
-                     : : "s"(__builtin_amdgcn_readfirstlane(stats(f_tile))), "v"(from) : "memory", "m0");
+                     : : "s"(__builtin_amdgcn_readfirstlane(stats(f_tile))), "v"(f_s + min(me, f_rest - 1)) : "memory", "m0");
         ++f_tile;
-        f_row += 32;
-        if (f_row >= seq.len) f_row = first, ++f_head;
+        f_rest -= 32;
+        f_q += 32 * a.qs, f_d += 32 * a.dos, f_s += 32;
+        if (f_rest <= 0) { // on to the next head
+            f_rest = seq.len - first;
+            f_q += a.d - (int64_t)per * 32 * a.qs, f_d += a.d - (int64_t)per * 32 * a.dos, f_s += a.rows - (int64_t)per * 32;
+        }
     };
+    bf16x8 k[D / 16], v[B::REGS];
+    if constexpr (B::OWN) {
+        AttnDma<D, 128> fv; // a wavefront's transfers are its own 32 rows
+        fv.plan(a.vs, a.d);
+        fv.issue(a.v + (int64_t)(seq.start + seq.tile * BN) * a.vs + (int64_t)hk * a.d, at + RING * B::SLOT, seq.len - seq.tile * BN);
+    }
     issue();
-    bf16x8 k[D / 16], v[D / 16];
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) {
         k[ks] = along_mem(a.k + row * a.ks + (int64_t)hk * a.d, a.ks, have, a.d, ks);
-        v[ks] = along_mem(a.v + row * a.vs + (int64_t)hk * a.d, a.vs, have, a.d, ks);
+        if constexpr (!B::OWN) v[ks] = along_mem(a.v + row * a.vs + (int64_t)hk * a.d, a.vs, have, a.d, ks);
     }
-    if (tiles > 1) issue();
+    if (RING > 2 && tiles > 1) issue();
     f32x16 dk[D / 32], dv[D / 32], s, dp;
 #pragma unroll
     for (int t = 0; t < D / 32; ++t) dk[t] = dv[t] = zeros16();
-    bf16x8 p[2], ds[2], pn[2], dn[2];
-    f32x4 nl[4], dl[4];
+    bf16x8 p[2], ds[2];
     typedef const __attribute__((address_space(3))) f32x4 *lds_f32x4;
     int n = 0; // tiles so far
     auto arrive = [&]() {
-        if (n + 1 < tiles) wait_vm<fq.N + fd.N + 1>();
+        if (RING > 2 && n + 1 < tiles) wait_vm<fq.N + fd.N + 1>();
         else wait_vm<0>();
         __syncthreads();
-        if (n + 2 < tiles) issue();
+        if (n + RING - 1 < tiles) issue();
         ++n;
     };
-    auto products = [&]() { // of the tile that has arrived
-        const uint32_t st = stats(n - 1) + 16 * (lane >> 5);
+    auto queries = [&]() { return AttnLane<D>(slot(n - 1)); }; // the tile that has arrived
+    auto grads = [&]() { return AttnLane<D>(slot(n - 1) + B::TILE); };
+    auto weigh = [&](auto in) { // p and ds; in(row): does the row see the lane's key
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-            nl[g] = *reinterpret_cast<lds_f32x4>(st + 32 * g);
-            dl[g] = *reinterpret_cast<lds_f32x4>(st + 128 + 32 * g);
+            const uint32_t st = stats(n - 1) + 16 * (lane >> 5) + 32 * g;
+            const f32x4 nl = *reinterpret_cast<lds_f32x4>(st), dl = *reinterpret_cast<lds_f32x4>(st + 128);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const int i = 4 * g + x;
+                const float e = __builtin_amdgcn_exp2f(fmaf(s[i], a.c2, nl[x])), z = e * (dp[i] - dl[x]);
+                p[i >> 3][i & 7] = (bf16_t)(in(row_of(i)) ? e : 0.f);
+                ds[i >> 3][i & 7] = (bf16_t)(in(row_of(i)) ? z : 0.f);
+            }
         }
-        pair_products<D>(s, dp, AttnLane<D>(slot(n - 1)), AttnLane<D>(slot(n - 1) + TILE), k, v);
     };
-    auto element = [&](int i) {
-        const float e = __builtin_amdgcn_exp2f(fmaf(s[i], a.c2, nl[i >> 2][i & 3]));
-        pn[i >> 3][i & 7] = (bf16_t)e;
-        dn[i >> 3][i & 7] = (bf16_t)(e * (dp[i] - dl[i >> 2][i & 3]));
-    };
-    auto taken = [&]() { p[0] = pn[0], p[1] = pn[1], ds[0] = dn[0], ds[1] = dn[1]; };
     // this wavefront's subtiles of a head: none, the first ones, where causal queries see none of its keys; then the diagonal, the main ones, and
     // one that ends with the sequence
     const int idle = have < 1 ? per : CAUSAL ? wave : 0, active = per - idle;
-    const bool odd_end = seq.len % 32 != 0;
-    const int middle = active - (CAUSAL && active > 0) - (odd_end && active > (CAUSAL ? 1 : 0));
+    const bool odd_end = seq.len % 32 != 0 && active > (CAUSAL ? 1 : 0);
+    const int middle = active - (CAUSAL && active > 0) - odd_end;
+    bool apart = false; // some subtile at a mask's border has to be added row by row
 #pragma unroll 1
-    for (int head = hk * a.group; head < (hk + 1) * a.group; ++head) {
+    for (int head = 0; head < a.group; ++head) {
         for (int i = 0; i < idle; ++i) arrive();
         if (active < 1) continue;
 #pragma unroll 1
         for (int side = 0; side < 2; ++side) {
-            if (side == 0 ? CAUSAL : odd_end && active > (CAUSAL ? 1 : 0)) {
+            if (side == 0 ? CAUSAL : odd_end) {
                 const int qr = side == 0 ? key0 : seq.len & ~31;
                 arrive();
-                products();
-                const int from = CAUSAL && qr == key0 ? me : 0, to = seq.len - qr; // the queries that see the lane's key
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const bool in = row_of(i) >= from && row_of(i) < to;
-                    element(i);
-                    pn[i >> 3][i & 7] = in ? pn[i >> 3][i & 7] : (bf16_t)0.f;
-                    dn[i >> 3][i & 7] = in ? dn[i >> 3][i & 7] : (bf16_t)0.f;
-                }
-                const AttnLane<D> lq(slot(n - 1)), ld(slot(n - 1) + TILE);
-                if (any_special<D>(lq, 0) || any_special<D>(ld, 0)) {
-                    const int64_t r0 = seq.start + qr, c0 = (int64_t)head * a.d;
-                    auto part = [&](int query, int) { return query >= from; };
-                    add_turned_apart<D>(dv, a.d_o + r0 * a.dos + c0, a.dos, to, a.d, pn, part);
-                    add_turned_apart<D>(dk, a.q + r0 * a.qs + c0, a.qs, to, a.d, dn, part);
+                if (any_special<D>(queries(), 0) || any_special<D>(grads(), 0)) {
+                    apart = true;
                 } else {
-                    add_pair<D, false>(dv, dk, ld, lq, pn, dn, [](int) {});
+                    pair_products<D>(s, dp, queries(), grads(), k, v, own, wave * 32);
+                    const int from = CAUSAL && qr == key0 ? me : 0, to = seq.len - qr; // the queries that see the lane's key
+                    weigh([&](int r) { return r >= from && r < to; });
+                    pair_sums<D, false>(dv, dk, grads(), queries(), p, ds);
                 }
             }
-            if (side == 0 && middle > 0) {
-                arrive();
-                products();
-#pragma unroll
-                for (int i = 0; i < 16; ++i) element(i);
-                taken();
-                for (int i = 1; i < middle; ++i) {
+            if (side == 0) {
+                for (int i = 0; i < middle; ++i) {
                     arrive();
-                    products();
-                    add_pair<D, false>(dv, dk, AttnLane<D>(slot(n + kAttnRing - 2) + TILE), AttnLane<D>(slot(n + kAttnRing - 2)), p, ds, element);
-                    taken();
+                    pair_products<D>(s, dp, queries(), grads(), k, v, own, wave * 32);
+                    weigh([](int) { return true; });
+                    pair_sums<D, false>(dv, dk, grads(), queries(), p, ds);
                 }
-                add_pair<D, false>(dv, dk, AttnLane<D>(slot(n - 1) + TILE), AttnLane<D>(slot(n - 1)), p, ds, [](int) {});
             }
+        }
+    }
+    if (have > 0 && apart) { // such subtiles again, their rows from memory
+#pragma unroll 1
+        for (int which = 0; which < 2 * a.group; ++which) {
+            const int head = hk * a.group + which / 2, qr = which % 2 == 0 ? key0 : seq.len & ~31, to = seq.len - qr;
+            if (which % 2 == 0 ? !CAUSAL : !odd_end) continue;
+            const int64_t r0 = seq.start + qr;
+            const bf16_t *qp = a.q + r0 * a.qs + (int64_t)head * a.d, *dp_ = a.d_o + r0 * a.dos + (int64_t)head * a.d;
+            const int64_t st = (int64_t)head * a.rows + r0;
+            s = zeros16(), dp = zeros16();
+            uint32_t bad = 0;
+#pragma unroll 1
+            for (int ks = 0; ks < D / 16; ++ks) {
+                const bf16x8 x = along_mem(qp, a.qs, to, a.d, ks), z = along_mem(dp_, a.dos, to, a.d, ks);
+                const bf16x8 kk = along_mem(a.k + row * a.ks + (int64_t)hk * a.d, a.ks, have, a.d, ks), vv = along_mem(a.v + row * a.vs + (int64_t)hk * a.d, a.vs, have, a.d, ks);
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, kk, s, 0, 0, 0);
+                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(z, vv, dp, 0, 0, 0);
+                bad |= special(x) | special(z);
+            }
+            if (!__any(bad != 0)) continue; // this one is in
+            const int from = CAUSAL && qr == key0 ? me : 0;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int r = row_of(i);
+                const bool in = r >= from && r < to;
+                const float e = in ? __builtin_amdgcn_exp2f(fmaf(s[i], a.c2, a.nlse2[st + min(r, to - 1)])) : 0.f;
+                p[i >> 3][i & 7] = (bf16_t)e;
+                ds[i >> 3][i & 7] = (bf16_t)(in ? e * (dp[i] - a.delta[st + min(r, to - 1)]) : 0.f);
+            }
+            auto part = [&](int query, int) { return query >= from; };
+            add_turned_apart<D>(dv, dp_, a.dos, to, a.d, p, part);
+            add_turned_apart<D>(dk, qp, a.qs, to, a.d, ds, part);
         }
     }
     if (have < 1) return;
