@@ -20,6 +20,8 @@ struct AttnArgs {
     int64_t dqs, dks, dvs;
     float *nlse2, *delta; // [heads][rows] each: -lse log2(e), do . o
     unsigned tiles; // tiles of a head, of all sequences together
+    int splits;     // of the queries that a tile of keys goes through, in dk and dv
+    float *part;    // [splits][rows][2][kv_heads d]: dk / scale and dv of the splits, where there are several
 };
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -438,7 +440,7 @@ template <int D> struct AttnBack {
 // s = (rows of the first tile) b1^T, dn = (rows of the second) b2^T, b2 from registers or from `own`; operands are read ahead
 template <int D>
 __device__ __forceinline__ void pair_products(f32x16 &s, f32x16 &dn, const AttnLane<D> &l1, const AttnLane<D> &l2, const bf16x8 (&b1)[D / 16],
-                                              const bf16x8 (&b2)[AttnBack<D>::REGS], const AttnLane<D> &own, int own_row)
+                                              const bf16x8 (&b2)[AttnBack<D>::REGS], const AttnLane<D> &own)
 {
     constexpr int N = D / 16, AHEAD = 2;
     constexpr bool OWN = AttnBack<D>::OWN;
@@ -446,7 +448,7 @@ __device__ __forceinline__ void pair_products(f32x16 &s, f32x16 &dn, const AttnL
     auto read = [&](int n) {
         f1[n % (AHEAD + 1)] = l1.along(0, n);
         f2[n % (AHEAD + 1)] = l2.along(0, n);
-        if constexpr (OWN) f3[n % (AHEAD + 1)] = own.along(own_row, n);
+        if constexpr (OWN) f3[n % (AHEAD + 1)] = own.along(0, n);
     };
 #pragma unroll
     for (int n = 0; n < AHEAD; ++n) read(n);
@@ -507,7 +509,7 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_d
     const int keys = CAUSAL ? min(seq.len, seq.tile * BM + BM) : seq.len, tiles = (keys + 31) / 32;
     const int subs = have < 1 ? 0 : CAUSAL ? q0 / 32 + 1 : tiles; // of this wavefront
     const uint32_t at = lds_address(lds);
-    const AttnLane<D> own(at + RING * B::SLOT);
+    const AttnLane<D> own(at + RING * B::SLOT + wave * 32 * AttnTile<D>::RB); // this wavefront's rows
 
     AttnDma<D, 32> fk, fv;
     fk.plan(a.ks, a.d);
@@ -532,7 +534,7 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_d
     for (int ks = 0; ks < D / 16; ++ks) {
         q[ks] = along_mem(a.q + row * a.qs + (int64_t)head * a.d, a.qs, have, a.d, ks);
         bf16x8 x;
-        if constexpr (B::OWN) x = own.along(wave * 32, ks);
+        if constexpr (B::OWN) x = own.along(0, ks);
         else x = d_o[ks] = along_mem(a.d_o + row * a.dos + (int64_t)head * a.d, a.dos, have, a.d, ks);
         s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(along_mem(a.o + row * a.os + (int64_t)head * a.d, a.os, have, a.d, ks), x, s, 0, 0, 0);
     }
@@ -562,7 +564,7 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_d
     for (; n < subs - 1; ++n) {
         arrive(n);
         const AttnLane<D> lk(slot(n)), lv(slot(n) + B::TILE);
-        pair_products<D>(s, dp, lk, lv, q, d_o, own, wave * 32);
+        pair_products<D>(s, dp, lk, lv, q, d_o, own);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const float e = __builtin_amdgcn_exp2f(fmaf(s[i], a.c2, nlse2)), z = e * (dp[i] - delta);
@@ -575,7 +577,7 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_d
     if (subs > 0) { // the last subtile, where the mask ends
         arrive(n);
         const AttnLane<D> lk(slot(n)), lv(slot(n) + B::TILE);
-        pair_products<D>(s, dp, lk, lv, q, d_o, own, wave * 32);
+        pair_products<D>(s, dp, lk, lv, q, d_o, own);
         const int last = CAUSAL ? me : seq.len - 1 - 32 * n;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -612,6 +614,8 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_d
 // ---------------------------------------------------------------------------
 // dk and dv: 128 keys a workgroup, 32 a wavefront, which holds them, their values and both gradients in registers; 32 queries and their
 // do at a time in LDS, of all heads of the group one after the other.  S = q K^T has a key's scores in one column.
+// The first keys of a long causal sequence have all of its queries to go through, and a launch ends with its longest workgroup, so the
+// queries may be dealt to several (attn_splits), whose sums another launch adds up in order.
 // ---------------------------------------------------------------------------
 template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_dkv(const AttnArgs a)
 {
@@ -619,14 +623,16 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_d
     constexpr int BN = 128, RING = B::RING;
     __shared__ __attribute__((aligned(1024))) char lds[RING * B::SLOT + B::HELD + RING * 256]; // 32 queries and their do a slot; v; -lse log2(e) and delta
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), me = lane & 31;
-    const AttnWork w = attn_work(a.kv_heads, a.tiles, false);
-    const AttnSeq seq = attn_seq<BN>(a, w.vt);
+    const AttnWork w = attn_work(a.kv_heads, a.tiles * a.splits, false);
+    const int split = w.vt % a.splits;
+    const AttnSeq seq = attn_seq<BN>(a, w.vt / a.splits);
     if (seq.len < 1) return;
     const int hk = w.head, key0 = seq.tile * BN + wave * 32, have = min(32, seq.len - key0);
     const int64_t row = seq.start + key0;
-    const int first = CAUSAL ? seq.tile * BN : 0, per = (seq.len - first + 31) / 32, tiles = per * a.group; // subtiles of a head, of all
+    const int first = CAUSAL ? seq.tile * BN : 0, per = (seq.len - first + 31) / 32; // subtiles of a head
+    const int from_tile = (int)((int64_t)per * a.group * split / a.splits), tiles = (int)((int64_t)per * a.group * (split + 1) / a.splits) - from_tile; // of this workgroup
     const uint32_t at = lds_address(lds);
-    const AttnLane<D> own(at + RING * B::SLOT);
+    const AttnLane<D> own(at + RING * B::SLOT + wave * 32 * AttnTile<D>::RB); // this wavefront's rows
 
     AttnDma<D, 32> fq, fd;
     fq.plan(a.qs, a.d);
@@ -634,11 +640,12 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_d
     if (a.d != D) clear_tiles<RING * B::SLOT + B::HELD>(lds);
     auto slot = [&](int tile) { return at + (uint32_t)(tile % RING) * B::SLOT; };
     auto stats = [&](int tile) { return at + RING * B::SLOT + B::HELD + (uint32_t)(tile % RING) * 256; };
-    // the tile to be fetched next: its number, how many of its head are left, and where its rows are
-    int f_tile = 0, f_rest = seq.len - first;
-    const bf16_t *f_q = a.q + (int64_t)(seq.start + first) * a.qs + (int64_t)hk * a.group * a.d;
-    const bf16_t *f_d = a.d_o + (int64_t)(seq.start + first) * a.dos + (int64_t)hk * a.group * a.d;
-    const float *f_s = (lane < 32 ? a.nlse2 : a.delta) + (int64_t)hk * a.group * a.rows + seq.start + first;
+    // the tile to be fetched next: its number, how many rows of its head are left, and where they are
+    const int head0 = hk * a.group + from_tile / per, skip = from_tile % per * 32;
+    int f_tile = 0, f_rest = seq.len - first - skip;
+    const bf16_t *f_q = a.q + (int64_t)(seq.start + first + skip) * a.qs + (int64_t)head0 * a.d;
+    const bf16_t *f_d = a.d_o + (int64_t)(seq.start + first + skip) * a.dos + (int64_t)head0 * a.d;
+    const float *f_s = (lane < 32 ? a.nlse2 : a.delta) + (int64_t)head0 * a.rows + seq.start + first + skip;
     auto issue = [&]() {
         fq.issue(f_q, slot(f_tile), f_rest);
         fd.issue(f_d, slot(f_tile) + B::TILE, f_rest);
@@ -659,7 +666,7 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_d
         fv.plan(a.vs, a.d);
         fv.issue(a.v + (int64_t)(seq.start + seq.tile * BN) * a.vs + (int64_t)hk * a.d, at + RING * B::SLOT, seq.len - seq.tile * BN);
     }
-    issue();
+    if (tiles > 0) issue();
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) {
         k[ks] = along_mem(a.k + row * a.ks + (int64_t)hk * a.d, a.ks, have, a.d, ks);
@@ -695,25 +702,27 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_d
             }
         }
     };
-    // this wavefront's subtiles of a head: none, the first ones, where causal queries see none of its keys; then the diagonal, the main ones, and
+    // this wavefront's subtiles of a head: the first ones, where causal queries see none of its keys; then the diagonal, the main ones, and
     // one that ends with the sequence
-    const int idle = have < 1 ? per : CAUSAL ? wave : 0, active = per - idle;
-    const bool odd_end = seq.len % 32 != 0 && active > (CAUSAL ? 1 : 0);
-    const int middle = active - (CAUSAL && active > 0) - odd_end;
+    const int idle = have < 1 ? per : CAUSAL ? wave : 0, odd_end = seq.len % 32 != 0 && per - idle > (CAUSAL ? 1 : 0);
     bool apart = false; // some subtile at a mask's border has to be added row by row
+    int left = tiles;
 #pragma unroll 1
-    for (int head = 0; head < a.group; ++head) {
-        for (int i = 0; i < idle; ++i) arrive();
-        if (active < 1) continue;
+    for (int j0 = from_tile % per; left > 0; j0 = 0) { // subtiles j0..j1 - 1 of a head
+        const int j1 = min(per, j0 + left);
+        left -= j1 - j0;
+        for (int j = j0; j < min(idle, j1); ++j) arrive();
+        if (idle >= j1) continue;
+        const int middle = min(j1, per - odd_end) - max(j0, idle + (CAUSAL ? 1 : 0));
 #pragma unroll 1
         for (int side = 0; side < 2; ++side) {
-            if (side == 0 ? CAUSAL : odd_end) {
+            if (side == 0 ? CAUSAL && j0 <= idle : odd_end && j1 == per) {
                 const int qr = side == 0 ? key0 : seq.len & ~31;
                 arrive();
                 if (any_special<D>(queries(), 0) || any_special<D>(grads(), 0)) {
                     apart = true;
                 } else {
-                    pair_products<D>(s, dp, queries(), grads(), k, v, own, wave * 32);
+                    pair_products<D>(s, dp, queries(), grads(), k, v, own);
                     const int from = CAUSAL && qr == key0 ? me : 0, to = seq.len - qr; // the queries that see the lane's key
                     weigh([&](int r) { return r >= from && r < to; });
                     pair_sums<D, false>(dv, dk, grads(), queries(), p, ds);
@@ -722,7 +731,7 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_d
             if (side == 0) {
                 for (int i = 0; i < middle; ++i) {
                     arrive();
-                    pair_products<D>(s, dp, queries(), grads(), k, v, own, wave * 32);
+                    pair_products<D>(s, dp, queries(), grads(), k, v, own);
                     weigh([](int) { return true; });
                     pair_sums<D, false>(dv, dk, grads(), queries(), p, ds);
                 }
@@ -733,7 +742,8 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_d
 #pragma unroll 1
         for (int which = 0; which < 2 * a.group; ++which) {
             const int head = hk * a.group + which / 2, qr = which % 2 == 0 ? key0 : seq.len & ~31, to = seq.len - qr;
-            if (which % 2 == 0 ? !CAUSAL : !odd_end) continue;
+            const int tile = which / 2 * per + (qr - first) / 32 - from_tile;
+            if ((which % 2 == 0 ? !CAUSAL : !odd_end) || tile < 0 || tile >= tiles) continue;
             const int64_t r0 = seq.start + qr;
             const bf16_t *qp = a.q + r0 * a.qs + (int64_t)head * a.d, *dp_ = a.d_o + r0 * a.dos + (int64_t)head * a.d;
             const int64_t st = (int64_t)head * a.rows + r0;
@@ -763,8 +773,46 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_d
         }
     }
     if (have < 1) return;
-    put_rows<D>(a.dk + row * a.dks + (int64_t)hk * a.d, a.dks, have, a.d, dk, a.scale);
-    put_rows<D>(a.dv + row * a.dvs + (int64_t)hk * a.d, a.dvs, have, a.d, dv, 1.f);
+    if (a.splits == 1) {
+        put_rows<D>(a.dk + row * a.dks + (int64_t)hk * a.d, a.dks, have, a.d, dk, a.scale);
+        put_rows<D>(a.dv + row * a.dvs + (int64_t)hk * a.d, a.dvs, have, a.d, dv, 1.f);
+        return;
+    }
+    const int64_t cols = (int64_t)a.kv_heads * a.d;
+    float *to = a.part + (((int64_t)split * a.rows + row + me) * 2 * a.kv_heads + hk) * a.d;
+    if (me < have) {
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int c = 32 * t + 8 * g + 4 * (lane >> 5);
+                if (c >= a.d) continue;
+                *reinterpret_cast<f32x4 *>(to + c) = f32x4{dk[t][4 * g], dk[t][4 * g + 1], dk[t][4 * g + 2], dk[t][4 * g + 3]};
+                *reinterpret_cast<f32x4 *>(to + cols + c) = f32x4{dv[t][4 * g], dv[t][4 * g + 1], dv[t][4 * g + 2], dv[t][4 * g + 3]};
+            }
+    }
+}
+
+// The splits' sums, in order: eight values a thread of dk and as many of dv.  Bound by memory.
+__global__ __launch_bounds__(256) void k_attn_join(const AttnArgs a)
+{
+    const int chunks = a.kv_heads * a.d / 8;
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, r = id / (2 * chunks);
+    const int c = (int)(id - r * 2 * chunks), first = min(max(a.off[0], 0), a.rows), end = min(max(a.off[a.batch], 0), a.rows);
+    if (r < first || r >= end) return;
+    const bool is_v = c >= chunks;
+    const float *from = a.part + r * 2 * a.kv_heads * a.d + (int64_t)c * 8;
+    f32x4 x = *reinterpret_cast<const f32x4 *>(from), y = *reinterpret_cast<const f32x4 *>(from + 4);
+    for (int s = 1; s < a.splits; ++s) {
+        from += (int64_t)a.rows * 2 * a.kv_heads * a.d;
+        x += *reinterpret_cast<const f32x4 *>(from);
+        y += *reinterpret_cast<const f32x4 *>(from + 4);
+    }
+    const float by = is_v ? 1.f : a.scale;
+    bf16x8 z;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) z[e] = (bf16_t)(x[e] * by), z[4 + e] = (bf16_t)(y[e] * by);
+    *reinterpret_cast<bf16x8 *>((is_v ? a.dv + r * a.dvs : a.dk + r * a.dks) + (int64_t)(is_v ? c - chunks : c) * 8) = z;
 }
 
 // ---------------------------------------------------------------------------
@@ -805,6 +853,21 @@ static AttnArgs attn_args(const pac_attn *a, const int32_t *off, int32_t batch, 
     return r;
 }
 static int64_t stat_bytes(const pac_attn *a, int64_t rows) { return (rows * a->heads * 4 + 255) / 256 * 256; }
+
+// Workgroups of dk and dv: as many as a launch needs to fill the card and to end evenly, if each then still has enough to do to pay for
+// sums that go through memory.  (There and back, us, without splits / with: 500 tokens of 64 heads on one key head 1040 / 83, 2048 tokens
+// 32/8 heads 429 / 256, 4001 + 6143 tokens 32/8 heads 2216 / 2149.  With 1536 workgroups wanted 6000 tokens of 16 heads take 453, not 430.)
+constexpr int64_t kAttnTarget = 1300, kAttnLeast = 32, kAttnSplits = 64; // workgroups wanted; subtiles worth one; at most
+static int attn_splits(const pac_attn *a, int32_t batch, int64_t rows)
+{
+    const int64_t groups = (rows / 128 + batch) * a->kv_heads, group = a->heads / a->kv_heads;
+    const int64_t subtiles = batch ? rows / batch * group / 32 : 0; // that a tile of keys goes through, on the average
+    int64_t s = kAttnTarget / (groups < 1 ? 1 : groups);
+    if (s > subtiles / kAttnLeast) s = subtiles / kAttnLeast;
+    return (int)(s < 1 ? 1 : s > kAttnSplits ? kAttnSplits : s);
+}
+static int64_t part_bytes(const pac_attn *a, int64_t rows, int64_t splits) { return splits < 2 ? 0 : rows * 2 * a->kv_heads * a->d * 4 * splits; }
+static int64_t attn_bytes(const pac_attn *a, int32_t batch, int64_t rows) { return 2 * stat_bytes(a, rows) + part_bytes(a, rows, attn_splits(a, batch, rows)); }
 
 template <typename F> static void by_width(int d, const F &f)
 {
@@ -855,7 +918,14 @@ pac_status pac_attn_forward(const pac_attn *a, const int32_t *offsets, int32_t b
 
 int64_t pac_attn_workspace_bytes(const pac_attn *a, int32_t batch, int64_t rows)
 {
-    return check_attn(a, batch, rows) == PAC_OK ? 2 * stat_bytes(a, rows) : -1;
+    if (check_attn(a, batch, rows) != PAC_OK) return -1;
+    // splits become fewer as tiles become more: room for as many (row, split) pairs as a call of at most this size may have
+    int64_t most = rows * (a->heads / a->kv_heads) / 32 / kAttnLeast, pairs;
+    most = most > kAttnSplits ? kAttnSplits : most;
+    pairs = most < 2 ? 0 : rows * most;
+    const int64_t filled = kAttnTarget * 128 / a->kv_heads + 128 * kAttnSplits;
+    if (pairs > filled) pairs = filled;
+    return 2 * stat_bytes(a, rows) + pairs * 2 * a->kv_heads * a->d * 4;
 }
 
 pac_status pac_attn_backward(const pac_attn *a, const int32_t *offsets, int32_t batch, int64_t rows, const void *q, int64_t q_stride,
@@ -873,7 +943,7 @@ pac_status pac_attn_backward(const pac_attn *a, const int32_t *offsets, int32_t 
     for (const AttnRows &m : {qm, km, vm, om, dom, dqm, dkm, dvm})
         if ((s = check_rows(m)) != PAC_OK) return s;
     if (!at_aligned(offsets, 4) || !at_aligned(lse, 4) || !at_aligned(workspace, 16)) return PAC_ERR_ALIGN;
-    const int64_t need = pac_attn_workspace_bytes(a, batch, rows);
+    const int64_t need = attn_bytes(a, batch, rows);
     if (workspace_bytes < need) return PAC_ERR_WORKSPACE;
     const Span qs = rows_span(qm, rows), ks = rows_span(km, rows), vs = rows_span(vm, rows), os = rows_span(om, rows);
     const Span ds = rows_span(dom, rows), ls(lse, rows * a->heads * 4), off(offsets, ((int64_t)batch + 1) * 4);
@@ -895,18 +965,21 @@ pac_status pac_attn_backward(const pac_attn *a, const int32_t *offsets, int32_t 
     r.lse = const_cast<float *>(lse);
     r.nlse2 = static_cast<float *>(workspace);
     r.delta = reinterpret_cast<float *>(static_cast<char *>(workspace) + stat_bytes(a, rows));
+    r.part = reinterpret_cast<float *>(static_cast<char *>(workspace) + 2 * stat_bytes(a, rows));
+    r.splits = attn_splits(a, batch, rows);
     (void)hipGetLastError();
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     by_width(a->d, [&](auto n) {
         constexpr int D = decltype(n)::value;
         if (a->causal) {
             hipLaunchKernelGGL((k_attn_dq<D, true>), dim3(r.tiles * r.heads), dim3(256), 0, st, r);
-            hipLaunchKernelGGL((k_attn_dkv<D, true>), dim3(r.tiles * r.kv_heads), dim3(256), 0, st, r);
+            hipLaunchKernelGGL((k_attn_dkv<D, true>), dim3(r.tiles * r.kv_heads * r.splits), dim3(256), 0, st, r);
         } else {
             hipLaunchKernelGGL((k_attn_dq<D, false>), dim3(r.tiles * r.heads), dim3(256), 0, st, r);
-            hipLaunchKernelGGL((k_attn_dkv<D, false>), dim3(r.tiles * r.kv_heads), dim3(256), 0, st, r);
+            hipLaunchKernelGGL((k_attn_dkv<D, false>), dim3(r.tiles * r.kv_heads * r.splits), dim3(256), 0, st, r);
         }
     });
+    if (r.splits > 1) hipLaunchKernelGGL(k_attn_join, dim3((unsigned)((rows * 2 * kc / 8 + 255) / 256)), dim3(256), 0, st, r);
     return hipGetLastError() == hipSuccess ? PAC_OK : PAC_ERR_DEVICE;
 }
 

@@ -304,3 +304,26 @@ def test_runtime_refuses():
     with pytest.raises(pb.PacError) as e:  # a result in an operand's place
         a.backward(q, k, v, off, o, lse, do, q, torch.empty_like(k), torch.empty_like(v))
     assert e.value.status == pb.PAC_ERR_RANGE
+
+
+@pytest.mark.parametrize("heads,kv,d,lens,causal", [(64, 1, 64, [500], True), (64, 1, 64, [500], False), (12, 1, 128, [1111, 300], True), (3, 3, 40, [2100], True),
+                                                    (16, 2, 96, [0, 1025, 0], False), (32, 2, 128, [640, 1, 33], True)])
+def test_queries_dealt_to_several_workgroups(heads, kv, d, lens, causal):
+    """Few tiles of keys with many queries each: partial sums through memory (the workspace is more than the two values a row), rows of no
+    sequence left alone."""
+    lead, tail = 3, 6
+    rows = lead + sum(lens) + tail
+    q, k, v, do = make(heads + d, rows, heads, kv, d)
+    a = rt.Attention(heads, d, kv_heads=kv, causal=causal)
+    assert pb.pac_attn_workspace_bytes(a._a, len(lens), rows) > 2 * ((rows * heads * 4 + 255) // 256 * 256)
+    off = rt.packed_offsets(lens) + lead
+    o, lse = torch.empty_like(q), torch.empty(heads, rows, device="cuda")
+    a.forward(q, k, v, off, o, lse)
+    dq, dk, dv = torch.full_like(q, 7.0), torch.full_like(k, 7.0), torch.full_like(v, 7.0)
+    a.backward(q, k, v, off, o, lse, do, dq, dk, dv)
+    check(a, lens, (o, lse, dq, dk, dv), q, k, v, do, d ** -0.5, causal, first=lead)
+    for t in (dq, dk, dv):
+        assert (t[:lead] == 7).all() and (t[-tail:] == 7).all()
+    again = torch.empty_like(dk)
+    a.backward(q, k, v, off, o, lse, do, dq, again, dv)
+    assert torch.equal(dk[lead:-tail], again[lead:-tail])
