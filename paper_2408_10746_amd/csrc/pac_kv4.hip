@@ -188,6 +188,7 @@ struct Kv4Attend {
 
 constexpr int kKvWaves = 4, kKvStep = 32; // wavefronts of a workgroup, tokens of a wavefront's step
 constexpr int kKvLeast = 256;             // tokens that are worth a workgroup of their own
+constexpr int kKvSplits = 128;            // of a sequence, at most
 
 // tokens of a split of a sequence of len tokens, and how many splits have any
 __host__ __device__ inline int kv4_per_split(int len, int splits)
@@ -207,50 +208,81 @@ __device__ __forceinline__ uint32_t pair_hi(bf16x2 a, bf16x2 b) { return __built
 // byte `at` of a lane's codes of V, as the bf16 pair (even value, odd value)
 template <int AT> __device__ __forceinline__ bf16x2 v_pair(const uint32_t *w, float s) { return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[AT / 4], s, AT % 4); }
 
-// what a lane holds of a step's 32 tokens: two tiles of 16 tokens of K, two groups of four tokens of V
-template <int NB> struct Kv4Step {
-    uint32_t k[2][NB], v[2][NB];
-    uint32_t ks[2][NB == 3 ? 3 : 1], vs[2][NB == 3 ? 3 : 1];
-    bool v_ok[2];
+// What a lane holds of a step's 32 tokens: two tiles of 16 tokens of K, two groups of four tokens of V.  Where a page has 32 tokens or
+// more (WIDE), a step lies in one page, whose place is the same for all lanes: its entry in the table comes through scalars, and a lane's
+// places are constant distances from there.  Else a lane looks up the pages of its tokens.  Entries are fetched a step before the codes, so that a
+// step waits for one trip to memory and not for two.
+template <int NB, bool WIDE> struct Kv4Step {
+    static constexpr int S = NB == 3 ? 3 : 1;
+    uint32_t k[2][NB], v[2][NB], ks[2][S], vs[2][S];
+    bool ok[2]; // the lane's group of V's tokens, which are the tokens of its scores, is there
 
-    __device__ __forceinline__ void load(const Kv4Attend &a, const int32_t *table, int head, int t0, int len, int lane)
+    // the lane's part of the tables: pages of its two tokens of K, of its two groups of V
+    struct Pages {
+        int k[WIDE ? 1 : 2], v[WIDE ? 1 : 2];
+        __device__ __forceinline__ void look(const Kv4Attend &a, const int32_t *table, int t0, int end, int lane)
+        {
+            if constexpr (WIDE) {
+                k[0] = t0 < end ? table[t0 >> a.c.shift] : -1;
+            } else {
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const int tk = t0 + 16 * x + (lane & 15), tv = t0 + 16 * x + 4 * (lane >> 4);
+                    k[x] = tk < end ? table[tk >> a.c.shift] : -1;
+                    v[x] = tv < end ? table[tv >> a.c.shift] : -1;
+                }
+            }
+        }
+    };
+    // codes and scales of a token of K at w and sc, of four tokens of V at w and sc
+    __device__ __forceinline__ void load_k(int x, const char *w, const char *sc, int g)
+    {
+        __builtin_memcpy(k[x], __builtin_assume_aligned(w, NB == 3 ? 4 : 4 * NB), 4 * NB);
+#pragma unroll
+        for (int j = 0; j < S; ++j) ks[x][j] = (uint8_t)sc[NB == 3 ? j : g * NB / 4];
+    }
+    __device__ __forceinline__ void load_v(int x, const char *w, const char *sc, int r)
+    {
+        __builtin_memcpy(v[x], __builtin_assume_aligned(w, NB == 3 ? 4 : 4 * NB), 4 * NB);
+#pragma unroll
+        for (int j = 0; j < S; ++j) vs[x][j] = reinterpret_cast<const uint32_t *>(sc)[NB == 3 ? j : r * NB / 16];
+    }
+    __device__ __forceinline__ void load(const Kv4Attend &a, const Pages &p, int head, int t0, int end, int lane)
     {
         const int r = lane & 15, g = lane >> 4, sh = a.c.shift, in = (1 << sh) - 1;
         const int64_t codes = (int64_t)(16 * NB) << sh;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-            const int tk = t0 + 16 * x + r, tv = t0 + 16 * x + 4 * g;
-            const int pk = tk < len ? table[tk >> sh] : -1, pv = tv < len ? table[tv >> sh] : -1;
-            const bool k_ok = pk >= 0 && pk < a.c.pages;
-            v_ok[x] = pv >= 0 && pv < a.c.pages;
+            ok[x] = false;
 #pragma unroll
             for (int j = 0; j < NB; ++j) k[x][j] = v[x][j] = 0;
 #pragma unroll
-            for (int j = 0; j < (NB == 3 ? 3 : 1); ++j) ks[x][j] = vs[x][j] = 0;
-            if (k_ok) {
-                const char *p = kv4_part(a.c, pk, head, NB);
-                const int tok = tk & in;
-                const char *w = p + (int64_t)tok * (16 * NB) + 4 * NB * g;
-                const uint8_t *s = reinterpret_cast<const uint8_t *>(p) + 2 * codes + (int64_t)tok * NB;
-                __builtin_memcpy(k[x], __builtin_assume_aligned(w, NB == 3 ? 4 : 4 * NB), 4 * NB);
-                if constexpr (NB == 3) {
+            for (int j = 0; j < S; ++j) ks[x][j] = vs[x][j] = 0;
+        }
+        if constexpr (WIDE) {
+            const int page = __builtin_amdgcn_readfirstlane(p.k[0]), tok = t0 & in;
+            if (page < 0 || page >= a.c.pages) return;
+            // (a page has places for all of the step's tokens, also past the sequence's end)
+            const char *at = kv4_part(a.c, page, head, NB), *kc = at + tok * (16 * NB), *kx = at + 2 * codes + tok * NB;
+            const char *vc = kc + codes, *vx = kx + ((int64_t)NB << sh);
 #pragma unroll
-                    for (int j = 0; j < 3; ++j) ks[x][j] = s[j];
-                } else {
-                    ks[x][0] = s[g * NB / 4];
-                }
+            for (int x = 0; x < 2; ++x) {
+                load_k(x, kc + (16 * x + r) * (16 * NB) + 4 * NB * g, kx + (16 * x + r) * NB, g);
+                load_v(x, vc + (4 * x + g) * (64 * NB) + r * (4 * NB), vx + (4 * x + g) * (4 * NB), r);
+                ok[x] = true;
             }
-            if (v_ok[x]) {
-                const char *p = kv4_part(a.c, pv, head, NB);
-                const int grp = (tv & in) >> 2;
-                const char *w = p + codes + (int64_t)grp * (64 * NB) + r * (4 * NB);
-                const char *s = p + 2 * codes + ((int64_t)NB << sh) + (int64_t)grp * (4 * NB);
-                __builtin_memcpy(v[x], __builtin_assume_aligned(w, NB == 3 ? 4 : 4 * NB), 4 * NB);
-                if constexpr (NB == 3) {
+        } else {
 #pragma unroll
-                    for (int j = 0; j < 3; ++j) vs[x][j] = reinterpret_cast<const uint32_t *>(s)[j];
-                } else {
-                    vs[x][0] = reinterpret_cast<const uint32_t *>(s)[r * NB / 16];
+            for (int x = 0; x < 2; ++x) {
+                const int tk = t0 + 16 * x + r & in, tv = t0 + 16 * x + 4 * g & in;
+                if (p.k[x] >= 0 && p.k[x] < a.c.pages) {
+                    const char *at = kv4_part(a.c, p.k[x], head, NB);
+                    load_k(x, at + tk * (16 * NB) + 4 * NB * g, at + 2 * codes + tk * NB, g);
+                }
+                if (p.v[x] >= 0 && p.v[x] < a.c.pages) {
+                    const char *at = kv4_part(a.c, p.v[x], head, NB);
+                    load_v(x, at + codes + (tv >> 2) * (64 * NB) + r * (4 * NB), at + 2 * codes + ((int64_t)NB << sh) + (tv >> 2) * (4 * NB), r);
+                    ok[x] = true;
                 }
             }
         }
@@ -261,10 +293,10 @@ template <int NB> struct Kv4Step {
 // S^T = K q^T, so that a lane has one head's scores of 8 tokens (its column of the result) and these are, in place, the operand of
 // o^T = V^T p^T, whose columns are heads again: maxima, sums and rescaling stay inside a lane or go over the four lanes of a head.
 // The wavefronts take steps of 32 tokens in turn, a step's loads ahead.
-template <int NB>
-__global__ __launch_bounds__(64 * kKvWaves) void k_kv4_attend(const Kv4Attend a)
+template <int NB, bool WIDE>
+__global__ __launch_bounds__(64 * kKvWaves, 3) void k_kv4_attend(const Kv4Attend a)
 {
-    constexpr int DP = 32 * NB;
+    constexpr int DP = 32 * NB, STRIDE = kKvWaves * kKvStep;
     __shared__ float join[kKvWaves][16][DP + 4];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     int id = blockIdx.x;
@@ -279,6 +311,10 @@ __global__ __launch_bounds__(64 * kKvWaves) void k_kv4_attend(const Kv4Attend a)
     const int32_t *table = a.table + b * a.table_stride;
     const int head0 = hk * a.group + tile * 16, mine = min(16, a.group - tile * 16);
 
+    Kv4Step<NB, WIDE> st;
+    typename Kv4Step<NB, WIDE>::Pages pages;
+    int t0 = begin + wave * kKvStep;
+    pages.look(a, table, t0, end, lane);
     bf16x8 q[NB];
     const bf16_t *qr = a.q + b * a.q_stride + (int64_t)(head0 + r) * a.c.d;
 #pragma unroll
@@ -292,12 +328,14 @@ __global__ __launch_bounds__(64 * kKvWaves) void k_kv4_attend(const Kv4Attend a)
     for (int n = 0; n < 2 * NB; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
     float top = -FLT_MAX, sum = 0.f; // scores are taken relative to `top`, which stays within 2^8 of the largest so far
 
-    Kv4Step<NB> st;
-    int t0 = begin + wave * kKvStep;
-    if (t0 < end) st.load(a, table, hk, t0, end, lane);
-    for (; t0 < end; t0 += kKvWaves * kKvStep) {
-        Kv4Step<NB> now = st;
-        if (t0 + kKvWaves * kKvStep < end) st.load(a, table, hk, t0 + kKvWaves * kKvStep, end, lane);
+    if (t0 < end) st.load(a, pages, hk, t0, end, lane);
+    pages.look(a, table, t0 + STRIDE, end, lane);
+    for (; t0 < end; t0 += STRIDE) {
+        Kv4Step<NB, WIDE> now = st;
+        if (t0 + STRIDE < end) {
+            st.load(a, pages, hk, t0 + STRIDE, end, lane);
+            pages.look(a, table, t0 + 2 * STRIDE, end, lane);
+        }
         f32x4 s[2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
@@ -311,15 +349,24 @@ __global__ __launch_bounds__(64 * kKvWaves) void k_kv4_attend(const Kv4Attend a)
                 s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[i], s[x], 0, 0, 0);
             }
         }
-        float most = -FLT_MAX;
+        // tokens that are not there, past the end or in a page outside the cache
+        const bool whole = t0 + kKvStep <= end && __all(now.ok[0] && now.ok[1]);
+        if (!whole) {
+            const int keep = end - t0 - 4 * g;
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
+            for (int x = 0; x < 2; ++x) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const bool there = now.v_ok[x] && t0 + 16 * x + 4 * g + i < end;
-                s[x][i] = there ? s[x][i] * a.c2 : -INFINITY;
-                most = fmaxf(most, s[x][i]);
+                for (int i = 0; i < 4; ++i) s[x][i] = now.ok[x] && 16 * x + i < keep ? s[x][i] : -INFINITY;
+                // V's may hold anything, no value among them: their scales become the least one
+                if (keep - 16 * x < 4) {
+                    const uint32_t mask = keep - 16 * x <= 0 ? 0u : (1u << 8 * (keep - 16 * x)) - 1u;
+#pragma unroll
+                    for (int j = 0; j < (NB == 3 ? 3 : 1); ++j) now.vs[x][j] &= mask;
+                }
             }
+        }
+        float most = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3]));
+        most = fmaxf(most, fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]))) * a.c2;
         if (__any(most > top + 8.f)) {
             most = fmaxf(most, __shfl_xor(most, 16, 64));
             most = fmaxf(most, __shfl_xor(most, 32, 64));
@@ -334,17 +381,10 @@ __global__ __launch_bounds__(64 * kKvWaves) void k_kv4_attend(const Kv4Attend a)
         for (int x = 0; x < 2; ++x)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float e = __builtin_amdgcn_exp2f(s[x][i] - top);
+                const float e = __builtin_amdgcn_exp2f(fmaf(s[x][i], a.c2, -top));
                 sum += e;
                 p[4 * x + i] = (bf16_t)e;
             }
-        // V: a token past the end may hold anything, no value among them: its scale becomes the least one
-        const int keep0 = end - t0 - 4 * g, keep1 = keep0 - 16;
-#pragma unroll
-        for (int j = 0; j < (NB == 3 ? 3 : 1); ++j) {
-            if (keep0 < 4) now.vs[0][j] &= keep0 <= 0 ? 0u : (1u << 8 * keep0) - 1u;
-            if (keep1 < 4) now.vs[1][j] &= keep1 <= 0 ? 0u : (1u << 8 * keep1) - 1u;
-        }
 #define PAC_KV4_PAIR(X, T, J) v_pair<(T) * NB + (J)>(now.v[X], kv4_scale(now.vs[X][NB == 3 ? (J) : 0] >> 8 * (T) & 255u))
 #define PAC_KV4_BYTE(J)                                                                                                           \
     if constexpr ((J) < NB) {                                                                                                     \
@@ -401,30 +441,44 @@ __global__ __launch_bounds__(64 * kKvWaves) void k_kv4_attend(const Kv4Attend a)
     }
 }
 
-// The splits of a sequence's head, in order.  One wavefront a head.
+// The splits of a sequence's head (at most kKvSplits), each four threads' worth of values for a set of splits, the sets in order.
 template <int NB>
-__global__ __launch_bounds__(64) void k_kv4_join(const Kv4Attend a)
+__global__ __launch_bounds__(256) void k_kv4_join(const Kv4Attend a)
 {
-    constexpr int DP = 32 * NB;
-    const int b = blockIdx.x / a.heads, h = blockIdx.x % a.heads, lane = threadIdx.x;
+    constexpr int DP = 32 * NB, SETS = 256 / DP;
+    __shared__ float by[kKvSplits], sums[SETS][DP], parts[4];
+    const int b = blockIdx.x / a.heads, h = blockIdx.x % a.heads, tid = threadIdx.x;
     const int len = kv4_tokens(a.lens[b], a.table_len, a.c.shift), per = kv4_per_split(len, a.splits);
     if (len <= per) return;
     const int n = (len + per - 1) / per;
     const float *part = a.part + ((int64_t)b * a.heads + h) * a.splits * (DP + 2);
+    // weights: every wavefront finds the largest score of all splits for itself
+    const int lane = tid & 63;
     float most = -FLT_MAX;
-    for (int s = 0; s < n; ++s) most = fmaxf(most, part[(int64_t)s * (DP + 2)]);
-    float l = 0.f, v[2] = {0.f, 0.f};
-    for (int s = 0; s < n; ++s) {
-        const float *p = part + (int64_t)s * (DP + 2);
-        const float by = __builtin_amdgcn_exp2f(p[0] - most);
-        l += by * p[1];
+    for (int s = lane; s < n; s += 64) most = fmaxf(most, part[(int64_t)s * (DP + 2)]);
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
-            if (lane + 64 * x < DP) v[x] += by * p[2 + lane + 64 * x];
+    for (int x = 1; x < 64; x *= 2) most = fmaxf(most, __shfl_xor(most, x, 64));
+    float l = 0.f;
+    for (int s = tid; s < n; s += 256) {
+        by[s] = __builtin_amdgcn_exp2f(part[(int64_t)s * (DP + 2)] - most);
+        l += by[s] * part[(int64_t)s * (DP + 2) + 1];
     }
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
-        if (lane + 64 * x < a.c.d) a.o[b * a.o_stride + (int64_t)h * a.c.d + lane + 64 * x] = (bf16_t)(l == 0.f ? 0.f : v[x] / l);
+    for (int x = 1; x < 64; x *= 2) l += __shfl_xor(l, x, 64);
+    if (lane == 0) parts[tid >> 6] = l;
+    __syncthreads();
+    l = (parts[0] + parts[1]) + (parts[2] + parts[3]);
+    const int set = tid / DP, at = tid % DP;
+    float v = 0.f;
+    if (set < SETS)
+        for (int s = set; s < n; s += SETS) v += by[s] * part[(int64_t)s * (DP + 2) + 2 + at];
+    if (set < SETS) sums[set][at] = v;
+    __syncthreads();
+    if (tid >= a.c.d) return;
+    v = sums[0][tid];
+#pragma unroll
+    for (int x = 1; x < SETS; ++x) v += sums[x][tid];
+    a.o[b * a.o_stride + (int64_t)h * a.c.d + tid] = (bf16_t)(l == 0.f ? 0.f : v / l);
 }
 
 // ---------------------------------------------------------------------------
@@ -453,7 +507,7 @@ static int kv4_splits(const pac_kv4 *c, int heads, int batch, int table_len)
     const int64_t base = (int64_t)batch * c->kv_heads * ((heads / c->kv_heads + 15) / 16), most = (int64_t)table_len * c->page;
     const int64_t want = (2048 + base - 1) / base, fit = (most + kKvLeast - 1) / kKvLeast;
     const int64_t s = want < fit ? want : fit;
-    return (int)(s < 1 ? 1 : s > 128 ? 128 : s);
+    return (int)(s < 1 ? 1 : s > kKvSplits ? kKvSplits : s);
 }
 static pac_status check_attend(const pac_kv4 *c, int32_t heads, int32_t batch, int32_t table_len)
 {
@@ -461,7 +515,7 @@ static pac_status check_attend(const pac_kv4 *c, int32_t heads, int32_t batch, i
     if (s != PAC_OK) return s;
     if (heads < 1 || heads > 4096 || heads % c->kv_heads || batch < 0 || table_len < 0) return PAC_ERR_SHAPE;
     if ((int64_t)table_len * c->page > INT32_MAX || (int64_t)batch * c->kv_heads * ((heads / c->kv_heads + 15) / 16) >= 1 << 23 ||
-        (int64_t)batch * heads >= 1 << 25)
+        (int64_t)batch * heads >= 1 << 23)
         return PAC_ERR_UNSUPPORTED;
     return PAC_OK;
 }
@@ -541,7 +595,7 @@ int64_t pac_kv4_attend_workspace_bytes(const pac_kv4 *c, int32_t heads, int32_t 
     const int64_t fit = ((int64_t)table_len * c->page + kKvLeast - 1) / kKvLeast;
     int64_t pairs = (2048 + 2 * base) / base + batch; // (sequence, split) pairs: want x batch <= 2048 / base + batch
     if (pairs > fit * batch) pairs = fit * batch;
-    if (pairs > 128 * (int64_t)batch) pairs = 128 * (int64_t)batch;
+    if (pairs > kKvSplits * (int64_t)batch) pairs = kKvSplits * (int64_t)batch;
     return (pairs * heads * (2 + 32 * kv4_blocks(c)) * 4 + 255) / 256 * 256;
 }
 
@@ -577,8 +631,9 @@ pac_status pac_kv4_attend(const pac_kv4 *c, int32_t heads, float scale, int32_t 
     const unsigned blocks = (unsigned)((int64_t)batch * c->kv_heads * a.tiles * splits);
     by_blocks(kv4_blocks(c), [&](auto n) {
         constexpr int NB = decltype(n)::value;
-        hipLaunchKernelGGL((k_kv4_attend<NB>), dim3(blocks), dim3(64 * kKvWaves), 0, st, a);
-        if (splits > 1) hipLaunchKernelGGL((k_kv4_join<NB>), dim3((unsigned)(batch * heads)), dim3(64), 0, st, a);
+        if (c->page >= kKvStep) hipLaunchKernelGGL((k_kv4_attend<NB, true>), dim3(blocks), dim3(64 * kKvWaves), 0, st, a);
+        else hipLaunchKernelGGL((k_kv4_attend<NB, false>), dim3(blocks), dim3(64 * kKvWaves), 0, st, a);
+        if (splits > 1) hipLaunchKernelGGL((k_kv4_join<NB>), dim3((unsigned)(batch * heads)), dim3(256), 0, st, a);
     });
     return hipGetLastError() == hipSuccess ? PAC_OK : PAC_ERR_DEVICE;
 }
