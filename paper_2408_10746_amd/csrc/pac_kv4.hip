@@ -183,11 +183,14 @@ struct Kv4Attend {
     int64_t q_stride;
     bf16_t *o;
     int64_t o_stride;
-    float *part; // [batch][heads][splits][2 + 32 NB]: largest score, sum, unscaled o
+    float *part;  // [batch][heads][splits][32 NB]: unscaled o of the splits
+    float2 *stat; // [batch][heads][splits]: largest score, sum
 };
 
-constexpr int kKvWaves = 4, kKvStep = 32; // wavefronts of a workgroup, tokens of a wavefront's step
+constexpr int kKvStep = 32;               // tokens of a wavefront's step
+constexpr int kKvShort = 1024;            // tokens that one workgroup of 16 wavefronts goes through instead of several of four
 constexpr int kKvLeast = 256;             // tokens that are worth a workgroup of their own
+constexpr int kKvTarget = 2048;            // workgroups wanted
 constexpr int kKvSplits = 128;            // of a sequence, at most
 
 // tokens of a split of a sequence of len tokens, and how many splits have any
@@ -293,11 +296,11 @@ template <int NB, bool WIDE> struct Kv4Step {
 // S^T = K q^T, so that a lane has one head's scores of 8 tokens (its column of the result) and these are, in place, the operand of
 // o^T = V^T p^T, whose columns are heads again: maxima, sums and rescaling stay inside a lane or go over the four lanes of a head.
 // The wavefronts take steps of 32 tokens in turn, a step's loads ahead.
-template <int NB, bool WIDE>
-__global__ __launch_bounds__(64 * kKvWaves, 3) void k_kv4_attend(const Kv4Attend a)
+template <int NB, bool WIDE, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 4) void k_kv4_attend(const Kv4Attend a)
 {
-    constexpr int DP = 32 * NB, STRIDE = kKvWaves * kKvStep;
-    __shared__ float join[kKvWaves][16][DP + 4];
+    constexpr int DP = 32 * NB, STRIDE = WAVES * kKvStep, PITCH = DP + 4;
+    extern __shared__ float join[]; // [WAVES][heads of a tile][PITCH]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     int id = blockIdx.x;
     const int split = id % a.splits;
@@ -305,7 +308,7 @@ __global__ __launch_bounds__(64 * kKvWaves, 3) void k_kv4_attend(const Kv4Attend
     const int tile = id % a.tiles;
     id /= a.tiles;
     const int hk = id % a.c.kv_heads, b = id / a.c.kv_heads;
-    const int len = kv4_tokens(a.lens[b], a.table_len, a.c.shift), per = kv4_per_split(len, a.splits);
+    const int len = kv4_tokens(a.lens[b], a.table_len, a.c.shift), per = WAVES == 16 ? len : kv4_per_split(len, a.splits);
     const int begin = (int64_t)split * per < len ? split * per : len, end = len - begin < per ? len : begin + per;
     if (split > 0 && begin >= end) return;
     const int32_t *table = a.table + b * a.table_stride;
@@ -406,80 +409,89 @@ __global__ __launch_bounds__(64 * kKvWaves, 3) void k_kv4_attend(const Kv4Attend
     sum += __shfl_xor(sum, 32, 64);
 
     // the wavefronts' results, each relative to its own `top`
-    float *row = join[wave][r];
+    const int heads = min(16, a.group);
+    auto joined = [&](int w, int h) { return join + (w * heads + h) * PITCH; };
+    float *row = joined(wave, r);
+    if (r < mine) {
 #pragma unroll
-    for (int j = 0; j < NB; ++j)
+        for (int j = 0; j < NB; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int at = kv4_v_at<NB>(4 * g + i, j);
-            row[at] = acc[2 * j][i];
-            row[at + 1] = acc[2 * j + 1][i];
+            for (int i = 0; i < 4; ++i) {
+                const int at = kv4_v_at<NB>(4 * g + i, j);
+                row[at] = acc[2 * j][i];
+                row[at + 1] = acc[2 * j + 1][i];
+            }
+        if (g == 0) {
+            row[DP] = top;
+            row[DP + 1] = sum;
         }
-    if (g == 0) {
-        row[DP] = top;
-        row[DP + 1] = sum;
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < mine * DP; e += 64 * kKvWaves) {
+    for (int e = threadIdx.x; e < mine * DP; e += 64 * WAVES) {
         const int h = e / DP, at = e % DP;
-        float most = join[0][h][DP], l = 0.f, v = 0.f;
+        float most = joined(0, h)[DP], l = 0.f, v = 0.f;
 #pragma unroll
-        for (int w = 1; w < kKvWaves; ++w) most = fmaxf(most, join[w][h][DP]);
+        for (int w = 1; w < WAVES; ++w) most = fmaxf(most, joined(w, h)[DP]);
 #pragma unroll
-        for (int w = 0; w < kKvWaves; ++w) {
-            const float by = __builtin_amdgcn_exp2f(join[w][h][DP] - most);
-            l += by * join[w][h][DP + 1];
-            v += by * join[w][h][at];
+        for (int w = 0; w < WAVES; ++w) {
+            const float by = __builtin_amdgcn_exp2f(joined(w, h)[DP] - most);
+            l += by * joined(w, h)[DP + 1];
+            v += by * joined(w, h)[at];
         }
         if (len <= per) { // the whole sequence was this workgroup's
             if (at < a.c.d) a.o[b * a.o_stride + (int64_t)(head0 + h) * a.c.d + at] = (bf16_t)(l == 0.f ? 0.f : v / l);
         } else {
-            float *part = a.part + (((int64_t)b * a.heads + head0 + h) * a.splits + split) * (DP + 2);
-            part[2 + at] = v;
-            if (at == 0) part[0] = most, part[1] = l;
+            const int64_t to = ((int64_t)b * a.heads + head0 + h) * a.splits + split;
+            a.part[to * DP + at] = v;
+            if (at == 0) a.stat[to] = float2{most, l};
         }
     }
 }
 
-// The splits of a sequence's head (at most kKvSplits), each four threads' worth of values for a set of splits, the sets in order.
+// The splits of a sequence's head (at most kKvSplits): a thread adds up four values of every SETS-th split, then the sets are added in order.
 template <int NB>
 __global__ __launch_bounds__(256) void k_kv4_join(const Kv4Attend a)
 {
-    constexpr int DP = 32 * NB, SETS = 256 / DP;
-    __shared__ float by[kKvSplits], sums[SETS][DP], parts[4];
+    constexpr int DP = 32 * NB, QUADS = DP / 4, SETS = 256 / QUADS;
+    __shared__ float by[kKvSplits], parts[4];
+    __shared__ f32x4 sums[SETS][QUADS];
     const int b = blockIdx.x / a.heads, h = blockIdx.x % a.heads, tid = threadIdx.x;
     const int len = kv4_tokens(a.lens[b], a.table_len, a.c.shift), per = kv4_per_split(len, a.splits);
     if (len <= per) return;
     const int n = (len + per - 1) / per;
-    const float *part = a.part + ((int64_t)b * a.heads + h) * a.splits * (DP + 2);
+    const float2 *stat = a.stat + ((int64_t)b * a.heads + h) * a.splits;
+    const f32x4 *part = reinterpret_cast<const f32x4 *>(a.part + ((int64_t)b * a.heads + h) * a.splits * DP);
     // weights: every wavefront finds the largest score of all splits for itself
     const int lane = tid & 63;
     float most = -FLT_MAX;
-    for (int s = lane; s < n; s += 64) most = fmaxf(most, part[(int64_t)s * (DP + 2)]);
+    for (int s = lane; s < n; s += 64) most = fmaxf(most, stat[s].x);
 #pragma unroll
     for (int x = 1; x < 64; x *= 2) most = fmaxf(most, __shfl_xor(most, x, 64));
     float l = 0.f;
-    for (int s = tid; s < n; s += 256) {
-        by[s] = __builtin_amdgcn_exp2f(part[(int64_t)s * (DP + 2)] - most);
-        l += by[s] * part[(int64_t)s * (DP + 2) + 1];
+    if (tid < n) {
+        by[tid] = __builtin_amdgcn_exp2f(stat[tid].x - most);
+        l = by[tid] * stat[tid].y;
     }
 #pragma unroll
     for (int x = 1; x < 64; x *= 2) l += __shfl_xor(l, x, 64);
     if (lane == 0) parts[tid >> 6] = l;
     __syncthreads();
     l = (parts[0] + parts[1]) + (parts[2] + parts[3]);
-    const int set = tid / DP, at = tid % DP;
-    float v = 0.f;
-    if (set < SETS)
-        for (int s = set; s < n; s += SETS) v += by[s] * part[(int64_t)s * (DP + 2) + 2 + at];
-    if (set < SETS) sums[set][at] = v;
+    const int set = tid / QUADS, at = tid % QUADS;
+    if (set < SETS) {
+        f32x4 v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+        for (int s = set; s < n; s += SETS) v += by[s] * part[(int64_t)s * QUADS + at];
+        sums[set][at] = v;
+    }
     __syncthreads();
     if (tid >= a.c.d) return;
-    v = sums[0][tid];
+    float v = 0.f;
 #pragma unroll
-    for (int x = 1; x < SETS; ++x) v += sums[x][tid];
+    for (int x = 0; x < SETS; ++x) v += sums[x][tid / 4][tid % 4];
     a.o[b * a.o_stride + (int64_t)h * a.c.d + tid] = (bf16_t)(l == 0.f ? 0.f : v / l);
 }
+static_assert(kKvSplits <= 256, "a thread a split");
 
 // ---------------------------------------------------------------------------
 // host
@@ -501,11 +513,13 @@ static Kv4 kv4_of(const pac_kv4 *c)
     return Kv4{static_cast<char *>(c->at), c->pages, shift, c->kv_heads, c->d};
 }
 
-// Splits of the long axis: workgroups for eight a compute unit, none of fewer than kKvLeast tokens.
+// Splits of the long axis: workgroups for eight a compute unit, none of fewer than kKvLeast tokens.  Short sequences that leave most of
+// the card idle take one workgroup of 16 wavefronts each (0 splits), which saves the second launch.
 static int kv4_splits(const pac_kv4 *c, int heads, int batch, int table_len)
 {
     const int64_t base = (int64_t)batch * c->kv_heads * ((heads / c->kv_heads + 15) / 16), most = (int64_t)table_len * c->page;
-    const int64_t want = (2048 + base - 1) / base, fit = (most + kKvLeast - 1) / kKvLeast;
+    const int64_t want = (kKvTarget + base - 1) / base, fit = (most + kKvLeast - 1) / kKvLeast;
+    if (most <= kKvShort && base <= 256 && fit > 1) return 0;
     const int64_t s = want < fit ? want : fit;
     return (int)(s < 1 ? 1 : s > kKvSplits ? kKvSplits : s);
 }
@@ -521,7 +535,7 @@ static pac_status check_attend(const pac_kv4 *c, int32_t heads, int32_t batch, i
 }
 static int64_t attend_bytes(const pac_kv4 *c, int32_t heads, int32_t batch, int splits)
 {
-    return splits < 2 ? 0 : ((int64_t)batch * heads * splits * (2 + 32 * kv4_blocks(c)) * 4 + 255) / 256 * 256;
+    return splits < 2 ? 0 : (int64_t)batch * heads * splits * (2 + 32 * kv4_blocks(c)) * 4;
 }
 
 template <typename F> static void by_blocks(int nb, const F &f)
@@ -593,10 +607,10 @@ int64_t pac_kv4_attend_workspace_bytes(const pac_kv4 *c, int32_t heads, int32_t 
     // splits grow as the batch shrinks: room for the most partial results that a batch of at most this size makes
     const int64_t base = (int64_t)c->kv_heads * ((heads / c->kv_heads + 15) / 16);
     const int64_t fit = ((int64_t)table_len * c->page + kKvLeast - 1) / kKvLeast;
-    int64_t pairs = (2048 + 2 * base) / base + batch; // (sequence, split) pairs: want x batch <= 2048 / base + batch
+    int64_t pairs = (kKvTarget + 2 * base) / base + batch; // (sequence, split) pairs: want x batch <= kKvTarget / base + batch
     if (pairs > fit * batch) pairs = fit * batch;
     if (pairs > kKvSplits * (int64_t)batch) pairs = kKvSplits * (int64_t)batch;
-    return (pairs * heads * (2 + 32 * kv4_blocks(c)) * 4 + 255) / 256 * 256;
+    return pairs * heads * (2 + 32 * kv4_blocks(c)) * 4;
 }
 
 pac_status pac_kv4_attend(const pac_kv4 *c, int32_t heads, float scale, int32_t batch, const int32_t *table, int32_t table_len,
@@ -622,19 +636,27 @@ pac_status pac_kv4_attend(const pac_kv4 *c, int32_t heads, float scale, int32_t 
     a.c = kv4_of(c);
     a.heads = heads; a.group = heads / c->kv_heads; a.tiles = (a.group + 15) / 16;
     a.c2 = scale * 1.4426950408889634f;
-    a.table = table; a.lens = lens; a.table_len = table_len; a.splits = splits; a.table_stride = table_stride;
+    a.table = table; a.lens = lens; a.table_len = table_len; a.splits = splits < 1 ? 1 : splits; a.table_stride = table_stride;
     a.q = static_cast<const bf16_t *>(q); a.q_stride = q_stride;
     a.o = static_cast<bf16_t *>(o); a.o_stride = o_stride;
     a.part = static_cast<float *>(workspace);
+    a.stat = reinterpret_cast<float2 *>(a.part + (int64_t)batch * heads * a.splits * 32 * kv4_blocks(c));
     (void)hipGetLastError();
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    const unsigned blocks = (unsigned)((int64_t)batch * c->kv_heads * a.tiles * splits);
+    const unsigned blocks = (unsigned)((int64_t)batch * c->kv_heads * a.tiles * a.splits);
+    const int waves = splits ? 4 : 16, lds = waves * (a.group < 16 ? a.group : 16) * (32 * kv4_blocks(c) + 4) * 4;
+    bool fits = true;
     by_blocks(kv4_blocks(c), [&](auto n) {
         constexpr int NB = decltype(n)::value;
-        if (c->page >= kKvStep) hipLaunchKernelGGL((k_kv4_attend<NB, true>), dim3(blocks), dim3(64 * kKvWaves), 0, st, a);
-        else hipLaunchKernelGGL((k_kv4_attend<NB, false>), dim3(blocks), dim3(64 * kKvWaves), 0, st, a);
-        if (splits > 1) hipLaunchKernelGGL((k_kv4_join<NB>), dim3((unsigned)(batch * heads)), dim3(256), 0, st, a);
+        auto go = [&](auto kernel) {
+            if (lds > 64 << 10) fits = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess;
+            if (fits) hipLaunchKernelGGL(kernel, dim3(blocks), dim3(64 * waves), lds, st, a);
+        };
+        if (splits) c->page >= kKvStep ? go(k_kv4_attend<NB, true, 4>) : go(k_kv4_attend<NB, false, 4>);
+        else c->page >= kKvStep ? go(k_kv4_attend<NB, true, 16>) : go(k_kv4_attend<NB, false, 16>);
+        if (fits && splits > 1) hipLaunchKernelGGL((k_kv4_join<NB>), dim3((unsigned)(batch * heads)), dim3(256), 0, st, a);
     });
+    if (!fits) return PAC_ERR_DEVICE;
     return hipGetLastError() == hipSuccess ? PAC_OK : PAC_ERR_DEVICE;
 }
 
