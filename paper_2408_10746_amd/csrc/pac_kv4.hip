@@ -44,24 +44,25 @@ struct Kv4Io {
     const int64_t *slots;
     void *k, *v;
     int64_t k_stride, v_stride;
-    int64_t units; // rows x kv_heads x 2 NB blocks
+    int rows;
+    int64_t threads; // rows in fours x kv_heads x 2 x 16 NB
 };
 
-// Where thread `id` of a conversion works: four threads a block of 32, eight values each; K's blocks of a head, then V's.
+// Where thread `id` of a conversion works: four threads a block of 32, eight values each.  Four rows of one head's keys, then of its
+// values, lie next to each other, because four tokens of V share their bytes' lines and should meet in one wavefront.
 template <int NB> struct Kv4Unit {
-    int64_t row, slot;
-    int head, col; // first value of eight
+    int64_t slot;
+    int row, head, col; // col: first value of eight
     bool is_v;
     __device__ __forceinline__ Kv4Unit(const Kv4Io &a, int64_t id)
     {
-        const int64_t u = id >> 2;
-        const int64_t rh = u / (2 * NB);
-        const int b = (int)(u - rh * (2 * NB));
-        row = rh / a.c.kv_heads;
-        head = (int)(rh - row * a.c.kv_heads);
-        is_v = b >= NB;
-        col = (is_v ? b - NB : b) * 32 + (int)(id & 3) * 8;
-        slot = a.slots[row];
+        const uint32_t part = (uint32_t)(id / (16 * NB)), in = (uint32_t)(id - (int64_t)part * (16 * NB)); // four rows of a head's keys or values
+        const uint32_t heads = part >> 1, rows = heads / (uint32_t)a.c.kv_heads;
+        is_v = part & 1;
+        head = (int)(heads - rows * (uint32_t)a.c.kv_heads);
+        row = (int)(4 * rows + in / (4 * NB));
+        col = (int)(in % (4 * NB)) * 8;
+        slot = row < a.rows ? a.slots[row] : -1;
         if (slot >> a.c.shift >= a.c.pages) slot = -1;
     }
 };
@@ -88,10 +89,10 @@ template <typename T, int NB, bool VEC>
 __global__ __launch_bounds__(256) void k_kv4_write(const Kv4Io a)
 {
     const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if ((id >> 2) >= a.units) return; // whole groups of four lanes leave: the exchanges below stay within four
+    if (id >= a.threads) return; // whole groups of four lanes leave, here and below: the exchanges stay within four
     const Kv4Unit<NB> u(a, id);
-    if (u.slot < 0) return; // all lanes of the row
-    const T *src = static_cast<const T *>(u.is_v ? a.v : a.k) + u.row * (u.is_v ? a.v_stride : a.k_stride) + (int64_t)u.head * a.c.d + u.col;
+    if (u.slot < 0) return;
+    const T *src = static_cast<const T *>(u.is_v ? a.v : a.k) + (int64_t)u.row * (u.is_v ? a.v_stride : a.k_stride) + (int64_t)u.head * a.c.d + u.col;
     float v[8];
     if (u.col >= a.c.d) {
 #pragma unroll
@@ -141,7 +142,7 @@ template <typename T, int NB, bool VEC>
 __global__ __launch_bounds__(256) void k_kv4_read(const Kv4Io a)
 {
     const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if ((id >> 2) >= a.units) return;
+    if (id >= a.threads) return;
     const Kv4Unit<NB> u(a, id);
     if (u.slot < 0 || u.col >= a.c.d) return;
     const int tok = (int)(u.slot & ((1 << a.c.shift) - 1));
@@ -157,7 +158,7 @@ __global__ __launch_bounds__(256) void k_kv4_read(const Kv4Io a)
     const bf16x2 p0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0), p1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1);
     const bf16x2 p2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2), p3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3);
     const bf16x8 r{p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
-    T *dst = static_cast<T *>(u.is_v ? a.v : a.k) + u.row * (u.is_v ? a.v_stride : a.k_stride) + (int64_t)u.head * a.c.d + u.col;
+    T *dst = static_cast<T *>(u.is_v ? a.v : a.k) + (int64_t)u.row * (u.is_v ? a.v_stride : a.k_stride) + (int64_t)u.head * a.c.d + u.col;
     if constexpr (!VEC) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) dst[e] = (T)r[e];
@@ -562,8 +563,9 @@ static pac_status kv4_convert(const pac_kv4 *c, int64_t rows, const int64_t *slo
     if (shares(cache, {ks, vs, sl}) || (read && (shares(ks, {vs, sl}) || shares(vs, {sl})))) return PAC_ERR_RANGE;
     if (c->pages == 0) return PAC_OK;
     const int nb = kv4_blocks(c);
-    const int64_t units = rows * c->kv_heads * 2 * nb, blocks = (units * 4 + 255) / 256;
-    const Kv4Io a{kv4_of(c), slots, k, v, k_stride, v_stride, units};
+    const int64_t threads = (rows + 3) / 4 * c->kv_heads * 2 * 16 * nb, blocks = (threads + 255) / 256;
+    if (blocks >= 1 << 24) return PAC_ERR_UNSUPPORTED;
+    const Kv4Io a{kv4_of(c), slots, k, v, k_stride, v_stride, (int)rows, threads};
     const bool vec = kv_aligned(k, 16) && kv_aligned(v, 16) && k_stride * size % 16 == 0 && v_stride * size % 16 == 0;
     (void)hipGetLastError();
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
