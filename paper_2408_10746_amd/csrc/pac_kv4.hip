@@ -212,8 +212,8 @@ __device__ __forceinline__ uint32_t pair_hi(bf16x2 a, bf16x2 b) { return __built
 // byte `at` of a lane's codes of V, as the bf16 pair (even value, odd value)
 template <int AT> __device__ __forceinline__ bf16x2 v_pair(const uint32_t *w, float s) { return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[AT / 4], s, AT % 4); }
 
-// What a lane holds of a step's 32 tokens: two tiles of 16 tokens of K, two groups of four tokens of V.  Where a page has 32 tokens or
-// more (WIDE), a step lies in one page, whose place is the same for all lanes: its entry in the table comes through scalars, and a lane's
+// What a lane holds of a step's 32 tokens: two tiles of 16 tokens of K, two groups of four tokens of V.  Where a page has 16 tokens or
+// more (WIDE), a tile lies in one page, whose place is the same for all lanes: its entry in the table comes through scalars, and a lane's
 // places are constant distances from there.  Else a lane looks up the pages of its tokens.  Entries are fetched a step before the codes, so that a
 // step waits for one trip to memory and not for two.
 template <int NB, bool WIDE> struct Kv4Step {
@@ -223,11 +223,12 @@ template <int NB, bool WIDE> struct Kv4Step {
 
     // the lane's part of the tables: pages of its two tokens of K, of its two groups of V
     struct Pages {
-        int k[WIDE ? 1 : 2], v[WIDE ? 1 : 2];
+        int k[2], v[WIDE ? 1 : 2]; // (WIDE: a tile's keys and values are in one page)
         __device__ __forceinline__ void look(const Kv4Attend &a, const int32_t *table, int t0, int end, int lane)
         {
             if constexpr (WIDE) {
-                k[0] = t0 < end ? table[t0 >> a.c.shift] : -1;
+#pragma unroll
+                for (int x = 0; x < 2; ++x) k[x] = t0 + 16 * x < end ? table[(t0 + 16 * x) >> a.c.shift] : -1;
             } else {
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
@@ -264,15 +265,14 @@ template <int NB, bool WIDE> struct Kv4Step {
             for (int j = 0; j < S; ++j) ks[x][j] = vs[x][j] = 0;
         }
         if constexpr (WIDE) {
-            const int page = __builtin_amdgcn_readfirstlane(p.k[0]), tok = t0 & in;
-            if (page < 0 || page >= a.c.pages) return;
-            // (a page has places for all of the step's tokens, also past the sequence's end)
-            const char *at = kv4_part(a.c, page, head, NB), *kc = at + tok * (16 * NB), *kx = at + 2 * codes + tok * NB;
-            const char *vc = kc + codes, *vx = kx + ((int64_t)NB << sh);
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                load_k(x, kc + (16 * x + r) * (16 * NB) + 4 * NB * g, kx + (16 * x + r) * NB, g);
-                load_v(x, vc + (4 * x + g) * (64 * NB) + r * (4 * NB), vx + (4 * x + g) * (4 * NB), r);
+                const int page = __builtin_amdgcn_readfirstlane(p.k[x]), tok = t0 + 16 * x & in;
+                if (page < 0 || page >= a.c.pages) continue;
+                // (a page has places for all of the tile's tokens, also past the sequence's end)
+                const char *at = kv4_part(a.c, page, head, NB), *kc = at + tok * (16 * NB), *kx = at + 2 * codes + tok * NB;
+                load_k(x, kc + r * (16 * NB) + 4 * NB * g, kx + r * NB, g);
+                load_v(x, kc + codes + g * (64 * NB) + r * (4 * NB), kx + ((int64_t)NB << sh) + g * (4 * NB), r);
                 ok[x] = true;
             }
         } else {
@@ -654,8 +654,8 @@ pac_status pac_kv4_attend(const pac_kv4 *c, int32_t heads, float scale, int32_t 
             if (lds > 64 << 10) fits = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess;
             if (fits) hipLaunchKernelGGL(kernel, dim3(blocks), dim3(64 * waves), lds, st, a);
         };
-        if (splits) c->page >= kKvStep ? go(k_kv4_attend<NB, true, 4>) : go(k_kv4_attend<NB, false, 4>);
-        else c->page >= kKvStep ? go(k_kv4_attend<NB, true, 16>) : go(k_kv4_attend<NB, false, 16>);
+        if (splits) c->page >= 16 ? go(k_kv4_attend<NB, true, 4>) : go(k_kv4_attend<NB, false, 4>);
+        else c->page >= 16 ? go(k_kv4_attend<NB, true, 16>) : go(k_kv4_attend<NB, false, 16>);
         if (fits && splits > 1) hipLaunchKernelGGL((k_kv4_join<NB>), dim3((unsigned)(batch * heads)), dim3(256), 0, st, a);
     });
     if (!fits) return PAC_ERR_DEVICE;
