@@ -373,20 +373,27 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_f
             fv.issue(vp + (int64_t)(t + 1) * BK * a.vs, to + TILE, keys - (t + 1) * BK);
         }
     };
-    int t = 0;
-    for (; t < full; ++t) {
+    const AttnLane<D> lk0(at), lv0(at + TILE);
+    // an unmasked tile; in which of the two places it lies is known at compile time, so that no address is made in the loop
+    auto tile = [&](auto place, int t) {
+        constexpr int ROW = decltype(place)::value * (2 * BK);
         arrive(t);
-        const AttnLane<D> lk(at + (uint32_t)(t & 1) * (2 * TILE)), lv(at + (uint32_t)(t & 1) * (2 * TILE) + TILE);
         f32x16 s[2];
-        scores<D, 2>(s, lk, 0, q);
+        scores<D, 2>(s, lk0, ROW, q);
         r.raise(fmaxf(largest(s[0]), largest(s[1])) * a.c2);
         r.weigh(s[0], a.c2);
         const bf16x8 p0[2] = {rounded(s[0], 0), rounded(s[0], 1)};
-        add_turned<D>(r.acc, lv, 0, p0);
+        add_turned<D>(r.acc, lv0, ROW, p0);
         r.weigh(s[1], a.c2);
         const bf16x8 p1[2] = {rounded(s[1], 0), rounded(s[1], 1)};
-        add_turned<D>(r.acc, lv, 32, p1);
+        add_turned<D>(r.acc, lv0, ROW + 32, p1);
+    };
+    int t = 0;
+    for (; t + 1 < full; t += 2) {
+        tile(std::integral_constant<int, 0>(), t);
+        tile(std::integral_constant<int, 1>(), t + 1);
     }
+    if (t < full) tile(std::integral_constant<int, 0>(), t), ++t;
     if (t < tiles && have > 0) {
         arrive(t);
         const AttnLane<D> lk(at + (uint32_t)(t & 1) * (2 * TILE)), lv(at + (uint32_t)(t & 1) * (2 * TILE) + TILE);
