@@ -77,15 +77,15 @@ template <int D> struct AttnTile {
 // A tile of ROWS rows on its way from memory straight to LDS, 16 bytes a lane, a wavefront's 1 KB in a row; the swizzle is in which
 // piece a lane fetches.  Rows past `have` repeat the last one, so that a wavefront always has N transfers under way; the kernels mask
 // them.  Pieces past d are not fetched: their places keep the zeros of clear_tiles.  (Offsets stay under 2^32 bytes for strides up to 2^24.)
-template <int D, int ROWS> struct AttnDma {
+template <int D, int ROWS, int WAVES = 4> struct AttnDma { // WAVES: that share the tile
     using T = AttnTile<D>;
-    static constexpr int WAVES = 4, P = T::RB / 16, RPI = 64 / P;                           // pieces of a row, rows of a transfer
+    static constexpr int P = T::RB / 16, RPI = 64 / P;                           // pieces of a row, rows of a transfer
     static constexpr int TOTAL = ROWS / RPI, N = TOTAL / WAVES > 0 ? TOTAL / WAVES : 1; // (few rows: wavefronts repeat one another's transfers)
     uint32_t stride2, off[N];
     int row, to, dd; // dd: values of a row that are fetched
     __device__ __forceinline__ void plan(int64_t stride, int d)
     {
-        const int lane = threadIdx.x & 63, first = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * N % TOTAL;
+        const int lane = threadIdx.x & 63, first = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % WAVES * N % TOTAL;
         row = first * RPI + lane / P;
         to = first * 1024;
         stride2 = (uint32_t)(stride * 2);
@@ -171,6 +171,16 @@ __device__ __forceinline__ f32x16 zeros16()
 }
 // row of a 32 x 32 result in register i
 __device__ __forceinline__ int row_of(int i) { return 8 * (i >> 2) + 4 * ((threadIdx.x & 63) >> 5) + (i & 3); }
+// the value on the diagonal of a 32 x 32 result in the lane's column
+__device__ __forceinline__ float diagonal_of(const f32x16 &s)
+{
+    const int lane = threadIdx.x & 63, me = lane & 31;
+    float x = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x = row_of(i) == me ? s[i] : x;
+    const float other = __shfl_xor(x, 32, 64);
+    return (me >> 2 & 1) == lane >> 5 ? x : other;
+}
 __device__ __forceinline__ bf16x8 rounded(const f32x16 &s, int j)
 {
     bf16x8 r;
@@ -276,6 +286,33 @@ template <int D> __device__ __forceinline__ void put_rows(bf16_t *base, int64_t 
             for (int e = 0; e < 4; ++e) r[e] = (bf16_t)(acc[t][4 * g + e] * by);
             if (at < d) *reinterpret_cast<bf16x4 *>(base + i * stride + at) = r;
         }
+}
+
+// Adds up what four wavefronts have for the same 32 rows: x[t] and, of each wavefront, a factor for the lane's row.  Through LDS at `at`, 16
+// bytes a lane side by side; wavefront w gets the sums of x[w] (all of them where D is 128, none past D / 32).
+typedef __attribute__((address_space(3))) f32x4 *lds_f32x4;
+template <int D> __device__ __forceinline__ void join_put(uint32_t at, const f32x16 (&x)[D / 32])
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            *reinterpret_cast<lds_f32x4>(at + ((wave * (D / 32) + t) * 4 + g) * 1024 + lane * 16) = f32x4{x[t][4 * g], x[t][4 * g + 1], x[t][4 * g + 2], x[t][4 * g + 3]};
+}
+template <int D> __device__ __forceinline__ f32x16 join_get(uint32_t at, const float (&by)[4])
+{
+    const int lane = threadIdx.x & 63, t = threadIdx.x >> 6;
+    f32x16 r = zeros16();
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const f32x4 y = *reinterpret_cast<lds_f32x4>(at + ((w * (D / 32) + t) * 4 + g) * 1024 + lane * 16);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r[4 * g + e] = fmaf(by[w], y[e], r[4 * g + e]);
+        }
+    return r;
 }
 
 // Tile and head of a workgroup.  Heads vary fastest; workgroups go to the eight dies in turn, so that where their number allows it a
@@ -431,6 +468,95 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_f
 }
 
 // ---------------------------------------------------------------------------
+// forward, few rows: 32 rows a workgroup, whose four wavefronts deal the keys among them, 32 at a time, each through two LDS places of its own
+// and without a barrier, and join what they have at the end.  Four times the workgroups, a quarter of the way for each; every key is fetched for
+// 32 rows instead of 128, so that it pays only where the card would be mostly idle (attn_few).
+// ---------------------------------------------------------------------------
+template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 1) void k_attn_fwd_few(const AttnArgs a)
+{
+    using T = AttnTile<D>;
+    constexpr int TILE = 32 * T::RB > 1024 ? 32 * T::RB : 1024, OWN = 4 * TILE;
+    extern __shared__ __attribute__((aligned(1024))) char lds[]; // keys and values of 32 rows, twice, of each wavefront; largest scores and sums
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), me = lane & 31;
+    const AttnWork w = attn_work(a.heads, a.tiles, CAUSAL);
+    const AttnSeq seq = attn_seq<32>(a, w.vt);
+    if (seq.len < 1) return;
+    const int head = w.head, hk = head / a.group, q0 = seq.tile * 32, have = min(32, seq.len - q0);
+    const bf16_t *kp = a.k + (int64_t)seq.start * a.ks + (int64_t)hk * a.d, *vp = a.v + (int64_t)seq.start * a.vs + (int64_t)hk * a.d;
+    const int subs = CAUSAL ? seq.tile + 1 : (seq.len + 31) / 32; // of all wavefronts
+    const uint32_t base = lds_address(lds), at = base + wave * OWN;
+
+    AttnDma<D, 32, 1> fk, fv;
+    fk.plan(a.ks, a.d);
+    fv.plan(a.vs, a.d);
+    if (a.d != D) clear_tiles<4 * OWN>(lds);
+    auto issue = [&](int sub) {
+        const uint32_t to = at + (uint32_t)(sub >> 2 & 1) * (2 * TILE);
+        fk.issue(kp + (int64_t)sub * 32 * a.ks, to, seq.len - sub * 32);
+        fv.issue(vp + (int64_t)sub * 32 * a.vs, to + TILE, seq.len - sub * 32);
+    };
+    if (wave < subs) issue(wave);
+    bf16x8 q[D / 16];
+    const bf16_t *qp = a.q + (int64_t)(seq.start + q0) * a.qs + (int64_t)head * a.d;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) q[ks] = along_mem(qp, a.qs, have, a.d, ks);
+    AttnRow<D> r;
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t) r.acc[t] = zeros16();
+    r.top = -FLT_MAX;
+    r.sum = 0.f;
+    const int last = CAUSAL ? me : seq.len - 1 - 32 * (subs - 1); // key of the last subtile
+    bf16x8 late[2];
+    bool apart = false;
+    for (int sub = wave; sub < subs; sub += 4) {
+        if (sub + 4 < subs) {
+            issue(sub + 4); // (this wavefront has all that it asked of that place)
+            wait_vm<fk.N + fv.N>();
+        } else {
+            wait_vm<0>();
+        }
+        const uint32_t here = at + (uint32_t)(sub >> 2 & 1) * (2 * TILE);
+        const AttnLane<D> lk(here), lv(here + TILE);
+        f32x16 s[1];
+        scores<D, 1>(s, lk, 0, q);
+        const bool cut = sub == subs - 1; // where the mask ends
+        if (cut) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[0][i] = row_of(i) <= last ? s[0][i] : -INFINITY;
+        }
+        r.raise(largest(s[0]) * a.c2);
+        r.weigh(s[0], a.c2);
+        const bf16x8 p[2] = {rounded(s[0], 0), rounded(s[0], 1)};
+        apart = cut && any_special<D>(lv, 0);
+        if (apart) late[0] = p[0], late[1] = p[1];
+        else add_turned<D>(r.acc, lv, 0, p);
+    }
+    if (apart) add_turned_apart<D>(r.acc, vp + (int64_t)(subs - 1) * 32 * a.vs, a.vs, seq.len - (subs - 1) * 32, a.d, late, [&](int key, int) { return key <= last; });
+    r.sum += __shfl_xor(r.sum, 32, 64);
+
+    float *stat = reinterpret_cast<float *>(lds + 4 * OWN); // [2][4][32]
+    __syncthreads();
+    join_put<D>(base, r.acc);
+    if (lane < 32) {
+        stat[wave * 32 + me] = r.top;
+        stat[128 + wave * 32 + me] = r.sum;
+    }
+    __syncthreads();
+    float by[4], top = stat[me], sum = 0.f;
+#pragma unroll
+    for (int x = 1; x < 4; ++x) top = fmaxf(top, stat[x * 32 + me]);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+        by[x] = __builtin_amdgcn_exp2f(stat[x * 32 + me] - top);
+        sum = fmaf(by[x], stat[128 + x * 32 + me], sum);
+    }
+    if (a.lse && wave == 0 && lane < have) a.lse[(int64_t)head * a.rows + seq.start + q0 + lane] = (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+    if (wave >= D / 32) return;
+    const f32x16 o[1] = {join_get<D>(base, by)};
+    put_rows<32>(a.out + (int64_t)(seq.start + q0) * a.os + (int64_t)head * a.d + 32 * wave, a.os, have, a.d - 32 * wave, o, 1.f / sum);
+}
+
+// ---------------------------------------------------------------------------
 // backward.  Both kernels walk over subtiles of 32 x 32 pairs, whose rows come through a ring of LDS slots: two products (scores, do . v),
 // 16 values of p and ds a lane, and the products that p and ds enter.  Two wavefronts share a SIMD: alone on it, one issues a vector
 // instruction in every second slot at best (measured: 6.5 cycles each against 4 with two).  At 128 values a head that takes one of the
@@ -546,13 +672,8 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_d
         s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(along_mem(a.o + row * a.os + (int64_t)head * a.d, a.os, have, a.d, ks), x, s, 0, 0, 0);
     }
     const float nlse2 = me < have ? a.lse[(int64_t)head * a.rows + row + me] * -1.4426950408889634f : 0.f;
-    float delta = 0.f, rest = 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) delta = row_of(i) == me ? s[i] : delta;
-    {
-        const float other = __shfl_xor(delta, 32, 64);
-        delta = (me >> 2 & 1) == lane >> 5 ? delta : other;
-    }
+    const float delta = diagonal_of(s);
+    float rest = 0.f;
     f32x16 acc[D / 32], y[D / 32];
 #pragma unroll
     for (int t = 0; t < D / 32; ++t) acc[t] = y[t] = zeros16();
@@ -616,6 +737,111 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_d
         a.nlse2[(int64_t)head * a.rows + row + lane] = nlse2;
         a.delta[(int64_t)head * a.rows + row + lane] = delta + rest;
     }
+}
+
+// dq, few rows: as the forward kernel for few rows
+template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 1) void k_attn_dq_few(const AttnArgs a)
+{
+    using B = AttnBack<D>;
+    constexpr int PLACE = 2 * B::SLOT, RB = AttnTile<D>::RB;
+    // keys and values of 32 rows, twice, of each wavefront; do; r
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), me = lane & 31;
+    const AttnWork w = attn_work(a.heads, a.tiles, CAUSAL);
+    const AttnSeq seq = attn_seq<32>(a, w.vt);
+    if (seq.len < 1) return;
+    const int head = w.head, hk = head / a.group, q0 = seq.tile * 32, have = min(32, seq.len - q0);
+    const int64_t row = seq.start + q0;
+    const bf16_t *kp = a.k + (int64_t)seq.start * a.ks + (int64_t)hk * a.d, *vp = a.v + (int64_t)seq.start * a.vs + (int64_t)hk * a.d;
+    const int subs = CAUSAL ? seq.tile + 1 : (seq.len + 31) / 32; // of all wavefronts
+    const uint32_t base = lds_address(lds), at = base + wave * PLACE;
+    const AttnLane<D> own(base + 4 * PLACE);
+
+    AttnDma<D, 32, 1> fk, fv;
+    fk.plan(a.ks, a.d);
+    fv.plan(a.vs, a.d);
+    if (a.d != D) clear_tiles<4 * PLACE + (B::OWN ? 32 * RB : 0)>(lds);
+    bf16x8 q[D / 16], d_o[B::REGS];
+    if constexpr (B::OWN) {
+        AttnDma<D, 32> fo;
+        fo.plan(a.dos, a.d);
+        fo.issue(a.d_o + row * a.dos + (int64_t)head * a.d, base + 4 * PLACE, have);
+        wait_vm<0>();
+        __syncthreads();
+    }
+    auto issue = [&](int sub) {
+        const uint32_t to = at + (uint32_t)(sub >> 2 & 1) * B::SLOT;
+        fk.issue(kp + (int64_t)sub * 32 * a.ks, to, seq.len - sub * 32);
+        fv.issue(vp + (int64_t)sub * 32 * a.vs, to + B::TILE, seq.len - sub * 32);
+    };
+    if (wave < subs) issue(wave);
+    f32x16 s = zeros16(), dp;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+        q[ks] = along_mem(a.q + row * a.qs + (int64_t)head * a.d, a.qs, have, a.d, ks);
+        bf16x8 x;
+        if constexpr (B::OWN) x = own.along(0, ks);
+        else x = d_o[ks] = along_mem(a.d_o + row * a.dos + (int64_t)head * a.d, a.dos, have, a.d, ks);
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(along_mem(a.o + row * a.os + (int64_t)head * a.d, a.os, have, a.d, ks), x, s, 0, 0, 0);
+    }
+    const float nlse2 = me < have ? a.lse[(int64_t)head * a.rows + row + me] * -1.4426950408889634f : 0.f;
+    const float delta = diagonal_of(s);
+    float rest = 0.f;
+    f32x16 acc[D / 32], y[D / 32];
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t) acc[t] = y[t] = zeros16();
+    const int last = CAUSAL ? me : seq.len - 1 - 32 * (subs - 1);
+    bf16x8 p[2], ds[2];
+    bool apart = false;
+    for (int sub = wave; sub < subs; sub += 4) {
+        if (sub + 4 < subs) {
+            issue(sub + 4); // (this wavefront has all that it asked of that place)
+            wait_vm<fk.N + fv.N>();
+        } else {
+            wait_vm<0>();
+        }
+        const uint32_t here = at + (uint32_t)(sub >> 2 & 1) * B::SLOT;
+        const AttnLane<D> lk(here), lv(here + B::TILE);
+        pair_products<D>(s, dp, lk, lv, q, d_o, own);
+        const bool cut = sub == subs - 1; // where the mask ends
+        const int to = cut ? last : 31;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const bool in = row_of(i) <= to;
+            const float e = __builtin_amdgcn_exp2f(fmaf(s[i], a.c2, nlse2)), z = in ? e * (dp[i] - delta) : 0.f;
+            rest += z;
+            p[i >> 3][i & 7] = (bf16_t)(in ? e : 0.f);
+            ds[i >> 3][i & 7] = (bf16_t)z;
+        }
+        apart = cut && any_special<D>(lk, 0);
+        if (!apart) pair_sums<D, true>(acc, y, lk, lk, ds, p);
+    }
+    if (apart) {
+        const int key0 = 32 * (subs - 1);
+        auto part = [&](int key, int query) { return !CAUSAL || key <= query; };
+        add_turned_apart<D>(acc, kp + (int64_t)key0 * a.ks, a.ks, seq.len - key0, a.d, ds, part);
+        add_turned_apart<D>(y, kp + (int64_t)key0 * a.ks, a.ks, seq.len - key0, a.d, p, part);
+    }
+    rest += __shfl_xor(rest, 32, 64);
+
+    float *stat = reinterpret_cast<float *>(lds + 4 * PLACE + (B::OWN ? 32 * RB : 0)); // [4][32]
+    __syncthreads();
+    join_put<D>(base, acc);
+    join_put<D>(base + D * 512, y); // 4 wavefronts x D / 32 x 4 KB after the other
+    if (lane < 32) stat[wave * 32 + me] = rest;
+    __syncthreads();
+    rest = (stat[me] + stat[32 + me]) + (stat[64 + me] + stat[96 + me]);
+    if (wave == 0 && lane < have) {
+        a.nlse2[(int64_t)head * a.rows + row + lane] = nlse2;
+        a.delta[(int64_t)head * a.rows + row + lane] = delta + rest;
+    }
+    if (wave >= D / 32) return;
+    const float one[4] = {1.f, 1.f, 1.f, 1.f};
+    f32x16 sum[1] = {join_get<D>(base, one)};
+    const f32x16 ys = join_get<D>(base + D * 512, one);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum[0][i] = fmaf(-rest, ys[i], sum[0][i]);
+    put_rows<32>(a.dq + row * a.dqs + (int64_t)head * a.d + 32 * wave, a.dqs, have, a.d - 32 * wave, sum, a.scale);
 }
 
 // ---------------------------------------------------------------------------
@@ -684,7 +910,6 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_d
 #pragma unroll
     for (int t = 0; t < D / 32; ++t) dk[t] = dv[t] = zeros16();
     bf16x8 p[2], ds[2];
-    typedef const __attribute__((address_space(3))) f32x4 *lds_f32x4;
     int n = 0; // tiles so far
     auto arrive = [&]() {
         if (RING > 2 && n + 1 < tiles) wait_vm<fq.N + fd.N + 1>();
@@ -861,6 +1086,27 @@ static AttnArgs attn_args(const pac_attn *a, const int32_t *off, int32_t batch, 
 }
 static int64_t stat_bytes(const pac_attn *a, int64_t rows) { return (rows * a->heads * 4 + 255) / 256 * 256; }
 
+// Whether a call's rows are few: forward and dq then take 32 rows a workgroup and deal the keys to its wavefronts.  Forward, us, 128 rows /
+// 32 rows a workgroup: causal 1 x 8000 of 4 heads (252 workgroups of 128 rows) 91 / 63, 1000 of 10 (80) 23 / 15, 1788 of 6 (102) 36 / 21, but
+// 4000 of 8 (256) 74 / 87 and 2000 of 12 (192) 39 / 42; not causal, whose workgroups all take as long, 1500 of 5 (60) 31 / 20, 4000 of 1 (32)
+// 68 / 36, but 1000 of 10 (80) 23 / 26 and 4000 of 4 (128) 68 / 69.  Below some 100 tokens there is nothing to deal: 19 tokens 7.5 / 8.7.
+static bool attn_few(const pac_attn *a, int32_t batch, int64_t rows)
+{
+    return (rows / 128 + batch) * a->heads <= (a->causal ? 192 : 72) && rows >= 128 * (int64_t)batch;
+}
+// Starts a kernel with that much LDS
+template <typename K> static bool attn_launch(K kernel, unsigned blocks, int lds, hipStream_t st, const AttnArgs &r)
+{
+    if (lds > 64 << 10 && hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess) return false;
+    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(256), lds, st, r);
+    return true;
+}
+template <int D> static int few_lds(bool back)
+{
+    const int place = 4 * AttnBack<D>::TILE;
+    return back ? 4 * place + (AttnBack<D>::OWN ? 32 * AttnTile<D>::RB : 0) + 512 : 4 * place + 1024;
+}
+
 // Workgroups of dk and dv: as many as a launch needs to fill the card and to end evenly, if each then still has enough to do to pay for
 // sums that go through memory.  (There and back, us, without splits / with: 500 tokens of 64 heads on one key head 1040 / 83, 2048 tokens
 // 32/8 heads 429 / 256, 4001 + 6143 tokens 32/8 heads 2216 / 2149.  With 1536 workgroups wanted 6000 tokens of 16 heads take 453, not 430.)
@@ -914,12 +1160,20 @@ pac_status pac_attn_forward(const pac_attn *a, const int32_t *offsets, int32_t b
     r.lse = lse;
     (void)hipGetLastError();
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    bool ok = true;
     by_width(a->d, [&](auto n) {
         constexpr int D = decltype(n)::value;
+        if (attn_few(a, batch, rows)) {
+            r.tiles = (unsigned)(rows / 32 + batch);
+            ok = a->causal ? attn_launch(k_attn_fwd_few<D, true>, r.tiles * r.heads, few_lds<D>(false), st, r)
+                           : attn_launch(k_attn_fwd_few<D, false>, r.tiles * r.heads, few_lds<D>(false), st, r);
+            return;
+        }
         const dim3 grid(r.tiles * r.heads);
         if (a->causal) hipLaunchKernelGGL((k_attn_fwd<D, true>), grid, dim3(256), 0, st, r);
         else hipLaunchKernelGGL((k_attn_fwd<D, false>), grid, dim3(256), 0, st, r);
     });
+    if (!ok) return PAC_ERR_DEVICE;
     return hipGetLastError() == hipSuccess ? PAC_OK : PAC_ERR_DEVICE;
 }
 
@@ -976,16 +1230,24 @@ pac_status pac_attn_backward(const pac_attn *a, const int32_t *offsets, int32_t 
     r.splits = attn_splits(a, batch, rows);
     (void)hipGetLastError();
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    bool ok = true;
     by_width(a->d, [&](auto n) {
         constexpr int D = decltype(n)::value;
-        if (a->causal) {
+        if (attn_few(a, batch, rows)) {
+            AttnArgs f = r;
+            f.tiles = (unsigned)(rows / 32 + batch);
+            ok = a->causal ? attn_launch(k_attn_dq_few<D, true>, f.tiles * f.heads, few_lds<D>(true), st, f)
+                           : attn_launch(k_attn_dq_few<D, false>, f.tiles * f.heads, few_lds<D>(true), st, f);
+            if (!ok) return;
+        } else if (a->causal) {
             hipLaunchKernelGGL((k_attn_dq<D, true>), dim3(r.tiles * r.heads), dim3(256), 0, st, r);
-            hipLaunchKernelGGL((k_attn_dkv<D, true>), dim3(r.tiles * r.kv_heads * r.splits), dim3(256), 0, st, r);
         } else {
             hipLaunchKernelGGL((k_attn_dq<D, false>), dim3(r.tiles * r.heads), dim3(256), 0, st, r);
-            hipLaunchKernelGGL((k_attn_dkv<D, false>), dim3(r.tiles * r.kv_heads * r.splits), dim3(256), 0, st, r);
         }
+        if (a->causal) hipLaunchKernelGGL((k_attn_dkv<D, true>), dim3(r.tiles * r.kv_heads * r.splits), dim3(256), 0, st, r);
+        else hipLaunchKernelGGL((k_attn_dkv<D, false>), dim3(r.tiles * r.kv_heads * r.splits), dim3(256), 0, st, r);
     });
+    if (!ok) return PAC_ERR_DEVICE;
     if (r.splits > 1) hipLaunchKernelGGL(k_attn_join, dim3((unsigned)((rows * 2 * kc / 8 + 255) / 256)), dim3(256), 0, st, r);
     return hipGetLastError() == hipSuccess ? PAC_OK : PAC_ERR_DEVICE;
 }

@@ -327,3 +327,49 @@ def test_queries_dealt_to_several_workgroups(heads, kv, d, lens, causal):
     again = torch.empty_like(dk)
     a.backward(q, k, v, off, o, lse, do, dq, again, dv)
     assert torch.equal(dk[lead:-tail], again[lead:-tail])
+
+
+@pytest.mark.parametrize("heads,kv,d,lens,causal", [(2, 1, 128, [1000], True), (2, 2, 128, [777, 0, 130], False), (3, 1, 64, [129, 300, 257], True), (1, 1, 32, [2049], False),
+                                                    (4, 2, 96, [160, 500], True), (2, 2, 40, [33, 640], False), (1, 1, 104, [1, 511], True)])
+def test_few_rows(heads, kv, d, lens, causal):
+    """Calls that leave most of the card idle deal the keys to the wavefronts of a workgroup (32 rows each); rows beside the sequences stay as
+    they are, values that are none where the mask lets them."""
+    lead, tail = 2, 5
+    rows = lead + sum(lens) + tail
+    assert (rows // 128 + len(lens)) * heads <= (192 if causal else 72) and rows >= 128 * len(lens)
+    q, k, v, do = make(heads + d, rows, heads, kv, d, 1.5)
+    for t in (q, k, v, do):
+        t[:lead], t[-tail:] = math.nan, math.inf
+    a, off = rt.Attention(heads, d, kv_heads=kv, causal=causal), rt.packed_offsets(lens) + lead
+    o, lse = torch.full_like(q, 7.0), torch.full((heads, rows), 7.0, device="cuda")
+    dq, dk, dv = (torch.full_like(t, 7.0) for t in (q, k, v))
+    a.forward(q, k, v, off, o, lse)
+    a.backward(q, k, v, off, o, lse, do, dq, dk, dv)
+    check(a, lens, (o, lse, dq, dk, dv), q, k, v, do, d ** -0.5, causal, first=lead)
+    for t in (o, lse.t(), dq, dk, dv):
+        assert (t[:lead] == 7).all() and (t[-tail:] == 7).all()
+
+
+@pytest.mark.parametrize("which", ["q", "k", "v", "do"])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_values_that_are_none_in_many_rows(which, bad):
+    """The same as for few rows, where 128 rows make a workgroup: 128 heads, a value in the last one's first tile and in its last."""
+    heads, d, n = 128, 64, 200
+    clean = dict(zip(("q", "k", "v", "do"), make(5, n, heads, heads, d)))
+    a, off = rt.Attention(heads, d, causal=True), rt.packed_offsets([n])
+    assert (n // 128 + 1) * heads > 192
+    ref = run(a, *clean.values(), off)
+    for at in (33, 190):
+        t = {name: x.clone() for name, x in clean.items()}
+        t[which][at, (heads - 1) * d + 5] = bad
+        got = run(a, *t.values(), off)
+        for r, g, out in zip(ref, got, ("o", "lse", "dq", "dk", "dv")):
+            r, g = (x.t() if out == "lse" else x for x in (r, g))
+            other = slice(0, heads - 1) if out == "lse" else slice(0, (heads - 1) * d)
+            assert torch.equal(r[:, other], g[:, other]), (which, out)
+            mine = torch.arange(n, device="cuda") // 32 < at // 32
+            if out in ("o", "lse", "dq"):  # rows before see none of it
+                assert torch.equal(r[mine], g[mine]), (which, out)
+        if which == "v":
+            seen = got[0][at:, (heads - 1) * d + 5]
+            assert seen.isnan().all() if math.isnan(bad) else (seen == bad).all()
