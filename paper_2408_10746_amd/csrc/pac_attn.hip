@@ -51,7 +51,8 @@ template <int BM> __device__ __forceinline__ AttnSeq attn_seq(const AttnArgs &a,
     lo = __builtin_amdgcn_readfirstlane(lo);
     const int start = at(lo), end = at(lo + 1);
     const int tile = vt - (start / BM + lo);
-    return AttnSeq{start, (int64_t)tile * BM < end - start ? end - start : 0, tile};
+    // (where offsets fall, the search may end anywhere: tiles before a sequence's first are none)
+    return AttnSeq{start, tile >= 0 && (int64_t)tile * BM < end - start ? end - start : 0, tile};
 }
 
 // ---------------------------------------------------------------------------

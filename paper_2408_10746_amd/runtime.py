@@ -509,9 +509,12 @@ class Kv4Cache:
         need = pb.pac_kv4_bytes(self._c)
         if need < 0:
             raise ValueError("pages: 0..2^31 - 1; page: a power of two, 8..65536; kv_heads: 1..4096; d: a multiple of 8, 8..128")
+        if torch.device(device).type != "cuda":
+            raise ValueError("device: a GPU")
         self.pages, self.page, self.kv_heads, self.d = pages, page, kv_heads, d
         self.data = torch.zeros(need, dtype=torch.uint8, device=device)
         self._gpu = self.data.get_device()
+        self._room = None, 0  # sizes of the last attend, and bytes of workspace for them
 
     def _at(self):
         self._c.at = self.data.data_ptr()
@@ -549,7 +552,10 @@ class Kv4Cache:
             raise ValueError(f"table: int32, ({batch}, pages), neighbouring columns, on GPU {gpu} is wanted")
         pages = _fits(table.shape[1], "pages of a sequence")
         c, st = self._at(), table.stride(0) if batch > 1 else pages
-        need = _lib().pac_kv4_attend_workspace_bytes(c, heads, batch, pages)
-        ws = torch.empty(max(need, 0), dtype=torch.uint8, device=q.device)  # for this call, on this stream
+        sizes, need = self._room
+        if sizes != (heads, batch, pages):
+            need = max(_lib().pac_kv4_attend_workspace_bytes(c, heads, batch, pages), 0)
+            self._room = (heads, batch, pages), need
+        ws = torch.empty(need, dtype=torch.uint8, device=q.device)  # for this call, on this stream
         _call(gpu, "pac_kv4_attend", c, heads, _scale(scale, d), batch, table.data_ptr(), pages, st, lens.data_ptr(), q.data_ptr(), sq, o.data_ptr(), so,
               ws.data_ptr(), need)
