@@ -576,8 +576,8 @@ template <int D>
 __device__ __forceinline__ void pair_products(f32x16 &s, f32x16 &dn, const AttnLane<D> &l1, const AttnLane<D> &l2, const bf16x8 (&b1)[D / 16],
                                               const bf16x8 (&b2)[AttnBack<D>::REGS], const AttnLane<D> &own)
 {
-    constexpr int N = D / 16, AHEAD = 2;
     constexpr bool OWN = AttnBack<D>::OWN;
+    constexpr int N = D / 16, AHEAD = OWN ? 1 : 2; // (with 128 values a head two sets of operands ahead are spilled registers)
     bf16x8 f1[AHEAD + 1], f2[AHEAD + 1], f3[AHEAD + 1];
     auto read = [&](int n) {
         f1[n % (AHEAD + 1)] = l1.along(0, n);
@@ -602,7 +602,7 @@ __device__ __forceinline__ void pair_sums(f32x16 (&acc)[D / 32], f32x16 (&more)[
                                           const bf16x8 (&q)[2])
 {
     // product n: tile n % 2, 16 rows j, 32 values t; operand m = n, or n / 2 where both tiles are one
-    constexpr int T = D / 32, N = 4 * T, M = SAME ? N / 2 : N, K = SAME ? 2 : 3;
+    constexpr int T = D / 32, N = 4 * T, M = SAME ? N / 2 : N, K = 2;
     bf16x8 g[4];
     auto read = [&](int m) { g[m % 4] = SAME ? l1.turned(0, m / T, m % T) : (m % 2 ? l2 : l1).turned(0, m / 2 / T, m / 2 % T); };
 #pragma unroll
