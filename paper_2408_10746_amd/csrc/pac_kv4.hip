@@ -459,7 +459,7 @@ __global__ __launch_bounds__(256) void k_kv4_join(const Kv4Attend a)
     const int b = blockIdx.x / a.heads, h = blockIdx.x % a.heads, tid = threadIdx.x;
     const int len = kv4_tokens(a.lens[b], a.table_len, a.c.shift), per = kv4_per_split(len, a.splits);
     if (len <= per) return;
-    const int n = (len + per - 1) / per;
+    const int n = (int)(((int64_t)len + per - 1) / per);
     const float2 *stat = a.stat + ((int64_t)b * a.heads + h) * a.splits;
     const f32x4 *part = reinterpret_cast<const f32x4 *>(a.part + ((int64_t)b * a.heads + h) * a.splits * DP);
     // weights: every wavefront finds the largest score of all splits for itself
@@ -497,15 +497,16 @@ static_assert(kKvSplits <= 256, "a thread a split");
 // ---------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------
+static int kv4_blocks(const pac_kv4 *c) { return (c->d + 31) / 32; }
 static pac_status check_kv4(const pac_kv4 *c)
 {
     if (!c) return PAC_ERR_NULL;
     if (c->pages < 0 || c->pages > INT32_MAX || c->page < 8 || c->page > 65536 || (c->page & (c->page - 1)) || c->kv_heads < 1 ||
         c->kv_heads > 4096 || c->d < 8 || c->d > 128 || c->d % 8)
         return PAC_ERR_SHAPE;
-    return PAC_OK;
+    // its bytes have to be a number
+    return c->pages * c->page > ((int64_t)1 << 62) / (c->kv_heads * 34 * kv4_blocks(c)) ? PAC_ERR_SHAPE : PAC_OK;
 }
-static int kv4_blocks(const pac_kv4 *c) { return (c->d + 31) / 32; }
 static int64_t kv4_bytes(const pac_kv4 *c) { return c->pages * c->page * c->kv_heads * 34 * kv4_blocks(c); }
 static Kv4 kv4_of(const pac_kv4 *c)
 {
@@ -529,7 +530,8 @@ static pac_status check_attend(const pac_kv4 *c, int32_t heads, int32_t batch, i
     const pac_status s = check_kv4(c);
     if (s != PAC_OK) return s;
     if (heads < 1 || heads > 4096 || heads % c->kv_heads || batch < 0 || table_len < 0) return PAC_ERR_SHAPE;
-    if ((int64_t)table_len * c->page > INT32_MAX || (int64_t)batch * c->kv_heads * ((heads / c->kv_heads + 15) / 16) >= 1 << 23 ||
+    // (the kernel's token numbers run up to two of its steps past a sequence's end)
+    if ((int64_t)table_len * c->page > INT32_MAX - 4096 || (int64_t)batch * c->kv_heads * ((heads / c->kv_heads + 15) / 16) >= 1 << 23 ||
         (int64_t)batch * heads >= 1 << 23)
         return PAC_ERR_UNSUPPORTED;
     return PAC_OK;

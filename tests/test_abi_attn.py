@@ -148,3 +148,20 @@ def test_a_workspace_for_a_large_batch_serves_smaller_ones(heads, kv_heads, d, p
     for b in (1, 3, 64):
         by = [need(b, t) for t in range(0, 3000, 13)]
         assert by == sorted(by)
+
+
+def test_caches_whose_bytes_are_no_number_are_refused():
+    for pages, page, kv_heads, d in (((1 << 31) - 1, 65536, 4096, 128), (1 << 30, 32768, 4096, 72), ((1 << 31) - 1, 65536, 964, 128)):
+        c = kv4(None, pages, page, kv_heads, d)
+        assert pb.pac_kv4_bytes(c) == pb.pac_kv4_attend_workspace_bytes(c, kv_heads, 1, 1) == -1
+    c = kv4(None, 1 << 30, 65536, 481, 128)  # as large as it gets
+    assert pb.pac_kv4_bytes(c) == (1 << 30) * 65536 * 481 * 136 < 1 << 62
+
+
+def test_tables_near_the_last_token_number_are_refused():
+    """Token numbers have 32 bits and run a little past a sequence's end: the last few thousand are not for tables."""
+    L = pb.lib()
+    for page, refused, taken in ((8, (1 << 28) - 1, (1 << 28) - 513), (4096, (1 << 19) - 1, (1 << 19) - 2), (65536, (1 << 15) - 0, (1 << 15) - 1)):
+        c = kv4(page=page, kv_heads=1)
+        assert pb.pac_kv4_attend_workspace_bytes(c, 2, 1, refused) == -1 and pb.pac_kv4_attend_workspace_bytes(c, 2, 1, taken) > 0
+        assert L.pac_kv4_attend(C.byref(c), 2, 1.0, 1, A, refused, refused, 1 << 50, 1 << 51, 128, 1 << 52, 128, 1 << 53, 1 << 40, None) == pb.PAC_ERR_UNSUPPORTED
