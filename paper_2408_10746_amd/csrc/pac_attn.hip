@@ -27,32 +27,52 @@ struct AttnArgs {
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 // ---------------------------------------------------------------------------
-// Which rows a workgroup has.  Tiles begin where sequences do; a sequence that begins at row s has the tiles s / BM + b and up, of
-// which there are never fewer than it needs, so that the grid follows from rows and batch alone and a tile's sequence is found by a
-// search over the offsets, 64 places a time.  (Tiles past a sequence's end do nothing.)
+// Which rows a workgroup has.  A sequence that begins at row s may have the numbers s / BM + b and up to the next one's, of which there are
+// never fewer than its tiles, so that the grid follows from rows and batch alone and a number's sequence is found by a search over the
+// offsets, 64 places a time.  The search ends at up to 64 sequences, whose tiles have the first of the numbers that they have together: numbers
+// without a tile come last, where no compute unit waits for its share behind them (numbers without one after every sequence / at the end, us:
+// 4 x 1024 tokens of 8 heads of 64 there and back 146 / 108, 8 x 128 of 32 of 128 56 / 50; but 16 x 256 of 32 forward 34.5 / 35.7, whose tiles
+// of one and of two steps then lie less evenly).  With causal a sequence's tiles begin with the one that takes longest.
+// (Most work first across sequences, us: 16 x 256 35 / 44, 8 x 512 175 / 201, 8 x 256..1024 280 / 290: a sequence's keys are read while they
+// are in the cache when its tiles follow each other.)
 // ---------------------------------------------------------------------------
 struct AttnSeq {
     int start, len, tile; // len < 1: nothing to do
 };
-template <int BM> __device__ __forceinline__ AttnSeq attn_seq(const AttnArgs &a, int vt)
+// sums over the lanes up to each
+__device__ __forceinline__ int wave_sums(int x)
+{
+#define PAC_ATTN_STEP(CTRL, ROWS) x += __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false)
+    PAC_ATTN_STEP(0x111, 0xf); // from the lanes 1, 2, 4, 8 places before in a row of 16, then from the rows before
+    PAC_ATTN_STEP(0x112, 0xf);
+    PAC_ATTN_STEP(0x114, 0xf);
+    PAC_ATTN_STEP(0x118, 0xf);
+    PAC_ATTN_STEP(0x142, 0xa);
+    PAC_ATTN_STEP(0x143, 0xc);
+#undef PAC_ATTN_STEP
+    return x;
+}
+template <int BM, bool CAUSAL, bool KEYS = false> __device__ __forceinline__ AttnSeq attn_seq(const AttnArgs &a, int number)
 {
     const int lane = threadIdx.x & 63;
     auto at = [&](int b) { return min(max(a.off[b], 0), a.rows); };
     int lo = 0, n = a.batch;
-    for (;;) {
+    while (n > 64) {
         const int step = (n + 63) / 64, b = lane * step;
-        const bool before = b < n && at(lo + b) / BM + lo + b <= vt;
+        const bool before = b < n && at(lo + b) / BM + lo + b <= number;
         const int cnt = __builtin_popcountll(__ballot(before));
         if (cnt == 0) return AttnSeq{0, 0, 0};
         lo += (cnt - 1) * step;
         n = min(step, n - (cnt - 1) * step);
-        if (step == 1) break;
     }
-    lo = __builtin_amdgcn_readfirstlane(lo);
-    const int start = at(lo), end = at(lo + 1);
-    const int tile = vt - (start / BM + lo);
-    // (where offsets fall, the search may end anywhere: tiles before a sequence's first are none)
-    return AttnSeq{start, tile >= 0 && (int64_t)tile * BM < end - start ? end - start : 0, tile};
+    const int start = lane < n ? at(lo + lane) : 0, len = lane < n ? at(lo + lane + 1) - start : 0, tiles = len > 0 ? (len - 1) / BM + 1 : 0;
+    const int r = number - (__builtin_amdgcn_readfirstlane(start) / BM + lo);
+    // (where offsets fall, the search may end anywhere: what is before the first number is none)
+    const int sums = wave_sums(tiles);
+    if (r < 0 || r >= __builtin_amdgcn_readlane(sums, 63)) return AttnSeq{0, 0, 0};
+    const int mine = __builtin_popcountll(__ballot(sums <= r)); // sequences whose tiles come before
+    const int its = __builtin_amdgcn_readlane(tiles, mine), i = __builtin_amdgcn_readlane(sums, mine) - 1 - r; // tiles from the last one
+    return AttnSeq{__builtin_amdgcn_readlane(start, mine), __builtin_amdgcn_readlane(len, mine), CAUSAL && !KEYS ? i : its - 1 - i};
 }
 
 // ---------------------------------------------------------------------------
@@ -316,15 +336,15 @@ template <int D> __device__ __forceinline__ f32x16 join_get(uint32_t at, const f
     return r;
 }
 
-// Tile and head of a workgroup.  Heads vary fastest; workgroups go to the eight dies in turn, so that where their number allows it a
-// die has neighbouring heads, which share keys and values, in its L2.  Later tiles go first: with causal they take longest.
+// Head and number of a workgroup.  Heads vary fastest; workgroups go to the eight dies in turn, so that where their number allows it a
+// die has neighbouring heads, which share keys and values, in its L2.
 struct AttnWork {
-    int head, vt;
+    int head, number;
 };
-__device__ __forceinline__ AttnWork attn_work(unsigned heads, unsigned tiles, bool last_first)
+__device__ __forceinline__ AttnWork attn_work(unsigned heads)
 {
-    const unsigned i = blockIdx.x % heads, vt = blockIdx.x / heads;
-    return AttnWork{(int)(heads % 8 == 0 ? (i % 8) * (heads / 8) + i / 8 : i), (int)(last_first ? tiles - 1 - vt : vt)};
+    const unsigned i = blockIdx.x % heads, number = blockIdx.x / heads;
+    return AttnWork{(int)(heads % 8 == 0 ? (i % 8) * (heads / 8) + i / 8 : i), (int)number};
 }
 
 // ---------------------------------------------------------------------------
@@ -372,8 +392,8 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_f
     constexpr int BM = 128, BK = 64, TILE = BK * T::RB;
     __shared__ __attribute__((aligned(1024))) char lds[4 * TILE]; // keys, values, keys, values
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const AttnWork w = attn_work(a.heads, a.tiles, CAUSAL);
-    const AttnSeq seq = attn_seq<BM>(a, w.vt);
+    const AttnWork w = attn_work(a.heads);
+    const AttnSeq seq = attn_seq<BM, CAUSAL>(a, w.number);
     if (seq.len < 1) return;
     const int head = w.head, hk = head / a.group;
     const int q0 = seq.tile * BM + wave * 32, have = min(32, seq.len - q0);
@@ -479,8 +499,8 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 1) void k_attn_f
     constexpr int TILE = 32 * T::RB > 1024 ? 32 * T::RB : 1024, OWN = 4 * TILE;
     extern __shared__ __attribute__((aligned(1024))) char lds[]; // keys and values of 32 rows, twice, of each wavefront; largest scores and sums
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), me = lane & 31;
-    const AttnWork w = attn_work(a.heads, a.tiles, CAUSAL);
-    const AttnSeq seq = attn_seq<32>(a, w.vt);
+    const AttnWork w = attn_work(a.heads);
+    const AttnSeq seq = attn_seq<32, CAUSAL>(a, w.number);
     if (seq.len < 1) return;
     const int head = w.head, hk = head / a.group, q0 = seq.tile * 32, have = min(32, seq.len - q0);
     const bf16_t *kp = a.k + (int64_t)seq.start * a.ks + (int64_t)hk * a.d, *vp = a.v + (int64_t)seq.start * a.vs + (int64_t)hk * a.d;
@@ -634,8 +654,8 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_d
     constexpr int BM = 128, RING = B::RING;
     __shared__ __attribute__((aligned(1024))) char lds[RING * B::SLOT + B::HELD]; // 32 keys and their values a slot; do
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const AttnWork w = attn_work(a.heads, a.tiles, CAUSAL);
-    const AttnSeq seq = attn_seq<BM>(a, w.vt);
+    const AttnWork w = attn_work(a.heads);
+    const AttnSeq seq = attn_seq<BM, CAUSAL>(a, w.number);
     if (seq.len < 1) return;
     const int head = w.head, hk = head / a.group;
     const int q0 = seq.tile * BM + wave * 32, have = min(32, seq.len - q0), me = lane & 31;
@@ -748,8 +768,8 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 1) void k_attn_d
     // keys and values of 32 rows, twice, of each wavefront; do; r
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), me = lane & 31;
-    const AttnWork w = attn_work(a.heads, a.tiles, CAUSAL);
-    const AttnSeq seq = attn_seq<32>(a, w.vt);
+    const AttnWork w = attn_work(a.heads);
+    const AttnSeq seq = attn_seq<32, CAUSAL>(a, w.number);
     if (seq.len < 1) return;
     const int head = w.head, hk = head / a.group, q0 = seq.tile * 32, have = min(32, seq.len - q0);
     const int64_t row = seq.start + q0;
@@ -857,9 +877,9 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_d
     constexpr int BN = 128, RING = B::RING;
     __shared__ __attribute__((aligned(1024))) char lds[RING * B::SLOT + B::HELD + RING * 256]; // 32 queries and their do a slot; v; -lse log2(e) and delta
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), me = lane & 31;
-    const AttnWork w = attn_work(a.kv_heads, a.tiles * a.splits, false);
-    const int split = w.vt % a.splits;
-    const AttnSeq seq = attn_seq<BN>(a, w.vt / a.splits);
+    const AttnWork w = attn_work(a.kv_heads);
+    const int split = w.number % a.splits;
+    const AttnSeq seq = attn_seq<BN, CAUSAL, true>(a, w.number / a.splits);
     if (seq.len < 1) return;
     const int hk = w.head, key0 = seq.tile * BN + wave * 32, have = min(32, seq.len - key0);
     const int64_t row = seq.start + key0;
