@@ -178,7 +178,8 @@ struct Kv4Attend {
     int heads, group, tiles; // query heads, of a key and value head, tiles of 16 of those
     float c2;                // scale log2(e)
     const int32_t *table, *lens;
-    int table_len, splits;
+    int table_len, splits, batch;
+    int coarse; // sequences start in the order of lens >> coarse; -1: in theirs
     int64_t table_stride;
     const bf16_t *q;
     int64_t q_stride;
@@ -293,6 +294,30 @@ template <int NB, bool WIDE> struct Kv4Step {
     }
 };
 
+// The j-th sequence to be started, and its tokens.  Workgroups start in the order of their numbers; where the longest may take several times as
+// long as others (kv4_coarse), of every 64 neighbouring sequences those with most tokens come first, in steps of 2^coarse tokens.
+struct Kv4Seq {
+    int b, len;
+};
+__device__ __forceinline__ Kv4Seq kv4_seq(const Kv4Attend &a, int j)
+{
+    if (a.coarse < 0) return Kv4Seq{j, kv4_tokens(a.lens[j], a.table_len, a.c.shift)};
+    const int lane = threadIdx.x & 63, b0 = j & ~63;
+    const int len = b0 + lane < a.batch ? kv4_tokens(a.lens[b0 + lane], a.table_len, a.c.shift) : -1, n = len >> a.coarse;
+    j &= 63;
+    int x = 0, longer = 0; // the n of the one looked for is the largest x with more than j of n >= x
+#pragma unroll
+    for (int bit = 8; bit; bit /= 2) {
+        const int c = __builtin_popcountll(__ballot(n >= x + bit));
+        longer = c > j ? longer : c;
+        x = c > j ? x + bit : x;
+    }
+    const uint64_t there = __ballot(n == x);
+    const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(there >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)there, 0));
+    const int at = __builtin_ctzll(__ballot(n == x && before == j - longer));
+    return Kv4Seq{b0 + at, __builtin_amdgcn_readlane(len, at)};
+}
+
 // One (sequence, tile of 16 query heads of a key and value head, split) a workgroup.  Scores are computed turned round, tokens by heads:
 // S^T = K q^T, so that a lane has one head's scores of 8 tokens (its column of the result) and these are, in place, the operand of
 // o^T = V^T p^T, whose columns are heads again: maxima, sums and rescaling stay inside a lane or go over the four lanes of a head.
@@ -308,8 +333,9 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 4) void k_kv4_attend(c
     id /= a.splits;
     const int tile = id % a.tiles;
     id /= a.tiles;
-    const int hk = id % a.c.kv_heads, b = id / a.c.kv_heads;
-    const int len = kv4_tokens(a.lens[b], a.table_len, a.c.shift), per = WAVES == 16 ? len : kv4_per_split(len, a.splits);
+    const int hk = id % a.c.kv_heads;
+    const Kv4Seq seq = kv4_seq(a, id / a.c.kv_heads);
+    const int b = seq.b, len = seq.len, per = WAVES == 16 ? len : kv4_per_split(len, a.splits);
     const int begin = (int64_t)split * per < len ? split * per : len, end = len - begin < per ? len : begin + per;
     if (split > 0 && begin >= end) return;
     const int32_t *table = a.table + b * a.table_stride;
@@ -525,6 +551,17 @@ static int kv4_splits(const pac_kv4 *c, int heads, int batch, int table_len)
     const int64_t s = want < fit ? want : fit;
     return (int)(s < 1 ? 1 : s > kKvSplits ? kKvSplits : s);
 }
+// In which steps of 2^.. tokens, at most 16 of them, sequences are sorted by their lengths (-1: not at all).  Worth the look at 64 lengths where a
+// workgroup may have many tokens; us, in order / sorted, 32/8 heads of 128: 64 x 1..4096 tokens (at most 1024 a workgroup) 41.1 / 36.7, 128 x
+// 1..4096 (2048) 69.6 / 63.1, 4 x 1..65536 (1024) 38.7 / 32.4, 16 heads of 64, 32 x 1000..3000 (768) 25.2 / 23.5; but 4 x 60001..65536 (1024) 54.1 /
+// 55.5, 32 x 1..4096 (512) 25.5 / 26.8, 16 x 1..4096 (256) 18.6 / 19.8, and with a workgroup for every sequence 200 x 1..2048 of 32 heads 110 / 113.
+static int kv4_coarse(int batch, int64_t most, int splits)
+{
+    if (batch < 2 || splits < 2 || most <= 512 * (int64_t)splits) return -1;
+    int c = 0;
+    while (most >> c > 15) ++c;
+    return c;
+}
 static pac_status check_attend(const pac_kv4 *c, int32_t heads, int32_t batch, int32_t table_len)
 {
     const pac_status s = check_kv4(c);
@@ -640,7 +677,9 @@ pac_status pac_kv4_attend(const pac_kv4 *c, int32_t heads, float scale, int32_t 
     a.c = kv4_of(c);
     a.heads = heads; a.group = heads / c->kv_heads; a.tiles = (a.group + 15) / 16;
     a.c2 = scale * 1.4426950408889634f;
-    a.table = table; a.lens = lens; a.table_len = table_len; a.splits = splits < 1 ? 1 : splits; a.table_stride = table_stride;
+    a.table = table; a.lens = lens; a.table_len = table_len; a.splits = splits < 1 ? 1 : splits; a.batch = batch;
+    a.coarse = kv4_coarse(batch, (int64_t)table_len * c->page, splits);
+    a.table_stride = table_stride;
     a.q = static_cast<const bf16_t *>(q); a.q_stride = q_stride;
     a.o = static_cast<bf16_t *>(o); a.o_stride = o_stride;
     a.part = static_cast<float *>(workspace);

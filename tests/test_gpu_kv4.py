@@ -384,3 +384,22 @@ def test_prompt_then_tokens():
         # 4 bits lose about a tenth of a value; the answer stays that near
         far = float((o.double() - whole[t:t + 1].double()).norm() / whole[t:t + 1].double().norm())
         assert far < 0.5, far
+
+
+@pytest.mark.parametrize("batch", [2, 63, 64, 65, 130])
+def test_sequences_of_any_lengths_in_any_order(batch):
+    """Long ones are started first, 64 sequences at a time: each is answered once, also those of one length, without tokens (a negative length)
+    and with all that the table holds (a length past it)."""
+    heads, kv, d, page, most = 2, 1, 32, 16, 16384
+    g = torch.Generator().manual_seed(batch)
+    lens = torch.randint(1, most, (batch,), generator=g)
+    lens[torch.rand(batch, generator=g) < 0.6] //= 40
+    lens[torch.rand(batch, generator=g) < 0.2] = 1023
+    lens[1], lens[batch // 2] = most, 0
+    lens = lens.tolist()
+    c, table, ln, kb, vb = filled(batch, lens, kv, d, page)
+    ln[1], ln[batch // 2] = most + 12345, -7
+    q = states(6, batch, heads * d) / 4
+    o = torch.full_like(q, 3.0)
+    c.attend(q, table, ln, o)
+    check(o, q, lens, kb, vb, kv, d, d ** -0.5)
