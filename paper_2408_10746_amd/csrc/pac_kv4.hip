@@ -190,9 +190,17 @@ struct Kv4Attend {
 };
 
 constexpr int kKvStep = 32;               // tokens of a wavefront's step
-constexpr int kKvShort = 1024;            // tokens that one workgroup of 16 wavefronts goes through instead of several of four
-constexpr int kKvLeast = 256;             // tokens that are worth a workgroup of their own
-constexpr int kKvTarget = 2048;            // workgroups wanted
+// Tokens that one workgroup of 16 wavefronts goes through instead of several of four.  One launch against two; us, with at most 512 / 1024 / 2048:
+// 700 tokens of 32 heads of 128 11.6 / 8.9 / 9.1, 4 x 900..1000 of 32/8 12.0 / 9.3 / 9.1, 8 x 900..1000 of 32 14.5 / 10.9 / 10.9, 8 x 500..1500 of
+// 32/8 11.9 / 11.8 / 10.8, 2000 tokens of 32 11.7 / 11.4 / 12.7.
+constexpr int kKvShort = 1024;
+// Tokens that are worth a workgroup of their own, us with 128 / 256 / 512: 8 x 1..4096 tokens of 32/8 heads of 128 13.3 / 14.6 / 14.1, 16 x
+// 1..4096 15.3 / 16.4 / 18.9, 30000 of one sequence 17.1 / 17.4 / 16.9.
+constexpr int kKvLeast = 128;
+// Workgroups wanted: the card once, four a compute unit.  With 768 / 1024 / 1536 / 2048 of them, us, caches that take turns: 4 x 60001..65536 tokens
+// of 32/8 heads of 128 57.6 / 59.4 / 64.3 / 63.1, 64 x 1..4096 40.1 / 40.0 / 41.4 / 41.6, 32 x 1..4096 23.3 / 22.9 / 24.9 / 26.0, 32 x
+// 1000..3000 of 16 heads of 64 22.3 / 22.1 / 23.6 / 24.1, but 4 x 1..65536 41.7 / 35.3 / 34.0 / 36.8, 16 x 1..32768 75.3 / 69.3 / 70.4 / 69.6.
+constexpr int kKvTarget = 1024;
 constexpr int kKvSplits = 128;            // of a sequence, at most
 
 // tokens of a split of a sequence of len tokens, and how many splits have any
@@ -541,7 +549,7 @@ static Kv4 kv4_of(const pac_kv4 *c)
     return Kv4{static_cast<char *>(c->at), c->pages, shift, c->kv_heads, c->d};
 }
 
-// Splits of the long axis: workgroups for eight a compute unit, none of fewer than kKvLeast tokens.  Short sequences that leave most of
+// Splits of the long axis: workgroups for four a compute unit, none of fewer than kKvLeast tokens.  Short sequences that leave most of
 // the card idle take one workgroup of 16 wavefronts each (0 splits), which saves the second launch.
 static int kv4_splits(const pac_kv4 *c, int heads, int batch, int table_len)
 {
@@ -552,12 +560,14 @@ static int kv4_splits(const pac_kv4 *c, int heads, int batch, int table_len)
     return (int)(s < 1 ? 1 : s > kKvSplits ? kKvSplits : s);
 }
 // In which steps of 2^.. tokens, at most 16 of them, sequences are sorted by their lengths (-1: not at all).  Worth the look at 64 lengths where a
-// workgroup may have many tokens; us, in order / sorted, 32/8 heads of 128: 64 x 1..4096 tokens (at most 1024 a workgroup) 41.1 / 36.7, 128 x
-// 1..4096 (2048) 69.6 / 63.1, 4 x 1..65536 (1024) 38.7 / 32.4, 16 heads of 64, 32 x 1000..3000 (768) 25.2 / 23.5; but 4 x 60001..65536 (1024) 54.1 /
-// 55.5, 32 x 1..4096 (512) 25.5 / 26.8, 16 x 1..4096 (256) 18.6 / 19.8, and with a workgroup for every sequence 200 x 1..2048 of 32 heads 110 / 113.
-static int kv4_coarse(int batch, int64_t most, int splits)
+// workgroup may have many tokens and the card is filled a few times at most; us, in order / sorted, 32/8 heads of 128 over caches that take turns:
+// 64 x 1..4096 tokens (2048 a workgroup at most) 48.9 / 40.0, 32 x 1..4096 (1024) 26.3 / 23.2, 4 x 1..65536 (2048) 38.6 / 35.5, 16 x 1..32768
+// (4096) 79.2 / 69.5, 256 x 1..4096 (4096) 127.7 / 121.7, of 32 heads without sharing 40 x 1..4096 84.3 / 69.2; lengths alike 59.2 / 59.4 (4 x
+// 60001..65536), 29.7 / 30.2 (64 x 1500); but 16 x 1..4096 (512) 18.6 / 19.8, and where workgroups are many anyhow, 200 x 1..2048 of 32 heads
+// of 64, 110.1 / 114.3.
+static int kv4_coarse(int batch, int64_t base, int64_t most, int splits)
 {
-    if (batch < 2 || splits < 2 || most <= 512 * (int64_t)splits) return -1;
+    if (batch < 2 || splits < 1 || most <= 512 * (int64_t)splits || base > 4096) return -1;
     int c = 0;
     while (most >> c > 15) ++c;
     return c;
@@ -678,7 +688,7 @@ pac_status pac_kv4_attend(const pac_kv4 *c, int32_t heads, float scale, int32_t 
     a.heads = heads; a.group = heads / c->kv_heads; a.tiles = (a.group + 15) / 16;
     a.c2 = scale * 1.4426950408889634f;
     a.table = table; a.lens = lens; a.table_len = table_len; a.splits = splits < 1 ? 1 : splits; a.batch = batch;
-    a.coarse = kv4_coarse(batch, (int64_t)table_len * c->page, splits);
+    a.coarse = kv4_coarse(batch, (int64_t)batch * c->kv_heads * a.tiles, (int64_t)table_len * c->page, splits);
     a.table_stride = table_stride;
     a.q = static_cast<const bf16_t *>(q); a.q_stride = q_stride;
     a.o = static_cast<bf16_t *>(o); a.o_stride = o_stride;
