@@ -47,7 +47,9 @@ pac_status pac_attn_forward(const pac_attn *a /*HOST*/, const int32_t *offsets /
                             const void *v /*DEVICE*/, int64_t v_stride, void *o /*DEVICE*/, int64_t o_stride,
                             float *lse /*DEVICE*/, void *hip_stream);
 
-/* Bytes of workspace for the gradients of `rows` rows in `batch` sequences, never fewer for more of either; -1 on bad arguments. */
+/* Bytes of workspace for the gradients of `rows` rows in `batch` sequences: two fp32 numbers a row and head, and partial sums of dk and dv where
+ * few tiles of keys have many queries.  A bound that never falls as either grows, so that it serves smaller calls too; a call asks for what its own sizes
+ * take.  -1 on bad arguments. */
 int64_t pac_attn_workspace_bytes(const pac_attn *a /*HOST*/, int32_t batch, int64_t rows);
 
 /* q, k, v, offsets as in the forward pass, o and lse what it wrote; do_ [rows][heads d]; dq [rows][heads d], dk, dv

@@ -25,7 +25,7 @@
 extern "C" {
 #endif
 
-/* HOST.  pages 0..2^31 - 1   page a power of two, 8..65536   kv_heads 1..4096   d values a head, 8..128, a multiple of 8
+/* HOST.  pages 0..2^31 - 1   page a power of two, 8..65536   kv_heads 1..4096   d values a head, 8..128, a multiple of 8   (2^62 bytes in all)
  * at DEVICE, pac_kv4_bytes bytes, 16-byte aligned (NULL where pages is 0) */
 typedef struct {
     void *at;
@@ -42,7 +42,7 @@ int64_t pac_kv4_bytes(const pac_kv4 *c /*HOST*/);
  *   k, v    DEVICE [rows][kv_heads d] of `dtype` (pac_dtype), k_stride and v_stride >= kv_heads d elements from row to row, any
  *           alignment of their type          slots   DEVICE int64 [rows], 8-byte aligned
  * rows = 0: nothing happens, and the addresses may be NULL.  Errors: NULL, SHAPE (the structure, dtype), RANGE (rows < 0, strides, k, v
- * or slots inside the cache), ALIGN, UNSUPPORTED (2^31 or more rows by heads), DEVICE. */
+ * or slots inside the cache), ALIGN, UNSUPPORTED (2^31 or more rows by heads, or 2^29 or more rows by blocks of all heads), DEVICE. */
 pac_status pac_kv4_write(const pac_kv4 *c /*HOST*/, int64_t rows, const int64_t *slots /*DEVICE*/, const void *k /*DEVICE*/,
                          int64_t k_stride, const void *v /*DEVICE*/, int64_t v_stride, int32_t dtype, void *hip_stream);
 
@@ -51,7 +51,8 @@ pac_status pac_kv4_write(const pac_kv4 *c /*HOST*/, int64_t rows, const int64_t 
 pac_status pac_kv4_read(const pac_kv4 *c /*HOST*/, int64_t rows, const int64_t *slots /*DEVICE*/, void *k /*DEVICE*/, int64_t k_stride,
                         void *v /*DEVICE*/, int64_t v_stride, int32_t dtype, void *hip_stream);
 
-/* Bytes of workspace for attend: partial results of long sequences, never fewer for a larger batch or table; -1 on bad arguments. */
+/* Bytes of workspace for attend: partial results of long sequences.  A bound that never falls as the batch or the table grows, so that it serves smaller calls
+ * too; a call asks for what its own sizes take, which may be nothing (NULL then).  -1 on bad arguments. */
 int64_t pac_kv4_attend_workspace_bytes(const pac_kv4 *c /*HOST*/, int32_t heads, int32_t batch, int32_t table_len);
 
 /* One query a head and sequence over the cache.
@@ -63,7 +64,7 @@ int64_t pac_kv4_attend_workspace_bytes(const pac_kv4 *c /*HOST*/, int32_t heads,
  *   o       DEVICE bf16, as q, sharing memory with nothing else of the call (rows beside q's do not)
  *   workspace  DEVICE, 16-byte aligned; its contents are scratch
  * batch = 0: nothing happens.  Errors: NULL, SHAPE (the structure, heads, batch or table_len < 0), RANGE (scale, strides, shared memory),
- * ALIGN, UNSUPPORTED (table_len pages past 2^31 - 1 tokens, or 2^23 or more (sequence, 16 heads of a group) pairs), WORKSPACE, DEVICE. */
+ * ALIGN, UNSUPPORTED (table_len pages past 2^31 - 4097 tokens, or 2^23 or more sequences by heads), WORKSPACE, DEVICE. */
 pac_status pac_kv4_attend(const pac_kv4 *c /*HOST*/, int32_t heads, float scale, int32_t batch, const int32_t *table /*DEVICE*/,
                           int32_t table_len, int64_t table_stride, const int32_t *lens /*DEVICE*/, const void *q /*DEVICE*/,
                           int64_t q_stride, void *o /*DEVICE*/, int64_t o_stride, void *workspace /*DEVICE*/,

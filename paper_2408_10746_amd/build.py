@@ -27,7 +27,7 @@ HIPCC_FLAGS = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
 ]
 # Products of attention's backward pass are read by the vector units one by one: their matrix instructions write vector registers, not
-# accumulation registers that would have to be copied (4001 + 6143 tokens there and back 2645 -> 2500 us)
+# accumulation registers that would have to be copied (4001 + 6143 tokens there and back, when it was chosen, 2645 -> 2500 us)
 SOURCE_FLAGS = {"pac_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 

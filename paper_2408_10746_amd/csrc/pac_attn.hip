@@ -348,9 +348,16 @@ __device__ __forceinline__ AttnWork attn_work(unsigned heads)
 }
 
 // ---------------------------------------------------------------------------
-// forward: 128 rows a workgroup, 32 a wavefront, which holds its queries and o in registers; 64 keys and values at a time in LDS, the
+// forward: one pass over the keys with a running maximum m and sum,
+//     o = (sum_j 2^(s_j c - m) v_j) / (sum_j 2^(s_j c - m)),     c = scale log2 e,     lse = (m + log2 of the sum) ln 2
+// 128 rows a workgroup, 32 a wavefront, which holds its queries and o in registers; 64 keys and values at a time in LDS, the
 // next ones on their way.  S^T = K q^T has a query's scores in one column, so that maximum, sum and rescaling stay in a lane, and p in
-// place as the operand of o^T = V^T p^T.
+// place as the operand of o^T = V^T p^T.  p is rounded to bf16 because the matrix units take it so; the sum is of the values before.
+// Long sequences: 8192 tokens of 32/8 heads of 128, causal, 510 us, 1.08 PFLOP/s (a product of 8192^3: 1.23 to 1.48).  Matrix units 60 % busy, LDS reads
+// 30 %, waiting 18 %, at the 1.9 GHz that such a load is given: bound by the issue of matrix and vector instructions side by side.  Short ones
+// by memory and the first loads' latency: 16 x 256 tokens of 32 heads 36 us (3.8 TB/s).  Two wavefronts a SIMD use all of the registers; without
+// tiles on their way and with spilled registers the first took 2173 us.  Rescaling only where a row's maximum has grown by 2^8 leaves most
+// steps without it, and p below 2^8, far from where sums of fp32 end.
 // ---------------------------------------------------------------------------
 template <int D> struct AttnRow { // a wavefront's 32 rows on their way
     f32x16 acc[D / 32];
@@ -491,7 +498,8 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_f
 // ---------------------------------------------------------------------------
 // forward, few rows: 32 rows a workgroup, whose four wavefronts deal the keys among them, 32 at a time, each through two LDS places of its own
 // and without a barrier, and join what they have at the end.  Four times the workgroups, a quarter of the way for each; every key is fetched for
-// 32 rows instead of 128, so that it pays only where the card would be mostly idle (attn_few).
+// 32 rows instead of 128, so that it pays only where the card would be mostly idle (attn_few has both sides' times).  Bound by the longest
+// workgroup's chain of steps: 1788 tokens of 6 heads of 128, causal, 20 us, 14 steps a wavefront.
 // ---------------------------------------------------------------------------
 template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 1) void k_attn_fwd_few(const AttnArgs a)
 {
@@ -581,7 +589,9 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 1) void k_attn_f
 // backward.  Both kernels walk over subtiles of 32 x 32 pairs, whose rows come through a ring of LDS slots: two products (scores, do . v),
 // 16 values of p and ds a lane, and the products that p and ds enter.  Two wavefronts share a SIMD: alone on it, one issues a vector
 // instruction in every second slot at best (measured: 6.5 cycles each against 4 with two).  At 128 values a head that takes one of the
-// wavefront's own two operands out of the registers: do (of dq) or v (of dk and dv) is read from LDS again for every subtile.
+// wavefront's own two operands out of the registers: do (of dq) or v (of dk and dv) is read from LDS again for every subtile, and leaves room
+// for a ring of two slots.  (4001 + 6143 tokens of 32/8 heads there and back, us: one wavefront a SIMD and four slots 2397, two wavefronts
+// and two slots 2238; with three or four slots for dk and dv, one workgroup a compute unit, 2479.)
 // ---------------------------------------------------------------------------
 template <int D> struct AttnBack {
     using T = AttnTile<D>;
@@ -597,7 +607,7 @@ __device__ __forceinline__ void pair_products(f32x16 &s, f32x16 &dn, const AttnL
                                               const bf16x8 (&b2)[AttnBack<D>::REGS], const AttnLane<D> &own)
 {
     constexpr bool OWN = AttnBack<D>::OWN;
-    constexpr int N = D / 16, AHEAD = OWN ? 1 : 2; // (with 128 values a head two sets of operands ahead are spilled registers)
+    constexpr int N = D / 16, AHEAD = OWN ? 1 : 2; // (128 values a head: two sets ahead are spilled registers; 8 x 256..1024 tokens there and back 321 us, one 287)
     bf16x8 f1[AHEAD + 1], f2[AHEAD + 1], f3[AHEAD + 1];
     auto read = [&](int n) {
         f1[n % (AHEAD + 1)] = l1.along(0, n);
@@ -647,6 +657,8 @@ __device__ __forceinline__ void pair_sums(f32x16 (&acc)[D / 32], f32x16 (&more)[
 // has the exact delta; r is small, so that p in bf16 is more than enough for y, whose products share their operand from LDS with dq's.
 // delta' + r goes to memory for the other kernel, with -lse log2(e).  delta' comes from the product that makes do . v too (the diagonal of
 // do o^T), so that a row with one key has exactly no gradient in q and k.
+// Four products instead of three: 4001 + 6143 tokens of 32/8 heads 757 us, 1.16 PFLOP/s, matrix units 66 % busy, LDS reads 33 %, waiting 22 %,
+// at 1.84 GHz; dq's error 0.0024 of its size, 0.0037 with bf16(o)'s delta.  8 x 256..1024 tokens of 32 heads 112 us: 45 % waiting for first loads.
 // ---------------------------------------------------------------------------
 template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a)
 {
@@ -760,7 +772,7 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_d
     }
 }
 
-// dq, few rows: as the forward kernel for few rows
+// dq, few rows: as the forward kernel for few rows (4096 tokens of one head of 64 there and back 168 us with 128 rows a workgroup, 98 with this)
 template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 1) void k_attn_dq_few(const AttnArgs a)
 {
     using B = AttnBack<D>;
@@ -870,6 +882,10 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 1) void k_attn_d
 // do at a time in LDS, of all heads of the group one after the other.  S = q K^T has a key's scores in one column.
 // The first keys of a long causal sequence have all of its queries to go through, and a launch ends with its longest workgroup, so the
 // queries may be dealt to several (attn_splits), whose sums another launch adds up in order.
+// 4001 + 6143 tokens of 32/8 heads of 128: 859 us, 1.03 PFLOP/s, matrix units 57 % busy, LDS reads 43 %, waiting 37 % (a barrier for every 32
+// queries, and two splits' workgroups of unequal lengths); 8 x 256..1024 tokens of 32 heads 131 us, 32 x 1..128 of 12 of 64 11 us: first loads.
+// Measured and not kept: eight wavefronts a workgroup (950 instead of 1025 us then, but 32 x 1..128 16.2 instead of 11.6), queries from
+// the last to the first (373 instead of 325), the next tile's operands asked for before the barrier (2529 instead of 2397 there and back).
 // ---------------------------------------------------------------------------
 template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_dkv(const AttnArgs a)
 {
@@ -1046,7 +1062,8 @@ template <int D, bool CAUSAL> __global__ __launch_bounds__(256, 2) void k_attn_d
     }
 }
 
-// The splits' sums, in order: eight values a thread of dk and as many of dv.  Bound by memory.
+// The splits' sums, in order: eight values a thread of dk or dv.  Bound by memory: 10144 rows, two splits of 8 heads of 128, 32 us (166 MB read, 42
+// written: 6.5 TB/s, partly from the last cache).
 __global__ __launch_bounds__(256) void k_attn_join(const AttnArgs a)
 {
     const int chunks = a.kv_heads * a.d / 8;
@@ -1107,13 +1124,18 @@ static AttnArgs attn_args(const pac_attn *a, const int32_t *off, int32_t batch, 
 }
 static int64_t stat_bytes(const pac_attn *a, int64_t rows) { return (rows * a->heads * 4 + 255) / 256 * 256; }
 
-// Whether a call's rows are few: forward and dq then take 32 rows a workgroup and deal the keys to its wavefronts.  Forward, us, 128 rows /
-// 32 rows a workgroup: causal 1 x 8000 of 4 heads (252 workgroups of 128 rows) 91 / 63, 1000 of 10 (80) 23 / 15, 1788 of 6 (102) 36 / 21, but
-// 4000 of 8 (256) 74 / 87 and 2000 of 12 (192) 39 / 42; not causal, whose workgroups all take as long, 1500 of 5 (60) 31 / 20, 4000 of 1 (32)
-// 68 / 36, but 1000 of 10 (80) 23 / 26 and 4000 of 4 (128) 68 / 69.  Below some 100 tokens there is nothing to deal: 19 tokens 7.5 / 8.7.
+// Whether a call's rows are few: forward and dq then take 32 rows a workgroup and deal the keys to its wavefronts.  Up to 64 values a head two such
+// workgroups share a compute unit, past that one has it alone.  Us, 128 rows / 32 rows a workgroup (workgroups of 128 rows in brackets):
+//   causal, 128 values, forward   1000 tokens of 10 heads (80) 24.0 / 16.1, 1788 of 6 (84) 36.1 / 22.0, 4000 of 5 (160) 70.2 / 61.1, 1600 of 12 (156)
+//                                 32.2 / 32.5, but 1000 of 20 (160) 25.3 / 28.0, 2000 of 12 (192) 38.9 / 42.5, 4000 of 8 (256) 73.0 / 83.9
+//           64 values             2000 of 12 (192) 27.4 / 19.7, 8000 of 4 (252) 92.5 / 71.9, but 1000 of 40 (320) 18.5 / 23.0, 4000 of 12 (384) 54.2 / 61.6
+//   not causal, 128 values        1500 of 5 (60) 31.6 / 20.6, but 1600 of 6 (78) 32.1 / 37.4; all tiles take as long there
+//           64 values             4000 of 4 (128) 48.1 / 33.9, 1000 of 16 (128) 17.1 / 12.8, but 2000 of 16 (256) 30.6 / 38.7
+// and there and back as these or better.  Below some 100 tokens there is nothing to deal: 19 tokens 8.2 / 8.7.
 static bool attn_few(const pac_attn *a, int32_t batch, int64_t rows)
 {
-    return (rows / 128 + batch) * a->heads <= (a->causal ? 192 : 72) && rows >= 128 * (int64_t)batch;
+    const int64_t most = a->d > 64 ? (a->causal ? 160 : 72) : (a->causal ? 256 : 128);
+    return (rows / 128 + batch) * a->heads <= most && rows >= 128 * (int64_t)batch;
 }
 // Starts a kernel with that much LDS
 template <typename K> static bool attn_launch(K kernel, unsigned blocks, int lds, hipStream_t st, const AttnArgs &r)
@@ -1129,8 +1151,8 @@ template <int D> static int few_lds(bool back)
 }
 
 // Workgroups of dk and dv: as many as a launch needs to fill the card and to end evenly, if each then still has enough to do to pay for
-// sums that go through memory.  (There and back, us, without splits / with: 500 tokens of 64 heads on one key head 1040 / 83, 2048 tokens
-// 32/8 heads 429 / 256, 4001 + 6143 tokens 32/8 heads 2216 / 2149.  With 1536 workgroups wanted 6000 tokens of 16 heads take 453, not 430.)
+// sums that go through memory.  (There and back, us, without splits / with: 500 tokens of 64 heads on one key head 1025 / 82, 2048 tokens
+// 32/8 heads 417 / 253, 4001 + 6143 tokens 32/8 heads 2180 / 2067.  With 1536 workgroups wanted 6000 tokens of 16 heads take 453, not 430.)
 constexpr int64_t kAttnTarget = 1300, kAttnLeast = 32, kAttnSplits = 64; // workgroups wanted; subtiles worth one; at most
 static int attn_splits(const pac_attn *a, int32_t batch, int64_t rows)
 {

@@ -85,6 +85,9 @@ template <int NB> __device__ __forceinline__ char *kv4_scales(const Kv4Io &a, co
 // offset of byte p = 0..3 of a unit of V
 template <int NB> __device__ constexpr int kv4_v_byte(int p) { return NB == 3 ? 12 * p : (p / NB) * (4 * NB) + p % NB; }
 
+// scale = 2^(exponent of the absmax - 2), codes = values / scale rounded once by the conversion instruction: exact but for that.
+// Bound by memory: 8192 tokens of 8 heads of 128 in bf16, 34 MB in and 9 out, 11 to 13 us (3.3 to 3.9 TB/s); 48 tokens a launch's time, 3.2 us.
+// With one token a wavefront, whose bytes of V lie in other wavefronts' lines, in and out took 26 us and now take 21.
 template <typename T, int NB, bool VEC>
 __global__ __launch_bounds__(256) void k_kv4_write(const Kv4Io a)
 {
@@ -138,6 +141,7 @@ __global__ __launch_bounds__(256) void k_kv4_write(const Kv4Io a)
     if ((id & 3) == 0) *kv4_scales<NB>(a, u, part, tok) = (char)byte;
 }
 
+// value = code scale, exact.  Bound by memory: 8192 tokens of 8 heads of 128, 9 MB in and 34 out, 9 to 10 us.
 template <typename T, int NB, bool VEC>
 __global__ __launch_bounds__(256) void k_kv4_read(const Kv4Io a)
 {
@@ -223,7 +227,8 @@ template <int AT> __device__ __forceinline__ bf16x2 v_pair(const uint32_t *w, fl
 
 // What a lane holds of a step's 32 tokens: two tiles of 16 tokens of K, two groups of four tokens of V.  Where a page has 16 tokens or
 // more (WIDE), a tile lies in one page, whose place is the same for all lanes: its entry in the table comes through scalars, and a lane's
-// places are constant distances from there.  Else a lane looks up the pages of its tokens.  Entries are fetched a step before the codes, so that a
+// places are constant distances from there (32 x 1000..3000 tokens of 16 heads of 64, pages of 16: 30 us by lanes, 26 so).  Else a lane looks up
+// the pages of its tokens.  Entries are fetched a step before the codes, so that a
 // step waits for one trip to memory and not for two.
 template <int NB, bool WIDE> struct Kv4Step {
     static constexpr int S = NB == 3 ? 3 : 1;
@@ -330,6 +335,9 @@ __device__ __forceinline__ Kv4Seq kv4_seq(const Kv4Attend &a, int j)
 // S^T = K q^T, so that a lane has one head's scores of 8 tokens (its column of the result) and these are, in place, the operand of
 // o^T = V^T p^T, whose columns are heads again: maxima, sums and rescaling stay inside a lane or go over the four lanes of a head.
 // The wavefronts take steps of 32 tokens in turn, a step's loads ahead.
+// Bound by memory: 4 x 60001..65536 tokens of 32/8 heads of 128, 273 MB, 47 us where the cache was just read (5.8 TB/s), 59 for the whole call over
+// caches that take turns; 64 x 1..4096 tokens 32 us, with the join 40.  700 tokens of 32 heads 7.5 us, a launch and three trips to memory.
+// (Without page entries a step ahead, and pages looked up by every lane, 4 x 65536 tokens took 125 us; two steps of codes ahead were slower.)
 template <int NB, bool WIDE, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 4) void k_kv4_attend(const Kv4Attend a)
 {
@@ -483,7 +491,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 4) void k_kv4_attend(c
     }
 }
 
-// The splits of a sequence's head (at most kKvSplits): a thread adds up four values of every SETS-th split, then the sets are added in order.
+// The splits of a sequence's head (at most kKvSplits), each weighed by 2^(its largest score - the largest): 4.7 to 5.4 us, a launch and two trips to
+// memory.  A thread adds up four values of every SETS-th split, then the sets are added in order.
 template <int NB>
 __global__ __launch_bounds__(256) void k_kv4_join(const Kv4Attend a)
 {
