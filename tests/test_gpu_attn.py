@@ -373,3 +373,22 @@ def test_values_that_are_none_in_many_rows(which, bad):
         if which == "v":
             seen = got[0][at:, (heads - 1) * d + 5]
             assert seen.isnan().all() if math.isnan(bad) else (seen == bad).all()
+
+
+@pytest.mark.parametrize("d,lens,causal", [(128, [200], True), (128, [150, 50], True), (64, [131, 1, 70], False), (64, [200], False)])
+def test_rows_as_far_apart_as_strides_go(d, lens, causal):
+    """2^24 values from row to row: a tile's rows lie up to 2^32 bytes from its first, and the last ones past 2^32 values of the first."""
+    heads, kv, rows, far = 2, 1, sum(lens), 1 << 24
+    buffer = torch.empty(rows, far, device="cuda", dtype=BF)
+    at, views = 0, []
+    for h in (heads, kv, kv, heads, heads, heads, kv, kv):  # q, k, v, do, o, dq, dk, dv
+        views.append(buffer[:, at:at + h * d])
+        at += far // 8 // 8 * 8 - 8
+    q, k, v, do, o, dq, dk, dv = views
+    for to, x in zip((q, k, v, do), make(d, rows, heads, kv, d)):
+        to.copy_(x)
+    a, off, lse = rt.Attention(heads, d, kv_heads=kv, causal=causal), rt.packed_offsets(lens), torch.empty(heads, rows, device="cuda")
+    a.forward(q, k, v, off, o, lse)
+    a.backward(q, k, v, off, o, lse, do, dq, dk, dv)
+    c = torch.Tensor.contiguous
+    check(a, lens, (c(o), lse, c(dq), c(dk), c(dv)), c(q), c(k), c(v), c(do), d ** -0.5, causal)
