@@ -183,7 +183,7 @@ struct Kv4Attend {
     float c2;                // scale log2(e)
     const int32_t *table, *lens;
     int table_len, splits, batch;
-    int coarse; // sequences start in the order of lens >> coarse; -1: in theirs
+    int coarse; // sequences start in the order of lens >> coarse, -1: in their own
     int64_t table_stride;
     const bf16_t *q;
     int64_t q_stride;
@@ -336,7 +336,7 @@ __device__ __forceinline__ Kv4Seq kv4_seq(const Kv4Attend &a, int j)
 // o^T = V^T p^T, whose columns are heads again: maxima, sums and rescaling stay inside a lane or go over the four lanes of a head.
 // The wavefronts take steps of 32 tokens in turn, a step's loads ahead.
 // Bound by memory: 4 x 60001..65536 tokens of 32/8 heads of 128, 273 MB, 47 us where the cache was just read (5.8 TB/s), 59 for the whole call over
-// caches that take turns; 64 x 1..4096 tokens 32 us, with the join 40.  700 tokens of 32 heads 7.5 us, a launch and three trips to memory.
+// caches that take turns; 64 x 1..4096 tokens, 150 MB, 33 to 34 us in one launch, the call 37 to 39.  700 tokens of 32 heads 7.5 us, a launch and three trips to memory.
 // (Without page entries a step ahead, and pages looked up by every lane, 4 x 65536 tokens took 125 us; two steps of codes ahead were slower.)
 template <int NB, bool WIDE, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 4) void k_kv4_attend(const Kv4Attend a)
@@ -558,25 +558,29 @@ static Kv4 kv4_of(const pac_kv4 *c)
     return Kv4{static_cast<char *>(c->at), c->pages, shift, c->kv_heads, c->d};
 }
 
-// Splits of the long axis: workgroups for four a compute unit, none of fewer than kKvLeast tokens.  Short sequences that leave most of
-// the card idle take one workgroup of 16 wavefronts each (0 splits), which saves the second launch.
+// Splits of the long axis: workgroups for four a compute unit, none of fewer than kKvLeast tokens.  Two cases take one workgroup of 16 wavefronts for every
+// sequence and head instead (0 splits), which saves the second launch: short sequences that leave most of the card idle (kKvShort), and as many
+// sequences by heads as come to two or three such workgroups a compute unit, the longest first, which else would be two splits each.  The latter,
+// us, splits / 16 wavefronts, 32/8 heads of 128: 64 x 1..4096 tokens 40.6 / 38.6, 64 x 1..1000 19.3 / 15.8, 64 x 1500 30.2 / 28.8, 64 x
+// 3500..4096 59.5 / 57.7, 100 x 1..16000 174 / 173; but with more workgroups, which have one split each, 256 x 1..4096 121.9 / 130.3, 40 x 1..4096 of 32
+// heads 69.8 / 78.9.
 static int kv4_splits(const pac_kv4 *c, int heads, int batch, int table_len)
 {
     const int64_t base = (int64_t)batch * c->kv_heads * ((heads / c->kv_heads + 15) / 16), most = (int64_t)table_len * c->page;
     const int64_t want = (kKvTarget + base - 1) / base, fit = (most + kKvLeast - 1) / kKvLeast;
-    if (most <= kKvShort && base <= 256 && fit > 1) return 0;
+    if (fit > 1 && ((most <= kKvShort && base <= 256) || (base >= kKvTarget / 2 && base < kKvTarget))) return 0;
     const int64_t s = want < fit ? want : fit;
     return (int)(s < 1 ? 1 : s > kKvSplits ? kKvSplits : s);
 }
 // In which steps of 2^.. tokens, at most 16 of them, sequences are sorted by their lengths (-1: not at all).  Worth the look at 64 lengths where a
 // workgroup may have many tokens and the card is filled a few times at most; us, in order / sorted, 32/8 heads of 128 over caches that take turns:
-// 64 x 1..4096 tokens (2048 a workgroup at most) 48.9 / 40.0, 32 x 1..4096 (1024) 26.3 / 23.2, 4 x 1..65536 (2048) 38.6 / 35.5, 16 x 1..32768
+// 32 x 1..4096 tokens (1024 a workgroup at most) 26.3 / 23.2, 4 x 1..65536 (2048) 38.6 / 35.5, 16 x 1..32768
 // (4096) 79.2 / 69.5, 256 x 1..4096 (4096) 127.7 / 121.7, of 32 heads without sharing 40 x 1..4096 84.3 / 69.2; lengths alike 59.2 / 59.4 (4 x
-// 60001..65536), 29.7 / 30.2 (64 x 1500); but 16 x 1..4096 (512) 18.6 / 19.8, and where workgroups are many anyhow, 200 x 1..2048 of 32 heads
+// 60001..65536); but 16 x 1..4096 (512) 18.6 / 19.8, and where workgroups are many anyhow, 200 x 1..2048 of 32 heads
 // of 64, 110.1 / 114.3.
 static int kv4_coarse(int batch, int64_t base, int64_t most, int splits)
 {
-    if (batch < 2 || splits < 1 || most <= 512 * (int64_t)splits || base > 4096) return -1;
+    if (batch < 2 || base > 4096 || (splits ? most <= 512 * (int64_t)splits : base <= 256)) return -1;
     int c = 0;
     while (most >> c > 15) ++c;
     return c;

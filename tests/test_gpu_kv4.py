@@ -403,3 +403,19 @@ def test_sequences_of_any_lengths_in_any_order(batch):
     o = torch.full_like(q, 3.0)
     c.attend(q, table, ln, o)
     check(o, q, lens, kb, vb, kv, d, d ** -0.5)
+
+
+@pytest.mark.parametrize("batch,kv,d,page,most", [(64, 8, 32, 16, 700), (128, 4, 64, 8, 300), (520, 1, 96, 32, 129), (1020, 1, 40, 16, 2000)])
+def test_one_workgroup_for_every_sequence_and_head(batch, kv, d, page, most):
+    """As many sequences by heads as fill the card without a split, of all lengths and in any order."""
+    heads = 2 * kv
+    g = torch.Generator().manual_seed(batch)
+    lens = (torch.rand(batch, generator=g) ** 3 * most).long()
+    lens[batch // 3], lens[5] = most, 0
+    lens = lens.tolist()
+    c, table, ln, kb, vb = filled(batch, lens, kv, d, page)
+    ln[5] = -1
+    q = states(8, batch, heads * d) / 4
+    o = torch.full_like(q, 3.0)
+    c.attend(q, table, ln, o)
+    check(o, q, lens, kb, vb, kv, d, d ** -0.5)
