@@ -84,7 +84,6 @@ template <int BM, bool CAUSAL, bool KEYS = false> __device__ __forceinline__ Att
 // piece c of row x lies at c ^ swz(x).
 // ---------------------------------------------------------------------------
 template <int D> struct AttnTile {
-    static constexpr int CH = D / 8;                 // 16-byte pieces of a row
     static constexpr int RB = D == 96 ? 256 : 2 * D; // bytes from row to row
     static __device__ __forceinline__ int swz(int row)
     {
