@@ -1149,17 +1149,29 @@ template <int D> static int few_lds(bool back)
     return back ? 4 * place + (AttnBack<D>::OWN ? 32 * AttnTile<D>::RB : 0) + 512 : 4 * place + 1024;
 }
 
-// Workgroups of dk and dv: as many as a launch needs to fill the card and to end evenly, if each then still has enough to do to pay for
-// sums that go through memory.  (There and back, us, without splits / with: 500 tokens of 64 heads on one key head 1025 / 82, 2048 tokens
-// 32/8 heads 417 / 253, 4001 + 6143 tokens 32/8 heads 2180 / 2067.  With 1536 workgroups wanted 6000 tokens of 16 heads take 453, not 430.)
-constexpr int64_t kAttnTarget = 1300, kAttnLeast = 32, kAttnSplits = 64; // workgroups wanted; subtiles worth one; at most
+// Workgroups that share a tile of keys in dk and dv, i.e. parts that its queries are dealt into: by estimated time.  A subtile of 32 x 32 takes
+// 1.8 us at 128 values a head, 1.26 at 64; a launch takes as long as its longest workgroup (the first keys of a sequence of average length), or as all
+// of them together at 384 a time, and a tenth of the other; more than 512 workgroups slow each other by 13 %; sums that go through memory cost
+// 2 us and their bytes, written and read, at 6.7 TB/s.  The estimate's best among 1, 2, 3, 4, 6, 8, 12, 16 is 0.9 % slower on the average than the best measured
+// over 27 calls; there and back, us, 1 / 2 / 4 / 8 / 16 parts (the estimate's choice): 4001 + 6143 tokens of 32/8 heads of 128 2179 / 2044 / 2063 / 2185 /
+// 2495 (2), 2048 of 32/8 416 / 293 / 245 / 253 / 313 (6: 242), 4 x 300..600 of 32/8 178 / 134 / 119 / 137 / 179 (4), 500 of 64 heads of 64 on one key head
+// 1026 / 537 / 287 / 143 / 105 (16), 16 x 100..200 of 16/4 heads of 64 73 / 58 / 53 / 57 / 70 (3: 52), 4 x 1024 of 8 heads of 64 114 / 128 / 154 / 214 / 360 (1).
+constexpr int64_t kAttnTarget = 1300, kAttnSplits = 64; // workgroups and parts at most
 static int attn_splits(const pac_attn *a, int32_t batch, int64_t rows)
 {
-    const int64_t groups = (rows / 128 + batch) * a->kv_heads, group = a->heads / a->kv_heads;
-    const int64_t subtiles = batch ? rows / batch * group / 32 : 0; // that a tile of keys goes through, on the average
-    int64_t s = kAttnTarget / (groups < 1 ? 1 : groups);
-    if (s > subtiles / kAttnLeast) s = subtiles / kAttnLeast;
-    return (int)(s < 1 ? 1 : s > kAttnSplits ? kAttnSplits : s);
+    const int64_t groups = (rows / 128 + batch) * a->kv_heads;
+    if (groups < 1 || batch < 1) return 1;
+    const double longest = (double)rows / batch * (a->heads / a->kv_heads) / 32; // subtiles
+    const double each = 1.8 * (0.4 + 0.6 / 128 * a->d), all = longest * (a->causal ? 0.5 : 1) * groups * each * 1.13 / 384;
+    const double bytes = (double)rows * a->kv_heads * a->d * 8;
+    double best = 0;
+    int splits = 1;
+    for (int64_t s = 1; s <= kAttnSplits && (s == 1 || (s * groups <= kAttnTarget && s <= longest)); ++s) {
+        const double chain = longest / s * each * (groups * s > 512 ? 1.13 : 1);
+        const double t = (chain > all ? chain + 0.1 * all : all + 0.1 * chain) + (s > 1 ? 2 + 0.3e-6 * bytes * s : 0);
+        if (s == 1 || t < best) best = t, splits = (int)s;
+    }
+    return splits;
 }
 static int64_t part_bytes(const pac_attn *a, int64_t rows, int64_t splits) { return splits < 2 ? 0 : rows * 2 * a->kv_heads * a->d * 4 * splits; }
 static int64_t attn_bytes(const pac_attn *a, int32_t batch, int64_t rows) { return 2 * stat_bytes(a, rows) + part_bytes(a, rows, attn_splits(a, batch, rows)); }
@@ -1223,7 +1235,7 @@ int64_t pac_attn_workspace_bytes(const pac_attn *a, int32_t batch, int64_t rows)
 {
     if (check_attn(a, batch, rows) != PAC_OK) return -1;
     // splits become fewer as tiles become more: room for as many (row, split) pairs as a call of at most this size may have
-    int64_t most = rows * (a->heads / a->kv_heads) / 32 / kAttnLeast, pairs;
+    int64_t most = rows * (a->heads / a->kv_heads) / 32, pairs;
     most = most > kAttnSplits ? kAttnSplits : most;
     pairs = most < 2 ? 0 : rows * most;
     const int64_t filled = kAttnTarget * 128 / a->kv_heads + 128 * kAttnSplits;

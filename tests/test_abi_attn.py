@@ -165,3 +165,19 @@ def test_tables_near_the_last_token_number_are_refused():
         c = kv4(page=page, kv_heads=1)
         assert pb.pac_kv4_attend_workspace_bytes(c, 2, 1, refused) == -1 and pb.pac_kv4_attend_workspace_bytes(c, 2, 1, taken) > 0
         assert L.pac_kv4_attend(C.byref(c), 2, 1.0, 1, A, refused, refused, 1 << 50, 1 << 51, 128, 1 << 52, 128, 1 << 53, 1 << 40, None) == pb.PAC_ERR_UNSUPPORTED
+
+
+def test_the_bound_of_the_workspace_is_enough_for_the_call():
+    """A call that has as much as the bound says is refused for something else (dq in q's place)."""
+    for heads, kv_heads, d in ((1, 1, 8), (8, 8, 64), (32, 8, 128), (64, 1, 64), (12, 12, 96), (500, 500, 8), (4096, 1, 128)):
+        for causal in (0, 1):
+            a = attn(heads, kv_heads, d, causal)
+            far = [(1 << 45) * (k + 1) for k in range(11)]
+            for batch in (1, 2, 5, 64, 300):
+                for rows in (1, 31, 127, 128, 200, 1000, 1023, 5000, 16383, 16384, 70000, 200000):
+                    if (rows // 128 + batch) * heads >= 1 << 23:
+                        continue
+                    sq, sk = heads * d, kv_heads * d
+                    n = pb.pac_attn_workspace_bytes(a, batch, rows)
+                    got = backward(a, far[0], batch, rows, far[1], sq, far[2], sk, far[3], sk, far[4], sq, far[5], far[6], sq, far[1], sq, far[7], sk, far[8], sk, far[9], n)
+                    assert got == pb.PAC_ERR_RANGE, (heads, kv_heads, d, causal, batch, rows)

@@ -392,3 +392,15 @@ def test_rows_as_far_apart_as_strides_go(d, lens, causal):
     a.backward(q, k, v, off, o, lse, do, dq, dk, dv)
     c = torch.Tensor.contiguous
     check(a, lens, (c(o), lse, c(dq), c(dk), c(dv)), c(q), c(k), c(v), c(do), d ** -0.5, causal)
+
+
+@pytest.mark.parametrize("heads,kv,d,lens,causal", [(32, 8, 128, [300, 600, 450, 33], True), (16, 4, 64, [100, 200, 131, 64, 1, 177], True), (4, 4, 128, [900, 700], False),
+                                                    (3, 3, 96, [200, 10, 0, 97], True), (32, 8, 128, [512], True)])
+def test_queries_of_short_sequences_dealt_to_several_workgroups(heads, kv, d, lens, causal):
+    """Few tiles of keys, few queries for each: parts of a handful of subtiles, some of them none in the shorter sequences."""
+    rows = sum(lens)
+    q, k, v, do = make(heads + d, rows, heads, kv, d)
+    a, off = rt.Attention(heads, d, kv_heads=kv, causal=causal), rt.packed_offsets(lens)
+    got = run(a, q, k, v, do, off)
+    check(a, lens, got, q, k, v, do, d ** -0.5, causal)
+    assert all(torch.equal(x, y) for x, y in zip(got, run(a, q, k, v, do, off)))
