@@ -284,8 +284,6 @@ def _plain(s):
     for n in s["seqs"]:
         rows = slice(at, at + n)
         at += n
-        if n == 0:
-            continue
         q, k, v = _by_head(s["q"][rows], heads), _by_head(s["k"][rows], kv), _by_head(s["v"][rows], kv)
         do = _by_head(s["do"][rows], heads) if kind == "grad" else None
         wide = heads * n * n <= 1 << 28  # all heads at once, or a group after the other where their scores would take gigabytes
