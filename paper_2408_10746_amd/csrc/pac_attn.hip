@@ -1,5 +1,6 @@
 // Attention over packed sequences and its gradients (declared in include/pac_attn.h).
 #include "../../include/pac_attn.h"
+#include "pac_attn_tile.h"
 #include "pac_mma.h"
 #include "pac_span.h"
 #include <cfloat>
@@ -75,46 +76,27 @@ template <int BM, bool CAUSAL, bool KEYS = false> __device__ __forceinline__ Att
     return AttnSeq{__builtin_amdgcn_readlane(start, mine), __builtin_amdgcn_readlane(len, mine), CAUSAL && !KEYS ? i : its - 1 - i};
 }
 
-// ---------------------------------------------------------------------------
-// Tiles of keys, values, queries or their gradients in LDS: rows of D values (padded with zeros), read in two ways.
-//   along the row   16 bytes a lane, 16 rows at the same place at a time
-//   turned round    ds_read_b64_tr_b16: 8 bytes a lane, four rows of 64 bytes at a time
-// Both are free of bank conflicts (64 banks of 4 bytes) where 16 neighbouring rows have their 16-byte pieces in 16 different
-// places of the 256-byte line, and any four rows that begin at a multiple of four have theirs in different quarters of it:
-// piece c of row x lies at c ^ swz(x).
-// ---------------------------------------------------------------------------
-template <int D> struct AttnTile {
-    static constexpr int RB = D == 96 ? 256 : 2 * D; // bytes from row to row
-    static __device__ __forceinline__ int swz(int row)
-    {
-        if constexpr (RB == 256) return (row & 3) << 2 | (row >> 2 & 3);
-        else if constexpr (RB == 128) return (row >> 1 & 1) << 2 | (row >> 2 & 3);
-        else return row >> 2 & 3;
-    }
-    static __device__ __forceinline__ int at(int row, int piece) { return row * RB + ((piece ^ swz(row)) << 4); }
-};
-
-// A tile of ROWS rows on its way from memory straight to LDS, 16 bytes a lane, a wavefront's 1 KB in a row; the swizzle is in which
-// piece a lane fetches.  Rows past `have` repeat the last one, so that a wavefront always has N transfers under way; the kernels mask
-// them.  Pieces past d are not fetched: their places keep the zeros of clear_tiles.  (Offsets stay under 2^32 bytes for strides up to 2^24.)
+// A tile of ROWS rows on its way from memory straight to LDS (pac_attn_tile.h: which lane fetches what).  Rows past `have` repeat the last one,
+// so that a wavefront always has N transfers under way; the kernels mask them.  Pieces past d are not fetched: their places keep the zeros of
+// clear_tiles, or, where D is 96 and a row's place has four pieces more, are never read.  (Offsets stay under 2^32 bytes for strides up to 2^24.)
 template <int D, int ROWS, int WAVES = 4> struct AttnDma { // WAVES: that share the tile
-    using T = AttnTile<D>;
-    static constexpr int P = T::RB / 16, RPI = 64 / P;                           // pieces of a row, rows of a transfer
-    static constexpr int TOTAL = ROWS / RPI, N = TOTAL / WAVES > 0 ? TOTAL / WAVES : 1; // (few rows: wavefronts repeat one another's transfers)
+    using F = AttnFetch<D, ROWS, WAVES>;
+    static_assert(F::steady(), "one decision for all transfers of a lane");
+    static constexpr int N = F::N;
     uint32_t stride2, off[N];
     int row, to, dd; // dd: values of a row that are fetched
     __device__ __forceinline__ void plan(int64_t stride, int d)
     {
-        const int lane = threadIdx.x & 63, first = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % WAVES * N % TOTAL;
-        row = first * RPI + lane / P;
+        const int lane = threadIdx.x & 63, first = F::first(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+        row = F::row(first, lane);
         to = first * 1024;
         stride2 = (uint32_t)(stride * 2);
         // (rows of a transfer begin at a multiple of RPI; the swizzle's period is 16 rows)
 #pragma unroll
-        for (int i = 0; i < N; ++i) off[i] = (uint32_t)(row + i * RPI) * stride2 + piece(i) * 16u;
+        for (int i = 0; i < N; ++i) off[i] = F::offset(row + i * F::RPI, piece(i), stride2);
         dd = d;
     }
-    __device__ __forceinline__ uint32_t piece(int i) const { return (uint32_t)((threadIdx.x & 63) % P ^ T::swz(row + i * RPI)); }
+    __device__ __forceinline__ int piece(int i) const { return F::piece(threadIdx.x & 63, row + i * F::RPI); }
     __device__ __forceinline__ static void one(const bf16_t *base, uint32_t off, uint32_t lds)
     {
         // one wait state between the write of M0 and the transfer that reads it; the compiler does not know of the transfer and so does
@@ -125,15 +107,15 @@ template <int D, int ROWS, int WAVES = 4> struct AttnDma { // WAVES: that share 
     __device__ __forceinline__ void issue(const bf16_t *base, uint32_t lds, int have) const
     {
         const uint32_t at = __builtin_amdgcn_readfirstlane(lds + to);
-        if (dd == D && have >= ROWS) {
+        if (F::whole(dd, have)) {
+            if (F::part_of_whole(threadIdx.x & 63, row)) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) one(base, off[i], at + i * 1024);
+                for (int i = 0; i < N; ++i) one(base, off[i], at + i * 1024);
+            }
         } else {
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const uint32_t c = piece(i);
-                if ((int)c * 8 < dd) one(base, (uint32_t)min(row + i * RPI, have - 1) * stride2 + c * 16u, at + i * 1024);
-            }
+            for (int i = 0; i < N; ++i)
+                if (F::part(piece(i), dd)) one(base, F::offset(min(row + i * F::RPI, have - 1), piece(i), stride2), at + i * 1024);
         }
     }
 };

@@ -1,0 +1,52 @@
+"""GPU parity of packed attention on each of its kernels' paths against oracle/attn_oracle.py (64 bits), with that oracle's bounds: tiles without a
+missing row at the end of their matrices."""
+import pytest
+import torch
+
+from oracle import attn_oracle as ao
+from paper_2408_10746_amd import runtime as rt
+
+pytestmark = pytest.mark.gpu
+BF = torch.bfloat16
+
+
+def make(seed, rows, heads, kv, d, spread=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    r = lambda h, s=1.0: (s * torch.randn(rows, h * d, generator=g, device="cuda")).to(BF)  # noqa: E731
+    return r(heads, spread), r(kv), r(kv), r(heads)
+
+
+def run(a, q, k, v, do, offsets):
+    o, lse = torch.empty_like(q), torch.empty(a.heads, q.shape[0], device="cuda")
+    a.forward(q, k, v, offsets, o, lse)
+    dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    a.backward(q, k, v, offsets, o, lse, do, dq, dk, dv)
+    return o, lse, dq, dk, dv
+
+
+def check(a, lens, got, q, k, v, do, scale, causal):
+    """Sequence by sequence and key head by key head: 64-bit scores of all heads at once would not fit for long ones."""
+    at, d, g = 0, a.d, a.heads // a.kv_heads
+    for n in lens:
+        rows = slice(at, at + n)
+        at += n
+        for h in range(a.kv_heads if n else 0):
+            mine, kvs = slice(h * g * d, (h + 1) * g * d), slice(h * d, (h + 1) * d)
+            by = lambda t, c: t[rows, c].double().reshape(n, -1, d).transpose(0, 1)  # noqa: E731
+            qh, kh, vh = by(q, mine), by(k, kvs), by(v, kvs)
+            o, lse, p, eps = ao.forward(qh, kh, vh, scale, causal)
+            ref, bound = ao.backward(qh, kh, vh, by(do, mine), scale, causal)
+            off = (got[1][h * g:(h + 1) * g, rows].double() - lse).abs()
+            assert float(off.amax()) <= 2 * eps + 4 * ao.F32 * float(lse.abs().amax()), ("lse", n, h)
+            for name, t, c, r, b in zip(("o", "dq", "dk", "dv"), (got[0], *got[2:]), (mine, mine, kvs, kvs), (o, *ref), (ao.forward_bound(p, vh, o, eps), *bound)):
+                off = (by(t, c) - r).abs()
+                assert torch.isfinite(off).all() and bool((off <= b).all()), (name, n, h, float((off / b).amax()))
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("heads,kv,lens", [(2, 1, [32]), (3, 3, [64]), (2, 2, [96, 128]), (4, 2, [256]), (24, 24, [128, 128]), (96, 48, [64, 64]), (48, 12, [1, 31, 256])], ids=str)
+def test_whole_tiles_of_96_values_at_the_end(heads, kv, lens, causal):
+    """The last row of the last head ends the matrix, and a whole tile ends there."""
+    q, k, v, do = make(sum(lens), sum(lens), heads, kv, 96, 1.5)
+    a = rt.Attention(heads, 96, kv_heads=kv, causal=causal)
+    check(a, lens, run(a, q, k, v, do, rt.packed_offsets(lens)), q, k, v, do, 96 ** -0.5, causal)
