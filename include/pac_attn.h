@@ -26,7 +26,8 @@
 extern "C" {
 #endif
 
-/* HOST.  heads a multiple of kv_heads, 1..4096   d values a head, 8..128, a multiple of 8   causal 0 or 1   scale positive, finite */
+/* HOST.  heads a multiple of kv_heads, 1..4096   d values a head, 8..128, a multiple of 8   causal 0 or 1   scale positive, up to 2.35e38
+ * (scale log2(e), which scores are taken times, is finite) */
 typedef struct {
     int32_t heads, kv_heads, d, causal;
     float scale;

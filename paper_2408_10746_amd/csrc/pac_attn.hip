@@ -1071,11 +1071,13 @@ __global__ __launch_bounds__(256) void k_attn_join(const AttnArgs a)
 // ---------------------------------------------------------------------------
 static inline bool at_aligned(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
+// What scores are taken times; infinite, it would make a score of 0 no number
+static float attn_c2(const pac_attn *a) { return a->scale * 1.4426950408889634f; }
 static pac_status check_attn(const pac_attn *a, int32_t batch, int64_t rows)
 {
     if (!a) return PAC_ERR_NULL;
     if (a->heads < 1 || a->heads > 4096 || a->kv_heads < 1 || a->heads % a->kv_heads || a->d < 8 || a->d > 128 || a->d % 8 ||
-        (a->causal != 0 && a->causal != 1) || !(a->scale > 0.f) || !std::isfinite(a->scale) || batch < 0)
+        (a->causal != 0 && a->causal != 1) || !(a->scale > 0.f) || !std::isfinite(attn_c2(a)) || batch < 0)
         return PAC_ERR_SHAPE;
     if (rows < 0 || rows > INT32_MAX) return PAC_ERR_RANGE;
     if ((rows / 128 + batch) * a->heads >= 1 << 23) return PAC_ERR_UNSUPPORTED;
@@ -1099,7 +1101,7 @@ static AttnArgs attn_args(const pac_attn *a, const int32_t *off, int32_t batch, 
     AttnArgs r{};
     r.off = off; r.batch = batch; r.rows = (int)rows;
     r.heads = a->heads; r.kv_heads = a->kv_heads; r.group = a->heads / a->kv_heads; r.d = a->d;
-    r.scale = a->scale; r.c2 = a->scale * 1.4426950408889634f;
+    r.scale = a->scale; r.c2 = attn_c2(a);
     r.tiles = (unsigned)(rows / 128 + batch);
     return r;
 }

@@ -459,7 +459,7 @@ class Attention:
         kv_heads = heads if kv_heads is None else kv_heads
         self._a = pb.pac_attn(_fits(heads, "heads"), _fits(kv_heads, "kv_heads"), _fits(d, "d"), int(causal), _scale(scale, d) if d > 0 else 1.0)
         if pb.pac_attn_workspace_bytes(self._a, 0, 0) < 0:
-            raise ValueError("heads: a multiple of kv_heads, 1..4096; d: a multiple of 8, 8..128; scale: positive, finite")
+            raise ValueError("heads: a multiple of kv_heads, 1..4096; d: a multiple of 8, 8..128; scale: positive, up to 2.35e38")
         self.heads, self.kv_heads, self.d = heads, kv_heads, d
 
     def _rows(self, q, offsets):

@@ -181,3 +181,12 @@ def test_the_bound_of_the_workspace_is_enough_for_the_call():
                     n = pb.pac_attn_workspace_bytes(a, batch, rows)
                     got = backward(a, far[0], batch, rows, far[1], sq, far[2], sk, far[3], sk, far[4], sq, far[5], far[6], sq, far[1], sq, far[7], sk, far[8], sk, far[9], n)
                     assert got == pb.PAC_ERR_RANGE, (heads, kv_heads, d, causal, batch, rows)
+
+
+def test_attention_scales_whose_product_with_log2_e_is_none_are_refused():
+    """Scores are taken times scale log2(e), in 32 bits: where that is infinite, a score of 0 would become none."""
+    for scale, want in ((2.36e38, False), (3.4e38, False), (2.35e38, True), (1e-45, True)):
+        a = attn(scale=scale)
+        assert (pb.pac_attn_workspace_bytes(a, 2, 10) >= 0) == want, scale
+        if not want:
+            assert forward(a) == backward(a) == pb.PAC_ERR_SHAPE, scale

@@ -33,3 +33,9 @@ def test_caches_that_are_refused(args):
     """Sizes, and memory that is not a GPU's (the last)."""
     with pytest.raises(ValueError):
         rt.Kv4Cache(*args, device="cpu")
+
+
+def test_a_scale_past_what_scores_are_taken_times_is_refused():
+    rt.Attention(4, 64, scale=2.35e38)
+    with pytest.raises(ValueError):
+        rt.Attention(4, 64, scale=2.36e38)
