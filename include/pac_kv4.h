@@ -56,7 +56,8 @@ pac_status pac_kv4_read(const pac_kv4 *c /*HOST*/, int64_t rows, const int64_t *
 int64_t pac_kv4_attend_workspace_bytes(const pac_kv4 *c /*HOST*/, int32_t heads, int32_t batch, int32_t table_len);
 
 /* One query a head and sequence over the cache.
- *   heads   a multiple of kv_heads, 1..4096, head h reads key and value head h / (heads / kv_heads)     scale   positive, finite
+ *   heads   a multiple of kv_heads, 1..4096, head h reads key and value head h / (heads / kv_heads)     scale   positive, up to 2.35e38 (scale log2(e), which
+ *           scores are taken times, is finite)
  *   table   DEVICE int32 [batch], table_stride entries from row to row, of which table_len are the sequence's pages in order; a page
  *           outside 0..pages - 1 holds no tokens (its tokens count as masked)
  *   lens    DEVICE int32 [batch], tokens of each sequence; negative as 0, past table_len pages as those

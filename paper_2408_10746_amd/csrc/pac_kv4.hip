@@ -684,7 +684,8 @@ pac_status pac_kv4_attend(const pac_kv4 *c, int32_t heads, float scale, int32_t 
     const pac_status s = check_attend(c, heads, batch, table_len);
     if (s != PAC_OK) return s;
     const int64_t cols = (int64_t)heads * c->d;
-    if (!(scale > 0.f) || !std::isfinite(scale) || q_stride < cols || o_stride < cols || table_stride < table_len) return PAC_ERR_RANGE;
+    const float c2 = scale * 1.4426950408889634f; // what scores are taken times; infinite, it would make a score of 0 no number
+    if (!(scale > 0.f) || !std::isfinite(c2) || q_stride < cols || o_stride < cols || table_stride < table_len) return PAC_ERR_RANGE;
     if (batch == 0) return PAC_OK;
     const int splits = kv4_splits(c, heads, batch, table_len);
     const int64_t need = attend_bytes(c, heads, batch, splits);
@@ -699,7 +700,7 @@ pac_status pac_kv4_attend(const pac_kv4 *c, int32_t heads, float scale, int32_t 
     Kv4Attend a{};
     a.c = kv4_of(c);
     a.heads = heads; a.group = heads / c->kv_heads; a.tiles = (a.group + 15) / 16;
-    a.c2 = scale * 1.4426950408889634f;
+    a.c2 = c2;
     a.table = table; a.lens = lens; a.table_len = table_len; a.splits = splits < 1 ? 1 : splits; a.batch = batch;
     a.coarse = kv4_coarse(batch, (int64_t)batch * c->kv_heads * a.tiles, (int64_t)table_len * c->page, splits);
     a.table_stride = table_stride;

@@ -190,3 +190,9 @@ def test_attention_scales_whose_product_with_log2_e_is_none_are_refused():
         assert (pb.pac_attn_workspace_bytes(a, 2, 10) >= 0) == want, scale
         if not want:
             assert forward(a) == backward(a) == pb.PAC_ERR_SHAPE, scale
+
+
+def test_attending_with_a_scale_whose_product_with_log2_e_is_none_is_refused():
+    L, c, far = pb.lib(), kv4(), [1 << (40 + k) for k in range(5)]
+    for scale, want in ((2.36e38, pb.PAC_ERR_RANGE), (3.4e38, pb.PAC_ERR_RANGE), (2.35e38, pb.PAC_OK), (1e-45, pb.PAC_OK)):
+        assert L.pac_kv4_attend(C.byref(c), 4, scale, 0, far[0], 5, 5, far[1], far[2], 256, far[3], 256, far[4], 1 << 30, None) == want, scale
