@@ -7,7 +7,7 @@
  *             last block of a head of d values is filled up with zeros (an infinity or NaN makes its block "no value": NaN)
  *   page      `page` tokens' keys and values of all heads; slot s is token s % page of page s / page
  *   attend    s_j = scale q . k_j over the first lens[b] tokens of sequence b, which lie in the pages of row b of a table;
- *             o = sum_j p_j v_j, p = softmax(s); no tokens: o = 0
+ *             o = sum_j p_j v_j, p = softmax(s); no tokens: o = 0 (scores that are all -infinity: NaN)
  *
  * The order inside a page is the library's own: pac_kv4_write fills pages, the other two calls read them.  Products with q in bf16 are
  * exact, scores, their largest value and sums fp32; p is rounded to bf16 where it enters the product with v, o once.

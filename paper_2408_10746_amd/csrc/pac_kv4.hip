@@ -190,7 +190,7 @@ struct Kv4Attend {
     bf16_t *o;
     int64_t o_stride;
     float *part;  // [batch][heads][splits][32 NB]: unscaled o of the splits
-    float2 *stat; // [batch][heads][splits]: largest score, sum
+    float2 *stat; // [batch][heads][splits]: largest score (-infinity: no tokens), sum
 };
 
 constexpr int kKvStep = 32;               // tokens of a wavefront's step
@@ -331,6 +331,9 @@ __device__ __forceinline__ Kv4Seq kv4_seq(const Kv4Attend &a, int j)
     return Kv4Seq{b0 + at, __builtin_amdgcn_readlane(len, at)};
 }
 
+// What parts' largest scores are taken relative to: the largest of them, or anything where none has a token (all are -infinity and weigh 0)
+__device__ __forceinline__ float kv4_finite(float most) { return most == -INFINITY ? 0.f : most; }
+
 // One (sequence, tile of 16 query heads of a key and value head, split) a workgroup.  Scores are computed turned round, tokens by heads:
 // S^T = K q^T, so that a lane has one head's scores of 8 tokens (its column of the result) and these are, in place, the operand of
 // o^T = V^T p^T, whose columns are heads again: maxima, sums and rescaling stay inside a lane or go over the four lanes of a head.
@@ -373,6 +376,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 4) void k_kv4_attend(c
 #pragma unroll
     for (int n = 0; n < 2 * NB; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
     float top = -FLT_MAX, sum = 0.f; // scores are taken relative to `top`, which stays within 2^8 of the largest so far
+    bool some = false;               // has this wavefront met a token?
 
     if (t0 < end) st.load(a, pages, hk, t0, end, lane);
     pages.look(a, table, t0 + STRIDE, end, lane);
@@ -397,8 +401,9 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 4) void k_kv4_attend(c
         }
         // tokens that are not there, past the end or in a page outside the cache
         const bool whole = t0 + kKvStep <= end && __all(now.ok[0] && now.ok[1]);
+        const int keep = end - t0 - 4 * g;
+        some = some || whole || __any((now.ok[0] && keep > 0) || (now.ok[1] && keep > 16));
         if (!whole) {
-            const int keep = end - t0 - 4 * g;
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
 #pragma unroll
@@ -451,7 +456,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 4) void k_kv4_attend(c
     sum += __shfl_xor(sum, 16, 64);
     sum += __shfl_xor(sum, 32, 64);
 
-    // the wavefronts' results, each relative to its own `top`
+    // the wavefronts' results, each relative to its own `top`; -infinity says that there were no tokens, which a sum of 0 does not: the scores of all
+    // of them may be -infinity, and o is no number then
     const int heads = min(16, a.group);
     auto joined = [&](int w, int h) { return join + (w * heads + h) * PITCH; };
     float *row = joined(wave, r);
@@ -465,7 +471,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 4) void k_kv4_attend(c
                 row[at + 1] = acc[2 * j + 1][i];
             }
         if (g == 0) {
-            row[DP] = top;
+            row[DP] = some ? top : -INFINITY;
             row[DP + 1] = sum;
         }
     }
@@ -475,14 +481,15 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 4) void k_kv4_attend(c
         float most = joined(0, h)[DP], l = 0.f, v = 0.f;
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) most = fmaxf(most, joined(w, h)[DP]);
+        const float from = kv4_finite(most);
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
-            const float by = __builtin_amdgcn_exp2f(joined(w, h)[DP] - most);
+            const float by = __builtin_amdgcn_exp2f(joined(w, h)[DP] - from);
             l += by * joined(w, h)[DP + 1];
             v += by * joined(w, h)[at];
         }
         if (len <= per) { // the whole sequence was this workgroup's
-            if (at < a.c.d) a.o[b * a.o_stride + (int64_t)(head0 + h) * a.c.d + at] = (bf16_t)(l == 0.f ? 0.f : v / l);
+            if (at < a.c.d) a.o[b * a.o_stride + (int64_t)(head0 + h) * a.c.d + at] = (bf16_t)(most == -INFINITY ? 0.f : v / l);
         } else {
             const int64_t to = ((int64_t)b * a.heads + head0 + h) * a.splits + split;
             a.part[to * DP + at] = v;
@@ -507,13 +514,13 @@ __global__ __launch_bounds__(256) void k_kv4_join(const Kv4Attend a)
     const f32x4 *part = reinterpret_cast<const f32x4 *>(a.part + ((int64_t)b * a.heads + h) * a.splits * DP);
     // weights: every wavefront finds the largest score of all splits for itself
     const int lane = tid & 63;
-    float most = -FLT_MAX;
+    float most = -INFINITY;
     for (int s = lane; s < n; s += 64) most = fmaxf(most, stat[s].x);
 #pragma unroll
     for (int x = 1; x < 64; x *= 2) most = fmaxf(most, __shfl_xor(most, x, 64));
     float l = 0.f;
     if (tid < n) {
-        by[tid] = __builtin_amdgcn_exp2f(stat[tid].x - most);
+        by[tid] = __builtin_amdgcn_exp2f(stat[tid].x - kv4_finite(most));
         l = by[tid] * stat[tid].y;
     }
 #pragma unroll
@@ -533,7 +540,7 @@ __global__ __launch_bounds__(256) void k_kv4_join(const Kv4Attend a)
     float v = 0.f;
 #pragma unroll
     for (int x = 0; x < SETS; ++x) v += sums[x][tid / 4][tid % 4];
-    a.o[b * a.o_stride + (int64_t)h * a.c.d + tid] = (bf16_t)(l == 0.f ? 0.f : v / l);
+    a.o[b * a.o_stride + (int64_t)h * a.c.d + tid] = (bf16_t)(most == -INFINITY ? 0.f : v / l);
 }
 static_assert(kKvSplits <= 256, "a thread a split");
 
