@@ -49,9 +49,10 @@ pac_status pac_attn_forward(const pac_attn *a /*HOST*/, const int32_t *offsets /
                             float *lse /*DEVICE*/, void *hip_stream);
 
 /* Bytes of workspace for the gradients of `rows` rows in `batch` sequences: two fp32 numbers a row and head, and partial sums of dk and dv where
- * few tiles of keys have many queries.  A bound that never falls as either grows, so that it serves smaller calls too; a call asks for what its own sizes
- * take.  -1 on bad arguments. */
+ * few tiles of keys have many queries.  A bound that never falls as either grows, so that it serves smaller calls too: up to hundreds of
+ * MB more than a call of just these sizes takes, which is what pac_attn_backward_bytes says.  -1 on bad arguments. */
 int64_t pac_attn_workspace_bytes(const pac_attn *a /*HOST*/, int32_t batch, int64_t rows);
+int64_t pac_attn_backward_bytes(const pac_attn *a /*HOST*/, int32_t batch, int64_t rows);
 
 /* q, k, v, offsets as in the forward pass, o and lse what it wrote; do_ [rows][heads d]; dq [rows][heads d], dk, dv
  * [rows][kv_heads d], overwritten.  workspace DEVICE, 16-byte aligned; its contents are scratch.  What is written shares no memory with

@@ -39,7 +39,7 @@ EXPORTS = [
     "pac_mx4_code_pitch", "pac_mx4_scale_pitch", "pac_mx4_quantize", "pac_mx4_dequantize", "pac_mx4_linear", "pac_mx4_linear_x4",
     "pac_mx4_linear_qx_workspace_bytes", "pac_mx4_linear_qx", "pac_mx4_linear_dx", "pac_mx4_tiles",
     "pac_block_norm_forward", "pac_block_norm_workspace_bytes", "pac_block_norm_backward",
-    "pac_attn_forward", "pac_attn_workspace_bytes", "pac_attn_backward",
+    "pac_attn_forward", "pac_attn_workspace_bytes", "pac_attn_backward_bytes", "pac_attn_backward",
     "pac_kv4_bytes", "pac_kv4_write", "pac_kv4_read", "pac_kv4_attend_workspace_bytes", "pac_kv4_attend",
 ]
 PAC_STATIC_WORKSPACE_BYTES = 64 << 20
@@ -213,8 +213,9 @@ def lib():
         L.pac_block_norm_backward.argtypes = [C.POINTER(pac_block_norm), i64] + [vp] * 13 + [i64, vp]
         L.pac_attn_forward.restype = C.c_int
         L.pac_attn_forward.argtypes = [C.POINTER(pac_attn), vp, i32, i64] + [vp, i64] * 4 + [vp, vp]
-        L.pac_attn_workspace_bytes.restype = i64
-        L.pac_attn_workspace_bytes.argtypes = [C.POINTER(pac_attn), i32, i64]
+        for f in (L.pac_attn_workspace_bytes, L.pac_attn_backward_bytes):
+            f.restype = i64
+            f.argtypes = [C.POINTER(pac_attn), i32, i64]
         L.pac_attn_backward.restype = C.c_int
         L.pac_attn_backward.argtypes = [C.POINTER(pac_attn), vp, i32, i64] + [vp, i64] * 4 + [vp] + [vp, i64] * 4 + [vp, i64, vp]
         L.pac_kv4_bytes.restype = i64
@@ -598,6 +599,10 @@ def pac_attn_forward(a: pac_attn, offsets_ptr, batch: int, rows: int, q_ptr, q_s
 
 def pac_attn_workspace_bytes(a: pac_attn, batch: int, rows: int) -> int:
     return int(lib().pac_attn_workspace_bytes(C.byref(a), batch, rows))
+
+
+def pac_attn_backward_bytes(a: pac_attn, batch: int, rows: int) -> int:
+    return int(lib().pac_attn_backward_bytes(C.byref(a), batch, rows))
 
 
 def pac_attn_backward(a: pac_attn, offsets_ptr, batch: int, rows: int, q_ptr, q_stride: int, k_ptr, k_stride: int, v_ptr, v_stride: int,

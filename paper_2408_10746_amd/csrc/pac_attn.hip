@@ -1227,6 +1227,11 @@ int64_t pac_attn_workspace_bytes(const pac_attn *a, int32_t batch, int64_t rows)
     return 2 * stat_bytes(a, rows) + pairs * 2 * a->kv_heads * a->d * 4;
 }
 
+int64_t pac_attn_backward_bytes(const pac_attn *a, int32_t batch, int64_t rows)
+{
+    return check_attn(a, batch, rows) == PAC_OK ? attn_bytes(a, batch, rows) : -1;
+}
+
 pac_status pac_attn_backward(const pac_attn *a, const int32_t *offsets, int32_t batch, int64_t rows, const void *q, int64_t q_stride,
                              const void *k, int64_t k_stride, const void *v, int64_t v_stride, const void *o, int64_t o_stride,
                              const float *lse, const void *do_, int64_t do_stride, void *dq, int64_t dq_stride, void *dk,

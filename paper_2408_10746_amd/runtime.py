@@ -491,7 +491,7 @@ class Attention:
         qc, kc, m = self.heads * self.d, self.kv_heads * self.d, self._matrix
         if lse is None:
             raise ValueError("lse: what forward wrote")
-        need = pb.pac_attn_workspace_bytes(self._a, batch, rows)
+        need = pb.pac_attn_backward_bytes(self._a, batch, rows)
         if need < 0:
             raise ValueError("rows: too many of them by heads")
         ws = torch.empty(need, dtype=torch.uint8, device=q.device)  # for this call, on this stream

@@ -196,3 +196,21 @@ def test_attending_with_a_scale_whose_product_with_log2_e_is_none_is_refused():
     L, c, far = pb.lib(), kv4(), [1 << (40 + k) for k in range(5)]
     for scale, want in ((2.36e38, pb.PAC_ERR_RANGE), (3.4e38, pb.PAC_ERR_RANGE), (2.35e38, pb.PAC_OK), (1e-45, pb.PAC_OK)):
         assert L.pac_kv4_attend(C.byref(c), 4, scale, 0, far[0], 5, 5, far[1], far[2], 256, far[3], 256, far[4], 1 << 30, None) == want, scale
+
+
+def test_the_bytes_of_a_call_are_what_the_call_asks_for():
+    """No more than the bound for all smaller calls, and just what is refused when it is less (dq in q's place: with enough, that is what is refused)."""
+    far = [(1 << 45) * (k + 1) for k in range(11)]
+    for heads, kv_heads, d in ((1, 1, 8), (12, 12, 64), (32, 8, 128), (64, 1, 64), (500, 500, 8)):
+        for causal in (0, 1):
+            a = attn(heads, kv_heads, d, causal)
+            for batch in (1, 2, 8, 64):
+                for rows in (1, 127, 128, 512, 1000, 5000, 16384, 70000):
+                    need, sq, sk = pb.pac_attn_backward_bytes(a, batch, rows), heads * d, kv_heads * d
+                    assert 0 < need <= pb.pac_attn_workspace_bytes(a, batch, rows)
+                    go = lambda n: backward(a, far[0], batch, rows, far[1], sq, far[2], sk, far[3], sk, far[4], sq, far[5], far[6], sq, far[1], sq, far[7], sk, far[8], sk, far[9], n)  # noqa: E731
+                    assert go(need - 1) == pb.PAC_ERR_WORKSPACE and go(need) == pb.PAC_ERR_RANGE, (heads, kv_heads, d, causal, batch, rows)
+    # two fp32 numbers a row and head where the queries are not dealt out, whatever smaller calls may take
+    assert pb.pac_attn_backward_bytes(attn(32, 32, 128, 1), 8, 5120) == 2 * 5120 * 32 * 4
+    assert pb.pac_attn_backward_bytes(attn(heads=3), 2, 10) == pb.pac_attn_backward_bytes(attn(), 2, -1) == pb.pac_attn_backward_bytes(attn(), -1, 10) == -1
+    assert pb.pac_attn_backward_bytes(attn(), 0, 10) == 2 * 256 and pb.pac_attn_backward_bytes(attn(), 2, 0) == 0

@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from oracle import attn_oracle as ao
+from paper_2408_10746_amd import binding as pb
 from paper_2408_10746_amd import runtime as rt
 
 pytestmark = pytest.mark.gpu
@@ -50,3 +51,18 @@ def test_whole_tiles_of_96_values_at_the_end(heads, kv, lens, causal):
     q, k, v, do = make(sum(lens), sum(lens), heads, kv, 96, 1.5)
     a = rt.Attention(heads, 96, kv_heads=kv, causal=causal)
     check(a, lens, run(a, q, k, v, do, rt.packed_offsets(lens)), q, k, v, do, 96 ** -0.5, causal)
+
+
+@pytest.mark.parametrize("heads,kv,d,rows,batch", [(32, 32, 128, 2000, 4), (12, 12, 64, 2000, 32), (32, 8, 128, 512, 1), (64, 1, 64, 500, 1)])
+def test_gradients_take_no_more_scratch_than_their_call(heads, kv, d, rows, batch):
+    """What the call itself asks for, and not room for every smaller one."""
+    q, k, v, do = make(rows, rows, heads, kv, d)
+    a, off = rt.Attention(heads, d, kv_heads=kv, causal=True), rt.packed_offsets([rows // batch] * (batch - 1) + [rows - rows // batch * (batch - 1)])
+    o, lse = torch.empty_like(q), torch.empty(heads, rows, device="cuda")
+    a.forward(q, k, v, off, o, lse)
+    dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    a.backward(q, k, v, off, o, lse, do, dq, dk, dv)
+    assert torch.cuda.max_memory_allocated() - before <= pb.pac_attn_backward_bytes(a._a, batch, rows) + 512  # (the allocator's granularity)
