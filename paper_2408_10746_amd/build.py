@@ -42,32 +42,54 @@ def _sources():
     return [s for s in SOURCES if os.path.exists(os.path.join(CSRC, s))]
 
 
+def _object(src: str) -> str:
+    return os.path.join(OBJ_DIR, os.path.splitext(src)[0] + ".o")
+
+
+def _command(src: str):
+    return [hipcc()] + HIPCC_FLAGS + SOURCE_FLAGS.get(src, [])
+
+
+def _made_alike(src: str) -> bool:
+    """Was the source's object made by the command that would make it now?"""
+    try:
+        with open(_object(src) + ".command") as f:
+            return f.read() == "\n".join(_command(src))
+    except FileNotFoundError:
+        return False
+
+
 def is_stale() -> bool:
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not all(os.path.exists(_object(s)) and _made_alike(s) for s in _sources()):
         return True
     t = os.path.getmtime(LIB)
-    return any(os.path.getmtime(os.path.join(CSRC, f)) > t for f in _sources() + HEADERS)
+    return any(os.path.getmtime(f) > t for f in [os.path.join(CSRC, f) for f in _sources() + HEADERS] + [_object(s) for s in _sources()])
 
 
 def _compile_one(src: str, force: bool) -> str:
-    obj = os.path.join(OBJ_DIR, os.path.splitext(src)[0] + ".o")
+    obj = _object(src)
     path = os.path.join(CSRC, src)
-    if not force and os.path.exists(obj):
+    if not force and os.path.exists(obj) and _made_alike(src):
         t = os.path.getmtime(obj)
         if all(os.path.getmtime(os.path.join(CSRC, f)) <= t for f in [src] + HEADERS):
             return obj
     tmp = obj + ".tmp%d" % os.getpid()
-    res = subprocess.run([hipcc()] + HIPCC_FLAGS + SOURCE_FLAGS.get(src, []) + ["-c", "-o", tmp, path],
+    res = subprocess.run(_command(src) + ["-c", "-o", tmp, path],
                          stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     if res.returncode != 0:
         raise RuntimeError("hipcc failed on %s:\n%s" % (src, res.stdout))
+    with open(tmp + ".command", "w") as f:
+        f.write("\n".join(_command(src)))
+    if os.path.exists(obj + ".command"):
+        os.remove(obj + ".command")  # at no time does it speak of another object
     os.replace(tmp, obj)
+    os.replace(tmp + ".command", obj + ".command")
     return obj
 
 
 def build_lib(force: bool = True) -> str:
     """Compile every HIP source (one hipcc process per file, side by side) and link libpac.so.
-    force=False recompiles only the objects older than their source or a header."""
+    force=False recompiles only the objects older than their source or a header, or made with other flags."""
     if not force and not is_stale():
         return LIB
     os.makedirs(OBJ_DIR, exist_ok=True)
