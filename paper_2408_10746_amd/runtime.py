@@ -209,8 +209,8 @@ _KIND = {torch.bfloat16: pb.PAC_BF16, torch.float32: pb.PAC_F32}
 
 def _fits(n: int, what: str) -> int:
     """n, which the library takes in 32 bits (ctypes drops what lies above)."""
-    if n >= 1 << 31:
-        raise ValueError(f"{what}: {n} is past 2^31 - 1")
+    if not -1 << 31 <= n < 1 << 31:
+        raise ValueError(f"{what}: {n} is past 2^31 - 1" if n > 0 else f"{what}: {n} is below -2^31")
     return n
 
 
@@ -505,7 +505,7 @@ class Kv4Cache:
     sequence has is the caller's: a row of a table."""
 
     def __init__(self, pages: int, page: int, kv_heads: int, d: int, device="cuda:0"):
-        self._c = pb.pac_kv4(None, pages, _fits(page, "page"), _fits(kv_heads, "kv_heads"), _fits(d, "d"))
+        self._c = pb.pac_kv4(None, _fits(pages, "pages"), _fits(page, "page"), _fits(kv_heads, "kv_heads"), _fits(d, "d"))
         need = pb.pac_kv4_bytes(self._c)
         if need < 0:
             raise ValueError("pages: 0..2^31 - 1; page: a power of two, 8..65536; kv_heads: 1..4096; d: a multiple of 8, 8..128")

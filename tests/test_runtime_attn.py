@@ -39,3 +39,16 @@ def test_a_scale_past_what_scores_are_taken_times_is_refused():
     rt.Attention(4, 64, scale=2.35e38)
     with pytest.raises(ValueError):
         rt.Attention(4, 64, scale=2.36e38)
+
+
+@pytest.mark.parametrize("kw", [dict(heads=4 - (1 << 32)), dict(kv_heads=2 - (1 << 32)), dict(d=64 - (1 << 32))])
+def test_sizes_that_32_bits_would_turn_into_others_are_refused(kw):
+    with pytest.raises(ValueError):
+        rt.Attention(**dict(dict(heads=4, d=64, kv_heads=2), **kw))
+
+
+@pytest.mark.parametrize("name,args", [("pages", ((1 << 64) + 4, 16, 2, 64)), ("pages", (4 - (1 << 64), 16, 2, 64)), ("page", (4, 16 - (1 << 32), 2, 64)),
+                                       ("kv_heads", (4, 16, 2 - (1 << 32), 64)), ("d", (4, 16, 2, 64 - (1 << 32)))])
+def test_cache_sizes_that_fewer_bits_would_turn_into_others_are_refused(name, args):
+    with pytest.raises(ValueError, match=f"^{name}: {args[('pages', 'page', 'kv_heads', 'd').index(name)]} is "):
+        rt.Kv4Cache(*args, device="cpu")
