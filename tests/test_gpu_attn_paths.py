@@ -1,8 +1,11 @@
 """GPU parity of packed attention on each of its kernels' paths against oracle/attn_oracle.py (64 bits), with that oracle's bounds: tiles without a
-missing row at the end of their matrices."""
+missing row at the end of their matrices, long sequences and values that are none on 128 and on 32 rows a workgroup, and what a call allocates."""
+import math
+
 import pytest
 import torch
 
+from attn_kernels import few
 from oracle import attn_oracle as ao
 from paper_2408_10746_amd import binding as pb
 from paper_2408_10746_amd import runtime as rt
@@ -66,3 +69,53 @@ def test_gradients_take_no_more_scratch_than_their_call(heads, kv, d, rows, batc
     before = torch.cuda.memory_allocated()
     a.backward(q, k, v, off, o, lse, do, dq, dk, dv)
     assert torch.cuda.max_memory_allocated() - before <= pb.pac_attn_backward_bytes(a._a, batch, rows) + 512  # (the allocator's granularity)
+
+
+@pytest.mark.parametrize("heads,kv,d,n,causal", [(16, 4, 128, 2500, True), (16, 16, 64, 3001, False), (24, 8, 96, 2600, True), (20, 20, 32, 2111, True), (8, 2, 104, 2333, False)])
+def test_long_sequences_of_128_rows_a_workgroup(heads, kv, d, n, causal):
+    assert not few(heads, d, 1, n, causal)
+    q, k, v, do = make(n, n, heads, kv, d, 1.5)
+    a = rt.Attention(heads, d, kv_heads=kv, causal=causal)
+    check(a, [n], run(a, q, k, v, do, rt.packed_offsets([n])), q, k, v, do, d ** -0.5, causal)
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("which", ["q", "k", "v", "do"])
+@pytest.mark.parametrize("heads,d,n", [(192, 32, 200), (192, 64, 200), (96, 96, 150), (96, 72, 161), (96, 128, 200), (2, 32, 200), (3, 64, 300), (2, 96, 200), (2, 128, 150)])
+def test_values_that_are_none_beside_the_mask(heads, d, n, which, bad):
+    """A value that is infinite or no number, in the last head alone, at places all over the tiles of 32 and 128 rows: who does not see it stays within
+    the oracle's bound of the exact values without it, rows of the same tile among them, and the other heads keep their bits."""
+    assert few(heads, d, 1, n, True) == (heads < 10)
+    clean = dict(zip(("q", "k", "v", "do"), make(d + n, n, heads, heads, d)))
+    a, off = rt.Attention(heads, d, causal=True), rt.packed_offsets([n])
+    ref = run(a, *clean.values(), off)
+    last, row, col = slice((heads - 1) * d, heads * d), torch.arange(n, device="cuda"), 5
+    x = {name: t[:, last].double()[None] for name, t in clean.items()}
+    o, lse, p, eps = ao.forward(x["q"], x["k"], x["v"], d ** -0.5, True)
+    grads, bounds = ao.backward(*x.values(), d ** -0.5, True)
+    exact = (o[0], lse[0][:, None], *(t[0] for t in grads))
+    bounds = (ao.forward_bound(p, x["v"], o, eps)[0], torch.full((n, 1), 2 * eps + 4 * ao.F32 * float(lse.abs().amax()), device="cuda"), *(t[0] for t in bounds))
+    for at in (0, 33, 127, n - 1):
+        t = {name: y.clone() for name, y in clean.items()}
+        t[which][at, last.start + col] = bad
+        got = run(a, *t.values(), off)
+        for g, r, e, b, out in zip(got, ref, exact, bounds, ("o", "lse", "dq", "dk", "dv")):
+            mine, others = (g[-1:].t(), (g[:-1], r[:-1])) if out == "lse" else (g[:, last], (g[:, :last.start], r[:, :last.start]))
+            assert torch.equal(*others), (at, out, "other heads")
+            if which == "do" and out in ("o", "lse") or which == "v" and out == "lse":
+                same = torch.ones_like(row, dtype=torch.bool)
+            elif out in ("dk", "dv"):  # keys see the rows from their own on
+                same = row > at if which in ("q", "do") else torch.zeros_like(row, dtype=torch.bool)
+            else:
+                same = row != at if which in ("q", "do") else row < at
+            away = (mine.double() - e).abs()
+            assert bool((away <= b)[same].all()), (at, out)
+            if which == "v" and out == "o":  # one column of it
+                rest = torch.arange(d, device="cuda") != col
+                assert bool((away <= b)[:, rest].all()), (at, "the other columns")
+                assert (mine[at:, col].isnan() if math.isnan(bad) else mine[at:, col] == bad).all()
+            if which == "do" and out == "dv":
+                rest = torch.arange(d, device="cuda") != col
+                assert bool((away <= b)[:, rest].all()) and not mine[:at + 1, col].isfinite().any(), at
+            if (which, out) in (("q", "o"), ("q", "lse"), ("q", "dq"), ("do", "dq")):
+                assert not mine[at].isfinite().all(), (at, out)
