@@ -119,3 +119,15 @@ def test_values_that_are_none_beside_the_mask(heads, d, n, which, bad):
                 assert bool((away <= b)[:, rest].all()) and not mine[:at + 1, col].isfinite().any(), at
             if (which, out) in (("q", "o"), ("q", "lse"), ("q", "dq"), ("do", "dq")):
                 assert not mine[at].isfinite().all(), (at, out)
+
+
+def test_results_a_row_beside_an_operand_are_refused():
+    """q in rows 0..9 of one buffer, o in rows 1..10."""
+    q, k, v, _ = make(0, 11, 4, 2, 64)
+    a, off, lse = rt.Attention(4, 64, kv_heads=2), rt.packed_offsets([4, 6]), torch.empty(4, 10, device="cuda")
+    keep = q.clone()
+    for o, x in ((q[1:], q[:10]), (q[:10], q[1:])):
+        with pytest.raises(pb.PacError) as e:
+            a.forward(x, k[:10], v[:10], off, o, lse)
+        assert e.value.status == pb.PAC_ERR_RANGE
+    assert torch.equal(q, keep)
