@@ -68,6 +68,36 @@ def backward(q, k, v, do, scale: float, causal: bool):
     return (dq, dk, dv), bounds
 
 
+def exact_delta_bounds(q, k, v, do, given, scale: float, causal: bool):
+    """Bounds of the errors of dq and dk where delta is exact, although o is at hand as `given`, in bf16 (in 64 bits here).  With D_i = do_i . (given_i - o_i),
+    the kernels' z_ij = p_ij (do_i . v_j - delta_i - D_i) and r_i = sum_j z_ij = -D_i,
+
+        dq_i = scale (sum_j z_ij k_j - r_i sum_j p_ij k_j)     and delta_i = do_i . given_i + r_i for dk
+
+    are free of D but for the roundings that it passes through: z and p to bf16, p's relative error e in 32 bits (so that the p of a row sum to 1 within e),
+    that of do . v, and sums in 32 bits."""
+    g, n, d = q.shape[0] // k.shape[0], q.shape[1], q.shape[2]
+    o, _, p, eps = forward(q, k, v, scale, causal)
+    kg, vg = k.repeat_interleave(g, 0), v.repeat_interleave(g, 0)
+    m, e = mask(n, causal, q.device), 3 * eps
+    dp = do @ vg.transpose(1, 2)
+    ds = p * (dp - (do * o).sum(2, keepdim=True))
+    far = (do * (given - o)).sum(2, keepdim=True).abs()
+    e_dp = (2 * (d + 8) * F32 * (do.abs() @ vg.abs().transpose(1, 2))).masked_fill(~m, 0.0)
+    e_far = 2 * (d + 8) * F32 * (do.abs() * given.abs()).sum(2, keepdim=True)  # of do . given
+    z = ds.abs() + p * far + p * (e_dp + e_far)
+    # r + D: p's sum, the errors of do . v, the sum itself; do . given's own error leaves as D does
+    e_r = e * (far + e_far + ds.abs().sum(2, keepdim=True)) + (p * e_dp).sum(2, keepdim=True) + 2 * F32 * (n + 64) * z.sum(2, keepdim=True)
+    y = p @ kg.abs()
+    e_z = ((BF16 + e) * z + p * e_dp) * (1 + BF16)
+    sums = 2 * F32 * (n * g + 64)
+    ref_q, ref_k = scale * (ds @ kg), scale * (ds.transpose(1, 2) @ q).reshape(-1, g, n, d).sum(1)
+    b_q = scale * ((e_z + sums * z) @ kg.abs() + (e_r + (far + e_far) * (BF16 + e + sums)) * y * (1 + BF16)) + BF16 * ref_q.abs()
+    e_ds = ((BF16 + e) * ds.abs() + p * (1 + e) * (e_dp + e_r + 4 * F32 * (do.abs() * given.abs()).sum(2, keepdim=True))) * (1 + BF16)
+    b_k = scale * ((e_ds + sums * ds.abs()).transpose(1, 2) @ q.abs()).reshape(-1, g, n, d).sum(1) + BF16 * ref_k.abs()
+    return (ref_q, 1.01 * b_q + 1e-30), (ref_k, 1.01 * b_k + 1e-30)
+
+
 def decode(q, k, v, scale: float):
     """o of one query a head, q [heads][d], over k, v [kv_heads][n][d], and the bound of its error."""
     g = q.shape[0] // k.shape[0]

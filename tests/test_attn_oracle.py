@@ -82,3 +82,29 @@ def test_decode_is_the_last_row_of_a_causal_prompt():
     got, bound = ao.decode(q[:, -1], k, v, 0.4)
     assert torch.allclose(got, o[:, -1], rtol=1e-12, atol=1e-12) and (bound > 0).all()
     assert (ao.decode(q[:, -1], k[:, :0], v[:, :0], 0.4)[0] == 0).all()
+
+
+@pytest.mark.parametrize("heads,kv,n,d,causal", [(2, 2, 40, 32, True), (4, 2, 60, 64, False), (4, 1, 33, 128, True)])
+def test_bounds_with_an_exact_delta_tell_it_from_that_of_the_rounded_o(heads, kv, n, d, causal):
+    """Values and keys that have much in common: what o loses when it is rounded is as large as what tells the values apart.  The kernels' arithmetic with its
+    roundings, in 64 bits else, stays inside the bounds; the same with the rounded o's delta does not."""
+    bf = lambda t: t.to(torch.bfloat16).double()  # noqa: E731
+    q, k, v, do = make(n, heads, kv, n, d)
+    q, k, v, do = bf(q), bf(k + 4), bf(v + 32), bf(do)
+    scale, g = d ** -0.5 / 4, heads // kv
+    o, _, p, _ = ao.forward(q, k, v, scale, causal)
+    kg, vg = k.repeat_interleave(g, 0), v.repeat_interleave(g, 0)
+    given = bf(bf(p) @ vg)
+    (dq, b_q), (dk, b_k) = ao.exact_delta_bounds(q, k, v, do, given, scale, causal)
+    want = ao.backward(q, k, v, do, scale, causal)[0]
+    assert torch.allclose(dq, want[0], rtol=1e-9, atol=1e-11) and torch.allclose(dk, want[1], rtol=1e-9, atol=1e-11)
+    delta, dp = (do * given).sum(2, keepdim=True), do @ vg.transpose(1, 2)
+    z = p * (dp - delta)
+    worst = {}
+    for exact in (True, False):
+        r = z.sum(2, keepdim=True) * exact
+        mine_q = bf(scale * (bf(z) @ kg - r * (bf(p) @ kg)))
+        mine_k = bf(scale * (bf(p * (dp - delta - r)).transpose(1, 2) @ q).reshape(-1, g, n, d).sum(1))
+        worst[exact] = float(((mine_q - dq).abs() / b_q).amax()), float(((mine_k - dk).abs() / b_k).amax())
+    assert 0.05 < worst[True][0] <= 1 and 0.02 < worst[True][1] <= 1, worst
+    assert worst[False][0] > 4 and worst[False][1] > 2, worst

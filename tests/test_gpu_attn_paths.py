@@ -131,3 +131,23 @@ def test_results_a_row_beside_an_operand_are_refused():
             a.forward(x, k[:10], v[:10], off, o, lse)
         assert e.value.status == pb.PAC_ERR_RANGE
     assert torch.equal(q, keep)
+
+
+@pytest.mark.parametrize("heads,kv,d,n,causal", [(2, 2, 32, 200, True), (2, 1, 64, 300, False), (2, 2, 96, 257, True), (4, 2, 128, 200, True), (192, 96, 64, 150, True),
+                                                 (96, 96, 128, 140, True), (96, 48, 96, 130, False), (96, 96, 32, 200, False), (64, 1, 64, 300, True)])
+def test_delta_is_exact_where_o_is_rounded(heads, kv, d, n, causal):
+    """Values and keys that have much in common, so that the rounded o's delta would miss dq and dk by several times the bounds (the oracle's own test
+    shows by how much)."""
+    g = heads // kv
+    q, k, v, do = make(n + d, n, heads, kv, d)
+    k, v = (k.float() + 4).to(BF), (v.float() + 32).to(BF)
+    scale = d ** -0.5 / 4
+    a = rt.Attention(heads, d, kv_heads=kv, causal=causal, scale=scale)
+    got = run(a, q, k, v, do, rt.packed_offsets([n]))
+    for h in range(0, kv, max(1, kv // 5)):
+        mine, kvs = slice(h * g * d, (h + 1) * g * d), slice(h * d, (h + 1) * d)
+        by = lambda t, c: t[:, c].double().reshape(n, -1, d).transpose(0, 1)  # noqa: E731
+        for name, t, c, (r, b) in zip(("dq", "dk"), (got[2], got[3]), (mine, kvs),
+                                      ao.exact_delta_bounds(by(q, mine), by(k, kvs), by(v, kvs), by(do, mine), by(got[0], mine), scale, causal)):
+            off = (by(t, c) - r).abs()
+            assert bool((off <= b).all()), (name, h, float((off / b).amax()))
