@@ -52,8 +52,9 @@ pac_status pac_kv4_read(const pac_kv4 *c /*HOST*/, int64_t rows, const int64_t *
                         void *v /*DEVICE*/, int64_t v_stride, int32_t dtype, void *hip_stream);
 
 /* Bytes of workspace for attend: partial results of long sequences.  A bound that never falls as the batch or the table grows, so that it serves smaller calls
- * too; a call asks for what its own sizes take, which may be nothing (NULL then).  -1 on bad arguments. */
+ * too; a call of just these sizes takes pac_kv4_attend_bytes, which may be nothing (NULL then).  -1 on bad arguments. */
 int64_t pac_kv4_attend_workspace_bytes(const pac_kv4 *c /*HOST*/, int32_t heads, int32_t batch, int32_t table_len);
+int64_t pac_kv4_attend_bytes(const pac_kv4 *c /*HOST*/, int32_t heads, int32_t batch, int32_t table_len);
 
 /* One query a head and sequence over the cache.
  *   heads   a multiple of kv_heads, 1..4096, head h reads key and value head h / (heads / kv_heads)     scale   positive, up to 2.35e38 (scale log2(e), which

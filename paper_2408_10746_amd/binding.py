@@ -40,7 +40,8 @@ EXPORTS = [
     "pac_mx4_linear_qx_workspace_bytes", "pac_mx4_linear_qx", "pac_mx4_linear_dx", "pac_mx4_tiles",
     "pac_block_norm_forward", "pac_block_norm_workspace_bytes", "pac_block_norm_backward",
     "pac_attn_forward", "pac_attn_workspace_bytes", "pac_attn_backward_bytes", "pac_attn_backward",
-    "pac_kv4_bytes", "pac_kv4_write", "pac_kv4_read", "pac_kv4_attend_workspace_bytes", "pac_kv4_attend",
+    "pac_kv4_bytes", "pac_kv4_write", "pac_kv4_read", "pac_kv4_attend_workspace_bytes", "pac_kv4_attend_bytes",
+    "pac_kv4_attend",
 ]
 PAC_STATIC_WORKSPACE_BYTES = 64 << 20
 PAC_MX4_ACT_NONE, PAC_MX4_ACT_GELU = 0, 1
@@ -223,8 +224,9 @@ def lib():
         for f in (L.pac_kv4_write, L.pac_kv4_read):
             f.restype = C.c_int
             f.argtypes = [C.POINTER(pac_kv4), i64, vp, vp, i64, vp, i64, i32, vp]
-        L.pac_kv4_attend_workspace_bytes.restype = i64
-        L.pac_kv4_attend_workspace_bytes.argtypes = [C.POINTER(pac_kv4), i32, i32, i32]
+        for f in (L.pac_kv4_attend_workspace_bytes, L.pac_kv4_attend_bytes):
+            f.restype = i64
+            f.argtypes = [C.POINTER(pac_kv4), i32, i32, i32]
         L.pac_kv4_attend.restype = C.c_int
         L.pac_kv4_attend.argtypes = [C.POINTER(pac_kv4), i32, C.c_float, i32, vp, i32, i64, vp, vp, i64, vp, i64, vp, i64, vp]
         L.pac_profile_begin.restype = C.c_int
@@ -627,6 +629,10 @@ def pac_kv4_read(c: pac_kv4, rows: int, slots_ptr, k_ptr, k_stride: int, v_ptr, 
 
 def pac_kv4_attend_workspace_bytes(c: pac_kv4, heads: int, batch: int, table_len: int) -> int:
     return int(lib().pac_kv4_attend_workspace_bytes(C.byref(c), heads, batch, table_len))
+
+
+def pac_kv4_attend_bytes(c: pac_kv4, heads: int, batch: int, table_len: int) -> int:
+    return int(lib().pac_kv4_attend_bytes(C.byref(c), heads, batch, table_len))
 
 
 def pac_kv4_attend(c: pac_kv4, heads: int, scale: float, batch: int, table_ptr, table_len: int, table_stride: int, lens_ptr, q_ptr,

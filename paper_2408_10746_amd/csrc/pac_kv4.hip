@@ -684,6 +684,12 @@ int64_t pac_kv4_attend_workspace_bytes(const pac_kv4 *c, int32_t heads, int32_t 
     return pairs * heads * (2 + 32 * kv4_blocks(c)) * 4;
 }
 
+int64_t pac_kv4_attend_bytes(const pac_kv4 *c, int32_t heads, int32_t batch, int32_t table_len)
+{
+    if (check_attend(c, heads, batch, table_len) != PAC_OK) return -1;
+    return batch == 0 ? 0 : attend_bytes(c, heads, batch, kv4_splits(c, heads, batch, table_len));
+}
+
 pac_status pac_kv4_attend(const pac_kv4 *c, int32_t heads, float scale, int32_t batch, const int32_t *table, int32_t table_len,
                           int64_t table_stride, const int32_t *lens, const void *q, int64_t q_stride, void *o, int64_t o_stride,
                           void *workspace, int64_t workspace_bytes, void *hip_stream)

@@ -554,7 +554,7 @@ class Kv4Cache:
         c, st = self._at(), table.stride(0) if batch > 1 else pages
         sizes, need = self._room
         if sizes != (heads, batch, pages):
-            need = max(_lib().pac_kv4_attend_workspace_bytes(c, heads, batch, pages), 0)
+            need = max(_lib().pac_kv4_attend_bytes(c, heads, batch, pages), 0)
             self._room = (heads, batch, pages), need
         ws = torch.empty(need, dtype=torch.uint8, device=q.device)  # for this call, on this stream
         _call(gpu, "pac_kv4_attend", c, heads, _scale(scale, d), batch, table.data_ptr(), pages, st, lens.data_ptr(), q.data_ptr(), sq, o.data_ptr(), so,

@@ -214,3 +214,20 @@ def test_the_bytes_of_a_call_are_what_the_call_asks_for():
     assert pb.pac_attn_backward_bytes(attn(32, 32, 128, 1), 8, 5120) == 2 * 5120 * 32 * 4
     assert pb.pac_attn_backward_bytes(attn(heads=3), 2, 10) == pb.pac_attn_backward_bytes(attn(), 2, -1) == pb.pac_attn_backward_bytes(attn(), -1, 10) == -1
     assert pb.pac_attn_backward_bytes(attn(), 0, 10) == 2 * 256 and pb.pac_attn_backward_bytes(attn(), 2, 0) == 0
+
+
+def test_the_bytes_of_an_attend_are_what_it_asks_for():
+    """No more than the bound for all smaller calls, and just what is refused when it is less; nothing where a sequence and head has one workgroup."""
+    L, far = pb.lib(), [1 << (40 + k) for k in range(6)]
+    for heads, kv_heads, d in ((1, 1, 8), (32, 8, 128), (32, 32, 64), (48, 3, 96), (64, 1, 128)):
+        for page, tables in ((16, (0, 1, 50, 700, 5000)), (1024, (1, 3, 64))):
+            c = kv4(1 << 50, 1 << 20, page, kv_heads, d)
+            for batch in (1, 2, 7, 64, 500, 4096):
+                for tl in tables:
+                    need = pb.pac_kv4_attend_bytes(c, heads, batch, tl)
+                    assert 0 <= need <= pb.pac_kv4_attend_workspace_bytes(c, heads, batch, tl)
+                    # (o in q's place: with enough, that is what is refused)
+                    go = lambda n: L.pac_kv4_attend(C.byref(c), heads, 0.1, batch, far[0], tl, tl, far[1], far[2], heads * d, far[2], heads * d, far[3], n, None)  # noqa: E731
+                    assert go(need) == pb.PAC_ERR_RANGE and (need == 0 or go(need - 1) == pb.PAC_ERR_WORKSPACE), (heads, kv_heads, d, page, batch, tl)
+    assert pb.pac_kv4_attend_bytes(kv4(kv_heads=8, d=128), 64, 4096, 100) == 0 < pb.pac_kv4_attend_bytes(kv4(kv_heads=8, d=128), 64, 4, 1000)
+    assert pb.pac_kv4_attend_bytes(kv4(), 3, 1, 1) == pb.pac_kv4_attend_bytes(kv4(), 2, -1, 1) == pb.pac_kv4_attend_bytes(kv4(d=4), 2, 1, 1) == -1

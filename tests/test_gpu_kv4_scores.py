@@ -1,11 +1,12 @@
 """GPU: attention over the 4-bit cache where scores are infinite or no number: the softmax over such scores is none, and is not taken for one over
-no tokens."""
+no tokens; and what a call allocates."""
 import math
 
 import pytest
 import torch
 
 from oracle import attn_oracle as ao
+from paper_2408_10746_amd import binding as pb
 from paper_2408_10746_amd import runtime as rt
 
 pytestmark = pytest.mark.gpu
@@ -47,3 +48,18 @@ def test_scores_that_are_all_minus_infinity_are_tokens_all_the_same(kv, batch, n
         off = (o[b].double().reshape(heads, d) - ref).abs()
         first = int(b < 3)
         assert bool((off[first:] <= bound[first:]).all()), b
+
+
+@pytest.mark.parametrize("batch,pages", [(64, 64), (4096, 2), (2, 1000), (1, 10)])
+def test_attending_takes_no_more_scratch_than_its_call(batch, pages):
+    """What the call itself asks for, and not room for every smaller one."""
+    heads, kv, d = 32, 8, 128
+    c = rt.Kv4Cache(4, 16, kv, d)
+    q, o = torch.zeros(batch, heads * d, device="cuda", dtype=BF), torch.empty(batch, heads * d, device="cuda", dtype=BF)
+    table, lens = torch.zeros(batch, pages, dtype=torch.int32, device="cuda"), torch.full((batch,), 5, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    c.attend(q, table, lens, o)
+    assert torch.cuda.max_memory_allocated() - before <= pb.pac_kv4_attend_bytes(c._at(), heads, batch, pages) + 512  # (the allocator's granularity)
+    assert not o.any()
