@@ -20,7 +20,6 @@ struct AttnArgs {
     bf16_t *dq, *dk, *dv;
     int64_t dqs, dks, dvs;
     float *nlse2, *delta; // [heads][rows] each: -lse log2(e), do . o
-    unsigned tiles; // tiles of a head, of all sequences together
     int splits;     // of the queries that a tile of keys goes through, in dk and dv
     float *part;    // [splits][rows][2][kv_heads d]: dk / scale and dv of the splits, where there are several
 };
@@ -1102,9 +1101,10 @@ static AttnArgs attn_args(const pac_attn *a, const int32_t *off, int32_t batch, 
     r.off = off; r.batch = batch; r.rows = (int)rows;
     r.heads = a->heads; r.kv_heads = a->kv_heads; r.group = a->heads / a->kv_heads; r.d = a->d;
     r.scale = a->scale; r.c2 = attn_c2(a);
-    r.tiles = (unsigned)(rows / 128 + batch);
     return r;
 }
+// Numbers of a head's tiles of `of` rows, all sequences together (attn_seq)
+static unsigned attn_numbers(int32_t batch, int64_t rows, int of) { return (unsigned)(rows / of + batch); }
 static int64_t stat_bytes(const pac_attn *a, int64_t rows) { return (rows * a->heads * 4 + 255) / 256 * 256; }
 
 // Whether a call's rows are few: forward and dq then take 32 rows a workgroup and deal the keys to its wavefronts.  Up to 64 values a head two such
@@ -1114,7 +1114,8 @@ static int64_t stat_bytes(const pac_attn *a, int64_t rows) { return (rows * a->h
 //           64 values             2000 of 12 (192) 27.4 / 19.7, 8000 of 4 (252) 92.5 / 71.9, but 1000 of 40 (320) 18.5 / 23.0, 4000 of 12 (384) 54.2 / 61.6
 //   not causal, 128 values        1500 of 5 (60) 31.6 / 20.6, but 1600 of 6 (78) 32.1 / 37.4; all tiles take as long there
 //           64 values             4000 of 4 (128) 48.1 / 33.9, 1000 of 16 (128) 17.1 / 12.8, but 2000 of 16 (256) 30.6 / 38.7
-// and there and back as these or better.  Below some 100 tokens there is nothing to deal: 19 tokens 8.2 / 8.7.
+// and there and back as these or better.  The rule counts workgroups and does not know how long their chains of keys are, which is what decides near its bounds: at 160
+// it takes the faster form for 4000 tokens of 5 heads and the slower one for 1000 of 20.  Below some 100 tokens there is nothing to deal: 19 tokens 8.2 / 8.7.
 static bool attn_few(const pac_attn *a, int32_t batch, int64_t rows)
 {
     const int64_t most = a->d > 64 ? (a->causal ? 160 : 72) : (a->causal ? 256 : 128);
@@ -1135,7 +1136,8 @@ template <int D> static int few_lds(bool back)
 
 // Workgroups that share a tile of keys in dk and dv, i.e. parts that its queries are dealt into: by estimated time.  A subtile of 32 x 32 takes
 // 1.8 us at 128 values a head, 1.26 at 64; a launch takes as long as its longest workgroup (the first keys of a sequence of average length), or as all
-// of them together at 384 a time, and a tenth of the other; more than 512 workgroups slow each other by 13 %; sums that go through memory cost
+// of them together at 384 a time, and a tenth of the other (lengths are on the device: a batch of one long and many short or empty sequences is taken for
+// one of average ones, and its long one gets fewer parts than alone); more than 512 workgroups slow each other by 13 %; sums that go through memory cost
 // 2 us and their bytes, written and read, at 6.7 TB/s.  The estimate's best among 1, 2, 3, 4, 6, 8, 12, 16 is 0.9 % slower on the average than the best measured
 // over 27 calls; there and back, us, 1 / 2 / 4 / 8 / 16 parts (the estimate's choice): 4001 + 6143 tokens of 32/8 heads of 128 2179 / 2044 / 2063 / 2185 /
 // 2495 (2), 2048 of 32/8 416 / 293 / 245 / 253 / 313 (6: 242), 4 x 300..600 of 32/8 178 / 134 / 119 / 137 / 179 (4), 500 of 64 heads of 64 on one key head
@@ -1202,12 +1204,11 @@ pac_status pac_attn_forward(const pac_attn *a, const int32_t *offsets, int32_t b
     by_width(a->d, [&](auto n) {
         constexpr int D = decltype(n)::value;
         if (attn_few(a, batch, rows)) {
-            r.tiles = (unsigned)(rows / 32 + batch);
-            ok = a->causal ? attn_launch(k_attn_fwd_few<D, true>, r.tiles * r.heads, few_lds<D>(false), st, r)
-                           : attn_launch(k_attn_fwd_few<D, false>, r.tiles * r.heads, few_lds<D>(false), st, r);
+            const unsigned grid = attn_numbers(batch, rows, 32) * r.heads;
+            ok = a->causal ? attn_launch(k_attn_fwd_few<D, true>, grid, few_lds<D>(false), st, r) : attn_launch(k_attn_fwd_few<D, false>, grid, few_lds<D>(false), st, r);
             return;
         }
-        const dim3 grid(r.tiles * r.heads);
+        const dim3 grid(attn_numbers(batch, rows, 128) * r.heads);
         if (a->causal) hipLaunchKernelGGL((k_attn_fwd<D, true>), grid, dim3(256), 0, st, r);
         else hipLaunchKernelGGL((k_attn_fwd<D, false>), grid, dim3(256), 0, st, r);
     });
@@ -1271,24 +1272,23 @@ pac_status pac_attn_backward(const pac_attn *a, const int32_t *offsets, int32_t 
     r.delta = reinterpret_cast<float *>(static_cast<char *>(workspace) + stat_bytes(a, rows));
     r.part = reinterpret_cast<float *>(static_cast<char *>(workspace) + 2 * stat_bytes(a, rows));
     r.splits = attn_splits(a, batch, rows);
+    const unsigned tiles = attn_numbers(batch, rows, 128);
     (void)hipGetLastError();
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     bool ok = true;
     by_width(a->d, [&](auto n) {
         constexpr int D = decltype(n)::value;
         if (attn_few(a, batch, rows)) {
-            AttnArgs f = r;
-            f.tiles = (unsigned)(rows / 32 + batch);
-            ok = a->causal ? attn_launch(k_attn_dq_few<D, true>, f.tiles * f.heads, few_lds<D>(true), st, f)
-                           : attn_launch(k_attn_dq_few<D, false>, f.tiles * f.heads, few_lds<D>(true), st, f);
+            const unsigned grid = attn_numbers(batch, rows, 32) * r.heads;
+            ok = a->causal ? attn_launch(k_attn_dq_few<D, true>, grid, few_lds<D>(true), st, r) : attn_launch(k_attn_dq_few<D, false>, grid, few_lds<D>(true), st, r);
             if (!ok) return;
         } else if (a->causal) {
-            hipLaunchKernelGGL((k_attn_dq<D, true>), dim3(r.tiles * r.heads), dim3(256), 0, st, r);
+            hipLaunchKernelGGL((k_attn_dq<D, true>), dim3(tiles * r.heads), dim3(256), 0, st, r);
         } else {
-            hipLaunchKernelGGL((k_attn_dq<D, false>), dim3(r.tiles * r.heads), dim3(256), 0, st, r);
+            hipLaunchKernelGGL((k_attn_dq<D, false>), dim3(tiles * r.heads), dim3(256), 0, st, r);
         }
-        if (a->causal) hipLaunchKernelGGL((k_attn_dkv<D, true>), dim3(r.tiles * r.kv_heads * r.splits), dim3(256), 0, st, r);
-        else hipLaunchKernelGGL((k_attn_dkv<D, false>), dim3(r.tiles * r.kv_heads * r.splits), dim3(256), 0, st, r);
+        if (a->causal) hipLaunchKernelGGL((k_attn_dkv<D, true>), dim3(tiles * r.kv_heads * r.splits), dim3(256), 0, st, r);
+        else hipLaunchKernelGGL((k_attn_dkv<D, false>), dim3(tiles * r.kv_heads * r.splits), dim3(256), 0, st, r);
     });
     if (!ok) return PAC_ERR_DEVICE;
     if (r.splits > 1) hipLaunchKernelGGL(k_attn_join, dim3((unsigned)((rows * 2 * kc / 8 + 255) / 256)), dim3(256), 0, st, r);
